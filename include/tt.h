@@ -500,6 +500,100 @@ int tt_step(const tt_vocab *vd, const tt_vocab *vt, int32_t n_streams, int32_t v
             int32_t *n_accepted, int32_t *out_token, float *residual,
             void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Rows of logits.  The three calls below read rows of v logits in bf16, fp16 or fp32 (TT_BF16, TT_F16,
+ * TT_F32) at a stride of logits_ld elements, each aligned to its own size.  Row i has the inverse
+ * temperature beta = inv_temperature[i] (device, fp32; NULL: 1 for every row), and with its logits x,
+ *     M = max x,  S = sum exp(beta (x_j - M)),  L = ln S,  lse = beta M + L,
+ *     lp_j = beta (x_j - M) - L,  p_j = exp(lp_j).
+ * A NaN logit counts as minus infinity (as in tt_verify_logits), and minus infinity is a token of
+ * probability 0.  A row with a logit of plus infinity, or with beta <= 0, infinite or NaN, has no
+ * distribution: its results are NaN (token ids -1).  v in 1..2^23, n_rows >= 0.
+ * Sums are formed in fp32 within a part of a row (at most 16,384 logits) and in fp64 over the parts;
+ * the results do not depend on scheduling.
+ */
+enum { TT_BF16 = 0, TT_F16 = 1, TT_F32 = 2 };
+
+/*
+ * tt_logprobs -- log probabilities of given tokens, with log-sum-exp, entropy and top alternatives.
+ *
+ *   ids          optional (device, [n_rows]): the tokens whose log probabilities are wanted
+ *   n_top        alternatives per row, 0..128
+ * Outputs (device; each optional but top_ids and top_logprobs, which n_top > 0 requires):
+ *   logprob      [n_rows] lp of token ids[i] (requires ids); NaN for an id outside [0, v)
+ *   lse          [n_rows] the row's log-sum-exp of beta x, as tt_verify_logits takes it
+ *   stats        [n_rows][2] M and L, what tt_logprobs_backward takes
+ *   entropy      [n_rows] H = -sum p_j lp_j
+ *   top_ids      [n_rows][n_top] the tokens of the largest logits, descending, equal ones in the
+ *                order of their ids; -1 where the row has fewer logits above minus infinity
+ *   top_logprobs [n_rows][n_top] their lp; minus infinity where top_ids is -1
+ * A row without a logit above minus infinity has M = lse = -inf, L = 0, H = 0, logprob = -inf and
+ * no alternatives.
+ * Reads every logit once.  workspace: tt_logprobs_workspace_size bytes, 16-byte aligned, no
+ * initialisation; calls that overlap in time must not share it.  Two kernels on `stream` (for large
+ * batches with alternatives: two for each group of rows).  TT_EINVAL on a bad size or type, a missing
+ * pointer or one not aligned to its elements, TT_EUNSUPPORTED for v > 2^23 or n_top > 128,
+ * TT_EWORKSPACE when the workspace is missing or too small.
+ */
+int tt_logprobs_workspace_size(int32_t n_rows, int32_t v, int32_t dtype, int32_t n_top, size_t *bytes);
+int tt_logprobs(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,
+                const float *inv_temperature, const int32_t *ids, int32_t n_top,
+                float *logprob, float *lse, float *stats, float *entropy, int32_t *top_ids, float *top_logprobs,
+                void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * tt_logprobs_backward -- the gradient of tt_logprobs' logprob and entropy with respect to the logits:
+ *     dlogits_j = beta (g ([j = id] - p_j) - h p_j (lp_j + H)),
+ * g = grad_logprob[i] (0 for an id outside [0, v)), h = grad_entropy[i].
+ *
+ *   stats        [n_rows][2] from tt_logprobs on the same logits and temperatures
+ *   ids, grad_logprob     both or neither (device, [n_rows])
+ *   entropy, grad_entropy both or neither (device, [n_rows]); entropy from tt_logprobs
+ *   dlogits      rows of v elements of the logits' type at a stride of dlogits_ld, rounded once to
+ *                nearest even; elements past v in a row are left alone.  It may be the logits' own
+ *                memory (the same address and stride), but must not overlap them otherwise.
+ * A row with g = h = 0, or without a logit above minus infinity, gets zeros and is not read.
+ * Logits are read once; no workspace; one kernel on `stream` (several for more than 2^18 workgroups).
+ */
+int tt_logprobs_backward(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,
+                         const float *inv_temperature, const int32_t *ids, const float *stats, const float *entropy,
+                         const float *grad_logprob, const float *grad_entropy, void *dlogits, int64_t dlogits_ld,
+                         void *stream);
+
+/*
+ * tt_distill -- distillation from a teacher's top tokens: every row's loss and, if wanted, its
+ * gradient.  The row's list holds n_top of the teacher's tokens with their log probabilities a_k (at
+ * the temperature of the loss); through id_map it may come from another vocabulary (t2d of
+ * tt_vocab_intersection maps the target's tokens to the draft's).  An entry is left out when its
+ * (mapped) id lies outside [0, v) or its a_k is minus infinity or NaN.
+ *   tail != 0: w_k = exp(a_k); the mass r = max(0, 1 - sum w) that the list leaves is matched with the
+ *              student's mass on all unlisted tokens
+ *   tail == 0: w_k = exp(a_k) / sum over the entries kept (scaled logits serve as well), r = 0
+ * With P_j the sum of the w_k whose token is j, Q_j = p_j of the student's row, R = sum of Q_j over the
+ * unlisted tokens and T = sum P_j + r,
+ *     loss = sum P_j (ln P_j - ln Q_j) + r (ln r - ln R),
+ *     dlogits_j = g beta (T Q_j - P_j) for listed j, g beta Q_j (T - r / R) for the others,
+ * g = grad_loss[i].  r counts as 0 where no unlisted token has a logit above minus infinity.  A row
+ * with an empty list or without a logit above minus infinity has loss 0 and gradient 0; a listed
+ * token with P > 0 and a logit of minus infinity makes the loss infinite (its gradient is finite); a
+ * list value of plus infinity makes the row NaN; a row with g = 0 has gradient 0 in any case.
+ *
+ *   top_ids, top_logprobs  [n_rows][n_top] (device), n_top in 1..128
+ *   id_map       optional (device, [n_map])
+ *   loss         [n_rows]
+ *   grad_loss    [n_rows], required with dlogits
+ *   dlogits      optional (NULL: the loss alone); layout, rounding and aliasing as in tt_logprobs_backward
+ * workspace: tt_distill_workspace_size bytes (with_grad: whether dlogits will be given), 16-byte
+ * aligned, no initialisation; calls that overlap in time must not share it.  Two kernels on `stream`,
+ * three with the gradient, for each group of rows (with the gradient a group's logits stay in the
+ * cache between their two readings).
+ */
+int tt_distill_workspace_size(int32_t n_rows, int32_t v, int32_t dtype, int32_t n_top, int32_t with_grad, size_t *bytes);
+int tt_distill(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,
+               const float *inv_temperature, int32_t n_top, const int32_t *top_ids, const float *top_logprobs,
+               const int32_t *id_map, int32_t n_map, int32_t tail, float *loss, const float *grad_loss,
+               void *dlogits, int64_t dlogits_ld, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,9 +18,13 @@ raised.
               (App. D Alg. 3): the intersection maps, q' rows, and the verification with q'
               formed on the fly
     verify_logits  tt_verify_logits  verification from bf16 logits and a temperature (App. F)
+    logprobs / logprobs_backward  log probabilities of given tokens, log-sum-exp (as verify_logits
+              takes it), entropy and top alternatives of rows of logits, and their gradient
+    distill   tt_distill  loss and gradient of a draft model's rows against its target's top tokens
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import functools
 import os
@@ -28,6 +32,7 @@ import os
 __all__ = ["Vocab", "align", "align_workspace", "transfer", "verify", "verify_noalloc", "verify_dense", "verify_workspace", "lib",
            "delta_histogram", "delta_quantile", "w_at_quantile", "token_index", "retokenize", "LIB_PATH",
            "vocab_intersection", "tli_proposal", "verify_tli", "verify_logits", "verify_logits_workspace", "verify_tli_workspace",
+           "logprobs", "logprobs_workspace", "logprobs_backward", "LogProbs", "distill", "distill_workspace",
            "TTError", "path_capacity"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtt.so")
@@ -110,6 +115,16 @@ def lib():
         L.tt_step.argtypes = [VP, VP, i32, i32, i32, P, P, P, P, i32, i32, i32, P, i64, P, i64, P, P,
                               P, P, P, P, P, P, P, P, P, sz, P]
         L.tt_step.restype = ctypes.c_int
+        L.tt_logprobs_workspace_size.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
+        L.tt_logprobs_workspace_size.restype = ctypes.c_int
+        L.tt_logprobs.argtypes = [i32, i32, i32, P, i64, P, P, i32, P, P, P, P, P, P, P, sz, P]
+        L.tt_logprobs.restype = ctypes.c_int
+        L.tt_logprobs_backward.argtypes = [i32, i32, i32, P, i64, P, P, P, P, P, P, P, i64, P]
+        L.tt_logprobs_backward.restype = ctypes.c_int
+        L.tt_distill_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+        L.tt_distill_workspace_size.restype = ctypes.c_int
+        L.tt_distill.argtypes = [i32, i32, i32, P, i64, P, i32, P, P, P, i32, i32, P, P, P, i64, P, sz, P]
+        L.tt_distill.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -401,6 +416,189 @@ def verify_logits(v_t: int, target_ids, target_off, q, target_logits, inv_temper
                                 ws, ws_bytes, _stream_handle(stream))
     _check(st, "tt_verify_logits")
     return out
+
+
+LogProbs = collections.namedtuple("LogProbs", "logprob lse stats entropy top_ids top_logprobs")
+LogProbs.__doc__ = """What logprobs() returns, float32 (top_ids int32) device tensors, None where not asked for: logprob [n] of
+the given tokens, lse [n], stats [n, 2] for logprobs_backward(), entropy [n], top_ids and top_logprobs [n, n_top]."""
+
+
+def _row_type(t, name):
+    """TT_BF16, TT_F16 or TT_F32 of a 2-D row-major device tensor."""
+    if t.dim() != 2 or t.stride(1) != 1 or not t.is_cuda:
+        raise ValueError(f"{name} must be a 2-D row-major device tensor")
+    dtype = t.dtype
+    if dtype is torch.bfloat16:
+        return 0
+    if dtype is torch.float16:
+        return 1
+    if dtype is torch.float32:
+        return 2
+    raise ValueError(f"{name} must be bfloat16, float16 or float32, got {dtype}")
+
+
+def _rows_at(t, v: int, n: int, name):
+    """(address, stride) of rows of at least v columns, n of them at least."""
+    if t.shape[1] < v or t.shape[0] < n:
+        raise ValueError(f"{name} must have at least {n} rows of {v}")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), v))
+
+
+def _sized(t, dtype, name, n: int, allow_none=False):
+    """_ptr of a tensor of n elements (an empty one of a call on no rows: None)."""
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+    return _ptr(t, dtype, name, allow_none) or None
+
+
+def _same_device(first, stream, *others):
+    """The device the call runs on (the stream's, or the current one) has to hold every tensor."""
+    device = first.device
+    for t in others:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors on {device} and {t.device} in one call")
+    if stream is None:
+        if device.index != torch.cuda.current_device():
+            raise ValueError(f"tensors on {device}, but the current device is cuda:{torch.cuda.current_device()}")
+    elif getattr(stream, "device", device) != device:
+        raise ValueError(f"tensors on {device}, but the stream belongs to {stream.device}")
+
+
+def _given_workspace(workspace, nbytes: int):
+    """(address, bytes) of the caller's workspace, or of nbytes on the current stream (held by the third)."""
+    if workspace is None:
+        workspace = torch.empty(max(1, nbytes), dtype=torch.uint8, device="cuda")
+        return workspace.data_ptr(), nbytes, workspace
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous device tensor")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+_DTYPE_CODES = {"bfloat16": 0, "float16": 1, "float32": 2}
+
+
+def _dtype_code(dtype) -> int:
+    code = _DTYPE_CODES.get(str(dtype).replace("torch.", ""))
+    if code is None:
+        raise ValueError(f"dtype must be bfloat16, float16 or float32, got {dtype}")
+    return code
+
+
+def logprobs_workspace(n_rows: int, v: int, dtype, n_top: int = 0, device="cuda"):
+    """A workspace for logprobs on n_rows rows of v logits of this type, reusable by calls that do not overlap in time."""
+    n = ctypes.c_size_t(0)
+    _check(lib().tt_logprobs_workspace_size(int(n_rows), int(v), _dtype_code(dtype), int(n_top), ctypes.byref(n)),
+           "tt_logprobs_workspace_size")
+    return torch.empty(max(1, n.value), dtype=torch.uint8, device=device)
+
+
+def logprobs(v: int, logits, ids=None, inv_temperature=None, n_top: int = 0, entropy: bool = False, out=None,
+             workspace=None, stream=None):
+    """tt_logprobs: of every row of logits ([n, >= v] bfloat16, float16 or float32, row-major, any row stride) the
+    log probability of its token ids[i] (int32 [n], optional), its log-sum-exp, the statistics that
+    logprobs_backward() takes, optionally its entropy, and its n_top (0..128) most probable tokens.
+    inv_temperature: float32 [n], 1 / T (1 if not given).  out: a LogProbs of the caller's tensors (a None among
+    them is left out); workspace: from logprobs_workspace(); both are made here if not given.  Returns a LogProbs."""
+    if stream is not None and (out is None or workspace is None):
+        return _on_stream(stream, logprobs, v, logits, ids, inv_temperature, n_top, entropy, out, workspace, None)
+    i32, f32 = torch.int32, torch.float32
+    v, n_top, code = int(v), int(n_top), _row_type(logits, "logits")
+    n = logits.shape[0]
+    address, ld = _rows_at(logits, v, n, "logits")
+    dev = logits.device
+    if out is None:
+        new = lambda *s: torch.empty(s, dtype=f32, device=dev)  # noqa: E731
+        out = LogProbs(None if ids is None else new(n), new(n), new(n, 2), new(n) if entropy else None,
+                       torch.empty((n, n_top), dtype=i32, device=dev) if n_top else None, new(n, n_top) if n_top else None)
+    _same_device(logits, stream, ids, inv_temperature, workspace, *out)
+    ws, ws_bytes, _held = _given_workspace(workspace, _spread_bytes("tt_logprobs_workspace_size", n, v, code, n_top))
+    st = lib().tt_logprobs(n, v, code, address, ld, _sized(inv_temperature, f32, "inv_temperature", n, True),
+                           _sized(ids, i32, "ids", n, True), n_top, _sized(out[0], f32, "logprob", n, True),
+                           _sized(out[1], f32, "lse", n, True), _sized(out[2], f32, "stats", 2 * n, True),
+                           _sized(out[3], f32, "entropy", n, True), _sized(out[4], i32, "top_ids", n * n_top, not n_top),
+                           _sized(out[5], f32, "top_logprobs", n * n_top, not n_top), ws, ws_bytes, _stream_handle(stream))
+    _check(st, "tt_logprobs")
+    return out
+
+
+def logprobs_backward(v: int, logits, ids, stats, grad_logprob, entropy=None, grad_entropy=None, inv_temperature=None,
+                      out=None, stream=None):
+    """tt_logprobs_backward: the gradient with respect to the logits of sum(grad_logprob * logprob) + sum(grad_entropy *
+    entropy), from the stats (and the entropy) that logprobs() gave for the same logits and temperatures.  ids and
+    grad_logprob may both be None, and so may entropy and grad_entropy.  out: rows of the logits' type, which may be the
+    logits themselves (they are overwritten then).  A model's backward pass goes on with logits.backward(result)."""
+    if stream is not None and out is None:
+        return _on_stream(stream, logprobs_backward, v, logits, ids, stats, grad_logprob, entropy, grad_entropy,
+                          inv_temperature, None, None)
+    i32, f32 = torch.int32, torch.float32
+    v, code = int(v), _row_type(logits, "logits")
+    n = logits.shape[0]
+    address, ld = _rows_at(logits, v, n, "logits")
+    if out is None:
+        out = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
+    if _row_type(out, "out") != code:
+        raise ValueError(f"out must be {logits.dtype}, got {out.dtype}")
+    to, out_ld = _rows_at(out, v, n, "out")
+    _same_device(logits, stream, ids, stats, grad_logprob, entropy, grad_entropy, inv_temperature, out)
+    st = lib().tt_logprobs_backward(n, v, code, address, ld, _sized(inv_temperature, f32, "inv_temperature", n, True),
+                                    _sized(ids, i32, "ids", n, True), _sized(stats, f32, "stats", 2 * n),
+                                    _sized(entropy, f32, "entropy", n, True),
+                                    _sized(grad_logprob, f32, "grad_logprob", n, True),
+                                    _sized(grad_entropy, f32, "grad_entropy", n, True), to, out_ld, _stream_handle(stream))
+    _check(st, "tt_logprobs_backward")
+    return out
+
+
+def distill_workspace(n_rows: int, v: int, dtype, n_top: int, grad: bool = False, device="cuda"):
+    """A workspace for distill with these bounds, reusable by calls that do not overlap in time."""
+    n = ctypes.c_size_t(0)
+    _check(lib().tt_distill_workspace_size(int(n_rows), int(v), _dtype_code(dtype), int(n_top), 1 if grad else 0,
+                                           ctypes.byref(n)), "tt_distill_workspace_size")
+    return torch.empty(max(1, n.value), dtype=torch.uint8, device=device)
+
+
+def distill(v: int, logits, top_ids, top_logprobs, tail: bool = False, id_map=None, inv_temperature=None, grad_loss=None,
+            loss=None, dlogits=None, workspace=None, stream=None):
+    """tt_distill: the loss (float32 [n]) of every row of a student's logits against its teacher's top tokens top_ids
+    (int32 [n, n_top], n_top in 1..128) with log probabilities top_logprobs (float32 [n, n_top]), as logprobs(n_top=...)
+    gives them.  tail: the mass that a list leaves is matched with the student's mass outside it; otherwise the list
+    is renormalised.  id_map: int32, the student's token of each of the teacher's (vocab_intersection()'s t2d), -1 for
+    none.  With grad_loss (float32 [n], the weights of the rows' losses) the gradient with respect to the logits is
+    formed as well, in dlogits: rows of the logits' type, made here if not given, which may be the logits themselves.
+    Returns (loss, dlogits or None)."""
+    if stream is not None and (loss is None or workspace is None or (grad_loss is not None and dlogits is None)):
+        return _on_stream(stream, distill, v, logits, top_ids, top_logprobs, tail, id_map, inv_temperature, grad_loss,
+                          loss, dlogits, workspace, None)
+    i32, f32 = torch.int32, torch.float32
+    v, code = int(v), _row_type(logits, "logits")
+    n = logits.shape[0]
+    address, ld = _rows_at(logits, v, n, "logits")
+    if top_ids.dim() != 2 or top_ids.shape != top_logprobs.shape:
+        raise ValueError("top_ids and top_logprobs must be 2-D tensors of one shape")
+    n_top = top_ids.shape[1]
+    if id_map is not None and id_map.numel() == 0:
+        raise ValueError("id_map must not be empty")
+    if loss is None:
+        loss = torch.empty(n, dtype=f32, device=logits.device)
+    to, out_ld = None, 0
+    if grad_loss is not None:
+        if dlogits is None:
+            dlogits = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
+        if _row_type(dlogits, "dlogits") != code:
+            raise ValueError(f"dlogits must be {logits.dtype}, got {dlogits.dtype}")
+        to, out_ld = _rows_at(dlogits, v, n, "dlogits")
+    elif dlogits is not None:
+        raise ValueError("dlogits needs grad_loss")
+    _same_device(logits, stream, top_ids, top_logprobs, id_map, inv_temperature, grad_loss, loss, dlogits, workspace)
+    nbytes = _spread_bytes("tt_distill_workspace_size", n, v, code, n_top, 0 if grad_loss is None else 1)
+    ws, ws_bytes, _held = _given_workspace(workspace, nbytes)
+    st = lib().tt_distill(n, v, code, address, ld, _sized(inv_temperature, f32, "inv_temperature", n, True), n_top,
+                          _sized(top_ids, i32, "top_ids", n * n_top), _sized(top_logprobs, f32, "top_logprobs", n * n_top),
+                          _ptr(id_map, i32, "id_map", True), 0 if id_map is None else id_map.numel(), 1 if tail else 0,
+                          _sized(loss, f32, "loss", n), _sized(grad_loss, f32, "grad_loss", n, True), to, out_ld, ws,
+                          ws_bytes, _stream_handle(stream))
+    _check(st, "tt_distill")
+    return loss, dlogits
 
 
 def delta_histogram(draft_off, target_off, path_len, path, n_bins: int, out=None, stream=None):

@@ -17,11 +17,32 @@ constexpr int32_t kMaxIndexTokens = 1 << 28;  // vocabulary size a token index a
 constexpr int32_t kMaxTokenBytes = 64;        // longest target token the index and lookups handle
 constexpr int32_t kMaxLogitsRow = 1 << 23;     // logits per row tt_verify_logits accepts (64-bit exact sums)
 constexpr int32_t kMaxTliRow = 1 << 21;        // target row tt_verify_tli accepts (chunk sums in 16 KB of LDS)
+constexpr int32_t kMaxListed = 128;            // top tokens per row of tt_logprobs and tt_distill
 constexpr int32_t kMaxRetokBytes = 4096;      // bytes of S (and tokens of T) per stream: 14 B of LDS each
 
 bool vocab_ok(const tt_vocab *v) {
     return v != nullptr && v->bytes != nullptr && v->offsets != nullptr && v->n_tokens >= 1 &&
            v->max_token_bytes >= 1;
+}
+
+bool dtype_ok(int32_t dtype) { return dtype == TT_BF16 || dtype == TT_F16 || dtype == TT_F32; }
+
+bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// Whether a matrix of n_rows x v elements at p ends within the 2^57 bytes that an address reaches.
+bool extent_ok(const void *p, int32_t n_rows, int32_t v, int64_t ld, int dtype) {
+    const uint64_t end = uint64_t(1) << 57, at = reinterpret_cast<uintptr_t>(p);
+    const uint64_t most = at < end ? (end - at) / (dtype == TT_F32 ? 4 : 2) : 0;
+    return (unsigned __int128)(uint64_t)(n_rows - 1) * (uint64_t)ld + (uint64_t)v <= most;
+}
+
+// Two matrices that either are the same memory or do not meet.
+bool same_or_apart(const void *a, int64_t lda, const void *b, int64_t ldb, int32_t n_rows, int32_t v, int dtype) {
+    if (a == b && (lda == ldb || n_rows == 1)) return true;
+    const uintptr_t e = dtype == TT_F32 ? 4 : 2, p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    const uintptr_t p_end = p + ((uintptr_t)(n_rows - 1) * (uintptr_t)lda + v) * e;
+    const uintptr_t q_end = q + ((uintptr_t)(n_rows - 1) * (uintptr_t)ldb + v) * e;
+    return p_end <= q || q_end <= p;
 }
 
 }  // namespace
@@ -437,6 +458,115 @@ int tt_step(const tt_vocab *vd, const tt_vocab *vt, int32_t n_streams, int32_t v
     if (rc == TT_OK) rc = tt::launch_transfer(s.tr, st);
     if (rc == TT_OK) rc = tt::launch_verify(s.ve, st);
     return rc;
+}
+
+int tt_logprobs_workspace_size(int32_t n_rows, int32_t v, int32_t dtype, int32_t n_top, size_t *bytes) {
+    if (bytes == nullptr || n_rows < 0 || v < 1 || !dtype_ok(dtype) || n_top < 0) return TT_EINVAL;
+    if (v > kMaxLogitsRow || n_top > kMaxListed) return TT_EUNSUPPORTED;
+    *bytes = tt::logprobs_workspace_bytes(n_rows, v, dtype, n_top);
+    return TT_OK;
+}
+
+int tt_logprobs(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,
+                const float *inv_temperature, const int32_t *ids, int32_t n_top, float *logprob, float *lse,
+                float *stats, float *entropy, int32_t *top_ids, float *top_logprobs, void *workspace,
+                size_t workspace_bytes, void *stream) {
+    if (n_rows < 0 || v < 1 || !dtype_ok(dtype) || logits_ld < v || n_top < 0) return TT_EINVAL;
+    if (v > kMaxLogitsRow || n_top > kMaxListed) return TT_EUNSUPPORTED;
+    if (n_rows == 0) return TT_OK;
+    if (!logits || (logprob && !ids) || (n_top > 0 && (!top_ids || !top_logprobs))) return TT_EINVAL;
+    if (!aligned(logits, dtype == TT_F32 ? 4 : 2) || !extent_ok(logits, n_rows, v, logits_ld, dtype)) return TT_EINVAL;
+    tt::LogprobsArgs a;
+    a.n_rows = n_rows;
+    a.v = v;
+    a.dtype = dtype;
+    a.logits = logits;
+    a.ld = logits_ld;
+    a.inv_temp = inv_temperature;
+    a.ids = ids;
+    a.n_top = n_top;
+    a.logprob = logprob;
+    a.lse = lse;
+    a.stats = stats;
+    a.entropy = entropy;
+    a.top_ids = top_ids;
+    a.top_logprobs = top_logprobs;
+    return tt::launch_logprobs(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+int tt_logprobs_backward(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,
+                         const float *inv_temperature, const int32_t *ids, const float *stats, const float *entropy,
+                         const float *grad_logprob, const float *grad_entropy, void *dlogits, int64_t dlogits_ld,
+                         void *stream) {
+    if (n_rows < 0 || v < 1 || !dtype_ok(dtype) || logits_ld < v || dlogits_ld < v) return TT_EINVAL;
+    if (v > kMaxLogitsRow) return TT_EUNSUPPORTED;
+    if (n_rows == 0) return TT_OK;
+    if (!logits || !stats || !dlogits || (ids == nullptr) != (grad_logprob == nullptr) ||
+        (entropy == nullptr) != (grad_entropy == nullptr))
+        return TT_EINVAL;
+    const size_t e = dtype == TT_F32 ? 4 : 2;
+    if (!aligned(logits, e) || !aligned(dlogits, e) || !extent_ok(logits, n_rows, v, logits_ld, dtype) ||
+        !extent_ok(dlogits, n_rows, v, dlogits_ld, dtype) ||
+        !same_or_apart(logits, logits_ld, dlogits, dlogits_ld, n_rows, v, dtype))
+        return TT_EINVAL;
+    tt::LogprobsGradArgs a;
+    a.n_rows = n_rows;
+    a.v = v;
+    a.dtype = dtype;
+    a.logits = logits;
+    a.ld = logits_ld;
+    a.inv_temp = inv_temperature;
+    a.ids = ids;
+    a.stats = stats;
+    a.entropy = entropy;
+    a.grad_logprob = grad_logprob;
+    a.grad_entropy = grad_entropy;
+    a.dlogits = dlogits;
+    a.out_ld = dlogits_ld;
+    return tt::launch_logprobs_backward(a, static_cast<hipStream_t>(stream));
+}
+
+int tt_distill_workspace_size(int32_t n_rows, int32_t v, int32_t dtype, int32_t n_top, int32_t with_grad,
+                              size_t *bytes) {
+    if (bytes == nullptr || n_rows < 0 || v < 1 || !dtype_ok(dtype) || n_top < 1) return TT_EINVAL;
+    if (v > kMaxLogitsRow || n_top > kMaxListed) return TT_EUNSUPPORTED;
+    *bytes = tt::distill_workspace_bytes(n_rows, v, dtype, n_top, with_grad != 0);
+    return TT_OK;
+}
+
+int tt_distill(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,
+               const float *inv_temperature, int32_t n_top, const int32_t *top_ids, const float *top_logprobs,
+               const int32_t *id_map, int32_t n_map, int32_t tail, float *loss, const float *grad_loss, void *dlogits,
+               int64_t dlogits_ld, void *workspace, size_t workspace_bytes, void *stream) {
+    if (n_rows < 0 || v < 1 || !dtype_ok(dtype) || logits_ld < v || n_top < 1 || n_map < 0 ||
+        (dlogits != nullptr && dlogits_ld < v))
+        return TT_EINVAL;
+    if (v > kMaxLogitsRow || n_top > kMaxListed) return TT_EUNSUPPORTED;
+    if (n_rows == 0) return TT_OK;
+    if (!logits || !top_ids || !top_logprobs || !loss || (dlogits != nullptr && grad_loss == nullptr)) return TT_EINVAL;
+    const size_t e = dtype == TT_F32 ? 4 : 2;
+    if (!aligned(logits, e) || !extent_ok(logits, n_rows, v, logits_ld, dtype)) return TT_EINVAL;
+    if (dlogits != nullptr && (!aligned(dlogits, e) || !extent_ok(dlogits, n_rows, v, dlogits_ld, dtype) ||
+                               !same_or_apart(logits, logits_ld, dlogits, dlogits_ld, n_rows, v, dtype)))
+        return TT_EINVAL;
+    tt::DistillArgs a;
+    a.n_rows = n_rows;
+    a.v = v;
+    a.dtype = dtype;
+    a.logits = logits;
+    a.ld = logits_ld;
+    a.inv_temp = inv_temperature;
+    a.n_top = n_top;
+    a.top_ids = top_ids;
+    a.top_logprobs = top_logprobs;
+    a.id_map = id_map;
+    a.n_map = n_map;
+    a.tail = tail;
+    a.loss = loss;
+    a.grad_loss = grad_loss;
+    a.dlogits = dlogits;
+    a.out_ld = dlogits_ld;
+    return tt::launch_distill(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

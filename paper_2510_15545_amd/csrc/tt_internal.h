@@ -149,6 +149,51 @@ int launch_verify_tli(const TliVerifyArgs &a, void *workspace, size_t workspace_
 size_t retok_lds_bytes(int32_t max_bytes);
 int launch_retokenize(const RetokArgs &a, hipStream_t stream);
 
+// ---------------------------------------------------------------- log probabilities (logprobs.hip)
+struct LogprobsArgs {
+    int32_t n_rows, v, dtype;
+    const void *logits;
+    int64_t ld;
+    const float *inv_temp;  // or null
+    const int32_t *ids;     // or null
+    int32_t n_top;
+    float *logprob, *lse, *stats, *entropy;  // each may be null
+    int32_t *top_ids;
+    float *top_logprobs;
+};
+size_t logprobs_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top);
+int launch_logprobs(const LogprobsArgs &a, void *workspace, size_t workspace_bytes, hipStream_t stream);
+struct LogprobsGradArgs {
+    int32_t n_rows, v, dtype;
+    const void *logits;
+    int64_t ld;
+    const float *inv_temp;
+    const int32_t *ids;
+    const float *stats, *entropy, *grad_logprob, *grad_entropy;
+    void *dlogits;
+    int64_t out_ld;
+};
+int launch_logprobs_backward(const LogprobsGradArgs &a, hipStream_t stream);
+
+// ---------------------------------------------------------------- distillation (distill.hip)
+struct DistillArgs {
+    int32_t n_rows, v, dtype;
+    const void *logits;
+    int64_t ld;
+    const float *inv_temp;
+    int32_t n_top;
+    const int32_t *top_ids;
+    const float *top_logprobs;
+    const int32_t *id_map;  // or null
+    int32_t n_map, tail;
+    float *loss;
+    const float *grad_loss;
+    void *dlogits;  // null: the loss alone
+    int64_t out_ld;
+};
+size_t distill_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top, bool grad);
+int launch_distill(const DistillArgs &a, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
 // ---------------------------------------------------------------- fused step (step.hip)
 struct StepArgs {
     AlignArgs al;     // alignment inputs and outputs

@@ -1,0 +1,362 @@
+"""tt.logprobs and tt.logprobs_backward against the definitions in 64 bits: lengths from one token on, widths around
+the kernels' parts, the three types, rows of any alignment, ties, masks, rows without a token or a distribution,
+offsets past 32 bits, streams, graphs, in-place gradients."""
+import numpy as np
+import pytest
+
+import util_rows as ur
+
+pytestmark = pytest.mark.gpu
+
+U = ur.U
+# L = ln S: S is summed in fp32 over a chain of at most 64 elements and a tree of 8 joins, each element off by 3 steps
+# of its exponent (at most 40 where it counts) and 2 of the exponential's; then one rounding of the result
+SUM = U * (64 + 8 + 3 * 40 + 2)
+
+
+def check_logprobs(x, rows, ids, beta, n_top, entropy=True, **kw):
+    import torch
+
+    import paper_2510_15545_amd as tt
+
+    v = x.shape[1]
+    dev = lambda a, t: None if a is None else torch.from_numpy(np.ascontiguousarray(a, t)).cuda()  # noqa: E731
+    got = tt.logprobs(v, rows, dev(ids, np.int32), inv_temperature=dev(beta, np.float32), n_top=n_top, entropy=entropy, **kw)
+    torch.cuda.synchronize()
+    compare_logprobs(ur.logprobs(ur.host(rows), ids, beta, n_top), got)
+    return got
+
+
+def close(got, want, bound, what):
+    got = ur.host(got)
+    want = np.where(np.abs(want) >= 2.0 ** 128 - 2.0 ** 103, np.copysign(np.inf, want), want)  # what rounds past fp32's largest value
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    far = np.isinf(want)
+    assert np.array_equal(np.isinf(got), far) and np.array_equal(got[far], want[far]), what
+    fine = np.isfinite(want)
+    off = np.abs(got[fine] - want[fine])
+    assert np.all(off <= bound[fine]), (what, float((off / bound[fine]).max()))
+
+
+def compare_logprobs(want, got):
+    size = lambda a: np.where(np.isfinite(a), np.abs(a), 0.0)  # noqa: E731
+    if got.top_ids is not None:
+        assert np.array_equal(got.top_ids.cpu().numpy(), want["top_ids"])
+        close(got.top_logprobs, want["top_logprobs"], SUM + U * size(want["top_logprobs"]), "top_logprobs")
+    if got.logprob is not None:
+        close(got.logprob, want["logprob"], SUM + U * size(want["logprob"]), "logprob")
+    close(got.lse, want["lse"], SUM + U * size(want["lse"]), "lse")
+    assert np.array_equal(ur.host(got.stats)[:, 0], want["stats"][:, 0], equal_nan=True)
+    close(got.stats[:, 1], want["stats"][:, 1], SUM + U * size(want["stats"][:, 1]), "L")
+    if got.entropy is not None:
+        # H = L - E/S; E's terms p |t| sum to at most H + L and are off as S's are
+        close(got.entropy, want["entropy"], SUM * (2 + 2 * size(want["entropy"]) + 2 * size(want["stats"][:, 1])), "entropy")
+
+
+CASES = [(1, 1, "bf16", 1), (1, 2, "f32", 5), (3, 3, "f16", 3), (5, 7, "bf16", 128), (4, 9, "f32", 0), (2, 63, "f16", 20),
+         (3, 255, "bf16", 64), (1, 2047, "f32", 8), (2, 2049, "bf16", 20), (3, 4096, "bf16", 128), (2, 4101, "f16", 64),
+         (7, 16383, "bf16", 5), (1, 16384, "f32", 128), (5, 16385, "bf16", 1), (3, 50257, "f16", 20), (2, 50257, "f32", 5),
+         (1, 151936, "bf16", 20), (3, 151936, "f32", 64),
+         # enough rows for the wide parts
+         (1100, 640, "bf16", 5), (1030, 50, "f32", 128), (300, 50257, "bf16", 20), (300, 50257, "f16", 0), (170, 50257, "f32", 64),
+         (520, 32768, "bf16", 128), (70, 262144, "bf16", 8)]
+
+
+@pytest.mark.parametrize("n,v,dtype,n_top", CASES)
+def test_logprobs(n, v, dtype, n_top):
+    print(f"[case] logprobs {n}x{v} {dtype} top {n_top}", flush=True)
+    rng = np.random.default_rng([n, v, n_top])
+    x = ur.model_rows(rng, n, v)
+    ids = rng.integers(0, v, n)
+    beta = (0.5 + rng.random(n)).astype(np.float32)
+    check_logprobs(x, ur.placed(x, dtype, pad=int(rng.integers(0, 9)), shift=int(rng.integers(0, 9))), ids, beta, n_top)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("shift", range(9))
+def test_rows_of_any_alignment(dtype, shift):
+    rng = np.random.default_rng(shift)
+    x = ur.model_rows(rng, 9, 4109)
+    check_logprobs(x, ur.placed(x, dtype, pad=shift % 3, shift=shift), rng.integers(0, 4109, 9), None, 7)
+
+
+@pytest.mark.parametrize("n_top", [1, 20, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_equal_logits_go_to_the_lower_token(dtype, n_top):
+    """Whole rows of one value, two levels, plateaus above and below the k-th value, signed zeros, rows in order."""
+    rng = np.random.default_rng(4)
+    n, v = 10, 40000
+    x = np.zeros((n, v), np.float32)
+    x[1] = rng.integers(0, 2, v)
+    x[2] = np.minimum(rng.standard_normal(v) * 3, 4.0)  # many at the cap
+    x[3, rng.permutation(v)[:n_top // 2]] = 5.0
+    x[4] = -0.0
+    x[4, rng.permutation(v)[:v // 2]] = 0.0
+    x[5] = np.arange(v) // 64
+    x[6] = -(np.arange(v) // 64)
+    x[7] = np.where(np.arange(v) % 2048 < 8, 6.0, 0.0) + (np.arange(v) % 2048 == 5)  # all in the same lanes
+    x[8] = np.where(np.arange(v) > v - 300, 2.0, rng.standard_normal(v))
+    x[9] = np.round(rng.standard_normal(v))
+    x = np.round(x * 4) / 4
+    check_logprobs(x, ur.placed(x, dtype, pad=3), rng.integers(0, v, n), None, n_top)
+    # the wide parts
+    many = np.tile(x, (40, 1))
+    check_logprobs(many, ur.placed(many, dtype, pad=1), rng.integers(0, v, len(many)), None, n_top)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n_top", [0, 1, 20, 128])
+def test_masks(dtype, n_top):
+    """Rows that a mask holds to no, one, a few or many tokens, by minus infinity, NaN, -1e9 or the type's lowest value."""
+    rng = np.random.default_rng(7)
+    lowest = {"bf16": -3.3895313892515355e38, "f16": -65504.0, "f32": -3.4028234663852886e38}[dtype]
+    rows = []
+    for v_left in (0, 1, 2, 19, 20, 127, 129, 700, 6000):
+        for mask in (-np.inf, np.nan, max(-1e9, lowest), lowest):
+            x = np.full(20011, mask, np.float32)
+            at = rng.permutation(len(x))[:v_left] if v_left != 700 else 19000 + np.arange(700)
+            x[at] = rng.standard_normal(v_left) * 3
+            rows.append(x)
+    x = np.array(rows)
+    ids = rng.integers(0, x.shape[1], len(x))
+    beta = (0.5 + rng.random(len(x))).astype(np.float32)
+    if dtype == "f16":
+        x = np.maximum(x, np.float32(-65504.0), where=np.isfinite(x), out=x)
+    got = check_logprobs(x, ur.placed(x, dtype), ids, beta, n_top)
+    assert ur.host(got.lse)[0] == -np.inf and ur.host(got.entropy)[0] == 0.0
+    big = np.tile(x, (16, 1))  # the wide parts
+    check_logprobs(big, ur.placed(big, dtype), np.tile(ids, 16), np.tile(beta, 16), n_top)
+
+
+def test_rows_without_a_distribution():
+    rng = np.random.default_rng(9)
+    x = ur.model_rows(rng, 8, 3001)
+    x[1, 17] = np.inf
+    x[2] = -np.inf
+    x[2, 5] = np.inf
+    beta = np.array([1.0, 1.0, 1.0, 0.0, -1.0, np.nan, np.inf, 2.0], np.float32)
+    ids = np.array([-1, 17, 3, 4, 5, 6, 7, 3001])
+    check_logprobs(x, ur.placed(x, "f32"), ids, beta, 5)
+
+
+def test_every_kind_of_nan_is_passed_over():
+    """Quiet and signalling NaN of either sign, in every place of a vector and in both halves of a word."""
+    import torch
+
+    rng = np.random.default_rng(3)
+    for dtype, patterns in (("bf16", (0x7F81, 0xFF81, 0x7FBF, 0x7FC0, 0xFFC1)), ("f16", (0x7C01, 0xFC01, 0x7E00)),
+                            ("f32", (0x7F800001, -0x7FFFFF, 0x7FC00000))):
+        x = ur.model_rows(rng, 40, 4099)
+        rows = ur.placed(x, dtype, pad=1)
+        bits = rows.view(torch.int32 if dtype == "f32" else torch.int16)
+        for i in range(40):
+            at = torch.from_numpy(rng.permutation(4099)[:rng.integers(1, 4000)]).cuda()
+            pattern = int(patterns[i % len(patterns)])
+            bits[i, at] = pattern if dtype == "f32" or pattern < 0x8000 else pattern - 0x10000
+        assert rows.isnan().any(1).all()
+        check_logprobs(x, rows, rng.integers(0, 4099, 40), None, 20)
+
+
+@pytest.mark.parametrize("scale", [1e-3, 40.0, 3000.0, 1e8])
+def test_scales(scale):
+    rng = np.random.default_rng(1)
+    x = (rng.standard_normal((6, 9000)) * scale).astype(np.float32)
+    x[3] -= np.float32(scale * 100)
+    check_logprobs(x, ur.placed(x, "f32"), rng.integers(0, 9000, 6), (0.5 + rng.random(6)).astype(np.float32), 3)
+
+
+def test_many_rows_with_alternatives_take_several_groups():
+    """The keys of more rows than the workspace's bound holds."""
+    import paper_2510_15545_amd as tt
+
+    rng = np.random.default_rng(2)
+    n, v = 17000, 60
+    one = tt.logprobs_workspace(1, v, "bfloat16", 128).numel()
+    assert tt.logprobs_workspace(n, v, "bfloat16", 128).numel() < n * one // 2 + (1 << 26)
+    x = ur.model_rows(rng, n, v)
+    check_logprobs(x, ur.placed(x, "bf16"), rng.integers(0, v, n), None, 128)
+
+
+def test_offsets_past_32_bits():
+    import torch
+
+    rng = np.random.default_rng(8)
+    x = ur.model_rows(rng, 3, 5000)
+    ld = 1100 * 1000 * 1001  # 2 ld elements lie past 2^31
+    flat = torch.zeros(2 * ld + 5000, dtype=torch.bfloat16, device="cuda")
+    rows = flat.as_strided((3, 5000), (ld, 1))
+    rows.copy_(torch.from_numpy(x))
+    got = check_logprobs(x, rows, rng.integers(0, 5000, 3), None, 9)
+    import paper_2510_15545_amd as tt
+
+    g = torch.ones(3, device="cuda")
+    ids = torch.tensor([1, 2, 3], dtype=torch.int32, device="cuda")
+    want = tt.logprobs_backward(5000, rows.contiguous(), ids, got.stats, g)
+    far = tt.logprobs_backward(5000, rows, ids, got.stats, g, out=rows)
+    assert torch.equal(want, far)
+
+
+def test_outputs_that_are_not_asked_for():
+    import torch
+
+    import paper_2510_15545_amd as tt
+
+    rng = np.random.default_rng(8)
+    rows = ur.placed(ur.model_rows(rng, 4, 3000), "bf16")
+    want = tt.logprobs(3000, rows, torch.zeros(4, dtype=torch.int32, device="cuda"), n_top=4, entropy=True)
+    assert tt.logprobs(3000, rows).logprob is None and tt.logprobs(3000, rows).top_ids is None
+    for i, f in enumerate(want._fields[:4]):
+        out = [None] * 6
+        out[i] = torch.full_like(want[i], -7.0)
+        tt.logprobs(3000, rows, torch.zeros(4, dtype=torch.int32, device="cuda"), out=tt.LogProbs(*out))
+        assert torch.equal(out[i], want[i]), f
+    assert tt.logprobs(3000, rows[:0]).lse.numel() == 0
+    assert tt.logprobs_backward(3000, rows[:0], None, want.stats[:0], None).shape == (0, 3000)
+
+
+# ------------------------------------------------------------------------------- gradients
+def check_gradient(x, rows, ids, beta, g, h, dtype, out=None):
+    import torch
+
+    import paper_2510_15545_amd as tt
+
+    dev = lambda a, t=np.float32: None if a is None else torch.from_numpy(np.ascontiguousarray(a, t)).cuda()  # noqa: E731
+    n, v = x.shape
+    values = ur.host(rows)
+    f = tt.logprobs(v, rows, dev(ids, np.int32), inv_temperature=dev(beta), entropy=True)
+    got = tt.logprobs_backward(v, rows, dev(ids, np.int32) if g is not None else None, f.stats, dev(g),
+                               entropy=f.entropy if h is not None else None, grad_entropy=dev(h), inv_temperature=dev(beta), out=out)
+    torch.cuda.synchronize()
+    want, off = ur.logprobs_gradient(values, ids, beta, g, h)
+    a = ur.host(got)[:n, :v]
+    most = {"f16": 65504.0}.get(dtype, 3.3e38)
+    want = np.where(np.abs(want) > most, np.copysign(np.inf, want), want)
+    assert np.array_equal(np.isnan(a), np.isnan(want)) and np.array_equal(np.isinf(a), np.isinf(want))
+    fine = np.isfinite(want)
+    bound = ur.HALF_STEP[dtype] * (np.abs(want) + off) + off + ur.SMALLEST[dtype]
+    assert np.all(np.abs(a[fine] - want[fine]) <= bound[fine]), float((np.abs(a[fine] - want[fine]) / bound[fine]).max())
+    return got
+
+
+@pytest.mark.parametrize("with_g,with_h", [(True, False), (False, True), (True, True)])
+@pytest.mark.parametrize("n,v,dtype", [(1, 1, "f32"), (2, 2, "bf16"), (3, 7, "f16"), (5, 9, "f32"), (3, 4099, "bf16"), (4, 8192, "f16"),
+                                       (3, 8193, "bf16"), (2, 50257, "f32"), (2, 151936, "bf16"), (1500, 700, "f16")])
+def test_gradient(n, v, dtype, with_g, with_h):
+    print(f"[case] gradient {n}x{v} {dtype}", flush=True)
+    rng = np.random.default_rng([n, v])
+    x = ur.model_rows(rng, n, v)
+    ids = np.where(rng.random(n) < 0.5, x.argmax(1), rng.integers(0, v, n))
+    beta = (0.5 + rng.random(n)).astype(np.float32)
+    g = rng.standard_normal(n).astype(np.float32) if with_g else None
+    h = (rng.standard_normal(n) * 0.1).astype(np.float32) if with_h else None
+    check_gradient(x, ur.placed(x, dtype, pad=int(rng.integers(0, 9)), shift=int(rng.integers(0, 9))), ids, beta, g, h, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_gradient_of_masked_and_unsound_rows(dtype):
+    rng = np.random.default_rng(5)
+    lowest = {"bf16": -3.3895313892515355e38, "f16": -65504.0, "f32": -3.4028234663852886e38}[dtype]
+    x = ur.model_rows(rng, 14, 5003)
+    x[1] = -np.inf
+    x[2] = np.nan
+    x[3] = lowest
+    x[4, 1:] = lowest
+    x[5, ::2] = -np.inf
+    x[6, ::3] = np.nan
+    x[7, 9] = np.inf
+    x[12] = max(lowest, -1e9)
+    beta = np.ones(14, np.float32)
+    beta[8] = -1.0
+    ids = rng.integers(0, 5003, 14)
+    ids[4], ids[5], ids[10], ids[11] = 0, 2, -1, 5003
+    g = rng.standard_normal(14).astype(np.float32)
+    g[9] = 0.0
+    h = rng.standard_normal(14).astype(np.float32)
+    h[9] = 0.0
+    check_gradient(x, ur.placed(x, dtype, pad=1), ids, beta, g, None, dtype)
+    got = check_gradient(x, ur.placed(x, dtype, pad=1), ids, beta, g, h, dtype)
+    for i in (1, 2, 9):
+        assert not ur.host(got)[i].any()
+    weight = g * (np.arange(14) % 2)  # padded rows: weight 0 gives zeros whatever the row holds
+    weight[[7, 8]] = 0.0
+    assert np.isfinite(ur.host(check_gradient(x, ur.placed(x, dtype), ids, beta, weight, None, dtype))).all()
+
+
+def test_a_confident_token_keeps_its_small_gradient():
+    """1 - p of a token with p near 1 has its own leading digits, not those that 1 leaves."""
+    x = np.zeros((3, 1000), np.float32)
+    x[0, 7], x[1, 7], x[2, 7] = 20.0, 30.0, 60.0
+    check_gradient(x, ur.placed(x, "f32"), np.full(3, 7), None, np.ones(3, np.float32), None, "f32")
+
+
+def test_gradient_in_place_and_in_wider_rows():
+    import torch
+
+    rng = np.random.default_rng(6)
+    n, v = 5, 9001
+    x = ur.model_rows(rng, n, v)
+    ids, g = rng.integers(0, v, n), rng.standard_normal(n).astype(np.float32)
+    for dtype in ("bf16", "f32"):
+        for shift in (0, 3):
+            want = check_gradient(x, ur.placed(x, dtype, shift=shift), ids, None, g, None, dtype)
+            rows = ur.placed(x, dtype, pad=5, shift=shift)
+            wide = torch.full((n, v + 13), 7.0, dtype=rows.dtype, device="cuda")
+            check_gradient(x, rows, ids, None, g, None, dtype, out=wide)
+            assert torch.equal(wide[:, :v], want) and (wide[:, v:] == 7.0).all()  # what lies past v is left alone
+            check_gradient(x, rows, ids, None, g, None, dtype, out=rows)
+            assert torch.equal(rows, want)
+
+
+# ------------------------------------------------------------------------------- streams, graphs
+def test_streams_and_workspaces_of_the_caller():
+    import torch
+
+    import paper_2510_15545_amd as tt
+
+    rng = np.random.default_rng(11)
+    v, n = 50257, 6
+    rows = [ur.placed(ur.model_rows(rng, n, v), "bf16") for _ in range(2)]
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    want = [tt.logprobs(v, r, ids, n_top=20, entropy=True) for r in rows]
+    side = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [tt.logprobs_workspace(n, v, r.dtype, 20) for r in rows]
+    torch.cuda.synchronize()
+    for _ in range(4):  # two calls at once, each with its workspace and its stream
+        got = [tt.logprobs(v, r, ids, n_top=20, entropy=True, stream=s, workspace=w) for r, s, w in zip(rows, side, spaces)]
+        back = [tt.logprobs_backward(v, r, ids, w.stats, w.lse, stream=s) for r, s, w in zip(rows, side, got)]
+        torch.cuda.synchronize()
+        for a, b, r, d in zip(got, want, rows, back):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+            assert torch.equal(d, tt.logprobs_backward(v, r, ids, b.stats, b.lse))
+    with pytest.raises(tt.TTError):
+        tt.logprobs(v, rows[0], ids, n_top=20, workspace=spaces[0][:-256])
+    with pytest.raises(tt.TTError):
+        tt.logprobs(v, rows[0], ids, n_top=20, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+
+
+def test_replayed_in_a_graph_on_new_inputs():
+    import torch
+
+    import paper_2510_15545_amd as tt
+
+    rng = np.random.default_rng(12)
+    v, n = 20011, 7
+    rows = ur.placed(ur.model_rows(rng, n, v), "bf16")
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    g, h = torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+
+    def calls():
+        f = tt.logprobs(v, rows, ids, n_top=20, entropy=True)
+        return [*f, tt.logprobs_backward(v, rows, ids, f.stats, g, entropy=f.entropy, grad_entropy=h)]
+
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = calls()
+    for k in range(4):
+        rows.copy_(torch.from_numpy(ur.model_rows(rng, n, v)))
+        ids.copy_(torch.from_numpy(rng.integers(0, v, n)))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, calls())), k

@@ -1,0 +1,131 @@
+"""Refusals of the calls on rows of logits, before anything is launched: sizes, types, strides, alignment, pointers,
+workspaces, overlapping gradients, and the binding's checks of its tensors."""
+import ctypes
+import types
+
+import pytest
+import torch
+
+import paper_2510_15545_amd as tt
+
+L = tt.lib()
+PTR = 0x100000000  # never read: every call below is refused
+
+
+def logprobs(n=2, v=100, dtype=0, logits=PTR, ld=100, temp=None, ids=PTR, n_top=3, logprob=PTR, lse=PTR, stats=PTR, entropy=PTR,
+             top_ids=PTR, top_lp=PTR, ws=PTR, nbytes=1 << 30):
+    return L.tt_logprobs(n, v, dtype, logits, ld, temp, ids, n_top, logprob, lse, stats, entropy, top_ids, top_lp, ws, nbytes, None)
+
+
+def backward(n=2, v=100, dtype=0, logits=PTR, ld=100, temp=None, ids=PTR, stats=PTR, entropy=None, g=PTR, h=None, out=2 * PTR, out_ld=100):
+    return L.tt_logprobs_backward(n, v, dtype, logits, ld, temp, ids, stats, entropy, g, h, out, out_ld, None)
+
+
+def distill(n=2, v=100, dtype=0, logits=PTR, ld=100, temp=None, k=3, ids=PTR, lp=PTR, id_map=None, n_map=0, tail=0, loss=PTR, g=PTR,
+            out=2 * PTR, out_ld=100, ws=PTR, nbytes=1 << 30):
+    return L.tt_distill(n, v, dtype, logits, ld, temp, k, ids, lp, id_map, n_map, tail, loss, g, out, out_ld, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("call", [logprobs, backward, distill])
+def test_sizes_types_and_pointers(call):
+    for bad in (dict(n=-1), dict(v=0), dict(v=-5), dict(dtype=3), dict(dtype=-1), dict(ld=99), dict(logits=None),
+                dict(logits=PTR + 1), dict(dtype=2, logits=PTR + 2), dict(ld=1 << 62), dict(n=2 ** 31 - 1, ld=1 << 33)):
+        assert call(**bad) == tt.TT_EINVAL, bad
+    assert call(v=(1 << 23) + 1, ld=1 << 24) in (tt.TT_EUNSUPPORTED, tt.TT_EINVAL)
+    assert call(n=0, logits=None) == tt.TT_OK
+
+
+def test_logprobs_refusals():
+    for bad in (dict(n_top=-1), dict(ids=None), dict(top_ids=None), dict(top_lp=None), dict(ws=PTR + 8)):
+        assert logprobs(**bad) == tt.TT_EINVAL, bad
+    assert logprobs(n_top=129) == tt.TT_EUNSUPPORTED
+    assert logprobs(v=(1 << 23) + 1, ld=1 << 24) == tt.TT_EUNSUPPORTED
+    n = ctypes.c_size_t(0)
+    assert L.tt_logprobs_workspace_size(2, 100, 0, 3, ctypes.byref(n)) == tt.TT_OK and n.value > 0
+    assert logprobs(nbytes=n.value - 1) == tt.TT_EWORKSPACE
+    assert logprobs(ws=None) == tt.TT_EWORKSPACE
+    for bad in ((-1, 100, 0, 3), (2, 0, 0, 3), (2, 100, 5, 3), (2, 100, 0, -1)):
+        assert L.tt_logprobs_workspace_size(*bad, ctypes.byref(n)) == tt.TT_EINVAL
+    assert L.tt_logprobs_workspace_size(2, 100, 0, 129, ctypes.byref(n)) == tt.TT_EUNSUPPORTED
+    assert L.tt_logprobs_workspace_size(2, (1 << 23) + 1, 0, 1, ctypes.byref(n)) == tt.TT_EUNSUPPORTED
+    assert L.tt_logprobs_workspace_size(2, 100, 0, 3, None) == tt.TT_EINVAL
+    assert L.tt_logprobs_workspace_size(0, 100, 0, 3, ctypes.byref(n)) == tt.TT_OK
+    # the largest sizes: the rows' groups bound the workspace
+    assert L.tt_logprobs_workspace_size(2 ** 31 - 1, 1 << 23, 2, 128, ctypes.byref(n)) == tt.TT_OK and n.value < 1 << 28
+
+
+def test_backward_refusals():
+    for bad in (dict(stats=None), dict(out=None), dict(out_ld=99), dict(ids=None), dict(g=None), dict(entropy=PTR), dict(h=PTR),
+                dict(out=2 * PTR + 1), dict(out_ld=1 << 62)):
+        assert backward(**bad) == tt.TT_EINVAL, bad
+    # memory that overlaps the logits, but for the logits themselves
+    for bad in (dict(out=PTR + 2), dict(out=PTR, out_ld=101), dict(out=PTR + 398), dict(out=PTR - 398), dict(out=PTR - 2)):
+        assert backward(**bad) == tt.TT_EINVAL, bad
+
+
+def test_distill_refusals():
+    for bad in (dict(k=0), dict(k=-1), dict(ids=None), dict(lp=None), dict(loss=None), dict(g=None), dict(n_map=-1), dict(out_ld=99),
+                dict(out=2 * PTR + 1), dict(out=PTR + 2), dict(out=PTR, out_ld=101), dict(ws=PTR + 8)):
+        assert distill(**bad) == tt.TT_EINVAL, bad
+    assert distill(k=129) == tt.TT_EUNSUPPORTED
+    assert distill(v=(1 << 23) + 1, ld=1 << 24, out_ld=1 << 24) == tt.TT_EUNSUPPORTED
+    n = ctypes.c_size_t(0)
+    for grad, out in ((1, 2 * PTR), (0, None)):
+        assert L.tt_distill_workspace_size(2, 100, 0, 3, grad, ctypes.byref(n)) == tt.TT_OK and n.value > 0
+        assert distill(out=out, nbytes=n.value - 1) == tt.TT_EWORKSPACE
+    assert distill(ws=None) == tt.TT_EWORKSPACE
+    for bad in ((-1, 100, 0, 3, 0), (2, 0, 0, 3, 0), (2, 100, 5, 3, 0), (2, 100, 0, 0, 0)):
+        assert L.tt_distill_workspace_size(*bad, ctypes.byref(n)) == tt.TT_EINVAL
+    assert L.tt_distill_workspace_size(2, 100, 0, 3, 0, None) == tt.TT_EINVAL
+    assert L.tt_distill_workspace_size(2 ** 31 - 1, 1 << 23, 2, 128, 1, ctypes.byref(n)) == tt.TT_OK and n.value < 1 << 28
+
+
+def test_host_tensors_and_wrong_shapes_are_refused():
+    x, ids, f = torch.zeros(2, 8), torch.zeros(2, dtype=torch.int32), torch.zeros(2)
+    with pytest.raises(ValueError):
+        tt.logprobs(8, x, ids)
+    with pytest.raises(ValueError):
+        tt.logprobs_backward(8, x, ids, f, f)
+    with pytest.raises(ValueError):
+        tt.distill(8, x, ids.view(2, 1), f.view(2, 1))
+    with pytest.raises(ValueError):
+        tt.logprobs_workspace(2, 8, torch.float64)
+    with pytest.raises(ValueError):
+        tt.distill_workspace(2, 8, "int8", 4)
+
+
+def fake(shape=(2, 8), dtype=torch.bfloat16, device=0, strides=None, numel=None):
+    strides = strides or (shape[-1], 1)
+    n = 1
+    for s in shape:
+        n *= s
+    return types.SimpleNamespace(dim=lambda: len(shape), stride=lambda i: strides[i], is_cuda=True, dtype=dtype, shape=shape,
+                                 numel=lambda: n if numel is None else numel, is_contiguous=lambda: True, data_ptr=lambda: PTR,
+                                 element_size=lambda: 2, device=types.SimpleNamespace(type="cuda", index=device))
+
+
+def test_devices_and_shapes_of_device_tensors(monkeypatch):
+    """Tensors of another device than the current one or the stream's, of another size or type: refused by the binding."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    d0 = fake().device
+    a = fake()
+    a.device = d0
+    tt._same_device(a, None)
+    with pytest.raises(ValueError, match="current device"):
+        tt._same_device(fake(device=1), None)
+    b = fake(device=1)
+    with pytest.raises(ValueError, match="in one call"):
+        tt._same_device(a, None, b)
+    with pytest.raises(ValueError, match="stream belongs"):
+        tt._same_device(a, types.SimpleNamespace(cuda_stream=1, device=b.device))
+    tt._same_device(a, types.SimpleNamespace(cuda_stream=1))
+    with pytest.raises(ValueError, match="bfloat16, float16 or float32"):
+        tt._row_type(fake(dtype=torch.float64), "logits")
+    with pytest.raises(ValueError, match="row-major"):
+        tt._row_type(fake(strides=(1, 2)), "logits")
+    with pytest.raises(ValueError, match="at least"):
+        tt._rows_at(fake(), 9, 2, "logits")
+    with pytest.raises(ValueError, match="elements"):
+        tt._sized(fake(shape=(3,), dtype=torch.int32), torch.int32, "ids", 2)
+    with pytest.raises(ValueError, match="required"):
+        tt._sized(None, torch.float32, "stats", 2)
