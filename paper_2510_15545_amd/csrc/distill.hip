@@ -25,6 +25,7 @@ namespace {
 using namespace rows;
 
 constexpr int kMaxTop = 128;
+constexpr int kWaves = kThreads / kWave;
 constexpr int kListThreads = 128;  // one thread an entry
 constexpr int64_t kMaxGrid = int64_t(1) << 18;
 constexpr size_t kCachedBytes = size_t(96) << 20;  // logits of one group of rows, with the gradient
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(kThreads) void list_parts(ListArgs a) {
     const int part = blockIdx.x % (uint32_t)a.parts, x_part = part * kPart;
     const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
     uint32_t w[NV][4];
-    load_part<DT, NV>(row, a.v, x_part, w);
+    load_part<DT, NV, kThreads>(row, a.v, x_part, w);
     for (int i = threadIdx.x; i < kPart / 32; i += kThreads) sh_bits[i] = 0;
     const float c2 = scale_of(a.inv_temp, row_i) * kLog2e;
     __syncthreads();
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void list_parts(ListArgs a) {
     float tm = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int at = vector_at<DT>(0, i);
+        const int at = vector_at<DT, kThreads>(0, i);
         const uint32_t hit = (sh_bits[at / 32] >> (at % 32)) & ((1u << kPer) - 1u);
         if (hit != 0) {
 #pragma unroll
@@ -239,10 +240,10 @@ __global__ __launch_bounds__(kThreads) void list_grad(ListArgs a, int parts) {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) d[j] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kGradVectors; ++i) store_vector<DT>(out, vector_at<DT>(x_part, i), a.v, d);
+        for (int i = 0; i < kGradVectors; ++i) store_vector<DT>(out, vector_at<DT, kThreads>(x_part, i), a.v, d);
     } else {
         uint32_t w[kGradVectors][4];
-        load_part<DT, kGradVectors>(row, a.v, x_part, w);
+        load_part<DT, kGradVectors, kThreads>(row, a.v, x_part, w);
 #pragma unroll
         for (int i = 0; i < kGradVectors; ++i) {
 #pragma unroll
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(kThreads) void list_grad(ListArgs a, int parts) {
                 const float t = fmaxf((value<DT>(w[i], j) - q.m) * q.c2 - q.shift, kLowest);
                 d[j] = q.factor * __builtin_amdgcn_exp2f(t);
             }
-            store_vector<DT>(out, vector_at<DT>(x_part, i), a.v, d);
+            store_vector<DT>(out, vector_at<DT, kThreads>(x_part, i), a.v, d);
         }
     }
     // the listed tokens over what was just written: after the workgroup's stores have been made
@@ -268,6 +269,7 @@ struct Plan {
 Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
     Plan p;
     p.split = split_rows(n_rows, v, dtype);
+    if (p.split.threads != kThreads) p.split = {kThreads, kWideVectors, (int)((v + 8 * 256 * elements_per_vector(dtype) - 1) / (8 * 256 * elements_per_vector(dtype)))};
     int64_t most = kMaxGrid / p.split.parts;
     if (grad) {
         const int64_t per = (int64_t)kGradVectors * kThreads * elements_per_vector(dtype);

@@ -12,8 +12,8 @@ namespace tt {
 namespace rows {
 
 constexpr int kWave = 64;
-constexpr int kThreads = 256;  // threads of a workgroup that takes a part of a row
-constexpr int kWaves = kThreads / kWave;
+constexpr int kThreads = 256;        // threads of a workgroup that takes a part of a row, or a short row
+constexpr int kWholeThreads = 1024;  // and of one that takes a longer row whole
 constexpr float kLog2e = 0x1.715476p+0f;      // log2(e) rounded to fp32
 constexpr double kLn2 = 0.693147180559945309;  // ln 2
 
@@ -64,6 +64,11 @@ __device__ __forceinline__ void set_bits(uint32_t (&w)[4], int j, uint32_t bits)
     else w[j >> 1] = (w[j >> 1] & 0xFFFF0000u) | bits;
 }
 
+// The address of an element of any type.
+__device__ __forceinline__ const void *row_at(const void *p, int dtype, int64_t at) {
+    return dtype == TT_F32 ? (const void *)(static_cast<const float *>(p) + at) : (const void *)(static_cast<const uint16_t *>(p) + at);
+}
+
 // One element of a row of any type, as fp32; NaN counts as minus infinity.
 __device__ inline float load_logit(const void *row, int dtype, int64_t x) {
     float f;
@@ -74,21 +79,21 @@ __device__ inline float load_logit(const void *row, int dtype, int64_t x) {
 }
 
 // Index of the first element of thread t's vector i in a part that starts at x_part.
-template <int DT>
+template <int DT, int THREADS>
 __device__ __forceinline__ int vector_at(int x_part, int i) {
-    return x_part + (i * kThreads + (int)threadIdx.x) * Elem<DT>::kPer;
+    return x_part + (i * THREADS + (int)threadIdx.x) * Elem<DT>::kPer;
 }
 
 // A part of a row: NV vectors of 16 bytes a thread, each load instruction of a wave covering 1 KB
 // of the row; minus infinity past v.  Nothing outside [0, v) is read: a vector that ends past v is
 // replaced by the row's last whole one (a valid address) and then formed element by element.
-template <int DT, int NV>
+template <int DT, int NV, int THREADS>
 __device__ __forceinline__ void load_part(const typename Elem<DT>::T *row, int v, int x_part, uint32_t (&w)[NV][4]) {
     constexpr int kPer = Elem<DT>::kPer;
-    if (x_part + NV * kThreads * kPer <= v) {
+    if (x_part + NV * THREADS * kPer <= v) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const u4u t = *reinterpret_cast<const u4u *>(row + vector_at<DT>(x_part, i));
+            const u4u t = *reinterpret_cast<const u4u *>(row + vector_at<DT, THREADS>(x_part, i));
             w[i][0] = t.x; w[i][1] = t.y; w[i][2] = t.z; w[i][3] = t.w;
         }
         return;
@@ -96,14 +101,14 @@ __device__ __forceinline__ void load_part(const typename Elem<DT>::T *row, int v
     if (v >= kPer) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int x = vector_at<DT>(x_part, i), last = v - kPer;
+            const int x = vector_at<DT, THREADS>(x_part, i), last = v - kPer;
             const u4u t = *reinterpret_cast<const u4u *>(row + (x < last ? x : last));
             w[i][0] = t.x; w[i][1] = t.y; w[i][2] = t.z; w[i][3] = t.w;
         }
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int x = vector_at<DT>(x_part, i);
+        const int x = vector_at<DT, THREADS>(x_part, i);
         if (x + kPer > v) {
 #pragma unroll
             for (int j = 0; j < kPer; ++j) set_bits<DT>(w[i], j, x + j < v ? (uint32_t)row[x + j] : Elem<DT>::kNone);
@@ -228,7 +233,9 @@ __device__ __forceinline__ Sum join(const Sum &a, const Sum &b, float c2) {
     return r;
 }
 
-// The kernels' choice of vectors per thread: wide parts where there are parts enough for the GPU.
+// The kernels' choice of threads and vectors a thread.  A row is taken whole by one workgroup up to
+// kThreads * kWideVectors vectors; longer ones by parts of that size, or smaller ones where they
+// would not fill the GPU.
 constexpr int kWideVectors = 8;
 constexpr int kNarrowVectors = 2;
 constexpr int kFullGrid = 1024;  // workgroups that fill the GPU: four a compute unit
@@ -237,16 +244,20 @@ inline int elements_per_vector(int dtype) { return dtype == TT_F32 ? 4 : 8; }
 inline int element_bytes(int dtype) { return dtype == TT_F32 ? 4 : 2; }
 
 struct Split {
-    int vectors;  // per thread
-    int parts;    // per row
+    int threads, vectors;  // of a workgroup, of a thread
+    int parts;             // of a row
 };
 
 inline Split split_rows(int64_t n_rows, int32_t v, int dtype) {
-    const int64_t wide = (int64_t)kWideVectors * kThreads * elements_per_vector(dtype);
     const int64_t narrow = (int64_t)kNarrowVectors * kThreads * elements_per_vector(dtype);
+    const int64_t wide = (int64_t)kWideVectors * kThreads * elements_per_vector(dtype);
+    const int64_t whole = (int64_t)kWideVectors * kWholeThreads * elements_per_vector(dtype);
+    if (v <= narrow) return {kThreads, kNarrowVectors, 1};
+    if (v <= wide) return {kThreads, kWideVectors, 1};
+    if (v <= whole) return {kWholeThreads, kWideVectors, 1};
     const int64_t parts = (v + wide - 1) / wide;
-    if (n_rows * parts >= kFullGrid) return {kWideVectors, (int)parts};
-    return {kNarrowVectors, (int)((v + narrow - 1) / narrow)};
+    if (n_rows * parts >= kFullGrid) return {kThreads, kWideVectors, (int)parts};
+    return {kThreads, kNarrowVectors, (int)((v + narrow - 1) / narrow)};
 }
 
 inline size_t round256(size_t n) { return (n + 255) & ~size_t(255); }

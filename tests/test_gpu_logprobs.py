@@ -58,7 +58,7 @@ CASES = [(1, 1, "bf16", 1), (1, 2, "f32", 5), (3, 3, "f16", 3), (5, 7, "bf16", 1
          (7, 16383, "bf16", 5), (1, 16384, "f32", 128), (5, 16385, "bf16", 1), (3, 50257, "f16", 20), (2, 50257, "f32", 5),
          (1, 151936, "bf16", 20), (3, 151936, "f32", 64),
          # enough rows for the wide parts
-         (1100, 640, "bf16", 5), (1030, 50, "f32", 128), (300, 50257, "bf16", 20), (300, 50257, "f16", 0), (170, 50257, "f32", 64),
+         (1100, 640, "bf16", 5), (5, 65535, "bf16", 20), (3, 65536, "f16", 128), (2, 65537, "bf16", 8), (6, 32768, "f32", 1), (3, 32771, "f32", 20), (1030, 50, "f32", 128), (300, 50257, "bf16", 20), (300, 50257, "f16", 0), (170, 50257, "f32", 64),
          (520, 32768, "bf16", 128), (70, 262144, "bf16", 8)]
 
 
@@ -167,14 +167,18 @@ def test_scales(scale):
 
 def test_many_rows_with_alternatives_take_several_groups():
     """The keys of more rows than the workspace's bound holds."""
+    import torch
+
     import paper_2510_15545_amd as tt
 
-    rng = np.random.default_rng(2)
-    n, v = 17000, 60
+    n, v = 3300, 65540
     one = tt.logprobs_workspace(1, v, "bfloat16", 128).numel()
-    assert tt.logprobs_workspace(n, v, "bfloat16", 128).numel() < n * one // 2 + (1 << 26)
-    x = ur.model_rows(rng, n, v)
-    check_logprobs(x, ur.placed(x, "bf16"), rng.integers(0, v, n), None, 128)
+    assert tt.logprobs_workspace(n, v, "bfloat16", 128).numel() < n * one // 2
+    rows = torch.randn((n, v), device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).mul_(3).bfloat16()
+    ids = torch.randint(0, v, (n,), device="cuda", dtype=torch.int32)
+    got = tt.logprobs(v, rows, ids, n_top=128, entropy=True)
+    some = [0, 1, 1649, 1650, 1651, 2000, 3298, 3299]
+    compare_logprobs(ur.logprobs(ur.host(rows[some]), ids[some].cpu().numpy(), None, 128), tt.LogProbs(*(t[some] for t in got)))
 
 
 def test_offsets_past_32_bits():
@@ -314,7 +318,7 @@ def test_streams_and_workspaces_of_the_caller():
     import paper_2510_15545_amd as tt
 
     rng = np.random.default_rng(11)
-    v, n = 50257, 6
+    v, n = 70001, 6  # more than a workgroup takes whole
     rows = [ur.placed(ur.model_rows(rng, n, v), "bf16") for _ in range(2)]
     ids = torch.zeros(n, dtype=torch.int32, device="cuda")
     want = [tt.logprobs(v, r, ids, n_top=20, entropy=True) for r in rows]

@@ -36,14 +36,16 @@ def test_sizes_types_and_pointers(call):
 
 
 def test_logprobs_refusals():
-    for bad in (dict(n_top=-1), dict(ids=None), dict(top_ids=None), dict(top_lp=None), dict(ws=PTR + 8)):
+    for bad in (dict(n_top=-1), dict(ids=None), dict(top_ids=None), dict(top_lp=None)):
         assert logprobs(**bad) == tt.TT_EINVAL, bad
     assert logprobs(n_top=129) == tt.TT_EUNSUPPORTED
     assert logprobs(v=(1 << 23) + 1, ld=1 << 24) == tt.TT_EUNSUPPORTED
     n = ctypes.c_size_t(0)
-    assert L.tt_logprobs_workspace_size(2, 100, 0, 3, ctypes.byref(n)) == tt.TT_OK and n.value > 0
-    assert logprobs(nbytes=n.value - 1) == tt.TT_EWORKSPACE
-    assert logprobs(ws=None) == tt.TT_EWORKSPACE
+    assert L.tt_logprobs_workspace_size(2, 100, 0, 3, ctypes.byref(n)) == tt.TT_OK and n.value == 0  # a row whole in a workgroup
+    assert L.tt_logprobs_workspace_size(2, 100000, 0, 3, ctypes.byref(n)) == tt.TT_OK and n.value > 0
+    assert logprobs(v=100000, ld=100000, nbytes=n.value - 1) == tt.TT_EWORKSPACE
+    assert logprobs(v=100000, ld=100000, ws=None) == tt.TT_EWORKSPACE
+    assert logprobs(v=100000, ld=100000, ws=PTR + 8) == tt.TT_EINVAL
     for bad in ((-1, 100, 0, 3), (2, 0, 0, 3), (2, 100, 5, 3), (2, 100, 0, -1)):
         assert L.tt_logprobs_workspace_size(*bad, ctypes.byref(n)) == tt.TT_EINVAL
     assert L.tt_logprobs_workspace_size(2, 100, 0, 129, ctypes.byref(n)) == tt.TT_EUNSUPPORTED
