@@ -11,12 +11,14 @@
 // The unlisted tokens' sums are formed without the listed ones (a difference of the two totals would
 // lose R where the student, too, puts nearly all its mass on the list), and so is their softmax u.
 //
-// list_parts: a workgroup holds a part of a row in registers, takes the listed tokens out by a bitmap
-// in LDS and forms the rest's largest value and sum.  list_rows: a workgroup per row joins them,
-// gathers the listed logits, merges equal tokens and forms the loss in fp64, and what the gradient
-// needs: the unlisted softmax's reference and factor, the listed tokens' gradients.  list_grad: reads
-// the row again and writes its gradient.  The three run for groups of rows small enough that the
-// second reading comes out of the Infinity Cache.
+// list_whole: a workgroup per row.  It takes the listed tokens out by a bitmap in LDS and streams the row
+// by chunks for the rest's largest value and sum; one wave merges equal tokens, gathers the listed
+// logits (while the first loads are in flight) and forms the loss in fp64, and what the gradient needs:
+// the unlisted softmax's reference and factor, the listed tokens' gradients; then the row is streamed
+// again for its gradient.  Few enough rows are worked on at once that the second reading comes out of
+// the Infinity Cache.
+// Where the rows are too few to fill the GPU they are split: list_parts forms the sums of parts,
+// list_rows joins them and does the one wave's work, list_grad writes the gradient of parts.
 #include "rows.h"
 
 namespace tt {
@@ -25,25 +27,26 @@ namespace {
 using namespace rows;
 
 constexpr int kMaxTop = 128;
-constexpr int kWaves = kThreads / kWave;
-constexpr int kListThreads = 128;  // one thread an entry
+constexpr int kSlots = kMaxTop / kWave;  // list entries of a lane
 constexpr int64_t kMaxGrid = int64_t(1) << 18;
-constexpr size_t kCachedBytes = size_t(96) << 20;  // logits of one group of rows, with the gradient
-
-struct Entry {
-    int32_t id;  // -1: none (left out, or an earlier entry has the token)
-    float grad;
-};
+constexpr int kChunkVectors = 4;
+constexpr int kMaxBits = 1 << 18;  // tokens of a bitmap: 32 KB
 
 // What the gradient of a row's unlisted tokens needs: factor * 2^((x - m) c2 - shift).
 struct RowGrad {
     float m, c2, shift, factor;
 };
 
+// A listed token and its gradient; id -1: none (left out, or an earlier entry has the token).
+struct Entry {
+    int32_t id;
+    float grad;
+};
+
 struct ListArgs {
     const void *logits;
     int64_t ld, row0;
-    int v, dtype, parts, n_top, tail;
+    int v, dtype, parts, part_width, n_top, tail;
     const float *inv_temp;
     const int32_t *ids;
     const float *logprobs;
@@ -59,53 +62,290 @@ struct ListArgs {
 };
 
 // Student token of list entry k, -1 if it is left out.
-__device__ __forceinline__ int32_t entry_id(const ListArgs &a, int64_t row, int k) {
-    const float lp = a.logprobs[row * a.n_top + k];
+__device__ __forceinline__ int32_t entry_id(const ListArgs &a, int64_t row, int k, float lp) {
     int32_t id = a.ids[row * a.n_top + k];
-    if (!(lp > -INFINITY)) return -1;  // probability 0, NaN
-    if (a.id_map != nullptr) {
-        if (id < 0 || id >= a.n_map) return -1;
-        id = a.id_map[id];
-    }
-    return id >= 0 && id < a.v ? id : -1;
+    if (a.id_map != nullptr) id = id >= 0 && id < a.n_map ? a.id_map[id] : -1;
+    return id >= 0 && id < a.v && lp > -INFINITY ? id : -1;  // no entry of probability 0 or NaN
 }
 
-template <int DT, int NV>
-__global__ __launch_bounds__(kThreads) void list_parts(ListArgs a) {
-    using T = typename Elem<DT>::T;
-    constexpr int kPer = Elem<DT>::kPer;
-    constexpr int kPart = NV * kThreads * kPer;
-    __shared__ uint32_t sh_bits[kPart / 32];
-    __shared__ Sum sh_sum[kWaves];
-    pass_over_nans();
-    const int64_t r = blockIdx.x / (uint32_t)a.parts, row_i = a.row0 + r;
-    const int part = blockIdx.x % (uint32_t)a.parts, x_part = part * kPart;
-    const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
-    uint32_t w[NV][4];
-    load_part<DT, NV, kThreads>(row, a.v, x_part, w);
-    for (int i = threadIdx.x; i < kPart / 32; i += kThreads) sh_bits[i] = 0;
-    const float c2 = scale_of(a.inv_temp, row_i) * kLog2e;
-    __syncthreads();
-    if ((int)threadIdx.x < a.n_top) {
-        const int at = entry_id(a, row_i, threadIdx.x) - x_part;
-        if (at >= 0 && at < kPart) atomicOr(&sh_bits[at / 32], 1u << (at % 32));
+// A row's list as one wave holds it, kSlots entries a lane: entry u * 64 + lane.
+struct List {
+    int32_t id[kSlots];    // -1: left out, or an earlier entry has the token
+    float x[kSlots];       // the token's logit
+    double mass[kSlots];   // the teacher's probability of the token
+    double log_mass[kSlots];
+    double listed;         // sum of the masses
+    float most;            // largest of the list's log probabilities
+    bool any;
+};
+
+// Entry e of a value held as a list, for every lane (e is the same in all of them).
+__device__ __forceinline__ int32_t entry_of(const int32_t (&x)[kSlots], int e) {
+    return __builtin_amdgcn_readlane(e < kWave ? x[0] : x[1], e % kWave);
+}
+__device__ __forceinline__ double entry_of(const double (&x)[kSlots], int e) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, e < kWave ? x[0] : x[1]);
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)b, e % kWave), hi = __builtin_amdgcn_readlane((uint32_t)(b >> 32), e % kWave);
+    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+static_assert(kSlots == 2, "entry_of chooses between two slots");
+
+__device__ __forceinline__ List read_list(const ListArgs &a, int64_t row) {
+    const int lane = threadIdx.x % kWave;
+    List q;
+    float lp[kSlots];
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u) {
+        const int k = u * kWave + lane;
+        q.id[u] = -1;
+        lp[u] = -INFINITY;
+        if (k < a.n_top) {
+            lp[u] = a.logprobs[row * a.n_top + k];
+            q.id[u] = entry_id(a, row, k, lp[u]);
+        }
+        if (q.id[u] < 0) lp[u] = -INFINITY;
     }
-    __syncthreads();
-    float tm = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u)
+        q.x[u] = q.id[u] >= 0 ? load_logit(row_at(a.logits, a.dtype, row * a.ld), a.dtype, q.id[u]) : -INFINITY;
+    q.most = wave_max(fmaxf(lp[0], lp[1]));
+    q.any = q.most > -INFINITY;
+    double all = 0.0;
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u) {
+        q.log_mass[u] = a.tail ? (double)lp[u] : (double)lp[u] - (double)q.most;
+        q.mass[u] = q.id[u] >= 0 ? exp(q.log_mass[u]) : 0.0;
+        all += q.mass[u];
+    }
+    if (!a.tail) {
+        all = wave_sum(all);
+        const double log_all = log(all);
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) {
+            q.mass[u] = q.id[u] >= 0 ? q.mass[u] / all : 0.0;
+            q.log_mass[u] -= log_all;
+        }
+    }
+    // equal tokens: the first entry stands for them
+    int same[kSlots] = {};
+    for (int e = 0; e < a.n_top; ++e) {
+        const int32_t id = entry_of(q.id, e);
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) same[u] += q.id[u] == id ? 1 : 0;
+    }
+    if (__ballot((q.id[0] >= 0 && same[0] > 1) || (q.id[1] >= 0 && same[1] > 1)) != 0) {
+        double mass[kSlots] = {};
+        bool first[kSlots] = {true, true};
+        for (int e = 0; e < a.n_top; ++e) {
+            const int32_t id = entry_of(q.id, e);
+            const double w = entry_of(q.mass, e);
+#pragma unroll
+            for (int u = 0; u < kSlots; ++u) {
+                if (q.id[u] == id) {
+                    mass[u] += w;
+                    first[u] = first[u] && e >= u * kWave + lane;
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) {
+            if (q.id[u] < 0) continue;
+            if (!first[u]) {
+                q.id[u] = -1;
+                q.x[u] = -INFINITY;
+                q.mass[u] = 0.0;
+            } else if (same[u] > 1) {
+                q.mass[u] = mass[u];
+                q.log_mass[u] = log(mass[u]);
+            }
+        }
+    }
+    q.listed = wave_sum(q.mass[0] + q.mass[1]);
+    return q;
+}
+
+// A row's loss (written by lane 0) and, with GRAD, what its gradient needs, from its list and its unlisted
+// tokens' largest logit m_out and sum s_out relative to it.  One wave.
+template <bool GRAD>
+__device__ __forceinline__ RowGrad finish_row(const ListArgs &a, int64_t row, const List &q, float m_out, double s_out,
+                                              double (&grad)[kSlots]) {
+    const double beta = scale_of(a.inv_temp, row);
+    const float m = fmaxf(m_out, wave_max(fmaxf(q.x[0], q.x[1])));
+    double t[kSlots], e[kSlots];  // -inf (or NaN, in a row without a finite logit) and 0 where x is -inf
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u) {
+        t[u] = ((double)q.x[u] - (double)m) * beta;
+        e[u] = q.x[u] > -INFINITY ? exp(t[u]) : 0.0;
+    }
+    const double t_out = ((double)m_out - (double)m) * beta;  // ln of the unlisted sum's scale
+    const double s = wave_sum(e[0] + e[1]) + (s_out > 0.0 ? s_out * exp(t_out) : 0.0), log_s = log(s);
+    const double rest = a.tail && s_out > 0.0 ? fmax(0.0, 1.0 - q.listed) : 0.0;
+    // nothing listed, or no finite logit: 0; a logit or list value of +inf, or an unsound temperature: NaN
+    const bool bad = !(beta > 0.0 && beta < INFINITY) || m == INFINITY || q.most == INFINITY;
+    const bool zero = !bad && (!q.any || m == -INFINITY);
+    double loss = 0.0;
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u)
+        if (q.mass[u] > 0.0) loss += q.x[u] > -INFINITY ? q.mass[u] * (q.log_mass[u] - (t[u] - log_s)) : INFINITY;
+    loss = wave_sum(loss);
+    const double log_out = log(s_out), log_rest = t_out + log_out - log_s;  // ln R
+    if (rest > 0.0) loss += rest * (log(rest) - log_rest);
+    if (bad) loss = NAN;
+    if (zero) loss = 0.0;
+    if (threadIdx.x % kWave == 0) a.loss[row] = (float)loss;
+    RowGrad r = {};
+    if constexpr (GRAD) {
+        const double g = a.grad_loss[row];
+        const double scale = g == 0.0 || zero ? 0.0 : (bad ? NAN : g * beta), total = q.listed + rest;
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) grad[u] = scale == 0.0 ? 0.0 : scale * (total * (e[u] / s) - q.mass[u]);
+        r.m = m_out;
+        r.c2 = (float)beta * kLog2e;
+        const double shift = s_out > 0.0 ? log_out * (1.0 / kLn2) : 0.0;
+        r.shift = (float)shift;
+        // the shift's rounding goes into the factor
+        const double factor = total * (s_out > 0.0 ? exp(log_rest) : 0.0) - rest;
+        r.factor = scale == 0.0 ? 0.0f : (float)(scale * factor * exp2((double)r.shift - shift));
+    }
+    return r;
+}
+
+// Takes the listed tokens out of a chunk: bits of the part that starts at x_part.
+template <int DT, int NV, int THREADS>
+__device__ __forceinline__ void take_out(uint32_t (&w)[NV][4], const uint32_t *sh_bits, int x_chunk, int x_part) {
+    constexpr int kPer = Elem<DT>::kPer;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int at = vector_at<DT, kThreads>(0, i);
+        const int at = vector_at<DT, THREADS>(x_chunk - x_part, i);
         const uint32_t hit = (sh_bits[at / 32] >> (at % 32)) & ((1u << kPer) - 1u);
         if (hit != 0) {
 #pragma unroll
             for (int j = 0; j < kPer; ++j)
                 if ((hit >> j) & 1u) set_bits<DT>(w[i], j, Elem<DT>::kNone);
         }
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) tm = fmaxf(tm, value<DT>(w[i], j));
     }
-    const Sum ws = wave_sums<DT, NV, false>(w, tm, c2);
-    if (threadIdx.x % kWave == 0) sh_sum[threadIdx.x / kWave] = ws;
+}
+
+// Words of a bitmap over `width` tokens that whole chunks may ask for.
+template <int DT, int NV, int THREADS>
+__host__ __device__ __forceinline__ int bitmap_words(int width) {
+    constexpr int kChunk = NV * THREADS * Elem<DT>::kPer;
+    return (width + kChunk - 1) / kChunk * (kChunk / 32);
+}
+
+// Gradients of the unlisted tokens of elements x0 .. x1 - 1; zeros, without a reading, where the factor is 0.
+template <int DT, int NV, int THREADS>
+__device__ __forceinline__ void write_grad(const ListArgs &a, int64_t row_i, int x0, int x1, const RowGrad &q) {
+    using T = typename Elem<DT>::T;
+    constexpr int kPer = Elem<DT>::kPer, kChunk = NV * THREADS * kPer;
+    const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
+    T *out = static_cast<T *>(a.out) + row_i * a.out_ld;
+    if (q.factor == 0.0f) {
+        const float d[kPer] = {};
+        for (int x = x0; x < x1; x += kChunk)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) store_vector<DT>(out, vector_at<DT, THREADS>(x, i), a.v, d);
+        return;
+    }
+    for_chunks<DT, NV, THREADS, true, 1>(row, a.v, x0, x1, [&](uint32_t(&w)[NV][4], int x) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float d[kPer];
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const float t = fmaxf((value<DT>(w[i], j) - q.m) * q.c2 - q.shift, kLowest);
+                d[j] = q.factor * __builtin_amdgcn_exp2f(t);
+            }
+            store_vector<DT>(out, vector_at<DT, THREADS>(x, i), a.v, d);
+        }
+    });
+}
+
+template <int DT, int NV, int THREADS, bool GRAD>
+__global__ __launch_bounds__(THREADS) void list_whole(ListArgs a) {
+    using T = typename Elem<DT>::T;
+    constexpr int kWaves = THREADS / kWave;
+    extern __shared__ uint32_t sh_bits[];
+    __shared__ Sum sh_sum[kWaves];
+    __shared__ Entry sh_entry[kMaxTop];
+    __shared__ RowGrad sh_grad;
+    pass_over_nans();
+    const int64_t row_i = a.row0 + blockIdx.x;
+    const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const float c2 = scale_of(a.inv_temp, row_i) * kLog2e;
+    for (int i = threadIdx.x; i < bitmap_words<DT, NV, THREADS>(a.v); i += THREADS) sh_bits[i] = 0;
+    __syncthreads();
+    List list;
+    if (wave == 0) {
+        list = read_list(a, row_i);
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u)
+            if (list.id[u] >= 0) atomicOr(&sh_bits[list.id[u] / 32], 1u << (list.id[u] % 32));
+    }
+    __syncthreads();
+    Sum mine = {-INFINITY, 0.0f, 0.0f};
+    for_chunks<DT, NV, THREADS, !GRAD, 1>(row, a.v, 0, a.v, [&](uint32_t(&w)[NV][4], int x) {
+        float vm[NV];
+        take_out<DT, NV, THREADS>(w, sh_bits, x, 0);
+        add_chunk<DT, NV, false>(w, c2, mine, vm);
+    });
+    mine = wave_join<false>(mine, c2);
+    if (lane == 0) sh_sum[wave] = mine;
+    __syncthreads();
+    if (wave == 0) {
+        const Sum q = lane < kWaves ? sh_sum[lane] : Sum{-INFINITY, 0.0f, 0.0f};
+        const float m_out = wave_max(q.m);
+        double s_out = 0.0, grad[kSlots];
+        if (q.s > 0.0f) s_out = q.s * exp(((double)q.m - (double)m_out) * (double)scale_of(a.inv_temp, row_i));
+        s_out = wave_sum(s_out);
+        const RowGrad r = finish_row<GRAD>(a, row_i, list, m_out, s_out, grad);
+        if constexpr (GRAD) {
+#pragma unroll
+            for (int u = 0; u < kSlots; ++u) sh_entry[u * kWave + lane] = {list.id[u], (float)grad[u]};
+            if (lane == 0) sh_grad = r;
+        }
+    }
+    if constexpr (GRAD) {
+        __syncthreads();
+        const RowGrad q = sh_grad;
+        write_grad<DT, NV, THREADS>(a, row_i, 0, a.v, q);
+        // the listed tokens over what was just written: after the workgroup's stores
+        __syncthreads();
+        if ((int)threadIdx.x < a.n_top) {
+            const Entry e = sh_entry[threadIdx.x];
+            if (e.id >= 0) (static_cast<T *>(a.out) + row_i * a.out_ld)[e.id] = (T)encode<DT>(e.grad);
+        }
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void list_parts(ListArgs a) {
+    using T = typename Elem<DT>::T;
+    constexpr int kWaves = kThreads / kWave, NV = kChunkVectors;
+    extern __shared__ uint32_t sh_bits[];
+    __shared__ Sum sh_sum[kWaves];
+    pass_over_nans();
+    const int64_t r = blockIdx.x / (uint32_t)a.parts, row_i = a.row0 + r;
+    const int part = blockIdx.x % (uint32_t)a.parts, x0 = part * a.part_width;
+    const int x1 = x0 + a.part_width < a.v ? x0 + a.part_width : a.v;
+    const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
+    const float c2 = scale_of(a.inv_temp, row_i) * kLog2e;
+    for (int i = threadIdx.x; i < bitmap_words<DT, NV, kThreads>(x1 - x0); i += kThreads) sh_bits[i] = 0;
+    __syncthreads();
+    if ((int)threadIdx.x < a.n_top) {
+        const int at = entry_id(a, row_i, threadIdx.x, a.logprobs[row_i * a.n_top + threadIdx.x]) - x0;
+        if (at >= 0 && at < x1 - x0) atomicOr(&sh_bits[at / 32], 1u << (at % 32));
+    }
+    __syncthreads();
+    Sum mine = {-INFINITY, 0.0f, 0.0f};
+    for_chunks<DT, NV, kThreads, false, 1>(row, a.v, x0, x1, [&](uint32_t(&w)[NV][4], int x) {
+        float vm[NV];
+        take_out<DT, NV, kThreads>(w, sh_bits, x, x0);
+        add_chunk<DT, NV, false>(w, c2, mine, vm);
+    });
+    mine = wave_join<false>(mine, c2);
+    if (threadIdx.x % kWave == 0) sh_sum[threadIdx.x / kWave] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
         Sum s = sh_sum[0];
@@ -115,182 +355,120 @@ __global__ __launch_bounds__(kThreads) void list_parts(ListArgs a) {
     }
 }
 
-// Reductions over the two waves of list_rows, the result in every thread.
-__device__ __forceinline__ float pair_max(float x, float *sh) {
-    x = wave_max(x);
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) sh[threadIdx.x / kWave] = x;
-    __syncthreads();
-    return fmaxf(sh[0], sh[1]);
-}
-__device__ __forceinline__ double pair_sum(double x, double *sh) {
-    x = wave_sum(x);
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) sh[threadIdx.x / kWave] = x;
-    __syncthreads();
-    return sh[0] + sh[1];
-}
-
+// One wave a row.
 template <bool GRAD>
-__global__ __launch_bounds__(kListThreads) void list_rows(ListArgs a) {
-    __shared__ float sh_f[2];
-    __shared__ double sh_d[2], sh_w[kMaxTop];
-    __shared__ int32_t sh_id[kMaxTop];
+__global__ __launch_bounds__(kWave) void list_rows(ListArgs a) {
     const int64_t r = blockIdx.x, row = a.row0 + r;
-    const int k = threadIdx.x;
+    const int lane = threadIdx.x;
     const float2 *sums = a.sums + (size_t)r * a.parts;
-    const double beta = scale_of(a.inv_temp, row);
-    const bool sound = beta > 0.0 && beta < INFINITY;
-    // the unlisted tokens: largest logit m_out, sum s_out relative to it
+    const List list = read_list(a, row);
     float m_out = -INFINITY;
-    for (int p = k; p < a.parts; p += kListThreads) m_out = fmaxf(m_out, sums[p].x);
-    m_out = pair_max(m_out, sh_f);
-    double s_out = 0.0;
-    for (int p = k; p < a.parts; p += kListThreads) {
+    for (int p = lane; p < a.parts; p += kWave) m_out = fmaxf(m_out, sums[p].x);
+    m_out = wave_max(m_out);
+    const double beta = scale_of(a.inv_temp, row);
+    double s_out = 0.0, grad[kSlots];
+    for (int p = lane; p < a.parts; p += kWave) {
         const float2 q = sums[p];
         if (q.y > 0.0f) s_out += q.y * exp(((double)q.x - (double)m_out) * beta);
     }
-    s_out = pair_sum(s_out, sh_d);
-    // the list
-    const int32_t id = k < a.n_top ? entry_id(a, row, k) : -1;
-    const float lp = id >= 0 ? a.logprobs[row * a.n_top + k] : -INFINITY;
-    const float lp_most = pair_max(lp, sh_f);
-    double w = id >= 0 ? exp(a.tail ? (double)lp : (double)lp - (double)lp_most) : 0.0;
-    if (!a.tail) {
-        const double all = pair_sum(w, sh_d);
-        w = id >= 0 ? w / all : 0.0;
-    }
-    sh_id[k] = id;
-    sh_w[k] = w;
-    __syncthreads();
-    bool first = id >= 0;  // the entry that stands for its token
-    double mass = 0.0;     // the teacher's probability of that token
-    for (int i = 0; i < a.n_top; ++i) {
-        if (sh_id[i] == id) {
-            mass += sh_w[i];
-            first = first && i >= k;
-        }
-    }
-    if (!first) mass = 0.0;
-    float x = -INFINITY;
-    if (first) {
-        const int64_t at = row * a.ld;
-        const void *base = a.dtype == TT_F32 ? (const void *)(static_cast<const float *>(a.logits) + at)
-                                             : (const void *)(static_cast<const uint16_t *>(a.logits) + at);
-        x = load_logit(base, a.dtype, id);
-    }
-    const float m = fmaxf(m_out, pair_max(x, sh_f));
-    const double t = ((double)x - (double)m) * beta;  // -inf (or NaN, in a row without a finite logit) where x is
-    const double e = x > -INFINITY ? exp(t) : 0.0;
-    const double t_out = ((double)m_out - (double)m) * beta;  // ln of the unlisted sum's scale
-    const double s_in = pair_sum(e, sh_d);
-    const double s = s_in + (s_out > 0.0 ? s_out * exp(t_out) : 0.0);
-    const double listed = pair_sum(mass, sh_d);
-    const bool any = pair_sum(first ? 1.0 : 0.0, sh_d) > 0.0;
-    const double rest = a.tail && s_out > 0.0 ? fmax(0.0, 1.0 - listed) : 0.0;
-    // nothing listed, or no finite logit: 0; a logit or list value of +inf, or an unsound temperature: NaN
-    const bool bad = !sound || m == INFINITY || lp_most == INFINITY;
-    const bool zero = !bad && (!any || m == -INFINITY);
-    const double log_s = log(s);
-    double term = 0.0;
-    if (mass > 0.0) term = x > -INFINITY ? mass * (log(mass) - (t - log_s)) : INFINITY;
-    double loss = pair_sum(term, sh_d);
-    const double log_rest = t_out + log(s_out) - log_s;  // ln R
-    if (rest > 0.0) loss += rest * (log(rest) - log_rest);
-    if (bad) loss = NAN;
-    if (zero) loss = 0.0;
-    if (k == 0) a.loss[row] = (float)loss;
+    s_out = wave_sum(s_out);
+    const RowGrad q = finish_row<GRAD>(a, row, list, m_out, s_out, grad);
     if constexpr (GRAD) {
-        const double g = a.grad_loss[row];
-        const double scale = g == 0.0 || zero ? 0.0 : (bad ? NAN : g * beta), total = listed + rest;
-        if (k < a.n_top) {
-            Entry out;
-            out.id = first ? id : -1;
-            out.grad = scale == 0.0 ? 0.0f : (float)(scale * (total * (e / s) - mass));
-            a.entries[(size_t)r * a.n_top + k] = out;
-        }
-        if (k == 0) {
-            RowGrad q;
-            q.m = m_out;
-            q.c2 = (float)beta * kLog2e;
-            q.shift = s_out > 0.0 ? (float)log2(s_out) : 0.0f;
-            const double share = s_out > 0.0 ? exp(log_rest) : 0.0;
-            q.factor = scale == 0.0 ? 0.0f : (float)(scale * (total * share - rest));
-            a.row_grad[r] = q;
-        }
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u)
+            if (u * kWave + lane < a.n_top) a.entries[(size_t)r * a.n_top + u * kWave + lane] = {list.id[u], (float)grad[u]};
+        if (lane == 0) a.row_grad[r] = q;
     }
 }
-
-constexpr int kGradVectors = 4;
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void list_grad(ListArgs a, int parts) {
     using T = typename Elem<DT>::T;
-    constexpr int kPer = Elem<DT>::kPer;
-    constexpr int kPart = kGradVectors * kThreads * kPer;
+    constexpr int kPart = kChunkVectors * kThreads * Elem<DT>::kPer;
     const int64_t r = blockIdx.x / (uint32_t)parts, row_i = a.row0 + r;
-    const int x_part = (int)(blockIdx.x % (uint32_t)parts) * kPart;
-    const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
-    T *out = static_cast<T *>(a.out) + row_i * a.out_ld;
-    const RowGrad q = a.row_grad[r];
+    const int x0 = (int)(blockIdx.x % (uint32_t)parts) * kPart, x1 = x0 + kPart < a.v ? x0 + kPart : a.v;
     Entry mine = {-1, 0.0f};
     if ((int)threadIdx.x < a.n_top) mine = a.entries[(size_t)r * a.n_top + threadIdx.x];
-    float d[kPer];
-    if (q.factor == 0.0f) {
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) d[j] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kGradVectors; ++i) store_vector<DT>(out, vector_at<DT, kThreads>(x_part, i), a.v, d);
-    } else {
-        uint32_t w[kGradVectors][4];
-        load_part<DT, kGradVectors, kThreads>(row, a.v, x_part, w);
-#pragma unroll
-        for (int i = 0; i < kGradVectors; ++i) {
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                const float t = fmaxf((value<DT>(w[i], j) - q.m) * q.c2 - q.shift, kLowest);
-                d[j] = q.factor * __builtin_amdgcn_exp2f(t);
-            }
-            store_vector<DT>(out, vector_at<DT, kThreads>(x_part, i), a.v, d);
-        }
-    }
-    // the listed tokens over what was just written: after the workgroup's stores have been made
-    __threadfence_block();
+    write_grad<DT, kChunkVectors, kThreads>(a, row_i, x0, x1, a.row_grad[r]);
+    // the listed tokens over what was just written: after the workgroup's stores
     __syncthreads();
-    if (mine.id >= x_part && mine.id < x_part + kPart) out[mine.id] = (T)encode<DT>(mine.grad);
+    if (mine.id >= x0 && mine.id < x1) (static_cast<T *>(a.out) + row_i * a.out_ld)[mine.id] = (T)encode<DT>(mine.grad);
 }
 
+// Threads and vectors of list_whole for rows of these bytes.
+constexpr int kLongThreads = 1024, kLongVectors = 2;
+constexpr int64_t kShortRow = 32 << 10;          // bytes of a row that kThreads threads take whole
+constexpr int64_t kSplitRow = 128 << 10;         // and of one that is split where there are few rows
+constexpr int64_t kFewRows = 256;                // fewer leave compute units without a row
+constexpr size_t kCachedBytes = size_t(96) << 20;  // logits of a group of split rows, with the gradient
+
 struct Plan {
-    Split split;
+    int parts, part_width;  // parts == 0: list_whole
+    int threads;
     int64_t rows;
     size_t row_grad, entries, total;
 };
 
 Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
-    Plan p;
-    p.split = split_rows(n_rows, v, dtype);
-    if (p.split.threads != kThreads) p.split = {kThreads, kWideVectors, (int)((v + 8 * 256 * elements_per_vector(dtype) - 1) / (8 * 256 * elements_per_vector(dtype)))};
-    int64_t most = kMaxGrid / p.split.parts;
-    if (grad) {
-        const int64_t per = (int64_t)kGradVectors * kThreads * elements_per_vector(dtype);
-        const int64_t grid = kMaxGrid / ((v + per - 1) / per);
-        const int64_t cached = (int64_t)(kCachedBytes / ((size_t)v * element_bytes(dtype)));
-        most = most < grid ? most : grid;
-        most = most < cached ? most : cached;
+    Plan p = {};
+    const int64_t bytes = (int64_t)v * element_bytes(dtype);
+    const int chunk = kChunkVectors * kThreads * elements_per_vector(dtype), chunks = (v + chunk - 1) / chunk;
+    int64_t most = kMaxGrid;
+    if (v <= kMaxBits && (n_rows >= kFewRows || bytes <= kSplitRow)) {
+        p.threads = bytes <= kShortRow || !grad ? kThreads : kLongThreads;
+    } else {
+        int64_t parts = n_rows > 0 ? (kFullGrid + n_rows - 1) / n_rows : 1;
+        const int64_t least = (v + kMaxBits - 1) / kMaxBits;
+        if (parts < least) parts = least;
+        if (parts > chunks) parts = chunks;
+        const int each = (int)((chunks + parts - 1) / parts);
+        p.part_width = each * chunk;
+        p.parts = (chunks + each - 1) / each;
+        most = kMaxGrid / (grad ? chunks : p.parts);
+        if (grad && (int64_t)(kCachedBytes / bytes) < most) most = (int64_t)(kCachedBytes / bytes);
+        if (most < 1) most = 1;
     }
-    if (most < 1) most = 1;
     const int64_t groups = (n_rows + most - 1) / most;
     p.rows = groups == 0 ? 0 : (n_rows + groups - 1) / groups;
-    p.row_grad = round256((size_t)p.rows * p.split.parts * sizeof(float2));
-    p.entries = p.row_grad + (grad ? round256((size_t)p.rows * sizeof(RowGrad)) : 0);
-    p.total = p.entries + (grad ? (size_t)p.rows * n_top * sizeof(Entry) : 0);
+    if (p.parts > 0) {
+        p.row_grad = round256((size_t)p.rows * p.parts * sizeof(float2));
+        p.entries = p.row_grad + (grad ? round256((size_t)p.rows * sizeof(RowGrad)) : 0);
+        p.total = p.entries + (grad ? (size_t)p.rows * n_top * sizeof(Entry) : 0);
+    }
     return p;
 }
 
+template <int DT, bool GRAD>
+void launch_whole(const ListArgs &a, int threads, int64_t n, hipStream_t stream) {
+    if (threads == kThreads) {
+        const size_t lds = bitmap_words<DT, kChunkVectors, kThreads>(a.v) * sizeof(uint32_t);
+        list_whole<DT, kChunkVectors, kThreads, GRAD><<<(unsigned)n, kThreads, lds, stream>>>(a);
+    } else if constexpr (GRAD) {
+        const size_t lds = bitmap_words<DT, kLongVectors, kLongThreads>(a.v) * sizeof(uint32_t);
+        list_whole<DT, kLongVectors, kLongThreads, true><<<(unsigned)n, kLongThreads, lds, stream>>>(a);
+    }
+}
+
 template <int DT>
-void launch_list_parts(const ListArgs &a, int vectors, unsigned grid, hipStream_t stream) {
-    if (vectors == kWideVectors) list_parts<DT, kWideVectors><<<grid, kThreads, 0, stream>>>(a);
-    else list_parts<DT, kNarrowVectors><<<grid, kThreads, 0, stream>>>(a);
+int launch_rows(const ListArgs &a, const Plan &p, int64_t n, hipStream_t stream) {
+    const bool grad = a.out != nullptr;
+    if (p.parts == 0) {
+        if (grad) launch_whole<DT, true>(a, p.threads, n, stream);
+        else launch_whole<DT, false>(a, p.threads, n, stream);
+        return hipGetLastError() == hipSuccess ? TT_OK : TT_ELAUNCH;
+    }
+    const size_t lds = bitmap_words<DT, kChunkVectors, kThreads>(a.part_width) * sizeof(uint32_t);
+    list_parts<DT><<<(unsigned)(n * p.parts), kThreads, lds, stream>>>(a);
+    if (hipGetLastError() != hipSuccess) return TT_ELAUNCH;
+    if (grad) list_rows<true><<<(unsigned)n, kWave, 0, stream>>>(a);
+    else list_rows<false><<<(unsigned)n, kWave, 0, stream>>>(a);
+    if (hipGetLastError() != hipSuccess) return TT_ELAUNCH;
+    if (grad) {
+        const int chunk = kChunkVectors * kThreads * Elem<DT>::kPer, parts = (a.v + chunk - 1) / chunk;
+        list_grad<DT><<<(unsigned)(n * parts), kThreads, 0, stream>>>(a, parts);
+        if (hipGetLastError() != hipSuccess) return TT_ELAUNCH;
+    }
+    return TT_OK;
 }
 
 }  // namespace
@@ -300,17 +478,17 @@ size_t distill_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top, 
 }
 
 int launch_distill(const DistillArgs &l, void *workspace, size_t workspace_bytes, hipStream_t stream) {
-    const bool grad = l.dlogits != nullptr;
-    const Plan p = plan_of(l.n_rows, l.v, l.dtype, l.n_top, grad);
-    if (workspace == nullptr || workspace_bytes < p.total) return TT_EWORKSPACE;
-    if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return TT_EINVAL;
+    const Plan p = plan_of(l.n_rows, l.v, l.dtype, l.n_top, l.dlogits != nullptr);
+    if (p.total > 0 && (workspace == nullptr || workspace_bytes < p.total)) return TT_EWORKSPACE;
+    if (p.total > 0 && reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return TT_EINVAL;
     char *ws = static_cast<char *>(workspace);
     ListArgs a;
     a.logits = l.logits;
     a.ld = l.ld;
     a.v = l.v;
     a.dtype = l.dtype;
-    a.parts = p.split.parts;
+    a.parts = p.parts;
+    a.part_width = p.part_width;
     a.n_top = l.n_top;
     a.tail = l.tail;
     a.inv_temp = l.inv_temp;
@@ -318,32 +496,21 @@ int launch_distill(const DistillArgs &l, void *workspace, size_t workspace_bytes
     a.logprobs = l.top_logprobs;
     a.id_map = l.id_map;
     a.n_map = l.n_map;
-    a.sums = reinterpret_cast<float2 *>(ws);
+    a.sums = p.total > 0 ? reinterpret_cast<float2 *>(ws) : nullptr;
     a.loss = l.loss;
     a.grad_loss = l.grad_loss;
-    a.row_grad = reinterpret_cast<RowGrad *>(ws + p.row_grad);
-    a.entries = reinterpret_cast<Entry *>(ws + p.entries);
+    a.row_grad = p.total > 0 ? reinterpret_cast<RowGrad *>(ws + p.row_grad) : nullptr;
+    a.entries = p.total > 0 ? reinterpret_cast<Entry *>(ws + p.entries) : nullptr;
     a.out = l.dlogits;
     a.out_ld = l.out_ld;
-    const int64_t per = (int64_t)kGradVectors * kThreads * elements_per_vector(l.dtype);
-    const int grad_parts = (int)((l.v + per - 1) / per);
     for (int64_t row0 = 0; row0 < l.n_rows; row0 += p.rows) {
         const int64_t n = l.n_rows - row0 < p.rows ? l.n_rows - row0 : p.rows;
         a.row0 = row0;
-        const unsigned grid = (unsigned)(n * a.parts);
-        if (l.dtype == TT_BF16) launch_list_parts<TT_BF16>(a, p.split.vectors, grid, stream);
-        else if (l.dtype == TT_F16) launch_list_parts<TT_F16>(a, p.split.vectors, grid, stream);
-        else launch_list_parts<TT_F32>(a, p.split.vectors, grid, stream);
-        if (hipGetLastError() != hipSuccess) return TT_ELAUNCH;
-        if (grad) list_rows<true><<<(unsigned)n, kListThreads, 0, stream>>>(a);
-        else list_rows<false><<<(unsigned)n, kListThreads, 0, stream>>>(a);
-        if (hipGetLastError() != hipSuccess) return TT_ELAUNCH;
-        if (!grad) continue;
-        const unsigned grad_grid = (unsigned)(n * grad_parts);
-        if (l.dtype == TT_BF16) list_grad<TT_BF16><<<grad_grid, kThreads, 0, stream>>>(a, grad_parts);
-        else if (l.dtype == TT_F16) list_grad<TT_F16><<<grad_grid, kThreads, 0, stream>>>(a, grad_parts);
-        else list_grad<TT_F32><<<grad_grid, kThreads, 0, stream>>>(a, grad_parts);
-        if (hipGetLastError() != hipSuccess) return TT_ELAUNCH;
+        int st;
+        if (l.dtype == TT_BF16) st = launch_rows<TT_BF16>(a, p, n, stream);
+        else if (l.dtype == TT_F16) st = launch_rows<TT_F16>(a, p, n, stream);
+        else st = launch_rows<TT_F32>(a, p, n, stream);
+        if (st != TT_OK) return st;
     }
     return TT_OK;
 }

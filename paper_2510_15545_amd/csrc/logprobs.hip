@@ -7,14 +7,14 @@
 //   alternatives: the largest x, ties by the lower index, minus infinity never listed
 //   d_j = beta (g ([j = id] - p_j) - h p_j (lp_j + H)), upstream gradients g of lp_id and h of H
 //
-// One pass over the row.  A workgroup holds a part of a row in registers, forms its largest value
-// first and then its sums (base 2, v_exp_f32), and, for the alternatives, a lower bound of its k-th
-// largest value: the k-th largest of 256 groups' largest values (a lane's, or four lanes'), found by
-// 16 ballots on the upper 16 bits of their order keys.  k distinct elements reach it, so the k largest
-// do, and about 1.2 to 2 k in all: these become 64-bit keys (value, then lower index).
-// row_parts: parts of 16 KB to 32 KB, their sums and keys to the workspace; row_finish: a workgroup
-// per row joins the sums in fp64 and selects the k largest keys in the same way, ordered by counting.
-// row_whole: a workgroup per row that takes the row as one part and finishes it itself.
+// One pass over the row: row_stream, a workgroup for a row or a part of it, by chunks of 16 KB whose loads are
+// in flight while the chunk before is worked on.  Each thread keeps the largest value and the sums
+// (base 2, v_exp_f32) of what it has seen.  For the alternatives it keeps the place of its largest
+// value as well: k of the workgroup's 256 lane groups hold a largest value that reaches the k-th largest
+// of the 256, so every one of the k largest elements does.  That bound is formed after chunks 1, 2, 4,
+// 8, ..., and elements that reach it are staged in LDS as 64-bit keys (value, then lower index); over a
+// row of N chunks about k (1 + ln N) of them.  A row's only workgroup finishes it (fp64 from the waves'
+// sums on; keys ordered by counting); with several, row_finish does.
 #include "rows.h"
 
 namespace tt {
@@ -25,17 +25,19 @@ using namespace rows;
 constexpr int kMaxTop = 128;
 constexpr int kSelect = 1024;                       // keys that are ordered in LDS
 constexpr int kGroups = 256;                        // lane groups whose largest values give the bound
+constexpr int kCrowd = 24;                          // groups beyond k at the bound that make it worth refining
+constexpr int kChunkVectors = 4;
+constexpr int kWholeChunks = 2;                     // rows of at most this many chunks are never split
 constexpr size_t kMaxKeyBytes = size_t(128) << 20;  // workspace: rows are taken in groups beyond
 constexpr int64_t kMaxGrid = int64_t(1) << 18;      // workgroups of one launch
 
-// Keys that a part may hand over.  Where fewer than k lanes hold a finite value, all their elements may
-// reach the bound (a lane has 8 then); more are ties, and the part selects its k largest exactly.
+// Keys that a part may hand over; a part with more that reach its bound selects its k largest exactly.
 inline int part_capacity(int n_top) { return 8 * n_top + 64; }
 
 struct RowArgs {
     const void *logits;
     int64_t ld, row0;  // row0: the first row of this launch
-    int v, dtype, parts, n_top, capacity;
+    int v, dtype, parts, part_width, n_top, capacity;
     const float *inv_temp;
     const int32_t *ids;
     float4 *sums;    // per part: m, s, e, number of keys (bits)
@@ -46,53 +48,89 @@ struct RowArgs {
 };
 
 // LDS of the selection; a wave stages its keys in a segment of its own.
-template <int THREADS>
 struct TopLds {
-    static constexpr int kStage = THREADS == kThreads ? 512 : 128;
-    uint32_t largest[THREADS];
-    uint64_t stage[THREADS / kWave][kStage];
-    int count[THREADS / kWave], slots[64], total;
+    static constexpr int kStage = 512;
+    uint32_t largest[kGroups];
+    int where[kGroups];
+    uint64_t stage[kThreads / kWave][kStage];
+    int slots[64], total;
 };
 
-// Largest bound P on 16-bit keys that at least k of the kGroups groups reach (each wave for itself).
-template <int THREADS>
-__device__ __forceinline__ uint32_t kth_key16(const uint32_t *sh_largest, int k) {
-    constexpr int kPerLane = kGroups / kWave;
-    const int lane = threadIdx.x % kWave;
-    uint32_t q[kPerLane];
-#pragma unroll
-    for (int u = 0; u < kPerLane; ++u) {
-        q[u] = sh_largest[u * kWave + lane];
-#pragma unroll
-        for (int g = 1; g < THREADS / kGroups; ++g) {
-            const uint32_t o = sh_largest[g * kGroups + u * kWave + lane];
-            q[u] = o > q[u] ? o : q[u];
-        }
-    }
-    uint32_t p = 0;
-#pragma unroll
-    for (int b = 15; b >= 0; --b) {
-        const uint32_t c = p | (1u << b);
-        int n = 0;
-#pragma unroll
-        for (int u = 0; u < kPerLane; ++u) n += __popcll(__ballot(q[u] >= c));
-        if (n >= k) p = c;
-    }
-    return p;
-}
+// An element reaches the bound if its order key is larger than `key`, or equal and its index at most `index`.
+struct Bound {
+    uint32_t key;
+    int index;
+    __device__ __forceinline__ float lowest() const { return key_value(key); }
+    __device__ __forceinline__ uint64_t full() const { return ((uint64_t)key << 32) | (0xFFFFFFFFu - (uint32_t)index); }
+};
 
-// The lowest finite value whose key's upper half reaches p.
-__device__ __forceinline__ float bound_value(uint32_t p) {
-    return p <= 0x007Fu ? -0x1.fffffep+127f : key_value(p << 16);
-}
+constexpr uint32_t kLowestFinite = 0x00800000u;  // order key of -FLT_MAX
 
-__device__ __forceinline__ uint64_t full_key(float x, int index) {
-    return ((uint64_t)order_key(x) << 32) | (0xFFFFFFFFu - (uint32_t)index);
+__device__ __forceinline__ uint64_t full_key(uint32_t order, int index) {
+    return ((uint64_t)order << 32) | (0xFFFFFFFFu - (uint32_t)index);
 }
 
 // Lanes below this one among those of a mask.
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// How many of the 256 values that a wave holds, four a lane, satisfy f.
+template <typename F>
+__device__ __forceinline__ int count_groups(F f) {
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < kGroups / kWave; ++u) n += __popcll(__ballot(f(u)));
+    return n;
+}
+
+// The upper 16 bits of the largest order key that at least k groups reach; n: how many reach it.
+__device__ __forceinline__ uint32_t kth_upper(const uint32_t (&q)[kGroups / kWave], int k, int &n) {
+    uint32_t p = 0;
+    n = kGroups;
+#pragma unroll
+    for (int b = 31; b >= 16; --b) {
+        const uint32_t c = p | (1u << b);
+        const int m = count_groups([&](int u) { return q[u] >= c; });
+        if (m >= k) {
+            p = c;
+            n = m;
+        }
+    }
+    return p;
+}
+
+// The bound from the groups' largest values and an index that each one's element does not pass: reached by k
+// groups' elements at least.  16 ballots; where many more groups tie at it (equal values, as in a row
+// of capped logits), the rest of the value and then the index decide.  Each wave for itself.
+__device__ __forceinline__ Bound kth_bound(const TopLds &sh, int k) {
+    const int lane = threadIdx.x % kWave;
+    uint32_t q[kGroups / kWave];
+#pragma unroll
+    for (int u = 0; u < kGroups / kWave; ++u) q[u] = sh.largest[u * kWave + lane];
+    int n;
+    Bound r = {kth_upper(q, k, n), INT_MAX};
+    if (r.key < kLowestFinite) return {kLowestFinite, INT_MAX};  // fewer than k groups hold a finite value
+    if (n < k + kCrowd) return r;
+    for (int b = 15; b >= 0; --b) {
+        const uint32_t c = r.key | (1u << b);
+        const int m = count_groups([&](int u) { return q[u] >= c; });
+        if (m >= k) {
+            r.key = c;
+            n = m;
+        }
+    }
+    if (n < k + kCrowd) return r;
+    int at[kGroups / kWave];
+#pragma unroll
+    for (int u = 0; u < kGroups / kWave; ++u) at[u] = sh.where[u * kWave + lane];
+    const int need = k - count_groups([&](int u) { return q[u] > r.key; });
+    r.index = 0;  // the largest index with fewer than `need` equal groups below it
+    for (int b = 23; b >= 0; --b) {
+        const int c = r.index | (1 << b);
+        if (count_groups([&](int u) { return q[u] == r.key && at[u] < c; }) < need) r.index = c;
+    }
+    return r;
 }
 
 // Sum over the workgroup of a count, through a zeroed LDS slot of its own.
@@ -104,43 +142,25 @@ __device__ __forceinline__ int block_count(int n, int *slot) {
     return *slot;
 }
 
-// Hides from the compiler that a value has not changed: what follows is formed from it again instead of
-// being held in registers from before.
-__device__ __forceinline__ void form_again(uint32_t &x) { asm volatile("" : "+v"(x)); }
-
-template <int NV>
-__device__ __forceinline__ void form_again(uint32_t (&w)[NV][4]) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) form_again(w[i][q]);
-}
-
-// Elements of a part that satisfy f(order key, index in the part), counted by this thread.
-template <int DT, int NV, int THREADS, typename F>
-__device__ __forceinline__ int count_if(uint32_t (&w)[NV][4], F f) {
-    constexpr int kPer = Elem<DT>::kPer;
+// Elements x0 .. x1 - 1 of a row that satisfy f(order key, index), counted by this thread.
+template <int DT, typename F>
+__device__ __forceinline__ int count_if(const typename Elem<DT>::T *row, int x0, int x1, F f) {
     int n = 0;
-    uint32_t first = threadIdx.x * kPer;
-    form_again(w);
-    form_again(first);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const float x = value<DT>(w[i], j);
-            n += (x > -INFINITY && f(order_key(x), (int)first + i * THREADS * kPer + j)) ? 1 : 0;
-        }
+#pragma unroll 4
+    for (int x = x0 + (int)threadIdx.x; x < x1; x += kThreads) {
+        const float y = decode<DT>(row[x]);
+        n += (y > -INFINITY && f(order_key(y), x)) ? 1 : 0;
     }
     return n;
 }
 
-// The part's k largest elements exactly, where too many reach the bound (many equal values): the k-th
-// largest value by binary search on its order key, then the last index among the elements equal to
-// it.  At least k elements are finite.  49 counts, each over the registers.
-template <int DT, int NV, int THREADS>
-__device__ __forceinline__ void select_exactly(uint32_t (&w)[NV][4], int x_part, int k, uint64_t *keys, int *sh_slots,
-                                               int *sh_total) {
+// The k largest of a part's elements exactly, where too many reach the bound (only rows made for it do that:
+// large values all in the same lanes): the k-th largest value by binary search on its order key, then
+// the last index among the elements equal to it, each step a count over the part, read again.  At
+// least k elements are finite.
+template <int DT>
+__device__ __noinline__ void select_exactly(const typename Elem<DT>::T *row, int x0, int x1, int k, uint64_t *keys, int *sh_slots,
+                                            int *sh_total) {
     if (threadIdx.x < 64) sh_slots[threadIdx.x] = 0;
     if (threadIdx.x == 0) *sh_total = 0;
     __syncthreads();
@@ -148,86 +168,135 @@ __device__ __forceinline__ void select_exactly(uint32_t (&w)[NV][4], int x_part,
     uint32_t kth = 0;
     for (int b = 31; b >= 0; --b) {
         const uint32_t c = kth | (1u << b);
-        const int n = count_if<DT, NV, THREADS>(w, [c](uint32_t o, int) { return o >= c; });
+        const int n = count_if<DT>(row, x0, x1, [c](uint32_t o, int) { return o >= c; });
         if (block_count(n, &sh_slots[slot++]) >= k) kth = c;
     }
-    const int above = count_if<DT, NV, THREADS>(w, [kth](uint32_t o, int) { return o > kth; });
+    const int above = count_if<DT>(row, x0, x1, [kth](uint32_t o, int) { return o > kth; });
     const int need = k - block_count(above, &sh_slots[slot++]);
-    int last = 0;  // the largest index bound with fewer than `need` equal elements below it
-    for (int b = 15; b >= 0; --b) {  // indices in a part are below 2^16
+    int last = 0;  // the largest index with fewer than `need` equal elements below it
+    for (int b = 23; b >= 0; --b) {
         const int c = last | (1 << b);
-        const int n = count_if<DT, NV, THREADS>(w, [kth, c](uint32_t o, int at) { return o == kth && at < c; });
+        const int n = count_if<DT>(row, x0, x1, [kth, c](uint32_t o, int x) { return o == kth && x < c; });
         if (block_count(n, &sh_slots[slot++]) < need) last = c;
     }
-    count_if<DT, NV, THREADS>(w, [=](uint32_t o, int at) {
-        if (o > kth || (o == kth && at <= last))
-            keys[atomicAdd(sh_total, 1)] = ((uint64_t)o << 32) | (0xFFFFFFFFu - (uint32_t)(x_part + at));
+    count_if<DT>(row, x0, x1, [=](uint32_t o, int x) {
+        if (o > kth || (o == kth && x <= last)) keys[atomicAdd(sh_total, 1)] = full_key(o, x);
         return false;
     });
+    __syncthreads();
 }
 
-// Keys of a part's elements that reach the bound, to dst (LDS or global); returns their number, at least
-// the part's finite elements or k, at most capacity (>= k).  sh.largest is written and a barrier passed.
-template <int DT, int NV, int THREADS>
-__device__ __forceinline__ int collect(uint32_t (&w)[NV][4], const float (&vm)[NV], int x_part, int k, uint64_t *dst, int capacity,
-                                       TopLds<THREADS> &sh) {
-    constexpr int kWaves = THREADS / kWave, kStage = TopLds<THREADS>::kStage;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const float bound = bound_value(kth_key16<THREADS>(sh.largest, k));
-    int n = 0;
-    form_again(w);
+// The elements of a row that may be among its k largest, chunk by chunk.
+template <int DT, int NV>
+struct TopSet {
+    static constexpr int kPer = Elem<DT>::kPer, kChunk = NV * kThreads * kPer;
+    TopLds &sh;
+    int k;
+    Bound bound = {kLowestFinite, INT_MAX};
+    float most = -INFINITY;     // the thread's largest value
+    int where = 0;              // first index of its vector
+    int staged = 0, chunks = 0; // of this wave; of the row
+    bool current = false;       // the bound is that of all chunks so far
+
+    __device__ __forceinline__ void raise() {
+        __syncthreads();  // the last bound has been read
+        sh.largest[threadIdx.x] = order_key(most);
+        sh.where[threadIdx.x] = where + kPer - 1;
+        __syncthreads();
+        bound = kth_bound(sh, k);
+        current = true;
+    }
+
+    __device__ __forceinline__ void add(const uint32_t (&w)[NV][4], const float (&vm)[NV], int x_chunk) {
+        const int wave = threadIdx.x / kWave;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (__ballot(vm[i] >= bound) == 0) continue;
+        for (int i = 0; i < NV; ++i) {
+            if (vm[i] > most) {
+                most = vm[i];
+                where = vector_at<DT, kThreads>(x_chunk, i);
+            }
+        }
+        current = false;
+        ++chunks;
+        if ((chunks & (chunks - 1)) == 0) raise();
+        const float lowest = bound.lowest();
 #pragma unroll
-        for (int j = 0; j < Elem<DT>::kPer; ++j) {
-            const float x = value<DT>(w[i], j);
-            const uint64_t hit = __ballot(x >= bound);
-            if (hit == 0) continue;
-            const int at = n + lanes_below(hit);
-            if (x >= bound && at < kStage) sh.stage[wave][at] = full_key(x, vector_at<DT, THREADS>(x_part, i) + j);
-            n += __popcll(hit);
+        for (int i = 0; i < NV; ++i) {
+            if (__ballot(vm[i] >= lowest) == 0) continue;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const float x = value<DT>(w[i], j);
+                if (__ballot(x >= lowest) == 0) continue;
+                const int at = vector_at<DT, kThreads>(x_chunk, i) + j;
+                const bool in = x > lowest || (x == lowest && at <= bound.index);
+                const uint64_t hit = __ballot(in);
+                const int slot = staged + lanes_below(hit);
+                if (in && slot < TopLds::kStage) sh.stage[wave][slot] = full_key(order_key(x), at);
+                staged += __popcll(hit);
+            }
         }
     }
-    if (lane == 0) sh.count[wave] = n;
-    __syncthreads();
-    int total = 0, before = 0;
-    bool over = false;
-#pragma unroll
-    for (int u = 0; u < kWaves; ++u) {
-        const int c = sh.count[u];
-        before += u < wave ? c : 0;
-        total += c;
-        over = over || c > kStage;
+
+    // The keys that reach the bound of the whole part, to dst (LDS or global, `capacity` >= k of them); returns their
+    // number: at least k, or all of the part's finite elements.
+    __device__ __forceinline__ int finish(const typename Elem<DT>::T *row, int x0, int x1, uint64_t *dst, int capacity) {
+        const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+        if (!current) raise();
+        const uint64_t from = bound.full();
+        if (threadIdx.x == 0) sh.total = 0;
+        __syncthreads();
+        const bool over = staged > TopLds::kStage;
+        int n = 0;
+        if (over) {
+            n = capacity + 1;
+        } else {
+            for (int i = lane; i - lane < staged; i += kWave) n += __popcll(__ballot(i < staged && sh.stage[wave][i] >= from));
+        }
+        int base = 0;
+        if (lane == 0) base = atomicAdd(&sh.total, n);
+        base = __builtin_amdgcn_readfirstlane(base);
+        __syncthreads();
+        const int total = sh.total;
+        if (total > capacity) {
+            __syncthreads();
+            select_exactly<DT>(row, x0, x1, k, dst, sh.slots, &sh.total);
+            return k;
+        }
+        for (int i = lane; i - lane < staged; i += kWave) {
+            const uint64_t key = i < staged ? sh.stage[wave][i] : 0;
+            const bool in = i < staged && key >= from;
+            const uint64_t hit = __ballot(in);
+            if (in) dst[base + lanes_below(hit)] = key;
+            base += __popcll(hit);
+        }
+        return total;
     }
-    if (over || total > capacity) {
-        select_exactly<DT, NV, THREADS>(w, x_part, k, dst, sh.slots, &sh.total);
-        return k;
-    }
-    for (int i = lane; i < n; i += kWave) dst[before + i] = sh.stage[wave][i];
-    return total;
-}
+};
 
 // The largest k (all, if fewer) of c <= kSelect distinct keys in LDS, descending, in sh_out; returns their number.
-template <int THREADS>
 __device__ __forceinline__ int order_keys(uint64_t *sh_sel, int c, int k, uint32_t *sh_largest, int *sh_total, uint64_t *sh_out) {
     const int lane = threadIdx.x % kWave;
-    if (c > kGroups) {  // counting is quadratic: the bound once more, a key or a few a lane
-        constexpr int kEach = kSelect / THREADS;
+    if (c > kGroups) {  // counting is quadratic: the bound once more, a few keys a lane
+        constexpr int kEach = kSelect / kThreads;
         uint64_t mine[kEach];
         uint32_t most = 0;
 #pragma unroll
         for (int u = 0; u < kEach; ++u) {
-            const int i = u * THREADS + (int)threadIdx.x;
+            const int i = u * kThreads + (int)threadIdx.x;
             mine[u] = i < c ? sh_sel[i] : 0;
-            const uint32_t o = (uint32_t)(mine[u] >> 48);
+            const uint32_t o = (uint32_t)(mine[u] >> 32);
             most = o > most ? o : most;
         }
+        __syncthreads();
         sh_largest[threadIdx.x] = most;
         if (threadIdx.x == 0) *sh_total = 0;
         __syncthreads();
-        const uint64_t from = (uint64_t)kth_key16<THREADS>(sh_largest, k) << 48;
-        int n = 0;
+        uint32_t q[kGroups / kWave];
+#pragma unroll
+        for (int u = 0; u < kGroups / kWave; ++u) q[u] = sh_largest[u * kWave + lane];
+        int n;
+        const uint64_t from = (uint64_t)kth_upper(q, k, n) << 32;
+        n = 0;
 #pragma unroll
         for (int u = 0; u < kEach; ++u) n += __popcll(__ballot(mine[u] != 0 && mine[u] >= from));
         int base = 0;
@@ -242,7 +311,7 @@ __device__ __forceinline__ int order_keys(uint64_t *sh_sel, int c, int k, uint32
         __syncthreads();
         c = *sh_total;
     }
-    for (int i = threadIdx.x; i < c; i += THREADS) {
+    for (int i = threadIdx.x; i < c; i += kThreads) {
         const uint64_t key = sh_sel[i];
         int rank = 0;
 #pragma unroll 4
@@ -259,8 +328,15 @@ struct RowStats {
     bool bad;
 };
 
-// A row's results but the alternatives, by one thread: m, s and e as in Sum, in natural units and fp64.
-__device__ __forceinline__ RowStats write_row(const RowArgs &a, int64_t row, double beta, float m, double s, double e) {
+// The logit of a row's token, 0 where there is none: read long before it is wanted.
+__device__ __forceinline__ float token_logit(const RowArgs &a, int64_t row) {
+    if (a.logprob == nullptr) return 0.0f;
+    const int32_t id = a.ids[row];
+    return id >= 0 && id < a.v ? load_logit(row_at(a.logits, a.dtype, row * a.ld), a.dtype, id) : 0.0f;
+}
+
+// A row's results but the alternatives, by one thread: m, s and e as in Sum, in natural units and fp64; the token's logit.
+__device__ __forceinline__ RowStats write_row(const RowArgs &a, int64_t row, double beta, float m, double s, double e, float x_id) {
     // m = -inf: nothing is finite (s = 0); m = +inf or an unsound temperature: NaN
     RowStats q;
     q.m = m;
@@ -277,10 +353,7 @@ __device__ __forceinline__ RowStats write_row(const RowArgs &a, int64_t row, dou
     if (a.logprob != nullptr) {
         const int32_t id = a.ids[row];
         double lp = NAN;
-        if (!q.bad && id >= 0 && id < a.v) {
-            const float x = load_logit(row_at(a.logits, a.dtype, row * a.ld), a.dtype, id);
-            lp = x == -INFINITY ? -INFINITY : ((double)x - q.m) * beta - q.log_sum;
-        }
+        if (!q.bad && id >= 0 && id < a.v) lp = x_id == -INFINITY ? -INFINITY : ((double)x_id - q.m) * beta - q.log_sum;
         a.logprob[row] = (float)lp;
     }
     return q;
@@ -297,93 +370,59 @@ __device__ __forceinline__ void write_top(const RowArgs &a, int64_t row, const R
     a.top_logprobs[row * a.n_top + i] = (float)lp;
 }
 
-// Largest values of a thread's vectors, and of the thread.
-template <int DT, int NV>
-__device__ __forceinline__ float vector_maxima(const uint32_t (&w)[NV][4], float (&vm)[NV]) {
-    float tm = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        vm[i] = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < Elem<DT>::kPer; ++j) vm[i] = fmaxf(vm[i], value<DT>(w[i], j));
-        tm = fmaxf(tm, vm[i]);
-    }
-    return tm;
-}
-
-template <int DT, int NV, bool TOP, bool ENTROPY>
-__global__ __launch_bounds__(kThreads) void row_parts(RowArgs a) {
+// A part of a row by a workgroup; FINISH: the row is one part, and finished here.
+template <int DT, bool TOP, bool ENTROPY, bool FINISH>
+__global__ __launch_bounds__(kThreads) void row_stream(RowArgs a) {
     constexpr int kWaves = kThreads / kWave;
     __shared__ Sum sh_sum[kWaves];
-    __shared__ TopLds<TOP ? kThreads : kWave> sh;
-    pass_over_nans();
-    const int64_t r = blockIdx.x / (uint32_t)a.parts;
-    const int part = blockIdx.x % (uint32_t)a.parts;
-    const int x_part = part * NV * kThreads * Elem<DT>::kPer;
-    uint32_t w[NV][4];
-    load_part<DT, NV, kThreads>(static_cast<const typename Elem<DT>::T *>(a.logits) + (a.row0 + r) * a.ld, a.v, x_part, w);
-    const float c2 = scale_of(a.inv_temp, a.row0 + r) * kLog2e;
-    float vm[NV];
-    const float tm = vector_maxima<DT, NV>(w, vm);
-    if constexpr (TOP) {
-        sh.largest[threadIdx.x] = order_key(tm) >> 16;
-        form_again(w);
-    }
-    const Sum ws = wave_sums<DT, NV, ENTROPY>(w, tm, c2);
-    if (threadIdx.x % kWave == 0) sh_sum[threadIdx.x / kWave] = ws;
-    __syncthreads();
-    const size_t slot = (size_t)r * a.parts + part;
-    int count = 0;
-    if constexpr (TOP)
-        count = collect<DT, NV, kThreads>(w, vm, x_part, a.n_top, a.keys + slot * a.capacity, a.capacity, sh);
-    if (threadIdx.x == 0) {
-        Sum s = sh_sum[0];
-#pragma unroll
-        for (int u = 1; u < kWaves; ++u) s = join(s, sh_sum[u], c2);
-        a.sums[slot] = make_float4(s.m, s.s, s.e, __int_as_float(count));
-    }
-}
-
-template <int DT, int NV, int THREADS, bool TOP, bool ENTROPY>
-__global__ __launch_bounds__(THREADS) void row_whole(RowArgs a) {
-    constexpr int kWaves = THREADS / kWave;
-    __shared__ Sum sh_sum[kWaves];
-    __shared__ TopLds<TOP ? THREADS : kWave> sh;
-    __shared__ uint64_t sh_sel[TOP ? kSelect : 1], sh_out[TOP ? kMaxTop : 1];
+    __shared__ TopLds sh;
+    __shared__ uint64_t sh_sel[kSelect], sh_out[kMaxTop];
     __shared__ RowStats sh_stats;
     pass_over_nans();
-    const int64_t row = a.row0 + blockIdx.x;
-    uint32_t w[NV][4];
-    load_part<DT, NV, THREADS>(static_cast<const typename Elem<DT>::T *>(a.logits) + row * a.ld, a.v, 0, w);
-    const float beta = scale_of(a.inv_temp, row), c2 = beta * kLog2e;
-    float vm[NV];
-    const float tm = vector_maxima<DT, NV>(w, vm);
-    if constexpr (TOP) {
-        sh.largest[threadIdx.x] = order_key(tm) >> 16;
-        form_again(w);
-    }
-    const Sum ws = wave_sums<DT, NV, ENTROPY>(w, tm, c2);
-    if (threadIdx.x % kWave == 0) sh_sum[threadIdx.x / kWave] = ws;
+    const int64_t r = FINISH ? blockIdx.x : blockIdx.x / (uint32_t)a.parts, row_i = a.row0 + r;
+    const int part = FINISH ? 0 : blockIdx.x % (uint32_t)a.parts, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int x0 = part * a.part_width, x1 = x0 + a.part_width < a.v ? x0 + a.part_width : a.v;
+    const auto *row = static_cast<const typename Elem<DT>::T *>(a.logits) + row_i * a.ld;
+    const float beta = scale_of(a.inv_temp, row_i), c2 = beta * kLog2e;
+    const float x_id = FINISH ? token_logit(a, row_i) : 0.0f;
+    int count = 0;
+    Sum mine = {-INFINITY, 0.0f, 0.0f};
+    TopSet<DT, kChunkVectors> top{sh, a.n_top};
+    for_chunks<DT, kChunkVectors, kThreads, true, TOP ? 1 : 2>(row, a.v, x0, x1, [&](uint32_t(&w)[kChunkVectors][4], int x) {
+        float vm[kChunkVectors];
+        add_chunk<DT, kChunkVectors, ENTROPY>(w, c2, mine, vm);
+        if constexpr (TOP) top.add(w, vm, x);
+    });
+    mine = wave_join<ENTROPY>(mine, c2);
+    if (lane == 0) sh_sum[wave] = mine;
+    if constexpr (TOP)
+        count = top.finish(row, x0, x1, FINISH ? sh_sel : a.keys + ((size_t)r * a.parts + part) * a.capacity, FINISH ? kSelect : a.capacity);
     __syncthreads();
-    if (threadIdx.x < kWave) {  // one wave joins the waves' sums
-        float m = -INFINITY;
-        const Sum mine = (int)threadIdx.x < kWaves ? sh_sum[threadIdx.x] : Sum{-INFINITY, 0.0f, 0.0f};
-        m = wave_max(mine.m);
+    if constexpr (!FINISH) {
+        if (threadIdx.x == 0) {
+            Sum s = sh_sum[0];
+#pragma unroll
+            for (int u = 1; u < kWaves; ++u) s = join(s, sh_sum[u], c2);
+            a.sums[(size_t)r * a.parts + part] = make_float4(s.m, s.s, s.e, __int_as_float(count));
+        }
+        return;
+    }
+    if (wave == 0) {  // one wave joins the waves' sums
+        const Sum q = lane < kWaves ? sh_sum[lane] : Sum{-INFINITY, 0.0f, 0.0f};
+        const float m = wave_max(q.m);
         double s = 0.0, e = 0.0;
-        if (mine.s > 0.0f) {
-            const double t = ((double)mine.m - (double)m) * (double)beta, f = exp(t);
-            s = mine.s * f;
-            e = (mine.e * kLn2 + mine.s * fmax(t, -1000.0)) * f;
+        if (q.s > 0.0f) {
+            const double t = ((double)q.m - (double)m) * (double)beta, f = exp(t);
+            s = q.s * f;
+            e = (q.e * kLn2 + q.s * fmax(t, -1000.0)) * f;
         }
         s = wave_sum(s);
         e = ENTROPY ? wave_sum(e) : 0.0;
-        if (threadIdx.x == 0) sh_stats = write_row(a, row, beta, m, s, e);
+        if (lane == 0) sh_stats = write_row(a, row_i, beta, m, s, e, x_id);
     }
-    if constexpr (TOP) {
-        int n = collect<DT, NV, THREADS>(w, vm, 0, a.n_top, sh_sel, kSelect, sh);
-        __syncthreads();
-        n = order_keys<THREADS>(sh_sel, n, a.n_top, sh.largest, &sh.total, sh_out);
-        if ((int)threadIdx.x < a.n_top) write_top(a, row, sh_stats, sh_out, n, threadIdx.x);
+    if constexpr (TOP && FINISH) {
+        count = order_keys(sh_sel, count, a.n_top, sh.largest, &sh.total, sh_out);
+        if ((int)threadIdx.x < a.n_top) write_top(a, row_i, sh_stats, sh_out, count, threadIdx.x);
     }
 }
 
@@ -399,24 +438,15 @@ __device__ __forceinline__ void for_each_key(const RowArgs &a, const float4 *sum
     }
 }
 
-// A row's keys that reach the bound on the k-th, in sh_sel; returns their number (<= kSelect).
-__device__ __forceinline__ int gather_keys(const RowArgs &a, const float4 *sums, const uint64_t *keys, uint64_t *sh_sel, uint32_t *sh_largest,
-                           int *sh_slots, int *sh_total) {
+// A row's keys that reach a bound on its k-th, in sh_sel; returns their number (<= kSelect).  sh_count: the parts'
+// numbers of keys, where there are at most kThreads parts; longest: the largest of them.
+__device__ __forceinline__ int gather_keys(const RowArgs &a, const float4 *sums, const uint64_t *keys, const int *sh_count, int longest,
+                                           uint64_t *sh_sel, uint32_t *sh_largest, int *sh_slots, int *sh_total) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     constexpr int kWaves = kThreads / kWave;
-    // the largest number of keys that a part has, for the layout of runs of 64 keys over the waves
-    int longest = 0;
-    for (int p = lane; p < a.parts; p += kWave) {
-        const int n = __float_as_int(sums[p].w);
-        longest = n > longest ? n : longest;
-    }
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int o = __shfl_xor(longest, d);
-        longest = o > longest ? o : longest;
-    }
     const int runs = (longest + kWave - 1) / kWave;
-    const bool held = a.parts * runs <= kHeld * kWaves;  // all keys in registers, their loads in flight together
+    // few keys: in registers, their loads in flight together
+    const bool held = a.parts <= kThreads && a.parts * runs <= kHeld * kWaves;
     uint64_t mine[kHeld];
     uint32_t most = 0;
     if (held) {
@@ -424,23 +454,27 @@ __device__ __forceinline__ int gather_keys(const RowArgs &a, const float4 *sums,
         for (int u = 0; u < kHeld; ++u) {
             const int c = u * kWaves + wave, p = runs > 0 ? c / runs : a.parts, i = (c - p * runs) * kWave + lane;
             mine[u] = 0;
-            if (p < a.parts && i < __float_as_int(sums[p].w)) mine[u] = keys[(size_t)p * a.capacity + i];
+            if (p < a.parts && i < sh_count[p]) mine[u] = keys[(size_t)p * a.capacity + i];
         }
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
-            const uint32_t o = (uint32_t)(mine[u] >> 48);
+            const uint32_t o = (uint32_t)(mine[u] >> 32);
             most = o > most ? o : most;
         }
     } else {
         for_each_key(a, sums, keys, [&](uint64_t key) {
-            const uint32_t o = (uint32_t)(key >> 48);
+            const uint32_t o = (uint32_t)(key >> 32);
             most = o > most ? o : most;
         });
     }
     sh_largest[threadIdx.x] = most;
     if (threadIdx.x == 0) *sh_total = 0;
     __syncthreads();
-    uint64_t from = (uint64_t)kth_key16<kThreads>(sh_largest, a.n_top) << 48;
+    uint32_t q[kGroups / kWave];
+#pragma unroll
+    for (int u = 0; u < kGroups / kWave; ++u) q[u] = sh_largest[u * kWave + lane];
+    int reach;
+    uint64_t from = (uint64_t)kth_upper(q, a.n_top, reach) << 32;
     from = from > 1 ? from : 1;
     for (;;) {
         auto put = [&](uint64_t key) {
@@ -482,25 +516,44 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
     constexpr int kWaves = kThreads / kWave;
     __shared__ float sh_m[kWaves];
     __shared__ double sh_s[kWaves], sh_e[kWaves];
-    __shared__ uint64_t sh_sel[TOP ? kSelect : 1], sh_out[TOP ? kMaxTop : 1];
-    __shared__ uint32_t sh_largest[TOP ? kThreads : 1];
-    __shared__ int sh_slots[1], sh_total;
+    __shared__ uint64_t sh_sel[kSelect], sh_out[kMaxTop];
+    __shared__ uint32_t sh_largest[kThreads];
+    __shared__ int sh_count[kThreads], sh_longest[kWaves], sh_slots[1], sh_total;
     __shared__ RowStats sh_stats;
     const int64_t r = blockIdx.x, row = a.row0 + r;
     const float4 *sums = a.sums + (size_t)r * a.parts;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const float x_id = token_logit(a, row);
     const double beta = scale_of(a.inv_temp, row);
-    int n = 0;
-    if constexpr (TOP) n = gather_keys(a, sums, a.keys + (size_t)r * a.parts * a.capacity, sh_sel, sh_largest, sh_slots, &sh_total);
-    float m = -INFINITY;
-    for (int p = threadIdx.x; p < a.parts; p += kThreads) m = fmaxf(m, sums[p].x);
+    // each wave's parts relative to its largest value, then the waves relative to the row's
+    float4 q = {-INFINITY, 0.0f, 0.0f, 0.0f};  // the thread's first part
+    if ((int)threadIdx.x < a.parts) q = sums[threadIdx.x];
+    float m = q.x;
+    int longest = __float_as_int(q.w);
+    for (int p = threadIdx.x + kThreads; p < a.parts; p += kThreads) {
+        m = fmaxf(m, sums[p].x);
+        const int n = __float_as_int(sums[p].w);
+        longest = n > longest ? n : longest;
+    }
+    if constexpr (TOP) {
+        sh_count[threadIdx.x] = __float_as_int(q.w);
+        longest = (int)wave_max((float)longest);  // at most 1,088: exact
+        if (lane == 0) sh_longest[wave] = longest;
+    }
     m = wave_max(m);
     if (lane == 0) sh_m[wave] = m;
     __syncthreads();
+    int n = 0;
+    if constexpr (TOP) {
+        longest = sh_longest[0];
+#pragma unroll
+        for (int u = 1; u < kWaves; ++u) longest = sh_longest[u] > longest ? sh_longest[u] : longest;
+        n = gather_keys(a, sums, a.keys + (size_t)r * a.parts * a.capacity, sh_count, longest, sh_sel, sh_largest, sh_slots, &sh_total);
+    }
     m = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
     double s = 0.0, e = 0.0;  // e in natural units
     for (int p = threadIdx.x; p < a.parts; p += kThreads) {
-        const float4 q = sums[p];
+        if (p >= kThreads) q = sums[p];
         if (q.y > 0.0f) {
             const double t = ((double)q.x - (double)m) * beta, f = exp(t);
             s += q.y * f;
@@ -517,56 +570,56 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
     if (threadIdx.x == 0) {
         s = sh_s[0] + sh_s[1] + sh_s[2] + sh_s[3];
         e = sh_e[0] + sh_e[1] + sh_e[2] + sh_e[3];
-        sh_stats = write_row(a, row, beta, m, s, e);
+        sh_stats = write_row(a, row, beta, m, s, e, x_id);
     }
     if constexpr (TOP) {
-        n = order_keys<kThreads>(sh_sel, n, a.n_top, sh_largest, &sh_total, sh_out);
+        n = order_keys(sh_sel, n, a.n_top, sh_largest, &sh_total, sh_out);
         if ((int)threadIdx.x < a.n_top) write_top(a, row, sh_stats, sh_out, n, threadIdx.x);
     }
 }
 
 struct Plan {
-    Split split;   // split.parts == 1: row_whole
-    int64_t rows;  // rows of one launch
+    int parts, part_width;  // of a row; one part: a row's workgroup finishes it
+    int64_t rows;           // of one launch
     size_t sums, total;
 };
 
+// Rows whole, a workgroup each, where the rows fill the GPU or have few chunks; else in as many parts as fill it.
 Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top) {
     Plan p;
-    p.split = split_rows(n_rows, v, dtype);
-    int64_t most = kMaxGrid / p.split.parts;
-    const size_t per_row = (size_t)p.split.parts * part_capacity(n_top) * sizeof(uint64_t);
-    if (p.split.parts > 1 && n_top > 0 && (int64_t)(kMaxKeyBytes / per_row) < most) most = (int64_t)(kMaxKeyBytes / per_row);
+    const int chunk = kChunkVectors * kThreads * elements_per_vector(dtype), chunks = (v + chunk - 1) / chunk;
+    int64_t parts = n_rows > 0 ? (kFullGrid + n_rows - 1) / n_rows : 1;
+    if (parts > chunks) parts = chunks;
+    if (chunks <= kWholeChunks) parts = 1;
+    const int each = (int)((chunks + parts - 1) / parts);
+    p.part_width = each * chunk;
+    p.parts = (chunks + each - 1) / each;
+    int64_t most = kMaxGrid / p.parts;
+    const size_t per_row = (size_t)p.parts * part_capacity(n_top) * sizeof(uint64_t);
+    if (p.parts > 1 && n_top > 0 && (int64_t)(kMaxKeyBytes / per_row) < most) most = (int64_t)(kMaxKeyBytes / per_row);
     if (most < 1) most = 1;
     const int64_t groups = (n_rows + most - 1) / most;
     p.rows = groups == 0 ? 0 : (n_rows + groups - 1) / groups;
-    p.sums = p.split.parts > 1 ? round256((size_t)p.rows * p.split.parts * sizeof(float4)) : 0;
-    p.total = p.sums + (p.split.parts > 1 && n_top > 0 ? (size_t)p.rows * per_row : 0);
+    p.sums = p.parts > 1 ? round256((size_t)p.rows * p.parts * sizeof(float4)) : 0;
+    p.total = p.sums + (p.parts > 1 && n_top > 0 ? (size_t)p.rows * per_row : 0);
     return p;
 }
 
-template <int DT, int NV, int THREADS, bool TOP, bool ENTROPY>
+template <int DT, bool TOP, bool ENTROPY>
 void launch_rows(const RowArgs &a, int64_t n, hipStream_t stream) {
-    if (a.parts == 1) row_whole<DT, NV, THREADS, TOP, ENTROPY><<<(unsigned)n, THREADS, 0, stream>>>(a);
-    else if constexpr (THREADS == kThreads) row_parts<DT, NV, TOP, ENTROPY><<<(unsigned)(n * a.parts), THREADS, 0, stream>>>(a);
-}
-
-template <int DT, int NV, int THREADS>
-void launch_rows(const RowArgs &a, int64_t n, hipStream_t stream) {
-    if (a.n_top > 0) {
-        if (a.entropy != nullptr) launch_rows<DT, NV, THREADS, true, true>(a, n, stream);
-        else launch_rows<DT, NV, THREADS, true, false>(a, n, stream);
-    } else {
-        if (a.entropy != nullptr) launch_rows<DT, NV, THREADS, false, true>(a, n, stream);
-        else launch_rows<DT, NV, THREADS, false, false>(a, n, stream);
-    }
+    if (a.parts == 1) row_stream<DT, TOP, ENTROPY, true><<<(unsigned)n, kThreads, 0, stream>>>(a);
+    else row_stream<DT, TOP, ENTROPY, false><<<(unsigned)(n * a.parts), kThreads, 0, stream>>>(a);
 }
 
 template <int DT>
-void launch_rows(const RowArgs &a, const Split &s, int64_t n, hipStream_t stream) {
-    if (s.threads == kWholeThreads) launch_rows<DT, kWideVectors, kWholeThreads>(a, n, stream);
-    else if (s.vectors == kWideVectors) launch_rows<DT, kWideVectors, kThreads>(a, n, stream);
-    else launch_rows<DT, kNarrowVectors, kThreads>(a, n, stream);
+void launch_rows(const RowArgs &a, int64_t n, hipStream_t stream) {
+    if (a.n_top > 0) {
+        if (a.entropy != nullptr) launch_rows<DT, true, true>(a, n, stream);
+        else launch_rows<DT, true, false>(a, n, stream);
+    } else {
+        if (a.entropy != nullptr) launch_rows<DT, false, true>(a, n, stream);
+        else launch_rows<DT, false, false>(a, n, stream);
+    }
 }
 
 // ---------------------------------------------------------------- gradient
@@ -586,9 +639,9 @@ struct GradArgs {
 template <int DT, bool ENTROPY>
 __global__ __launch_bounds__(kThreads) void logprob_grad(GradArgs a) {
     using T = typename Elem<DT>::T;
-    constexpr int kPer = Elem<DT>::kPer;
+    constexpr int kPer = Elem<DT>::kPer, kPart = kGradVectors * kThreads * kPer;
     const int64_t r = a.row0 + blockIdx.x / (uint32_t)a.parts;
-    const int x_part = (int)(blockIdx.x % (uint32_t)a.parts) * kGradVectors * kThreads * kPer;
+    const int x_part = (int)(blockIdx.x % (uint32_t)a.parts) * kPart;
     const T *row = static_cast<const T *>(a.logits) + r * a.ld;
     T *out = static_cast<T *>(a.out) + r * a.out_ld;
     const int32_t id = a.ids == nullptr ? -1 : a.ids[r];
@@ -596,10 +649,9 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(GradArgs a) {
     const float g = given && a.g != nullptr ? a.g[r] : 0.0f;
     const float h = ENTROPY ? a.h[r] : 0.0f;
     const float m = a.stats[2 * r], log_sum = a.stats[2 * r + 1];
-    float d[kPer];
+    const int x_end = x_part + kPart < a.v ? x_part + kPart : a.v;
     if ((g == 0.0f && h == 0.0f) || m == -INFINITY) {
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) d[j] = 0.0f;
+        const float d[kPer] = {};
 #pragma unroll
         for (int i = 0; i < kGradVectors; ++i) store_vector<DT>(out, vector_at<DT, kThreads>(x_part, i), a.v, d);
         return;
@@ -608,30 +660,31 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(GradArgs a) {
     const float ent = ENTROPY ? a.entropy[r] : 0.0f;
     // d = p (first + second t), t = lp / ln 2 held above -200 (p is 0 there); NaN statistics make it NaN
     const float first = -beta * (g + h * ent) + (log_sum - log_sum), second = ENTROPY ? -beta * h * (float)kLn2 : 0.0f;
-    uint32_t w[kGradVectors][4];
-    load_part<DT, kGradVectors, kThreads>(row, a.v, x_part, w);
+    for_chunks<DT, kGradVectors, kThreads, true, 1>(row, a.v, x_part, x_end, [&](uint32_t(&w)[kGradVectors][4], int x_chunk) {
 #pragma unroll
-    for (int i = 0; i < kGradVectors; ++i) {
-        const int x = vector_at<DT, kThreads>(x_part, i);
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const float t = fmaxf((value<DT>(w[i], j) - m) * c2 - l2, kLowest);
-            const float p = __builtin_amdgcn_exp2f(t);
-            d[j] = p * (ENTROPY ? fmaf(second, t, first) : first);
-        }
-        if (given && id >= x && id < x + kPer) {  // the token itself: 1 - p from its log probability
+        for (int i = 0; i < kGradVectors; ++i) {
+            const int x = vector_at<DT, kThreads>(x_chunk, i);
+            float d[kPer];
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
-                if (id == x + j) {
-                    const float y = value<DT>(w[i], j);
-                    const float lp = y == y ? (y - m) * beta - log_sum : -INFINITY;
-                    const float rest = -expm1f(lp);
-                    d[j] = beta * (g * rest - (ENTROPY ? h * expf(lp) * (fmaxf(lp, kLowest) + ent) : 0.0f)) + (log_sum - log_sum);
+                const float t = fmaxf((value<DT>(w[i], j) - m) * c2 - l2, kLowest);
+                const float p = __builtin_amdgcn_exp2f(t);
+                d[j] = p * (ENTROPY ? fmaf(second, t, first) : first);
+            }
+            if (given && id >= x && id < x + kPer) {  // the token itself: 1 - p from its log probability
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    if (id == x + j) {
+                        const float y = value<DT>(w[i], j);
+                        const float lp = y == y ? (y - m) * beta - log_sum : -INFINITY;
+                        const float rest = -expm1f(lp);
+                        d[j] = beta * (g * rest - (ENTROPY ? h * expf(lp) * (fmaxf(lp, kLowest) + ent) : 0.0f)) + (log_sum - log_sum);
+                    }
                 }
             }
+            store_vector<DT>(out, x, a.v, d);
         }
-        store_vector<DT>(out, x, a.v, d);
-    }
+    });
 }
 
 template <int DT>
@@ -653,7 +706,8 @@ int launch_logprobs(const LogprobsArgs &l, void *workspace, size_t workspace_byt
     a.ld = l.ld;
     a.v = l.v;
     a.dtype = l.dtype;
-    a.parts = p.split.parts;
+    a.parts = p.parts;
+    a.part_width = p.part_width;
     a.n_top = l.n_top;
     a.capacity = part_capacity(l.n_top);
     a.inv_temp = l.inv_temp;
@@ -669,9 +723,9 @@ int launch_logprobs(const LogprobsArgs &l, void *workspace, size_t workspace_byt
     for (int64_t row0 = 0; row0 < l.n_rows; row0 += p.rows) {
         const int64_t n = l.n_rows - row0 < p.rows ? l.n_rows - row0 : p.rows;
         a.row0 = row0;
-        if (l.dtype == TT_BF16) launch_rows<TT_BF16>(a, p.split, n, stream);
-        else if (l.dtype == TT_F16) launch_rows<TT_F16>(a, p.split, n, stream);
-        else launch_rows<TT_F32>(a, p.split, n, stream);
+        if (l.dtype == TT_BF16) launch_rows<TT_BF16>(a, n, stream);
+        else if (l.dtype == TT_F16) launch_rows<TT_F16>(a, n, stream);
+        else launch_rows<TT_F32>(a, n, stream);
         if (hipGetLastError() != hipSuccess) return TT_ELAUNCH;
         if (a.parts == 1) continue;
         if (l.n_top > 0) row_finish<true><<<(unsigned)n, kThreads, 0, stream>>>(a);

@@ -12,14 +12,23 @@ namespace tt {
 namespace rows {
 
 constexpr int kWave = 64;
-constexpr int kThreads = 256;        // threads of a workgroup that takes a part of a row, or a short row
-constexpr int kWholeThreads = 1024;  // and of one that takes a longer row whole
+constexpr int kThreads = 256;  // of a workgroup, unless said otherwise
 constexpr float kLog2e = 0x1.715476p+0f;      // log2(e) rounded to fp32
 constexpr double kLn2 = 0.693147180559945309;  // ln 2
 
 // 16 bytes at an address aligned to an element only: rows of an odd stride start anywhere, and
 // gfx950's 16-byte global accesses take any address.
 typedef unsigned int u4u __attribute__((ext_vector_type(4), aligned(2)));
+
+// A load known to the compiler as one from global memory, where a pointer's origin does not tell it (a flat
+// load's wait would wait for every load in flight).
+// LAST: this is the only or the last reading (the non-temporal hint keeps such lines from displacing others).
+template <bool LAST>
+__device__ __forceinline__ u4u load_global(const void *p) {
+    const auto *g = reinterpret_cast<const __attribute__((address_space(1))) u4u *>(reinterpret_cast<uintptr_t>(p));
+    if constexpr (LAST) return __builtin_nontemporal_load(g);
+    else return *g;
+}
 
 template <int DT>
 struct Elem;
@@ -84,38 +93,6 @@ __device__ __forceinline__ int vector_at(int x_part, int i) {
     return x_part + (i * THREADS + (int)threadIdx.x) * Elem<DT>::kPer;
 }
 
-// A part of a row: NV vectors of 16 bytes a thread, each load instruction of a wave covering 1 KB
-// of the row; minus infinity past v.  Nothing outside [0, v) is read: a vector that ends past v is
-// replaced by the row's last whole one (a valid address) and then formed element by element.
-template <int DT, int NV, int THREADS>
-__device__ __forceinline__ void load_part(const typename Elem<DT>::T *row, int v, int x_part, uint32_t (&w)[NV][4]) {
-    constexpr int kPer = Elem<DT>::kPer;
-    if (x_part + NV * THREADS * kPer <= v) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const u4u t = *reinterpret_cast<const u4u *>(row + vector_at<DT, THREADS>(x_part, i));
-            w[i][0] = t.x; w[i][1] = t.y; w[i][2] = t.z; w[i][3] = t.w;
-        }
-        return;
-    }
-    if (v >= kPer) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int x = vector_at<DT, THREADS>(x_part, i), last = v - kPer;
-            const u4u t = *reinterpret_cast<const u4u *>(row + (x < last ? x : last));
-            w[i][0] = t.x; w[i][1] = t.y; w[i][2] = t.z; w[i][3] = t.w;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int x = vector_at<DT, THREADS>(x_part, i);
-        if (x + kPer > v) {
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) set_bits<DT>(w[i], j, x + j < v ? (uint32_t)row[x + j] : Elem<DT>::kNone);
-        }
-    }
-}
-
 // An fp32 value rounded to the row's type, to nearest even.
 template <int DT>
 __device__ __forceinline__ uint32_t encode(float x) {
@@ -156,22 +133,44 @@ __device__ __forceinline__ void pass_over_nans() {
     __builtin_amdgcn_s_setreg(kModeIeee, 0);
 }
 
+// x of other lanes by a DPP control; lanes without a source get `none`.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float dpp(float x, float none) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(x), CTRL, ROW_MASK, 0xF, false));
+}
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ double dpp(double x, double none) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x), o = __builtin_bit_cast(uint64_t, none);
+    const uint32_t lo = __builtin_amdgcn_update_dpp((uint32_t)o, (uint32_t)b, CTRL, ROW_MASK, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp((uint32_t)(o >> 32), (uint32_t)(b >> 32), CTRL, ROW_MASK, 0xF, false);
+    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+__device__ __forceinline__ float last_lane(float x) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), kWave - 1)); }
+__device__ __forceinline__ double last_lane(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)b, kWave - 1), hi = __builtin_amdgcn_readlane((uint32_t)(b >> 32), kWave - 1);
+    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+
+// The wave's maximum and sum, the same in every lane (prefixes within rows of 16 lanes, then row broadcasts).
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) x = fmaxf(x, __shfl_xor(x, d));
-    return x;
+    x = fmaxf(x, dpp<0x111, 0xF>(x, -INFINITY));
+    x = fmaxf(x, dpp<0x112, 0xF>(x, -INFINITY));
+    x = fmaxf(x, dpp<0x114, 0xF>(x, -INFINITY));
+    x = fmaxf(x, dpp<0x118, 0xF>(x, -INFINITY));
+    x = fmaxf(x, dpp<0x142, 0xA>(x, -INFINITY));
+    x = fmaxf(x, dpp<0x143, 0xC>(x, -INFINITY));
+    return last_lane(x);
 }
-
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d);
-    return x;
-}
-
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d);
-    return x;
+template <typename F>
+__device__ __forceinline__ F wave_sum(F x) {
+    x += dpp<0x111, 0xF>(x, F(0));
+    x += dpp<0x112, 0xF>(x, F(0));
+    x += dpp<0x114, 0xF>(x, F(0));
+    x += dpp<0x118, 0xF>(x, F(0));
+    x += dpp<0x142, 0xA>(x, F(0));
+    x += dpp<0x143, 0xC>(x, F(0));
+    return last_lane(x);
 }
 
 // Unsigned keys in the order of the values (-0 as +0, minus infinity lowest, no NaN).
@@ -193,13 +192,65 @@ struct Sum {
 // Scaled exponents are held above this bound: 2^-200 is 0 in fp32, and 0 * -200 is 0 (0 * -inf is not).
 constexpr float kLowest = -200.0f;
 
-// The sums of a wave's vectors, the same in every lane; a wave without a finite logit has m = -inf, s = e = 0
-// (exponents that are NaN, from NaN logits or from -inf - -inf, count 0).
-template <int DT, int NV, bool ENTROPY>
-__device__ __forceinline__ Sum wave_sums(const uint32_t (&w)[NV][4], float thread_max, float c2) {
+// A chunk of a row: NV vectors of 16 bytes a thread.  The loads are unconditional, so that a chunk's loads
+// stay in flight while the one before is worked on: a vector that would end past v is taken from the
+// row's end instead (v >= kPer), and put right by fix_chunk once it has arrived.
+template <int DT, int NV, int THREADS, bool LAST>
+__device__ __forceinline__ void load_chunk(const typename Elem<DT>::T *row, int v, int x_chunk, uint32_t (&w)[NV][4]) {
+    const int last = v - Elem<DT>::kPer;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int x = vector_at<DT, THREADS>(x_chunk, i);
+        const u4u t = load_global<LAST>(row + (x < last ? x : last));
+        w[i][0] = t.x; w[i][1] = t.y; w[i][2] = t.z; w[i][3] = t.w;
+    }
+}
+
+// Minus infinity past v: the vectors that load_chunk took from the row's end lose the elements that are
+// other vectors', the rest move to the front.
+template <int DT, int NV, int THREADS>
+__device__ __forceinline__ void fix_chunk(int v, int x_chunk, uint32_t (&w)[NV][4]) {
     constexpr int kPer = Elem<DT>::kPer;
-    const float m = wave_max(thread_max);
-    float s[2] = {0.0f, 0.0f}, e[2] = {0.0f, 0.0f};
+    constexpr uint32_t kNone = Elem<DT>::kNone, kNones = DT == TT_F32 ? kNone : kNone * 0x10001u;
+    if (x_chunk + NV * THREADS * kPer <= v) return;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int over = vector_at<DT, THREADS>(x_chunk, i) - (v - kPer);  // elements to drop
+        if (over <= 0) continue;
+        int words = over;
+        if constexpr (DT != TT_F32) {
+            if (over & 1) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) w[i][q] = (w[i][q] >> 16) | ((q < 3 ? w[i][q + 1 < 4 ? q + 1 : 3] : kNones) << 16);
+            }
+            words = over >> 1;
+        }
+#pragma unroll
+        for (int step = 1; step <= 2; step <<= 1) {
+            if (words & step) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) w[i][q] = q + step < 4 ? w[i][q + step < 4 ? q + step : 3] : kNones;
+            }
+        }
+        if (words >= 4) w[i][0] = w[i][1] = w[i][2] = w[i][3] = kNones;
+    }
+}
+
+// A thread's sums with its vectors of one more chunk; vm: the largest values of these.  NaN logits and
+// those of a thread without a finite one count 0 (their exponents are NaN: held at kLowest, or clamped).
+template <int DT, int NV, bool ENTROPY>
+__device__ __forceinline__ void add_chunk(const uint32_t (&w)[NV][4], float c2, Sum &a, float (&vm)[NV]) {
+    constexpr int kPer = Elem<DT>::kPer;
+    float m = a.m;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        vm[i] = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) vm[i] = fmaxf(vm[i], value<DT>(w[i], j));
+        m = fmaxf(m, vm[i]);
+    }
+    const float d = fmaxf((a.m - m) * c2, kLowest), f = __builtin_amdgcn_exp2f(d);
+    float s[2] = {a.s * f, 0.0f}, e[2] = {ENTROPY ? fmaf(a.s, d, a.e) * f : 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
 #pragma unroll
@@ -215,11 +266,51 @@ __device__ __forceinline__ Sum wave_sums(const uint32_t (&w)[NV][4], float threa
             }
         }
     }
+    a.m = m;
+    a.s = s[0] + s[1];
+    a.e = e[0] + e[1];
+}
+
+// The wave's sums from its threads', the same in every lane.
+template <bool ENTROPY>
+__device__ __forceinline__ Sum wave_join(const Sum &a, float c2) {
     Sum r;
-    r.m = m;
-    r.s = wave_sum(s[0] + s[1]);
-    r.e = ENTROPY ? wave_sum(e[0] + e[1]) : 0.0f;
+    r.m = wave_max(a.m);
+    const float d = fmaxf((a.m - r.m) * c2, kLowest), f = __builtin_amdgcn_exp2f(d);
+    r.s = wave_sum(a.s * f);
+    r.e = ENTROPY ? wave_sum(fmaf(a.s, d, a.e) * f) : 0.0f;
     return r;
+}
+
+// What rows shorter than a vector are loaded from (their elements are then read one by one).
+static __device__ const uint32_t kNoRow[4] = {};
+
+// Calls f(vectors, first element) for every chunk of a row's elements x0 .. x1 - 1 (x0 a multiple of the chunk),
+// minus infinity past v, while the next chunk's loads are in flight.
+template <int DT, int NV, int THREADS, bool LAST, int UNROLL, typename F>
+__device__ __forceinline__ void for_chunks(const typename Elem<DT>::T *row, int v, int x0, int x1, F f) {
+    using T = typename Elem<DT>::T;
+    constexpr int kPer = Elem<DT>::kPer, kChunk = NV * THREADS * kPer;
+    const bool tiny = v < kPer;
+    const T *from = tiny ? reinterpret_cast<const T *>(kNoRow) : row;
+    const int width = tiny ? kPer : v;
+    uint32_t w[NV][4];
+    load_chunk<DT, NV, THREADS, LAST>(from, width, x0, w);
+    if (tiny) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) set_bits<DT>(w[0], j, j < v ? (uint32_t)row[j] : Elem<DT>::kNone);
+    }
+#pragma unroll UNROLL
+    for (int x = x0; x < x1; x += kChunk) {
+        uint32_t next[NV][4];
+        load_chunk<DT, NV, THREADS, LAST>(from, width, x + kChunk < x1 ? x + kChunk : x0, next);
+        fix_chunk<DT, NV, THREADS>(width, x, w);
+        f(w, x);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[i][q] = next[i][q];
+    }
 }
 
 // The union of two sets' sums.
@@ -233,32 +324,10 @@ __device__ __forceinline__ Sum join(const Sum &a, const Sum &b, float c2) {
     return r;
 }
 
-// The kernels' choice of threads and vectors a thread.  A row is taken whole by one workgroup up to
-// kThreads * kWideVectors vectors; longer ones by parts of that size, or smaller ones where they
-// would not fill the GPU.
-constexpr int kWideVectors = 8;
-constexpr int kNarrowVectors = 2;
-constexpr int kFullGrid = 1024;  // workgroups that fill the GPU: four a compute unit
+constexpr int kFullGrid = 1024;  // workgroups of kThreads that fill the GPU: four a compute unit
 
 inline int elements_per_vector(int dtype) { return dtype == TT_F32 ? 4 : 8; }
 inline int element_bytes(int dtype) { return dtype == TT_F32 ? 4 : 2; }
-
-struct Split {
-    int threads, vectors;  // of a workgroup, of a thread
-    int parts;             // of a row
-};
-
-inline Split split_rows(int64_t n_rows, int32_t v, int dtype) {
-    const int64_t narrow = (int64_t)kNarrowVectors * kThreads * elements_per_vector(dtype);
-    const int64_t wide = (int64_t)kWideVectors * kThreads * elements_per_vector(dtype);
-    const int64_t whole = (int64_t)kWideVectors * kWholeThreads * elements_per_vector(dtype);
-    if (v <= narrow) return {kThreads, kNarrowVectors, 1};
-    if (v <= wide) return {kThreads, kWideVectors, 1};
-    if (v <= whole) return {kWholeThreads, kWideVectors, 1};
-    const int64_t parts = (v + wide - 1) / wide;
-    if (n_rows * parts >= kFullGrid) return {kThreads, kWideVectors, (int)parts};
-    return {kThreads, kNarrowVectors, (int)((v + narrow - 1) / narrow)};
-}
 
 inline size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 

@@ -67,15 +67,18 @@ def test_backward_refusals():
 
 def test_distill_refusals():
     for bad in (dict(k=0), dict(k=-1), dict(ids=None), dict(lp=None), dict(loss=None), dict(g=None), dict(n_map=-1), dict(out_ld=99),
-                dict(out=2 * PTR + 1), dict(out=PTR + 2), dict(out=PTR, out_ld=101), dict(ws=PTR + 8)):
+                dict(out=2 * PTR + 1), dict(out=PTR + 2), dict(out=PTR, out_ld=101)):
         assert distill(**bad) == tt.TT_EINVAL, bad
     assert distill(k=129) == tt.TT_EUNSUPPORTED
     assert distill(v=(1 << 23) + 1, ld=1 << 24, out_ld=1 << 24) == tt.TT_EUNSUPPORTED
     n = ctypes.c_size_t(0)
+    assert L.tt_distill_workspace_size(2, 100, 0, 3, 1, ctypes.byref(n)) == tt.TT_OK and n.value == 0  # a row whole in a workgroup
     for grad, out in ((1, 2 * PTR), (0, None)):
-        assert L.tt_distill_workspace_size(2, 100, 0, 3, grad, ctypes.byref(n)) == tt.TT_OK and n.value > 0
-        assert distill(out=out, nbytes=n.value - 1) == tt.TT_EWORKSPACE
-    assert distill(ws=None) == tt.TT_EWORKSPACE
+        assert L.tt_distill_workspace_size(2, 100000, 0, 3, grad, ctypes.byref(n)) == tt.TT_OK and n.value > 0
+        split = dict(v=100000, ld=100000, out=out, out_ld=100000)
+        assert distill(nbytes=n.value - 1, **split) == tt.TT_EWORKSPACE
+        assert distill(ws=None, **split) == tt.TT_EWORKSPACE
+        assert distill(ws=PTR + 8, **split) == tt.TT_EINVAL
     for bad in ((-1, 100, 0, 3, 0), (2, 0, 0, 3, 0), (2, 100, 5, 3, 0), (2, 100, 0, 0, 0)):
         assert L.tt_distill_workspace_size(*bad, ctypes.byref(n)) == tt.TT_EINVAL
     assert L.tt_distill_workspace_size(2, 100, 0, 3, 0, None) == tt.TT_EINVAL
