@@ -101,6 +101,7 @@ __device__ __forceinline__ uint32_t encode(float x) {
     else return __builtin_bit_cast(unsigned short, (__bf16)x);
 }
 
+// The non-temporal hint: written once and not read here, such lines would displace the logits that will be.
 template <int DT>
 __device__ __forceinline__ void store_vector(typename Elem<DT>::T *row, int x, int v, const float (&d)[Elem<DT>::kPer]) {
     constexpr int kPer = Elem<DT>::kPer;
@@ -113,7 +114,7 @@ __device__ __forceinline__ void store_vector(typename Elem<DT>::T *row, int x, i
     if (x + kPer <= v) {
         u4u t;
         t.x = w[0]; t.y = w[1]; t.z = w[2]; t.w = w[3];
-        *reinterpret_cast<u4u *>(row + x) = t;
+        __builtin_nontemporal_store(t, reinterpret_cast<u4u *>(row + x));
     } else {
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
@@ -303,7 +304,7 @@ __device__ __forceinline__ void for_chunks(const typename Elem<DT>::T *row, int 
 #pragma unroll UNROLL
     for (int x = x0; x < x1; x += kChunk) {
         uint32_t next[NV][4];
-        load_chunk<DT, NV, THREADS, LAST>(from, width, x + kChunk < x1 ? x + kChunk : x0, next);
+        load_chunk<DT, NV, THREADS, LAST>(from, width, x + kChunk < x1 ? x + kChunk : width, next);  // past the end: one line
         fix_chunk<DT, NV, THREADS>(width, x, w);
         f(w, x);
 #pragma unroll
