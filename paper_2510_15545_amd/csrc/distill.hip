@@ -233,21 +233,16 @@ __host__ __device__ __forceinline__ int bitmap_words(int width) {
     return (width + kChunk - 1) / kChunk * (kChunk / 32);
 }
 
-// Gradients of the unlisted tokens of elements x0 .. x1 - 1; zeros, without a reading, where the factor is 0.
-template <int DT, int NV, int THREADS>
-__device__ __forceinline__ void write_grad(const ListArgs &a, int64_t row_i, int x0, int x1, const RowGrad &q) {
+// Gradients of the unlisted tokens of elements x0 .. x1 - 1, from what get() returns (called once the first loads
+// are in flight); zeros where the factor is 0.
+template <int DT, int NV, int THREADS, typename G>
+__device__ __forceinline__ void write_grad(const ListArgs &a, int64_t row_i, int x0, int x1, G get) {
     using T = typename Elem<DT>::T;
-    constexpr int kPer = Elem<DT>::kPer, kChunk = NV * THREADS * kPer;
+    constexpr int kPer = Elem<DT>::kPer;
     const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
     T *out = static_cast<T *>(a.out) + row_i * a.out_ld;
-    if (q.factor == 0.0f) {
-        const float d[kPer] = {};
-        for (int x = x0; x < x1; x += kChunk)
-#pragma unroll
-            for (int i = 0; i < NV; ++i) store_vector<DT>(out, vector_at<DT, THREADS>(x, i), a.v, d);
-        return;
-    }
-    for_chunks<DT, NV, THREADS, true, 1>(row, a.v, x0, x1, [&](uint32_t(&w)[NV][4], int x) {
+    RowGrad q;
+    for_chunks<DT, NV, THREADS, true, 1>(row, a.v, x0, x1, [&] { q = get(); }, [&](uint32_t(&w)[NV][4], int x) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float d[kPer];
@@ -274,48 +269,54 @@ __global__ __launch_bounds__(THREADS) void list_whole(ListArgs a) {
     const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const float c2 = scale_of(a.inv_temp, row_i) * kLog2e;
-    for (int i = threadIdx.x; i < bitmap_words<DT, NV, THREADS>(a.v); i += THREADS) sh_bits[i] = 0;
-    __syncthreads();
     List list;
-    if (wave == 0) {
-        list = read_list(a, row_i);
-#pragma unroll
-        for (int u = 0; u < kSlots; ++u)
-            if (list.id[u] >= 0) atomicOr(&sh_bits[list.id[u] / 32], 1u << (list.id[u] % 32));
-    }
-    __syncthreads();
     Sum mine = {-INFINITY, 0.0f, 0.0f};
-    for_chunks<DT, NV, THREADS, !GRAD, 1>(row, a.v, 0, a.v, [&](uint32_t(&w)[NV][4], int x) {
+    auto read = [&] {
+        for (int i = threadIdx.x; i < bitmap_words<DT, NV, THREADS>(a.v); i += THREADS) sh_bits[i] = 0;
+        __syncthreads();
+        if (wave == 0) {
+            list = read_list(a, row_i);
+#pragma unroll
+            for (int u = 0; u < kSlots; ++u)
+                if (list.id[u] >= 0) atomicOr(&sh_bits[list.id[u] / 32], 1u << (list.id[u] % 32));
+        }
+        __syncthreads();
+    };
+    for_chunks<DT, NV, THREADS, !GRAD, 1>(row, a.v, 0, a.v, read, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         take_out<DT, NV, THREADS>(w, sh_bits, x, 0);
         add_chunk<DT, NV, false>(w, c2, mine, vm);
     });
     mine = wave_join<false>(mine, c2);
     if (lane == 0) sh_sum[wave] = mine;
-    __syncthreads();
-    if (wave == 0) {
-        const Sum q = lane < kWaves ? sh_sum[lane] : Sum{-INFINITY, 0.0f, 0.0f};
-        const float m_out = wave_max(q.m);
-        double s_out = 0.0, grad[kSlots];
-        if (q.s > 0.0f) s_out = q.s * exp(((double)q.m - (double)m_out) * (double)scale_of(a.inv_temp, row_i));
-        s_out = wave_sum(s_out);
-        const RowGrad r = finish_row<GRAD>(a, row_i, list, m_out, s_out, grad);
-        if constexpr (GRAD) {
-#pragma unroll
-            for (int u = 0; u < kSlots; ++u) sh_entry[u * kWave + lane] = {list.id[u], (float)grad[u]};
-            if (lane == 0) sh_grad = r;
-        }
-    }
-    if constexpr (GRAD) {
+    auto finish = [&] {
         __syncthreads();
-        const RowGrad q = sh_grad;
-        write_grad<DT, NV, THREADS>(a, row_i, 0, a.v, q);
+        if (wave == 0) {
+            const Sum q = lane < kWaves ? sh_sum[lane] : Sum{-INFINITY, 0.0f, 0.0f};
+            const float m_out = wave_max(q.m);
+            double s_out = 0.0, grad[kSlots];
+            if (q.s > 0.0f) s_out = q.s * exp(((double)q.m - (double)m_out) * (double)scale_of(a.inv_temp, row_i));
+            s_out = wave_sum(s_out);
+            const RowGrad r = finish_row<GRAD>(a, row_i, list, m_out, s_out, grad);
+            if constexpr (GRAD) {
+#pragma unroll
+                for (int u = 0; u < kSlots; ++u) sh_entry[u * kWave + lane] = {list.id[u], (float)grad[u]};
+                if (lane == 0) sh_grad = r;
+            }
+        }
+        if constexpr (GRAD) __syncthreads();
+        return sh_grad;
+    };
+    if constexpr (GRAD) {
+        write_grad<DT, NV, THREADS>(a, row_i, 0, a.v, finish);
         // the listed tokens over what was just written: after the workgroup's stores
         __syncthreads();
         if ((int)threadIdx.x < a.n_top) {
             const Entry e = sh_entry[threadIdx.x];
             if (e.id >= 0) (static_cast<T *>(a.out) + row_i * a.out_ld)[e.id] = (T)encode<DT>(e.grad);
         }
+    } else {
+        finish();
     }
 }
 
@@ -331,15 +332,17 @@ __global__ __launch_bounds__(kThreads) void list_parts(ListArgs a) {
     const int x1 = x0 + a.part_width < a.v ? x0 + a.part_width : a.v;
     const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
     const float c2 = scale_of(a.inv_temp, row_i) * kLog2e;
-    for (int i = threadIdx.x; i < bitmap_words<DT, NV, kThreads>(x1 - x0); i += kThreads) sh_bits[i] = 0;
-    __syncthreads();
-    if ((int)threadIdx.x < a.n_top) {
-        const int at = entry_id(a, row_i, threadIdx.x, a.logprobs[row_i * a.n_top + threadIdx.x]) - x0;
-        if (at >= 0 && at < x1 - x0) atomicOr(&sh_bits[at / 32], 1u << (at % 32));
-    }
-    __syncthreads();
+    auto read = [&] {
+        for (int i = threadIdx.x; i < bitmap_words<DT, NV, kThreads>(x1 - x0); i += kThreads) sh_bits[i] = 0;
+        __syncthreads();
+        if ((int)threadIdx.x < a.n_top) {
+            const int at = entry_id(a, row_i, threadIdx.x, a.logprobs[row_i * a.n_top + threadIdx.x]) - x0;
+            if (at >= 0 && at < x1 - x0) atomicOr(&sh_bits[at / 32], 1u << (at % 32));
+        }
+        __syncthreads();
+    };
     Sum mine = {-INFINITY, 0.0f, 0.0f};
-    for_chunks<DT, NV, kThreads, false, 1>(row, a.v, x0, x1, [&](uint32_t(&w)[NV][4], int x) {
+    for_chunks<DT, NV, kThreads, false, 1>(row, a.v, x0, x1, read, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         take_out<DT, NV, kThreads>(w, sh_bits, x, x0);
         add_chunk<DT, NV, false>(w, c2, mine, vm);
@@ -389,7 +392,7 @@ __global__ __launch_bounds__(kThreads) void list_grad(ListArgs a, int parts) {
     const int x0 = (int)(blockIdx.x % (uint32_t)parts) * kPart, x1 = x0 + kPart < a.v ? x0 + kPart : a.v;
     Entry mine = {-1, 0.0f};
     if ((int)threadIdx.x < a.n_top) mine = a.entries[(size_t)r * a.n_top + threadIdx.x];
-    write_grad<DT, kChunkVectors, kThreads>(a, row_i, x0, x1, a.row_grad[r]);
+    write_grad<DT, kChunkVectors, kThreads>(a, row_i, x0, x1, [&] { return a.row_grad[r]; });
     // the listed tokens over what was just written: after the workgroup's stores
     __syncthreads();
     if (mine.id >= x0 && mine.id < x1) (static_cast<T *>(a.out) + row_i * a.out_ld)[mine.id] = (T)encode<DT>(mine.grad);

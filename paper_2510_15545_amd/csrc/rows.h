@@ -287,9 +287,9 @@ __device__ __forceinline__ Sum wave_join(const Sum &a, float c2) {
 static __device__ const uint32_t kNoRow[4] = {};
 
 // Calls f(vectors, first element) for every chunk of a row's elements x0 .. x1 - 1 (x0 a multiple of the chunk),
-// minus infinity past v, while the next chunk's loads are in flight.
-template <int DT, int NV, int THREADS, bool LAST, int UNROLL, typename F>
-__device__ __forceinline__ void for_chunks(const typename Elem<DT>::T *row, int v, int x0, int x1, F f) {
+// minus infinity past v, while the next chunk's loads are in flight; before() once the first chunk's are.
+template <int DT, int NV, int THREADS, bool LAST, int UNROLL, typename B, typename F>
+__device__ __forceinline__ void for_chunks(const typename Elem<DT>::T *row, int v, int x0, int x1, B before, F f) {
     using T = typename Elem<DT>::T;
     constexpr int kPer = Elem<DT>::kPer, kChunk = NV * THREADS * kPer;
     const bool tiny = v < kPer;
@@ -301,6 +301,7 @@ __device__ __forceinline__ void for_chunks(const typename Elem<DT>::T *row, int 
 #pragma unroll
         for (int j = 0; j < kPer; ++j) set_bits<DT>(w[0], j, j < v ? (uint32_t)row[j] : Elem<DT>::kNone);
     }
+    before();
 #pragma unroll UNROLL
     for (int x = x0; x < x1; x += kChunk) {
         uint32_t next[NV][4];
