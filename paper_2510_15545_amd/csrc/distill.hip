@@ -32,10 +32,12 @@ constexpr int64_t kMaxGrid = int64_t(1) << 18;
 constexpr int kChunkVectors = 4;
 constexpr int kMaxBits = 1 << 18;  // tokens of a bitmap: 32 KB
 
-// What the gradient of a row's unlisted tokens needs: factor * 2^((x - m) c2 - shift).
+// What the gradient of a row's unlisted tokens needs: factor * 2^t, t = x c2 - shift <= 0 (m = 0), or
+// (x - m) c2 - shift where x c2 may be so large that its own steps would show.
 struct RowGrad {
     float m, c2, shift, factor;
 };
+constexpr double kNear = 0x1p14;
 
 // A listed token and its gradient; id -1: none (left out, or an earlier entry has the token).
 struct Entry {
@@ -90,10 +92,9 @@ __device__ __forceinline__ double entry_of(const double (&x)[kSlots], int e) {
 }
 static_assert(kSlots == 2, "entry_of chooses between two slots");
 
-__device__ __forceinline__ List read_list(const ListArgs &a, int64_t row) {
+// The list's tokens, log probabilities (-inf for an entry that is left out) and logits.
+__device__ __forceinline__ void read_list(const ListArgs &a, int64_t row, List &q, float (&lp)[kSlots]) {
     const int lane = threadIdx.x % kWave;
-    List q;
-    float lp[kSlots];
 #pragma unroll
     for (int u = 0; u < kSlots; ++u) {
         const int k = u * kWave + lane;
@@ -108,6 +109,22 @@ __device__ __forceinline__ List read_list(const ListArgs &a, int64_t row) {
 #pragma unroll
     for (int u = 0; u < kSlots; ++u)
         q.x[u] = q.id[u] >= 0 ? load_logit(row_at(a.logits, a.dtype, row * a.ld), a.dtype, q.id[u]) : -INFINITY;
+}
+
+// Whether a token is listed twice.
+__device__ __forceinline__ bool repeats(const List &q, int n_top) {
+    int same[kSlots] = {};
+    for (int e = 0; e < n_top; ++e) {
+        const int32_t id = entry_of(q.id, e);
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) same[u] += q.id[u] == id ? 1 : 0;
+    }
+    return __ballot((q.id[0] >= 0 && same[0] > 1) || (q.id[1] >= 0 && same[1] > 1)) != 0;
+}
+
+// The list's masses; equal tokens are merged into their first entry.
+__device__ __forceinline__ void weigh_list(const ListArgs &a, List &q, const float (&lp)[kSlots], bool repeated) {
+    const int lane = threadIdx.x % kWave;
     q.most = wave_max(fmaxf(lp[0], lp[1]));
     q.any = q.most > -INFINITY;
     double all = 0.0;
@@ -126,42 +143,34 @@ __device__ __forceinline__ List read_list(const ListArgs &a, int64_t row) {
             q.log_mass[u] -= log_all;
         }
     }
-    // equal tokens: the first entry stands for them
-    int same[kSlots] = {};
-    for (int e = 0; e < a.n_top; ++e) {
-        const int32_t id = entry_of(q.id, e);
-#pragma unroll
-        for (int u = 0; u < kSlots; ++u) same[u] += q.id[u] == id ? 1 : 0;
-    }
-    if (__ballot((q.id[0] >= 0 && same[0] > 1) || (q.id[1] >= 0 && same[1] > 1)) != 0) {
+    if (repeated) {
         double mass[kSlots] = {};
-        bool first[kSlots] = {true, true};
-        for (int e = 0; e < a.n_top; ++e) {
+        int first[kSlots] = {kMaxTop, kMaxTop};
+        for (int e = a.n_top - 1; e >= 0; --e) {
             const int32_t id = entry_of(q.id, e);
             const double w = entry_of(q.mass, e);
 #pragma unroll
             for (int u = 0; u < kSlots; ++u) {
                 if (q.id[u] == id) {
                     mass[u] += w;
-                    first[u] = first[u] && e >= u * kWave + lane;
+                    first[u] = e;
                 }
             }
         }
 #pragma unroll
         for (int u = 0; u < kSlots; ++u) {
             if (q.id[u] < 0) continue;
-            if (!first[u]) {
+            if (first[u] < u * kWave + lane) {
                 q.id[u] = -1;
                 q.x[u] = -INFINITY;
                 q.mass[u] = 0.0;
-            } else if (same[u] > 1) {
+            } else {
                 q.mass[u] = mass[u];
                 q.log_mass[u] = log(mass[u]);
             }
         }
     }
     q.listed = wave_sum(q.mass[0] + q.mass[1]);
-    return q;
 }
 
 // A row's loss (written by lane 0) and, with GRAD, what its gradient needs, from its list and its unlisted
@@ -199,11 +208,14 @@ __device__ __forceinline__ RowGrad finish_row(const ListArgs &a, int64_t row, co
         const double scale = g == 0.0 || zero ? 0.0 : (bad ? NAN : g * beta), total = q.listed + rest;
 #pragma unroll
         for (int u = 0; u < kSlots; ++u) grad[u] = scale == 0.0 ? 0.0 : scale * (total * (e[u] / s) - q.mass[u]);
-        r.m = m_out;
+        // u_j = 2^((x_j - m_out) c2 - log2 s_out); the exponent is kept one below, so that its power can be
+        // held in [0, 1] (which makes a NaN 0), and what rounding its offset loses goes into the factor
         r.c2 = (float)beta * kLog2e;
-        const double shift = s_out > 0.0 ? log_out * (1.0 / kLn2) : 0.0;
-        r.shift = (float)shift;
-        // the shift's rounding goes into the factor
+        const double log2_out = s_out > 0.0 ? log_out * (1.0 / kLn2) : 0.0, offset = (double)m_out * (double)r.c2;
+        const bool near = fabs(offset) <= kNear;
+        r.m = near ? 0.0f : m_out;
+        const double shift = log2_out + (near ? offset : 0.0);
+        r.shift = (float)(shift + 1.0);
         const double factor = total * (s_out > 0.0 ? exp(log_rest) : 0.0) - rest;
         r.factor = scale == 0.0 ? 0.0f : (float)(scale * factor * exp2((double)r.shift - shift));
     }
@@ -242,17 +254,19 @@ __device__ __forceinline__ void write_grad(const ListArgs &a, int64_t row_i, int
     const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
     T *out = static_cast<T *>(a.out) + row_i * a.out_ld;
     RowGrad q;
-    for_chunks<DT, NV, THREADS, true, 1>(row, a.v, x0, x1, [&] { q = get(); }, [&](uint32_t(&w)[NV][4], int x) {
+    for_chunks<DT, NV, THREADS, true, true, 1>(row, a.v, x0, x1, [&] { q = get(); }, [&](uint32_t(&w)[NV][4], int x) {
+        auto store = [&](auto exponent) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float d[kPer];
+            for (int i = 0; i < NV; ++i) {
+                float d[kPer];
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                const float t = fmaxf((value<DT>(w[i], j) - q.m) * q.c2 - q.shift, kLowest);
-                d[j] = q.factor * __builtin_amdgcn_exp2f(t);
+                for (int j = 0; j < kPer; ++j)
+                    d[j] = q.factor * fminf(fmaxf(__builtin_amdgcn_exp2f(exponent(value<DT>(w[i], j))), 0.0f), 1.0f);
+                store_vector<DT>(out, vector_at<DT, THREADS>(x, i), a.v, d);
             }
-            store_vector<DT>(out, vector_at<DT, THREADS>(x, i), a.v, d);
-        }
+        };
+        if (q.m == 0.0f) store([&](float y) { return fmaf(y, q.c2, -q.shift); });
+        else store([&](float y) { return (y - q.m) * q.c2 - q.shift; });
     });
 }
 
@@ -274,15 +288,21 @@ __global__ __launch_bounds__(THREADS) void list_whole(ListArgs a) {
     auto read = [&] {
         for (int i = threadIdx.x; i < bitmap_words<DT, NV, THREADS>(a.v); i += THREADS) sh_bits[i] = 0;
         __syncthreads();
+        float lp[kSlots];
+        bool repeated = false;
         if (wave == 0) {
-            list = read_list(a, row_i);
+            read_list(a, row_i, list, lp);
 #pragma unroll
-            for (int u = 0; u < kSlots; ++u)
-                if (list.id[u] >= 0) atomicOr(&sh_bits[list.id[u] / 32], 1u << (list.id[u] % 32));
+            for (int u = 0; u < kSlots; ++u) {
+                if (list.id[u] < 0) continue;
+                const uint32_t bit = 1u << (list.id[u] % 32);
+                repeated = (atomicOr(&sh_bits[list.id[u] / 32], bit) & bit) != 0 || repeated;
+            }
         }
         __syncthreads();
+        if (wave == 0) weigh_list(a, list, lp, __ballot(repeated) != 0);
     };
-    for_chunks<DT, NV, THREADS, !GRAD, 1>(row, a.v, 0, a.v, read, [&](uint32_t(&w)[NV][4], int x) {
+    for_chunks<DT, NV, THREADS, !GRAD, false, 1>(row, a.v, 0, a.v, read, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         take_out<DT, NV, THREADS>(w, sh_bits, x, 0);
         add_chunk<DT, NV, false>(w, c2, mine, vm);
@@ -342,7 +362,7 @@ __global__ __launch_bounds__(kThreads) void list_parts(ListArgs a) {
         __syncthreads();
     };
     Sum mine = {-INFINITY, 0.0f, 0.0f};
-    for_chunks<DT, NV, kThreads, false, 1>(row, a.v, x0, x1, read, [&](uint32_t(&w)[NV][4], int x) {
+    for_chunks<DT, NV, kThreads, false, false, 1>(row, a.v, x0, x1, read, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         take_out<DT, NV, kThreads>(w, sh_bits, x, x0);
         add_chunk<DT, NV, false>(w, c2, mine, vm);
@@ -364,7 +384,10 @@ __global__ __launch_bounds__(kWave) void list_rows(ListArgs a) {
     const int64_t r = blockIdx.x, row = a.row0 + r;
     const int lane = threadIdx.x;
     const float2 *sums = a.sums + (size_t)r * a.parts;
-    const List list = read_list(a, row);
+    List list;
+    float lp[kSlots];
+    read_list(a, row, list, lp);
+    weigh_list(a, list, lp, repeats(list, a.n_top));
     float m_out = -INFINITY;
     for (int p = lane; p < a.parts; p += kWave) m_out = fmaxf(m_out, sums[p].x);
     m_out = wave_max(m_out);

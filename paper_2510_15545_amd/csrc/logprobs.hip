@@ -388,7 +388,7 @@ __global__ __launch_bounds__(kThreads) void row_stream(RowArgs a) {
     int count = 0;
     Sum mine = {-INFINITY, 0.0f, 0.0f};
     TopSet<DT, kChunkVectors> top{sh, a.n_top};
-    for_chunks<DT, kChunkVectors, kThreads, true, TOP ? 1 : 2>(row, a.v, x0, x1, [] {}, [&](uint32_t(&w)[kChunkVectors][4], int x) {
+    for_chunks<DT, kChunkVectors, kThreads, true, false, TOP ? 1 : 2>(row, a.v, x0, x1, [] {}, [&](uint32_t(&w)[kChunkVectors][4], int x) {
         float vm[kChunkVectors];
         add_chunk<DT, kChunkVectors, ENTROPY>(w, c2, mine, vm);
         if constexpr (TOP) top.add(w, vm, x);
@@ -660,7 +660,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(GradArgs a) {
     const float ent = ENTROPY ? a.entropy[r] : 0.0f;
     // d = p (first + second t), t = lp / ln 2 held above -200 (p is 0 there); NaN statistics make it NaN
     const float first = -beta * (g + h * ent) + (log_sum - log_sum), second = ENTROPY ? -beta * h * (float)kLn2 : 0.0f;
-    for_chunks<DT, kGradVectors, kThreads, true, 1>(row, a.v, x_part, x_end, [] {}, [&](uint32_t(&w)[kGradVectors][4], int x_chunk) {
+    for_chunks<DT, kGradVectors, kThreads, true, false, 1>(row, a.v, x_part, x_end, [] {}, [&](uint32_t(&w)[kGradVectors][4], int x_chunk) {
 #pragma unroll
         for (int i = 0; i < kGradVectors; ++i) {
             const int x = vector_at<DT, kThreads>(x_chunk, i);

@@ -101,6 +101,17 @@ __device__ __forceinline__ uint32_t encode(float x) {
     else return __builtin_bit_cast(unsigned short, (__bf16)x);
 }
 
+// Two values as the row holds them, the first in the lower half.
+template <int DT>
+__device__ __forceinline__ uint32_t encode_pair(float x, float y) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    const f2 v = {x, y};
+    if constexpr (DT == TT_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
+}
+
 // The non-temporal hint: written once and not read here, such lines would displace the logits that will be.
 template <int DT>
 __device__ __forceinline__ void store_vector(typename Elem<DT>::T *row, int x, int v, const float (&d)[Elem<DT>::kPer]) {
@@ -109,7 +120,7 @@ __device__ __forceinline__ void store_vector(typename Elem<DT>::T *row, int x, i
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if constexpr (DT == TT_F32) w[q] = __float_as_uint(d[q]);
-        else w[q] = encode<DT>(d[2 * q]) | (encode<DT>(d[2 * q + 1]) << 16);
+        else w[q] = encode_pair<DT>(d[2 * q], d[2 * q + 1]);
     }
     if (x + kPer <= v) {
         u4u t;
@@ -288,24 +299,27 @@ static __device__ const uint32_t kNoRow[4] = {};
 
 // Calls f(vectors, first element) for every chunk of a row's elements x0 .. x1 - 1 (x0 a multiple of the chunk),
 // minus infinity past v, while the next chunk's loads are in flight; before() once the first chunk's are.
-template <int DT, int NV, int THREADS, bool LAST, int UNROLL, typename B, typename F>
+// BACK: from the last chunk to the first.
+template <int DT, int NV, int THREADS, bool LAST, bool BACK, int UNROLL, typename B, typename F>
 __device__ __forceinline__ void for_chunks(const typename Elem<DT>::T *row, int v, int x0, int x1, B before, F f) {
     using T = typename Elem<DT>::T;
     constexpr int kPer = Elem<DT>::kPer, kChunk = NV * THREADS * kPer;
     const bool tiny = v < kPer;
     const T *from = tiny ? reinterpret_cast<const T *>(kNoRow) : row;
     const int width = tiny ? kPer : v;
+    const int n = (x1 - x0 + kChunk - 1) / kChunk, step = BACK ? -kChunk : kChunk;
+    int x = BACK ? x0 + (n - 1) * kChunk : x0;
     uint32_t w[NV][4];
-    load_chunk<DT, NV, THREADS, LAST>(from, width, x0, w);
+    load_chunk<DT, NV, THREADS, LAST>(from, width, x, w);
     if (tiny) {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) set_bits<DT>(w[0], j, j < v ? (uint32_t)row[j] : Elem<DT>::kNone);
     }
     before();
 #pragma unroll UNROLL
-    for (int x = x0; x < x1; x += kChunk) {
+    for (int c = 1; c <= n; ++c, x += step) {
         uint32_t next[NV][4];
-        load_chunk<DT, NV, THREADS, LAST>(from, width, x + kChunk < x1 ? x + kChunk : width, next);  // past the end: one line
+        load_chunk<DT, NV, THREADS, LAST>(from, width, c < n ? x + step : width, next);  // past the end: one line
         fix_chunk<DT, NV, THREADS>(width, x, w);
         f(w, x);
 #pragma unroll
