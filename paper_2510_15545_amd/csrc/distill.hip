@@ -441,7 +441,7 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
     const int chunk = kChunkVectors * kThreads * elements_per_vector(dtype), chunks = (v + chunk - 1) / chunk;
     int64_t most = kMaxGrid;
     if (v <= kMaxBits && (n_rows >= kFewRows || bytes <= kSplitRow)) {
-        p.threads = bytes <= kShortRow || !grad ? kThreads : kLongThreads;
+        p.threads = bytes <= kShortRow || (!grad && n_rows >= kFullGrid) ? kThreads : kLongThreads;
     } else {
         int64_t parts = n_rows > 0 ? (kFullGrid + n_rows - 1) / n_rows : 1;
         const int64_t least = (v + kMaxBits - 1) / kMaxBits;
@@ -469,9 +469,9 @@ void launch_whole(const ListArgs &a, int threads, int64_t n, hipStream_t stream)
     if (threads == kThreads) {
         const size_t lds = bitmap_words<DT, kChunkVectors, kThreads>(a.v) * sizeof(uint32_t);
         list_whole<DT, kChunkVectors, kThreads, GRAD><<<(unsigned)n, kThreads, lds, stream>>>(a);
-    } else if constexpr (GRAD) {
+    } else {
         const size_t lds = bitmap_words<DT, kLongVectors, kLongThreads>(a.v) * sizeof(uint32_t);
-        list_whole<DT, kLongVectors, kLongThreads, true><<<(unsigned)n, kLongThreads, lds, stream>>>(a);
+        list_whole<DT, kLongVectors, kLongThreads, GRAD><<<(unsigned)n, kLongThreads, lds, stream>>>(a);
     }
 }
 

@@ -25,9 +25,11 @@ using namespace rows;
 constexpr int kMaxTop = 128;
 constexpr int kSelect = 1024;                       // keys that are ordered in LDS
 constexpr int kGroups = 256;                        // lane groups whose largest values give the bound
-constexpr int kCrowd = 24;                          // groups beyond k at the bound that make it worth refining
 constexpr int kChunkVectors = 4;
 constexpr int kWholeChunks = 2;                     // rows of at most this many chunks are never split
+constexpr int kLongThreads = 1024, kLongVectors = 2;  // for rows taken whole where they are few
+constexpr int64_t kLongRows = 96;                   // rows from which on they are, whatever their length,
+constexpr int64_t kLongBytes = 128 << 10;           // and the length up to which they are, however few
 constexpr size_t kMaxKeyBytes = size_t(128) << 20;  // workspace: rows are taken in groups beyond
 constexpr int64_t kMaxGrid = int64_t(1) << 18;      // workgroups of one launch
 
@@ -48,11 +50,13 @@ struct RowArgs {
 };
 
 // LDS of the selection; a wave stages its keys in a segment of its own.
+template <int THREADS>
 struct TopLds {
-    static constexpr int kStage = 512;
-    uint32_t largest[kGroups];
-    int where[kGroups];
-    uint64_t stage[kThreads / kWave][kStage];
+    static constexpr int kStage = THREADS == kThreads ? 512 : 256;
+    uint32_t group[2][kGroups];  // in turn, so that one barrier does
+    uint32_t largest[THREADS];
+    int where[THREADS];
+    uint64_t stage[THREADS / kWave][kStage];
     int slots[64], total;
 };
 
@@ -75,79 +79,100 @@ __device__ __forceinline__ int lanes_below(uint64_t mask) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// How many of the 256 values that a wave holds, four a lane, satisfy f.
-template <typename F>
-__device__ __forceinline__ int count_groups(F f) {
-    int n = 0;
-#pragma unroll
-    for (int u = 0; u < kGroups / kWave; ++u) n += __popcll(__ballot(f(u)));
-    return n;
+// The largest of the keys of GROUP lanes (1, 4 or 16 in a row of 16), in each of them.
+template <int GROUP>
+__device__ __forceinline__ uint32_t group_max(uint32_t x) {
+    auto with = [&](uint32_t y) { x = y > x ? y : x; };
+    if constexpr (GROUP >= 4) {
+        with(__builtin_amdgcn_update_dpp(0u, x, 0xB1, 0xF, 0xF, true));  // quad_perm 1,0,3,2
+        with(__builtin_amdgcn_update_dpp(0u, x, 0x4E, 0xF, 0xF, true));  // quad_perm 2,3,0,1
+    }
+    if constexpr (GROUP >= 16) {
+        with(__builtin_amdgcn_update_dpp(0u, x, 0x124, 0xF, 0xF, true));  // row_ror 4
+        with(__builtin_amdgcn_update_dpp(0u, x, 0x128, 0xF, 0xF, true));  // row_ror 8
+    }
+    return x;
 }
 
-// The upper 16 bits of the largest order key that at least k groups reach; n: how many reach it.
-__device__ __forceinline__ uint32_t kth_upper(const uint32_t (&q)[kGroups / kWave], int k, int &n) {
-    uint32_t p = 0;
-    n = kGroups;
+// A key that at least k of the wave's keys reach, G a lane, and how many do: not many more than k, unless that many
+// are equal to it (then it is the k-th largest itself).  kLowestFinite where fewer than k are finite.
+struct Kth {
+    uint32_t key;
+    int n;
+    bool tied;
+};
+
+template <int G>
+__device__ __forceinline__ Kth kth_key(const uint32_t (&q)[G], int k) {
+    auto reach = [&](uint32_t c) {
+        int n = 0;
 #pragma unroll
-    for (int b = 31; b >= 16; --b) {
-        const uint32_t c = p | (1u << b);
-        const int m = count_groups([&](int u) { return q[u] >= c; });
-        if (m >= k) {
-            p = c;
-            n = m;
+        for (int u = 0; u < G; ++u) n += __popcll(__ballot(q[u] >= c));
+        return n;
+    };
+    uint32_t most = 0, least = 0xFFFFFFFFu;  // of the finite ones: a close range to search
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+        most = q[u] > most ? q[u] : most;
+        least = q[u] >= kLowestFinite && q[u] < least ? q[u] : least;
+    }
+    uint32_t lo = wave_min(least), hi = wave_max(most);
+    const int enough = k + k / 4 + 2;
+    int n = reach(lo);
+    if (n < k) return {kLowestFinite, n, false};
+    const int m = reach(hi);
+    if (m >= k) return {hi, m, m > enough};
+    while (n > enough && hi - lo > 1) {  // n reach lo, fewer than k reach hi
+        const uint32_t c = lo + (hi - lo) / 2;
+        const int r = reach(c);
+        if (r >= k) {
+            lo = c;
+            n = r;
+        } else {
+            hi = c;
         }
     }
-    return p;
+    return {lo, n, n > enough};
 }
 
-// The bound from the groups' largest values and an index that each one's element does not pass: reached by k
-// groups' elements at least.  16 ballots; where many more groups tie at it (equal values, as in a row
-// of capped logits), the rest of the value and then the index decide.  Each wave for itself.
-__device__ __forceinline__ Bound kth_bound(const TopLds &sh, int k) {
+// The same for the workgroup's keys, one a thread: by 64 groups of threads for small k (a group counts once), 256 else.
+// sh_group: kGroups words that nobody reads until the barrier in here.
+constexpr int kFewTop = 32;
+
+template <int THREADS>
+__device__ __forceinline__ Kth kth_of_threads(uint32_t key, int k, uint32_t *sh_group) {
+    constexpr int kFew = THREADS / kWave, kMany = THREADS / kGroups;  // threads of a group
     const int lane = threadIdx.x % kWave;
+    if (k <= kFewTop) {
+        key = group_max<kFew>(key);
+        if (lane % kFew == 0) sh_group[threadIdx.x / kFew] = key;
+        __syncthreads();
+        const uint32_t q[1] = {sh_group[lane]};
+        return kth_key<1>(q, k);
+    }
+    key = group_max<kMany>(key);
+    if (lane % kMany == 0) sh_group[threadIdx.x / kMany] = key;
+    __syncthreads();
     uint32_t q[kGroups / kWave];
 #pragma unroll
-    for (int u = 0; u < kGroups / kWave; ++u) q[u] = sh.largest[u * kWave + lane];
-    int n;
-    Bound r = {kth_upper(q, k, n), INT_MAX};
-    if (r.key < kLowestFinite) return {kLowestFinite, INT_MAX};  // fewer than k groups hold a finite value
-    if (n < k + kCrowd) return r;
-    for (int b = 15; b >= 0; --b) {
-        const uint32_t c = r.key | (1u << b);
-        const int m = count_groups([&](int u) { return q[u] >= c; });
-        if (m >= k) {
-            r.key = c;
-            n = m;
-        }
-    }
-    if (n < k + kCrowd) return r;
-    int at[kGroups / kWave];
-#pragma unroll
-    for (int u = 0; u < kGroups / kWave; ++u) at[u] = sh.where[u * kWave + lane];
-    const int need = k - count_groups([&](int u) { return q[u] > r.key; });
-    r.index = 0;  // the largest index with fewer than `need` equal groups below it
-    for (int b = 23; b >= 0; --b) {
-        const int c = r.index | (1 << b);
-        if (count_groups([&](int u) { return q[u] == r.key && at[u] < c; }) < need) r.index = c;
-    }
-    return r;
+    for (int u = 0; u < kGroups / kWave; ++u) q[u] = sh_group[u * kWave + lane];
+    return kth_key<kGroups / kWave>(q, k);
 }
 
 // Sum over the workgroup of a count, through a zeroed LDS slot of its own.
 __device__ __forceinline__ int block_count(int n, int *slot) {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) n += __shfl_xor(n, d);
+    n = (int)wave_sum((uint32_t)n);
     if (threadIdx.x % kWave == 0) atomicAdd(slot, n);
     __syncthreads();
     return *slot;
 }
 
 // Elements x0 .. x1 - 1 of a row that satisfy f(order key, index), counted by this thread.
-template <int DT, typename F>
+template <int DT, int THREADS, typename F>
 __device__ __forceinline__ int count_if(const typename Elem<DT>::T *row, int x0, int x1, F f) {
     int n = 0;
 #pragma unroll 4
-    for (int x = x0 + (int)threadIdx.x; x < x1; x += kThreads) {
+    for (int x = x0 + (int)threadIdx.x; x < x1; x += THREADS) {
         const float y = decode<DT>(row[x]);
         n += (y > -INFINITY && f(order_key(y), x)) ? 1 : 0;
     }
@@ -158,7 +183,7 @@ __device__ __forceinline__ int count_if(const typename Elem<DT>::T *row, int x0,
 // large values all in the same lanes): the k-th largest value by binary search on its order key, then
 // the last index among the elements equal to it, each step a count over the part, read again.  At
 // least k elements are finite.
-template <int DT>
+template <int DT, int THREADS>
 __device__ __noinline__ void select_exactly(const typename Elem<DT>::T *row, int x0, int x1, int k, uint64_t *keys, int *sh_slots,
                                             int *sh_total) {
     if (threadIdx.x < 64) sh_slots[threadIdx.x] = 0;
@@ -168,18 +193,18 @@ __device__ __noinline__ void select_exactly(const typename Elem<DT>::T *row, int
     uint32_t kth = 0;
     for (int b = 31; b >= 0; --b) {
         const uint32_t c = kth | (1u << b);
-        const int n = count_if<DT>(row, x0, x1, [c](uint32_t o, int) { return o >= c; });
+        const int n = count_if<DT, THREADS>(row, x0, x1, [c](uint32_t o, int) { return o >= c; });
         if (block_count(n, &sh_slots[slot++]) >= k) kth = c;
     }
-    const int above = count_if<DT>(row, x0, x1, [kth](uint32_t o, int) { return o > kth; });
+    const int above = count_if<DT, THREADS>(row, x0, x1, [kth](uint32_t o, int) { return o > kth; });
     const int need = k - block_count(above, &sh_slots[slot++]);
     int last = 0;  // the largest index with fewer than `need` equal elements below it
     for (int b = 23; b >= 0; --b) {
         const int c = last | (1 << b);
-        const int n = count_if<DT>(row, x0, x1, [kth, c](uint32_t o, int x) { return o == kth && x < c; });
+        const int n = count_if<DT, THREADS>(row, x0, x1, [kth, c](uint32_t o, int x) { return o == kth && x < c; });
         if (block_count(n, &sh_slots[slot++]) < need) last = c;
     }
-    count_if<DT>(row, x0, x1, [=](uint32_t o, int x) {
+    count_if<DT, THREADS>(row, x0, x1, [=](uint32_t o, int x) {
         if (o > kth || (o == kth && x <= last)) keys[atomicAdd(sh_total, 1)] = full_key(o, x);
         return false;
     });
@@ -187,24 +212,52 @@ __device__ __noinline__ void select_exactly(const typename Elem<DT>::T *row, int
 }
 
 // The elements of a row that may be among its k largest, chunk by chunk.
-template <int DT, int NV>
+template <int DT, int NV, int THREADS>
 struct TopSet {
-    static constexpr int kPer = Elem<DT>::kPer, kChunk = NV * kThreads * kPer;
-    TopLds &sh;
+    static constexpr int kPer = Elem<DT>::kPer, kStage = TopLds<THREADS>::kStage;
+    TopLds<THREADS> &sh;
     int k;
     Bound bound = {kLowestFinite, INT_MAX};
     float most = -INFINITY;     // the thread's largest value
     int where = 0;              // first index of its vector
     int staged = 0, chunks = 0; // of this wave; of the row
+    int turn = 0;
     bool current = false;       // the bound is that of all chunks so far
 
+    // The bound from the threads' largest values.
     __device__ __forceinline__ void raise() {
-        __syncthreads();  // the last bound has been read
-        sh.largest[threadIdx.x] = order_key(most);
+        const uint32_t key = order_key(most);
+        turn ^= 1;
+        const Kth q = kth_of_threads<THREADS>(key, k, sh.group[turn]);
+        bound = {q.key, INT_MAX};
+        if (q.tied) break_tie(key);
+        current = true;
+    }
+
+    // Many groups are equal to the bound (a row of capped or of few different logits): of the elements equal to it,
+    // those up to an index that enough threads' elements do not pass.
+    __device__ __forceinline__ void break_tie(uint32_t key) {
+        const int lane = threadIdx.x % kWave;
+        __syncthreads();
+        sh.largest[threadIdx.x] = key;
         sh.where[threadIdx.x] = where + kPer - 1;
         __syncthreads();
-        bound = kth_bound(sh, k);
-        current = true;
+        auto count = [&](auto f) {
+            int n = 0;
+            for (int u = 0; u < THREADS / kWave; ++u) n += __popcll(__ballot(f(sh.largest[u * kWave + lane], sh.where[u * kWave + lane])));
+            return n;
+        };
+        const uint32_t kth = bound.key;
+        const int need = k - count([=](uint32_t o, int) { return o > kth; });
+        if (need <= 0) {
+            ++bound.key;  // enough lie above it
+            return;
+        }
+        bound.index = 0;  // the largest index with fewer than `need` equal ones below it
+        for (int b = 23; b >= 0; --b) {
+            const int c = bound.index | (1 << b);
+            if (count([=](uint32_t o, int at) { return o == kth && at < c; }) < need) bound.index = c;
+        }
     }
 
     __device__ __forceinline__ void add(const uint32_t (&w)[NV][4], const float (&vm)[NV], int x_chunk) {
@@ -213,7 +266,7 @@ struct TopSet {
         for (int i = 0; i < NV; ++i) {
             if (vm[i] > most) {
                 most = vm[i];
-                where = vector_at<DT, kThreads>(x_chunk, i);
+                where = vector_at<DT, THREADS>(x_chunk, i);
             }
         }
         current = false;
@@ -227,11 +280,11 @@ struct TopSet {
             for (int j = 0; j < kPer; ++j) {
                 const float x = value<DT>(w[i], j);
                 if (__ballot(x >= lowest) == 0) continue;
-                const int at = vector_at<DT, kThreads>(x_chunk, i) + j;
+                const int at = vector_at<DT, THREADS>(x_chunk, i) + j;
                 const bool in = x > lowest || (x == lowest && at <= bound.index);
                 const uint64_t hit = __ballot(in);
                 const int slot = staged + lanes_below(hit);
-                if (in && slot < TopLds::kStage) sh.stage[wave][slot] = full_key(order_key(x), at);
+                if (in && slot < kStage) sh.stage[wave][slot] = full_key(order_key(x), at);
                 staged += __popcll(hit);
             }
         }
@@ -245,7 +298,7 @@ struct TopSet {
         const uint64_t from = bound.full();
         if (threadIdx.x == 0) sh.total = 0;
         __syncthreads();
-        const bool over = staged > TopLds::kStage;
+        const bool over = staged > kStage;
         int n = 0;
         if (over) {
             n = capacity + 1;
@@ -259,7 +312,7 @@ struct TopSet {
         const int total = sh.total;
         if (total > capacity) {
             __syncthreads();
-            select_exactly<DT>(row, x0, x1, k, dst, sh.slots, &sh.total);
+            select_exactly<DT, THREADS>(row, x0, x1, k, dst, sh.slots, &sh.total);
             return k;
         }
         for (int i = lane; i - lane < staged; i += kWave) {
@@ -274,29 +327,24 @@ struct TopSet {
 };
 
 // The largest k (all, if fewer) of c <= kSelect distinct keys in LDS, descending, in sh_out; returns their number.
-__device__ __forceinline__ int order_keys(uint64_t *sh_sel, int c, int k, uint32_t *sh_largest, int *sh_total, uint64_t *sh_out) {
+template <int THREADS>
+__device__ __forceinline__ int order_keys(uint64_t *sh_sel, int c, int k, uint32_t *sh_group, int *sh_total, uint64_t *sh_out) {
     const int lane = threadIdx.x % kWave;
     if (c > kGroups) {  // counting is quadratic: the bound once more, a few keys a lane
-        constexpr int kEach = kSelect / kThreads;
+        constexpr int kEach = kSelect / THREADS;
         uint64_t mine[kEach];
         uint32_t most = 0;
 #pragma unroll
         for (int u = 0; u < kEach; ++u) {
-            const int i = u * kThreads + (int)threadIdx.x;
+            const int i = u * THREADS + (int)threadIdx.x;
             mine[u] = i < c ? sh_sel[i] : 0;
             const uint32_t o = (uint32_t)(mine[u] >> 32);
             most = o > most ? o : most;
         }
         __syncthreads();
-        sh_largest[threadIdx.x] = most;
         if (threadIdx.x == 0) *sh_total = 0;
-        __syncthreads();
-        uint32_t q[kGroups / kWave];
-#pragma unroll
-        for (int u = 0; u < kGroups / kWave; ++u) q[u] = sh_largest[u * kWave + lane];
-        int n;
-        const uint64_t from = (uint64_t)kth_upper(q, k, n) << 32;
-        n = 0;
+        const uint64_t from = (uint64_t)kth_of_threads<THREADS>(most, k, sh_group).key << 32;
+        int n = 0;
 #pragma unroll
         for (int u = 0; u < kEach; ++u) n += __popcll(__ballot(mine[u] != 0 && mine[u] >= from));
         int base = 0;
@@ -311,7 +359,7 @@ __device__ __forceinline__ int order_keys(uint64_t *sh_sel, int c, int k, uint32
         __syncthreads();
         c = *sh_total;
     }
-    for (int i = threadIdx.x; i < c; i += kThreads) {
+    for (int i = threadIdx.x; i < c; i += THREADS) {
         const uint64_t key = sh_sel[i];
         int rank = 0;
 #pragma unroll 4
@@ -335,28 +383,31 @@ __device__ __forceinline__ float token_logit(const RowArgs &a, int64_t row) {
     return id >= 0 && id < a.v ? load_logit(row_at(a.logits, a.dtype, row * a.ld), a.dtype, id) : 0.0f;
 }
 
-// A row's results but the alternatives, by one thread: m, s and e as in Sum, in natural units and fp64; the token's logit.
-__device__ __forceinline__ RowStats write_row(const RowArgs &a, int64_t row, double beta, float m, double s, double e, float x_id) {
+// From the row's largest logit m and the sum s relative to it.
+__device__ __forceinline__ RowStats row_stats(double beta, float m, double s) {
     // m = -inf: nothing is finite (s = 0); m = +inf or an unsound temperature: NaN
     RowStats q;
     q.m = m;
     q.beta = beta;
     q.bad = !(beta > 0.0 && beta < INFINITY) || m == INFINITY;
-    const bool empty = m == -INFINITY;
-    q.log_sum = q.bad ? NAN : (empty ? 0.0 : log(s));
+    q.log_sum = q.bad ? NAN : (m == -INFINITY ? 0.0 : log(s));
+    return q;
+}
+
+// A row's results but the alternatives, by one thread: s and e as in Sum, in natural units; the token's logit.
+__device__ __forceinline__ void write_row(const RowArgs &a, int64_t row, const RowStats &q, double s, double e, float x_id) {
     if (a.stats != nullptr) {
-        a.stats[2 * row] = q.bad ? NAN : m;
+        a.stats[2 * row] = q.bad ? NAN : (float)q.m;
         a.stats[2 * row + 1] = (float)q.log_sum;
     }
-    if (a.lse != nullptr) a.lse[row] = (float)(q.bad ? NAN : q.m * beta + q.log_sum);
-    if (a.entropy != nullptr) a.entropy[row] = (float)(q.bad ? NAN : (empty ? 0.0 : q.log_sum - e / s));
+    if (a.lse != nullptr) a.lse[row] = (float)(q.bad ? NAN : q.m * q.beta + q.log_sum);
+    if (a.entropy != nullptr) a.entropy[row] = (float)(q.bad ? NAN : (q.m == -INFINITY ? 0.0 : q.log_sum - e / s));
     if (a.logprob != nullptr) {
         const int32_t id = a.ids[row];
         double lp = NAN;
-        if (!q.bad && id >= 0 && id < a.v) lp = x_id == -INFINITY ? -INFINITY : ((double)x_id - q.m) * beta - q.log_sum;
+        if (!q.bad && id >= 0 && id < a.v) lp = x_id == -INFINITY ? -INFINITY : ((double)x_id - q.m) * q.beta - q.log_sum;
         a.logprob[row] = (float)lp;
     }
-    return q;
 }
 
 __device__ __forceinline__ void write_top(const RowArgs &a, int64_t row, const RowStats &q, const uint64_t *sh_out, int n, int i) {
@@ -371,11 +422,11 @@ __device__ __forceinline__ void write_top(const RowArgs &a, int64_t row, const R
 }
 
 // A part of a row by a workgroup; FINISH: the row is one part, and finished here.
-template <int DT, bool TOP, bool ENTROPY, bool FINISH>
-__global__ __launch_bounds__(kThreads) void row_stream(RowArgs a) {
-    constexpr int kWaves = kThreads / kWave;
+template <int DT, int THREADS, bool TOP, bool ENTROPY, bool FINISH>
+__global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stream(RowArgs a) {
+    constexpr int kWaves = THREADS / kWave, NV = THREADS == kThreads ? kChunkVectors : kLongVectors;
     __shared__ Sum sh_sum[kWaves];
-    __shared__ TopLds sh;
+    __shared__ TopLds<THREADS> sh;
     __shared__ uint64_t sh_sel[kSelect], sh_out[kMaxTop];
     __shared__ RowStats sh_stats;
     pass_over_nans();
@@ -387,10 +438,10 @@ __global__ __launch_bounds__(kThreads) void row_stream(RowArgs a) {
     const float x_id = FINISH ? token_logit(a, row_i) : 0.0f;
     int count = 0;
     Sum mine = {-INFINITY, 0.0f, 0.0f};
-    TopSet<DT, kChunkVectors> top{sh, a.n_top};
-    for_chunks<DT, kChunkVectors, kThreads, true, false, TOP ? 1 : 2>(row, a.v, x0, x1, [] {}, [&](uint32_t(&w)[kChunkVectors][4], int x) {
-        float vm[kChunkVectors];
-        add_chunk<DT, kChunkVectors, ENTROPY>(w, c2, mine, vm);
+    TopSet<DT, NV, THREADS> top{sh, a.n_top};
+    for_chunks<DT, NV, THREADS, true, false, TOP ? 1 : 2>(row, a.v, x0, x1, [] {}, [&](uint32_t(&w)[NV][4], int x) {
+        float vm[NV];
+        add_chunk<DT, NV, ENTROPY>(w, c2, mine, vm);
         if constexpr (TOP) top.add(w, vm, x);
     });
     mine = wave_join<ENTROPY>(mine, c2);
@@ -418,10 +469,14 @@ __global__ __launch_bounds__(kThreads) void row_stream(RowArgs a) {
         }
         s = wave_sum(s);
         e = ENTROPY ? wave_sum(e) : 0.0;
-        if (lane == 0) sh_stats = write_row(a, row_i, beta, m, s, e, x_id);
+        const RowStats stats = row_stats(beta, m, s);
+        if (lane == 0) {
+            sh_stats = stats;
+            write_row(a, row_i, stats, s, e, x_id);
+        }
     }
     if constexpr (TOP && FINISH) {
-        count = order_keys(sh_sel, count, a.n_top, sh.largest, &sh.total, sh_out);
+        count = order_keys<THREADS>(sh_sel, count, a.n_top, sh.group[0], &sh.total, sh_out);
         if ((int)threadIdx.x < a.n_top) write_top(a, row_i, sh_stats, sh_out, count, threadIdx.x);
     }
 }
@@ -438,117 +493,55 @@ __device__ __forceinline__ void for_each_key(const RowArgs &a, const float4 *sum
     }
 }
 
-// A row's keys that reach a bound on its k-th, in sh_sel; returns their number (<= kSelect).  sh_count: the parts'
-// numbers of keys, where there are at most kThreads parts; longest: the largest of them.
-__device__ __forceinline__ int gather_keys(const RowArgs &a, const float4 *sums, const uint64_t *keys, const int *sh_count, int longest,
-                                           uint64_t *sh_sel, uint32_t *sh_largest, int *sh_slots, int *sh_total) {
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    constexpr int kWaves = kThreads / kWave;
-    const int runs = (longest + kWave - 1) / kWave;
-    // few keys: in registers, their loads in flight together
-    const bool held = a.parts <= kThreads && a.parts * runs <= kHeld * kWaves;
-    uint64_t mine[kHeld];
-    uint32_t most = 0;
-    if (held) {
-#pragma unroll
-        for (int u = 0; u < kHeld; ++u) {
-            const int c = u * kWaves + wave, p = runs > 0 ? c / runs : a.parts, i = (c - p * runs) * kWave + lane;
-            mine[u] = 0;
-            if (p < a.parts && i < sh_count[p]) mine[u] = keys[(size_t)p * a.capacity + i];
-        }
-#pragma unroll
-        for (int u = 0; u < kHeld; ++u) {
-            const uint32_t o = (uint32_t)(mine[u] >> 32);
-            most = o > most ? o : most;
-        }
-    } else {
-        for_each_key(a, sums, keys, [&](uint64_t key) {
-            const uint32_t o = (uint32_t)(key >> 32);
-            most = o > most ? o : most;
-        });
-    }
-    sh_largest[threadIdx.x] = most;
-    if (threadIdx.x == 0) *sh_total = 0;
-    __syncthreads();
-    uint32_t q[kGroups / kWave];
-#pragma unroll
-    for (int u = 0; u < kGroups / kWave; ++u) q[u] = sh_largest[u * kWave + lane];
-    int reach;
-    uint64_t from = (uint64_t)kth_upper(q, a.n_top, reach) << 32;
-    from = from > 1 ? from : 1;
-    for (;;) {
-        auto put = [&](uint64_t key) {
-            const uint64_t hit = __ballot(key >= from);
-            if (hit == 0) return;
-            int base = 0;
-            if (lane == 0) base = atomicAdd(sh_total, __popcll(hit));
-            base = __builtin_amdgcn_readfirstlane(base) + lanes_below(hit);
-            if (key >= from && base < kSelect) sh_sel[base] = key;
-        };
-        if (held) {
-#pragma unroll
-            for (int u = 0; u < kHeld; ++u) put(mine[u]);
-        } else {
-            for_each_key(a, sums, keys, put);
-        }
-        __syncthreads();
-        if (*sh_total <= kSelect) return *sh_total;
-        // many equal values: the k-th largest key itself (keys are distinct, so k reach it), by binary search
-        uint64_t kth = 0;
-        for (int b = 63; b >= 0; --b) {
-            const uint64_t c = kth | (1ull << b);
-            int n = 0;
-            for_each_key(a, sums, keys, [&](uint64_t key) { n += key >= c ? 1 : 0; });
-            __syncthreads();
-            if (threadIdx.x == 0) sh_slots[0] = 0;
-            __syncthreads();
-            if (block_count(n, sh_slots) >= a.n_top) kth = c;
-        }
-        from = kth;
-        __syncthreads();
-        if (threadIdx.x == 0) *sh_total = 0;
-        __syncthreads();
-    }
-}
-
 template <bool TOP>
 __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
     constexpr int kWaves = kThreads / kWave;
     __shared__ float sh_m[kWaves];
     __shared__ double sh_s[kWaves], sh_e[kWaves];
     __shared__ uint64_t sh_sel[kSelect], sh_out[kMaxTop];
-    __shared__ uint32_t sh_largest[kThreads];
+    __shared__ uint32_t sh_group[kGroups];
     __shared__ int sh_count[kThreads], sh_longest[kWaves], sh_slots[1], sh_total;
-    __shared__ RowStats sh_stats;
     const int64_t r = blockIdx.x, row = a.row0 + r;
     const float4 *sums = a.sums + (size_t)r * a.parts;
+    const uint64_t *keys = a.keys + (size_t)r * a.parts * a.capacity;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const float x_id = token_logit(a, row);
     const double beta = scale_of(a.inv_temp, row);
-    // each wave's parts relative to its largest value, then the waves relative to the row's
     float4 q = {-INFINITY, 0.0f, 0.0f, 0.0f};  // the thread's first part
     if ((int)threadIdx.x < a.parts) q = sums[threadIdx.x];
     float m = q.x;
-    int longest = __float_as_int(q.w);
+    uint32_t longest = __float_as_uint(q.w);
     for (int p = threadIdx.x + kThreads; p < a.parts; p += kThreads) {
         m = fmaxf(m, sums[p].x);
-        const int n = __float_as_int(sums[p].w);
+        const uint32_t n = __float_as_uint(sums[p].w);
         longest = n > longest ? n : longest;
-    }
-    if constexpr (TOP) {
-        sh_count[threadIdx.x] = __float_as_int(q.w);
-        longest = (int)wave_max((float)longest);  // at most 1,088: exact
-        if (lane == 0) sh_longest[wave] = longest;
     }
     m = wave_max(m);
     if (lane == 0) sh_m[wave] = m;
-    __syncthreads();
-    int n = 0;
     if constexpr (TOP) {
-        longest = sh_longest[0];
+        sh_count[threadIdx.x] = __float_as_int(q.w);
+        longest = wave_max(longest);
+        if (lane == 0) sh_longest[wave] = (int)longest;
+    }
+    if (threadIdx.x == 0) sh_total = 0;
+    __syncthreads();
+    // the keys: where they are few, all of them in registers, a run of 64 of a part's a load, in flight together
+    uint64_t mine[kHeld];
+    bool held = false;
+    if constexpr (TOP) {
+        int most = sh_longest[0];
 #pragma unroll
-        for (int u = 1; u < kWaves; ++u) longest = sh_longest[u] > longest ? sh_longest[u] : longest;
-        n = gather_keys(a, sums, a.keys + (size_t)r * a.parts * a.capacity, sh_count, longest, sh_sel, sh_largest, sh_slots, &sh_total);
+        for (int u = 1; u < kWaves; ++u) most = sh_longest[u] > most ? sh_longest[u] : most;
+        const int runs = (most + kWave - 1) / kWave;
+        held = a.parts <= kThreads && a.parts * runs <= kHeld * kWaves;
+        if (held) {
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u) {
+                const int c = u * kWaves + wave, p = runs > 0 ? c / runs : a.parts, i = (c - p * runs) * kWave + lane;
+                mine[u] = 0;
+                if (p < a.parts && i < sh_count[p]) mine[u] = keys[(size_t)p * a.capacity + i];
+            }
+        }
     }
     m = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
     double s = 0.0, e = 0.0;  // e in natural units
@@ -566,20 +559,69 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
         sh_s[wave] = s;
         sh_e[wave] = e;
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        s = sh_s[0] + sh_s[1] + sh_s[2] + sh_s[3];
-        e = sh_e[0] + sh_e[1] + sh_e[2] + sh_e[3];
-        sh_stats = write_row(a, row, beta, m, s, e, x_id);
-    }
+    uint64_t from = 0;
     if constexpr (TOP) {
-        n = order_keys(sh_sel, n, a.n_top, sh_largest, &sh_total, sh_out);
-        if ((int)threadIdx.x < a.n_top) write_top(a, row, sh_stats, sh_out, n, threadIdx.x);
+        uint32_t most = 0;
+        auto larger = [&](uint64_t key) {
+            const uint32_t o = (uint32_t)(key >> 32);
+            most = o > most ? o : most;
+        };
+        if (held) {
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u) larger(mine[u]);
+        } else {
+            for_each_key(a, sums, keys, larger);
+        }
+        from = (uint64_t)kth_of_threads<kThreads>(most, a.n_top, sh_group).key << 32;  // (a barrier)
+    } else {
+        __syncthreads();
+    }
+    s = sh_s[0] + sh_s[1] + sh_s[2] + sh_s[3];
+    e = sh_e[0] + sh_e[1] + sh_e[2] + sh_e[3];
+    const RowStats stats = row_stats(beta, m, s);
+    if (threadIdx.x == kThreads - 1) write_row(a, row, stats, s, e, x_id);
+    if constexpr (TOP) {
+        for (;;) {
+            auto put = [&](uint64_t key) {
+                const uint64_t hit = __ballot(key >= from);
+                if (hit == 0) return;
+                int base = 0;
+                if (lane == 0) base = atomicAdd(&sh_total, __popcll(hit));
+                base = __builtin_amdgcn_readfirstlane(base) + lanes_below(hit);
+                if (key >= from && base < kSelect) sh_sel[base] = key;
+            };
+            if (held) {
+#pragma unroll
+                for (int u = 0; u < kHeld; ++u) put(mine[u]);
+            } else {
+                for_each_key(a, sums, keys, put);
+            }
+            __syncthreads();
+            if (sh_total <= kSelect) break;
+            // many equal values: the k-th largest key itself (keys are distinct, so k reach it), by binary search
+            uint64_t kth = 0;
+            for (int b = 63; b >= 0; --b) {
+                const uint64_t c = kth | (1ull << b);
+                int n = 0;
+                for_each_key(a, sums, keys, [&](uint64_t key) { n += key >= c ? 1 : 0; });
+                __syncthreads();
+                if (threadIdx.x == 0) sh_slots[0] = 0;
+                __syncthreads();
+                if (block_count(n, sh_slots) >= a.n_top) kth = c;
+            }
+            from = kth;
+            __syncthreads();
+            if (threadIdx.x == 0) sh_total = 0;
+            __syncthreads();
+        }
+        const int n = order_keys<kThreads>(sh_sel, sh_total, a.n_top, sh_group, &sh_total, sh_out);
+        if ((int)threadIdx.x < a.n_top) write_top(a, row, stats, sh_out, n, threadIdx.x);
     }
 }
 
 struct Plan {
     int parts, part_width;  // of a row; one part: a row's workgroup finishes it
+    int threads;
     int64_t rows;           // of one launch
     size_t sums, total;
 };
@@ -590,7 +632,12 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top) {
     const int chunk = kChunkVectors * kThreads * elements_per_vector(dtype), chunks = (v + chunk - 1) / chunk;
     int64_t parts = n_rows > 0 ? (kFullGrid + n_rows - 1) / n_rows : 1;
     if (parts > chunks) parts = chunks;
+    p.threads = kThreads;
     if (chunks <= kWholeChunks) parts = 1;
+    if (parts > 1 && (n_rows >= kLongRows || (int64_t)v * element_bytes(dtype) <= kLongBytes)) {
+        p.threads = kLongThreads;
+        parts = 1;
+    }
     const int each = (int)((chunks + parts - 1) / parts);
     p.part_width = each * chunk;
     p.parts = (chunks + each - 1) / each;
@@ -606,19 +653,20 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top) {
 }
 
 template <int DT, bool TOP, bool ENTROPY>
-void launch_rows(const RowArgs &a, int64_t n, hipStream_t stream) {
-    if (a.parts == 1) row_stream<DT, TOP, ENTROPY, true><<<(unsigned)n, kThreads, 0, stream>>>(a);
-    else row_stream<DT, TOP, ENTROPY, false><<<(unsigned)(n * a.parts), kThreads, 0, stream>>>(a);
+void launch_rows(const RowArgs &a, int threads, int64_t n, hipStream_t stream) {
+    if (threads == kLongThreads) row_stream<DT, kLongThreads, TOP, ENTROPY, true><<<(unsigned)n, kLongThreads, 0, stream>>>(a);
+    else if (a.parts == 1) row_stream<DT, kThreads, TOP, ENTROPY, true><<<(unsigned)n, kThreads, 0, stream>>>(a);
+    else row_stream<DT, kThreads, TOP, ENTROPY, false><<<(unsigned)(n * a.parts), kThreads, 0, stream>>>(a);
 }
 
 template <int DT>
-void launch_rows(const RowArgs &a, int64_t n, hipStream_t stream) {
+void launch_rows(const RowArgs &a, int threads, int64_t n, hipStream_t stream) {
     if (a.n_top > 0) {
-        if (a.entropy != nullptr) launch_rows<DT, true, true>(a, n, stream);
-        else launch_rows<DT, true, false>(a, n, stream);
+        if (a.entropy != nullptr) launch_rows<DT, true, true>(a, threads, n, stream);
+        else launch_rows<DT, true, false>(a, threads, n, stream);
     } else {
-        if (a.entropy != nullptr) launch_rows<DT, false, true>(a, n, stream);
-        else launch_rows<DT, false, false>(a, n, stream);
+        if (a.entropy != nullptr) launch_rows<DT, false, true>(a, threads, n, stream);
+        else launch_rows<DT, false, false>(a, threads, n, stream);
     }
 }
 
@@ -723,9 +771,9 @@ int launch_logprobs(const LogprobsArgs &l, void *workspace, size_t workspace_byt
     for (int64_t row0 = 0; row0 < l.n_rows; row0 += p.rows) {
         const int64_t n = l.n_rows - row0 < p.rows ? l.n_rows - row0 : p.rows;
         a.row0 = row0;
-        if (l.dtype == TT_BF16) launch_rows<TT_BF16>(a, n, stream);
-        else if (l.dtype == TT_F16) launch_rows<TT_F16>(a, n, stream);
-        else launch_rows<TT_F32>(a, n, stream);
+        if (l.dtype == TT_BF16) launch_rows<TT_BF16>(a, p.threads, n, stream);
+        else if (l.dtype == TT_F16) launch_rows<TT_F16>(a, p.threads, n, stream);
+        else launch_rows<TT_F32>(a, p.threads, n, stream);
         if (hipGetLastError() != hipSuccess) return TT_ELAUNCH;
         if (a.parts == 1) continue;
         if (l.n_top > 0) row_finish<true><<<(unsigned)n, kThreads, 0, stream>>>(a);

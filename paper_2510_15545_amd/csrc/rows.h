@@ -157,6 +157,11 @@ __device__ __forceinline__ double dpp(double x, double none) {
     const uint32_t hi = __builtin_amdgcn_update_dpp((uint32_t)(o >> 32), (uint32_t)(b >> 32), CTRL, ROW_MASK, 0xF, false);
     return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ uint32_t dpp(uint32_t x, uint32_t none) {
+    return __builtin_amdgcn_update_dpp(none, x, CTRL, ROW_MASK, 0xF, false);
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return __builtin_amdgcn_readlane(x, kWave - 1); }
 __device__ __forceinline__ float last_lane(float x) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), kWave - 1)); }
 __device__ __forceinline__ double last_lane(double x) {
     const uint64_t b = __builtin_bit_cast(uint64_t, x);
@@ -164,25 +169,29 @@ __device__ __forceinline__ double last_lane(double x) {
     return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
 
-// The wave's maximum and sum, the same in every lane (prefixes within rows of 16 lanes, then row broadcasts).
-__device__ __forceinline__ float wave_max(float x) {
-    x = fmaxf(x, dpp<0x111, 0xF>(x, -INFINITY));
-    x = fmaxf(x, dpp<0x112, 0xF>(x, -INFINITY));
-    x = fmaxf(x, dpp<0x114, 0xF>(x, -INFINITY));
-    x = fmaxf(x, dpp<0x118, 0xF>(x, -INFINITY));
-    x = fmaxf(x, dpp<0x142, 0xA>(x, -INFINITY));
-    x = fmaxf(x, dpp<0x143, 0xC>(x, -INFINITY));
+// A wave's reduction by f, the same in every lane (prefixes within rows of 16 lanes, then row broadcasts).
+template <typename T, typename F>
+__device__ __forceinline__ T wave_reduce(T x, T none, F f) {
+    x = f(x, dpp<0x111, 0xF>(x, none));
+    x = f(x, dpp<0x112, 0xF>(x, none));
+    x = f(x, dpp<0x114, 0xF>(x, none));
+    x = f(x, dpp<0x118, 0xF>(x, none));
+    x = f(x, dpp<0x142, 0xA>(x, none));
+    x = f(x, dpp<0x143, 0xC>(x, none));
     return last_lane(x);
 }
-template <typename F>
-__device__ __forceinline__ F wave_sum(F x) {
-    x += dpp<0x111, 0xF>(x, F(0));
-    x += dpp<0x112, 0xF>(x, F(0));
-    x += dpp<0x114, 0xF>(x, F(0));
-    x += dpp<0x118, 0xF>(x, F(0));
-    x += dpp<0x142, 0xA>(x, F(0));
-    x += dpp<0x143, 0xC>(x, F(0));
-    return last_lane(x);
+__device__ __forceinline__ float wave_max(float x) {
+    return wave_reduce(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    return wave_reduce(x, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+__device__ __forceinline__ uint32_t wave_min(uint32_t x) {
+    return wave_reduce(x, 0xFFFFFFFFu, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+template <typename T>
+__device__ __forceinline__ T wave_sum(T x) {
+    return wave_reduce(x, T(0), [](T a, T b) { return a + b; });
 }
 
 // Unsigned keys in the order of the values (-0 as +0, minus infinity lowest, no NaN).
