@@ -423,73 +423,81 @@ LogProbs.__doc__ = """What logprobs() returns, float32 (top_ids int32) device te
 the given tokens, lse [n], stats [n, 2] for logprobs_backward(), entropy [n], top_ids and top_logprobs [n, n_top]."""
 
 
-def _row_type(t, name):
-    """TT_BF16, TT_F16 or TT_F32 of a 2-D row-major device tensor."""
-    if t.dim() != 2 or t.stride(1) != 1 or not t.is_cuda:
+def _rows(t, v: int, n: int, name):
+    """(type, address, stride) of the rows of a 2-D row-major device tensor, at least n of at least v columns."""
+    code = _DTYPE_CODES.get(t.dtype)
+    if t.dim() != 2 or not t.is_cuda or t.stride(1) != 1:
         raise ValueError(f"{name} must be a 2-D row-major device tensor")
-    dtype = t.dtype
-    if dtype is torch.bfloat16:
-        return 0
-    if dtype is torch.float16:
-        return 1
-    if dtype is torch.float32:
-        return 2
-    raise ValueError(f"{name} must be bfloat16, float16 or float32, got {dtype}")
-
-
-def _rows_at(t, v: int, n: int, name):
-    """(address, stride) of rows of at least v columns, n of them at least."""
-    if t.shape[1] < v or t.shape[0] < n:
+    if code is None:
+        raise ValueError(f"{name} must be bfloat16, float16 or float32, got {t.dtype}")
+    rows, columns = t.shape
+    if columns < v or rows < n:
         raise ValueError(f"{name} must have at least {n} rows of {v}")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), v))
+    return code, t.data_ptr(), (t.stride(0) if rows > 1 else max(t.stride(0), v))
 
 
-def _sized(t, dtype, name, n: int, allow_none=False):
-    """_ptr of a tensor of n elements (an empty one of a call on no rows: None)."""
-    if t is not None and t.numel() != n:
+def _array(t, dtype, n: int, name, device: int):
+    """The address of a contiguous tensor of n elements on that device (None: NULL, and so is an empty tensor)."""
+    if t is None:
+        return None
+    if t.get_device() == device and t.dtype is dtype and t.numel() == n and t.is_contiguous():
+        return t.data_ptr() or None
+    address = _ptr(t, dtype, name)
+    if t.numel() != n:
         raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
-    return _ptr(t, dtype, name, allow_none) or None
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the logits on cuda:{device}")
+    return address or None
 
 
-def _same_device(first, stream, *others):
-    """The device the call runs on (the stream's, or the current one) has to hold every tensor."""
-    device = first.device
-    for t in others:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensors on {device} and {t.device} in one call")
+def _launch_device(t, stream) -> int:
+    """The logits' device, which has to be the one that the call runs on: the stream's, or the current one."""
+    device = t.get_device()
     if stream is None:
-        if device.index != torch.cuda.current_device():
-            raise ValueError(f"tensors on {device}, but the current device is cuda:{torch.cuda.current_device()}")
-    elif getattr(stream, "device", device) != device:
-        raise ValueError(f"tensors on {device}, but the stream belongs to {stream.device}")
+        if device != torch.cuda.current_device():
+            raise ValueError(f"tensors on cuda:{device}, but the current device is cuda:{torch.cuda.current_device()}")
+    elif getattr(stream, "device_index", device) != device:
+        raise ValueError(f"tensors on cuda:{device}, but the stream belongs to cuda:{stream.device_index}")
+    return device
 
 
-def _given_workspace(workspace, nbytes: int):
+def _needed_workspace(workspace, nbytes: int, device: int):
     """(address, bytes) of the caller's workspace, or of nbytes on the current stream (held by the third)."""
     if workspace is None:
-        workspace = torch.empty(max(1, nbytes), dtype=torch.uint8, device="cuda")
-        return workspace.data_ptr(), nbytes, workspace
-    if not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous device tensor")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+        if nbytes == 0:
+            return None, 0, None
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the logits' device")
+    return workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), workspace
 
 
-_DTYPE_CODES = {"bfloat16": 0, "float16": 1, "float32": 2}
+class _TypeCodes(dict):
+    """TT_BF16, TT_F16 and TT_F32 by torch's types, filled at the first use (torch is imported then)."""
+
+    def get(self, dtype):
+        if not self:
+            self.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
+        return dict.get(self, dtype)
+
+
+_DTYPE_CODES = _TypeCodes()
 
 
 def _dtype_code(dtype) -> int:
-    code = _DTYPE_CODES.get(str(dtype).replace("torch.", ""))
+    code = _DTYPE_CODES.get(dtype)
     if code is None:
-        raise ValueError(f"dtype must be bfloat16, float16 or float32, got {dtype}")
+        raise ValueError(f"dtype must be torch.bfloat16, torch.float16 or torch.float32, got {dtype}")
     return code
 
 
 def logprobs_workspace(n_rows: int, v: int, dtype, n_top: int = 0, device="cuda"):
-    """A workspace for logprobs on n_rows rows of v logits of this type, reusable by calls that do not overlap in time."""
+    """A workspace for logprobs on n_rows rows of v logits of this type (empty when none is needed), reusable by calls
+    that do not overlap in time."""
     n = ctypes.c_size_t(0)
     _check(lib().tt_logprobs_workspace_size(int(n_rows), int(v), _dtype_code(dtype), int(n_top), ctypes.byref(n)),
            "tt_logprobs_workspace_size")
-    return torch.empty(max(1, n.value), dtype=torch.uint8, device=device)
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
 
 
 def logprobs(v: int, logits, ids=None, inv_temperature=None, n_top: int = 0, entropy: bool = False, out=None,
@@ -502,22 +510,25 @@ def logprobs(v: int, logits, ids=None, inv_temperature=None, n_top: int = 0, ent
     if stream is not None and (out is None or workspace is None):
         return _on_stream(stream, logprobs, v, logits, ids, inv_temperature, n_top, entropy, out, workspace, None)
     i32, f32 = torch.int32, torch.float32
-    v, n_top, code = int(v), int(n_top), _row_type(logits, "logits")
-    n = logits.shape[0]
-    address, ld = _rows_at(logits, v, n, "logits")
-    dev = logits.device
+    v, n_top, n = int(v), int(n_top), logits.shape[0]
+    code, address, ld = _rows(logits, v, n, "logits")
+    dev = _launch_device(logits, stream)
     if out is None:
-        new = lambda *s: torch.empty(s, dtype=f32, device=dev)  # noqa: E731
-        out = LogProbs(None if ids is None else new(n), new(n), new(n, 2), new(n) if entropy else None,
-                       torch.empty((n, n_top), dtype=i32, device=dev) if n_top else None, new(n, n_top) if n_top else None)
-    _same_device(logits, stream, ids, inv_temperature, workspace, *out)
-    ws, ws_bytes, _held = _given_workspace(workspace, _spread_bytes("tt_logprobs_workspace_size", n, v, code, n_top))
-    st = lib().tt_logprobs(n, v, code, address, ld, _sized(inv_temperature, f32, "inv_temperature", n, True),
-                           _sized(ids, i32, "ids", n, True), n_top, _sized(out[0], f32, "logprob", n, True),
-                           _sized(out[1], f32, "lse", n, True), _sized(out[2], f32, "stats", 2 * n, True),
-                           _sized(out[3], f32, "entropy", n, True), _sized(out[4], i32, "top_ids", n * n_top, not n_top),
-                           _sized(out[5], f32, "top_logprobs", n * n_top, not n_top), ws, ws_bytes, _stream_handle(stream))
-    _check(st, "tt_logprobs")
+        on = logits.device
+        out = LogProbs(None if ids is None else torch.empty(n, dtype=f32, device=on), torch.empty(n, dtype=f32, device=on),
+                       torch.empty((n, 2), dtype=f32, device=on), torch.empty(n, dtype=f32, device=on) if entropy else None,
+                       torch.empty((n, n_top), dtype=i32, device=on) if n_top > 0 else None,
+                       torch.empty((n, n_top), dtype=f32, device=on) if n_top > 0 else None)
+        to = [None if t is None else t.data_ptr() for t in out]
+    else:
+        to = [_array(out[0], f32, n, "logprob", dev), _array(out[1], f32, n, "lse", dev), _array(out[2], f32, 2 * n, "stats", dev),
+              _array(out[3], f32, n, "entropy", dev), _array(out[4], i32, n * n_top, "top_ids", dev),
+              _array(out[5], f32, n * n_top, "top_logprobs", dev)]
+    ws, ws_bytes, _held = _needed_workspace(workspace, _spread_bytes("tt_logprobs_workspace_size", n, v, code, n_top), dev)
+    st = lib().tt_logprobs(n, v, code, address, ld, _array(inv_temperature, f32, n, "inv_temperature", dev),
+                           _array(ids, i32, n, "ids", dev), n_top, *to, ws, ws_bytes, _stream_handle(stream))
+    if st:
+        _check(st, "tt_logprobs")
     return out
 
 
@@ -531,30 +542,32 @@ def logprobs_backward(v: int, logits, ids, stats, grad_logprob, entropy=None, gr
         return _on_stream(stream, logprobs_backward, v, logits, ids, stats, grad_logprob, entropy, grad_entropy,
                           inv_temperature, None, None)
     i32, f32 = torch.int32, torch.float32
-    v, code = int(v), _row_type(logits, "logits")
-    n = logits.shape[0]
-    address, ld = _rows_at(logits, v, n, "logits")
+    v, n = int(v), logits.shape[0]
+    code, address, ld = _rows(logits, v, n, "logits")
+    dev = _launch_device(logits, stream)
     if out is None:
         out = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
-    if _row_type(out, "out") != code:
-        raise ValueError(f"out must be {logits.dtype}, got {out.dtype}")
-    to, out_ld = _rows_at(out, v, n, "out")
-    _same_device(logits, stream, ids, stats, grad_logprob, entropy, grad_entropy, inv_temperature, out)
-    st = lib().tt_logprobs_backward(n, v, code, address, ld, _sized(inv_temperature, f32, "inv_temperature", n, True),
-                                    _sized(ids, i32, "ids", n, True), _sized(stats, f32, "stats", 2 * n),
-                                    _sized(entropy, f32, "entropy", n, True),
-                                    _sized(grad_logprob, f32, "grad_logprob", n, True),
-                                    _sized(grad_entropy, f32, "grad_entropy", n, True), to, out_ld, _stream_handle(stream))
-    _check(st, "tt_logprobs_backward")
+    out_code, to, out_ld = _rows(out, v, n, "out")
+    if out_code != code or out.get_device() != dev:
+        raise ValueError(f"out must be {logits.dtype} on the logits' device")
+    if stats is None:
+        raise ValueError("stats is required")
+    st = lib().tt_logprobs_backward(n, v, code, address, ld, _array(inv_temperature, f32, n, "inv_temperature", dev),
+                                    _array(ids, i32, n, "ids", dev), _array(stats, f32, 2 * n, "stats", dev),
+                                    _array(entropy, f32, n, "entropy", dev), _array(grad_logprob, f32, n, "grad_logprob", dev),
+                                    _array(grad_entropy, f32, n, "grad_entropy", dev), to, out_ld, _stream_handle(stream))
+    if st:
+        _check(st, "tt_logprobs_backward")
     return out
 
 
 def distill_workspace(n_rows: int, v: int, dtype, n_top: int, grad: bool = False, device="cuda"):
-    """A workspace for distill with these bounds, reusable by calls that do not overlap in time."""
+    """A workspace for distill with these bounds (empty when none is needed), reusable by calls that do not overlap in
+    time."""
     n = ctypes.c_size_t(0)
     _check(lib().tt_distill_workspace_size(int(n_rows), int(v), _dtype_code(dtype), int(n_top), 1 if grad else 0,
                                            ctypes.byref(n)), "tt_distill_workspace_size")
-    return torch.empty(max(1, n.value), dtype=torch.uint8, device=device)
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
 
 
 def distill(v: int, logits, top_ids, top_logprobs, tail: bool = False, id_map=None, inv_temperature=None, grad_loss=None,
@@ -570,34 +583,35 @@ def distill(v: int, logits, top_ids, top_logprobs, tail: bool = False, id_map=No
         return _on_stream(stream, distill, v, logits, top_ids, top_logprobs, tail, id_map, inv_temperature, grad_loss,
                           loss, dlogits, workspace, None)
     i32, f32 = torch.int32, torch.float32
-    v, code = int(v), _row_type(logits, "logits")
-    n = logits.shape[0]
-    address, ld = _rows_at(logits, v, n, "logits")
+    v, n = int(v), logits.shape[0]
+    code, address, ld = _rows(logits, v, n, "logits")
+    dev = _launch_device(logits, stream)
     if top_ids.dim() != 2 or top_ids.shape != top_logprobs.shape:
         raise ValueError("top_ids and top_logprobs must be 2-D tensors of one shape")
-    n_top = top_ids.shape[1]
-    if id_map is not None and id_map.numel() == 0:
-        raise ValueError("id_map must not be empty")
+    n_top, n_map = top_ids.shape[1], 0
+    if id_map is not None:
+        n_map = id_map.numel()
+        if n_map == 0:
+            raise ValueError("id_map must not be empty")
     if loss is None:
         loss = torch.empty(n, dtype=f32, device=logits.device)
     to, out_ld = None, 0
     if grad_loss is not None:
         if dlogits is None:
             dlogits = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
-        if _row_type(dlogits, "dlogits") != code:
-            raise ValueError(f"dlogits must be {logits.dtype}, got {dlogits.dtype}")
-        to, out_ld = _rows_at(dlogits, v, n, "dlogits")
+        out_code, to, out_ld = _rows(dlogits, v, n, "dlogits")
+        if out_code != code or dlogits.get_device() != dev:
+            raise ValueError(f"dlogits must be {logits.dtype} on the logits' device")
     elif dlogits is not None:
         raise ValueError("dlogits needs grad_loss")
-    _same_device(logits, stream, top_ids, top_logprobs, id_map, inv_temperature, grad_loss, loss, dlogits, workspace)
     nbytes = _spread_bytes("tt_distill_workspace_size", n, v, code, n_top, 0 if grad_loss is None else 1)
-    ws, ws_bytes, _held = _given_workspace(workspace, nbytes)
-    st = lib().tt_distill(n, v, code, address, ld, _sized(inv_temperature, f32, "inv_temperature", n, True), n_top,
-                          _sized(top_ids, i32, "top_ids", n * n_top), _sized(top_logprobs, f32, "top_logprobs", n * n_top),
-                          _ptr(id_map, i32, "id_map", True), 0 if id_map is None else id_map.numel(), 1 if tail else 0,
-                          _sized(loss, f32, "loss", n), _sized(grad_loss, f32, "grad_loss", n, True), to, out_ld, ws,
-                          ws_bytes, _stream_handle(stream))
-    _check(st, "tt_distill")
+    ws, ws_bytes, _held = _needed_workspace(workspace, nbytes, dev)
+    st = lib().tt_distill(n, v, code, address, ld, _array(inv_temperature, f32, n, "inv_temperature", dev), n_top,
+                          _array(top_ids, i32, n * n_top, "top_ids", dev), _array(top_logprobs, f32, n * n_top, "top_logprobs", dev),
+                          _array(id_map, i32, n_map, "id_map", dev), n_map, 1 if tail else 0, _array(loss, f32, n, "loss", dev),
+                          _array(grad_loss, f32, n, "grad_loss", dev), to, out_ld, ws, ws_bytes, _stream_handle(stream))
+    if st:
+        _check(st, "tt_distill")
     return loss, dlogits
 
 

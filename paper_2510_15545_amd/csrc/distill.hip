@@ -425,7 +425,7 @@ __global__ __launch_bounds__(kThreads) void list_grad(ListArgs a, int parts) {
 constexpr int kLongThreads = 1024, kLongVectors = 2;
 constexpr int64_t kShortRow = 32 << 10;          // bytes of a row that kThreads threads take whole
 constexpr int64_t kSplitRow = 128 << 10;         // and of one that is split where there are few rows
-constexpr int64_t kFewRows = 256;                // fewer leave compute units without a row
+constexpr int64_t kFewRows = 96;                 // fewer long rows leave too many compute units without one
 constexpr size_t kCachedBytes = size_t(96) << 20;  // logits of a group of split rows, with the gradient
 
 struct Plan {

@@ -172,8 +172,8 @@ def test_many_rows_with_alternatives_take_several_groups():
     import paper_2510_15545_amd as tt
 
     n, v = 3300, 65540
-    one = tt.logprobs_workspace(1, v, "bfloat16", 128).numel()
-    assert tt.logprobs_workspace(n, v, "bfloat16", 128).numel() < n * one // 2
+    one = tt.logprobs_workspace(1, v, torch.bfloat16, 128).numel()
+    assert tt.logprobs_workspace(n, v, torch.bfloat16, 128).numel() < n * one // 2
     rows = torch.randn((n, v), device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).mul_(3).bfloat16()
     ids = torch.randint(0, v, (n,), device="cuda", dtype=torch.int32)
     got = tt.logprobs(v, rows, ids, n_top=128, entropy=True)

@@ -99,38 +99,39 @@ def test_host_tensors_and_wrong_shapes_are_refused():
         tt.distill_workspace(2, 8, "int8", 4)
 
 
-def fake(shape=(2, 8), dtype=torch.bfloat16, device=0, strides=None, numel=None):
+def fake(shape=(2, 8), dtype=torch.bfloat16, device=0, strides=None, contiguous=True):
     strides = strides or (shape[-1], 1)
     n = 1
     for s in shape:
         n *= s
     return types.SimpleNamespace(dim=lambda: len(shape), stride=lambda i: strides[i], is_cuda=True, dtype=dtype, shape=shape,
-                                 numel=lambda: n if numel is None else numel, is_contiguous=lambda: True, data_ptr=lambda: PTR,
-                                 element_size=lambda: 2, device=types.SimpleNamespace(type="cuda", index=device))
+                                 numel=lambda: n, is_contiguous=lambda: contiguous, data_ptr=lambda: PTR, element_size=lambda: 2,
+                                 get_device=lambda: device)
 
 
 def test_devices_and_shapes_of_device_tensors(monkeypatch):
-    """Tensors of another device than the current one or the stream's, of another size or type: refused by the binding."""
+    """Tensors of another device than the current one or the stream's, of another size, type or layout: refused by the binding."""
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    d0 = fake().device
-    a = fake()
-    a.device = d0
-    tt._same_device(a, None)
+    assert tt._launch_device(fake(), None) == 0
     with pytest.raises(ValueError, match="current device"):
-        tt._same_device(fake(device=1), None)
-    b = fake(device=1)
-    with pytest.raises(ValueError, match="in one call"):
-        tt._same_device(a, None, b)
+        tt._launch_device(fake(device=1), None)
     with pytest.raises(ValueError, match="stream belongs"):
-        tt._same_device(a, types.SimpleNamespace(cuda_stream=1, device=b.device))
-    tt._same_device(a, types.SimpleNamespace(cuda_stream=1))
-    with pytest.raises(ValueError, match="bfloat16, float16 or float32"):
-        tt._row_type(fake(dtype=torch.float64), "logits")
-    with pytest.raises(ValueError, match="row-major"):
-        tt._row_type(fake(strides=(1, 2)), "logits")
-    with pytest.raises(ValueError, match="at least"):
-        tt._rows_at(fake(), 9, 2, "logits")
-    with pytest.raises(ValueError, match="elements"):
-        tt._sized(fake(shape=(3,), dtype=torch.int32), torch.int32, "ids", 2)
+        tt._launch_device(fake(), types.SimpleNamespace(cuda_stream=1, device_index=1))
+    assert tt._launch_device(fake(device=1), types.SimpleNamespace(cuda_stream=1, device_index=1)) == 1
+    assert tt._launch_device(fake(), types.SimpleNamespace(cuda_stream=1)) == 0
+    assert tt._rows(fake(), 8, 2, "logits") == (0, PTR, 8)
+    assert tt._rows(fake(shape=(1, 9), strides=(1, 1), dtype=torch.float32), 8, 1, "logits") == (2, PTR, 8)
+    for bad, why in ((dict(dtype=torch.float64), "bfloat16, float16 or float32"), (dict(strides=(1, 2)), "row-major"),
+                     (dict(shape=(2, 7)), "at least"), (dict(shape=(1, 8)), "at least"), (dict(shape=(16,), strides=(1, 1)), "row-major")):
+        with pytest.raises(ValueError, match=why):
+            tt._rows(fake(**bad), 8, 2, "logits")
+    ids = dict(shape=(2,), dtype=torch.int32)
+    assert tt._array(fake(**ids), torch.int32, 2, "ids", 0) == PTR and tt._array(None, torch.int32, 2, "ids", 0) is None
+    for bad, why in ((dict(ids, shape=(3,)), "elements"), (dict(ids, dtype=torch.int64), "int32"), (dict(ids, contiguous=False), "contiguous"),
+                     (dict(ids, device=1), "cuda:1")):
+        with pytest.raises(ValueError, match=why):
+            tt._array(fake(**bad), torch.int32, 2, "ids", 0)
+    with pytest.raises(ValueError, match="workspace"):
+        tt._needed_workspace(fake(device=1), 16, 0)
     with pytest.raises(ValueError, match="required"):
-        tt._sized(None, torch.float32, "stats", 2)
+        tt.logprobs_backward(8, fake(), fake(**ids), None, fake(shape=(2,), dtype=torch.float32), out=fake())
