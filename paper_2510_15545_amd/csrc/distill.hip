@@ -238,11 +238,11 @@ __device__ __forceinline__ void take_out(uint32_t (&w)[NV][4], const uint32_t *s
     }
 }
 
-// Words of a bitmap over `width` tokens that whole chunks may ask for.
+// Words of a bitmap over `width` tokens, after a row's lead, that whole chunks may ask for.
 template <int DT, int NV, int THREADS>
 __host__ __device__ __forceinline__ int bitmap_words(int width) {
     constexpr int kChunk = NV * THREADS * Elem<DT>::kPer;
-    return (width + kChunk - 1) / kChunk * (kChunk / 32);
+    return (width + kLead + kChunk - 1) / kChunk * (kChunk / 32);
 }
 
 // Gradients of the unlisted tokens of elements x0 .. x1 - 1, from what get() returns (called once the first loads
@@ -255,18 +255,19 @@ __device__ __forceinline__ void write_grad(const ListArgs &a, int64_t row_i, int
     T *out = static_cast<T *>(a.out) + row_i * a.out_ld;
     RowGrad q;
     for_chunks<DT, NV, THREADS, true, true, 1>(row, a.v, x0, x1, [&] { q = get(); }, [&](uint32_t(&w)[NV][4], int x) {
-        auto store = [&](auto exponent) {
+        auto form = [&](auto exponent) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 float d[kPer];
 #pragma unroll
                 for (int j = 0; j < kPer; ++j)
                     d[j] = q.factor * fminf(fmaxf(__builtin_amdgcn_exp2f(exponent(value<DT>(w[i], j))), 0.0f), 1.0f);
-                store_vector<DT>(out, vector_at<DT, THREADS>(x, i), a.v, d);
+                encode_vector<DT>(d, w[i]);
             }
         };
-        if (q.m == 0.0f) store([&](float y) { return fmaf(y, q.c2, -q.shift); });
-        else store([&](float y) { return (y - q.m) * q.c2 - q.shift; });
+        if (q.m == 0.0f) form([&](float y) { return fmaf(y, q.c2, -q.shift); });
+        else form([&](float y) { return (y - q.m) * q.c2 - q.shift; });
+        store_chunk<DT, NV, THREADS>(out, a.v, x, w);
     });
 }
 
@@ -283,6 +284,7 @@ __global__ __launch_bounds__(THREADS) void list_whole(ListArgs a) {
     const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const float c2 = scale_of(a.inv_temp, row_i) * kLog2e;
+    const int x0 = -lead_of<DT>(GRAD ? static_cast<const void *>(static_cast<T *>(a.out) + row_i * a.out_ld) : row, a.v);
     List list;
     Sum mine = {-INFINITY, 0.0f, 0.0f};
     auto read = [&] {
@@ -295,16 +297,17 @@ __global__ __launch_bounds__(THREADS) void list_whole(ListArgs a) {
 #pragma unroll
             for (int u = 0; u < kSlots; ++u) {
                 if (list.id[u] < 0) continue;
-                const uint32_t bit = 1u << (list.id[u] % 32);
-                repeated = (atomicOr(&sh_bits[list.id[u] / 32], bit) & bit) != 0 || repeated;
+                const int at = list.id[u] - x0;
+                const uint32_t bit = 1u << (at % 32);
+                repeated = (atomicOr(&sh_bits[at / 32], bit) & bit) != 0 || repeated;
             }
         }
         __syncthreads();
         if (wave == 0) weigh_list(a, list, lp, __ballot(repeated) != 0);
     };
-    for_chunks<DT, NV, THREADS, !GRAD, false, 1>(row, a.v, 0, a.v, read, [&](uint32_t(&w)[NV][4], int x) {
+    for_chunks<DT, NV, THREADS, !GRAD, false, 1>(row, a.v, x0, a.v, read, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
-        take_out<DT, NV, THREADS>(w, sh_bits, x, 0);
+        take_out<DT, NV, THREADS>(w, sh_bits, x, x0);
         add_chunk<DT, NV, false>(w, c2, mine, vm);
     });
     mine = wave_join<false>(mine, c2);
@@ -328,7 +331,7 @@ __global__ __launch_bounds__(THREADS) void list_whole(ListArgs a) {
         return sh_grad;
     };
     if constexpr (GRAD) {
-        write_grad<DT, NV, THREADS>(a, row_i, 0, a.v, finish);
+        write_grad<DT, NV, THREADS>(a, row_i, x0, a.v, finish);
         // the listed tokens over what was just written: after the workgroup's stores
         __syncthreads();
         if ((int)threadIdx.x < a.n_top) {
@@ -348,16 +351,16 @@ __global__ __launch_bounds__(kThreads) void list_parts(ListArgs a) {
     __shared__ Sum sh_sum[kWaves];
     pass_over_nans();
     const int64_t r = blockIdx.x / (uint32_t)a.parts, row_i = a.row0 + r;
-    const int part = blockIdx.x % (uint32_t)a.parts, x0 = part * a.part_width;
-    const int x1 = x0 + a.part_width < a.v ? x0 + a.part_width : a.v;
+    const int part = blockIdx.x % (uint32_t)a.parts;
     const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
+    const int x0 = part * a.part_width - lead_of<DT>(row, a.v), x1 = part + 1 == a.parts ? a.v : x0 + a.part_width;
     const float c2 = scale_of(a.inv_temp, row_i) * kLog2e;
     auto read = [&] {
         for (int i = threadIdx.x; i < bitmap_words<DT, NV, kThreads>(x1 - x0); i += kThreads) sh_bits[i] = 0;
         __syncthreads();
         if ((int)threadIdx.x < a.n_top) {
-            const int at = entry_id(a, row_i, threadIdx.x, a.logprobs[row_i * a.n_top + threadIdx.x]) - x0;
-            if (at >= 0 && at < x1 - x0) atomicOr(&sh_bits[at / 32], 1u << (at % 32));
+            const int id = entry_id(a, row_i, threadIdx.x, a.logprobs[row_i * a.n_top + threadIdx.x]), at = id - x0;
+            if (id >= 0 && at >= 0 && at < x1 - x0) atomicOr(&sh_bits[at / 32], 1u << (at % 32));
         }
         __syncthreads();
     };
@@ -412,13 +415,15 @@ __global__ __launch_bounds__(kThreads) void list_grad(ListArgs a, int parts) {
     using T = typename Elem<DT>::T;
     constexpr int kPart = kChunkVectors * kThreads * Elem<DT>::kPer;
     const int64_t r = blockIdx.x / (uint32_t)parts, row_i = a.row0 + r;
-    const int x0 = (int)(blockIdx.x % (uint32_t)parts) * kPart, x1 = x0 + kPart < a.v ? x0 + kPart : a.v;
+    const int part = (int)(blockIdx.x % (uint32_t)parts);
+    T *out = static_cast<T *>(a.out) + row_i * a.out_ld;
+    const int x0 = part * kPart - lead_of<DT>(out, a.v), x1 = part + 1 == parts ? a.v : x0 + kPart;
     Entry mine = {-1, 0.0f};
     if ((int)threadIdx.x < a.n_top) mine = a.entries[(size_t)r * a.n_top + threadIdx.x];
     write_grad<DT, kChunkVectors, kThreads>(a, row_i, x0, x1, [&] { return a.row_grad[r]; });
     // the listed tokens over what was just written: after the workgroup's stores
     __syncthreads();
-    if (mine.id >= x0 && mine.id < x1) (static_cast<T *>(a.out) + row_i * a.out_ld)[mine.id] = (T)encode<DT>(mine.grad);
+    if (mine.id >= 0 && mine.id >= x0 && mine.id < x1) out[mine.id] = (T)encode<DT>(mine.grad);
 }
 
 // Threads and vectors of list_whole for rows of these bytes.
@@ -441,7 +446,7 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
     const int chunk = kChunkVectors * kThreads * elements_per_vector(dtype), chunks = (v + chunk - 1) / chunk;
     int64_t most = kMaxGrid;
     if (v <= kMaxBits && (n_rows >= kFewRows || bytes <= kSplitRow)) {
-        p.threads = bytes <= kShortRow || (!grad && n_rows >= kFullGrid) ? kThreads : kLongThreads;
+        p.threads = bytes <= kShortRow || (!grad && n_rows >= many_rows(bytes)) ? kThreads : kLongThreads;
     } else {
         int64_t parts = n_rows > 0 ? (kFullGrid + n_rows - 1) / n_rows : 1;
         const int64_t least = (v + kMaxBits - 1) / kMaxBits;

@@ -312,7 +312,7 @@ struct TopSet {
         const int total = sh.total;
         if (total > capacity) {
             __syncthreads();
-            select_exactly<DT, THREADS>(row, x0, x1, k, dst, sh.slots, &sh.total);
+            select_exactly<DT, THREADS>(row, x0 > 0 ? x0 : 0, x1, k, dst, sh.slots, &sh.total);
             return k;
         }
         for (int i = lane; i - lane < staged; i += kWave) {
@@ -432,8 +432,8 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stre
     pass_over_nans();
     const int64_t r = FINISH ? blockIdx.x : blockIdx.x / (uint32_t)a.parts, row_i = a.row0 + r;
     const int part = FINISH ? 0 : blockIdx.x % (uint32_t)a.parts, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int x0 = part * a.part_width, x1 = x0 + a.part_width < a.v ? x0 + a.part_width : a.v;
     const auto *row = static_cast<const typename Elem<DT>::T *>(a.logits) + row_i * a.ld;
+    const int x0 = part * a.part_width - lead_of<DT>(row, a.v), x1 = FINISH || part + 1 == a.parts ? a.v : x0 + a.part_width;
     const float beta = scale_of(a.inv_temp, row_i), c2 = beta * kLog2e;
     const float x_id = FINISH ? token_logit(a, row_i) : 0.0f;
     int count = 0;
@@ -630,13 +630,13 @@ struct Plan {
 Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top) {
     Plan p;
     const int chunk = kChunkVectors * kThreads * elements_per_vector(dtype), chunks = (v + chunk - 1) / chunk;
-    int64_t parts = n_rows > 0 ? (kFullGrid + n_rows - 1) / n_rows : 1;
-    if (parts > chunks) parts = chunks;
+    int64_t parts = 1;
     p.threads = kThreads;
-    if (chunks <= kWholeChunks) parts = 1;
-    if (parts > 1 && (n_rows >= kLongRows || (int64_t)v * element_bytes(dtype) <= kLongBytes)) {
-        p.threads = kLongThreads;
-        parts = 1;
+    const int64_t bytes = (int64_t)v * element_bytes(dtype);
+    if (chunks > kWholeChunks && n_rows < many_rows(bytes)) {
+        if (n_rows >= kLongRows || bytes <= kLongBytes) p.threads = kLongThreads;
+        else parts = n_rows > 0 ? (kFullGrid + n_rows - 1) / n_rows : 1;
+        if (parts > chunks) parts = chunks;
     }
     const int each = (int)((chunks + parts - 1) / parts);
     p.part_width = each * chunk;
@@ -689,7 +689,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(GradArgs a) {
     using T = typename Elem<DT>::T;
     constexpr int kPer = Elem<DT>::kPer, kPart = kGradVectors * kThreads * kPer;
     const int64_t r = a.row0 + blockIdx.x / (uint32_t)a.parts;
-    const int x_part = (int)(blockIdx.x % (uint32_t)a.parts) * kPart;
+    const int part = (int)(blockIdx.x % (uint32_t)a.parts);
     const T *row = static_cast<const T *>(a.logits) + r * a.ld;
     T *out = static_cast<T *>(a.out) + r * a.out_ld;
     const int32_t id = a.ids == nullptr ? -1 : a.ids[r];
@@ -697,18 +697,17 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(GradArgs a) {
     const float g = given && a.g != nullptr ? a.g[r] : 0.0f;
     const float h = ENTROPY ? a.h[r] : 0.0f;
     const float m = a.stats[2 * r], log_sum = a.stats[2 * r + 1];
-    const int x_end = x_part + kPart < a.v ? x_part + kPart : a.v;
+    const int x0 = part * kPart - lead_of<DT>(out, a.v), x1 = part + 1 == a.parts ? a.v : x0 + kPart;
     if ((g == 0.0f && h == 0.0f) || m == -INFINITY) {
-        const float d[kPer] = {};
-#pragma unroll
-        for (int i = 0; i < kGradVectors; ++i) store_vector<DT>(out, vector_at<DT, kThreads>(x_part, i), a.v, d);
+        const uint32_t none[kGradVectors][4] = {};
+        for (int x = x0; x < x1; x += kPart) store_chunk<DT, kGradVectors, kThreads>(out, a.v, x, none);
         return;
     }
     const float beta = scale_of(a.inv_temp, r), c2 = beta * kLog2e, l2 = log_sum * kLog2e;
     const float ent = ENTROPY ? a.entropy[r] : 0.0f;
     // d = p (first + second t), t = lp / ln 2 held above -200 (p is 0 there); NaN statistics make it NaN
     const float first = -beta * (g + h * ent) + (log_sum - log_sum), second = ENTROPY ? -beta * h * (float)kLn2 : 0.0f;
-    for_chunks<DT, kGradVectors, kThreads, true, false, 1>(row, a.v, x_part, x_end, [] {}, [&](uint32_t(&w)[kGradVectors][4], int x_chunk) {
+    for_chunks<DT, kGradVectors, kThreads, true, false, 1>(row, a.v, x0, x1, [] {}, [&](uint32_t(&w)[kGradVectors][4], int x_chunk) {
 #pragma unroll
         for (int i = 0; i < kGradVectors; ++i) {
             const int x = vector_at<DT, kThreads>(x_chunk, i);
@@ -720,18 +719,17 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(GradArgs a) {
                 d[j] = p * (ENTROPY ? fmaf(second, t, first) : first);
             }
             if (given && id >= x && id < x + kPer) {  // the token itself: 1 - p from its log probability
+                float y = 0.0f;
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    if (id == x + j) {
-                        const float y = value<DT>(w[i], j);
-                        const float lp = y == y ? (y - m) * beta - log_sum : -INFINITY;
-                        const float rest = -expm1f(lp);
-                        d[j] = beta * (g * rest - (ENTROPY ? h * expf(lp) * (fmaxf(lp, kLowest) + ent) : 0.0f)) + (log_sum - log_sum);
-                    }
-                }
+                for (int j = 0; j < kPer; ++j) y = id == x + j ? value<DT>(w[i], j) : y;
+                const float lp = y == y ? (y - m) * beta - log_sum : -INFINITY, rest = -expm1f(lp);
+                const float own = beta * (g * rest - (ENTROPY ? h * expf(lp) * (fmaxf(lp, kLowest) + ent) : 0.0f)) + (log_sum - log_sum);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) d[j] = id == x + j ? own : d[j];
             }
-            store_vector<DT>(out, x, a.v, d);
+            encode_vector<DT>(d, w[i]);
         }
+        store_chunk<DT, kGradVectors, kThreads>(out, a.v, x_chunk, w);
     });
 }
 

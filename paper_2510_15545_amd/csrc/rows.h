@@ -112,25 +112,55 @@ __device__ __forceinline__ uint32_t encode_pair(float x, float y) {
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
 }
 
-// The non-temporal hint: written once and not read here, such lines would displace the logits that will be.
+// A vector's values in the row's type.
 template <int DT>
-__device__ __forceinline__ void store_vector(typename Elem<DT>::T *row, int x, int v, const float (&d)[Elem<DT>::kPer]) {
-    constexpr int kPer = Elem<DT>::kPer;
-    uint32_t w[4];
+__device__ __forceinline__ void encode_vector(const float (&d)[Elem<DT>::kPer], uint32_t (&w)[4]) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if constexpr (DT == TT_F32) w[q] = __float_as_uint(d[q]);
         else w[q] = encode_pair<DT>(d[2 * q], d[2 * q + 1]);
     }
-    if (x + kPer <= v) {
-        u4u t;
-        t.x = w[0]; t.y = w[1]; t.z = w[2]; t.w = w[3];
-        __builtin_nontemporal_store(t, reinterpret_cast<u4u *>(row + x));
-    } else {
+}
+
+// A vector's elements at 0 <= x < v, one by one.
+template <int DT>
+__device__ __forceinline__ void store_elements(typename Elem<DT>::T *row, int x, int v, const uint32_t (&w)[4]) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j)
-            if (x + j < v) row[x + j] = (typename Elem<DT>::T)(DT == TT_F32 ? w[j & 3] : (j & 1) ? (w[j >> 1] >> 16) : (w[j >> 1] & 0xFFFFu));
+    for (int j = 0; j < Elem<DT>::kPer; ++j)
+        if (x + j >= 0 && x + j < v)
+            row[x + j] = (typename Elem<DT>::T)(DT == TT_F32 ? w[j & 3] : (j & 1) ? (w[j >> 1] >> 16) : (w[j >> 1] & 0xFFFFu));
+}
+
+// A chunk's vectors, in the row's type, to the row.  The non-temporal hint: written once and not read here, such
+// lines would displace the logits that will be (distillation of 2,048 rows of 151,936: 371 us without, 301 with).
+template <int DT, int NV, int THREADS>
+__device__ __forceinline__ void store_chunk(typename Elem<DT>::T *row, int v, int x_chunk, const uint32_t (&w)[NV][4]) {
+    constexpr int kPer = Elem<DT>::kPer;
+    auto store = [&](int i, int x) {
+        u4u t;
+        t.x = w[i][0]; t.y = w[i][1]; t.z = w[i][2]; t.w = w[i][3];
+        __builtin_nontemporal_store(t, reinterpret_cast<u4u *>(row + x));
+    };
+    if (x_chunk >= 0 && x_chunk + NV * THREADS * kPer <= v) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) store(i, vector_at<DT, THREADS>(x_chunk, i));
+        return;
     }
+    int end = v;  // where the thread's vector begins that the row ends in
+    uint32_t part[4] = {};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int x = vector_at<DT, THREADS>(x_chunk, i);
+        if (x >= 0 && x + kPer <= v) {
+            store(i, x);
+        } else if (x >= 0 && x < v) {
+            end = x;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) part[q] = w[i][q];
+        }
+    }
+    if (end < v) store_elements<DT>(row, end, v, part);
+    if (x_chunk < 0 && threadIdx.x == 0) store_elements<DT>(row, x_chunk, v, w[0]);
 }
 
 __device__ __forceinline__ float scale_of(const float *inv_temp, int64_t row) {
@@ -213,47 +243,71 @@ struct Sum {
 // Scaled exponents are held above this bound: 2^-200 is 0 in fp32, and 0 * -200 is 0 (0 * -inf is not).
 constexpr float kLowest = -200.0f;
 
+// Chunks of long rows begin at the row's address rounded down to 16 bytes (rows of an odd width begin
+// anywhere): the row's first element is this many elements into its first chunk.  1,000 rows of 50,257 bf16
+// and their gradients: 58.9 to 51.2 us (distillation), 43.6 to 40.7 (backward); rows of 60, whose first
+// vectors would all be guarded: 50.9 to 71.4, so short rows begin where they begin.
+constexpr int kLead = 7;           // at most
+constexpr int kLeadRows = 4096;    // elements of a row from which on it has one
+
+template <int DT>
+__device__ __forceinline__ int lead_of(const void *row, int v) {
+    return v < kLeadRows ? 0 : (int)(reinterpret_cast<uintptr_t>(row) % 16) / (int)sizeof(typename Elem<DT>::T);
+}
+
 // A chunk of a row: NV vectors of 16 bytes a thread.  The loads are unconditional, so that a chunk's loads
-// stay in flight while the one before is worked on: a vector that would end past v is taken from the
-// row's end instead (v >= kPer), and put right by fix_chunk once it has arrived.
+// stay in flight while the one before is worked on: a vector that would begin before the row or end past
+// v is taken from the row's first or last elements instead (v >= kPer), and put right by fix_chunk once
+// it has arrived.
 template <int DT, int NV, int THREADS, bool LAST>
 __device__ __forceinline__ void load_chunk(const typename Elem<DT>::T *row, int v, int x_chunk, uint32_t (&w)[NV][4]) {
     const int last = v - Elem<DT>::kPer;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int x = vector_at<DT, THREADS>(x_chunk, i);
-        const u4u t = load_global<LAST>(row + (x < last ? x : last));
+        int x = vector_at<DT, THREADS>(x_chunk, i);
+        x = x < last ? x : last;
+        const u4u t = load_global<LAST>(row + (x > 0 ? x : 0));
         w[i][0] = t.x; w[i][1] = t.y; w[i][2] = t.z; w[i][3] = t.w;
     }
 }
 
-// Minus infinity past v: the vectors that load_chunk took from the row's end lose the elements that are
-// other vectors', the rest move to the front.
+// Moves a vector's elements by 0 < n < kPer places towards the front (DOWN) or the back, minus infinity behind them.
+template <int DT, bool DOWN>
+__device__ __forceinline__ void shift_vector(uint32_t (&w)[4], int n) {
+    constexpr uint32_t kNone = Elem<DT>::kNone, kNones = DT == TT_F32 ? kNone : kNone * 0x10001u;
+    auto at = [&](const uint32_t(&o)[4], int q) { return q >= 0 && q < 4 ? o[q & 3] : kNones; };
+    int words = n;
+    if constexpr (DT != TT_F32) {
+        if (n & 1) {
+            const uint32_t o[4] = {w[0], w[1], w[2], w[3]};
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                w[q] = DOWN ? (o[q] >> 16) | (at(o, q + 1) << 16) : (o[q] << 16) | (at(o, q - 1) >> 16);
+        }
+        words = n >> 1;
+    }
+#pragma unroll
+    for (int step = 1; step <= 2; step <<= 1) {
+        if (words & step) {
+            const uint32_t o[4] = {w[0], w[1], w[2], w[3]};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[q] = at(o, DOWN ? q + step : q - step);
+        }
+    }
+}
+
+// Minus infinity before the row and past v: the vectors that load_chunk took from the row's ends lose the elements
+// that are other vectors', the rest move to their places.
 template <int DT, int NV, int THREADS>
 __device__ __forceinline__ void fix_chunk(int v, int x_chunk, uint32_t (&w)[NV][4]) {
     constexpr int kPer = Elem<DT>::kPer;
-    constexpr uint32_t kNone = Elem<DT>::kNone, kNones = DT == TT_F32 ? kNone : kNone * 0x10001u;
+    if (x_chunk < 0 && threadIdx.x == 0) shift_vector<DT, false>(w[0], -x_chunk);  // the row's lead
     if (x_chunk + NV * THREADS * kPer <= v) return;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int over = vector_at<DT, THREADS>(x_chunk, i) - (v - kPer);  // elements to drop
-        if (over <= 0) continue;
-        int words = over;
-        if constexpr (DT != TT_F32) {
-            if (over & 1) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) w[i][q] = (w[i][q] >> 16) | ((q < 3 ? w[i][q + 1 < 4 ? q + 1 : 3] : kNones) << 16);
-            }
-            words = over >> 1;
-        }
-#pragma unroll
-        for (int step = 1; step <= 2; step <<= 1) {
-            if (words & step) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) w[i][q] = q + step < 4 ? w[i][q + step < 4 ? q + step : 3] : kNones;
-            }
-        }
-        if (words >= 4) w[i][0] = w[i][1] = w[i][2] = w[i][3] = kNones;
+        if (over >= kPer) w[i][0] = w[i][1] = w[i][2] = w[i][3] = DT == TT_F32 ? Elem<DT>::kNone : Elem<DT>::kNone * 0x10001u;
+        else if (over > 0) shift_vector<DT, true>(w[i], over);
     }
 }
 
@@ -306,8 +360,8 @@ __device__ __forceinline__ Sum wave_join(const Sum &a, float c2) {
 // What rows shorter than a vector are loaded from (their elements are then read one by one).
 static __device__ const uint32_t kNoRow[4] = {};
 
-// Calls f(vectors, first element) for every chunk of a row's elements x0 .. x1 - 1 (x0 a multiple of the chunk),
-// minus infinity past v, while the next chunk's loads are in flight; before() once the first chunk's are.
+// Calls f(vectors, first element) for every chunk from x0 to x1 (x0: whole chunks from the row's lead before it),
+// minus infinity before the row and past v, while the next chunk's loads are in flight; before() once the first chunk's are.
 // BACK: from the last chunk to the first.
 template <int DT, int NV, int THREADS, bool LAST, bool BACK, int UNROLL, typename B, typename F>
 __device__ __forceinline__ void for_chunks(const typename Elem<DT>::T *row, int v, int x0, int x1, B before, F f) {
@@ -350,9 +404,13 @@ __device__ __forceinline__ Sum join(const Sum &a, const Sum &b, float c2) {
 }
 
 constexpr int kFullGrid = 1024;  // workgroups of kThreads that fill the GPU: four a compute unit
-
 inline int elements_per_vector(int dtype) { return dtype == TT_F32 ? 4 : 8; }
 inline int element_bytes(int dtype) { return dtype == TT_F32 ? 4 : 2; }
+
+// Rows from which on a workgroup of kThreads each keeps the GPU busy; fewer are better taken by 1,024 threads
+// each (alternatives of 333 rows of 201 KB: 18.9 us by 256 threads, 20.9 by 1,024; of 400 rows of 304 KB: 36.4
+// and 32.7; of 1,000: 54.5 and 62.0).
+inline int64_t many_rows(int64_t row_bytes) { return row_bytes <= (256 << 10) ? 256 : 512; }
 
 inline size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 

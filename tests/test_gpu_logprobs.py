@@ -296,18 +296,23 @@ def test_a_confident_token_keeps_its_small_gradient():
 def test_gradient_in_place_and_in_wider_rows():
     import torch
 
+    import paper_2510_15545_amd as tt
+
     rng = np.random.default_rng(6)
     n, v = 5, 9001
     x = ur.model_rows(rng, n, v)
-    ids, g = rng.integers(0, v, n), rng.standard_normal(n).astype(np.float32)
+    ids = torch.from_numpy(rng.integers(0, v, n)).int().cuda()
+    g = torch.from_numpy(rng.standard_normal(n).astype(np.float32)).cuda()
     for dtype in ("bf16", "f32"):
         for shift in (0, 3):
-            want = check_gradient(x, ur.placed(x, dtype, shift=shift), ids, None, g, None, dtype)
             rows = ur.placed(x, dtype, pad=5, shift=shift)
+            check_gradient(x, rows, ids.cpu().numpy(), None, g.cpu().numpy(), None, dtype)
+            stats = tt.logprobs(v, rows).stats
+            want = tt.logprobs_backward(v, rows, ids, stats, g)
             wide = torch.full((n, v + 13), 7.0, dtype=rows.dtype, device="cuda")
-            check_gradient(x, rows, ids, None, g, None, dtype, out=wide)
+            tt.logprobs_backward(v, rows, ids, stats, g, out=wide)
             assert torch.equal(wide[:, :v], want) and (wide[:, v:] == 7.0).all()  # what lies past v is left alone
-            check_gradient(x, rows, ids, None, g, None, dtype, out=rows)
+            tt.logprobs_backward(v, rows, ids, stats, g, out=rows)
             assert torch.equal(rows, want)
 
 
