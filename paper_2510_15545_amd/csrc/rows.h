@@ -131,15 +131,17 @@ __device__ __forceinline__ void store_elements(typename Elem<DT>::T *row, int x,
             row[x + j] = (typename Elem<DT>::T)(DT == TT_F32 ? w[j & 3] : (j & 1) ? (w[j >> 1] >> 16) : (w[j >> 1] & 0xFFFFu));
 }
 
-// A chunk's vectors, in the row's type, to the row.  The non-temporal hint: written once and not read here, such
-// lines would displace the logits that will be (distillation of 2,048 rows of 151,936: 371 us without, 301 with).
-template <int DT, int NV, int THREADS>
+// A chunk's vectors, in the row's type, to the row; KEEP: without the non-temporal hint, which keeps lines that are
+// not read here from displacing others.  (Not a value: of two stores that differ in the hint alone the compiler
+// makes one without it.)
+template <int DT, int NV, int THREADS, bool KEEP>
 __device__ __forceinline__ void store_chunk(typename Elem<DT>::T *row, int v, int x_chunk, const uint32_t (&w)[NV][4]) {
     constexpr int kPer = Elem<DT>::kPer;
     auto store = [&](int i, int x) {
         u4u t;
         t.x = w[i][0]; t.y = w[i][1]; t.z = w[i][2]; t.w = w[i][3];
-        __builtin_nontemporal_store(t, reinterpret_cast<u4u *>(row + x));
+        if constexpr (KEEP) *reinterpret_cast<u4u *>(row + x) = t;
+        else __builtin_nontemporal_store(t, reinterpret_cast<u4u *>(row + x));
     };
     if (x_chunk >= 0 && x_chunk + NV * THREADS * kPer <= v) {
 #pragma unroll
