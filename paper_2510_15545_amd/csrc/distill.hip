@@ -29,7 +29,7 @@ using namespace rows;
 constexpr int kMaxTop = 128;
 constexpr int kSlots = kMaxTop / kWave;  // list entries of a lane
 constexpr int64_t kMaxGrid = int64_t(1) << 18;
-constexpr int kChunkVectors = 4;
+constexpr int kChunkVectors = 4;  // of a thread, for a part of a row
 constexpr int kMaxBits = 1 << 18;  // tokens of a bitmap: 32 KB
 
 // What the gradient of a row's unlisted tokens needs: factor * 2^t, t = x c2 - shift <= 0 (m = 0), or
@@ -247,14 +247,14 @@ __host__ __device__ __forceinline__ int bitmap_words(int width) {
 
 // Gradients of the unlisted tokens of elements x0 .. x1 - 1, from what get() returns (called once the first loads
 // are in flight); zeros where the factor is 0.
-template <int DT, int NV, int THREADS, typename G>
+template <int DT, int NV, int THREADS, bool AHEAD, typename G>
 __device__ __forceinline__ void write_grad(const ListArgs &a, int64_t row_i, int x0, int x1, G get) {
     using T = typename Elem<DT>::T;
     constexpr int kPer = Elem<DT>::kPer;
     const T *row = static_cast<const T *>(a.logits) + row_i * a.ld;
     T *out = static_cast<T *>(a.out) + row_i * a.out_ld;
     RowGrad q;
-    for_chunks<DT, NV, THREADS, true, true, 1>(row, a.v, x0, x1, [&] { q = get(); }, [&](uint32_t(&w)[NV][4], int x) {
+    for_chunks<DT, NV, THREADS, true, true, AHEAD, 1>(row, a.v, x0, x1, [&] { q = get(); }, [&](uint32_t(&w)[NV][4], int x) {
         auto form = [&](auto exponent) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(THREADS) void list_whole(ListArgs a) {
         __syncthreads();
         if (wave == 0) weigh_list(a, list, lp, __ballot(repeated) != 0);
     };
-    for_chunks<DT, NV, THREADS, !GRAD, false, 1>(row, a.v, x0, a.v, read, [&](uint32_t(&w)[NV][4], int x) {
+    for_chunks<DT, NV, THREADS, !GRAD, false, true, 1>(row, a.v, x0, a.v, read, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         take_out<DT, NV, THREADS>(w, sh_bits, x, x0);
         add_chunk<DT, NV, false>(w, c2, mine, vm);
@@ -332,7 +332,7 @@ __global__ __launch_bounds__(THREADS) void list_whole(ListArgs a) {
         return sh_grad;
     };
     if constexpr (GRAD) {
-        write_grad<DT, NV, THREADS>(a, row_i, x0, a.v, finish);
+        write_grad<DT, NV, THREADS, true>(a, row_i, x0, a.v, finish);
         // the listed tokens over what was just written: after the workgroup's stores
         __syncthreads();
         if ((int)threadIdx.x < a.n_top) {
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(kThreads) void list_parts(ListArgs a) {
         __syncthreads();
     };
     Sum mine = {-INFINITY, 0.0f, 0.0f};
-    for_chunks<DT, NV, kThreads, false, false, 1>(row, a.v, x0, x1, read, [&](uint32_t(&w)[NV][4], int x) {
+    for_chunks<DT, NV, kThreads, false, false, true, 1>(row, a.v, x0, x1, read, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         take_out<DT, NV, kThreads>(w, sh_bits, x, x0);
         add_chunk<DT, NV, false>(w, c2, mine, vm);
@@ -421,7 +421,7 @@ __global__ __launch_bounds__(kThreads) void list_grad(ListArgs a, int parts) {
     const int x0 = part * kPart - lead_of<DT>(out, a.v), x1 = part + 1 == parts ? a.v : x0 + kPart;
     Entry mine = {-1, 0.0f};
     if ((int)threadIdx.x < a.n_top) mine = a.entries[(size_t)r * a.n_top + threadIdx.x];
-    write_grad<DT, kChunkVectors, kThreads>(a, row_i, x0, x1, [&] { return a.row_grad[r]; });
+    write_grad<DT, kChunkVectors, kThreads, false>(a, row_i, x0, x1, [&] { return a.row_grad[r]; });
     // the listed tokens over what was just written: after the workgroup's stores
     __syncthreads();
     if (mine.id >= 0 && mine.id >= x0 && mine.id < x1) out[mine.id] = (T)encode<DT>(mine.grad);
@@ -430,6 +430,9 @@ __global__ __launch_bounds__(kThreads) void list_grad(ListArgs a, int parts) {
 // Threads and vectors of list_whole for rows of these bytes.
 constexpr int kLongThreads = 1024, kLongVectors = 2;
 constexpr int64_t kShortRow = 32 << 10;          // bytes of a row that kThreads threads take whole
+// Without the gradient kThreads take rows whole from this many rows on (1,000 of 50,257: 21.9 us, 25.0 by 1,024
+// threads each; 512 of 151,936: 34.2 and 30.3; 700: 37.7 and 40.6).
+int64_t many_rows(int64_t row_bytes) { return row_bytes <= (256 << 10) ? 256 : 640; }
 constexpr int64_t kSplitRow = 128 << 10;         // and of one that is split where there are few rows
 constexpr int64_t kFewRows = 96;                 // fewer long rows leave too many compute units without one
 constexpr size_t kCachedBytes = size_t(96) << 20;  // logits of a group of split rows, with the gradient
@@ -473,8 +476,11 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
 template <int DT, bool GRAD>
 void launch_whole(const ListArgs &a, int threads, int64_t n, hipStream_t stream) {
     if (threads == kThreads) {
-        const size_t lds = bitmap_words<DT, kChunkVectors, kThreads>(a.v) * sizeof(uint32_t);
-        list_whole<DT, kChunkVectors, kThreads, GRAD><<<(unsigned)n, kThreads, lds, stream>>>(a);
+        // short rows with the gradient, rows of any length without: 17,000 of 60 and 2,000 of 700 take 58 and 10.6 us
+        // with the gradient by one vector, 69 and 12.5 by two; 800 of 128,256 without it 44.0 and 39.3
+        constexpr int kVectors = GRAD ? 1 : 2;
+        const size_t lds = bitmap_words<DT, kVectors, kThreads>(a.v) * sizeof(uint32_t);
+        list_whole<DT, kVectors, kThreads, GRAD><<<(unsigned)n, kThreads, lds, stream>>>(a);
     } else {
         const size_t lds = bitmap_words<DT, kLongVectors, kLongThreads>(a.v) * sizeof(uint32_t);
         list_whole<DT, kLongVectors, kLongThreads, GRAD><<<(unsigned)n, kLongThreads, lds, stream>>>(a);

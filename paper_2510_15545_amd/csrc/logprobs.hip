@@ -26,10 +26,16 @@ constexpr int kMaxTop = 128;
 constexpr int kSelect = 1024;                       // keys that are ordered in LDS
 constexpr int kGroups = 256;                        // lane groups whose largest values give the bound
 constexpr int kChunkVectors = 4;
+constexpr int64_t kShortBytes = 8 << 10;            // rows up to these bytes are taken by one vector a thread
 constexpr int kWholeChunks = 2;                     // rows of at most this many chunks are never split
 constexpr int kLongThreads = 1024, kLongVectors = 2;  // for rows taken whole where they are few
 constexpr int64_t kLongRows = 96;                   // rows from which on they are, whatever their length,
 constexpr int64_t kLongBytes = 128 << 10;           // and the length up to which they are, however few
+
+// Rows from which on a workgroup of kThreads each keeps the GPU busy; fewer are better taken by 1,024 threads
+// each (alternatives of 333 rows of 201 KB: 18.9 us by 256 threads, 20.9 by 1,024; of 400 rows of 304 KB: 36.4
+// and 32.7; of 1,000: 54.5 and 62.0).
+int64_t many_rows(int64_t row_bytes) { return row_bytes <= (256 << 10) ? 256 : 512; }
 constexpr size_t kMaxKeyBytes = size_t(128) << 20;  // workspace: rows are taken in groups beyond
 constexpr int64_t kMaxGrid = int64_t(1) << 18;      // workgroups of one launch
 
@@ -422,9 +428,9 @@ __device__ __forceinline__ void write_top(const RowArgs &a, int64_t row, const R
 }
 
 // A part of a row by a workgroup; FINISH: the row is one part, and finished here.
-template <int DT, int THREADS, bool TOP, bool ENTROPY, bool FINISH>
+template <int DT, int THREADS, int NV, bool TOP, bool ENTROPY, bool FINISH>
 __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stream(RowArgs a) {
-    constexpr int kWaves = THREADS / kWave, NV = THREADS == kThreads ? kChunkVectors : kLongVectors;
+    constexpr int kWaves = THREADS / kWave;
     __shared__ Sum sh_sum[kWaves];
     __shared__ TopLds<THREADS> sh;
     __shared__ uint64_t sh_sel[kSelect], sh_out[kMaxTop];
@@ -439,7 +445,7 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stre
     int count = 0;
     Sum mine = {-INFINITY, 0.0f, 0.0f};
     TopSet<DT, NV, THREADS> top{sh, a.n_top};
-    for_chunks<DT, NV, THREADS, true, false, TOP ? 1 : 2>(row, a.v, x0, x1, [] {}, [&](uint32_t(&w)[NV][4], int x) {
+    for_chunks<DT, NV, THREADS, true, false, true, TOP ? 1 : 2>(row, a.v, x0, x1, [] {}, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         add_chunk<DT, NV, ENTROPY>(w, c2, mine, vm);
         if constexpr (TOP) top.add(w, vm, x);
@@ -654,9 +660,12 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top) {
 
 template <int DT, bool TOP, bool ENTROPY>
 void launch_rows(const RowArgs &a, int threads, int64_t n, hipStream_t stream) {
-    if (threads == kLongThreads) row_stream<DT, kLongThreads, TOP, ENTROPY, true><<<(unsigned)n, kLongThreads, 0, stream>>>(a);
-    else if (a.parts == 1) row_stream<DT, kThreads, TOP, ENTROPY, true><<<(unsigned)n, kThreads, 0, stream>>>(a);
-    else row_stream<DT, kThreads, TOP, ENTROPY, false><<<(unsigned)(n * a.parts), kThreads, 0, stream>>>(a);
+    const unsigned grid = (unsigned)(n * a.parts);
+    if (threads == kLongThreads) row_stream<DT, kLongThreads, kLongVectors, TOP, ENTROPY, true><<<grid, kLongThreads, 0, stream>>>(a);
+    else if (a.parts > 1) row_stream<DT, kThreads, kChunkVectors, TOP, ENTROPY, false><<<grid, kThreads, 0, stream>>>(a);
+    // 4,000 rows of 2,000 (5 alternatives): 19.4 us by one vector, 22.8 by four; 333 of 50,257 fp32: 33.4 and 19.1
+    else if ((int64_t)a.v * element_bytes(DT) <= kShortBytes) row_stream<DT, kThreads, 1, TOP, ENTROPY, true><<<grid, kThreads, 0, stream>>>(a);
+    else row_stream<DT, kThreads, kChunkVectors, TOP, ENTROPY, true><<<grid, kThreads, 0, stream>>>(a);
 }
 
 template <int DT>
@@ -671,7 +680,7 @@ void launch_rows(const RowArgs &a, int threads, int64_t n, hipStream_t stream) {
 }
 
 // ---------------------------------------------------------------- gradient
-constexpr int kGradVectors = 4;
+constexpr int kGradVectors = 2;
 
 // Gradients up to the Infinity Cache's size are left in it for what reads them next, which is faster here, too
 // (1,000 rows of 128,256, 256 MB: 78 us, 89 with the non-temporal hint); larger ones would only pass through it
@@ -712,7 +721,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(GradArgs a) {
     const float ent = ENTROPY ? a.entropy[r] : 0.0f;
     // d = p (first + second t), t = lp / ln 2 held above -200 (p is 0 there); NaN statistics make it NaN
     const float first = -beta * (g + h * ent) + (log_sum - log_sum), second = ENTROPY ? -beta * h * (float)kLn2 : 0.0f;
-    for_chunks<DT, kGradVectors, kThreads, true, false, 1>(row, a.v, x0, x1, [] {}, [&](uint32_t(&w)[kGradVectors][4], int x_chunk) {
+    for_chunks<DT, kGradVectors, kThreads, true, false, false, 1>(row, a.v, x0, x1, [] {}, [&](uint32_t(&w)[kGradVectors][4], int x_chunk) {
 #pragma unroll
         for (int i = 0; i < kGradVectors; ++i) {
             const int x = vector_at<DT, kThreads>(x_chunk, i);

@@ -364,8 +364,9 @@ static __device__ const uint32_t kNoRow[4] = {};
 
 // Calls f(vectors, first element) for every chunk from x0 to x1 (x0: whole chunks from the row's lead before it),
 // minus infinity before the row and past v, while the next chunk's loads are in flight; before() once the first chunk's are.
-// BACK: from the last chunk to the first.
-template <int DT, int NV, int THREADS, bool LAST, bool BACK, int UNROLL, typename B, typename F>
+// BACK: from the last chunk to the first.  AHEAD false: a chunk's loads only when it is its turn (for a workgroup
+// of one chunk, or now and then two).
+template <int DT, int NV, int THREADS, bool LAST, bool BACK, bool AHEAD, int UNROLL, typename B, typename F>
 __device__ __forceinline__ void for_chunks(const typename Elem<DT>::T *row, int v, int x0, int x1, B before, F f) {
     using T = typename Elem<DT>::T;
     constexpr int kPer = Elem<DT>::kPer, kChunk = NV * THREADS * kPer;
@@ -384,13 +385,17 @@ __device__ __forceinline__ void for_chunks(const typename Elem<DT>::T *row, int 
 #pragma unroll UNROLL
     for (int c = 1; c <= n; ++c, x += step) {
         uint32_t next[NV][4];
-        load_chunk<DT, NV, THREADS, LAST>(from, width, c < n ? x + step : width, next);  // past the end: one line
+        if constexpr (AHEAD) load_chunk<DT, NV, THREADS, LAST>(from, width, c < n ? x + step : width, next);  // past the end: one line
         fix_chunk<DT, NV, THREADS>(width, x, w);
         f(w, x);
+        if constexpr (AHEAD) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) w[i][q] = next[i][q];
+                for (int q = 0; q < 4; ++q) w[i][q] = next[i][q];
+        } else if (c < n) {
+            load_chunk<DT, NV, THREADS, LAST>(from, width, x + step, w);
+        }
     }
 }
 
@@ -408,11 +413,6 @@ __device__ __forceinline__ Sum join(const Sum &a, const Sum &b, float c2) {
 constexpr int kFullGrid = 1024;  // workgroups of kThreads that fill the GPU: four a compute unit
 inline int elements_per_vector(int dtype) { return dtype == TT_F32 ? 4 : 8; }
 inline int element_bytes(int dtype) { return dtype == TT_F32 ? 4 : 2; }
-
-// Rows from which on a workgroup of kThreads each keeps the GPU busy; fewer are better taken by 1,024 threads
-// each (alternatives of 333 rows of 201 KB: 18.9 us by 256 threads, 20.9 by 1,024; of 400 rows of 304 KB: 36.4
-// and 32.7; of 1,000: 54.5 and 62.0).
-inline int64_t many_rows(int64_t row_bytes) { return row_bytes <= (256 << 10) ? 256 : 512; }
 
 inline size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
