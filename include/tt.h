@@ -507,10 +507,11 @@ int tt_step(const tt_vocab *vd, const tt_vocab *vt, int32_t n_streams, int32_t v
  *     M = max x,  S = sum exp(beta (x_j - M)),  L = ln S,  lse = beta M + L,
  *     lp_j = beta (x_j - M) - L,  p_j = exp(lp_j).
  * A NaN logit counts as minus infinity (as in tt_verify_logits), and minus infinity is a token of
- * probability 0.  A row with a logit of plus infinity, or with beta <= 0, infinite or NaN, has no
+ * probability 0.  A row with a logit of plus infinity, or with beta outside (0, 2^100], has no
  * distribution: its results are NaN (token ids -1).  v in 1..2^23, n_rows >= 0.
- * Sums are formed in fp32 within a part of a row (at most 16,384 logits) and in fp64 over the parts;
- * the results do not depend on scheduling.
+ * Each thread sums its share of a row in fp32, relative to its largest logit; these sums are joined in
+ * fp32 within a wave and in fp64 beyond.  Which logits a thread takes depends on the rows' number, width
+ * and alignment, so the last digits of a row's results may; they do not depend on scheduling.
  */
 enum { TT_BF16 = 0, TT_F16 = 1, TT_F32 = 2 };
 
@@ -529,9 +530,10 @@ enum { TT_BF16 = 0, TT_F16 = 1, TT_F32 = 2 };
  *   top_logprobs [n_rows][n_top] their lp; minus infinity where top_ids is -1
  * A row without a logit above minus infinity has M = lse = -inf, L = 0, H = 0, logprob = -inf and
  * no alternatives.
- * Reads every logit once.  workspace: tt_logprobs_workspace_size bytes, 16-byte aligned, no
- * initialisation; calls that overlap in time must not share it.  Two kernels on `stream` (for large
- * batches with alternatives: two for each group of rows).  TT_EINVAL on a bad size or type, a missing
+ * Reads every logit once.  workspace: tt_logprobs_workspace_size bytes (0 where a row is one
+ * workgroup's: rows of at most 128 KB, or 96 rows or more), 16-byte aligned, no initialisation; calls that
+ * overlap in time must not share it.  One kernel on `stream`, two where rows are split (each for at most
+ * 2^18 workgroups, or 128 MB of workspace).  TT_EINVAL on a bad size or type, a missing
  * pointer or one not aligned to its elements, TT_EUNSUPPORTED for v > 2^23 or n_top > 128,
  * TT_EWORKSPACE when the workspace is missing or too small.
  */
@@ -554,6 +556,7 @@ int tt_logprobs(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, in
  *                memory (the same address and stride), but must not overlap them otherwise.
  * A row with g = h = 0, or without a logit above minus infinity, gets zeros and is not read.
  * Logits are read once; no workspace; one kernel on `stream` (several for more than 2^18 workgroups).
+ * Errors as for tt_logprobs, and TT_EINVAL for a dlogits that overlaps the logits otherwise.
  */
 int tt_logprobs_backward(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,
                          const float *inv_temperature, const int32_t *ids, const float *stats, const float *entropy,
@@ -583,10 +586,11 @@ int tt_logprobs_backward(int32_t n_rows, int32_t v, int32_t dtype, const void *l
  *   loss         [n_rows]
  *   grad_loss    [n_rows], required with dlogits
  *   dlogits      optional (NULL: the loss alone); layout, rounding and aliasing as in tt_logprobs_backward
- * workspace: tt_distill_workspace_size bytes (with_grad: whether dlogits will be given), 16-byte
- * aligned, no initialisation; calls that overlap in time must not share it.  Two kernels on `stream`,
- * three with the gradient, for each group of rows (with the gradient a group's logits stay in the
- * cache between their two readings).
+ * workspace: tt_distill_workspace_size bytes (with_grad: whether dlogits will be given; 0 where a row is
+ * one workgroup's: v <= 2^18, and rows of at most 128 KB or 96 rows or more), 16-byte aligned, no
+ * initialisation; calls that overlap in time must not share it.  One kernel on `stream`, or where rows are
+ * split two, three with the gradient, for each group of rows.  With the gradient every logit is read
+ * twice, the second time mostly from a cache.  Errors as for tt_logprobs (n_top < 1 is TT_EINVAL).
  */
 int tt_distill_workspace_size(int32_t n_rows, int32_t v, int32_t dtype, int32_t n_top, int32_t with_grad, size_t *bytes);
 int tt_distill(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,

@@ -190,7 +190,7 @@ __device__ __forceinline__ RowGrad finish_row(const ListArgs &a, int64_t row, co
     const double s = wave_sum(e[0] + e[1]) + (s_out > 0.0 ? s_out * exp(t_out) : 0.0), log_s = log(s);
     const double rest = a.tail && s_out > 0.0 ? fmax(0.0, 1.0 - q.listed) : 0.0;
     // nothing listed, or no finite logit: 0; a logit or list value of +inf, or an unsound temperature: NaN
-    const bool bad = !(beta > 0.0 && beta < INFINITY) || m == INFINITY || q.most == INFINITY;
+    const bool bad = !sound(beta) || m == INFINITY || q.most == INFINITY;
     const bool zero = !bad && (!q.any || m == -INFINITY);
     double loss = 0.0;
 #pragma unroll

@@ -395,7 +395,7 @@ __device__ __forceinline__ RowStats row_stats(double beta, float m, double s) {
     RowStats q;
     q.m = m;
     q.beta = beta;
-    q.bad = !(beta > 0.0 && beta < INFINITY) || m == INFINITY;
+    q.bad = !sound(beta) || m == INFINITY;
     q.log_sum = q.bad ? NAN : (m == -INFINITY ? 0.0 : log(s));
     return q;
 }

@@ -169,6 +169,10 @@ __device__ __forceinline__ float scale_of(const float *inv_temp, int64_t row) {
     return inv_temp == nullptr ? 1.0f : inv_temp[row];
 }
 
+// Whether a row has a distribution at this inverse temperature: above 2^100 the scaled exponents of equal logits
+// would no longer be numbers.
+__device__ __forceinline__ bool sound(double beta) { return beta > 0.0 && beta <= 0x1p100; }
+
 // With the IEEE bit of the MODE register set, v_max returns a signalling NaN operand quieted and loses
 // the other one; with it clear, every NaN operand is passed over.  Cleared at a kernel's start, it
 // makes fmaxf over raw logits the maximum of those that are no NaN, at no cost per element.

@@ -130,12 +130,13 @@ def test_masks(dtype, n_top):
 
 def test_rows_without_a_distribution():
     rng = np.random.default_rng(9)
-    x = ur.model_rows(rng, 8, 3001)
+    x = ur.model_rows(rng, 10, 3001)
     x[1, 17] = np.inf
     x[2] = -np.inf
     x[2, 5] = np.inf
-    beta = np.array([1.0, 1.0, 1.0, 0.0, -1.0, np.nan, np.inf, 2.0], np.float32)
-    ids = np.array([-1, 17, 3, 4, 5, 6, 7, 3001])
+    beta = np.array([1.0, 1.0, 1.0, 0.0, -1.0, np.nan, np.inf, 2.0, 2.0 ** 101, 2.0 ** 100], np.float32)
+    ids = np.array([-1, 17, 3, 4, 5, 6, 7, 3001, 8, x[9].argmax()])
+    x[9, 5:9] = x[9].max()  # equal largest logits at the steepest temperature
     check_logprobs(x, ur.placed(x, "f32"), ids, beta, 5)
 
 

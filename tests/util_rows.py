@@ -17,7 +17,7 @@ def clean(x):
 def row_statistics(x, beta):
     """(M, L, lp) of one row; None where the row has no distribution."""
     m = x.max()
-    if m == np.inf or not (0.0 < beta < np.inf):
+    if m == np.inf or not (0.0 < beta <= 2.0 ** 100):
         return None
     if m == -np.inf:
         return m, 0.0, np.full(len(x), -np.inf)
@@ -150,7 +150,7 @@ def distill(x, beta, top_ids, top_logprobs, tail, id_map=None, weight=None):
         loss[i], g, loss_off[i], o = distill_row(x[i], b, ids, np.asarray(top_logprobs[i], np.float64), tail)
         w = 1.0 if weight is None else float(weight[i])
         d[i] = 0.0 if w == 0.0 else w * b * g
-        off[i] = abs(w) * b * o if w != 0.0 and 0.0 < b < np.inf else 0.0
+        off[i] = abs(w) * b * o if w != 0.0 and 0.0 < b <= 2.0 ** 100 else 0.0
     return loss, d, loss_off, off
 
 
