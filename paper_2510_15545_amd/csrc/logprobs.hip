@@ -382,11 +382,13 @@ struct RowStats {
     bool bad;
 };
 
-// The logit of a row's token, 0 where there is none: read long before it is wanted.
-__device__ __forceinline__ float token_logit(const RowArgs &a, int64_t row) {
-    if (a.logprob == nullptr) return 0.0f;
-    const int32_t id = a.ids[row];
-    return id >= 0 && id < a.v ? load_logit(row_at(a.logits, a.dtype, row * a.ld), a.dtype, id) : 0.0f;
+// A row's token, -1 where there is none, and its logit: both read long before they are wanted.
+__device__ __forceinline__ int32_t token_of(const RowArgs &a, int64_t row) {
+    const int32_t id = a.logprob == nullptr ? -1 : a.ids[row];
+    return id < a.v ? id : -1;
+}
+__device__ __forceinline__ float token_logit(const RowArgs &a, int64_t row, int32_t id) {
+    return id >= 0 ? load_logit(row_at(a.logits, a.dtype, row * a.ld), a.dtype, id) : 0.0f;
 }
 
 // From the row's largest logit m and the sum s relative to it.
@@ -400,8 +402,8 @@ __device__ __forceinline__ RowStats row_stats(double beta, float m, double s) {
     return q;
 }
 
-// A row's results but the alternatives, by one thread: s and e as in Sum, in natural units; the token's logit.
-__device__ __forceinline__ void write_row(const RowArgs &a, int64_t row, const RowStats &q, double s, double e, float x_id) {
+// A row's results but the alternatives, by one thread: s and e as in Sum, in natural units; the token and its logit.
+__device__ __forceinline__ void write_row(const RowArgs &a, int64_t row, const RowStats &q, double s, double e, int32_t id, float x_id) {
     if (a.stats != nullptr) {
         a.stats[2 * row] = q.bad ? NAN : (float)q.m;
         a.stats[2 * row + 1] = (float)q.log_sum;
@@ -409,9 +411,8 @@ __device__ __forceinline__ void write_row(const RowArgs &a, int64_t row, const R
     if (a.lse != nullptr) a.lse[row] = (float)(q.bad ? NAN : q.m * q.beta + q.log_sum);
     if (a.entropy != nullptr) a.entropy[row] = (float)(q.bad ? NAN : (q.m == -INFINITY ? 0.0 : q.log_sum - e / s));
     if (a.logprob != nullptr) {
-        const int32_t id = a.ids[row];
         double lp = NAN;
-        if (!q.bad && id >= 0 && id < a.v) lp = x_id == -INFINITY ? -INFINITY : ((double)x_id - q.m) * q.beta - q.log_sum;
+        if (!q.bad && id >= 0) lp = x_id == -INFINITY ? -INFINITY : ((double)x_id - q.m) * q.beta - q.log_sum;
         a.logprob[row] = (float)lp;
     }
 }
@@ -441,11 +442,12 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stre
     const auto *row = static_cast<const typename Elem<DT>::T *>(a.logits) + row_i * a.ld;
     const int x0 = part * a.part_width - lead_of<DT>(row, a.v), x1 = FINISH || part + 1 == a.parts ? a.v : x0 + a.part_width;
     const float beta = scale_of(a.inv_temp, row_i), c2 = beta * kLog2e;
-    const float x_id = FINISH ? token_logit(a, row_i) : 0.0f;
+    const int32_t id = FINISH ? token_of(a, row_i) : -1;
+    float x_id = 0.0f;
     int count = 0;
     Sum mine = {-INFINITY, 0.0f, 0.0f};
     TopSet<DT, NV, THREADS> top{sh, a.n_top};
-    for_chunks<DT, NV, THREADS, true, false, true, TOP ? 1 : 2>(row, a.v, x0, x1, [] {}, [&](uint32_t(&w)[NV][4], int x) {
+    for_chunks<DT, NV, THREADS, true, false, true, TOP ? 1 : 2>(row, a.v, x0, x1, [&] { x_id = token_logit(a, row_i, id); }, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         add_chunk<DT, NV, ENTROPY>(w, c2, mine, vm);
         if constexpr (TOP) top.add(w, vm, x);
@@ -478,7 +480,7 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stre
         const RowStats stats = row_stats(beta, m, s);
         if (lane == 0) {
             sh_stats = stats;
-            write_row(a, row_i, stats, s, e, x_id);
+            write_row(a, row_i, stats, s, e, id, x_id);
         }
     }
     if constexpr (TOP && FINISH) {
@@ -511,7 +513,7 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
     const float4 *sums = a.sums + (size_t)r * a.parts;
     const uint64_t *keys = a.keys + (size_t)r * a.parts * a.capacity;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const float x_id = token_logit(a, row);
+    const int32_t id = token_of(a, row);
     const double beta = scale_of(a.inv_temp, row);
     float4 q = {-INFINITY, 0.0f, 0.0f, 0.0f};  // the thread's first part
     if ((int)threadIdx.x < a.parts) q = sums[threadIdx.x];
@@ -531,6 +533,7 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
     }
     if (threadIdx.x == 0) sh_total = 0;
     __syncthreads();
+    const float x_id = token_logit(a, row, id);
     // the keys: where they are few, all of them in registers, a run of 64 of a part's a load, in flight together
     uint64_t mine[kHeld];
     bool held = false;
@@ -585,7 +588,7 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
     s = sh_s[0] + sh_s[1] + sh_s[2] + sh_s[3];
     e = sh_e[0] + sh_e[1] + sh_e[2] + sh_e[3];
     const RowStats stats = row_stats(beta, m, s);
-    if (threadIdx.x == kThreads - 1) write_row(a, row, stats, s, e, x_id);
+    if (threadIdx.x == kThreads - 1) write_row(a, row, stats, s, e, id, x_id);
     if constexpr (TOP) {
         for (;;) {
             auto put = [&](uint64_t key) {
