@@ -19,6 +19,12 @@
 // the Infinity Cache.
 // Where the rows are too few to fill the GPU they are split: list_parts forms the sums of parts,
 // list_rows joins them and does the one wave's work, list_grad writes the gradient of parts.
+//
+// What bounds it: the loss alone reads at 5.1 TB/s with 512 rows of 151,936 bf16 (30.5 us; two workgroups a compute
+// unit, whose start and end are 7 of them).  The gradient of 2,048 such rows takes 275 us: 4.5 TB/s of the 1.24 GB
+// that HBM has to carry, where a large copy gets 5.1, and 6.8 TB/s of the 1.87 GB with the second reading, which
+// HBM alone would not give.  Between the two readings a workgroup writes nothing, and both want an exponential
+// an element (the VALU is busy 60% of the cycles).
 #include "rows.h"
 
 namespace tt {
@@ -427,15 +433,21 @@ __global__ __launch_bounds__(kThreads) void list_grad(ListArgs a, int parts) {
     if (mine.id >= 0 && mine.id >= x0 && mine.id < x1) out[mine.id] = (T)encode<DT>(mine.grad);
 }
 
-// Threads and vectors of list_whole for rows of these bytes.
+// Threads and vectors of list_whole for rows of more than kShortRow bytes; shorter rows are few vectors long and
+// taken by kThreads, more of them at once.
 constexpr int kLongThreads = 1024, kLongVectors = 2;
-constexpr int64_t kShortRow = 32 << 10;          // bytes of a row that kThreads threads take whole
+constexpr int64_t kShortRow = 32 << 10;
 // Without the gradient kThreads take rows whole from this many rows on (1,000 of 50,257: 21.9 us, 25.0 by 1,024
 // threads each; 512 of 151,936: 34.2 and 30.3; 700: 37.7 and 40.6).
 int64_t many_rows(int64_t row_bytes) { return row_bytes <= (256 << 10) ? 256 : 640; }
-constexpr int64_t kSplitRow = 128 << 10;         // and of one that is split where there are few rows
-constexpr int64_t kFewRows = 96;                 // fewer long rows leave too many compute units without one
-constexpr size_t kCachedBytes = size_t(96) << 20;  // logits of a group of split rows, with the gradient
+// Rows of more than kSplitRow bytes are split where there are fewer than kFewRows of them: too many compute units
+// would be without one (gradients of 16 rows of 151,936: 15.5 us split, 24.2 whole; of 96: 27.5 and 26.0; of 128: 33
+// and 26.8; of 96 rows of 32,000 fp32, 128,000 bytes: 15.7 and 10.9).
+constexpr int64_t kSplitRow = 128 << 10;
+constexpr int64_t kFewRows = 96;
+// Logits of a group of split rows whose gradient is wanted: list_grad reads them again, from the Infinity Cache
+// (256 MB) if the group and its gradients fit.
+constexpr size_t kCachedBytes = size_t(96) << 20;
 
 struct Plan {
     int parts, part_width;  // parts == 0: list_whole

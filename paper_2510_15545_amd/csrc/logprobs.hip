@@ -7,14 +7,24 @@
 //   alternatives: the largest x, ties by the lower index, minus infinity never listed
 //   d_j = beta (g ([j = id] - p_j) - h p_j (lp_j + H)), upstream gradients g of lp_id and h of H
 //
-// One pass over the row: row_stream, a workgroup for a row or a part of it, by chunks of 16 KB whose loads are
-// in flight while the chunk before is worked on.  Each thread keeps the largest value and the sums
-// (base 2, v_exp_f32) of what it has seen.  For the alternatives it keeps the place of its largest
-// value as well: k of the workgroup's 256 lane groups hold a largest value that reaches the k-th largest
-// of the 256, so every one of the k largest elements does.  That bound is formed after chunks 1, 2, 4,
-// 8, ..., and elements that reach it are staged in LDS as 64-bit keys (value, then lower index); over a
-// row of N chunks about k (1 + ln N) of them.  A row's only workgroup finishes it (fp64 from the waves'
-// sums on; keys ordered by counting); with several, row_finish does.
+// One pass over the row: row_stream, a workgroup for a row or a part of it, by chunks of 16 to 32 KB whose
+// loads are in flight while the chunk before is worked on.  Each thread keeps the largest value and the sums
+// (base 2, v_exp_f32) of what it has seen: in fp32 over a thread's elements, chunk by chunk, in fp64
+// from the waves' sums on.  The token's logit is read behind the first chunk's loads.
+//
+// Alternatives, in the same pass: each thread keeps the place of its largest value as well.  k of the
+// workgroup's 64 or 256 groups of threads hold a largest value that reaches the k-th largest of the groups',
+// so every one of the k largest elements does.  That bound is formed after chunks 1, 2, 4, 8, ..., and elements
+// that reach it are staged in LDS as 64-bit keys (value, then lower index), over a row of N chunks about
+// k (1 + ln N) of them; in the end the keys are ordered by counting.  A row's only workgroup finishes it; with
+// several, each hands its sums and keys to row_finish.
+//
+// What bounds it: the reading of the logits, at 6.4 to 6.9 TB/s on a row set beyond the Infinity Cache (4,096
+// rows of 151,936 bf16: 187 us a pass, 6.7 TB/s; a kernel that only reads gets no more), and the VALU where the
+// alternatives are wanted (about 9 issue slots an element for the statistics, the exponential four of them; 1,024
+// rows of 262,144 with 64 alternatives: 96 us against 80 to read them; the VALU is busy 78% of the cycles).  Few rows
+// are latency: one row of 640 takes 5 us on the GPU, one of 151,936 with 20 alternatives 6.3 for its 19 parts and 6.5
+// to join them.
 #include "rows.h"
 
 namespace tt {
@@ -29,8 +39,11 @@ constexpr int kChunkVectors = 4;
 constexpr int64_t kShortBytes = 8 << 10;            // rows up to these bytes are taken by one vector a thread
 constexpr int kWholeChunks = 2;                     // rows of at most this many chunks are never split
 constexpr int kLongThreads = 1024, kLongVectors = 2;  // for rows taken whole where they are few
-constexpr int64_t kLongRows = 96;                   // rows from which on they are, whatever their length,
-constexpr int64_t kLongBytes = 128 << 10;           // and the length up to which they are, however few
+// Few rows are taken whole, by 1,024 threads each, from kLongRows on and up to kLongBytes; else they are split over
+// more workgroups and joined by a second kernel (20 alternatives of 128 rows of 128,256 bf16: 18.7 us whole, 21.2
+// split; of 48: 19.4 and 15.5; of one row of 151,936: 21.9 and 12.9; of 32 of 262,144, none: 17.8 and 8.5).
+constexpr int64_t kLongRows = 96;
+constexpr int64_t kLongBytes = 128 << 10;
 
 // Rows from which on a workgroup of kThreads each keeps the GPU busy; fewer are better taken by 1,024 threads
 // each (alternatives of 333 rows of 201 KB: 18.9 us by 256 threads, 20.9 by 1,024; of 400 rows of 304 KB: 36.4
@@ -683,6 +696,10 @@ void launch_rows(const RowArgs &a, int threads, int64_t n, hipStream_t stream) {
 }
 
 // ---------------------------------------------------------------- gradient
+// One reading and one writing of the row, nothing kept between elements: p from the row's statistics, one
+// exponential each.  A workgroup takes one part of two vectors a thread, so that very many are at different
+// points of load and store, which mixes reads and writes best; loads ahead of the stores gain nothing.  Bound by HBM: 2,048
+// rows of 128,256 bf16 take 160 us, 6.5 TB/s read and written (a large copy gets 5.1).
 constexpr int kGradVectors = 2;
 
 // Gradients up to the Infinity Cache's size are left in it for what reads them next, which is faster here, too

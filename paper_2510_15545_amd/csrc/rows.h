@@ -331,7 +331,7 @@ __device__ __forceinline__ void add_chunk(const uint32_t (&w)[NV][4], float c2, 
         m = fmaxf(m, vm[i]);
     }
     const float d = fmaxf((a.m - m) * c2, kLowest), f = __builtin_amdgcn_exp2f(d);
-    float s[2] = {a.s * f, 0.0f}, e[2] = {ENTROPY ? fmaf(a.s, d, a.e) * f : 0.0f, 0.0f};
+    float s[2] = {}, e[2] = {};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
 #pragma unroll
@@ -347,9 +347,10 @@ __device__ __forceinline__ void add_chunk(const uint32_t (&w)[NV][4], float c2, 
             }
         }
     }
+    // the chunk's sums by themselves, then to the others': one rounding a chunk at the size of the whole sum
+    if constexpr (ENTROPY) a.e = fmaf(fmaf(a.s, d, a.e), f, e[0] + e[1]);
+    a.s = fmaf(a.s, f, s[0] + s[1]);
     a.m = m;
-    a.s = s[0] + s[1];
-    a.e = e[0] + e[1];
 }
 
 // The wave's sums from its threads', the same in every lane.
