@@ -166,6 +166,29 @@ def test_scales(scale):
     check_logprobs(x, ur.placed(x, "f32"), rng.integers(0, 9000, 6), (0.5 + rng.random(6)).astype(np.float32), 3)
 
 
+@pytest.mark.parametrize("n", [100, 512])
+@pytest.mark.parametrize("below", [0.0, 0.859375, 4.78125])
+def test_long_rows_of_equal_logits(n, below):
+    """Every addition to such a row's sum rounds the same way: it must not be one an element at the size of the sum."""
+    import torch
+
+    import paper_2510_15545_amd as tt
+
+    v = 300007
+    row = np.zeros((1, v))
+    row[0, 777] = below
+    want = ur.logprobs(row, np.array([777]), None, 2)
+    logits = torch.from_numpy(row).to(torch.bfloat16).cuda().expand(n, v).contiguous()
+    ids = torch.full((n,), 777, dtype=torch.int32, device="cuda")
+    got = tt.logprobs(v, logits, ids, n_top=2, entropy=True)
+    # 16 additions within a chunk and 1 to join its halves, at most 37 (or 19) chunks, 8 joins of threads and waves;
+    # the exponent is off by 3 steps of at most 6.9, the exponential by 2
+    bound = U * (17 + 37 + 8 + 3 * 6.9 + 2)
+    for name in ("logprob", "lse"):
+        close(getattr(got, name), np.repeat(want[name], n), bound + U * np.repeat(np.abs(want[name]), n), name)
+    assert np.array_equal(got.top_ids.cpu().numpy(), np.repeat(want["top_ids"], n, 0))
+
+
 def test_many_rows_with_alternatives_take_several_groups():
     """The keys of more rows than the workspace's bound holds."""
     import torch
