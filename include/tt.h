@@ -531,11 +531,11 @@ enum { TT_BF16 = 0, TT_F16 = 1, TT_F32 = 2 };
  * A row without a logit above minus infinity has M = lse = -inf, L = 0, H = 0, logprob = -inf and
  * no alternatives.
  * Reads every logit once.  workspace: tt_logprobs_workspace_size bytes (0 where a row is one
- * workgroup's: rows of at most 128 KB, or 96 rows or more), 16-byte aligned, no initialisation; calls that
- * overlap in time must not share it.  One kernel on `stream`, two where rows are split (each for at most
- * 2^18 workgroups, or 128 MB of workspace).  TT_EINVAL on a bad size or type, a missing
- * pointer or one not aligned to its elements, TT_EUNSUPPORTED for v > 2^23 or n_top > 128,
- * TT_EWORKSPACE when the workspace is missing or too small.
+ * workgroup's: rows of at most 128 KB, or 96 rows or more, 192 of over 512 KB), 16-byte aligned, no
+ * initialisation; calls that overlap in time must not share it.  One kernel on `stream`, two where rows
+ * are split (each for at most 2^18 workgroups, or 128 MB of workspace).  TT_EINVAL on a bad size or
+ * type, a missing pointer or one not aligned to its elements, TT_EUNSUPPORTED for v > 2^23 or
+ * n_top > 128, TT_EWORKSPACE when the workspace is missing or too small.
  */
 int tt_logprobs_workspace_size(int32_t n_rows, int32_t v, int32_t dtype, int32_t n_top, size_t *bytes);
 int tt_logprobs(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,

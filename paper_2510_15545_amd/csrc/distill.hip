@@ -433,12 +433,13 @@ __global__ __launch_bounds__(kThreads) void list_grad(ListArgs a, int parts) {
     if (mine.id >= 0 && mine.id >= x0 && mine.id < x1) out[mine.id] = (T)encode<DT>(mine.grad);
 }
 
-// Threads and vectors of list_whole for rows of more than kShortRow bytes; shorter rows are few vectors long and
-// taken by kThreads, more of them at once.
+// list_whole takes rows by 1,024 threads each, or by kThreads: up to kTinyRow bytes, and from many_rows on up to
+// kShortRow bytes with the gradient and of any length without (gradients of one row of 16,000 bf16 take 7.3 us by 1,024
+// threads and 10.0 by kThreads, of 2,000 of them 38.7 and 31.7, of 500 of 8,000 11.6 and 9.8; losses of 1,000 of 50,257
+// 25.0 and 21.9, of 512 of 151,936 30.3 and 34.2, of 700 40.6 and 37.7).
 constexpr int kLongThreads = 1024, kLongVectors = 2;
+constexpr int64_t kTinyRow = 12 << 10;
 constexpr int64_t kShortRow = 32 << 10;
-// Without the gradient kThreads take rows whole from this many rows on (1,000 of 50,257: 21.9 us, 25.0 by 1,024
-// threads each; 512 of 151,936: 34.2 and 30.3; 700: 37.7 and 40.6).
 int64_t many_rows(int64_t row_bytes) { return row_bytes <= (256 << 10) ? 256 : 640; }
 // Rows of more than kSplitRow bytes are split where there are fewer than kFewRows of them: too many compute units
 // would be without one (gradients of 16 rows of 151,936: 15.5 us split, 24.2 whole; of 96: 27.5 and 26.0; of 128: 33
@@ -462,7 +463,7 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
     const int chunk = kChunkVectors * kThreads * elements_per_vector(dtype), chunks = (v + chunk - 1) / chunk;
     int64_t most = kMaxGrid;
     if (v <= kMaxBits && (n_rows >= kFewRows || bytes <= kSplitRow)) {
-        p.threads = bytes <= kShortRow || (!grad && n_rows >= many_rows(bytes)) ? kThreads : kLongThreads;
+        p.threads = bytes <= kTinyRow || (n_rows >= many_rows(bytes) && (!grad || bytes <= kShortRow)) ? kThreads : kLongThreads;
     } else {
         int64_t parts = n_rows > 0 ? (kFullGrid + n_rows - 1) / n_rows : 1;
         const int64_t least = (v + kMaxBits - 1) / kMaxBits;

@@ -7,7 +7,7 @@
 //   alternatives: the largest x, ties by the lower index, minus infinity never listed
 //   d_j = beta (g ([j = id] - p_j) - h p_j (lp_j + H)), upstream gradients g of lp_id and h of H
 //
-// One pass over the row: row_stream, a workgroup for a row or a part of it, by chunks of 16 to 32 KB whose
+// One pass over the row: row_stream, a workgroup for a row or a part of it, by chunks of 4 to 32 KB whose
 // loads are in flight while the chunk before is worked on.  Each thread keeps the largest value and the sums
 // (base 2, v_exp_f32) of what it has seen: in fp32 over a thread's elements, chunk by chunk, in fp64
 // from the waves' sums on.  The token's logit is read behind the first chunk's loads.
@@ -37,13 +37,14 @@ constexpr int kSelect = 1024;                       // keys that are ordered in 
 constexpr int kGroups = 256;                        // lane groups whose largest values give the bound
 constexpr int kChunkVectors = 4;
 constexpr int64_t kShortBytes = 8 << 10;            // rows up to these bytes are taken by one vector a thread
-constexpr int kWholeChunks = 2;                     // rows of at most this many chunks are never split
-constexpr int kLongThreads = 1024, kLongVectors = 2;  // for rows taken whole where they are few
-// Few rows are taken whole, by 1,024 threads each, from kLongRows on and up to kLongBytes; else they are split over
-// more workgroups and joined by a second kernel (20 alternatives of 128 rows of 128,256 bf16: 18.7 us whole, 21.2
-// split; of 48: 19.4 and 15.5; of one row of 151,936: 21.9 and 12.9; of 32 of 262,144, none: 17.8 and 8.5).
-constexpr int64_t kLongRows = 96;
+// For rows of over one chunk taken whole where they are few (20 alternatives of one row of 16,000 bf16: 7.2 us, 9.3 by
+// kThreads; of 200: 8.2 and 10.4; of 50,257 of one to 64: 11.9 to 13.3, 11.9 to 15.2 split).
+constexpr int kLongThreads = 1024, kLongVectors = 2;
+// Rows up to these bytes are taken whole, by 1,024 threads each, however few they are; longer ones from few_rows on; fewer are split over more workgroups and
+// joined by a second kernel (20 alternatives of one row of 151,936 bf16: 12.9 us, 21.9 whole; of 48 of 128,256: 15.5
+// and 19.4; of 128: 21.2 and 18.7; of 96 of a million: 50 and 75; of 160: 67 and 75; of 250: 88 and 83).
 constexpr int64_t kLongBytes = 128 << 10;
+int64_t few_rows(int64_t row_bytes) { return row_bytes <= (512 << 10) ? 96 : 192; }
 
 // Rows from which on a workgroup of kThreads each keeps the GPU busy; fewer are better taken by 1,024 threads
 // each (alternatives of 333 rows of 201 KB: 18.9 us by 256 threads, 20.9 by 1,024; of 400 rows of 304 KB: 36.4
@@ -648,15 +649,15 @@ struct Plan {
     size_t sums, total;
 };
 
-// Rows whole, a workgroup each, where the rows fill the GPU or have few chunks; else in as many parts as fill it.
+// Rows whole, a workgroup each, where they are enough or short; else in as many parts as fill the GPU.
 Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top) {
     Plan p;
     const int chunk = kChunkVectors * kThreads * elements_per_vector(dtype), chunks = (v + chunk - 1) / chunk;
     int64_t parts = 1;
     p.threads = kThreads;
     const int64_t bytes = (int64_t)v * element_bytes(dtype);
-    if (chunks > kWholeChunks && n_rows < many_rows(bytes)) {
-        if (n_rows >= kLongRows || bytes <= kLongBytes) p.threads = kLongThreads;
+    if (chunks > 1 && n_rows < many_rows(bytes)) {
+        if (n_rows >= few_rows(bytes) || bytes <= kLongBytes) p.threads = kLongThreads;
         else parts = n_rows > 0 ? (kFullGrid + n_rows - 1) / n_rows : 1;
         if (parts > chunks) parts = chunks;
     }

@@ -56,7 +56,7 @@ def compare(loss, grad, values, ids, lp, beta, tail, weight, dtype, id_map=None)
 @pytest.mark.parametrize("n,v,dtype,k", [(1, 1, "bf16", 1), (2, 2, "f32", 1), (3, 7, "f16", 5), (2, 9, "f32", 9), (4, 640, "bf16", 20),
                                          (3, 4099, "f32", 64), (5, 16385, "bf16", 128), (2, 50257, "f16", 20), (3, 50257, "f32", 33),
                                          (2, 151936, "bf16", 64), (1100, 700, "bf16", 8), (260, 50257, "bf16", 64), (140, 50257, "f32", 16),
-                                         (3, 300007, "bf16", 128), (2, 270001, "f32", 20), (257, 20000, "f16", 128)])
+                                         (3, 300007, "bf16", 128), (2, 270001, "f32", 20), (257, 20000, "f16", 128), (300, 9001, "bf16", 20), (4, 3001, "f32", 20)])
 def test_distill(n, v, dtype, k, tail):
     print(f"[case] distill {n}x{v} {dtype} top {k} tail {tail}", flush=True)
     rng = np.random.default_rng([n, v, k])

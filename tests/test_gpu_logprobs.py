@@ -59,7 +59,7 @@ CASES = [(1, 1, "bf16", 1), (1, 2, "f32", 5), (3, 3, "f16", 3), (5, 7, "bf16", 1
          (1, 151936, "bf16", 20), (3, 151936, "f32", 64),
          # enough rows for the wide parts
          (1100, 640, "bf16", 5), (5, 65535, "bf16", 20), (3, 65536, "f16", 128), (2, 65537, "bf16", 8), (6, 32768, "f32", 1), (3, 32771, "f32", 20), (1030, 50, "f32", 128), (300, 50257, "bf16", 20), (300, 50257, "f16", 0), (170, 50257, "f32", 64),
-         (520, 32768, "bf16", 128), (70, 262144, "bf16", 8)]
+         (520, 32768, "bf16", 128), (70, 262144, "bf16", 8), (97, 262151, "bf16", 20), (260, 9001, "f16", 5)]
 
 
 @pytest.mark.parametrize("n,v,dtype,n_top", CASES)
