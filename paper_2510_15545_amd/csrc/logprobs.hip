@@ -16,13 +16,13 @@
 // workgroup's 64 or 256 groups of threads hold a largest value that reaches the k-th largest of the groups',
 // so every one of the k largest elements does.  That bound is formed after chunks 1, 2, 4, 8, ..., and elements
 // that reach it are staged in LDS as 64-bit keys (value, then lower index), over a row of N chunks about
-// k (1 + ln N) of them; in the end the keys are ordered by counting.  A row's only workgroup finishes it; with
-// several, each hands its sums and keys to row_finish.
+// k (1 + log2 N) of them (of long rows their whole vectors, told apart at the end); then the keys are ordered by
+// counting.  A row's only workgroup finishes it; with several, each hands its sums and keys to row_finish.
 //
 // What bounds it: the reading of the logits, at 6.4 to 6.9 TB/s on a row set beyond the Infinity Cache (4,096
 // rows of 151,936 bf16: 187 us a pass, 6.7 TB/s; a kernel that only reads gets no more), and the VALU where the
 // alternatives are wanted (about 9 issue slots an element for the statistics, the exponential four of them; 1,024
-// rows of 262,144 with 64 alternatives: 96 us against 80 to read them; the VALU is busy 78% of the cycles).  Few rows
+// rows of 262,144 with 64 alternatives: 94 us against 80 to read them; the VALU is busy 77% of the cycles).  Few rows
 // are latency: one row of 640 takes 5 us on the GPU, one of 151,936 with 20 alternatives 6.3 for its 19 parts and 6.5
 // to join them.
 #include "rows.h"
@@ -40,9 +40,14 @@ constexpr int64_t kShortBytes = 8 << 10;            // rows up to these bytes ar
 // For rows of over one chunk taken whole where they are few (20 alternatives of one row of 16,000 bf16: 7.2 us, 9.3 by
 // kThreads; of 200: 8.2 and 10.4; of 50,257 of one to 64: 11.9 to 13.3, 11.9 to 15.2 split).
 constexpr int kLongThreads = 1024, kLongVectors = 2;
-// Rows up to these bytes are taken whole, by 1,024 threads each, however few they are; longer ones from few_rows on; fewer are split over more workgroups and
-// joined by a second kernel (20 alternatives of one row of 151,936 bf16: 12.9 us, 21.9 whole; of 48 of 128,256: 15.5
-// and 19.4; of 128: 21.2 and 18.7; of 96 of a million: 50 and 75; of 160: 67 and 75; of 250: 88 and 83).
+// Rows of more bytes stage whole vectors where they are taken by kThreads, or have many alternatives (20 of 1,000 rows
+// of 24,000 bf16: 19.0 us so, 19.4 by elements; of 50,257: 26.9 and 29.4, 128: 38.4 and 47.3; 20 of 2,000 of 16,000: 27.8
+// and 26.0; by 1,024 threads, 128 of 64 rows of 50,257: 19.7 and 21.4, 20: 13.3 and 12.7).
+constexpr int64_t kVectorBytes = 32 << 10;
+// Rows up to these bytes are taken whole, by 1,024 threads each, however few they are; longer ones from few_rows
+// on; fewer are split over more workgroups and joined by a second kernel (20 alternatives of one row of 151,936 bf16:
+// 12.9 us, 21.9 whole; of 48 of 128,256: 15.5 and 19.4; of 128: 21.2 and 18.7; of 96 of a million: 50 and 75; of 160: 67
+// and 75; of 250: 88 and 83).
 constexpr int64_t kLongBytes = 128 << 10;
 int64_t few_rows(int64_t row_bytes) { return row_bytes <= (512 << 10) ? 96 : 192; }
 
@@ -231,8 +236,10 @@ __device__ __noinline__ void select_exactly(const typename Elem<DT>::T *row, int
     __syncthreads();
 }
 
-// The elements of a row that may be among its k largest, chunk by chunk.
-template <int DT, int NV, int THREADS>
+// The elements of a row that may be among its k largest, chunk by chunk.  VECTORS: whole vectors are staged, with
+// their largest value, and those that reach the last bound are read again for their elements: fewer instructions in
+// a long row's stream, but another round trip at its end.
+template <int DT, int NV, int THREADS, bool VECTORS>
 struct TopSet {
     static constexpr int kPer = Elem<DT>::kPer, kStage = TopLds<THREADS>::kStage;
     TopLds<THREADS> &sh;
@@ -296,16 +303,51 @@ struct TopSet {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (__ballot(vm[i] >= lowest) == 0) continue;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                const float x = value<DT>(w[i], j);
-                if (__ballot(x >= lowest) == 0) continue;
-                const int at = vector_at<DT, THREADS>(x_chunk, i) + j;
+            auto put = [&](float x, int at) {
                 const bool in = x > lowest || (x == lowest && at <= bound.index);
                 const uint64_t hit = __ballot(in);
                 const int slot = staged + lanes_below(hit);
                 if (in && slot < kStage) sh.stage[wave][slot] = full_key(order_key(x), at);
                 staged += __popcll(hit);
+            };
+            const int at = vector_at<DT, THREADS>(x_chunk, i);
+            if constexpr (VECTORS) {
+                put(vm[i], at);
+                continue;
+            }
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const float x = value<DT>(w[i], j);
+                if (__ballot(x >= lowest) != 0) put(x, at + j);
+            }
+        }
+    }
+
+    // The elements of the staged vectors, read again, that reach the bound, to dst; their number goes to sh.total.
+    __device__ __forceinline__ void expand(const typename Elem<DT>::T *row, int x1, uint64_t *dst, int capacity) {
+        const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+        const uint64_t from = bound.full();
+        for (int i = lane; i - lane < staged; i += kWave) {
+            const uint64_t key = i < staged ? sh.stage[wave][i] : 0;
+            const bool in = i < staged && (uint32_t)(key >> 32) >= bound.key;
+            const int at = (int)(0xFFFFFFFFu - (uint32_t)key);
+            uint64_t mine[kPer];
+            int n = 0;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const float x = in && at + j >= 0 && at + j < x1 ? decode<DT>(row[at + j]) : -INFINITY;
+                mine[j] = x > -INFINITY ? full_key(order_key(x), at + j) : 0;  // no NaN
+                n += __popcll(__ballot(mine[j] >= from));
+            }
+            int base = 0;
+            if (lane == 0) base = atomicAdd(&sh.total, n);
+            base = __builtin_amdgcn_readfirstlane(base);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const uint64_t hit = __ballot(mine[j] >= from);
+                const int slot = base + lanes_below(hit);
+                if (mine[j] >= from && slot < capacity) dst[slot] = mine[j];
+                base += __popcll(hit);
             }
         }
     }
@@ -322,6 +364,8 @@ struct TopSet {
         int n = 0;
         if (over) {
             n = capacity + 1;
+        } else if constexpr (VECTORS) {
+            expand(row, x1, dst, capacity);
         } else {
             for (int i = lane; i - lane < staged; i += kWave) n += __popcll(__ballot(i < staged && sh.stage[wave][i] >= from));
         }
@@ -335,6 +379,7 @@ struct TopSet {
             select_exactly<DT, THREADS>(row, x0 > 0 ? x0 : 0, x1, k, dst, sh.slots, &sh.total);
             return k;
         }
+        if constexpr (VECTORS) return total;
         for (int i = lane; i - lane < staged; i += kWave) {
             const uint64_t key = i < staged ? sh.stage[wave][i] : 0;
             const bool in = i < staged && key >= from;
@@ -442,8 +487,8 @@ __device__ __forceinline__ void write_top(const RowArgs &a, int64_t row, const R
     a.top_logprobs[row * a.n_top + i] = (float)lp;
 }
 
-// A part of a row by a workgroup; FINISH: the row is one part, and finished here.
-template <int DT, int THREADS, int NV, bool TOP, bool ENTROPY, bool FINISH>
+// A part of a row by a workgroup; FINISH: the row is one part, and finished here.  VECTORS: as in TopSet.
+template <int DT, int THREADS, int NV, bool TOP, bool ENTROPY, bool FINISH, bool VECTORS>
 __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stream(RowArgs a) {
     constexpr int kWaves = THREADS / kWave;
     __shared__ Sum sh_sum[kWaves];
@@ -457,15 +502,17 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stre
     const int x0 = part * a.part_width - lead_of<DT>(row, a.v), x1 = FINISH || part + 1 == a.parts ? a.v : x0 + a.part_width;
     const float beta = scale_of(a.inv_temp, row_i), c2 = beta * kLog2e;
     const int32_t id = FINISH ? token_of(a, row_i) : -1;
-    float x_id = 0.0f;
+    float x_id = 0.0f;  // read behind the first chunk's loads, or where registers are few behind the sums
+    constexpr bool kLate = TOP && THREADS == kLongThreads;
     int count = 0;
     Sum mine = {-INFINITY, 0.0f, 0.0f};
-    TopSet<DT, NV, THREADS> top{sh, a.n_top};
-    for_chunks<DT, NV, THREADS, true, false, true, TOP ? 1 : 2>(row, a.v, x0, x1, [&] { x_id = token_logit(a, row_i, id); }, [&](uint32_t(&w)[NV][4], int x) {
+    TopSet<DT, NV, THREADS, VECTORS> top{sh, a.n_top};
+    for_chunks<DT, NV, THREADS, true, false, true, TOP ? 1 : 2>(row, a.v, x0, x1, [&] { if (!kLate) x_id = token_logit(a, row_i, id); }, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         add_chunk<DT, NV, ENTROPY>(w, c2, mine, vm);
         if constexpr (TOP) top.add(w, vm, x);
     });
+    if (kLate) x_id = token_logit(a, row_i, id);
     mine = wave_join<ENTROPY>(mine, c2);
     if (lane == 0) sh_sum[wave] = mine;
     if constexpr (TOP)
@@ -678,11 +725,21 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top) {
 template <int DT, bool TOP, bool ENTROPY>
 void launch_rows(const RowArgs &a, int threads, int64_t n, hipStream_t stream) {
     const unsigned grid = (unsigned)(n * a.parts);
-    if (threads == kLongThreads) row_stream<DT, kLongThreads, kLongVectors, TOP, ENTROPY, true><<<grid, kLongThreads, 0, stream>>>(a);
-    else if (a.parts > 1) row_stream<DT, kThreads, kChunkVectors, TOP, ENTROPY, false><<<grid, kThreads, 0, stream>>>(a);
-    // 4,000 rows of 2,000 (5 alternatives): 19.4 us by one vector, 22.8 by four; 333 of 50,257 fp32: 33.4 and 19.1
-    else if ((int64_t)a.v * element_bytes(DT) <= kShortBytes) row_stream<DT, kThreads, 1, TOP, ENTROPY, true><<<grid, kThreads, 0, stream>>>(a);
-    else row_stream<DT, kThreads, kChunkVectors, TOP, ENTROPY, true><<<grid, kThreads, 0, stream>>>(a);
+    const int64_t bytes = (int64_t)a.v * element_bytes(DT);
+    const bool vectors = TOP && bytes > kVectorBytes && (threads == kThreads || a.n_top > kFewTop);
+    if (threads == kLongThreads) {
+        if (vectors) row_stream<DT, kLongThreads, kLongVectors, TOP, ENTROPY, true, TOP><<<grid, kLongThreads, 0, stream>>>(a);
+        else row_stream<DT, kLongThreads, kLongVectors, TOP, ENTROPY, true, false><<<grid, kLongThreads, 0, stream>>>(a);
+    } else if (a.parts > 1) {
+        row_stream<DT, kThreads, kChunkVectors, TOP, ENTROPY, false, false><<<grid, kThreads, 0, stream>>>(a);
+    } else if (bytes <= kShortBytes) {
+        // 4,000 rows of 2,000 (5 alternatives): 19.4 us by one vector, 22.8 by four; 333 of 50,257 fp32: 33.4 and 19.1
+        row_stream<DT, kThreads, 1, TOP, ENTROPY, true, false><<<grid, kThreads, 0, stream>>>(a);
+    } else if (vectors) {
+        row_stream<DT, kThreads, kChunkVectors, TOP, ENTROPY, true, TOP><<<grid, kThreads, 0, stream>>>(a);
+    } else {
+        row_stream<DT, kThreads, kChunkVectors, TOP, ENTROPY, true, false><<<grid, kThreads, 0, stream>>>(a);
+    }
 }
 
 template <int DT>
@@ -699,8 +756,8 @@ void launch_rows(const RowArgs &a, int threads, int64_t n, hipStream_t stream) {
 // ---------------------------------------------------------------- gradient
 // One reading and one writing of the row, nothing kept between elements: p from the row's statistics, one
 // exponential each.  A workgroup takes one part of two vectors a thread, so that very many are at different
-// points of load and store, which mixes reads and writes best; loads ahead of the stores gain nothing.  Bound by HBM: 2,048
-// rows of 128,256 bf16 take 160 us, 6.5 TB/s read and written (a large copy gets 5.1).
+// points of load and store, which mixes reads and writes best; loads ahead of the stores gain nothing.  Bound by
+// HBM: 2,048 rows of 128,256 bf16 take 160 us, 6.5 TB/s read and written (a large copy gets 5.1).
 constexpr int kGradVectors = 2;
 
 // Gradients up to the Infinity Cache's size are left in it for what reads them next, which is faster here, too

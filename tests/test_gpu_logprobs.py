@@ -177,10 +177,10 @@ def test_long_rows_of_equal_logits(n, below):
     v = 300007
     row = np.zeros((1, v))
     row[0, 777] = below
-    want = ur.logprobs(row, np.array([777]), None, 2)
+    want = ur.logprobs(row, np.array([777]), None, 128)
     logits = torch.from_numpy(row).to(torch.bfloat16).cuda().expand(n, v).contiguous()
     ids = torch.full((n,), 777, dtype=torch.int32, device="cuda")
-    got = tt.logprobs(v, logits, ids, n_top=2, entropy=True)
+    got = tt.logprobs(v, logits, ids, n_top=128, entropy=True)
     # 16 additions within a chunk and 1 to join its halves, at most 37 (or 19) chunks, 8 joins of threads and waves;
     # the exponent is off by 3 steps of at most 6.9, the exponential by 2
     bound = U * (17 + 37 + 8 + 3 * 6.9 + 2)
