@@ -115,14 +115,16 @@ def lib():
         L.tt_step.argtypes = [VP, VP, i32, i32, i32, P, P, P, P, i32, i32, i32, P, i64, P, i64, P, P,
                               P, P, P, P, P, P, P, P, P, sz, P]
         L.tt_step.restype = ctypes.c_int
-        L.tt_logprobs_workspace_size.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
-        L.tt_logprobs_workspace_size.restype = ctypes.c_int
+        for f in (L.tt_logprobs_workspace_size, L.tt_logprobs_workspace_used):
+            f.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
+            f.restype = ctypes.c_int
         L.tt_logprobs.argtypes = [i32, i32, i32, P, i64, P, P, i32, P, P, P, P, P, P, P, sz, P]
         L.tt_logprobs.restype = ctypes.c_int
         L.tt_logprobs_backward.argtypes = [i32, i32, i32, P, i64, P, P, P, P, P, P, P, i64, P]
         L.tt_logprobs_backward.restype = ctypes.c_int
-        L.tt_distill_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
-        L.tt_distill_workspace_size.restype = ctypes.c_int
+        for f in (L.tt_distill_workspace_size, L.tt_distill_workspace_used):
+            f.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+            f.restype = ctypes.c_int
         L.tt_distill.argtypes = [i32, i32, i32, P, i64, P, i32, P, P, P, i32, i32, P, P, P, i64, P, sz, P]
         L.tt_distill.restype = ctypes.c_int
         _lib = L
@@ -492,8 +494,8 @@ def _dtype_code(dtype) -> int:
 
 
 def logprobs_workspace(n_rows: int, v: int, dtype, n_top: int = 0, device="cuda"):
-    """A workspace for logprobs on n_rows rows of v logits of this type (empty when none is needed), reusable by calls
-    that do not overlap in time."""
+    """A workspace for logprobs on up to n_rows rows of v logits of this type and up to n_top alternatives (empty when
+    none is needed), reusable by calls that do not overlap in time."""
     n = ctypes.c_size_t(0)
     _check(lib().tt_logprobs_workspace_size(int(n_rows), int(v), _dtype_code(dtype), int(n_top), ctypes.byref(n)),
            "tt_logprobs_workspace_size")
@@ -524,7 +526,7 @@ def logprobs(v: int, logits, ids=None, inv_temperature=None, n_top: int = 0, ent
         to = [_array(out[0], f32, n, "logprob", dev), _array(out[1], f32, n, "lse", dev), _array(out[2], f32, 2 * n, "stats", dev),
               _array(out[3], f32, n, "entropy", dev), _array(out[4], i32, n * n_top, "top_ids", dev),
               _array(out[5], f32, n * n_top, "top_logprobs", dev)]
-    ws, ws_bytes, _held = _needed_workspace(workspace, _spread_bytes("tt_logprobs_workspace_size", n, v, code, n_top), dev)
+    ws, ws_bytes, _held = _needed_workspace(workspace, _spread_bytes("tt_logprobs_workspace_used", n, v, code, n_top), dev)
     st = lib().tt_logprobs(n, v, code, address, ld, _array(inv_temperature, f32, n, "inv_temperature", dev),
                            _array(ids, i32, n, "ids", dev), n_top, *to, ws, ws_bytes, _stream_handle(stream))
     if st:
@@ -562,8 +564,8 @@ def logprobs_backward(v: int, logits, ids, stats, grad_logprob, entropy=None, gr
 
 
 def distill_workspace(n_rows: int, v: int, dtype, n_top: int, grad: bool = False, device="cuda"):
-    """A workspace for distill with these bounds (empty when none is needed), reusable by calls that do not overlap in
-    time."""
+    """A workspace for distill on up to n_rows rows of v logits of this type and lists of up to n_top tokens (empty when
+    none is needed), reusable by calls that do not overlap in time."""
     n = ctypes.c_size_t(0)
     _check(lib().tt_distill_workspace_size(int(n_rows), int(v), _dtype_code(dtype), int(n_top), 1 if grad else 0,
                                            ctypes.byref(n)), "tt_distill_workspace_size")
@@ -604,7 +606,7 @@ def distill(v: int, logits, top_ids, top_logprobs, tail: bool = False, id_map=No
             raise ValueError(f"dlogits must be {logits.dtype} on the logits' device")
     elif dlogits is not None:
         raise ValueError("dlogits needs grad_loss")
-    nbytes = _spread_bytes("tt_distill_workspace_size", n, v, code, n_top, 0 if grad_loss is None else 1)
+    nbytes = _spread_bytes("tt_distill_workspace_used", n, v, code, n_top, 0 if grad_loss is None else 1)
     ws, ws_bytes, _held = _needed_workspace(workspace, nbytes, dev)
     st = lib().tt_distill(n, v, code, address, ld, _array(inv_temperature, f32, n, "inv_temperature", dev), n_top,
                           _array(top_ids, i32, n * n_top, "top_ids", dev), _array(top_logprobs, f32, n * n_top, "top_logprobs", dev),

@@ -453,7 +453,7 @@ constexpr size_t kCachedBytes = size_t(96) << 20;
 struct Plan {
     int parts, part_width;  // parts == 0: list_whole
     int threads;
-    int64_t rows;
+    int64_t rows, most;  // of one launch; at most
     size_t row_grad, entries, total;
 };
 
@@ -478,6 +478,7 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
     }
     const int64_t groups = (n_rows + most - 1) / most;
     p.rows = groups == 0 ? 0 : (n_rows + groups - 1) / groups;
+    p.most = most;
     if (p.parts > 0) {
         p.row_grad = round256((size_t)p.rows * p.parts * sizeof(float2));
         p.entries = p.row_grad + (grad ? round256((size_t)p.rows * sizeof(RowGrad)) : 0);
@@ -524,8 +525,22 @@ int launch_rows(const ListArgs &a, const Plan &p, int64_t n, hipStream_t stream)
 
 }  // namespace
 
-size_t distill_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
+size_t distill_workspace_used(int32_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
     return plan_of(n_rows, v, dtype, n_top, grad).total;
+}
+
+// The most that any number of rows up to n_rows uses.  From kFullGrid rows on their parts are as few as the bitmap
+// allows, and a group of them is largest where it is the only one.
+size_t distill_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
+    size_t most = 0;
+    auto add = [&](int64_t n) {
+        const size_t used = plan_of(n, v, dtype, n_top, grad).total;
+        most = used > most ? used : most;
+    };
+    for (int64_t n = 1; n <= n_rows && n <= kFullGrid; ++n) add(n);
+    const int64_t group = n_rows > kFullGrid ? plan_of(n_rows, v, dtype, n_top, grad).most : 0;
+    if (group > kFullGrid) add(group < n_rows ? group : n_rows);
+    return most;
 }
 
 int launch_distill(const DistillArgs &l, void *workspace, size_t workspace_bytes, hipStream_t stream) {

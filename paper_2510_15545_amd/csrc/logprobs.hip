@@ -839,7 +839,18 @@ void launch_grad(const GradArgs &a, bool keep, unsigned grid, hipStream_t stream
 
 }  // namespace
 
-size_t logprobs_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top) { return plan_of(n_rows, v, dtype, n_top).total; }
+size_t logprobs_workspace_used(int32_t n_rows, int32_t v, int dtype, int n_top) { return plan_of(n_rows, v, dtype, n_top).total; }
+
+// The most that any number of rows up to n_rows uses: more rows are split less, and from few_rows on not at all.
+size_t logprobs_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top) {
+    const int64_t few = few_rows((int64_t)v * element_bytes(dtype));
+    size_t most = 0;
+    for (int64_t n = 1; n <= n_rows && n < few; ++n) {
+        const size_t used = plan_of(n, v, dtype, n_top).total;
+        most = used > most ? used : most;
+    }
+    return most;
+}
 
 int launch_logprobs(const LogprobsArgs &l, void *workspace, size_t workspace_bytes, hipStream_t stream) {
     const Plan p = plan_of(l.n_rows, l.v, l.dtype, l.n_top);

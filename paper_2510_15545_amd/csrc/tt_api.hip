@@ -467,6 +467,13 @@ int tt_logprobs_workspace_size(int32_t n_rows, int32_t v, int32_t dtype, int32_t
     return TT_OK;
 }
 
+int tt_logprobs_workspace_used(int32_t n_rows, int32_t v, int32_t dtype, int32_t n_top, size_t *bytes) {
+    if (bytes == nullptr || n_rows < 0 || v < 1 || !dtype_ok(dtype) || n_top < 0) return TT_EINVAL;
+    if (v > kMaxLogitsRow || n_top > kMaxListed) return TT_EUNSUPPORTED;
+    *bytes = tt::logprobs_workspace_used(n_rows, v, dtype, n_top);
+    return TT_OK;
+}
+
 int tt_logprobs(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,
                 const float *inv_temperature, const int32_t *ids, int32_t n_top, float *logprob, float *lse,
                 float *stats, float *entropy, int32_t *top_ids, float *top_logprobs, void *workspace,
@@ -531,6 +538,14 @@ int tt_distill_workspace_size(int32_t n_rows, int32_t v, int32_t dtype, int32_t 
     if (bytes == nullptr || n_rows < 0 || v < 1 || !dtype_ok(dtype) || n_top < 1) return TT_EINVAL;
     if (v > kMaxLogitsRow || n_top > kMaxListed) return TT_EUNSUPPORTED;
     *bytes = tt::distill_workspace_bytes(n_rows, v, dtype, n_top, with_grad != 0);
+    return TT_OK;
+}
+
+int tt_distill_workspace_used(int32_t n_rows, int32_t v, int32_t dtype, int32_t n_top, int32_t with_grad,
+                              size_t *bytes) {
+    if (bytes == nullptr || n_rows < 0 || v < 1 || !dtype_ok(dtype) || n_top < 1) return TT_EINVAL;
+    if (v > kMaxLogitsRow || n_top > kMaxListed) return TT_EUNSUPPORTED;
+    *bytes = tt::distill_workspace_used(n_rows, v, dtype, n_top, with_grad != 0);
     return TT_OK;
 }
 

@@ -161,7 +161,8 @@ struct LogprobsArgs {
     int32_t *top_ids;
     float *top_logprobs;
 };
-size_t logprobs_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top);
+size_t logprobs_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top);  // of up to n_rows rows
+size_t logprobs_workspace_used(int32_t n_rows, int32_t v, int dtype, int n_top);   // of n_rows rows
 int launch_logprobs(const LogprobsArgs &a, void *workspace, size_t workspace_bytes, hipStream_t stream);
 struct LogprobsGradArgs {
     int32_t n_rows, v, dtype;
@@ -191,7 +192,8 @@ struct DistillArgs {
     void *dlogits;  // null: the loss alone
     int64_t out_ld;
 };
-size_t distill_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top, bool grad);
+size_t distill_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top, bool grad);  // of up to n_rows rows
+size_t distill_workspace_used(int32_t n_rows, int32_t v, int dtype, int n_top, bool grad);   // of n_rows rows
 int launch_distill(const DistillArgs &a, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 // ---------------------------------------------------------------- fused step (step.hip)
