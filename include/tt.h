@@ -533,8 +533,8 @@ enum { TT_BF16 = 0, TT_F16 = 1, TT_F32 = 2 };
  * Reads every logit once.  workspace: tt_logprobs_workspace_size bytes serve every call of up to n_rows
  * rows and n_top alternatives (0 for rows of at most 128 KB); a call uses tt_logprobs_workspace_used bytes
  * of it, by its own numbers (0 where a row is one workgroup's: at those widths, or for 96 rows or more, 192 of over 512 KB).
- * 16-byte aligned, no initialisation; calls that overlap in time must not share it.  One kernel on `stream`, two where rows
- * are split (each for at most 2^18 workgroups, or 128 MB of workspace).  TT_EINVAL on a bad size or
+ * 16-byte aligned, no initialisation; calls that overlap in time must not share it.  One kernel on
+ * `stream`, two where rows are split (one for each 2^18 rows that are not).  TT_EINVAL on a bad size or
  * type, a missing pointer or one not aligned to its elements, TT_EUNSUPPORTED for v > 2^23 or
  * n_top > 128, TT_EWORKSPACE when the workspace is missing or smaller than what the call uses.
  */

@@ -473,8 +473,7 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top, bool grad) {
         p.part_width = each * chunk;
         p.parts = (chunks + each - 1) / each;
         most = kMaxGrid / (grad ? chunks : p.parts);
-        if (grad && (int64_t)(kCachedBytes / bytes) < most) most = (int64_t)(kCachedBytes / bytes);
-        if (most < 1) most = 1;
+        if (grad && (int64_t)(kCachedBytes / bytes) < most) most = (int64_t)(kCachedBytes / bytes);  // 3 or more: v <= 2^23
     }
     const int64_t groups = (n_rows + most - 1) / most;
     p.rows = groups == 0 ? 0 : (n_rows + groups - 1) / groups;

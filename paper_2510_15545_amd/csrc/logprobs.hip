@@ -55,7 +55,6 @@ int64_t few_rows(int64_t row_bytes) { return row_bytes <= (512 << 10) ? 96 : 192
 // each (alternatives of 333 rows of 201 KB: 18.9 us by 256 threads, 20.9 by 1,024; of 400 rows of 304 KB: 36.4
 // and 32.7; of 1,000: 54.5 and 62.0).
 int64_t many_rows(int64_t row_bytes) { return row_bytes <= (256 << 10) ? 256 : 512; }
-constexpr size_t kMaxKeyBytes = size_t(128) << 20;  // workspace: rows are taken in groups beyond
 constexpr int64_t kMaxGrid = int64_t(1) << 18;      // workgroups of one launch
 
 // Keys that a part may hand over; a part with more that reach its bound selects its k largest exactly.
@@ -711,14 +710,11 @@ Plan plan_of(int64_t n_rows, int32_t v, int dtype, int n_top) {
     const int each = (int)((chunks + parts - 1) / parts);
     p.part_width = each * chunk;
     p.parts = (chunks + each - 1) / each;
-    int64_t most = kMaxGrid / p.parts;
-    const size_t per_row = (size_t)p.parts * part_capacity(n_top) * sizeof(uint64_t);
-    if (p.parts > 1 && n_top > 0 && (int64_t)(kMaxKeyBytes / per_row) < most) most = (int64_t)(kMaxKeyBytes / per_row);
-    if (most < 1) most = 1;
+    const int64_t most = kMaxGrid / p.parts;
     const int64_t groups = (n_rows + most - 1) / most;
     p.rows = groups == 0 ? 0 : (n_rows + groups - 1) / groups;
     p.sums = p.parts > 1 ? round256((size_t)p.rows * p.parts * sizeof(float4)) : 0;
-    p.total = p.sums + (p.parts > 1 && n_top > 0 ? (size_t)p.rows * per_row : 0);
+    p.total = p.sums + (p.parts > 1 && n_top > 0 ? (size_t)p.rows * p.parts * part_capacity(n_top) * sizeof(uint64_t) : 0);
     return p;
 }
 
