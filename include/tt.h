@@ -555,10 +555,11 @@ int tt_logprobs(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, in
  *   entropy, grad_entropy both or neither (device, [n_rows]); entropy from tt_logprobs
  *   dlogits      rows of v elements of the logits' type at a stride of dlogits_ld, rounded once to
  *                nearest even; elements past v in a row are left alone.  It may be the logits' own
- *                memory (the same address and stride), but must not overlap them otherwise.
+ *                memory (the same address and stride), but must not overlap them otherwise; at another
+ *                stride its rows must not lie between theirs either.
  * A row with g = h = 0, or without a logit above minus infinity, gets zeros and is not read.
  * Logits are read once; no workspace; one kernel on `stream` (several for more than 2^18 workgroups).
- * Errors as for tt_logprobs, and TT_EINVAL for a dlogits that overlaps the logits otherwise.
+ * Errors as for tt_logprobs, and TT_EINVAL for a dlogits that meets the logits otherwise.
  */
 int tt_logprobs_backward(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int64_t logits_ld,
                          const float *inv_temperature, const int32_t *ids, const float *stats, const float *entropy,

@@ -36,13 +36,16 @@ bool extent_ok(const void *p, int32_t n_rows, int32_t v, int64_t ld, int dtype) 
     return (unsigned __int128)(uint64_t)(n_rows - 1) * (uint64_t)ld + (uint64_t)v <= most;
 }
 
-// Two matrices that either are the same memory or do not meet.
+// Two matrices that either are the same memory or do not meet: neither their spans nor, at one stride, their rows
+// (the columns of one wide buffer).
 bool same_or_apart(const void *a, int64_t lda, const void *b, int64_t ldb, int32_t n_rows, int32_t v, int dtype) {
     if (a == b && (lda == ldb || n_rows == 1)) return true;
     const uintptr_t e = dtype == TT_F32 ? 4 : 2, p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
     const uintptr_t p_end = p + ((uintptr_t)(n_rows - 1) * (uintptr_t)lda + v) * e;
     const uintptr_t q_end = q + ((uintptr_t)(n_rows - 1) * (uintptr_t)ldb + v) * e;
-    return p_end <= q || q_end <= p;
+    if (p_end <= q || q_end <= p) return true;
+    const uintptr_t ld = (uintptr_t)lda * e, row = (uintptr_t)v * e, apart = (p < q ? q - p : p - q) % ld;
+    return lda == ldb && apart >= row && ld - apart >= row;  // from a row of one to the other's next, and back
 }
 
 }  // namespace
