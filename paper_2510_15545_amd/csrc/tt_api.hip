@@ -29,6 +29,12 @@ bool dtype_ok(int32_t dtype) { return dtype == TT_BF16 || dtype == TT_F16 || dty
 
 bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+// Whether arrays of 4-byte elements are aligned to them (null is).
+template <typename... T>
+bool words_aligned(const T *...p) {
+    return ((reinterpret_cast<uintptr_t>(p) | ...) % 4) == 0;
+}
+
 // Whether a matrix of n_rows x v elements at p ends within the 2^57 bytes that an address reaches.
 bool extent_ok(const void *p, int32_t n_rows, int32_t v, int64_t ld, int dtype) {
     const uint64_t end = uint64_t(1) << 57, at = reinterpret_cast<uintptr_t>(p);
@@ -486,6 +492,7 @@ int tt_logprobs(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, in
     if (n_rows == 0) return TT_OK;
     if (!logits || (logprob && !ids) || (n_top > 0 && (!top_ids || !top_logprobs))) return TT_EINVAL;
     if (!aligned(logits, dtype == TT_F32 ? 4 : 2) || !extent_ok(logits, n_rows, v, logits_ld, dtype)) return TT_EINVAL;
+    if (!words_aligned(inv_temperature, ids, logprob, lse, stats, entropy, top_ids, top_logprobs)) return TT_EINVAL;
     tt::LogprobsArgs a;
     a.n_rows = n_rows;
     a.v = v;
@@ -512,7 +519,8 @@ int tt_logprobs_backward(int32_t n_rows, int32_t v, int32_t dtype, const void *l
     if (v > kMaxLogitsRow) return TT_EUNSUPPORTED;
     if (n_rows == 0) return TT_OK;
     if (!logits || !stats || !dlogits || (ids == nullptr) != (grad_logprob == nullptr) ||
-        (entropy == nullptr) != (grad_entropy == nullptr))
+        (entropy == nullptr) != (grad_entropy == nullptr) ||
+        !words_aligned(inv_temperature, ids, stats, entropy, grad_logprob, grad_entropy))
         return TT_EINVAL;
     const size_t e = dtype == TT_F32 ? 4 : 2;
     if (!aligned(logits, e) || !aligned(dlogits, e) || !extent_ok(logits, n_rows, v, logits_ld, dtype) ||
@@ -561,7 +569,9 @@ int tt_distill(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int
         return TT_EINVAL;
     if (v > kMaxLogitsRow || n_top > kMaxListed) return TT_EUNSUPPORTED;
     if (n_rows == 0) return TT_OK;
-    if (!logits || !top_ids || !top_logprobs || !loss || (dlogits != nullptr && grad_loss == nullptr)) return TT_EINVAL;
+    if (!logits || !top_ids || !top_logprobs || !loss || (dlogits != nullptr && grad_loss == nullptr) ||
+        !words_aligned(inv_temperature, top_ids, top_logprobs, id_map, loss, grad_loss))
+        return TT_EINVAL;
     const size_t e = dtype == TT_F32 ? 4 : 2;
     if (!aligned(logits, e) || !extent_ok(logits, n_rows, v, logits_ld, dtype)) return TT_EINVAL;
     if (dlogits != nullptr && (!aligned(dlogits, e) || !extent_ok(dlogits, n_rows, v, dlogits_ld, dtype) ||
