@@ -428,7 +428,7 @@ the given tokens, lse [n], stats [n, 2] for logprobs_backward(), entropy [n], to
 def _rows(t, v: int, n: int, name):
     """(type, address, stride) of the rows of a 2-D row-major device tensor, at least n of at least v columns."""
     code = _DTYPE_CODES.get(t.dtype)
-    if t.dim() != 2 or not t.is_cuda or t.stride(1) != 1:
+    if t.dim() != 2 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] != 1):
         raise ValueError(f"{name} must be a 2-D row-major device tensor")
     if code is None:
         raise ValueError(f"{name} must be bfloat16, float16 or float32, got {t.dtype}")
