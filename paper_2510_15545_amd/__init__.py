@@ -452,6 +452,12 @@ def _array(t, dtype, n: int, name, device: int):
     return address or None
 
 
+def _written(*tensors):
+    """Tells autograd that the caller's tensors were overwritten (a kernel's stores through their addresses pass it by):
+    a backward pass that saved one of them raises then, as after torch's own writes."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def _launch_device(t, stream) -> int:
     """The logits' device, which has to be the one that the call runs on: the stream's, or the current one."""
     device = t.get_device()
@@ -515,6 +521,7 @@ def logprobs(v: int, logits, ids=None, inv_temperature=None, n_top: int = 0, ent
     v, n_top, n = int(v), int(n_top), logits.shape[0]
     code, address, ld = _rows(logits, v, n, "logits")
     dev = _launch_device(logits, stream)
+    given = out
     if out is None:
         on = logits.device
         out = LogProbs(None if ids is None else torch.empty(n, dtype=f32, device=on), torch.empty(n, dtype=f32, device=on),
@@ -531,6 +538,8 @@ def logprobs(v: int, logits, ids=None, inv_temperature=None, n_top: int = 0, ent
                            _array(ids, i32, n, "ids", dev), n_top, *to, ws, ws_bytes, _stream_handle(stream))
     if st:
         _check(st, "tt_logprobs")
+    if given is not None:
+        _written(*given)
     return out
 
 
@@ -539,7 +548,8 @@ def logprobs_backward(v: int, logits, ids, stats, grad_logprob, entropy=None, gr
     """tt_logprobs_backward: the gradient with respect to the logits of sum(grad_logprob * logprob) + sum(grad_entropy *
     entropy), from the stats (and the entropy) that logprobs() gave for the same logits and temperatures.  ids and
     grad_logprob may both be None, and so may entropy and grad_entropy.  out: rows of the logits' type, which may be the
-    logits themselves (they are overwritten then).  A model's backward pass goes on with logits.backward(result)."""
+    logits themselves (they are overwritten then, which is an error later on if the operation that made them saved them
+    for its own backward pass).  A model's backward pass goes on with logits.backward(result)."""
     if stream is not None and out is None:
         return _on_stream(stream, logprobs_backward, v, logits, ids, stats, grad_logprob, entropy, grad_entropy,
                           inv_temperature, None, None)
@@ -547,6 +557,7 @@ def logprobs_backward(v: int, logits, ids, stats, grad_logprob, entropy=None, gr
     v, n = int(v), logits.shape[0]
     code, address, ld = _rows(logits, v, n, "logits")
     dev = _launch_device(logits, stream)
+    given = out
     if out is None:
         out = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
     out_code, to, out_ld = _rows(out, v, n, "out")
@@ -560,6 +571,8 @@ def logprobs_backward(v: int, logits, ids, stats, grad_logprob, entropy=None, gr
                                     _array(grad_entropy, f32, n, "grad_entropy", dev), to, out_ld, _stream_handle(stream))
     if st:
         _check(st, "tt_logprobs_backward")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -579,7 +592,8 @@ def distill(v: int, logits, top_ids, top_logprobs, tail: bool = False, id_map=No
     gives them.  tail: the mass that a list leaves is matched with the student's mass outside it; otherwise the list
     is renormalised.  id_map: int32, the student's token of each of the teacher's (vocab_intersection()'s t2d), -1 for
     none.  With grad_loss (float32 [n], the weights of the rows' losses) the gradient with respect to the logits is
-    formed as well, in dlogits: rows of the logits' type, made here if not given, which may be the logits themselves.
+    formed as well, in dlogits: rows of the logits' type, made here if not given, which may be the logits themselves
+    (as in logprobs_backward()).
     Returns (loss, dlogits or None)."""
     if stream is not None and (loss is None or workspace is None or (grad_loss is not None and dlogits is None)):
         return _on_stream(stream, distill, v, logits, top_ids, top_logprobs, tail, id_map, inv_temperature, grad_loss,
@@ -595,6 +609,7 @@ def distill(v: int, logits, top_ids, top_logprobs, tail: bool = False, id_map=No
         n_map = id_map.numel()
         if n_map == 0:
             raise ValueError("id_map must not be empty")
+    given = [t for t in (loss, dlogits) if t is not None]
     if loss is None:
         loss = torch.empty(n, dtype=f32, device=logits.device)
     to, out_ld = None, 0
@@ -614,6 +629,8 @@ def distill(v: int, logits, top_ids, top_logprobs, tail: bool = False, id_map=No
                           _array(grad_loss, f32, n, "grad_loss", dev), to, out_ld, ws, ws_bytes, _stream_handle(stream))
     if st:
         _check(st, "tt_distill")
+    if given:
+        _written(*given)
     return loss, dlogits
 
 
