@@ -469,12 +469,22 @@ def _launch_device(t, stream) -> int:
     return device
 
 
+def _kept_by_a_graph(t) -> bool:
+    """Whether memory allocated under a capture is of a pool of its own, as torch's graphs have it, which keep it as
+    long as they are there; a capture begun outside torch leaves it in the common pool."""
+    address = t.data_ptr()
+    return not any(s["address"] <= address < s["address"] + s["total_size"] and tuple(s["segment_pool_id"]) == (0, 0)
+                   for s in torch.cuda.memory_snapshot())
+
+
 def _needed_workspace(workspace, nbytes: int, device: int):
     """(address, bytes) of the caller's workspace, or of nbytes on the current stream (held by the third)."""
     if workspace is None:
         if nbytes == 0:
             return None, 0, None
         workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        if torch.cuda.is_current_stream_capturing() and not _kept_by_a_graph(workspace):
+            raise ValueError("a capture begun outside torch does not keep a workspace made here: give the call one")
     elif workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the logits' device")
     return workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), workspace
@@ -514,7 +524,8 @@ def logprobs(v: int, logits, ids=None, inv_temperature=None, n_top: int = 0, ent
     log probability of its token ids[i] (int32 [n], optional), its log-sum-exp, the statistics that
     logprobs_backward() takes, optionally its entropy, and its n_top (0..128) most probable tokens.
     inv_temperature: float32 [n], 1 / T (1 if not given).  out: a LogProbs of the caller's tensors (a None among
-    them is left out); workspace: from logprobs_workspace(); both are made here if not given.  Returns a LogProbs."""
+    them is left out); workspace: from logprobs_workspace(); both are made here if not given (a capture begun outside
+    torch has to be given a workspace where one is needed: it would not keep it).  Returns a LogProbs."""
     if stream is not None and (out is None or workspace is None):
         return _on_stream(stream, logprobs, v, logits, ids, inv_temperature, n_top, entropy, out, workspace, None)
     i32, f32 = torch.int32, torch.float32
@@ -593,7 +604,7 @@ def distill(v: int, logits, top_ids, top_logprobs, tail: bool = False, id_map=No
     is renormalised.  id_map: int32, the student's token of each of the teacher's (vocab_intersection()'s t2d), -1 for
     none.  With grad_loss (float32 [n], the weights of the rows' losses) the gradient with respect to the logits is
     formed as well, in dlogits: rows of the logits' type, made here if not given, which may be the logits themselves
-    (as in logprobs_backward()).
+    (as in logprobs_backward()).  workspace: from distill_workspace(), as in logprobs().
     Returns (loss, dlogits or None)."""
     if stream is not None and (loss is None or workspace is None or (grad_loss is not None and dlogits is None)):
         return _on_stream(stream, distill, v, logits, top_ids, top_logprobs, tail, id_map, inv_temperature, grad_loss,
