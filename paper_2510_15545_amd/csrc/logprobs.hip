@@ -14,7 +14,7 @@
 //
 // Alternatives, in the same pass: each thread keeps the place of its largest value as well.  k of the
 // workgroup's 64 or 256 groups of threads hold a largest value that reaches the k-th largest of the groups',
-// so every one of the k largest elements does.  That bound is formed after chunks 1, 2, 4, 8, ..., and elements
+// so every one of the k largest elements does (of the threads, where hardly more groups than k hold a token).  That bound is formed after chunks 1, 2, 4, 8, ..., and elements
 // that reach it are staged in LDS as 64-bit keys (value, then lower index), over a row of N chunks about
 // k (1 + log2 N) of them (of long rows their whole vectors, told apart at the end); then the keys are ordered by
 // counting.  A row's only workgroup finishes it; with several, each hands its sums and keys to row_finish.
@@ -124,6 +124,7 @@ struct Kth {
     uint32_t key;
     int n;
     bool tied;
+    int finite;  // of the wave's keys
 };
 
 template <int G>
@@ -142,10 +143,11 @@ __device__ __forceinline__ Kth kth_key(const uint32_t (&q)[G], int k) {
     }
     uint32_t lo = wave_min(least), hi = wave_max(most);
     const int enough = k + k / 4 + 2;
-    int n = reach(lo);
-    if (n < k) return {kLowestFinite, n, false};
+    const int finite = reach(lo);
+    int n = finite;
+    if (n < k) return {kLowestFinite, n, false, finite};
     const int m = reach(hi);
-    if (m >= k) return {hi, m, m > enough};
+    if (m >= k) return {hi, m, m > enough, finite};
     while (n > enough && hi - lo > 1) {  // n reach lo, fewer than k reach hi
         const uint32_t c = lo + (hi - lo) / 2;
         const int r = reach(c);
@@ -156,7 +158,7 @@ __device__ __forceinline__ Kth kth_key(const uint32_t (&q)[G], int k) {
             hi = c;
         }
     }
-    return {lo, n, n > enough};
+    return {lo, n, n > enough, finite};
 }
 
 // The same for the workgroup's keys, one a thread: by 64 groups of threads for small k (a group counts once), 256 else.
@@ -183,6 +185,25 @@ __device__ __forceinline__ Kth kth_of_threads(uint32_t key, int k, uint32_t *sh_
     return kth_key<kGroups / kWave>(q, k);
 }
 
+// The same by the threads themselves, a closer bound where few more groups than k hold a key or fewer: a mask has left a
+// run of tokens, or a part is short.  Fewer than k threads hold at most 8 k elements of a run.  (Short rows whose keys
+// fit anyway do without: 1,100 rows of 640 with 20 alternatives 8.8 us, 10.5 with it.)  sh_each: THREADS words.
+template <int THREADS>
+__device__ __forceinline__ Kth kth_of_each(uint32_t key, int k, uint32_t *sh_each) {
+    constexpr int kEach = THREADS / kWave;
+    __syncthreads();
+    sh_each[threadIdx.x] = key;
+    __syncthreads();
+    uint32_t q[kEach];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) q[u] = sh_each[u * kWave + threadIdx.x % kWave];
+    return kth_key<kEach>(q, k);
+}
+
+// Whether the groups are of more than one thread.
+template <int THREADS>
+__device__ __forceinline__ bool grouped(int k) { return THREADS > kGroups || k <= kFewTop; }
+
 // Sum over the workgroup of a count, through a zeroed LDS slot of its own.
 __device__ __forceinline__ int block_count(int n, int *slot) {
     n = (int)wave_sum((uint32_t)n);
@@ -203,8 +224,10 @@ __device__ __forceinline__ int count_if(const typename Elem<DT>::T *row, int x0,
     return n;
 }
 
-// The k largest of a part's elements exactly, where too many reach the bound (only rows made for it do that:
-// large values all in the same lanes): the k-th largest value by binary search on its order key, then
+// The k largest of a part's elements exactly, where too many reach the bound or more than the staging holds: rows that
+// rise along the vocabulary, large values all in the same lanes, over 32 alternatives of a run of 256 tokens or more in
+// rows of 16 to 32 KB.  It reads the part 57 times, element by element (20 alternatives of rising rows of 50,257: of one
+// 439 us, of 300 2,150; of one of 151,936 217; other rows 12.5, 19.8 and 12.7): the k-th largest value by binary search on its order key, then
 // the last index among the elements equal to it, each step a count over the part, read again.  At
 // least k elements are finite.
 template <int DT, int THREADS>
@@ -243,6 +266,7 @@ struct TopSet {
     static constexpr int kPer = Elem<DT>::kPer, kStage = TopLds<THREADS>::kStage;
     TopLds<THREADS> &sh;
     int k;
+    bool wide;  // more elements than there is room for whatever the bound
     Bound bound = {kLowestFinite, INT_MAX};
     float most = -INFINITY;     // the thread's largest value
     int where = 0;              // first index of its vector
@@ -254,7 +278,8 @@ struct TopSet {
     __device__ __forceinline__ void raise() {
         const uint32_t key = order_key(most);
         turn ^= 1;
-        const Kth q = kth_of_threads<THREADS>(key, k, sh.group[turn]);
+        Kth q = kth_of_threads<THREADS>(key, k, sh.group[turn]);
+        if (q.finite < 2 * k && wide && grouped<THREADS>(k)) q = kth_of_each<THREADS>(key, k, sh.largest);
         bound = {q.key, INT_MAX};
         if (q.tied) break_tie(key);
         current = true;
@@ -505,7 +530,7 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stre
     constexpr bool kLate = TOP && THREADS == kLongThreads;
     int count = 0;
     Sum mine = {-INFINITY, 0.0f, 0.0f};
-    TopSet<DT, NV, THREADS, VECTORS> top{sh, a.n_top};
+    TopSet<DT, NV, THREADS, VECTORS> top{sh, a.n_top, x1 - x0 > (!FINISH ? a.capacity : THREADS == kThreads ? kSelect : TopLds<THREADS>::kStage)};
     for_chunks<DT, NV, THREADS, true, false, true, TOP ? 1 : 2>(row, a.v, x0, x1, [&] { if (!kLate) x_id = token_logit(a, row_i, id); }, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         add_chunk<DT, NV, ENTROPY>(w, c2, mine, vm);
@@ -629,8 +654,8 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
         sh_e[wave] = e;
     }
     uint64_t from = 0;
+    uint32_t most = 0;  // of the thread's keys
     if constexpr (TOP) {
-        uint32_t most = 0;
         auto larger = [&](uint64_t key) {
             const uint32_t o = (uint32_t)(key >> 32);
             most = o > most ? o : most;
@@ -650,7 +675,7 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
     const RowStats stats = row_stats(beta, m, s);
     if (threadIdx.x == kThreads - 1) write_row(a, row, stats, s, e, id, x_id);
     if constexpr (TOP) {
-        for (;;) {
+        for (bool closer = grouped<kThreads>(a.n_top);; closer = false) {
             auto put = [&](uint64_t key) {
                 const uint64_t hit = __ballot(key >= from);
                 if (hit == 0) return;
@@ -667,18 +692,21 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
             }
             __syncthreads();
             if (sh_total <= kSelect) break;
-            // many equal values: the k-th largest key itself (keys are distinct, so k reach it), by binary search
-            uint64_t kth = 0;
-            for (int b = 63; b >= 0; --b) {
-                const uint64_t c = kth | (1ull << b);
-                int n = 0;
-                for_each_key(a, sums, keys, [&](uint64_t key) { n += key >= c ? 1 : 0; });
-                __syncthreads();
-                if (threadIdx.x == 0) sh_slots[0] = 0;
-                __syncthreads();
-                if (block_count(n, sh_slots) >= a.n_top) kth = c;
+            if (closer) {  // hardly more groups than k hold a key (a wave's lanes past the parts' keys have none)
+                from = (uint64_t)kth_of_each<kThreads>(most, a.n_top, sh_group).key << 32;
+            } else {  // many equal values: the k-th largest key itself (keys are distinct, so k reach it), by binary search
+                uint64_t kth = 0;
+                for (int b = 63; b >= 0; --b) {
+                    const uint64_t c = kth | (1ull << b);
+                    int n = 0;
+                    for_each_key(a, sums, keys, [&](uint64_t key) { n += key >= c ? 1 : 0; });
+                    __syncthreads();
+                    if (threadIdx.x == 0) sh_slots[0] = 0;
+                    __syncthreads();
+                    if (block_count(n, sh_slots) >= a.n_top) kth = c;
+                }
+                from = kth;
             }
-            from = kth;
             __syncthreads();
             if (threadIdx.x == 0) sh_total = 0;
             __syncthreads();

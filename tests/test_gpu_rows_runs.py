@@ -1,0 +1,77 @@
+"""Alternatives of rows that a mask holds to a run of tokens, and of rows whose last part is short: right, and about as
+fast as those of other rows."""
+import numpy as np
+import pytest
+import torch
+
+import util_rows as ur
+from test_gpu_logprobs import check_logprobs
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_top", [8, 20, 32, 33, 128])
+@pytest.mark.parametrize("n,v", [(2, 600), (2, 12000), (2, 50257), (2, 151936), (260, 20000)])
+def test_runs_of_every_length(n, v, n_top, dtype):
+    """Runs of 1 to 3,000 tokens anywhere, of different, equal and few different logits."""
+    print(f"[case] {n}x{v} {dtype} top {n_top}", flush=True)
+    rng = np.random.default_rng([n, v, n_top])
+    rows = []
+    for i, m in enumerate((1, 7, 19, 20, 64, 127, 150, 256, 300, 500, 1000, 1017, 3000)):
+        for kind in range(3):
+            m = min(m, v)
+            x = np.full(v, -np.inf if (i + kind) % 2 else np.nan, np.float32)
+            at = int(rng.integers(0, v - m + 1))
+            x[at:at + m] = (rng.standard_normal(m) * 3, 1.5, rng.integers(0, 3, m))[kind]
+            rows.append(x)
+    x = np.array(rows)
+    x = np.tile(x, (-(-n // len(x)), 1))
+    check_logprobs(x, ur.placed(x, dtype, pad=1), rng.integers(0, v, len(x)), None, n_top)
+
+
+def gpu_time(rows, n_top, reps=10):
+    """us of the GPU for a call, the least of five replays of a graph of several."""
+    import paper_2510_15545_amd as tt
+
+    call = lambda: tt.logprobs(rows.shape[1], rows, n_top=n_top)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(reps):
+            call()
+    best = float("inf")
+    for _ in range(6):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        graph.replay()
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b) * 1e3 / reps)
+    return best
+
+
+@pytest.mark.parametrize("n,v,n_top,m", [(1, 151936, 20, 256), (1, 151936, 32, 500), (48, 128256, 20, 300), (1, 50257, 20, 500), (64, 50257, 32, 1000)])
+def test_a_run_takes_no_longer(n, v, n_top, m):
+    """Every element read again 57 times, one by one, would take 15 to 30 times as long."""
+    x = torch.randn((n, v), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).mul_(3).bfloat16()
+    ordinary = gpu_time(x, n_top)
+    x[:, :v // 3] = -float("inf")
+    x[:, v // 3 + m:] = -float("inf")
+    run = gpu_time(x, n_top)
+    print(f"[time] {n}x{v} top {n_top}: {ordinary:.1f} us, a run of {m}: {run:.1f}", flush=True)
+    assert run <= 4 * ordinary
+
+
+@pytest.mark.parametrize("n", [1, 48])
+def test_parts_with_few_or_many_keys_take_no_longer(n):
+    """A short last part, and as many alternatives as take the joining kernel to the keys it can hold."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = {v: torch.randn((n, v), device="cuda", generator=gen).mul_(3).bfloat16() for v in (151936, 147856, 147556)}
+    ordinary = gpu_time(x[151936], 20)
+    for n_top in (20, 28, 31, 32, 33):
+        for v, rows in x.items():
+            us = gpu_time(rows, n_top)
+            print(f"[time] {n}x{v} top {n_top}: {us:.1f} us", flush=True)
+            assert us <= 2 * ordinary
