@@ -14,7 +14,7 @@
 //
 // Alternatives, in the same pass: each thread keeps the place of its largest value as well.  k of the
 // workgroup's 64 or 256 groups of threads hold a largest value that reaches the k-th largest of the groups',
-// so every one of the k largest elements does (of the threads, where hardly more groups than k hold a token).  That bound is formed after chunks 1, 2, 4, 8, ..., and elements
+// so every one of the k largest elements does.  That bound is formed after chunks 1, 2, 4, 8, ..., and elements
 // that reach it are staged in LDS as 64-bit keys (value, then lower index), over a row of N chunks about
 // k (1 + log2 N) of them (of long rows their whole vectors, told apart at the end); then the keys are ordered by
 // counting.  A row's only workgroup finishes it; with several, each hands its sums and keys to row_finish.
@@ -118,17 +118,16 @@ __device__ __forceinline__ uint32_t group_max(uint32_t x) {
     return x;
 }
 
-// A key that at least k of the wave's keys reach, G a lane, and how many do: not many more than k, unless that many
+// A key that at least k of the wave's keys reach, G a lane, and how many do: not more than `enough`, unless that many
 // are equal to it (then it is the k-th largest itself).  kLowestFinite where fewer than k are finite.
 struct Kth {
     uint32_t key;
     int n;
     bool tied;
-    int finite;  // of the wave's keys
 };
 
 template <int G>
-__device__ __forceinline__ Kth kth_key(const uint32_t (&q)[G], int k) {
+__device__ __forceinline__ Kth kth_key(const uint32_t (&q)[G], int k, int enough) {
     auto reach = [&](uint32_t c) {
         int n = 0;
 #pragma unroll
@@ -142,12 +141,10 @@ __device__ __forceinline__ Kth kth_key(const uint32_t (&q)[G], int k) {
         least = q[u] >= kLowestFinite && q[u] < least ? q[u] : least;
     }
     uint32_t lo = wave_min(least), hi = wave_max(most);
-    const int enough = k + k / 4 + 2;
-    const int finite = reach(lo);
-    int n = finite;
-    if (n < k) return {kLowestFinite, n, false, finite};
+    int n = reach(lo);
+    if (n < k) return {kLowestFinite, n, false};
     const int m = reach(hi);
-    if (m >= k) return {hi, m, m > enough, finite};
+    if (m >= k) return {hi, m, m > enough};
     while (n > enough && hi - lo > 1) {  // n reach lo, fewer than k reach hi
         const uint32_t c = lo + (hi - lo) / 2;
         const int r = reach(c);
@@ -158,7 +155,7 @@ __device__ __forceinline__ Kth kth_key(const uint32_t (&q)[G], int k) {
             hi = c;
         }
     }
-    return {lo, n, n > enough, finite};
+    return {lo, n, n > enough};
 }
 
 // The same for the workgroup's keys, one a thread: by 64 groups of threads for small k (a group counts once), 256 else.
@@ -168,13 +165,13 @@ constexpr int kFewTop = 32;
 template <int THREADS>
 __device__ __forceinline__ Kth kth_of_threads(uint32_t key, int k, uint32_t *sh_group) {
     constexpr int kFew = THREADS / kWave, kMany = THREADS / kGroups;  // threads of a group
-    const int lane = threadIdx.x % kWave;
+    const int lane = threadIdx.x % kWave, enough = k + k / 4 + 2;
     if (k <= kFewTop) {
         key = group_max<kFew>(key);
         if (lane % kFew == 0) sh_group[threadIdx.x / kFew] = key;
         __syncthreads();
         const uint32_t q[1] = {sh_group[lane]};
-        return kth_key<1>(q, k);
+        return kth_key<1>(q, k, enough);
     }
     key = group_max<kMany>(key);
     if (lane % kMany == 0) sh_group[threadIdx.x / kMany] = key;
@@ -182,12 +179,11 @@ __device__ __forceinline__ Kth kth_of_threads(uint32_t key, int k, uint32_t *sh_
     uint32_t q[kGroups / kWave];
 #pragma unroll
     for (int u = 0; u < kGroups / kWave; ++u) q[u] = sh_group[u * kWave + lane];
-    return kth_key<kGroups / kWave>(q, k);
+    return kth_key<kGroups / kWave>(q, k, enough);
 }
 
-// The same by the threads themselves, a closer bound where few more groups than k hold a key or fewer: a mask has left a
-// run of tokens, or a part is short.  Fewer than k threads hold at most 8 k elements of a run.  (Short rows whose keys
-// fit anyway do without: 1,100 rows of 640 with 20 alternatives 8.8 us, 10.5 with it.)  sh_each: THREADS words.
+// The same by the threads themselves and exactly: a closer bound, of which a run of tokens that rise has 8 k elements.
+// (Not for every row: 1,100 rows of 640 with 20 alternatives take 8.8 us, 10.5 with it.)  sh_each: THREADS words.
 template <int THREADS>
 __device__ __forceinline__ Kth kth_of_each(uint32_t key, int k, uint32_t *sh_each) {
     constexpr int kEach = THREADS / kWave;
@@ -197,12 +193,8 @@ __device__ __forceinline__ Kth kth_of_each(uint32_t key, int k, uint32_t *sh_eac
     uint32_t q[kEach];
 #pragma unroll
     for (int u = 0; u < kEach; ++u) q[u] = sh_each[u * kWave + threadIdx.x % kWave];
-    return kth_key<kEach>(q, k);
+    return kth_key<kEach>(q, k, k);
 }
-
-// Whether the groups are of more than one thread.
-template <int THREADS>
-__device__ __forceinline__ bool grouped(int k) { return THREADS > kGroups || k <= kFewTop; }
 
 // Sum over the workgroup of a count, through a zeroed LDS slot of its own.
 __device__ __forceinline__ int block_count(int n, int *slot) {
@@ -224,10 +216,9 @@ __device__ __forceinline__ int count_if(const typename Elem<DT>::T *row, int x0,
     return n;
 }
 
-// The k largest of a part's elements exactly, where too many reach the bound or more than the staging holds: rows that
-// rise along the vocabulary, large values all in the same lanes, over 32 alternatives of a run of 256 tokens or more in
-// rows of 16 to 32 KB.  It reads the part 57 times, element by element (20 alternatives of rising rows of 50,257: of one
-// 439 us, of 300 2,150; of one of 151,936 217; other rows 12.5, 19.8 and 12.7): the k-th largest value by binary search on its order key, then
+// The k largest of a part's elements exactly, where too many reach the closest bound, too (only rows made for it do
+// that: large values all in the same lanes).  It reads the part 57 times, element by element (of one row of 50,257 400
+// us): the k-th largest value by binary search on its order key, then
 // the last index among the elements equal to it, each step a count over the part, read again.  At
 // least k elements are finite.
 template <int DT, int THREADS>
@@ -258,6 +249,10 @@ __device__ __noinline__ void select_exactly(const typename Elem<DT>::T *row, int
     __syncthreads();
 }
 
+template <int DT, int THREADS>
+__device__ __noinline__ int select_again(const typename Elem<DT>::T *row, int v, int x0, int x1, int k, float most, int where,
+                                         TopLds<THREADS> *sh, uint64_t *dst, int capacity);
+
 // The elements of a row that may be among its k largest, chunk by chunk.  VECTORS: whole vectors are staged, with
 // their largest value, and those that reach the last bound are read again for their elements: fewer instructions in
 // a long row's stream, but another round trip at its end.
@@ -266,7 +261,6 @@ struct TopSet {
     static constexpr int kPer = Elem<DT>::kPer, kStage = TopLds<THREADS>::kStage;
     TopLds<THREADS> &sh;
     int k;
-    bool wide;  // more elements than there is room for whatever the bound
     Bound bound = {kLowestFinite, INT_MAX};
     float most = -INFINITY;     // the thread's largest value
     int where = 0;              // first index of its vector
@@ -278,11 +272,13 @@ struct TopSet {
     __device__ __forceinline__ void raise() {
         const uint32_t key = order_key(most);
         turn ^= 1;
-        Kth q = kth_of_threads<THREADS>(key, k, sh.group[turn]);
-        if (q.finite < 2 * k && wide && grouped<THREADS>(k)) q = kth_of_each<THREADS>(key, k, sh.largest);
+        set(kth_of_threads<THREADS>(key, k, sh.group[turn]), key);
+        current = true;
+    }
+
+    __device__ __forceinline__ void set(const Kth &q, uint32_t key) {
         bound = {q.key, INT_MAX};
         if (q.tied) break_tie(key);
-        current = true;
     }
 
     // Many groups are equal to the bound (a row of capped or of few different logits): of the elements equal to it,
@@ -378,7 +374,7 @@ struct TopSet {
 
     // The keys that reach the bound of the whole part, to dst (LDS or global, `capacity` >= k of them); returns their
     // number: at least k, or all of the part's finite elements.
-    __device__ __forceinline__ int finish(const typename Elem<DT>::T *row, int x0, int x1, uint64_t *dst, int capacity) {
+    __device__ __forceinline__ int finish(const typename Elem<DT>::T *row, int v, int x0, int x1, uint64_t *dst, int capacity) {
         const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
         if (!current) raise();
         const uint64_t from = bound.full();
@@ -398,11 +394,7 @@ struct TopSet {
         base = __builtin_amdgcn_readfirstlane(base);
         __syncthreads();
         const int total = sh.total;
-        if (total > capacity) {
-            __syncthreads();
-            select_exactly<DT, THREADS>(row, x0 > 0 ? x0 : 0, x1, k, dst, sh.slots, &sh.total);
-            return k;
-        }
+        if (total > capacity) return select_again<DT, THREADS>(row, v, x0, x1, k, most, where, &sh, dst, capacity);
         if constexpr (VECTORS) return total;
         for (int i = lane; i - lane < staged; i += kWave) {
             const uint64_t key = i < staged ? sh.stage[wave][i] : 0;
@@ -414,6 +406,51 @@ struct TopSet {
         return total;
     }
 };
+
+// A part's keys, of which more were staged than there is room for: by bounds that came too late (what precedes the likely
+// tokens is masked or low, or the row rises) or were too low (a mask has left a run of tokens, or the part is short, and
+// hardly more groups of threads than k hold one).  The part is read again by the threads' own bound, from their largest
+// values and these ones' vectors.  20 alternatives of one row of 50,257 held to 500 tokens: 23 us, other rows 12.6; 64 of
+// 1,024 rows of 262,144 whose first half is masked: 245 and 108.  The keys' number: at least k.
+template <int DT, int THREADS>
+__device__ __noinline__ int select_again(const typename Elem<DT>::T *row, int v, int x0, int x1, int k, float most, int where,
+                                         TopLds<THREADS> *sh, uint64_t *dst, int capacity) {
+    constexpr int kPer = Elem<DT>::kPer, NV = 2;
+    const int lane = threadIdx.x % kWave;
+    TopSet<DT, NV, THREADS, false> top{*sh, k};
+    top.most = most;
+    top.where = where;
+    const uint32_t key = order_key(most);
+    top.set(kth_of_each<THREADS>(key, k, sh->largest), key);
+    const Bound bound = top.bound;
+    const float lowest = bound.lowest();
+    __syncthreads();
+    if (threadIdx.x == 0) sh->total = 0;
+    __syncthreads();
+    for_chunks<DT, NV, THREADS, true, false, true, 1>(row, v, x0, x1, [] {}, [&](uint32_t(&w)[NV][4], int x_chunk) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const float x = value<DT>(w[i], j);
+                const int at = vector_at<DT, THREADS>(x_chunk, i) + j;
+                const bool in = at < x1 && (x > lowest || (x == lowest && at <= bound.index));
+                const uint64_t hit = __ballot(in);
+                if (hit == 0) continue;
+                int base = 0;
+                if (lane == 0) base = atomicAdd(&sh->total, __popcll(hit));
+                base = __builtin_amdgcn_readfirstlane(base) + lanes_below(hit);
+                if (in && base < capacity) dst[base] = full_key(order_key(x), at);
+            }
+        }
+    });
+    __syncthreads();
+    const int n = sh->total;
+    __syncthreads();
+    if (n <= capacity) return n;
+    select_exactly<DT, THREADS>(row, x0 > 0 ? x0 : 0, x1, k, dst, sh->slots, &sh->total);
+    return k;
+}
 
 // The largest k (all, if fewer) of c <= kSelect distinct keys in LDS, descending, in sh_out; returns their number.
 template <int THREADS>
@@ -530,7 +567,7 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stre
     constexpr bool kLate = TOP && THREADS == kLongThreads;
     int count = 0;
     Sum mine = {-INFINITY, 0.0f, 0.0f};
-    TopSet<DT, NV, THREADS, VECTORS> top{sh, a.n_top, x1 - x0 > (!FINISH ? a.capacity : THREADS == kThreads ? kSelect : TopLds<THREADS>::kStage)};
+    TopSet<DT, NV, THREADS, VECTORS> top{sh, a.n_top};
     for_chunks<DT, NV, THREADS, true, false, true, TOP ? 1 : 2>(row, a.v, x0, x1, [&] { if (!kLate) x_id = token_logit(a, row_i, id); }, [&](uint32_t(&w)[NV][4], int x) {
         float vm[NV];
         add_chunk<DT, NV, ENTROPY>(w, c2, mine, vm);
@@ -540,7 +577,7 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 1 : 8) void row_stre
     mine = wave_join<ENTROPY>(mine, c2);
     if (lane == 0) sh_sum[wave] = mine;
     if constexpr (TOP)
-        count = top.finish(row, x0, x1, FINISH ? sh_sel : a.keys + ((size_t)r * a.parts + part) * a.capacity, FINISH ? kSelect : a.capacity);
+        count = top.finish(row, a.v, x0, x1, FINISH ? sh_sel : a.keys + ((size_t)r * a.parts + part) * a.capacity, FINISH ? kSelect : a.capacity);
     __syncthreads();
     if constexpr (!FINISH) {
         if (threadIdx.x == 0) {
@@ -675,7 +712,7 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
     const RowStats stats = row_stats(beta, m, s);
     if (threadIdx.x == kThreads - 1) write_row(a, row, stats, s, e, id, x_id);
     if constexpr (TOP) {
-        for (bool closer = grouped<kThreads>(a.n_top);; closer = false) {
+        for (bool closer = a.n_top <= kFewTop;; closer = false) {
             auto put = [&](uint64_t key) {
                 const uint64_t hit = __ballot(key >= from);
                 if (hit == 0) return;

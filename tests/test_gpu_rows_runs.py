@@ -75,3 +75,53 @@ def test_parts_with_few_or_many_keys_take_no_longer(n):
             us = gpu_time(rows, n_top)
             print(f"[time] {n}x{v} top {n_top}: {us:.1f} us", flush=True)
             assert us <= 2 * ordinary
+
+
+def spoilt(rng, v):
+    """Rows whose likely tokens come late: their first part masked, low or rising, by minus infinity, NaN or -30."""
+    rows = []
+    for share in (0.1, 0.35, 0.51, 0.7, 0.95):
+        for low in (-np.inf, np.nan, -30.0):
+            x = (rng.standard_normal(v) * 3).astype(np.float32)
+            x[:int(v * share)] = low
+            rows.append(x)
+    at = np.arange(v, dtype=np.float32)
+    rows += [at / v * 20, -at / v * 20, at / v * 20 + rng.standard_normal(v).astype(np.float32), np.where(at > v // 2, 5.0, at / v).astype(np.float32)]
+    return np.array(rows, np.float32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_top", [1, 20, 32, 33, 128])
+@pytest.mark.parametrize("n,v", [(1, 9001), (1, 20011), (1, 50257), (260, 30011), (1, 200003), (500, 50257)])
+def test_likely_tokens_late_in_the_row(n, v, n_top, dtype):
+    print(f"[case] {n}x{v} {dtype} top {n_top}", flush=True)
+    rng = np.random.default_rng([n, v, n_top])
+    x = spoilt(rng, v)
+    rows = ur.placed(x, dtype, pad=1).repeat(-(-n // len(x)), 1)[:, :v]
+    got = tt_logprobs(rows, n_top)
+    for a in range(0, len(rows), len(x)):  # every copy of them has the first one's (sums' last digits go by alignment)
+        assert torch.equal(got.top_ids[a:a + len(x)], got.top_ids[:len(x)])
+    check_logprobs(x, rows[:len(x)], rng.integers(0, v, len(x)), None, n_top)
+    want = ur.logprobs(ur.host(rows[:len(x)]), None, None, n_top)
+    assert np.array_equal(got.top_ids[:len(x)].cpu().numpy(), want["top_ids"])
+
+
+def tt_logprobs(rows, n_top):
+    import paper_2510_15545_amd as tt
+
+    return tt.logprobs(rows.shape[1], rows, n_top=n_top)
+
+
+@pytest.mark.parametrize("n,v,n_top", [(1, 65536, 20), (64, 50257, 32), (300, 128256, 20), (512, 262144, 64), (40, 1000000, 20)])
+def test_likely_tokens_late_in_the_row_take_no_longer(n, v, n_top):
+    """A row's second reading at most, not 57 of them."""
+    x = torch.randn((n, v), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).mul_(3).bfloat16()
+    ordinary = gpu_time(x, n_top)
+    for share in (0.2, 0.51, 0.7):
+        x[:, :int(v * share)] = -float("inf")
+        late = gpu_time(x, n_top, 3)
+        print(f"[time] {n}x{v} top {n_top}: {ordinary:.1f} us, the first {share} masked: {late:.1f}", flush=True)
+        assert late <= 6 * ordinary
+    rising = gpu_time((torch.arange(v, device="cuda") / v * 20).bfloat16().expand(n, v).contiguous(), n_top, 3)
+    print(f"[time] {n}x{v} top {n_top}: {ordinary:.1f} us, rising: {rising:.1f}", flush=True)
+    assert rising <= 6 * ordinary
