@@ -182,10 +182,10 @@ __device__ __forceinline__ Kth kth_of_threads(uint32_t key, int k, uint32_t *sh_
     return kth_key<kGroups / kWave>(q, k, enough);
 }
 
-// The same by the threads themselves and exactly: a closer bound, of which a run of tokens that rise has 8 k elements.
-// (Not for every row: 1,100 rows of 640 with 20 alternatives take 8.8 us, 10.5 with it.)  sh_each: THREADS words.
+// The same by the threads themselves: a closer bound.  (Not for every row: 1,100 rows of 640 with 20 alternatives take
+// 8.8 us, 10.5 with it.)  sh_each: THREADS words.
 template <int THREADS>
-__device__ __forceinline__ Kth kth_of_each(uint32_t key, int k, uint32_t *sh_each) {
+__device__ __forceinline__ Kth kth_of_each(uint32_t key, int k, int enough, uint32_t *sh_each) {
     constexpr int kEach = THREADS / kWave;
     __syncthreads();
     sh_each[threadIdx.x] = key;
@@ -193,7 +193,7 @@ __device__ __forceinline__ Kth kth_of_each(uint32_t key, int k, uint32_t *sh_eac
     uint32_t q[kEach];
 #pragma unroll
     for (int u = 0; u < kEach; ++u) q[u] = sh_each[u * kWave + threadIdx.x % kWave];
-    return kth_key<kEach>(q, k, k);
+    return kth_key<kEach>(q, k, enough);
 }
 
 // Sum over the workgroup of a count, through a zeroed LDS slot of its own.
@@ -217,10 +217,9 @@ __device__ __forceinline__ int count_if(const typename Elem<DT>::T *row, int x0,
 }
 
 // The k largest of a part's elements exactly, where too many reach the closest bound, too (only rows made for it do
-// that: large values all in the same lanes).  It reads the part 57 times, element by element (of one row of 50,257 400
-// us): the k-th largest value by binary search on its order key, then
-// the last index among the elements equal to it, each step a count over the part, read again.  At
-// least k elements are finite.
+// that: large values all in the same lanes): the k-th largest value by binary search on its order key, then the last
+// index among the elements equal to it, each step a count over the part, read again element by element (57 of them: 400
+// us for a row of 50,257).  At least k elements are finite.
 template <int DT, int THREADS>
 __device__ __noinline__ void select_exactly(const typename Elem<DT>::T *row, int x0, int x1, int k, uint64_t *keys, int *sh_slots,
                                             int *sh_total) {
@@ -249,9 +248,74 @@ __device__ __noinline__ void select_exactly(const typename Elem<DT>::T *row, int
     __syncthreads();
 }
 
+// The keys of a part that reach a bound, to dst (as many as fit), the part read again; returns their number.
 template <int DT, int THREADS>
-__device__ __noinline__ int select_again(const typename Elem<DT>::T *row, int v, int x0, int x1, int k, float most, int where,
-                                         TopLds<THREADS> *sh, uint64_t *dst, int capacity);
+__device__ __noinline__ int read_again(const typename Elem<DT>::T *row, int v, int x0, int x1, Bound bound, uint64_t *dst, int capacity,
+                                       int *sh_total) {
+    constexpr int kPer = Elem<DT>::kPer, NV = 2;
+    const int lane = threadIdx.x % kWave;
+    const float lowest = bound.lowest();
+    __syncthreads();
+    if (threadIdx.x == 0) *sh_total = 0;
+    __syncthreads();
+    for_chunks<DT, NV, THREADS, true, false, true, 1>(row, v, x0, x1, [] {}, [&](uint32_t(&w)[NV][4], int x_chunk) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const float x = value<DT>(w[i], j);
+                const int at = vector_at<DT, THREADS>(x_chunk, i) + j;
+                const bool in = at < x1 && (x > lowest || (x == lowest && at <= bound.index));
+                const uint64_t hit = __ballot(in);
+                if (hit == 0) continue;
+                int base = 0;
+                if (lane == 0) base = atomicAdd(sh_total, __popcll(hit));
+                base = __builtin_amdgcn_readfirstlane(base) + lanes_below(hit);
+                if (in && base < capacity) dst[base] = full_key(order_key(x), at);
+            }
+        }
+    });
+    __syncthreads();
+    const int n = *sh_total;
+    __syncthreads();
+    return n;
+}
+
+// Many keys are equal to a bound (a row of capped or of few different logits): of the elements equal to it, those up to
+// an index that enough threads' elements do not pass.  largest, last: of each thread, in LDS.
+template <int THREADS>
+__device__ __forceinline__ void break_tie(Bound &bound, int k, uint32_t key, int last, TopLds<THREADS> &sh) {
+    const int lane = threadIdx.x % kWave;
+    __syncthreads();
+    sh.largest[threadIdx.x] = key;
+    sh.where[threadIdx.x] = last;
+    __syncthreads();
+    auto count = [&](auto f) {
+        int n = 0;
+        for (int u = 0; u < THREADS / kWave; ++u) n += __popcll(__ballot(f(sh.largest[u * kWave + lane], sh.where[u * kWave + lane])));
+        return n;
+    };
+    const uint32_t kth = bound.key;
+    const int need = k - count([=](uint32_t o, int) { return o > kth; });
+    if (need <= 0) {
+        ++bound.key;  // enough lie above it
+        return;
+    }
+    bound.index = 0;  // the largest index with fewer than `need` equal ones below it
+    for (int b = 23; b >= 0; --b) {
+        const int c = bound.index | (1 << b);
+        if (count([=](uint32_t o, int at) { return o == kth && at < c; }) < need) bound.index = c;
+    }
+}
+
+// The bound from the threads' own largest values.
+template <int THREADS>
+__device__ __forceinline__ Bound closer_bound(uint32_t key, int last, int k, int enough, TopLds<THREADS> *sh) {
+    const Kth q = kth_of_each<THREADS>(key, k, enough, sh->largest);
+    Bound bound = {q.key, INT_MAX};
+    if (q.tied) break_tie<THREADS>(bound, k, key, last, *sh);
+    return bound;
+}
 
 // The elements of a row that may be among its k largest, chunk by chunk.  VECTORS: whole vectors are staged, with
 // their largest value, and those that reach the last bound are read again for their elements: fewer instructions in
@@ -272,39 +336,10 @@ struct TopSet {
     __device__ __forceinline__ void raise() {
         const uint32_t key = order_key(most);
         turn ^= 1;
-        set(kth_of_threads<THREADS>(key, k, sh.group[turn]), key);
-        current = true;
-    }
-
-    __device__ __forceinline__ void set(const Kth &q, uint32_t key) {
+        const Kth q = kth_of_threads<THREADS>(key, k, sh.group[turn]);
         bound = {q.key, INT_MAX};
-        if (q.tied) break_tie(key);
-    }
-
-    // Many groups are equal to the bound (a row of capped or of few different logits): of the elements equal to it,
-    // those up to an index that enough threads' elements do not pass.
-    __device__ __forceinline__ void break_tie(uint32_t key) {
-        const int lane = threadIdx.x % kWave;
-        __syncthreads();
-        sh.largest[threadIdx.x] = key;
-        sh.where[threadIdx.x] = where + kPer - 1;
-        __syncthreads();
-        auto count = [&](auto f) {
-            int n = 0;
-            for (int u = 0; u < THREADS / kWave; ++u) n += __popcll(__ballot(f(sh.largest[u * kWave + lane], sh.where[u * kWave + lane])));
-            return n;
-        };
-        const uint32_t kth = bound.key;
-        const int need = k - count([=](uint32_t o, int) { return o > kth; });
-        if (need <= 0) {
-            ++bound.key;  // enough lie above it
-            return;
-        }
-        bound.index = 0;  // the largest index with fewer than `need` equal ones below it
-        for (int b = 23; b >= 0; --b) {
-            const int c = bound.index | (1 << b);
-            if (count([=](uint32_t o, int at) { return o == kth && at < c; }) < need) bound.index = c;
-        }
+        if (q.tied) break_tie<THREADS>(bound, k, key, where + kPer - 1, sh);
+        current = true;
     }
 
     __device__ __forceinline__ void add(const uint32_t (&w)[NV][4], const float (&vm)[NV], int x_chunk) {
@@ -372,11 +407,10 @@ struct TopSet {
         }
     }
 
-    // The keys that reach the bound of the whole part, to dst (LDS or global, `capacity` >= k of them); returns their
-    // number: at least k, or all of the part's finite elements.
-    __device__ __forceinline__ int finish(const typename Elem<DT>::T *row, int v, int x0, int x1, uint64_t *dst, int capacity) {
+    // The staged keys that reach the bound, to dst (as many as `capacity`, or none); returns their number, or more than
+    // `capacity` where a wave's did not fit.
+    __device__ __forceinline__ int gather(const typename Elem<DT>::T *row, int x1, uint64_t *dst, int capacity) {
         const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-        if (!current) raise();
         const uint64_t from = bound.full();
         if (threadIdx.x == 0) sh.total = 0;
         __syncthreads();
@@ -394,8 +428,7 @@ struct TopSet {
         base = __builtin_amdgcn_readfirstlane(base);
         __syncthreads();
         const int total = sh.total;
-        if (total > capacity) return select_again<DT, THREADS>(row, v, x0, x1, k, most, where, &sh, dst, capacity);
-        if constexpr (VECTORS) return total;
+        if (VECTORS || total > capacity) return total;
         for (int i = lane; i - lane < staged; i += kWave) {
             const uint64_t key = i < staged ? sh.stage[wave][i] : 0;
             const bool in = i < staged && key >= from;
@@ -405,52 +438,29 @@ struct TopSet {
         }
         return total;
     }
-};
 
-// A part's keys, of which more were staged than there is room for: by bounds that came too late (what precedes the likely
-// tokens is masked or low, or the row rises) or were too low (a mask has left a run of tokens, or the part is short, and
-// hardly more groups of threads than k hold one).  The part is read again by the threads' own bound, from their largest
-// values and these ones' vectors.  20 alternatives of one row of 50,257 held to 500 tokens: 23 us, other rows 12.6; 64 of
-// 1,024 rows of 262,144 whose first half is masked: 245 and 108.  The keys' number: at least k.
-template <int DT, int THREADS>
-__device__ __noinline__ int select_again(const typename Elem<DT>::T *row, int v, int x0, int x1, int k, float most, int where,
-                                         TopLds<THREADS> *sh, uint64_t *dst, int capacity) {
-    constexpr int kPer = Elem<DT>::kPer, NV = 2;
-    const int lane = threadIdx.x % kWave;
-    TopSet<DT, NV, THREADS, false> top{*sh, k};
-    top.most = most;
-    top.where = where;
-    const uint32_t key = order_key(most);
-    top.set(kth_of_each<THREADS>(key, k, sh->largest), key);
-    const Bound bound = top.bound;
-    const float lowest = bound.lowest();
-    __syncthreads();
-    if (threadIdx.x == 0) sh->total = 0;
-    __syncthreads();
-    for_chunks<DT, NV, THREADS, true, false, true, 1>(row, v, x0, x1, [] {}, [&](uint32_t(&w)[NV][4], int x_chunk) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                const float x = value<DT>(w[i], j);
-                const int at = vector_at<DT, THREADS>(x_chunk, i) + j;
-                const bool in = at < x1 && (x > lowest || (x == lowest && at <= bound.index));
-                const uint64_t hit = __ballot(in);
-                if (hit == 0) continue;
-                int base = 0;
-                if (lane == 0) base = atomicAdd(&sh->total, __popcll(hit));
-                base = __builtin_amdgcn_readfirstlane(base) + lanes_below(hit);
-                if (in && base < capacity) dst[base] = full_key(order_key(x), at);
-            }
+    // The keys that reach the bound of the whole part, to dst (LDS or global, `capacity` >= k of them); returns their
+    // number: at least k, or all of the part's finite elements.  Where more were staged than there is room for, the
+    // running bounds were too low (a mask has left a run of tokens, or the part is short, and hardly more groups of
+    // threads than k hold one) or came too late (what precedes the likely tokens is masked or low, or the row rises): the
+    // part is read again by the threads' own bound (20 alternatives of one row of 50,257 held to 500 tokens: 22 us, other
+    // rows 12.6; 64 of 1,024 rows of 262,144 whose first half is masked: 245 and 108).
+    __device__ __forceinline__ int finish(const typename Elem<DT>::T *row, int v, int x0, int x1, uint64_t *dst, int capacity) {
+        if (!current) raise();
+        const uint32_t key = order_key(most);
+        const int last = where + kPer - 1;
+        const int total = gather(row, x1, dst, capacity);
+        if (total <= capacity) return total;
+        for (int enough = k + k / 4 + 2;; enough = k) {  // the second time exactly: of tokens that rise 8 k reach it
+            bound = closer_bound<THREADS>(key, last, k, enough, &sh);
+            const int n = read_again<DT, THREADS>(row, v, x0, x1, bound, dst, capacity, &sh.total);
+            if (n <= capacity) return n;
+            if (enough == k) break;
         }
-    });
-    __syncthreads();
-    const int n = sh->total;
-    __syncthreads();
-    if (n <= capacity) return n;
-    select_exactly<DT, THREADS>(row, x0 > 0 ? x0 : 0, x1, k, dst, sh->slots, &sh->total);
-    return k;
-}
+        select_exactly<DT, THREADS>(row, x0 > 0 ? x0 : 0, x1, k, dst, sh.slots, &sh.total);
+        return k;
+    }
+};
 
 // The largest k (all, if fewer) of c <= kSelect distinct keys in LDS, descending, in sh_out; returns their number.
 template <int THREADS>
@@ -712,7 +722,7 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
     const RowStats stats = row_stats(beta, m, s);
     if (threadIdx.x == kThreads - 1) write_row(a, row, stats, s, e, id, x_id);
     if constexpr (TOP) {
-        for (bool closer = a.n_top <= kFewTop;; closer = false) {
+        for (bool closer = true;; closer = false) {
             auto put = [&](uint64_t key) {
                 const uint64_t hit = __ballot(key >= from);
                 if (hit == 0) return;
@@ -729,9 +739,34 @@ __global__ __launch_bounds__(kThreads) void row_finish(RowArgs a) {
             }
             __syncthreads();
             if (sh_total <= kSelect) break;
-            if (closer) {  // hardly more groups than k hold a key (a wave's lanes past the parts' keys have none)
-                from = (uint64_t)kth_of_each<kThreads>(most, a.n_top, sh_group).key << 32;
-            } else {  // many equal values: the k-th largest key itself (keys are distinct, so k reach it), by binary search
+            if (closer) {
+                // many equal values, or hardly more groups than k hold a key (a wave's lanes past the parts' keys have
+                // none): the k-th largest of the threads' largest keys, lower tokens first (64 alternatives of 48
+                // rows of 151,936 zeros: 67 us, 482 by the search below; other rows 19.6)
+                uint64_t own = 0, q[kWaves];
+                auto larger = [&](uint64_t key) { own = key > own ? key : own; };
+                if (held) {
+#pragma unroll
+                    for (int u = 0; u < kHeld; ++u) larger(mine[u]);
+                } else {  // a part's keys over all threads: of equal values those of the row's first parts decide
+                    for (int p = 0; p < a.parts; ++p)
+                        for (int i = threadIdx.x, n = __float_as_int(sums[p].w); i < n; i += kThreads) larger(keys[(size_t)p * a.capacity + i]);
+                }
+                __syncthreads();
+                sh_sel[threadIdx.x] = own;
+                __syncthreads();
+#pragma unroll
+                for (int u = 0; u < kWaves; ++u) q[u] = sh_sel[u * kWave + lane];
+                from = 0;
+                for (int b = 63; b >= 0; --b) {
+                    const uint64_t c = from | (1ull << b);
+                    int n = 0;
+#pragma unroll
+                    for (int u = 0; u < kWaves; ++u) n += __popcll(__ballot(q[u] >= c));
+                    if (n >= a.n_top) from = c;
+                }
+                from = from > 0 ? from : 1;  // fewer threads have one: all keys
+            } else {  // the k-th largest key itself (keys are distinct, so k reach it), by binary search
                 uint64_t kth = 0;
                 for (int b = 63; b >= 0; --b) {
                     const uint64_t c = kth | (1ull << b);

@@ -125,3 +125,18 @@ def test_likely_tokens_late_in_the_row_take_no_longer(n, v, n_top):
     rising = gpu_time((torch.arange(v, device="cuda") / v * 20).bfloat16().expand(n, v).contiguous(), n_top, 3)
     print(f"[time] {n}x{v} top {n_top}: {ordinary:.1f} us, rising: {rising:.1f}", flush=True)
     assert rising <= 6 * ordinary
+
+
+@pytest.mark.parametrize("n,v,n_top", [(1, 151936, 64), (48, 151936, 64), (48, 128256, 128), (9, 300007, 128), (90, 262144, 100)])
+def test_rows_of_equal_logits_take_no_longer(n, v, n_top):
+    """Rows of zeros (a padded batch), of two values, and rows that rise by steps, of which every part hands over n_top."""
+    x = torch.randn((n, v), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).mul_(3).bfloat16()
+    ordinary = gpu_time(x, n_top)
+    at = torch.arange(v, device="cuda")
+    for name, row in (("zeros", at * 0.0), ("two values", at % 3 // 2 * 1.0), ("steps", at // 1000 * 0.125)):
+        x.copy_(row)
+        us = gpu_time(x, n_top, 3)
+        print(f"[time] {n}x{v} top {n_top}: {ordinary:.1f} us, {name}: {us:.1f}", flush=True)
+        assert us <= 5 * ordinary
+        want = torch.sort(x[0].float(), descending=True, stable=True).indices[:n_top].int()
+        assert torch.equal(tt_logprobs(x, n_top).top_ids, want.expand(n, n_top))
