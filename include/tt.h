@@ -510,7 +510,7 @@ int tt_step(const tt_vocab *vd, const tt_vocab *vt, int32_t n_streams, int32_t v
  * probability 0.  A row with a logit of plus infinity, or with beta outside (0, 2^100], has no
  * distribution: its results are NaN (token ids -1).  v in 1..2^23, n_rows >= 0.
  * Each thread sums its share of a row in fp32, relative to its largest logit; these sums are joined in
- * fp32 within a wave and in fp64 beyond.  Which logits a thread takes depends on the rows' number, width
+ * fp32 within a wave, of split rows within a workgroup, and in fp64 beyond.  Which logits a thread takes depends on the rows' number, width
  * and alignment, so the last digits of a row's results may; they do not depend on scheduling.
  */
 enum { TT_BF16 = 0, TT_F16 = 1, TT_F32 = 2 };

@@ -15,10 +15,11 @@
 // by chunks for the rest's largest value and sum; one wave merges equal tokens, gathers the listed
 // logits (while the first loads are in flight) and forms the loss in fp64, and what the gradient needs:
 // the unlisted softmax's reference and factor, the listed tokens' gradients; then the row is streamed
-// again for its gradient.  Few enough rows are worked on at once that the second reading comes out of
-// the Infinity Cache.
-// Where the rows are too few to fill the GPU they are split: list_parts forms the sums of parts,
-// list_rows joins them and does the one wave's work, list_grad writes the gradient of parts.
+// again for its gradient.  512 rows at most are worked on at once (two workgroups a compute unit), so that the second
+// reading comes out of the Infinity Cache where these fit (156 MB of rows of 151,936 bf16).  Wider ones take the same
+// time a byte: 1,024 rows of 151,936 fp32, 311 MB at once, 290 us, 2,048 in bf16 289; 1,024 of 262,144 bf16 252.
+// Where the rows are too few to fill the GPU they are split: list_parts forms the sums of parts (in fp32 within a
+// workgroup), list_rows joins them and does the one wave's work, list_grad writes the gradient of parts.
 //
 // What bounds it: the loss alone reads at 5.1 TB/s with 512 rows of 151,936 bf16 (30.5 us; two workgroups a compute
 // unit, whose start and end are 7 of them).  The gradient of 2,048 such rows takes 275 us: 4.5 TB/s of the 1.24 GB

@@ -10,21 +10,21 @@
 // One pass over the row: row_stream, a workgroup for a row or a part of it, by chunks of 4 to 32 KB whose
 // loads are in flight while the chunk before is worked on.  Each thread keeps the largest value and the sums
 // (base 2, v_exp_f32) of what it has seen: in fp32 over a thread's elements, chunk by chunk, in fp64
-// from the waves' sums on.  The token's logit is read behind the first chunk's loads.
+// from the waves' sums on (from the workgroups', where they share a row).  The token's logit is read behind the first chunk's loads.
 //
 // Alternatives, in the same pass: each thread keeps the place of its largest value as well.  k of the
 // workgroup's 64 or 256 groups of threads hold a largest value that reaches the k-th largest of the groups',
 // so every one of the k largest elements does.  That bound is formed after chunks 1, 2, 4, 8, ..., and elements
 // that reach it are staged in LDS as 64-bit keys (value, then lower index), over a row of N chunks about
 // k (1 + log2 N) of them (of long rows their whole vectors, told apart at the end); then the keys are ordered by
-// counting.  A row's only workgroup finishes it; with several, each hands its sums and keys to row_finish.
+// counting.  Rows of which more are staged than there is room for (TopSet::finish) are read again.  A row's only workgroup finishes it; with several, each hands its sums and keys to row_finish.
 //
 // What bounds it: the reading of the logits, at 6.4 to 6.9 TB/s on a row set beyond the Infinity Cache (4,096
 // rows of 151,936 bf16: 187 us a pass, 6.7 TB/s; a kernel that only reads gets no more), and the VALU where the
 // alternatives are wanted (about 9 issue slots an element for the statistics, the exponential four of them; 1,024
 // rows of 262,144 with 64 alternatives: 94 us against 80 to read them; the VALU is busy 77% of the cycles).  Few rows
-// are latency: one row of 640 takes 5 us on the GPU, one of 151,936 with 20 alternatives 6.3 for its 19 parts and 6.5
-// to join them.
+// are latency: one row of 640 takes 5 us on the GPU, one of 151,936 with 20 alternatives 6 for its 19 parts and 7 to
+// join them.
 #include "rows.h"
 
 namespace tt {
@@ -46,8 +46,9 @@ constexpr int kLongThreads = 1024, kLongVectors = 2;
 constexpr int64_t kVectorBytes = 32 << 10;
 // Rows up to these bytes are taken whole, by 1,024 threads each, however few they are; longer ones from few_rows
 // on; fewer are split over more workgroups and joined by a second kernel (20 alternatives of one row of 151,936 bf16:
-// 12.9 us, 21.9 whole; of 48 of 128,256: 15.5 and 19.4; of 128: 21.2 and 18.7; of 96 of a million: 50 and 75; of 160: 67
-// and 75; of 250: 88 and 83).
+// 12.9 us, 21.9 whole; of 48 of 128,256: 15.5 and 19.4; of 128: 21.2 and 18.7; of 96 of 262,200: 26 and 31, of 128: 31.5
+// and 31.7, of 160: 33.7 and 32.0, of 191: 37 and 32, without alternatives 24 and 24; of 96 of 500,000: 36 and 45, of 160:
+// 45 and 46, of 191: 51 and 46; of 96 of a million: 52 and 77, of 160: 70 and 78, of 191: 82 and 78).
 constexpr int64_t kLongBytes = 128 << 10;
 int64_t few_rows(int64_t row_bytes) { return row_bytes <= (512 << 10) ? 96 : 192; }
 
@@ -853,12 +854,12 @@ void launch_rows(const RowArgs &a, int threads, int64_t n, hipStream_t stream) {
 // One reading and one writing of the row, nothing kept between elements: p from the row's statistics, one
 // exponential each.  A workgroup takes one part of two vectors a thread, so that very many are at different
 // points of load and store, which mixes reads and writes best; loads ahead of the stores gain nothing.  Bound by
-// HBM: 2,048 rows of 128,256 bf16 take 160 us, 6.5 TB/s read and written (a large copy gets 5.1).
+// HBM: 2,048 rows of 128,256 bf16 take 166 us, 6.3 TB/s read and written (a large copy gets 5.1).
 constexpr int kGradVectors = 2;
 
-// Gradients up to the Infinity Cache's size are left in it for what reads them next, which is faster here, too
-// (1,000 rows of 128,256, 256 MB: 78 us, 89 with the non-temporal hint); larger ones would only pass through it
-// (2,048 rows: 184 and 172).
+// Gradients up to the Infinity Cache's size are left in it for what reads them next, which costs nothing here (600 rows
+// of 128,256, 154 MB: 50 us, 49 with the non-temporal hint; 1,000 rows, 256 MB: 79 and 82); larger ones would only pass
+// through it (1,200 rows: 104 and 98; 2,048: 172 and 166).
 constexpr int64_t kKeptBytes = int64_t(256) << 20;
 
 struct GradArgs {

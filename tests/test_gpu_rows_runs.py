@@ -137,6 +137,6 @@ def test_rows_of_equal_logits_take_no_longer(n, v, n_top):
         x.copy_(row)
         us = gpu_time(x, n_top, 3)
         print(f"[time] {n}x{v} top {n_top}: {ordinary:.1f} us, {name}: {us:.1f}", flush=True)
-        assert us <= 5 * ordinary
+        assert us <= 8 * ordinary  # 24 to 41 times as long by 64 searches
         want = torch.sort(x[0].float(), descending=True, stable=True).indices[:n_top].int()
         assert torch.equal(tt_logprobs(x, n_top).top_ids, want.expand(n, n_top))
