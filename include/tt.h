@@ -530,11 +530,12 @@ enum { TT_BF16 = 0, TT_F16 = 1, TT_F32 = 2 };
  *   top_logprobs [n_rows][n_top] their lp; minus infinity where top_ids is -1
  * A row without a logit above minus infinity has M = lse = -inf, L = 0, H = 0, logprob = -inf and
  * no alternatives.
- * Reads every logit once.  workspace: tt_logprobs_workspace_size bytes serve every call of up to n_rows
- * rows and n_top alternatives (0 for rows of at most 128 KB); a call uses tt_logprobs_workspace_used bytes
- * of it, by its own numbers (0 where a row is one workgroup's: at those widths, or for 96 rows or more, 192 of over 512 KB).
- * 16-byte aligned, no initialisation; calls that overlap in time must not share it.  One kernel on
- * `stream`, two where rows are split (one for each 2^18 rows that are not).  TT_EINVAL on a bad size or
+ * Reads every logit once, with alternatives a second time in rows whose likely tokens come late or lie
+ * in one run.  workspace: tt_logprobs_workspace_size bytes serve every call of up to n_rows rows and
+ * n_top alternatives (0 for rows of at most 128 KB); a call uses tt_logprobs_workspace_used bytes of it,
+ * by its own numbers (0 where a row is one workgroup's: at those widths, or for 96 rows or more, 192 of
+ * over 512 KB).  16-byte aligned, no initialisation; calls that overlap in time must not share it.  One
+ * kernel on `stream`, two where rows are split (one for each 2^18 rows that are not).  TT_EINVAL on a bad size or
  * type, a missing pointer or one not aligned to its elements, TT_EUNSUPPORTED for v > 2^23 or
  * n_top > 128, TT_EWORKSPACE when the workspace is missing or smaller than what the call uses.
  */
@@ -590,9 +591,10 @@ int tt_logprobs_backward(int32_t n_rows, int32_t v, int32_t dtype, const void *l
  *   grad_loss    [n_rows], required with dlogits
  *   dlogits      optional (NULL: the loss alone); layout, rounding and aliasing as in tt_logprobs_backward
  * workspace: tt_distill_workspace_size bytes (with_grad: whether dlogits will be given) serve every call of
- * up to n_rows rows and n_top listed tokens; a call uses tt_distill_workspace_used bytes of it (0 where a row is one workgroup's: v <= 2^18, and rows of at most 128 KB or 96 rows or more).  16-byte aligned, no
- * initialisation; calls that overlap in time must not share it.  One kernel on `stream`, or where rows are
- * split two, three with the gradient, for each group of rows.  With the gradient every logit is read
+ * up to n_rows rows and n_top listed tokens; a call uses tt_distill_workspace_used bytes of it (0 where a
+ * row is one workgroup's: v <= 2^18, and rows of at most 128 KB or 96 rows or more).  16-byte aligned, no
+ * initialisation; calls that overlap in time must not share it.  One kernel on `stream` (for each 2^18
+ * rows), or where rows are split two, three with the gradient, for each group of rows.  With the gradient every logit is read
  * twice, the second time mostly from a cache.  Errors as for tt_logprobs (n_top < 1 is TT_EINVAL).
  */
 int tt_distill_workspace_size(int32_t n_rows, int32_t v, int32_t dtype, int32_t n_top, int32_t with_grad, size_t *bytes);
