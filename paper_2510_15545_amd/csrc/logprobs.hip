@@ -10,14 +10,16 @@
 // One pass over the row: row_stream, a workgroup for a row or a part of it, by chunks of 4 to 32 KB whose
 // loads are in flight while the chunk before is worked on.  Each thread keeps the largest value and the sums
 // (base 2, v_exp_f32) of what it has seen: in fp32 over a thread's elements, chunk by chunk, in fp64
-// from the waves' sums on (from the workgroups', where they share a row).  The token's logit is read behind the first chunk's loads.
+// from the waves' sums on (from the workgroups', where they share a row).  The token's logit is read behind
+// the first chunk's loads.
 //
 // Alternatives, in the same pass: each thread keeps the place of its largest value as well.  k of the
 // workgroup's 64 or 256 groups of threads hold a largest value that reaches the k-th largest of the groups',
 // so every one of the k largest elements does.  That bound is formed after chunks 1, 2, 4, 8, ..., and elements
 // that reach it are staged in LDS as 64-bit keys (value, then lower index), over a row of N chunks about
 // k (1 + log2 N) of them (of long rows their whole vectors, told apart at the end); then the keys are ordered by
-// counting.  Rows of which more are staged than there is room for (TopSet::finish) are read again.  A row's only workgroup finishes it; with several, each hands its sums and keys to row_finish.
+// counting.  Rows of which more are staged than there is room for (TopSet::finish) are read again.  A row's only
+// workgroup finishes it; with several, each hands its sums and keys to row_finish.
 //
 // What bounds it: the reading of the logits, at 6.4 to 6.9 TB/s on a row set beyond the Infinity Cache (4,096
 // rows of 151,936 bf16: 187 us a pass, 6.7 TB/s; a kernel that only reads gets no more), and the VALU where the
