@@ -1,0 +1,270 @@
+"""Performance cases of the output head: log probabilities from hidden states and the head's weights without keeping the
+logits, their gradient, 8-bit quantisation by rows, and the matrix product in 8-bit integers that the head is in 8 bits.
+
+A case is a dict of plain values.  Its "kind" names the public call it stands for:
+
+  score       log probabilities of given tokens from hidden states (tt.head_logprobs)
+  train       their gradient with respect to hidden states and weights (tt.head_logprobs_backward)
+  quantize    rows to 8-bit integers with a scale each (tt.quantize_i8)
+  matmul      8-bit integers' product with scales for each token and channel, and its rows' log-sum-exp (tt.matmul_i8)
+
+run() takes the framework's calls where `own` is true and otherwise the same operators in elementary torch
+operations in fp32.  prepare() makes what a program has in hand: hidden states, weights, tokens, temperatures, the
+saved statistics of the forward pass, upstream gradients, weights quantised once.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+_DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+_BYTES = {"bf16": 2, "f16": 2, "f32": 4}
+_FLOPS = 2.5e12   # operations of a drawn case at most
+_WEIGHTS = 3.2e8  # elements of a drawn case's weights at most
+
+
+def listed():
+    return [
+        # one interactive stream of a small model: launches are all there is
+        dict(name="score 1x640 h256", kind="score", n=1, v=640, h=256, dtype="bf16"),
+        # a few streams' decode step, the log probabilities of what was sampled: the weights are read once
+        dict(name="score 8x151936 h2048", kind="score", n=8, v=151936, h=2048, dtype="bf16"),
+        # a ragged batch of scored answers, odd vocabulary
+        dict(name="score 333x50257 h768 f16", kind="score", n=333, v=50257, h=768, dtype="f16"),
+        # the forward pass of a training step
+        dict(name="score 4096x151936 h2048", kind="score", n=4096, v=151936, h=2048, dtype="bf16"),
+        # a small drafter's accumulation step in fp32
+        dict(name="train 96x32000 h512 f32", kind="train", n=96, v=32000, h=512, dtype="f32", ignored=0.0),
+        # ragged answers behind prompts that carry no loss, odd vocabulary, fp16 with its loss scale
+        dict(name="train 391x50257 h1024 f16", kind="train", n=391, v=50257, h=1024, dtype="f16", ignored=0.3),
+        # the backward pass of a training step
+        dict(name="train 2048x128256 h2048", kind="train", n=2048, v=128256, h=2048, dtype="bf16", ignored=0.0),
+        # one token's hidden state before the head in 8 bits
+        dict(name="quantize 1x2048", kind="quantize", n=1, k=2048, dtype="bf16"),
+        # a prompt's activations
+        dict(name="quantize 8192x4096", kind="quantize", n=8192, k=4096, dtype="bf16"),
+        # one stream's decode step through the head in 8 bits: the weights are read once
+        dict(name="matmul 1x151936 k4096 lse", kind="matmul", n=1, v=151936, k=4096, dtype="bf16", lse=True, bias=False),
+        # the verification of 32 streams of 8 drafted tokens
+        dict(name="matmul 288x128256 k2048 lse", kind="matmul", n=288, v=128256, k=2048, dtype="bf16", lse=True, bias=False),
+        # the verification of 256 streams of 8 drafted tokens
+        dict(name="matmul 2304x151936 k4096 lse", kind="matmul", n=2304, v=151936, k=4096, dtype="bf16", lse=True, bias=False),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(("score", "score", "train", "train", "quantize", "matmul", "matmul"))
+    dtype = rng.choice(("bf16", "bf16", "bf16", "f16", "f32"))
+    if kind == "quantize":
+        return dict(kind=kind, n=_log_int(rng, 1, 8192), k=_log_int(rng, 64, 4096), dtype=dtype)
+    v, width = _log_int(rng, 500, 262144), _log_int(rng, 64, 4096)
+    if rng.random() < 0.8:  # widths of models are multiples of some power of two; some are not
+        width = max(64, width // 64 * 64)
+    width = min(width, int(_WEIGHTS / v) if kind != "matmul" else 4096)
+    passes = (3 if kind == "train" else 1) * (8 if dtype == "f32" and kind != "matmul" else 1)
+    n = _log_int(rng, 1, max(1, min(4096, int(_FLOPS / (2.0 * passes * v * width)))))
+    if kind == "score":
+        return dict(kind=kind, n=n, v=v, h=width, dtype=dtype)
+    if kind == "train":
+        return dict(kind=kind, n=n, v=v, h=width, dtype=dtype, ignored=rng.choice((0.0, 0.0, 0.3, 0.6)))
+    return dict(kind=kind, n=n, v=v, k=width, dtype=dtype, lse=rng.random() < 0.6, bias=rng.random() < 0.3)
+
+
+# ------------------------------------------------------------------------------- inputs
+def _rand(gen, *shape):
+    return torch.rand(shape, generator=gen, device="cuda")
+
+
+def _randn(gen, *shape):
+    return torch.randn(shape, generator=gen, device="cuda")
+
+
+def _activations(gen, n, k):
+    """Activations as a model has them: some channels far wider than the rest, rows of different sizes."""
+    channel = torch.where(_rand(gen, k) < 0.01, 8.0 + 24.0 * _rand(gen, k), 0.5 + _rand(gen, k))
+    return _randn(gen, n, k) * channel * (0.3 + 2.0 * _rand(gen, n, 1))
+
+
+def _to_i8(x):
+    """(integers, scales) of a program's own one-time quantisation."""
+    scale = x.abs().amax(1) / 127.0
+    return torch.round(x / scale[:, None]).to(torch.int8), scale
+
+
+def _ignored(case):
+    return int(case["ignored"] * case["n"])
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(int(seed) * 4 + 3)
+    n, dtype = case["n"], _DTYPES[case["dtype"]]
+    state = dict(case)
+    if case["kind"] == "quantize":
+        state["x"] = _activations(gen, n, case["k"]).to(dtype)
+        return state
+    v = case["v"]
+    if case["kind"] == "matmul":
+        k = case["k"]
+        state["x"], state["xs"] = _to_i8(_activations(gen, n, k))
+        state["w"], state["ws"] = _to_i8(_randn(gen, v, k) * (0.5 + _rand(gen, v, 1)) / k)
+        state["ws"] = state["ws"] * (3.0 * math.sqrt(k) / 2.0)  # logits of a few units
+        state["beta"] = 0.7 + 0.8 * _rand(gen, n)
+        state["b"] = _randn(gen, v) if case["bias"] else None
+        return state
+    h = case["h"]
+    weight = (_randn(gen, v, h) / math.sqrt(h)).to(dtype)
+    ids = torch.randint(0, v, (n,), generator=gen, device="cuda")
+    # most tokens are likely ones: the hidden state leans towards their weights
+    hidden = (2.0 * _randn(gen, n, h) + 14.0 * _rand(gen, n, 1) * weight[ids].float()).to(dtype)
+    state.update(hidden=hidden, weight=weight, beta=0.7 + 0.8 * _rand(gen, n), ids=ids.int())
+    if case["kind"] == "train":
+        state["g"] = -(0.5 + _rand(gen, n)) / n * (1024.0 if case["dtype"] == "f16" else 1.0)  # the loss scale of fp16 training
+        without = torch.randperm(n, generator=gen, device="cuda")[:_ignored(case)]
+        state["g"][without] = 0.0
+        state["ids"][without] = -1
+        state["stats"] = _statistics(hidden, weight, state["beta"])
+    return state
+
+
+def _statistics(hidden, weight, beta):
+    """What a forward pass saved: the largest logit and the log of the sum relative to it."""
+    z = hidden.float() @ weight.float().T
+    top = z.amax(1, keepdim=True)
+    return torch.cat((top, z.sub_(top).mul_(beta[:, None]).exp_().sum(1, keepdim=True, dtype=torch.float64).log().float()), 1)
+
+
+# ------------------------------------------------------------------------------- the framework's calls
+def _own(s):
+    import paper_2510_15545_amd as tt
+
+    kind = s["kind"]
+    if kind == "score":
+        return tt.head_logprobs(s["v"], s["hidden"], s["weight"], s["ids"], inv_temperature=s["beta"])._asdict()
+    if kind == "train":
+        dhidden, dweight = tt.head_logprobs_backward(s["v"], s["hidden"], s["weight"], s["ids"], s["stats"], s["g"], inv_temperature=s["beta"])
+        return {"dhidden": dhidden, "dweight": dweight}
+    if kind == "quantize":
+        q, scale = tt.quantize_i8(s["x"])
+        return {"q": q, "scale": scale}
+    out, lse = tt.matmul_i8(s["x"], s["xs"], s["w"], s["ws"], bias=s["b"], dtype=_DTYPES[s["dtype"]], lse=s["lse"],
+                            inv_temperature=s["beta"] if s["lse"] else None)
+    return {"out": out, "lse": lse}
+
+
+# ------------------------------------------------------------------------------- the plain forms
+def _plain_score(s):
+    z = s["hidden"].float() @ s["weight"].float().T
+    beta = s["beta"][:, None]
+    top = z.amax(1, keepdim=True)
+    y = (z - top) * beta
+    log_sum = y.exp().sum(1, keepdim=True).log()
+    return {"logprob": (y.gather(1, s["ids"].long()[:, None]) - log_sum)[:, 0], "lse": (top * beta + log_sum)[:, 0],
+            "stats": torch.cat((top, log_sum), 1)}
+
+
+def _plain_train(s):
+    hidden, weight, beta = s["hidden"].float(), s["weight"].float(), s["beta"][:, None]
+    keep = (s["ids"] >= 0)[:, None]
+    g = torch.where(keep, s["g"][:, None], torch.zeros_like(beta))
+    lp = (hidden @ weight.T - s["stats"][:, :1]) * beta - s["stats"][:, 1:]
+    at = s["ids"].long().clamp_min(0)[:, None]
+    d = -g * lp.exp()
+    d.scatter_(1, at, -g * torch.expm1(lp.gather(1, at)))
+    d = d * beta
+    return {"dhidden": (d @ weight).to(s["hidden"].dtype), "dweight": (d.T @ hidden).to(s["weight"].dtype)}
+
+
+def _plain_quantize(s):
+    x = s["x"].float()
+    scale = x.abs().amax(1) / 127.0
+    q = torch.round(x / torch.where(scale > 0, scale, torch.ones_like(scale))[:, None])
+    return {"q": q.clamp(-127.0, 127.0).to(torch.int8), "scale": scale}
+
+
+def _plain_matmul(s):
+    y = (s["x"].float() @ s["w"].float().T) * s["xs"][:, None] * s["ws"]
+    y = (y if s["b"] is None else y + s["b"]).to(_DTYPES[s["dtype"]])
+    lse = None
+    if s["lse"]:  # of the logits as they are written
+        z = y.float() * s["beta"][:, None]
+        top = z.amax(1, keepdim=True)
+        lse = (top + (z - top).exp().sum(1, keepdim=True).log())[:, 0]
+    return {"out": y, "lse": lse}
+
+
+def run(state):
+    if own:
+        return _own(state)
+    kind = state["kind"]
+    if kind in ("score", "train"):
+        return _plain_score(state) if kind == "score" else _plain_train(state)
+    return _plain_quantize(state) if kind == "quantize" else _plain_matmul(state)
+
+
+# ------------------------------------------------------------------------------- what a pass cannot do without
+def work(case):
+    n, e = case["n"], _BYTES[case["dtype"]]
+    if case["kind"] == "quantize":  # the row; its integers and its scale
+        return {"bytes": n * case["k"] * (e + 1) + 4 * n, "flops": 4 * n * case["k"]}
+    v = case["v"]
+    if case["kind"] == "matmul":  # both operands and their scales; the result, log-sum-exp and temperature
+        k = case["k"]
+        more = (8 * n if case["lse"] else 0) + (4 * v if case["bias"] else 0)
+        return {"bytes": n * k + v * k + 4 * (n + v) + n * v * e + more, "flops": 2 * n * v * k}
+    h = case["h"]
+    if case["kind"] == "score":  # hidden states and weights; token, temperature; logprob, lse, statistics
+        return {"bytes": (n + v) * h * e + n * (8 + 16), "flops": 2 * n * v * h}
+    kept = n - _ignored(case)  # three products over the rows that carry a loss; both gradients are written
+    return {"bytes": (kept + n + 2 * v) * h * e + n * 20, "flops": 6 * kept * v * h}
+
+
+# ------------------------------------------------------------------------------- 64 bits
+def exact(case, seed):
+    s = prepare(case, seed)
+    n = case["n"]
+    if case["kind"] == "quantize":
+        return {"q": None, "scale": s["x"].double().abs().max(1).values / 127.0}
+    v = case["v"]
+    step = max(1, int(2.5e8 / v))  # rows whose logits are held at once
+    if case["kind"] == "matmul":
+        out, lse = [], []
+        w = s["w"].double() * s["ws"].double()[:, None]
+        for a in range(0, n, step):
+            y = (s["x"][a:a + step].double() * s["xs"][a:a + step, None].double()) @ w.T
+            if s["b"] is not None:
+                y += s["b"].double()
+            # the logits as they are written, beside their values
+            lse.append(torch.logsumexp(y.to(_DTYPES[case["dtype"]]).double() * s["beta"][a:a + step, None].double(), 1))
+            out.append(y if n * v <= 4e8 else y.float())
+        return {"out": torch.cat(out), "lse": torch.cat(lse) if case["lse"] else None}
+    weight = s["weight"].double()
+    if case["kind"] == "score":
+        logprob, lse, stats = [], [], []
+        for a in range(0, n, step):
+            z = s["hidden"][a:a + step].double() @ weight.T
+            m, beta = z.max(1).values, s["beta"][a:a + step].double()
+            total = torch.logsumexp(z * beta[:, None], 1)
+            logprob.append(z.gather(1, s["ids"][a:a + step, None].long())[:, 0] * beta - total)
+            lse.append(total)
+            stats.append(torch.stack((m, total - beta * m), 1))
+        return {"logprob": torch.cat(logprob), "lse": torch.cat(lse), "stats": torch.cat(stats)}
+    dhidden = torch.zeros((n, case["h"]), dtype=torch.float64, device="cuda")
+    dweight = torch.zeros((v, case["h"]), dtype=torch.float64, device="cuda")
+    for a in range(0, n, step):
+        x, beta = s["hidden"][a:a + step].double(), s["beta"][a:a + step, None].double()
+        g, ids = s["g"][a:a + step, None].double(), s["ids"][a:a + step].long()
+        d = -torch.softmax((x @ weight.T) * beta, 1)
+        rows = torch.nonzero(ids >= 0)[:, 0]
+        d[rows, ids[rows]] += 1.0
+        d *= g * beta
+        d[ids < 0] = 0.0
+        dhidden[a:a + step] = d @ weight
+        dweight += d.T @ x
+    return {"dhidden": dhidden, "dweight": dweight}
