@@ -183,7 +183,8 @@ def _plain_train(s):
 
 def _plain_quantize(s):
     x = s["x"].float()
-    scale = x.abs().amax(1) / 127.0
+    top = x.abs().amax(1)
+    scale = top / torch.full_like(top, 127.0)  # the quotient; by a number torch would multiply with its reciprocal
     q = torch.round(x / torch.where(scale > 0, scale, torch.ones_like(scale))[:, None])
     return {"q": q.clamp(-127.0, 127.0).to(torch.int8), "scale": scale}
 
