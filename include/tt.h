@@ -604,6 +604,81 @@ int tt_distill(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int
                const int32_t *id_map, int32_t n_map, int32_t tail, float *loss, const float *grad_loss,
                void *dlogits, int64_t dlogits_ld, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * The output head.  The calls below take hidden states (n_rows rows of h elements at a stride of hidden_ld) and the head's
+ * weights (v rows of h elements at a stride of weight_ld), both in bf16, fp16 or fp32 and aligned to their elements, and
+ * form the logits x_ij = sum_k hidden_ik weight_jk themselves, a tile at a time: none is kept.  Products are exact and
+ * summed in fp32 (fp32 operands as three bf16 parts each, to 2^-24 of every product).  M, S, L, lse, lp_j and p_j are as
+ * above, but a logit that is NaN makes its row's results NaN (here it is the outcome of a sum, not a mask).
+ * n_rows <= 2^20, v <= 2^23, h <= 2^16.
+ *
+ * tt_head_logprobs -- log probabilities of given tokens, the cross entropy's forward pass.
+ *   ids          optional (device, [n_rows])
+ * Outputs (device, each optional): logprob (requires ids; NaN for an id outside [0, v)), lse, stats [n_rows][2], as of tt_logprobs.
+ * workspace: tt_head_logprobs_workspace_size bytes for up to n_rows rows; 16-byte aligned, no initialisation; calls that overlap
+ * in time must not share it.  TT_EINVAL on a bad size or type, a missing pointer or one not aligned to its elements,
+ * TT_EUNSUPPORTED above the sizes named, TT_EWORKSPACE when the workspace is missing or too small.
+ */
+int tt_head_logprobs_workspace_size(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, size_t *bytes);
+int tt_head_logprobs(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, const void *hidden, int64_t hidden_ld, const void *weight,
+                     int64_t weight_ld, const float *inv_temperature, const int32_t *ids, float *logprob, float *lse,
+                     float *stats, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * tt_head_logprobs_backward -- the gradient of sum_i (grad_logprob[i] logprob_i + grad_lse[i] lse_i):
+ *     dx_j = beta (g ([j = id] - p_j) + w p_j),  dhidden = dx weight,  dweight = dx^T hidden,
+ * g = grad_logprob[i] (0 for an id outside [0, v)), w = grad_lse[i].
+ *
+ *   stats        [n_rows][2] from tt_head_logprobs on the same operands and temperatures
+ *   ids, grad_logprob     both or neither (device, [n_rows])
+ *   grad_lse     optional (device, [n_rows])
+ *   dhidden, dweight      either may be NULL; n_rows and v rows of h elements of the operands' type at strides of their own,
+ *                rounded once to nearest even; elements past h in a row are left alone.  They must meet neither the
+ *                operands nor each other.
+ * A row with g = w = 0, or with M minus infinity, gets zeros, adds nothing to dweight and is not read (NaN in it is harmless).
+ * The logits are formed again, a piece of the vocabulary at a time; dx is rounded to the operands' type (fp32: three bf16
+ * parts) relative to the largest beta (|g| + |w|) of the rows before it is multiplied: in fp16 a row whose weight is below
+ * 2^-20 of the largest loses digits.  Sums are fp32, without atomics.  With n_rows = 0 dweight is zeros.
+ * workspace: tt_head_logprobs_backward_workspace_size bytes serve every call of up to n_rows rows, a call uses
+ * ..._workspace_used bytes.  Errors and workspaces as for tt_head_logprobs, and TT_EINVAL for gradients that meet something.
+ */
+int tt_head_logprobs_backward_workspace_size(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, size_t *bytes);
+int tt_head_logprobs_backward_workspace_used(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, size_t *bytes);
+int tt_head_logprobs_backward(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, const void *hidden, int64_t hidden_ld,
+                              const void *weight, int64_t weight_ld, const float *inv_temperature, const int32_t *ids,
+                              const float *stats, const float *grad_logprob, const float *grad_lse, void *dhidden,
+                              int64_t dhidden_ld, void *dweight, int64_t dweight_ld, void *workspace, size_t workspace_bytes,
+                              void *stream);
+
+/*
+ * tt_quantize_i8 -- rows of k elements (bf16, fp16 or fp32) to 8-bit integers with a scale each:
+ *     scale = max |x| / 127 (fp32),  q = x / scale rounded to nearest even, in -127 .. 127.
+ * A row of zeros (or with a scale that underflows) has scale 0 and q = 0; a row with a NaN or an infinity scale NaN and q = 0.
+ * k <= 131,071.  One kernel on `stream`; q must not meet x.
+ */
+int tt_quantize_i8(int32_t n_rows, int32_t k, int32_t dtype, const void *x, int64_t x_ld, int8_t *q, int64_t q_ld, float *scale,
+                   void *stream);
+
+/*
+ * tt_matmul_i8 -- matrix product in 8-bit integers with scales for each token and channel, an output head in 8 bits:
+ *     y_ij = x_scale[i] w_scale[j] sum_k x_ik w_jk (+ bias[j])
+ * The integers' sum is exact, converted to fp32 and multiplied by x_scale, then w_scale, then the bias is added (each
+ * rounded), and the result rounded to out_dtype (TT_BF16, TT_F16, TT_F32).
+ *   x, w         [n_rows][k] and [n_cols][k] int8 at strides x_ld, w_ld, as tt_quantize_i8 writes them (-128 is taken as well)
+ *   bias         optional (device, fp32 [n_cols])
+ *   out          [n_rows][n_cols] at a stride of out_ld elements; elements past n_cols are left alone; it must meet neither x nor w
+ *   lse          optional (device, [n_rows]): the log-sum-exp of inv_temperature[i] (NULL: 1) times the row's results as they are
+ *                written, as tt_verify_logits takes it; NaN for a row with a result that is NaN or plus infinity and for an
+ *                inverse temperature outside (0, 2^100]
+ * n_rows <= 2^20, n_cols <= 2^23, k <= 131,071.  workspace: tt_matmul_i8_workspace_size bytes for up to n_rows rows (with_lse:
+ * whether lse is wanted); 16-byte aligned, no initialisation; calls that overlap in time must not share it.  Errors as for
+ * tt_head_logprobs.
+ */
+int tt_matmul_i8_workspace_size(int32_t n_rows, int32_t n_cols, int32_t k, int32_t with_lse, size_t *bytes);
+int tt_matmul_i8(int32_t n_rows, int32_t n_cols, int32_t k, const int8_t *x, int64_t x_ld, const float *x_scale, const int8_t *w,
+                 int64_t w_ld, const float *w_scale, const float *bias, int32_t out_dtype, void *out, int64_t out_ld,
+                 const float *inv_temperature, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,10 @@ raised.
     logprobs / logprobs_backward  log probabilities of given tokens, log-sum-exp (as verify_logits
               takes it), entropy and top alternatives of rows of logits, and their gradient
     distill   tt_distill  loss and gradient of a draft model's rows against its target's top tokens
+    head_logprobs / head_logprobs_backward  the log probabilities of given tokens from hidden states and the
+              head's weights, no logits kept, and the gradient with respect to both
+    quantize_i8 / matmul_i8  rows to 8-bit integers with a scale each, and their product with scales for each
+              token and channel: a head in 8 bits, with the log-sum-exp that verify_logits takes
 """
 from __future__ import annotations
 
@@ -33,6 +37,8 @@ __all__ = ["Vocab", "align", "align_workspace", "transfer", "verify", "verify_no
            "delta_histogram", "delta_quantile", "w_at_quantile", "token_index", "retokenize", "LIB_PATH",
            "vocab_intersection", "tli_proposal", "verify_tli", "verify_logits", "verify_logits_workspace", "verify_tli_workspace",
            "logprobs", "logprobs_workspace", "logprobs_backward", "LogProbs", "distill", "distill_workspace",
+           "head_logprobs", "head_logprobs_workspace", "head_logprobs_backward", "head_logprobs_backward_workspace", "HeadLogProbs",
+           "quantize_i8", "matmul_i8", "matmul_i8_workspace",
            "TTError", "path_capacity"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtt.so")
@@ -127,6 +133,18 @@ def lib():
             f.restype = ctypes.c_int
         L.tt_distill.argtypes = [i32, i32, i32, P, i64, P, i32, P, P, P, i32, i32, P, P, P, i64, P, sz, P]
         L.tt_distill.restype = ctypes.c_int
+        for f in (L.tt_head_logprobs_workspace_size, L.tt_head_logprobs_backward_workspace_size,
+                  L.tt_head_logprobs_backward_workspace_used, L.tt_matmul_i8_workspace_size):
+            f.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
+            f.restype = ctypes.c_int
+        L.tt_head_logprobs.argtypes = [i32, i32, i32, i32, P, i64, P, i64, P, P, P, P, P, P, sz, P]
+        L.tt_head_logprobs.restype = ctypes.c_int
+        L.tt_head_logprobs_backward.argtypes = [i32, i32, i32, i32, P, i64, P, i64, P, P, P, P, P, P, i64, P, i64, P, sz, P]
+        L.tt_head_logprobs_backward.restype = ctypes.c_int
+        L.tt_quantize_i8.argtypes = [i32, i32, i32, P, i64, P, i64, P, P]
+        L.tt_quantize_i8.restype = ctypes.c_int
+        L.tt_matmul_i8.argtypes = [i32, i32, i32, P, i64, P, P, i64, P, P, i32, P, i64, P, P, P, sz, P]
+        L.tt_matmul_i8.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -643,6 +661,200 @@ def distill(v: int, logits, top_ids, top_logprobs, tail: bool = False, id_map=No
     if given:
         _written(*given)
     return loss, dlogits
+
+
+HeadLogProbs = collections.namedtuple("HeadLogProbs", "logprob lse stats")
+HeadLogProbs.__doc__ = """What head_logprobs() returns, float32 device tensors: logprob [n] of the given tokens (None without
+them), lse [n], stats [n, 2] for head_logprobs_backward()."""
+
+
+def _head(v: int, hidden, weight, stream):
+    """(n, h, type, address and stride of the hidden states and of the weights, device) of a call on the head."""
+    if hidden.dim() != 2 or weight.dim() != 2:
+        raise ValueError("hidden and weight must be 2-D row-major device tensors")
+    n, h = hidden.shape
+    code, x, x_ld = _rows(hidden, h, n, "hidden")
+    w_code, w, w_ld = _rows(weight, h, v, "weight")
+    if weight.shape[1] != h or w_code != code:
+        raise ValueError(f"weight must be {hidden.dtype} with rows of {h}")
+    dev = _launch_device(hidden, stream)
+    if weight.get_device() != dev:
+        raise ValueError(f"weight is on cuda:{weight.get_device()}, hidden on cuda:{dev}")
+    return n, h, code, x, x_ld, w, w_ld, dev
+
+
+def _sized(query: str, *sizes, device="cuda"):
+    n = ctypes.c_size_t(0)
+    _check(getattr(lib(), query)(*sizes, ctypes.byref(n)), query)
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
+def head_logprobs_workspace(n_rows: int, v: int, h: int, dtype, device="cuda"):
+    """A workspace for head_logprobs on up to n_rows hidden states of h elements of this type and v tokens, reusable by
+    calls that do not overlap in time."""
+    return _sized("tt_head_logprobs_workspace_size", int(n_rows), int(v), int(h), _dtype_code(dtype), device=device)
+
+
+def head_logprobs(v: int, hidden, weight, ids=None, inv_temperature=None, out=None, workspace=None, stream=None):
+    """tt_head_logprobs: logprobs() of the logits hidden @ weight[:v].T without these: of every hidden state ([n, h]
+    bfloat16, float16 or float32, row-major, any row stride) the log probability of its token ids[i] (int32 [n],
+    optional), its log-sum-exp, and the statistics that head_logprobs_backward() takes.  weight: [>= v, h] of the same
+    type, any row stride.  inv_temperature: float32 [n], 1 / T (1 if not given).  out: a HeadLogProbs of the caller's
+    tensors (a None among them is left out); workspace: from head_logprobs_workspace(); both are made here if not given.
+    Returns a HeadLogProbs; a training step's loss is -logprob."""
+    if stream is not None and (out is None or workspace is None):
+        return _on_stream(stream, head_logprobs, v, hidden, weight, ids, inv_temperature, out, workspace, None)
+    i32, f32 = torch.int32, torch.float32
+    v = int(v)
+    n, h, code, x, x_ld, w, w_ld, dev = _head(v, hidden, weight, stream)
+    given = out
+    if out is None:
+        on = hidden.device
+        out = HeadLogProbs(None if ids is None else torch.empty(n, dtype=f32, device=on), torch.empty(n, dtype=f32, device=on),
+                           torch.empty((n, 2), dtype=f32, device=on))
+    to = [_array(out[0], f32, n, "logprob", dev), _array(out[1], f32, n, "lse", dev), _array(out[2], f32, 2 * n, "stats", dev)]
+    ws, ws_bytes, _held = _needed_workspace(workspace, _spread_bytes("tt_head_logprobs_workspace_size", n, v, h, code), dev)
+    st = lib().tt_head_logprobs(n, v, h, code, x, x_ld, w, w_ld, _array(inv_temperature, f32, n, "inv_temperature", dev),
+                                _array(ids, i32, n, "ids", dev), *to, ws, ws_bytes, _stream_handle(stream))
+    if st:
+        _check(st, "tt_head_logprobs")
+    if given is not None:
+        _written(*given)
+    return out
+
+
+def head_logprobs_backward_workspace(n_rows: int, v: int, h: int, dtype, device="cuda"):
+    """A workspace for head_logprobs_backward on up to n_rows hidden states, as head_logprobs_workspace()."""
+    return _sized("tt_head_logprobs_backward_workspace_size", int(n_rows), int(v), int(h), _dtype_code(dtype), device=device)
+
+
+def head_logprobs_backward(v: int, hidden, weight, ids, stats, grad_logprob, grad_lse=None, inv_temperature=None, dhidden=True,
+                           dweight=True, workspace=None, stream=None):
+    """tt_head_logprobs_backward: the gradient of sum(grad_logprob * logprob) + sum(grad_lse * lse) with respect to the hidden
+    states and to weight[:v], from the stats that head_logprobs() gave for the same operands and temperatures.  ids and
+    grad_logprob may both be None, and so may grad_lse.  A row without a weight (an id outside [0, v), as prompts and padding
+    have it, and no grad_lse) is left out.  dhidden, dweight: True for a new tensor, False for none (a frozen head has no
+    dweight), or the caller's tensor of the operands' type, of which n and v rows are written.  workspace: from
+    head_logprobs_backward_workspace(), made here if not given.  Returns (dhidden, dweight), None for one not wanted; a
+    model's backward pass goes on with hidden.backward(dhidden)."""
+    if stream is not None and (workspace is None or dhidden is True or dweight is True):
+        return _on_stream(stream, head_logprobs_backward, v, hidden, weight, ids, stats, grad_logprob, grad_lse, inv_temperature,
+                          dhidden, dweight, workspace, None)
+    i32, f32 = torch.int32, torch.float32
+    v = int(v)
+    n, h, code, x, x_ld, w, w_ld, dev = _head(v, hidden, weight, stream)
+    if stats is None:
+        raise ValueError("stats is required")
+    given, results, to = [], [], []
+    for name, t, rows in (("dhidden", dhidden, n), ("dweight", dweight, v)):
+        if t is None or t is False:
+            results.append(None)
+            to += [None, 0]
+            continue
+        if t is True:
+            t = torch.empty((rows, h), dtype=hidden.dtype, device=hidden.device)
+        else:
+            given.append(t)
+        t_code, address, ld = _rows(t, h, rows, name)
+        if t_code != code or t.get_device() != dev:
+            raise ValueError(f"{name} must be {hidden.dtype} on the hidden states' device")
+        results.append(t)
+        to += [address or None, ld]
+    ws, ws_bytes, _held = _needed_workspace(workspace, _spread_bytes("tt_head_logprobs_backward_workspace_used", n, v, h, code), dev)
+    st = lib().tt_head_logprobs_backward(n, v, h, code, x, x_ld, w, w_ld, _array(inv_temperature, f32, n, "inv_temperature", dev),
+                                         _array(ids, i32, n, "ids", dev), _array(stats, f32, 2 * n, "stats", dev),
+                                         _array(grad_logprob, f32, n, "grad_logprob", dev), _array(grad_lse, f32, n, "grad_lse", dev),
+                                         *to, ws, ws_bytes, _stream_handle(stream))
+    if st:
+        _check(st, "tt_head_logprobs_backward")
+    if given:
+        _written(*given)
+    return tuple(results)
+
+
+def _bytes(t, name, device: int):
+    """(address, stride) of a 2-D row-major int8 tensor on that device."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype is not torch.int8 or (t.stride(1) != 1 and t.shape[1] != 1):
+        raise ValueError(f"{name} must be a 2-D row-major int8 device tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the call on cuda:{device}")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+
+
+def quantize_i8(x, out=None, stream=None):
+    """tt_quantize_i8: rows ([n, k] bfloat16, float16 or float32, row-major, any row stride) as int8 [n, k] and a scale each
+    (float32 [n]), x about q * scale: activations for each token, a weight matrix [channels, k] for each channel.
+    out: the caller's (q, scale).  Returns (q, scale)."""
+    if stream is not None and out is None:
+        return _on_stream(stream, quantize_i8, x, None, None)
+    if x.dim() != 2:
+        raise ValueError("x must be a 2-D row-major device tensor")
+    n, k = x.shape
+    code, address, ld = _rows(x, k, n, "x")
+    dev = _launch_device(x, stream)
+    given = out
+    if out is None:
+        out = torch.empty((n, k), dtype=torch.int8, device=x.device), torch.empty(n, dtype=torch.float32, device=x.device)
+    q, scale = out
+    to, q_ld = _bytes(q, "q", dev)
+    if tuple(q.shape) != (n, k):
+        raise ValueError(f"q must be [{n}, {k}]")
+    st = lib().tt_quantize_i8(n, k, code, address, ld, to, q_ld, _array(scale, torch.float32, n, "scale", dev), _stream_handle(stream))
+    if st:
+        _check(st, "tt_quantize_i8")
+    if given is not None:
+        _written(q, scale)
+    return out
+
+
+def matmul_i8_workspace(n_rows: int, n_cols: int, k: int, lse: bool = False, device="cuda"):
+    """A workspace for matmul_i8 on up to n_rows rows (empty when none is needed), reusable by calls that do not overlap
+    in time."""
+    return _sized("tt_matmul_i8_workspace_size", int(n_rows), int(n_cols), int(k), 1 if lse else 0, device=device)
+
+
+def matmul_i8(x, x_scale, weight, weight_scale, bias=None, dtype=None, lse=False, inv_temperature=None, out=None, workspace=None,
+              stream=None):
+    """tt_matmul_i8: x ([n, k] int8) times weight ([m, k] int8) transposed, times x_scale (float32 [n]) and weight_scale
+    (float32 [m]), plus bias (float32 [m], optional), in `dtype` (bfloat16 if neither it nor out is given); all row-major with
+    any row stride.  lse: True for the log-sum-exp of every row's results times inv_temperature (float32 [n], 1 if not
+    given), as verify_logits() takes it, or the caller's float32 [n].  out: the caller's rows of at least m.  workspace:
+    from matmul_i8_workspace().  Returns (out, lse or None)."""
+    if stream is not None and (out is None or workspace is None or lse is True):
+        return _on_stream(stream, matmul_i8, x, x_scale, weight, weight_scale, bias, dtype, lse, inv_temperature, out, workspace, None)
+    f32 = torch.float32
+    if x.dim() != 2 or weight.dim() != 2 or x.shape[1] != weight.shape[1]:
+        raise ValueError("x and weight must be 2-D with rows of one length")
+    (n, k), m = x.shape, weight.shape[0]
+    xa, x_ld = _bytes(x, "x", x.get_device())
+    dev = _launch_device(x, stream)
+    wa, w_ld = _bytes(weight, "weight", dev)
+    if x_scale is None or weight_scale is None:
+        raise ValueError("x_scale and weight_scale are required")
+    given = [t for t in (out, lse) if t is not None and t is not True and t is not False]
+    if out is None:
+        out = torch.empty((n, m), dtype=dtype or torch.bfloat16, device=x.device)
+    elif dtype is not None and out.dtype is not dtype:
+        raise ValueError(f"out is {out.dtype}, dtype {dtype}")
+    code, to, out_ld = _rows(out, m, n, "out")
+    if out.get_device() != dev:
+        raise ValueError("out must be on the device of x")
+    if lse is True:
+        lse = torch.empty(n, dtype=f32, device=x.device)
+    elif lse is False:
+        lse = None
+    if inv_temperature is not None and lse is None:
+        raise ValueError("inv_temperature is for lse")
+    nbytes = _spread_bytes("tt_matmul_i8_workspace_size", n, m, k, 0 if lse is None else 1)
+    ws, ws_bytes, _held = _needed_workspace(workspace, nbytes, dev)
+    st = lib().tt_matmul_i8(n, m, k, xa, x_ld, _array(x_scale, f32, n, "x_scale", dev), wa, w_ld, _array(weight_scale, f32, m, "weight_scale", dev),
+                            _array(bias, f32, m, "bias", dev), code, to, out_ld, _array(inv_temperature, f32, n, "inv_temperature", dev),
+                            _array(lse, f32, n, "lse", dev), ws, ws_bytes, _stream_handle(stream))
+    if st:
+        _check(st, "tt_matmul_i8")
+    if given:
+        _written(*given)
+    return out, lse
 
 
 def delta_histogram(draft_off, target_off, path_len, path, n_bins: int, out=None, stream=None):

@@ -18,6 +18,9 @@ constexpr int32_t kMaxTokenBytes = 64;        // longest target token the index 
 constexpr int32_t kMaxLogitsRow = 1 << 23;     // logits per row tt_verify_logits accepts (64-bit exact sums)
 constexpr int32_t kMaxTliRow = 1 << 21;        // target row tt_verify_tli accepts (chunk sums in 16 KB of LDS)
 constexpr int32_t kMaxListed = 128;            // top tokens per row of tt_logprobs and tt_distill
+constexpr int32_t kMaxHeadRows = 1 << 20;      // rows of tt_head_logprobs, tt_matmul_i8 and the calls beside them
+constexpr int32_t kMaxHeadWidth = 1 << 16;     // elements of a hidden state
+constexpr int32_t kMaxI8Sum = (1 << 17) - 1;   // products of -128 .. 127 whose sum stays in 32 bits
 constexpr int32_t kMaxRetokBytes = 4096;      // bytes of S (and tokens of T) per stream: 14 B of LDS each
 
 bool vocab_ok(const tt_vocab *v) {
@@ -52,6 +55,37 @@ bool same_or_apart(const void *a, int64_t lda, const void *b, int64_t ldb, int32
     if (p_end <= q || q_end <= p) return true;
     const uintptr_t ld = (uintptr_t)lda * e, row = (uintptr_t)v * e, apart = (p < q ? q - p : p - q) % ld;
     return lda == ldb && apart >= row && ld - apart >= row;  // from a row of one to the other's next, and back
+}
+
+// A matrix of n_rows rows of `row` bytes, `ld` bytes from one to the next.
+struct Extent {
+    const void *p;
+    int64_t n_rows, row, ld;
+};
+
+// Whether it ends within the 2^57 bytes that an address reaches.
+bool extent_ok(const Extent &a) {
+    const uint64_t end = uint64_t(1) << 57, at = reinterpret_cast<uintptr_t>(a.p);
+    return at < end && a.ld >= 0 && (unsigned __int128)(uint64_t)(a.n_rows - 1) * (uint64_t)a.ld + (uint64_t)a.row <= end - at;
+}
+
+// Whether two matrices do not meet: neither their spans nor, at one stride, their rows.  One that is null meets none.
+bool apart(const Extent &a, const Extent &b) {
+    if (!a.p || !b.p) return true;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a.p), q = reinterpret_cast<uintptr_t>(b.p);
+    if (p + (uintptr_t)(a.n_rows - 1) * a.ld + a.row <= q || q + (uintptr_t)(b.n_rows - 1) * b.ld + b.row <= p) return true;
+    if (a.ld != b.ld || a.ld == 0) return false;
+    const uintptr_t ld = a.ld, from_p = q >= p ? (q - p) % ld : (ld - (p - q) % ld) % ld;  // q's place in a row of a's
+    return from_p >= (uintptr_t)a.row && from_p + b.row <= ld;
+}
+
+int64_t bytes_of(int32_t dtype) { return dtype == TT_F32 ? 4 : 2; }
+
+// The operands' checks that both calls on the head make; TT_OK, or why not.
+int head_ok(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, int64_t hidden_ld, int64_t weight_ld) {
+    if (n_rows < 0 || v < 1 || h < 1 || !dtype_ok(dtype) || hidden_ld < h || weight_ld < h || hidden_ld > INT64_MAX / 4 || weight_ld > INT64_MAX / 4)
+        return TT_EINVAL;
+    return n_rows > kMaxHeadRows || v > kMaxLogitsRow || h > kMaxHeadWidth ? TT_EUNSUPPORTED : TT_OK;
 }
 
 }  // namespace
@@ -595,6 +629,155 @@ int tt_distill(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int
     a.dlogits = dlogits;
     a.out_ld = dlogits_ld;
     return tt::launch_distill(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+int tt_head_logprobs_workspace_size(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, size_t *bytes) {
+    const int st = head_ok(n_rows, v, h, dtype, h, h);
+    if (bytes == nullptr || st != TT_OK) return bytes == nullptr ? TT_EINVAL : st;
+    *bytes = n_rows == 0 ? 0 : tt::head_workspace_bytes(n_rows, v, h, dtype);
+    return TT_OK;
+}
+
+int tt_head_logprobs(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, const void *hidden, int64_t hidden_ld, const void *weight,
+                     int64_t weight_ld, const float *inv_temperature, const int32_t *ids, float *logprob, float *lse,
+                     float *stats, void *workspace, size_t workspace_bytes, void *stream) {
+    const int st = head_ok(n_rows, v, h, dtype, hidden_ld, weight_ld);
+    if (st != TT_OK || n_rows == 0) return st;
+    const int64_t e = bytes_of(dtype);
+    if (!hidden || !weight || (logprob && !ids) || !aligned(hidden, e) || !aligned(weight, e) || !aligned(workspace, 16) ||
+        !words_aligned(inv_temperature, ids, logprob, lse, stats) || !extent_ok({hidden, n_rows, h * e, hidden_ld * e}) ||
+        !extent_ok({weight, v, h * e, weight_ld * e}))
+        return TT_EINVAL;
+    tt::HeadArgs a;
+    a.n_rows = n_rows;
+    a.v = v;
+    a.h = h;
+    a.dtype = dtype;
+    a.hidden = hidden;
+    a.weight = weight;
+    a.x_ld = hidden_ld;
+    a.w_ld = weight_ld;
+    a.inv_temp = inv_temperature;
+    a.ids = ids;
+    a.logprob = logprob;
+    a.lse = lse;
+    a.stats = stats;
+    return tt::launch_head_logprobs(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+int tt_head_logprobs_backward_workspace_size(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, size_t *bytes) {
+    const int st = head_ok(n_rows, v, h, dtype, h, h);
+    if (bytes == nullptr || st != TT_OK) return bytes == nullptr ? TT_EINVAL : st;
+    *bytes = n_rows == 0 ? 0 : tt::head_backward_workspace_bytes(n_rows, v, h, dtype);
+    return TT_OK;
+}
+
+int tt_head_logprobs_backward_workspace_used(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, size_t *bytes) {
+    const int st = head_ok(n_rows, v, h, dtype, h, h);
+    if (bytes == nullptr || st != TT_OK) return bytes == nullptr ? TT_EINVAL : st;
+    *bytes = n_rows == 0 ? 0 : tt::head_backward_workspace_used(n_rows, v, h, dtype);
+    return TT_OK;
+}
+
+int tt_head_logprobs_backward(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, const void *hidden, int64_t hidden_ld,
+                              const void *weight, int64_t weight_ld, const float *inv_temperature, const int32_t *ids,
+                              const float *stats, const float *grad_logprob, const float *grad_lse, void *dhidden,
+                              int64_t dhidden_ld, void *dweight, int64_t dweight_ld, void *workspace, size_t workspace_bytes,
+                              void *stream) {
+    const int st = head_ok(n_rows, v, h, dtype, hidden_ld, weight_ld);
+    if (st != TT_OK) return st;
+    if ((dhidden && (dhidden_ld < h || dhidden_ld > INT64_MAX / 4)) || (dweight && (dweight_ld < h || dweight_ld > INT64_MAX / 4)) ||
+        (!dhidden && !dweight))
+        return TT_EINVAL;
+    const int64_t e = bytes_of(dtype);
+    const Extent dx = {dhidden, n_rows, h * e, dhidden_ld * e}, dw = {dweight, v, h * e, dweight_ld * e};
+    if (!aligned(dhidden, e) || !aligned(dweight, e) || (dweight && !extent_ok(dw))) return TT_EINVAL;
+    const Extent x = {hidden, n_rows, h * e, hidden_ld * e}, w = {weight, v, h * e, weight_ld * e};
+    if (n_rows > 0) {
+        if (!hidden || !weight || !stats || (ids == nullptr) != (grad_logprob == nullptr) || !aligned(hidden, e) ||
+            !aligned(weight, e) || !aligned(workspace, 16) || !words_aligned(inv_temperature, ids, stats, grad_logprob, grad_lse) ||
+            !extent_ok(x) || !extent_ok(w) || (dhidden && !extent_ok(dx)) || !apart(x, dx) || !apart(x, dw) || !apart(w, dx) ||
+            !apart(w, dw) || !apart(dx, dw))
+            return TT_EINVAL;
+    }
+    tt::HeadGradArgs a;
+    a.n_rows = n_rows;
+    a.v = v;
+    a.h = h;
+    a.dtype = dtype;
+    a.hidden = hidden;
+    a.weight = weight;
+    a.x_ld = hidden_ld;
+    a.w_ld = weight_ld;
+    a.inv_temp = inv_temperature;
+    a.ids = ids;
+    a.stats = stats;
+    a.grad = grad_logprob;
+    a.grad_lse = grad_lse;
+    a.dhidden = dhidden;
+    a.dweight = dweight;
+    a.dx_ld = dhidden_ld;
+    a.dw_ld = dweight_ld;
+    return tt::launch_head_logprobs_backward(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+int tt_quantize_i8(int32_t n_rows, int32_t k, int32_t dtype, const void *x, int64_t x_ld, int8_t *q, int64_t q_ld, float *scale,
+                   void *stream) {
+    if (n_rows < 0 || k < 1 || !dtype_ok(dtype) || x_ld < k || q_ld < k || x_ld > INT64_MAX / 4) return TT_EINVAL;
+    if (k > kMaxI8Sum) return TT_EUNSUPPORTED;
+    if (n_rows == 0) return TT_OK;
+    const int64_t e = bytes_of(dtype);
+    const Extent in = {x, n_rows, k * e, x_ld * e}, out = {q, n_rows, k, q_ld};
+    if (!x || !q || !scale || !aligned(x, e) || !words_aligned(scale) || !extent_ok(in) || !extent_ok(out) || !apart(in, out)) return TT_EINVAL;
+    tt::QuantizeI8Args a;
+    a.n_rows = n_rows;
+    a.k = k;
+    a.dtype = dtype;
+    a.x = x;
+    a.ld = x_ld;
+    a.q = q;
+    a.q_ld = q_ld;
+    a.scale = scale;
+    return tt::launch_quantize_i8(a, static_cast<hipStream_t>(stream));
+}
+
+int tt_matmul_i8_workspace_size(int32_t n_rows, int32_t n_cols, int32_t k, int32_t with_lse, size_t *bytes) {
+    if (bytes == nullptr || n_rows < 0 || n_cols < 1 || k < 1) return TT_EINVAL;
+    if (n_rows > kMaxHeadRows || n_cols > kMaxLogitsRow || k > kMaxI8Sum) return TT_EUNSUPPORTED;
+    *bytes = n_rows == 0 ? 0 : tt::matmul_i8_workspace_bytes(n_rows, n_cols, with_lse != 0);
+    return TT_OK;
+}
+
+int tt_matmul_i8(int32_t n_rows, int32_t n_cols, int32_t k, const int8_t *x, int64_t x_ld, const float *x_scale, const int8_t *w,
+                 int64_t w_ld, const float *w_scale, const float *bias, int32_t out_dtype, void *out, int64_t out_ld,
+                 const float *inv_temperature, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    if (n_rows < 0 || n_cols < 1 || k < 1 || !dtype_ok(out_dtype) || x_ld < k || w_ld < k || out_ld < n_cols || out_ld > INT64_MAX / 4)
+        return TT_EINVAL;
+    if (n_rows > kMaxHeadRows || n_cols > kMaxLogitsRow || k > kMaxI8Sum) return TT_EUNSUPPORTED;
+    if (n_rows == 0) return TT_OK;
+    const int64_t e = bytes_of(out_dtype);
+    const Extent xe = {x, n_rows, k, x_ld}, we = {w, n_cols, k, w_ld}, oe = {out, n_rows, n_cols * e, out_ld * e};
+    if (!x || !w || !x_scale || !w_scale || !out || !aligned(out, e) || !aligned(workspace, 16) ||
+        !words_aligned(x_scale, w_scale, bias, inv_temperature, lse) || !extent_ok(xe) || !extent_ok(we) || !extent_ok(oe) || !apart(xe, oe) ||
+        !apart(we, oe))
+        return TT_EINVAL;
+    tt::MatmulI8Args a;
+    a.n_rows = n_rows;
+    a.n_cols = n_cols;
+    a.k = k;
+    a.x = x;
+    a.w = w;
+    a.x_ld = x_ld;
+    a.w_ld = w_ld;
+    a.x_scale = x_scale;
+    a.w_scale = w_scale;
+    a.bias = bias;
+    a.out_dtype = out_dtype;
+    a.out = out;
+    a.out_ld = out_ld;
+    a.inv_temp = inv_temperature;
+    a.lse = lse;
+    return tt::launch_matmul_i8(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

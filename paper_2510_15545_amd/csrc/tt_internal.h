@@ -196,6 +196,55 @@ size_t distill_workspace_bytes(int32_t n_rows, int32_t v, int dtype, int n_top, 
 size_t distill_workspace_used(int32_t n_rows, int32_t v, int dtype, int n_top, bool grad);   // of n_rows rows
 int launch_distill(const DistillArgs &a, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
+// ---------------------------------------------------------------- output head (head.hip)
+struct HeadArgs {
+    int32_t n_rows, v, h, dtype;
+    const void *hidden, *weight;
+    int64_t x_ld, w_ld;
+    const float *inv_temp;  // or null
+    const int32_t *ids;     // or null
+    float *logprob, *lse, *stats;  // each may be null
+};
+size_t head_workspace_bytes(int32_t n_rows, int32_t v, int32_t h, int dtype);
+int launch_head_logprobs(const HeadArgs &a, void *workspace, size_t workspace_bytes, hipStream_t stream);
+struct HeadGradArgs {
+    int32_t n_rows, v, h, dtype;
+    const void *hidden, *weight;
+    int64_t x_ld, w_ld;
+    const float *inv_temp;
+    const int32_t *ids;
+    const float *stats, *grad, *grad_lse;
+    void *dhidden, *dweight;  // either may be null
+    int64_t dx_ld, dw_ld;
+};
+size_t head_backward_workspace_bytes(int32_t n_rows, int32_t v, int32_t h, int dtype);  // of up to n_rows rows
+size_t head_backward_workspace_used(int32_t n_rows, int32_t v, int32_t h, int dtype);   // of n_rows rows
+int launch_head_logprobs_backward(const HeadGradArgs &a, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+// ---------------------------------------------------------------- 8-bit integers (i8.hip)
+struct QuantizeI8Args {
+    int32_t n_rows, k, dtype;
+    const void *x;
+    int64_t ld;
+    int8_t *q;
+    int64_t q_ld;
+    float *scale;
+};
+int launch_quantize_i8(const QuantizeI8Args &a, hipStream_t stream);
+struct MatmulI8Args {
+    int32_t n_rows, n_cols, k;
+    const int8_t *x, *w;
+    int64_t x_ld, w_ld;
+    const float *x_scale, *w_scale, *bias;  // bias may be null
+    int32_t out_dtype;
+    void *out;
+    int64_t out_ld;
+    const float *inv_temp;
+    float *lse;  // or null
+};
+size_t matmul_i8_workspace_bytes(int32_t n_rows, int32_t n_cols, bool lse);
+int launch_matmul_i8(const MatmulI8Args &a, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
 // ---------------------------------------------------------------- fused step (step.hip)
 struct StepArgs {
     AlignArgs al;     // alignment inputs and outputs
