@@ -607,8 +607,8 @@ int tt_distill(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int
 /*
  * The output head.  The calls below take hidden states (n_rows rows of h elements at a stride of hidden_ld) and the head's
  * weights (v rows of h elements at a stride of weight_ld), both in bf16, fp16 or fp32 and aligned to their elements, and
- * form the logits x_ij = sum_k hidden_ik weight_jk themselves, a tile at a time: none is kept.  Products are exact and
- * summed in fp32 (fp32 operands as three bf16 parts each, to 2^-24 of every product).  M, S, L, lse, lp_j and p_j are as
+ * form the logits x_ij = sum_k hidden_ik weight_jk themselves, a tile at a time: none is kept.  Sums are fp32, and so are the
+ * products of fp32 operands; those of 16-bit ones are exact.  M, S, L, lse, lp_j and p_j are as
  * above, but a logit that is NaN makes its row's results NaN (here it is the outcome of a sum, not a mask).
  * n_rows <= 2^20, v <= 2^23, h <= 2^16.
  *
@@ -636,8 +636,7 @@ int tt_head_logprobs(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, const 
  *                rounded once to nearest even; elements past h in a row are left alone.  They must meet neither the
  *                operands nor each other.
  * A row with g = w = 0, or with M minus infinity, gets zeros, adds nothing to dweight and is not read (NaN in it is harmless).
- * The logits are formed again, a piece of the vocabulary at a time; dx is rounded to the operands' type (fp32: three bf16
- * parts) relative to the largest beta (|g| + |w|) of the rows before it is multiplied: in fp16 a row whose weight is below
+ * The logits are formed again, a piece of the vocabulary at a time; dx is rounded to the operands' type relative to the largest beta (|g| + |w|) of the rows before it is multiplied: in fp16 a row whose weight is below
  * 2^-20 of the largest loses digits.  Sums are fp32, without atomics.  With n_rows = 0 dweight is zeros.
  * workspace: tt_head_logprobs_backward_workspace_size bytes serve every call of up to n_rows rows, a call uses
  * ..._workspace_used bytes.  Errors and workspaces as for tt_head_logprobs, and TT_EINVAL for gradients that meet something.

@@ -5,11 +5,11 @@
 //   dz_j = beta (g ([j = t] - p_j) + q p_j),  dx = dz W,  dW = dz^T x
 //
 // Forward: one product by tiles (tiles.h), whose epilogue leaves each tile's largest logit and sum of exponentials for
-// every row, and a second kernel that joins a row's parts.  Backward: the rows that carry a weight are gathered, with
-// their transpose; then, for one piece of the vocabulary after another, the product again with an epilogue that makes dz of
-// it, rounded to the operands' type (relative to the largest row weight, so that a small weight costs no digits), and two more
-// products: dx += dz W (in fp32, over all pieces) and the piece's rows of dW, written once.  No atomics: results do not
-// depend on scheduling.  fp32 operands are held as three bf16 parts and multiplied in six products (tiles.h).
+// every row, and a second kernel that joins a row's parts.  Backward: the rows that carry a weight are gathered; then, for
+// one piece of the vocabulary after another, the product again with an epilogue that makes dz of it, rounded to the operands'
+// type (relative to the largest row weight, so that a small weight costs no digits), and two more products: dx += dz W (in
+// fp32, over all pieces) and the piece's rows of dW, written once.  Of these three products' operands dz, W and x each is kept
+// as it is, whichever of its indices is summed over (tiles.h).  No atomics: results do not depend on scheduling.
 #include <algorithm>
 
 #include "tiles.h"
@@ -20,19 +20,19 @@ namespace {
 using namespace tiles;
 using rows::round256;
 
-constexpr int kTile = 128;      // rows of either side in a tile
-constexpr int kAlign = 256;     // rows, tokens and pieces of the vocabulary in a workspace come in multiples of this
-constexpr int kStepElements = kStepBytes / 2;
-typedef Shape<kTile, kTile, 2, 2> Tile;
+constexpr int kTile = 256;   // tokens (or hidden elements) of a wide tile
+constexpr int kAlign = 256;  // rows, tokens and pieces of the vocabulary in a workspace come in multiples of this
+typedef Shape<128, 128, 2, 2> Any;  // of the products of matrices that lie in any way
 
-constexpr int64_t kSplitTiles = 768;  // workgroups that the sum over a piece's tokens is split into at most
-constexpr size_t kPieceBytes = size_t(192) << 20;  // what the pieces of the vocabulary may take of the workspace
+constexpr int64_t kSplitTiles = 256;  // workgroups that the sum over a piece's tokens is split into at most
+constexpr int64_t kPieceBytes = int64_t(160) << 20;  // what a piece of the vocabulary may take of the workspace
+constexpr int kRowsPerLaunch = 1 << 15;
 
-__host__ __device__ constexpr int parts_of(int dtype) { return dtype == TT_F32 ? kParts : 1; }
 __host__ __device__ inline int64_t round_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
-// The type that the matrix cores are given.
-template <int DT>
-constexpr int kCore = DT == TT_F32 ? TT_BF16 : DT;
+__host__ __device__ constexpr int step_elements(int dtype) { return kStepBytes / bytes_of(dtype); }
+inline int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
+// Rows to a tile of a wide product, in units of 64.
+inline int columns_for(int64_t n, int dtype) { return n <= 128 || dtype == TT_F32 ? 2 : 4; }
 
 // A row that carries a weight, for the gradient's epilogue: p = 2^((z - m) c - l), dz = (w - g) p, and g (1 - p) + w p at
 // its token; padding rows are zeros.
@@ -45,69 +45,72 @@ struct Totals {
     float scale;   // of the stored dz: the true one is scale times as large
 };
 
-// ------------------------------------------------------------------------------------------------ copies into parts
-// A matrix's elements [r0, r0 + n_rows) x [0, cols) in the parts' layout: `out` [parts][out_rows][out_cols], rounded up with
-// zeros, and its transpose `out_t` [parts][out_cols][out_rows], either of which may be null.  list: rows by their index
-// in it, totals->rows of them (rounded up to a tile are written), or null.
-template <int DT>
-__global__ __launch_bounds__(256) void lay_out(const void *src, int64_t ld, int n_rows, int cols, const int32_t *list, const Totals *totals,
-                                               uint16_t *out, int64_t out_ld, int64_t out_plane, uint16_t *out_t, int64_t t_ld, int64_t t_plane) {
-    constexpr int P = parts_of(DT);
-    __shared__ uint16_t block[P][64][66];
-    using T = typename rows::Elem<DT>::T;
-    const int r0 = (int)blockIdx.x * 64, c0 = (int)blockIdx.y * 64;
-    const int count = totals ? totals->rows : n_rows;
-    if (totals && r0 >= round_to(count, kTile)) return;
-    const T *in = static_cast<const T *>(src);
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-        const int r = i * 4 + (int)threadIdx.x / 64, c = (int)threadIdx.x % 64;
-        uint32_t part[kParts] = {0, 0, 0};
-        if (r0 + r < count && c0 + c < cols) {
-            const int64_t row = list ? list[r0 + r] : r0 + r;
-            const T x = in[row * ld + c0 + c];
-            if constexpr (DT == TT_F32) split(__uint_as_float(x), part);
-            else part[0] = x;
-        }
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            block[p][r][c] = (uint16_t)part[p];
-            if (out) out[p * out_plane + (int64_t)(r0 + r) * out_ld + c0 + c] = (uint16_t)part[p];
-        }
+// ------------------------------------------------------------------------------------------------ copies
+// Rows of `bytes` bytes at any address, at a stride of `ld` bytes, into rows of `out_bytes` (a multiple of 16), filled up with zeros.
+// list: the rows by their index in it, totals->rows of them, rounded up with rows of zeros; or null.
+__global__ __launch_bounds__(256) void lay_out(const char *src, int64_t ld, int n_rows, int bytes, const int32_t *list, const Totals *totals,
+                                               char *out, int out_bytes) {
+    const int count = totals ? totals->rows : n_rows, pieces = out_bytes / 16;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r = i / pieces;
+    const int c = (int)(i % pieces) * 16;
+    if (r >= (totals ? round_to(count, kAlign) : n_rows)) return;
+    u4 v = {0, 0, 0, 0};
+    if (r < count && c < bytes) {
+        const char *q = src + (list ? (int64_t)list[r] : r) * ld + c;
+        v = c + 16 <= bytes ? (u4)*reinterpret_cast<const u4b *>(q) : load_some(q, bytes - c);
     }
-    if (!out_t) return;
-    __syncthreads();
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-        const int c = i * 4 + (int)threadIdx.x / 64, r = (int)threadIdx.x % 64;
-#pragma unroll
-        for (int p = 0; p < P; ++p) out_t[p * t_plane + (int64_t)(c0 + c) * t_ld + r0 + r] = block[p][r][c];
-    }
+    *reinterpret_cast<u4 *>(out + r * out_bytes + c) = v;
 }
 
 // ------------------------------------------------------------------------------------------------ forward
-// Parts of the rows' distributions from the tokens [v0 + 128 tile, + 128), and the given tokens' logits.
-template <int DT, int PASSES>
-__global__ __launch_bounds__(Tile::THREADS) void head_parts(Side w, Side x, int64_t bytes, int v0, const float *inv_temp, const int32_t *ids,
-                                                            Part *parts, int tile0, int n_tiles, float *token) {
-    __shared__ __attribute__((aligned(16))) char lds[Tile::LDS];
-    f4 acc[Tile::FM][Tile::FN];
-    const int m0 = (int)blockIdx.x * kTile, n0 = (int)blockIdx.y * kTile;
-    product<DT, Tile, PASSES>(w, x, m0, n0, 0, bytes, bytes, lds, acc);
-    const int n_rows = x.rows, lane = (int)threadIdx.x & 63, wm = ((int)threadIdx.x >> 6) % Tile::WM;
-    const int base = m0 + wm * Tile::FM * 16 + (lane >> 4) * 4;
+// Parts of the rows' distributions from a tile's tokens, and the given tokens' logits.
+template <int DT, typename S>
+__device__ __forceinline__ void parts_of_tile(const Side &w, const Side &x, int m0, int n0, f4 (&acc)[S::FM][S::FN], const float *inv_temp,
+                                              const int32_t *ids, Part *parts, int n_tiles, float *token, char *lds) {
+    const int n_rows = x.rows;
     if (ids)
-        for_blocks<Tile>(m0, n0, [&](int m, int n, int i, int j) {
-            const int at = n < n_rows ? ids[n] - v0 - m : -1;
+        for_columns<S>(n0, [&](int n, int j) {
+            const int at = n < n_rows ? ids[n] : -1;
+            if (at < w.rows)
+                for_rows<S>(m0, [&](int m, int i) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (at == q && m + q < w.rows) token[n] = acc[i][j][q];
+                    for (int q = 0; q < 4; ++q)
+                        if (at == m + q) token[n] = acc[i][j][q];
+                });
         });
-    const Part p = column_parts<Tile>(
-        n0, lds, [&](int i, int j, int q) { return base + i * 16 + q < w.rows ? acc[i][j][q] : -INFINITY; },
+    if (m0 + S::TM > w.rows)
+        for_columns<S>(n0, [&](int, int j) {
+            for_rows<S>(m0, [&](int m, int i) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (m + q >= w.rows) acc[i][j][q] = -INFINITY;
+            });
+        });
+    const Part p = column_parts<S>(
+        n0, lds, [&](int i, int j, int q) { return acc[i][j][q]; },
         [&](int n) { return (n < n_rows ? rows::scale_of(inv_temp, n) : 1.0f) * rows::kLog2e; });
     const int n = n0 + (int)threadIdx.x;
-    if ((int)threadIdx.x < kTile && n < n_rows) parts[(int64_t)n * n_tiles + tile0 + blockIdx.x] = p;
+    if ((int)threadIdx.x < S::TN && n < n_rows) parts[(int64_t)n * n_tiles + m0 / S::TM] = p;
+}
+
+template <int DT, int FN>
+__global__ __launch_bounds__(512) void head_parts(Side w, Side x, int mt, int nt, const float *inv_temp, const int32_t *ids, Part *parts, float *token) {
+    TT_WIDE_LDS(FN);
+    f4 acc[8][FN];
+    int m, n;
+    tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m, n);
+    Product<DT, false, false, FN>::run(w, x, m * 256, n * 64 * FN, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
+    parts_of_tile<DT, Wide<FN>>(w, x, m * 256, n * 64 * FN, acc, inv_temp, ids, parts, mt, token, a0);
+}
+
+template <int DT>
+__global__ __launch_bounds__(Any::THREADS) void head_parts_any(Side w, Side x, const float *inv_temp, const int32_t *ids, Part *parts, float *token) {
+    __shared__ __attribute__((aligned(16))) char lds[Any::LDS];
+    f4 acc[Any::FM][Any::FN];
+    const int m0 = (int)blockIdx.x * Any::TM, n0 = (int)blockIdx.y * Any::TN;
+    product_any<DT, Any>(w, x, m0, n0, lds, acc);
+    parts_of_tile<DT, Any>(w, x, m0, n0, acc, inv_temp, ids, parts, gridDim.x, token, lds);
 }
 
 // A wave a row.
@@ -187,56 +190,72 @@ __global__ __launch_bounds__(1024) void head_select(int n, int v, const float *i
     if (t == 0) *totals = {before, top / store_scale};
 }
 
-// dz of the piece's tokens [128 tile, + 128) for the listed rows, stored as [n][token] and [token][n].
-template <int DT>
-__global__ __launch_bounds__(Tile::THREADS) void head_dlogits(Side w, Side x, int64_t bytes, int v0, const Row *meta, const Totals *totals,
-                                                              uint16_t *d, int64_t d_ld, int64_t d_plane, uint16_t *dt, int64_t dt_ld,
-                                                              int64_t dt_plane) {
-    constexpr int P = parts_of(DT);
-    __shared__ __attribute__((aligned(16))) char lds[Tile::LDS];
-    f4 acc[Tile::FM][Tile::FN];
-    const int m0 = (int)blockIdx.x * kTile, n0 = (int)blockIdx.y * kTile;
+// dz of a piece's tokens (the first of them v0) for the listed rows, stored as [row][token].
+template <int DT, int FN>
+__global__ __launch_bounds__(512) void head_dlogits(Side w, Side x, int mt, int nt, int v0, const Row *meta, const Totals *totals, char *d, int64_t d_ld) {
+    TT_WIDE_LDS(FN);
+    using T = typename rows::Elem<DT>::T;
+    typedef Wide<FN> S;
+    f4 acc[8][FN];
+    int m0, n0;
+    tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m0, n0);
+    m0 *= S::TM;
+    n0 *= S::TN;
     if (n0 >= totals->rows) return;
-    product<kCore<DT>, Tile, P == 1 ? 1 : kPasses>(w, x, m0, n0, 0, bytes, bytes, lds, acc);
-    for_blocks<Tile>(m0, n0, [&](int m, int n, int i, int j) {
+    Product<DT, false, false, FN>::run(w, x, m0, n0, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
+    for_columns<S>(n0, [&](int n, int j) {
         const Row r = meta[n];
-        uint32_t part[4][kParts];
+        T *row = reinterpret_cast<T *>(d) + (int64_t)n * d_ld;
+        const int id = r.id - v0;
+        const float f = r.w - r.g;
+        // the exponential's argument; at the row's token what is left of 1 beside p, not 1 - p
+        const auto exponent = [&](float z) { return fmaf(z - r.m, r.c, -r.l); };
+        if (__any(id >= m0 && id < m0 + S::TM) || m0 + S::TM > w.rows) {
+            for_rows<S>(m0, [&](int m, int i) {
+                float y[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float y = fmaf(acc[i][j][q] - r.m, r.c, -r.l), p = __builtin_amdgcn_exp2f(y);
-            float g = (r.w - r.g) * p;
-            if (v0 + m + q == r.id) g = r.g * -expm1f(y * (float)rows::kLn2) + r.w * p;
-            if (m + q >= w.rows) g = 0.0f;
-            if constexpr (DT == TT_F32) split(g, part[q]);
-            else part[q][0] = rows::encode<DT>(g);
-        }
+                for (int q = 0; q < 4; ++q) {
+                    const float e = exponent(acc[i][j][q]), p = __builtin_amdgcn_exp2f(e);
+                    y[q] = f * p;
+                    if (m + q == id) y[q] = r.g * -expm1f(e * (float)rows::kLn2) + r.w * p;
+                    if (m + q >= w.rows) y[q] = 0.0f;
+                }
+                store4<DT>(row, m, (int)d_ld, y);
+            });
+        } else {
+            for_rows<S>(m0, [&](int m, int i) {
+                float y[4];
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-            typedef unsigned int u2 __attribute__((ext_vector_type(2)));
-            if (d) *reinterpret_cast<u2 *>(d + k * d_plane + (int64_t)n * d_ld + m) = u2{part[0][k] | part[1][k] << 16, part[2][k] | part[3][k] << 16};
-            if (dt)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) dt[k * dt_plane + (int64_t)(m + q) * dt_ld + n] = (uint16_t)part[q][k];
+                for (int q = 0; q < 4; ++q) y[q] = f * __builtin_amdgcn_exp2f(exponent(acc[i][j][q]));
+                store4<DT>(row, m, (int)d_ld, y);
+            });
         }
     });
 }
 
 // dx of the listed rows over one piece of the vocabulary, split into parts of its tokens, added to what the pieces before
-// gave: sums[split][n][h] in fp32.
-template <int DT>
-__global__ __launch_bounds__(Tile::THREADS) void head_dhidden(Side wt, Side d, int64_t bytes, int64_t split_bytes, const Totals *totals,
-                                                              float *sums, int64_t ld, int64_t plane, int first) {
-    __shared__ __attribute__((aligned(16))) char lds[Tile::LDS];
-    f4 acc[Tile::FM][Tile::FN];
-    const int m0 = (int)blockIdx.x * kTile, n0 = (int)blockIdx.y * kTile;
+// gave: sums[split][row][h] in fp32.
+template <int DT, int FN>
+__global__ __launch_bounds__(512) void head_dhidden(Side w, Side d, int mt, int nt, int split_steps, const Totals *totals, float *sums, int64_t ld,
+                                                    int64_t plane, int first) {
+    TT_WIDE_LDS(FN);
+    typedef Wide<FN> S;
+    f4 acc[8][FN];
+    const int split = (int)blockIdx.x / (mt * nt);
+    int m0, n0;
+    tile_of((int)blockIdx.x % (mt * nt), mt * nt, mt, nt, m0, n0);
+    m0 *= S::TM;
+    n0 *= S::TN;
     if (n0 >= totals->rows) return;
-    const int64_t k0 = (int64_t)blockIdx.z * split_bytes, k1 = k0 + split_bytes < bytes ? k0 + split_bytes : bytes;
-    product<kCore<DT>, Tile, DT == TT_F32 ? kPasses : 1>(wt, d, m0, n0, k0, k1, bytes, lds, acc);
-    float *out = sums + blockIdx.z * plane;
-    for_blocks<Tile>(m0, n0, [&](int m, int n, int i, int j) {
-        if (m >= ld) return;
-        f4 *to = reinterpret_cast<f4 *>(out + (int64_t)n * ld + m);
-        *to = first ? acc[i][j] : *to + acc[i][j];
+    const int steps = (w.rows + step_elements(DT) - 1) / step_elements(DT), from = split * split_steps;
+    Product<DT, true, false, FN>::run(w, d, m0, n0, from, min(split_steps, steps - from), a0, a1, b0, b1, acc);
+    for_columns<S>(n0, [&](int n, int j) {
+        float *out = sums + split * plane + (int64_t)n * ld;
+        for_rows<S>(m0, [&](int m, int i) {
+            if (m >= ld) return;
+            f4 *to = reinterpret_cast<f4 *>(out + m);
+            *to = first ? acc[i][j] : *to + acc[i][j];
+        });
     });
 }
 
@@ -257,26 +276,32 @@ __global__ __launch_bounds__(256) void head_place(const float *sums, int64_t ld,
 }
 
 // A piece's rows of dW.
-template <int DT>
-__global__ __launch_bounds__(Tile::THREADS) void head_dweight(Side xt, Side dt, const Totals *totals, int h, void *dweight, int64_t ld) {
-    __shared__ __attribute__((aligned(16))) char lds[Tile::LDS];
-    f4 acc[Tile::FM][Tile::FN];
-    const int m0 = (int)blockIdx.x * kTile, n0 = (int)blockIdx.y * kTile;
-    const int64_t bytes = round_to(totals->rows, kStepElements) * 2;
-    product<kCore<DT>, Tile, DT == TT_F32 ? kPasses : 1>(xt, dt, m0, n0, 0, bytes, bytes, lds, acc);
+template <int DT, int FN>
+__global__ __launch_bounds__(512) void head_dweight(Side x, Side d, int mt, int nt, const Totals *totals, int n_tokens, int h, void *dweight, int64_t ld) {
+    TT_WIDE_LDS(FN);
+    using T = typename rows::Elem<DT>::T;
+    typedef Wide<FN> S;
+    f4 acc[8][FN];
+    int m0, n0;
+    tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m0, n0);
+    m0 *= S::TM;
+    n0 *= S::TN;
+    const int steps = (totals->rows + step_elements(DT) - 1) / step_elements(DT);
+    Product<DT, true, true, FN>::run(x, d, m0, n0, 0, steps, a0, a1, b0, b1, acc);
     const float scale = totals->scale;
-    for_blocks<Tile>(m0, n0, [&](int m, int n, int i, int j) {
-        if (n >= dt.rows) return;
-        const float y[4] = {acc[i][j][0] * scale, acc[i][j][1] * scale, acc[i][j][2] * scale, acc[i][j][3] * scale};
-        store4<DT>(static_cast<typename rows::Elem<DT>::T *>(dweight) + (int64_t)n * ld, m, h, y);
+    for_columns<S>(n0, [&](int n, int j) {
+        if (n >= n_tokens) return;
+        T *row = static_cast<T *>(dweight) + (int64_t)n * ld;
+        for_rows<S>(m0, [&](int m, int i) {
+            const float y[4] = {acc[i][j][0] * scale, acc[i][j][1] * scale, acc[i][j][2] * scale, acc[i][j][3] * scale};
+            store4<DT>(row, m, h, y);
+        });
     });
 }
 
 __global__ __launch_bounds__(256) void head_zero(int h, int e, char *out, int64_t ld) {
     for (int64_t c = threadIdx.x; c < (int64_t)h * e; c += 256) out[blockIdx.x * ld * e + c] = 0;
 }
-
-unsigned int tiles_of(int64_t n) { return (unsigned int)((n + kTile - 1) / kTile); }
 
 // ------------------------------------------------------------------------------------------------ workspaces
 struct Layout {
@@ -289,144 +314,158 @@ struct Layout {
 };
 
 struct ForwardLayout : Layout {
-    int64_t piece;  // tokens of a piece (fp32: the weights' parts are made piece by piece)
-    int64_t width;  // of a row of parts
-    int n_tiles;
-    size_t parts, token, x, w;
-    ForwardLayout(int64_t n, int64_t v, int64_t h, int dtype) {
-        n_tiles = (int)tiles_of(v);
-        width = round_to(h, kStepElements);
-        piece = v;
-        parts = take((size_t)n * n_tiles * sizeof(Part));
+    size_t parts, token;
+    ForwardLayout(int64_t n, int64_t v) {
+        parts = take((size_t)(n * tiles_of(v, Any::TM)) * sizeof(Part));
         token = take((size_t)n * 4);
-        x = w = 0;
-        if (dtype == TT_F32) {
-            const int64_t most = (int64_t)(kPieceBytes / (size_t)(kParts * width * 2));
-            piece = std::min(round_to(v, kAlign), std::max<int64_t>(kAlign, most / kAlign * kAlign));
-            x = take((size_t)(kParts * round_to(n, kAlign) * width * 2));
-            w = take((size_t)(kParts * piece * width * 2));
-        }
     }
 };
 
 struct BackwardLayout : Layout {
-    int64_t n_pad, width, piece;
+    int64_t n_pad, width, piece;  // width: elements of a hidden state in a copy
     int splits;
-    size_t totals, place, list, meta, x, xt, w, wt, d, dt, sums;
-    // most: what no number of rows up to n takes more than (fewer rows make longer pieces and more splits)
-    BackwardLayout(int64_t n, int64_t v, int64_t h, int dtype, bool most = false) {
-        const int64_t p = parts_of(dtype);
+    size_t totals, place, list, meta, x, w, d, sums;
+    BackwardLayout(int64_t n, int64_t v, int64_t h, int dtype) {
+        const int64_t e = rows::element_bytes(dtype), all = round_to(v, kAlign);
         n_pad = round_to(n, kAlign);
-        width = round_to(h, kStepElements);
-        const int64_t row = p * (2 * n_pad + (dtype == TT_F32 ? 2 : 1) * width) * 2, all = round_to(v, kAlign);
-        const int64_t fit = most ? ((int64_t)kPieceBytes + row - 1) / row : (int64_t)kPieceBytes / row / kAlign * kAlign;
-        piece = std::min(all, std::max<int64_t>(kAlign, fit));
-        const int64_t tiles = (int64_t)tiles_of(n_pad) * tiles_of(width);
-        splits = (int)std::min<int64_t>(std::max<int64_t>(1, most ? (kSplitTiles + tiles - 1) / tiles : kSplitTiles / tiles), std::max<int64_t>(1, all / 1024));
+        width = round_to(h, step_elements(dtype));
+        const int64_t row = (n_pad + width) * e;  // of dz and of the weights' copy, for a token
+        piece = std::min(all, std::max<int64_t>(kAlign, kPieceBytes / row / kAlign * kAlign));
+        splits = (int)std::min<int64_t>(std::max<int64_t>(1, kSplitTiles / (row_tiles(n, dtype) * tiles_of(width, kTile))), std::max<int64_t>(1, all / 1024));
+        rows_of(n, e);
+        d = take((size_t)(piece * n_pad * e));
+        w = take((size_t)(piece * width * e));
+        sums = take((size_t)(splits * n_pad * width * 4));
+    }
+    // What no number of rows up to n takes more than (fewer rows make longer pieces and more splits).
+    static size_t most(int64_t n, int64_t v, int64_t h, int dtype) {
+        BackwardLayout l;
+        const int64_t e = rows::element_bytes(dtype);
+        l.n_pad = round_to(n, kAlign);
+        l.width = round_to(h, step_elements(dtype));
+        l.rows_of(n, e);
+        const int64_t row = (l.n_pad + l.width) * e;
+        l.take((size_t)std::min(round_to(v, kAlign) * row, std::max(kAlign * row, kPieceBytes)) + 256);
+        l.take((size_t)(std::max(kSplitTiles / tiles_of(l.width, kTile), row_tiles(n, dtype)) * kAlign * l.width * 4));
+        return l.total;
+    }
+
+  private:
+    BackwardLayout() {}
+    static int64_t row_tiles(int64_t n, int dtype) { return tiles_of(n, 64 * columns_for(n, dtype)); }
+    void rows_of(int64_t n, int64_t e) {
         totals = take(sizeof(Totals));
         place = take((size_t)n * 4);
         list = take((size_t)n * 4);
         meta = take((size_t)n_pad * sizeof(Row));
-        x = take((size_t)(p * n_pad * width * 2));
-        xt = take((size_t)(p * n_pad * width * 2));
-        w = dtype == TT_F32 ? take((size_t)(p * piece * width * 2)) : 0;
-        wt = take((size_t)(p * piece * width * 2));
-        d = take((size_t)(p * piece * n_pad * 2));
-        dt = take((size_t)(p * piece * n_pad * 2));
-        sums = take((size_t)(splits * n_pad * width * 4));
+        x = take((size_t)(n_pad * width * e));
     }
 };
 
 int status() { return hipGetLastError() == hipSuccess ? TT_OK : TT_ELAUNCH; }
 
+Side matrix(const void *p, int64_t ld, int64_t n, int64_t width, int64_t e) { return {static_cast<const char *>(p), ld * e, (int)n, (int)(width * e)}; }
+
+void copy_rows(const void *src, int64_t ld, int64_t n_rows, int64_t width, int64_t e, const int32_t *list, const Totals *totals, char *out,
+               int64_t out_width, hipStream_t stream) {
+    const int64_t pieces = (totals ? round_to(n_rows, kAlign) : n_rows) * out_width * e / 16;
+    lay_out<<<(unsigned int)((pieces + 255) / 256), 256, 0, stream>>>(static_cast<const char *>(src), ld * e, (int)n_rows, (int)(width * e), list, totals,
+                                                                  out, (int)(out_width * e));
+}
+
 template <int DT>
 int forward(const HeadArgs &a, char *ws, hipStream_t stream) {
-    const ForwardLayout lay(a.n_rows, a.v, a.h, a.dtype);
+    const ForwardLayout lay(a.n_rows, a.v);
     const int64_t e = rows::element_bytes(DT);
     Part *parts = reinterpret_cast<Part *>(ws + lay.parts);
     float *token = reinterpret_cast<float *>(ws + lay.token);
     const int32_t *ids = a.logprob ? a.ids : nullptr;
-    if constexpr (DT != TT_F32) {
-        const Side w = {static_cast<const char *>(a.weight), a.w_ld * e, 0, a.v}, x = {static_cast<const char *>(a.hidden), a.x_ld * e, 0, a.n_rows};
-        head_parts<DT, 1><<<dim3(tiles_of(a.v), tiles_of(a.n_rows)), Tile::THREADS, 0, stream>>>(w, x, a.h * e, 0, a.inv_temp, ids, parts, 0,
-                                                                                              lay.n_tiles, token);
-    } else {
-        uint16_t *xp = reinterpret_cast<uint16_t *>(ws + lay.x), *wp = reinterpret_cast<uint16_t *>(ws + lay.w);
-        const int64_t x_plane = round_to(a.n_rows, kAlign) * lay.width, w_plane = lay.piece * lay.width;
-        const unsigned int wide = (unsigned int)(lay.width / 64);
-        lay_out<DT><<<dim3((unsigned int)(round_to(a.n_rows, 64) / 64), wide), 256, 0, stream>>>(a.hidden, a.x_ld, a.n_rows, a.h, nullptr, nullptr, xp,
-                                                                                             lay.width, x_plane, nullptr, 0, 0);
-        for (int64_t v0 = 0; v0 < a.v; v0 += lay.piece) {
-            const int here = (int)std::min<int64_t>(lay.piece, a.v - v0);
-            lay_out<DT><<<dim3((unsigned int)(round_to(here, 64) / 64), wide), 256, 0, stream>>>(
-                static_cast<const float *>(a.weight) + v0 * a.w_ld, a.w_ld, here, a.h, nullptr, nullptr, wp, lay.width, w_plane, nullptr, 0, 0);
-            const Side w = {reinterpret_cast<const char *>(wp), lay.width * 2, w_plane * 2, here};
-            const Side x = {reinterpret_cast<const char *>(xp), lay.width * 2, x_plane * 2, a.n_rows};
-            head_parts<TT_BF16, kPasses><<<dim3(tiles_of(here), tiles_of(a.n_rows)), Tile::THREADS, 0, stream>>>(
-                w, x, lay.width * 2, (int)v0, a.inv_temp, ids, parts, (int)(v0 / kTile), lay.n_tiles, token);
+    const Side w = matrix(a.weight, a.w_ld, a.v, a.h, e);
+    int n_tiles = (int)tiles_of(a.v, kTile);
+    if (whole_steps(w) && whole_steps(matrix(a.hidden, a.x_ld, a.n_rows, a.h, e))) {
+        for (int64_t n0 = 0; n0 < a.n_rows; n0 += kRowsPerLaunch) {
+            const int64_t n = std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0);
+            const Side x = matrix(static_cast<const char *>(a.hidden) + n0 * a.x_ld * e, a.x_ld, n, a.h, e);
+            const int fn = columns_for(n, DT), nt = (int)tiles_of(n, 64 * fn);
+            const auto run = [&](auto kernel) {
+                kernel<<<(unsigned int)(n_tiles * nt), 512, 0, stream>>>(w, x, n_tiles, nt, a.inv_temp ? a.inv_temp + n0 : nullptr, ids ? ids + n0 : nullptr,
+                                                                      parts + n0 * n_tiles, token + n0);
+            };
+            if constexpr (DT == TT_F32) run(head_parts<DT, 2>);
+            else if (fn == 2) run(head_parts<DT, 2>);
+            else run(head_parts<DT, 4>);
         }
+    } else {
+        n_tiles = (int)tiles_of(a.v, Any::TM);
+        const Side x = matrix(a.hidden, a.x_ld, a.n_rows, a.h, e);
+        head_parts_any<DT><<<dim3(n_tiles, (unsigned int)tiles_of(a.n_rows, Any::TN)), Any::THREADS, 0, stream>>>(w, x, a.inv_temp, ids, parts, token);
     }
-    head_join<<<(unsigned int)((a.n_rows + 3) / 4), 256, 0, stream>>>(parts, lay.n_tiles, a.n_rows, a.v, a.inv_temp, a.ids, token, a.logprob, a.lse,
-                                                                   a.stats);
+    head_join<<<(unsigned int)((a.n_rows + 3) / 4), 256, 0, stream>>>(parts, n_tiles, a.n_rows, a.v, a.inv_temp, a.ids, token, a.logprob, a.lse, a.stats);
     return status();
+}
+
+// Whether the gradient's products need a copy of the weights' rows.
+bool copies_weight(const HeadGradArgs &a) {
+    const Side w = matrix(a.weight, a.w_ld, a.v, a.h, rows::element_bytes(a.dtype));
+    return !whole_steps(w);
+}
+
+template <int DT, int FN>
+void backward_piece(const HeadGradArgs &a, const BackwardLayout &lay, char *ws, int64_t v0, bool copy_w, hipStream_t stream) {
+    const int64_t e = rows::element_bytes(DT), here = std::min<int64_t>(lay.piece, a.v - v0);
+    const Totals *totals = reinterpret_cast<Totals *>(ws + lay.totals);
+    const char *weight = static_cast<const char *>(a.weight) + v0 * a.w_ld * e;
+    Side w = matrix(weight, a.w_ld, here, a.h, e);
+    if (copy_w) {
+        copy_rows(weight, a.w_ld, here, a.h, e, nullptr, nullptr, ws + lay.w, lay.width, stream);
+        w = matrix(ws + lay.w, lay.width, here, lay.width, e);
+    }
+    const Side x = matrix(ws + lay.x, lay.width, lay.n_pad, lay.width, e), d = matrix(ws + lay.d, lay.piece, lay.n_pad, lay.piece, e);
+    const int mt = (int)tiles_of(here, kTile), nt = (int)tiles_of(a.n_rows, 64 * FN), ht = (int)tiles_of(a.h, kTile);
+    head_dlogits<DT, FN><<<mt * nt, 512, 0, stream>>>(w, x, mt, nt, (int)v0, reinterpret_cast<const Row *>(ws + lay.meta), totals, ws + lay.d, lay.piece);
+    if (a.dhidden) {
+        const int steps = (int)tiles_of(here, step_elements(DT)), split = (int)tiles_of(steps, lay.splits);
+        head_dhidden<DT, FN><<<ht * nt * lay.splits, 512, 0, stream>>>(w, d, ht, nt, split, totals, reinterpret_cast<float *>(ws + lay.sums), lay.width,
+                                                                    lay.n_pad * lay.width, v0 == 0);
+    }
+    if (a.dweight) {
+        constexpr int VN = DT == TT_F32 ? 2 : 4;
+        const int vt = (int)tiles_of(here, 64 * VN);
+        head_dweight<DT, VN><<<ht * vt, 512, 0, stream>>>(x, d, ht, vt, totals, (int)here, a.h, static_cast<char *>(a.dweight) + v0 * a.dw_ld * e, a.dw_ld);
+    }
 }
 
 template <int DT>
 int backward(const HeadGradArgs &a, char *ws, hipStream_t stream) {
+    const bool copy_w = copies_weight(a);
     const BackwardLayout lay(a.n_rows, a.v, a.h, a.dtype);
     const int64_t e = rows::element_bytes(DT);
     Totals *totals = reinterpret_cast<Totals *>(ws + lay.totals);
     int32_t *place = reinterpret_cast<int32_t *>(ws + lay.place), *list = reinterpret_cast<int32_t *>(ws + lay.list);
-    Row *meta = reinterpret_cast<Row *>(ws + lay.meta);
-    const auto part = [&](size_t at) { return reinterpret_cast<uint16_t *>(ws + at); };
-    uint16_t *x = part(lay.x), *xt = part(lay.xt), *wp = part(lay.w), *wt = part(lay.wt), *d = part(lay.d), *dt = part(lay.dt);
-    float *sums = reinterpret_cast<float *>(ws + lay.sums);
-    const int64_t x_plane = lay.n_pad * lay.width, w_plane = lay.piece * lay.width, d_plane = lay.piece * lay.n_pad;
-    const unsigned int wide = (unsigned int)(lay.width / 64);
-    head_select<<<1, 1024, 0, stream>>>(a.n_rows, a.v, a.inv_temp, a.ids, a.stats, a.grad, a.grad_lse, DT == TT_F16 ? 0x1p14f : 1.0f, place, list, meta,
-                                        totals);
-    lay_out<DT><<<dim3((unsigned int)(lay.n_pad / 64), wide), 256, 0, stream>>>(a.hidden, a.x_ld, a.n_rows, a.h, list, totals, x, lay.width, x_plane,
-                                                                             a.dweight ? xt : nullptr, lay.n_pad, x_plane);
-    const Side xs = {reinterpret_cast<const char *>(x), lay.width * 2, x_plane * 2, (int)lay.n_pad};
-    const Side xts = {reinterpret_cast<const char *>(xt), lay.n_pad * 2, x_plane * 2, (int)lay.width};
+    head_select<<<1, 1024, 0, stream>>>(a.n_rows, a.v, a.inv_temp, a.ids, a.stats, a.grad, a.grad_lse, DT == TT_F16 ? 0x1p14f : 1.0f, place, list,
+                                        reinterpret_cast<Row *>(ws + lay.meta), totals);
+    copy_rows(a.hidden, a.x_ld, a.n_rows, a.h, e, list, totals, ws + lay.x, lay.width, stream);
     for (int64_t v0 = 0; v0 < a.v; v0 += lay.piece) {
-        const int here = (int)std::min<int64_t>(lay.piece, a.v - v0);
-        const char *weight = static_cast<const char *>(a.weight) + v0 * a.w_ld * e;
-        if (a.dhidden || DT == TT_F32)
-            lay_out<DT><<<dim3((unsigned int)(round_to(here, 64) / 64), wide), 256, 0, stream>>>(
-                weight, a.w_ld, here, a.h, nullptr, nullptr, DT == TT_F32 ? wp : nullptr, lay.width, w_plane, a.dhidden ? wt : nullptr, lay.piece, w_plane);
-        const Side ws_ = DT == TT_F32 ? Side{reinterpret_cast<const char *>(wp), lay.width * 2, w_plane * 2, here} : Side{weight, a.w_ld * e, 0, here};
-        head_dlogits<DT><<<dim3(tiles_of(here), tiles_of(a.n_rows)), Tile::THREADS, 0, stream>>>(
-            ws_, xs, DT == TT_F32 ? lay.width * 2 : a.h * e, (int)v0, meta, totals, a.dhidden ? d : nullptr, lay.piece, d_plane, a.dweight ? dt : nullptr,
-            lay.n_pad, d_plane);
-        if (a.dhidden) {
-            const int64_t bytes = round_to(here, kStepElements) * 2, split = round_to((bytes + lay.splits - 1) / lay.splits, kStepBytes);
-            const Side wts = {reinterpret_cast<const char *>(wt), lay.piece * 2, w_plane * 2, (int)lay.width};
-            const Side ds = {reinterpret_cast<const char *>(d), lay.piece * 2, d_plane * 2, (int)lay.n_pad};
-            head_dhidden<DT><<<dim3(tiles_of(lay.width), tiles_of(a.n_rows), lay.splits), Tile::THREADS, 0, stream>>>(
-                wts, ds, bytes, split, totals, sums, lay.width, x_plane, v0 == 0);
-        }
-        if (a.dweight) {
-            const Side dts = {reinterpret_cast<const char *>(dt), lay.n_pad * 2, d_plane * 2, here};
-            head_dweight<DT><<<dim3(tiles_of(a.h), tiles_of(here)), Tile::THREADS, 0, stream>>>(
-                xts, dts, totals, a.h, static_cast<char *>(a.dweight) + v0 * a.dw_ld * e, a.dw_ld);
-        }
+        if constexpr (DT == TT_F32) backward_piece<DT, 2>(a, lay, ws, v0, copy_w, stream);
+        else if (columns_for(a.n_rows, DT) == 2) backward_piece<DT, 2>(a, lay, ws, v0, copy_w, stream);
+        else backward_piece<DT, 4>(a, lay, ws, v0, copy_w, stream);
     }
     if (a.dhidden)
-        head_place<DT><<<dim3(a.n_rows, (unsigned int)((a.h + 255) / 256)), 256, 0, stream>>>(sums, lay.width, x_plane, lay.splits, place, totals, a.h,
+        head_place<DT><<<dim3(a.n_rows, (unsigned int)((a.h + 255) / 256)), 256, 0, stream>>>(reinterpret_cast<float *>(ws + lay.sums), lay.width,
+                                                                                         lay.n_pad * lay.width, lay.splits, place, totals, a.h,
                                                                                          a.dhidden, a.dx_ld);
     return status();
 }
 
 }  // namespace
 
-size_t head_workspace_bytes(int32_t n_rows, int32_t v, int32_t h, int dtype) { return ForwardLayout(n_rows, v, h, dtype).total; }
+size_t head_workspace_bytes(int32_t n_rows, int32_t v) { return ForwardLayout(n_rows, v).total; }
 
-size_t head_backward_workspace_bytes(int32_t n_rows, int32_t v, int32_t h, int dtype) { return BackwardLayout(n_rows, v, h, dtype, true).total; }
+size_t head_backward_workspace_bytes(int32_t n_rows, int32_t v, int32_t h, int dtype) { return BackwardLayout::most(n_rows, v, h, dtype); }
 size_t head_backward_workspace_used(int32_t n_rows, int32_t v, int32_t h, int dtype) { return BackwardLayout(n_rows, v, h, dtype).total; }
 
 int launch_head_logprobs(const HeadArgs &a, void *workspace, size_t workspace_bytes, hipStream_t stream) {
-    if (!workspace || workspace_bytes < head_workspace_bytes(a.n_rows, a.v, a.h, a.dtype)) return TT_EWORKSPACE;
+    if (!workspace || workspace_bytes < head_workspace_bytes(a.n_rows, a.v)) return TT_EWORKSPACE;
     char *ws = static_cast<char *>(workspace);
     return a.dtype == TT_BF16 ? forward<TT_BF16>(a, ws, stream) : a.dtype == TT_F16 ? forward<TT_F16>(a, ws, stream) : forward<TT_F32>(a, ws, stream);
 }

@@ -3,6 +3,8 @@
 //
 //   scale_i = max_k |x_ik| / 127,  q_ik = rint(x_ik / scale_i)
 //   y_ij = sx_i sw_j sum_k q_ik w_jk (+ bias_j)
+#include <algorithm>
+
 #include "tiles.h"
 
 namespace tt {
@@ -11,8 +13,8 @@ namespace {
 using namespace tiles;
 using rows::round256;
 
-constexpr int kTile = 128;
-typedef Shape<kTile, kTile, 2, 2> Tile;
+typedef Shape<128, 128, 2, 2> Any;  // of the product of matrices that lie in any way
+constexpr int kRowsPerLaunch = 1 << 15;
 
 // A workgroup a row, read twice (the second time from a cache).
 template <int DT>
@@ -46,36 +48,66 @@ __global__ __launch_bounds__(256) void quantize_rows(int k, const void *x, int64
     if (threadIdx.x == 0) scale[n] = none ? NAN : s;
 }
 
-template <int DT, bool LSE>
-__global__ __launch_bounds__(Tile::THREADS) void product_i8(Side w, Side x, int k, const float *x_scale, const float *w_scale, const float *bias,
-                                                            void *out, int64_t out_ld, const float *inv_temp, Part *parts, int n_tiles) {
-    __shared__ __attribute__((aligned(16))) char lds[Tile::LDS];
-    i4 acc[Tile::FM][Tile::FN];
+struct Scales {
+    const float *x, *w, *bias, *inv_temp;
+};
+
+// A tile's results, and the parts of their rows' log-sum-exp.
+template <int DT, bool LSE, typename S>
+__device__ __forceinline__ void finish_tile(const Side &w, const Side &x, int m0, int n0, i4 (&acc)[S::FM][S::FN], const Scales &scales, void *out,
+                                            int64_t out_ld, Part *parts, int n_tiles, char *lds) {
     using T = typename rows::Elem<DT>::T;
-    const int m0 = (int)blockIdx.x * kTile, n0 = (int)blockIdx.y * kTile;
-    product<kI8, Tile, 1>(w, x, m0, n0, 0, k, k, lds, acc);
     const int n_rows = x.rows;
-    float y[Tile::FM][Tile::FN][4];
-    for_blocks<Tile>(m0, n0, [&](int m, int n, int i, int j) {
-        const float sx = n < n_rows ? x_scale[n] : 0.0f;
+    float sw[S::FM][4], bias[S::FM][4];
+    for_rows<S>(m0, [&](int m, int i) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            float f = -INFINITY;
-            if (m + q < w.rows) {
-                f = (float)acc[i][j][q] * sx * w_scale[m + q];
-                if (bias) f += bias[m + q];
-            }
-            y[i][j][q] = f;
+            sw[i][q] = m + q < w.rows ? scales.w[m + q] : 0.0f;
+            bias[i][q] = scales.bias && m + q < w.rows ? scales.bias[m + q] : 0.0f;
         }
-        if (n < n_rows) store4<DT>(static_cast<T *>(out) + (int64_t)n * out_ld, m, w.rows, y[i][j]);
+    });
+    for_columns<S>(n0, [&](int n, int j) {
+        const float sx = n < n_rows ? scales.x[n] : 0.0f;
+        T *row = static_cast<T *>(out) + (int64_t)n * out_ld;
+        for_rows<S>(m0, [&](int m, int i) {
+            float y[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                y[q] = (float)acc[i][j][q] * sx * sw[i][q];
+                if (scales.bias) y[q] += bias[i][q];
+            }
+            if (n < n_rows) store4<DT>(row, m, w.rows, y);
+            if constexpr (LSE)  // of the results as they are written
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[i][j][q] = __float_as_int(m + q < w.rows ? rows::decode<DT>(rows::encode<DT>(y[q])) : -INFINITY);
+        });
     });
     if constexpr (LSE) {
-        const Part p = column_parts<Tile>(
-            n0, lds, [&](int i, int j, int q) { return rows::decode<DT>(rows::encode<DT>(y[i][j][q])); },
-            [&](int n) { return (n < n_rows ? rows::scale_of(inv_temp, n) : 1.0f) * rows::kLog2e; });
+        const Part p = column_parts<S>(
+            n0, lds, [&](int i, int j, int q) { return __int_as_float(acc[i][j][q]); },
+            [&](int n) { return (n < n_rows ? rows::scale_of(scales.inv_temp, n) : 1.0f) * rows::kLog2e; });
         const int n = n0 + (int)threadIdx.x;
-        if ((int)threadIdx.x < kTile && n < n_rows) parts[(int64_t)n * n_tiles + blockIdx.x] = p;
+        if ((int)threadIdx.x < S::TN && n < n_rows) parts[(int64_t)n * n_tiles + m0 / S::TM] = p;
     }
+}
+
+template <int DT, bool LSE, int FN>
+__global__ __launch_bounds__(512) void product_i8(Side w, Side x, int mt, int nt, Scales scales, void *out, int64_t out_ld, Part *parts) {
+    TT_WIDE_LDS(FN);
+    i4 acc[8][FN];
+    int m, n;
+    tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m, n);
+    Product<kI8, false, false, FN>::run(w, x, m * 256, n * 64 * FN, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
+    finish_tile<DT, LSE, Wide<FN>>(w, x, m * 256, n * 64 * FN, acc, scales, out, out_ld, parts, mt, a0);
+}
+
+template <int DT, bool LSE>
+__global__ __launch_bounds__(Any::THREADS) void product_i8_any(Side w, Side x, Scales scales, void *out, int64_t out_ld, Part *parts) {
+    __shared__ __attribute__((aligned(16))) char lds[Any::LDS];
+    i4 acc[Any::FM][Any::FN];
+    const int m0 = (int)blockIdx.x * Any::TM, n0 = (int)blockIdx.y * Any::TN;
+    product_any<kI8, Any>(w, x, m0, n0, lds, acc);
+    finish_tile<DT, LSE, Any>(w, x, m0, n0, acc, scales, out, out_ld, parts, gridDim.x, lds);
 }
 
 // A wave a row.
@@ -87,15 +119,35 @@ __global__ __launch_bounds__(256) void join_lse(const Part *parts, int n_tiles, 
     if (((int)threadIdx.x & 63) == 0) lse[n] = rows::sound(beta) && r.s == r.s ? fmaf(beta, r.m, r.s) : NAN;
 }
 
+template <int DT, bool LSE>
+int multiply(const MatmulI8Args &a, Part *parts, hipStream_t stream) {
+    const Side w = {reinterpret_cast<const char *>(a.w), a.w_ld, a.n_cols, a.k}, x = {reinterpret_cast<const char *>(a.x), a.x_ld, a.n_rows, a.k};
+    const int64_t e = rows::element_bytes(DT);
+    int n_tiles = (a.n_cols + 255) / 256;
+    if (whole_steps(w) && whole_steps(x)) {
+        for (int64_t n0 = 0; n0 < a.n_rows; n0 += kRowsPerLaunch) {
+            const int n = (int)std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0), fn = n <= 128 ? 2 : 4, nt = (n + 64 * fn - 1) / (64 * fn);
+            const Side part = {x.p + n0 * x.ld, x.ld, n, x.bytes};
+            const Scales scales = {a.x_scale + n0, a.w_scale, a.bias, a.inv_temp ? a.inv_temp + n0 : nullptr};
+            const auto run = [&](auto kernel) {
+                kernel<<<(unsigned int)(n_tiles * nt), 512, 0, stream>>>(w, part, n_tiles, nt, scales, static_cast<char *>(a.out) + n0 * a.out_ld * e, a.out_ld,
+                                                                      parts + n0 * n_tiles);
+            };
+            if (fn == 2) run(product_i8<DT, LSE, 2>);
+            else run(product_i8<DT, LSE, 4>);
+        }
+    } else {
+        n_tiles = (a.n_cols + Any::TM - 1) / Any::TM;
+        product_i8_any<DT, LSE><<<dim3(n_tiles, (a.n_rows + Any::TN - 1) / Any::TN), Any::THREADS, 0, stream>>>(
+            w, x, Scales{a.x_scale, a.w_scale, a.bias, a.inv_temp}, a.out, a.out_ld, parts);
+    }
+    if (LSE) join_lse<<<(unsigned int)((a.n_rows + 3) / 4), 256, 0, stream>>>(parts, n_tiles, a.n_rows, a.inv_temp, a.lse);
+    return hipGetLastError() == hipSuccess ? TT_OK : TT_ELAUNCH;
+}
+
 template <int DT>
 int multiply(const MatmulI8Args &a, Part *parts, hipStream_t stream) {
-    const Side w = {reinterpret_cast<const char *>(a.w), a.w_ld, 0, a.n_cols}, x = {reinterpret_cast<const char *>(a.x), a.x_ld, 0, a.n_rows};
-    const int n_tiles = (a.n_cols + kTile - 1) / kTile;
-    const dim3 grid(n_tiles, (a.n_rows + kTile - 1) / kTile);
-    if (a.lse) product_i8<DT, true><<<grid, Tile::THREADS, 0, stream>>>(w, x, a.k, a.x_scale, a.w_scale, a.bias, a.out, a.out_ld, a.inv_temp, parts, n_tiles);
-    else product_i8<DT, false><<<grid, Tile::THREADS, 0, stream>>>(w, x, a.k, a.x_scale, a.w_scale, a.bias, a.out, a.out_ld, a.inv_temp, parts, n_tiles);
-    if (a.lse) join_lse<<<(unsigned int)((a.n_rows + 3) / 4), 256, 0, stream>>>(parts, n_tiles, a.n_rows, a.inv_temp, a.lse);
-    return hipGetLastError() == hipSuccess ? TT_OK : TT_ELAUNCH;
+    return a.lse ? multiply<DT, true>(a, parts, stream) : multiply<DT, false>(a, parts, stream);
 }
 
 }  // namespace
@@ -109,7 +161,7 @@ int launch_quantize_i8(const QuantizeI8Args &a, hipStream_t stream) {
 }
 
 size_t matmul_i8_workspace_bytes(int32_t n_rows, int32_t n_cols, bool lse) {
-    return lse ? round256((size_t)n_rows * ((n_cols + kTile - 1) / kTile) * sizeof(Part)) : 0;
+    return lse ? round256((size_t)n_rows * ((n_cols + Any::TM - 1) / Any::TM) * sizeof(Part)) : 0;
 }
 
 int launch_matmul_i8(const MatmulI8Args &a, void *workspace, size_t workspace_bytes, hipStream_t stream) {

@@ -1,5 +1,5 @@
-// Matrix products of 16-bit floats and 8-bit integers on the matrix cores, by tiles: C[n][m] = sum_k A[m][k] B[n][k],
-// both operands with k contiguous.  Internal to the library (head.hip, i8.hip).
+// Matrix products of bf16, fp16, fp32 and 8-bit integers on the matrix cores, by tiles: C[n][m] = sum_k A[m][k] B[n][k].
+// Internal to the library (head.hip, i8.hip).
 //
 // The operand with the rows m gives the result's contiguous index: a lane holds 4 consecutive m of one n for each 16 x 16
 // block, so what goes on along a row of the result (a softmax over the vocabulary, a store) stays mostly within a lane.
@@ -10,16 +10,19 @@
 namespace tt {
 namespace tiles {
 
-constexpr int kI8 = 3;         // the 8-bit integers, beside TT_BF16 and TT_F16
-constexpr int kStepBytes = 128;  // of k in a row of a tile: 64 elements of 16 bits, 128 of 8
+constexpr int kI8 = 3;           // the 8-bit integers, beside TT_BF16, TT_F16 and TT_F32
+constexpr int kStepBytes = 128;  // of k that a step takes of every row: 64 elements of 16 bits, 32 of 32, 128 of 8
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef int i4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u4b __attribute__((ext_vector_type(4), aligned(1)));  // 16 bytes at any address
 
+constexpr __host__ __device__ int bytes_of(int dt) { return dt == TT_F32 ? 4 : dt == kI8 ? 1 : 2; }
+
 // One 16 x 16 block's product over 64 bytes of k: lane l holds row l % 16 of either operand, bytes 16 (l / 16) and up;
-// the result's rows 4 (l / 16) .. + 3 (of the first operand) in column l % 16 (of the second).
+// the result's rows 4 (l / 16) .. + 3 (of the first operand) in column l % 16 (of the second).  fp32: four products over 4
+// elements each, the j-th over elements j of the four lanes' 16 bytes.
 template <int DT>
 struct Mfma {
     typedef f4 Acc;
@@ -31,6 +34,15 @@ struct Mfma {
     }
 };
 template <>
+struct Mfma<TT_F32> {
+    typedef f4 Acc;
+    static __device__ __forceinline__ f4 run(u4 a, u4 b, f4 c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0, 0, 0);
+        return c;
+    }
+};
+template <>
 struct Mfma<kI8> {
     typedef i4 Acc;
     static __device__ __forceinline__ i4 run(u4 a, u4 b, i4 c) {
@@ -38,45 +50,38 @@ struct Mfma<kI8> {
     }
 };
 
-// A matrix with contiguous rows of `bytes` bytes; rows at and past `rows` count as zero.
+// A matrix of `rows` rows of `bytes` bytes, `ld` bytes from one to the next.
 struct Side {
     const char *p;
-    int64_t ld;     // bytes from a row to the next
-    int64_t plane;  // bytes from a part of an fp32 matrix to the next one
+    int64_t ld;
     int rows;
+    int bytes;
 };
 
-// The sequence of products of fp32 operands held as three bf16 parts each, largest part 0: those of parts i + j <= 2, the
-// small ones first.  What is left out is below 2^-24 of the product.
-constexpr int kParts = 3, kPasses = 6;
-__device__ constexpr int kPartA[kPasses] = {2, 0, 1, 1, 0, 0}, kPartB[kPasses] = {0, 2, 1, 0, 1, 0};
-
-// An fp32 value as three bf16 parts; what is not finite is all in the first.
-__device__ __forceinline__ void split(float x, uint32_t (&part)[kParts]) {
-    uint32_t hi = rows::encode<TT_BF16>(x);
-    if ((hi & 0x7F80u) == 0x7F80u) {
-        if ((__float_as_uint(x) & 0x7F800000u) != 0x7F800000u) hi = __float_as_uint(x) >> 16;  // rounded up to infinity
-        else {
-            part[0] = hi;
-            part[1] = part[2] = 0;
-            return;
-        }
-    }
-    const float r = x - rows::decode<TT_BF16>(hi);
-    const uint32_t mid = rows::encode<TT_BF16>(r);
-    part[0] = hi;
-    part[1] = mid;
-    part[2] = rows::encode<TT_BF16>(r - rows::decode<TT_BF16>(mid));
-}
-
-// A tile of TM x TN by WM x WN waves.
+// A tile of TM x TN by WM x WN waves, wave w at (w / WN, w % WN).
 template <int TM_, int TN_, int WM_, int WN_>
 struct Shape {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_;
     static constexpr int THREADS = WM * WN * 64;
     static constexpr int FM = TM / WM / 16, FN = TN / WN / 16;  // blocks of a wave
     static constexpr int LDS = 2 * (TM + TN) * kStepBytes;
+    // The blocks of 16 rows and columns that a wave's blocks (i, j) lie in.
+    static __device__ __forceinline__ int row_block(int wave, int i) { return wave / WN * FM + i; }
+    static __device__ __forceinline__ int column_block(int wave, int j) { return wave % WN * FN + j; }
 };
+
+// The first n (below 16) bytes at q, one by one; zeros behind them.
+__device__ inline u4 load_some(const char *q, int n) {
+    u4 v = {0, 0, 0, 0};
+    for (int j = 0; j < n; ++j) {
+        const uint32_t b = (uint32_t)(uint8_t)q[j] << (8 * (j & 3));
+        if (j < 4) v.x |= b;
+        else if (j < 8) v.y |= b;
+        else if (j < 12) v.z |= b;
+        else v.w |= b;
+    }
+    return v;
+}
 
 template <int ROWS, int THREADS>
 struct Staged {
@@ -84,24 +89,15 @@ struct Staged {
     u4 w[N];
 
     // Bytes k .. k + 127 of the rows from r0 on, into registers; zero outside the matrix.
-    __device__ __forceinline__ void load(const Side &s, int64_t part, int r0, int64_t k, int64_t bytes) {
+    __device__ __forceinline__ void load(const Side &s, int r0, int k) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = i * THREADS + (int)threadIdx.x, r = r0 + (c >> 3);
-            const int64_t at = k + (c & 7) * 16;
+            const int at = k + (c & 7) * 16;
             u4 v = {0, 0, 0, 0};
-            if (r < s.rows && at < bytes) {
-                const char *q = s.p + part + (int64_t)r * s.ld + at;
-                if (at + 16 <= bytes) v = *reinterpret_cast<const u4b *>(q);
-                else {
-                    for (int j = 0; j < (int)(bytes - at); ++j) {
-                        const uint32_t b = (uint32_t)(uint8_t)q[j] << (8 * (j & 3));
-                        if (j < 4) v.x |= b;
-                        else if (j < 8) v.y |= b;
-                        else if (j < 12) v.z |= b;
-                        else v.w |= b;
-                    }
-                }
+            if (r < s.rows && at < s.bytes) {
+                const char *q = s.p + (int64_t)r * s.ld + at;
+                v = at + 16 <= s.bytes ? (u4)*reinterpret_cast<const u4b *>(q) : load_some(q, s.bytes - at);
             }
             w[i] = v;
         }
@@ -117,25 +113,21 @@ struct Staged {
     }
 };
 
-// The tile at (m0, n0) of the product over bytes [k0, k1) of both sides' rows (multiples of 128, or the rows' end `bytes`).
-template <int DT, typename S, int PASSES>
-__device__ __forceinline__ void product(const Side &a, const Side &b, int m0, int n0, int64_t k0, int64_t k1, int64_t bytes, char *lds,
-                                        typename Mfma<DT>::Acc (&acc)[S::FM][S::FN]) {
+// The tile at (m0, n0) of the product of two matrices with k contiguous, staged through registers: any alignment, any width.
+template <int DT, typename S>
+__device__ __forceinline__ void product_any(const Side &a, const Side &b, int m0, int n0, char *lds, typename Mfma<DT>::Acc (&acc)[S::FM][S::FN]) {
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const int wm = wave % S::WM, wn = wave / S::WM;
+    const int wm = wave / S::WN, wn = wave % S::WN;
 #pragma unroll
     for (int i = 0; i < S::FM; ++i)
 #pragma unroll
         for (int j = 0; j < S::FN; ++j) acc[i][j] = {0, 0, 0, 0};
-    const int steps = (int)((k1 - k0 + kStepBytes - 1) / kStepBytes), total = steps * PASSES;
-    if (total <= 0) return;
+    const int total = (a.bytes + kStepBytes - 1) / kStepBytes;
     Staged<S::TM, S::THREADS> sa;
     Staged<S::TN, S::THREADS> sb;
     auto load = [&](int t) {
-        const int pass = PASSES == 1 ? 0 : t / steps;
-        const int64_t k = k0 + (int64_t)(t - pass * steps) * kStepBytes;
-        sa.load(a, PASSES == 1 ? 0 : a.plane * kPartA[pass], m0, k, bytes);
-        sb.load(b, PASSES == 1 ? 0 : b.plane * kPartB[pass], n0, k, bytes);
+        sa.load(a, m0, t * kStepBytes);
+        sb.load(b, n0, t * kStepBytes);
     };
     load(0);
     for (int t = 0; t < total; ++t) {
@@ -163,15 +155,235 @@ __device__ __forceinline__ void product(const Side &a, const Side &b, int m0, in
     __syncthreads();
 }
 
-// f(m, n, i, j) for every block of this thread's wave: m the first of its 4 rows, n its column.
+// ------------------------------------------------------------------------------------------------ wide tiles
+typedef __attribute__((address_space(3))) void *lds_ptr;
+
+// 256 rows of the first operand by 64 FN of the second; 8 waves, each 128 x 16 FN, of every fourth block.
+template <int FN_>
+struct Wide {
+    static constexpr int TM = 256, TN = 64 * FN_, WM = 2, WN = 4, THREADS = 512, FM = 8, FN = FN_;
+    static __device__ __forceinline__ int row_block(int wave, int i) { return (i & 3) * 4 + (wave >> 2) * 2 + (i >> 2); }
+    static __device__ __forceinline__ int column_block(int wave, int j) { return j * 4 + (wave & 3); }
+};
+
+// 16 bytes a lane from the memory's start + `at`, to LDS at `to` and on, in the order of the lanes.  Written as an instruction
+// because the compiler, which cannot tell the two steps' buffers apart across a loop, would have every read of LDS wait for all
+// loads; here they are waited for where a step begins (vmcnt).  Nothing is returned to registers, and addresses are read at issue.
+__device__ __forceinline__ void load_to_lds(u4 memory, uint32_t at, uint32_t to) {
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(at), "s"(memory), "{m0}"(to) : "memory");
+}
+
+// One operand's tile of a step: ROWS rows of the result by 128 bytes of k, brought to LDS by loads that go past the
+// registers (a wave's 64 lanes fill 1 KB), from memory with k contiguous, or (KM) with the rows of the result contiguous.
+// k contiguous: rows of 128 bytes, the 16-byte pieces of row r at place piece ^ (r & 7).  KM: lines of one k; the 16
+// elements of a block at place block ^ s(k), s different for the four lines that lanes read together; the 16-bit elements are
+// transposed by the reading (ds_read_b64_tr_b16: lane l of 16 gets element l of the four lines that their lanes' 8 bytes
+// lie in), the 32-bit ones read one by one.  All of LDS's banks are reached evenly in every case.
+template <int DT, bool KM, int ROWS>
+struct Operand {
+    static constexpr int E = DT == TT_F32 ? 4 : 2;         // KM: bytes of an element
+    static constexpr int LINE = ROWS * E, BLOCK = 16 * E;  // KM: bytes of a line and of a block in it
+    static constexpr int K = kStepBytes / E;               // KM: lines of a step
+    static constexpr int N = ROWS / 64;                    // loads of a wave
+    const char *p;
+    int64_t ld;
+    uint32_t at[N];
+    int lane, wave, lines;  // KM: lines from the first step's first to the end
+
+    static __device__ __forceinline__ int place(int k) { return (E == 2 ? k : k >> 2) & 3; }
+    // r0: the tile's first row; step0: steps to leave out.  Rows past the matrix's end are those of its last row, bytes
+    // past a line's end those of its end.
+    __device__ __forceinline__ void begin(const Side &s, int r0, int step0) {
+        lane = (int)threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        if constexpr (!KM) {
+            p = s.p + r0 * s.ld + (int64_t)step0 * kStepBytes;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                at[i] = __umul24(min((wave * N + i) * 8 + (lane >> 3), s.rows - 1 - r0), (int)s.ld) + ((lane & 7) ^ (lane >> 3)) * 16;
+        } else {
+            p = s.p + (int64_t)step0 * K * s.ld + r0 * E;
+            ld = s.ld;
+            lines = s.rows - step0 * K;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int b = (wave * N + i) * 1024 + lane * 16, k = b / LINE, c = (b % LINE / BLOCK ^ place(k)) * BLOCK + b % BLOCK;
+                at[i] = __umul24(k, (int)s.ld) + min(c, s.bytes - 16 - r0 * E);
+            }
+        }
+    }
+    __device__ __forceinline__ void fetch(char *tile, int t) const {
+        const uint64_t from = reinterpret_cast<uint64_t>(p) + (KM ? (int64_t)t * K * ld : (int64_t)t * kStepBytes);
+        const u4 memory = {(uint32_t)from, (uint32_t)(from >> 32), 0xFFFFFFFFu, 0x00027000u};
+        const uint32_t to = (uint32_t)reinterpret_cast<uintptr_t>((lds_ptr)tile) + wave * N * 1024;
+        if (KM && (t + 1) * K > lines) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                load_to_lds(memory, at[i] - __umul24(max(0, ((wave * N + i) * 1024 + lane * 16) / LINE - (lines - 1 - t * K)), (int)ld), to + i * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_to_lds(memory, at[i], to + i * 1024);
+        }
+    }
+    // Both 64-byte halves of a step for the rows of block 4 i + c (c below 4: one address serves all i).
+    __device__ __forceinline__ void read(u4 (&f)[2], const char *tile, int c, int i) const {
+        if constexpr (!KM) {
+            const char *q = tile + c * 2048 + i * 8192 + (lane & 15) * kStepBytes;
+            f[0] = *reinterpret_cast<const u4 *>(q + ((lane >> 4) ^ (lane & 7)) * 16);
+            f[1] = *reinterpret_cast<const u4 *>(q + ((4 + (lane >> 4)) ^ (lane & 7)) * 16);
+        } else if constexpr (E == 2) {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s4 *s4_ptr;
+            const int k = (lane >> 4) * 8 + (lane >> 2 & 3);
+            const char *q = tile + k * LINE + (lane & 3) * 8 + (c ^ place(k)) * BLOCK + i * 4 * BLOCK;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4_ptr)(q + h * 32 * LINE)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4_ptr)(q + (h * 32 + 4) * LINE));
+                typedef short s8 __attribute__((ext_vector_type(8)));
+                f[h] = __builtin_bit_cast(u4, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        } else {
+            const int k = (lane >> 4) * 4;
+            const char *q = tile + k * LINE + (lane & 15) * 4 + (c ^ place(k)) * BLOCK + i * 4 * BLOCK;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[h][j] = *reinterpret_cast<const uint32_t *>(q + (h * 16 + j) * LINE);
+        }
+    }
+};
+
+// LDS of a wide product: two steps of either operand.  Arrays of their own, so that the compiler knows that what is read
+// of one step does not wait for the loads of the next.
+#define TT_WIDE_LDS(FN) __shared__ __attribute__((aligned(1024))) char a0[32768], a1[32768], b0[8192 * (FN)], b1[8192 * (FN)]
+
+// The tile at (m0, n0) of the product over the steps [step0, step0 + steps).  Needs 16-byte aligned rows; k contiguous: whole
+// steps of 128 bytes; 256 rows within 2^31 bytes, KM: all of the steps' lines.
+//
+// Waves 0-3 hold the upper half of the 256 rows, 4-7 the lower one; every SIMD runs one of each.  A step is four pieces of
+// 64 x 8 FN (of a wave): reads from LDS, barrier, matrix instructions, barrier.  The second half's waves are one barrier
+// behind, so that on every SIMD one wave's reads lie beside the other's matrix instructions.  Reads of a step's first rows are
+// done in the last piece of the step before, and there the loads for the step after next begin, into the memory that was
+// read last; they have a whole step's time.  LDS is read at 75% of its rate.
+template <int DT, bool AKM, bool BKM, int FN>
+struct Product {
+static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0, int n0, int step0, int steps, char *a0, char *a1, char *b0, char *b1,
+                                           typename Mfma<DT>::Acc (&acc)[8][FN]) {
+    constexpr int H = FN / 2;
+    Operand<DT, AKM, 256> oa;
+    Operand<DT, BKM, 64 * FN> ob;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = {0, 0, 0, 0};
+    if (steps <= 0) return;
+    oa.begin(a, m0, step0);
+    ob.begin(b, n0, step0);
+    const int wm = oa.wave >> 2, wn = oa.wave & 3;
+    u4 fa0[4][2], fa1[4][2], fb0[H][2], fb1[H][2];
+    const auto read_a = [&](u4 (&f)[4][2], const char *tile, int half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) oa.read(f[i], tile, wm * 2 + half, i);
+    };
+    const auto read_b = [&](u4 (&f)[H][2], const char *tile, int half) {
+#pragma unroll
+        for (int j = 0; j < H; ++j) ob.read(f[j], tile, wn, half * H + j);
+    };
+    const auto multiply = [&](const u4 (&f)[4][2], const u4 (&g)[H][2], int ah, int bh) {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < H; ++j) acc[ah * 4 + i][bh * H + j] = Mfma<DT>::run(f[i][k], g[j][k], acc[ah * 4 + i][bh * H + j]);
+        __builtin_amdgcn_s_setprio(0);
+    };
+    const auto wait_reads = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };
+    const auto wait_loads = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };
+    const auto barrier = [] {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    oa.fetch(a0, 0);
+    ob.fetch(b0, 0);
+    if (steps > 1) {
+        oa.fetch(a1, 1);
+        ob.fetch(b1, 1);
+        __builtin_amdgcn_s_waitcnt(0x0f70 | (4 + FN));  // the first step's
+    } else {
+        wait_loads();
+    }
+    barrier();
+    read_a(fa0, a0, 0);
+    if (wm == 1) barrier();
+    const auto step = [&](char *at, char *bt, const char *an, int t) {
+        read_b(fb0, bt, 0);
+        wait_reads();
+        barrier();
+        multiply(fa0, fb0, 0, 0);
+        barrier();
+        read_b(fb1, bt, 1);
+        wait_reads();
+        barrier();
+        multiply(fa0, fb1, 0, 1);
+        barrier();
+        read_a(fa1, at, 1);
+        wait_reads();
+        wait_loads();  // the next step's
+        barrier();
+        multiply(fa1, fb1, 1, 1);
+        barrier();
+        if (t + 1 < steps) read_a(fa0, an, 0);
+        if (t + 2 < steps) {
+            oa.fetch(at, t + 2);
+            ob.fetch(bt, t + 2);
+        }
+        wait_reads();
+        barrier();
+        multiply(fa1, fb0, 1, 0);
+        barrier();
+    };
+    int t = 0;
+    for (; t + 1 < steps; t += 2) {
+        step(a0, b0, a1, t);
+        step(a1, b1, a0, t + 1);
+    }
+    if (t < steps) step(a0, b0, a1, t);
+    if (wm == 0) barrier();
+    __syncthreads();
+}
+};
+
+// The tile of workgroup `id` of mt x nt: neighbours in time on one XCD (every eighth workgroup) share rows of both operands in
+// its L2: they go through 8 tiles of the first operand by all of the second's.
+__device__ __forceinline__ void tile_of(int id, int total, int mt, int nt, int &m, int &n) {
+    constexpr int kXcds = 8, kGroup = 8;
+    const int xcd = id % kXcds, per = total / kXcds, more = total % kXcds;
+    const int at = xcd * per + min(xcd, more) + id / kXcds, group = at / (kGroup * nt), in = at % (kGroup * nt);
+    const int wide = min(kGroup, mt - group * kGroup);
+    m = group * kGroup + in % wide;
+    n = in / wide;
+}
+
+// Whether a matrix's rows can go to LDS as they are, with k contiguous: whole steps, 16-byte aligned.
+inline bool whole_steps(const Side &s) {
+    return reinterpret_cast<uintptr_t>(s.p) % 16 == 0 && s.ld % 16 == 0 && s.bytes % kStepBytes == 0 && s.ld < (1 << 22);
+}
+
+// f(n, j) for the columns n that this thread holds parts of, f(m, i) for its blocks' first rows m.
 template <typename S, typename F>
-__device__ __forceinline__ void for_blocks(int m0, int n0, F f) {
+__device__ __forceinline__ void for_columns(int n0, F f) {
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const int wm = wave % S::WM, wn = wave / S::WM;
 #pragma unroll
-    for (int j = 0; j < S::FN; ++j)
+    for (int j = 0; j < S::FN; ++j) f(n0 + S::column_block(wave, j) * 16 + (lane & 15), j);
+}
+template <typename S, typename F>
+__device__ __forceinline__ void for_rows(int m0, F f) {
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i) f(m0 + (wm * S::FM + i) * 16 + (lane >> 4) * 4, n0 + (wn * S::FN + j) * 16 + (lane & 15), i, j);
+    for (int i = 0; i < S::FM; ++i) f(m0 + S::row_block(wave, i) * 16 + (lane >> 4) * 4, i);
 }
 
 // Four consecutive elements of a row that ends at `end`, rounded to the type.
@@ -202,11 +414,11 @@ __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.
 template <typename S, typename Z, typename C>
 __device__ __forceinline__ Part column_parts(int n0, char *lds, Z z, C scale) {
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const int wm = wave % S::WM, wn = wave / S::WM;
+    const int wm = wave / S::WN;
     Part *part = reinterpret_cast<Part *>(lds);  // [WM][TN]
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
-        const int at = (wn * S::FN + j) * 16 + (lane & 15);
+        const int at = S::column_block(wave, j) * 16 + (lane & 15);
         float m = -INFINITY, s = 0.0f;
 #pragma unroll
         for (int i = 0; i < S::FM; ++i)

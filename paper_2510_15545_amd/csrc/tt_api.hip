@@ -634,7 +634,7 @@ int tt_distill(int32_t n_rows, int32_t v, int32_t dtype, const void *logits, int
 int tt_head_logprobs_workspace_size(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, size_t *bytes) {
     const int st = head_ok(n_rows, v, h, dtype, h, h);
     if (bytes == nullptr || st != TT_OK) return bytes == nullptr ? TT_EINVAL : st;
-    *bytes = n_rows == 0 ? 0 : tt::head_workspace_bytes(n_rows, v, h, dtype);
+    *bytes = n_rows == 0 ? 0 : tt::head_workspace_bytes(n_rows, v);
     return TT_OK;
 }
 

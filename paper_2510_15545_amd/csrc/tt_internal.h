@@ -205,7 +205,7 @@ struct HeadArgs {
     const int32_t *ids;     // or null
     float *logprob, *lse, *stats;  // each may be null
 };
-size_t head_workspace_bytes(int32_t n_rows, int32_t v, int32_t h, int dtype);
+size_t head_workspace_bytes(int32_t n_rows, int32_t v);
 int launch_head_logprobs(const HeadArgs &a, void *workspace, size_t workspace_bytes, hipStream_t stream);
 struct HeadGradArgs {
     int32_t n_rows, v, h, dtype;

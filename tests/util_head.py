@@ -8,7 +8,7 @@ U = 2.0 ** -24  # half a step of fp32, relative to the value
 HALF_STEP = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 2.0 ** -24}  # half of finfo(type).eps
 TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
 # A gradient row's values as the products take them, at the scale of the largest row weight: relative and absolute rounding
-# (fp16 is stored 2^14 times as large, so steps of 2^-24 are 2^-38; fp32's three parts hold 24 bits and more)
+# (fp16 is stored 2^14 times as large, so steps of 2^-24 are 2^-38)
 STORED = {"bf16": (2.0 ** -8, 2.0 ** -126), "f16": (2.0 ** -11, 2.0 ** -39), "f32": (2.0 ** -23, 2.0 ** -120)}
 LEAST = 2.0 ** -126  # fp32's (and bf16's) smallest normal value: what is smaller may count as 0, probabilities and results alike
 
