@@ -16,36 +16,109 @@ using rows::round256;
 typedef Shape<128, 128, 2, 2> Any;  // of the product of matrices that lie in any way
 constexpr int kRowsPerLaunch = 1 << 15;
 
-// A workgroup a row, read twice (the second time from a cache).
-template <int DT>
-__global__ __launch_bounds__(256) void quantize_rows(int k, const void *x, int64_t ld, int8_t *q, int64_t q_ld, float *scale) {
-    using T = typename rows::Elem<DT>::T;
-    __shared__ float tops[4];
-    __shared__ int bad[4];
-    const int64_t n = blockIdx.x;
-    const T *row = static_cast<const T *>(x) + n * ld;
-    float top = 0.0f;
-    bool odd = false;
-    for (int i = (int)threadIdx.x; i < k; i += 256) {
-        const float f = fabsf(rows::decode<DT>(row[i]));
-        odd |= !(f < INFINITY);
-        top = fmaxf(top, f);
+// fp32 quotients x / s rounded as a division rounds them, from r = 1 / s correctly rounded (Markstein 1990: a product and one
+// correction by the exact remainder), where s is far from fp32's ends.  A tiny x leaves a remainder that is not exact, and a
+// quotient that rounds to 0 all the same.
+__device__ __forceinline__ float quotient(float x, float s, float r) {
+    const float y = x * r;
+    return fmaf(fmaf(-y, s, x), r, y);
+}
+
+// Rows quantised by WAVES waves each, 4 / WAVES rows to a workgroup (of 256 threads, WAVES = 16: 1,024): 16 bytes a
+// lane and load.  NV > 0: the row stays in NV registers' worth of loads; 0: it is read again.  Bound by memory: 8,192 x 4,096
+// bf16, 101 MB, NFIG us.
+template <int DT, int WAVES, int NV>
+__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void quantize_rows(int n_rows, int k, const char *x, int64_t ld, int8_t *q, int64_t q_ld, float *scale) {
+    constexpr int E = DT == TT_F32 ? 4 : 2, PER = 16 / E, ROWS = WAVES == 16 ? 1 : 4 / WAVES, LANES = WAVES * 64;
+    const int lane = (int)threadIdx.x % LANES, wave = (int)threadIdx.x / 64;
+    const int64_t n = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+    if (WAVES == 1 && n >= n_rows) return;
+    const char *row = x + n * ld;
+    const auto load = [&](int i) {
+        const int at = i * PER;
+        if (at + PER <= k) return (u4)*reinterpret_cast<const u4b *>(row + (int64_t)at * E);
+        return at < k ? load_some(row + (int64_t)at * E, (k - at) * E) : u4{0, 0, 0, 0};
+    };
+    // the largest size, as bits: those of a NaN or an infinity are above all others
+    uint32_t top = 0;
+    const auto add = [&](u4 v) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (DT == TT_F32) top = max(top, v[j] & 0x7FFFFFFFu);
+            else top = max(top, max(v[j] & 0x7FFFu, v[j] >> 16 & 0x7FFFu));
+        }
+    };
+    u4 held[NV ? NV : 1];
+    const int vectors = (k + PER - 1) / PER;
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) held[i] = i * LANES + lane < vectors ? load(i * LANES + lane) : u4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) add(held[i]);
+    } else {
+        for (int i = lane; i < vectors; i += LANES) add(load(i));
     }
     top = rows::wave_max(top);
-    const bool any = __ballot(odd) != 0;
-    if (((int)threadIdx.x & 63) == 0) {
-        tops[threadIdx.x >> 6] = top;
-        bad[threadIdx.x >> 6] = any;
+    if constexpr (WAVES > 1) {
+        __shared__ uint32_t tops[16];
+        if (((int)threadIdx.x & 63) == 0) tops[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
     }
-    __syncthreads();
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const bool none = bad[0] | bad[1] | bad[2] | bad[3];
-    const float s = top / 127.0f;
-    for (int i = (int)threadIdx.x; i < k; i += 256) {
-        const float y = rows::decode<DT>(row[i]) / s;
-        q[n * q_ld + i] = none || s == 0.0f ? 0 : (int8_t)rintf(fminf(fmaxf(y, -127.0f), 127.0f));
+    const float most = rows::decode<DT>(top), s = most / 127.0f;
+    const bool none = !(most < INFINITY) || s == 0.0f, plain = s > 0x1p-100f && s < 0x1p100f;
+    const float r = 1.0f / s;
+    int8_t *out = q + n * q_ld;
+    const auto store = [&](int i, u4 v) {
+        const int at = i * PER;
+        uint32_t b[PER / 4];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            const float f = rows::value<DT>(w, j);
+            const float y = plain ? quotient(f, s, r) : fminf(fmaxf(f / s, -127.0f), 127.0f);
+            const uint32_t c = none ? 0 : (uint32_t)(int)rintf(y) & 0xFFu;
+            b[j / 4] = j % 4 ? b[j / 4] | c << (j % 4 * 8) : c;
+        }
+        if (at + PER <= k) {
+            typedef unsigned int u1b __attribute__((aligned(1)));
+            typedef unsigned int u2b __attribute__((ext_vector_type(2), aligned(1)));
+            if constexpr (PER == 8) *reinterpret_cast<u2b *>(out + at) = u2b{b[0], b[1]};
+            else *reinterpret_cast<u1b *>(out + at) = b[0];
+        } else {
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                if (at + j < k) out[at + j] = (int8_t)(b[j / 4] >> (j % 4 * 8));
+        }
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * LANES + lane < vectors) store(i * LANES + lane, held[i]);
+    } else {
+        for (int i = lane; i < vectors; i += LANES) store(i, load(i));
     }
-    if (threadIdx.x == 0) scale[n] = none ? NAN : s;
+    if (lane == 0) scale[n] = most < INFINITY ? s : NAN;
+}
+
+// Rows of up to 8 KB (16 bits: 4,096 elements) in one wave's registers, of up to 32 KB in four waves', longer ones by 16 waves,
+// read twice.
+template <int DT>
+void quantize(const QuantizeI8Args &a, hipStream_t stream) {
+    constexpr int per = DT == TT_F32 ? 4 : 8;
+    const int vectors = (a.k + per - 1) / per;
+    const auto run = [&](auto kernel, int rows, int threads) {
+        kernel<<<(unsigned int)((a.n_rows + (int64_t)rows - 1) / rows), threads, 0, stream>>>(
+            a.n_rows, a.k, static_cast<const char *>(a.x), a.ld * rows::element_bytes(DT), a.q, a.q_ld, a.scale);
+    };
+    if (vectors <= 64) run(quantize_rows<DT, 1, 1>, 4, 256);
+    else if (vectors <= 128) run(quantize_rows<DT, 1, 2>, 4, 256);
+    else if (vectors <= 256) run(quantize_rows<DT, 1, 4>, 4, 256);
+    else if (vectors <= 512) run(quantize_rows<DT, 1, 8>, 4, 256);
+    else if (vectors <= 1024) run(quantize_rows<DT, 4, 4>, 1, 256);
+    else if (vectors <= 2048) run(quantize_rows<DT, 4, 8>, 1, 256);
+    else run(quantize_rows<DT, 16, 0>, 1, 1024);
 }
 
 struct Scales {
@@ -153,10 +226,9 @@ int multiply(const MatmulI8Args &a, Part *parts, hipStream_t stream) {
 }  // namespace
 
 int launch_quantize_i8(const QuantizeI8Args &a, hipStream_t stream) {
-    const auto run = [&](auto kernel) { kernel<<<(unsigned int)a.n_rows, 256, 0, stream>>>(a.k, a.x, a.ld, a.q, a.q_ld, a.scale); };
-    if (a.dtype == TT_BF16) run(quantize_rows<TT_BF16>);
-    else if (a.dtype == TT_F16) run(quantize_rows<TT_F16>);
-    else run(quantize_rows<TT_F32>);
+    if (a.dtype == TT_BF16) quantize<TT_BF16>(a, stream);
+    else if (a.dtype == TT_F16) quantize<TT_F16>(a, stream);
+    else quantize<TT_F32>(a, stream);
     return hipGetLastError() == hipSuccess ? TT_OK : TT_ELAUNCH;
 }
 
