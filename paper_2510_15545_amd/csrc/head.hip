@@ -113,14 +113,44 @@ __global__ __launch_bounds__(Any::THREADS) void head_parts_any(Side w, Side x, c
     parts_of_tile<DT, Any>(w, x, m0, n0, acc, inv_temp, ids, parts, gridDim.x, token, lds);
 }
 
-// A wave a row.
-__global__ __launch_bounds__(256) void head_join(const Part *parts, int n_tiles, int n_rows, int v, const float *inv_temp, const int32_t *ids,
+// Few rows: every workgroup's part of them.
+template <int DT, int FN>
+__global__ __launch_bounds__(kThinThreads, 4) void head_parts_thin(Side w, Side x, const float *inv_temp, const int32_t *ids, Part *parts, float *token) {
+    __shared__ __attribute__((aligned(16))) char lds[kThinLds];
+    const int column = (int)threadIdx.x & 15;
+    const auto scale = [&](int n) { return (n < x.rows ? rows::scale_of(inv_temp, n) : 1.0f) * rows::kLog2e; };
+    Part p[FN];
+    float c[FN];
+    int id[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        p[j] = {-INFINITY, 0.0f};
+        c[j] = scale(j * 16 + column);
+        id[j] = ids && j * 16 + column < x.rows ? ids[j * 16 + column] : -1;
+    }
+    product_thin<DT, FN>(w, x, lds, [&](int m, f4 (&acc)[FN]) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            float z[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                z[q] = m + q < w.rows ? acc[j][q] : -INFINITY;
+                if (m + q == id[j] && m + q < w.rows) token[j * 16 + column] = acc[j][q];
+            }
+            add_part(p[j], z, c[j]);
+        }
+    });
+    const Part r = join_lanes<FN>(p, x.rows, lds, scale);
+    if ((int)threadIdx.x < x.rows) parts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = r;
+}
+
+// A workgroup a row.
+__global__ __launch_bounds__(256) void head_join(const Part *parts, int n_tiles, int v, const float *inv_temp, const int32_t *ids,
                                                  const float *token, float *logprob, float *lse, float *stats) {
-    const int n = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6);
-    if (n >= n_rows) return;
+    const int n = (int)blockIdx.x;
     const float beta = rows::scale_of(inv_temp, n);
     Part r = join_row(parts + (int64_t)n * n_tiles, n_tiles, beta);
-    if (((int)threadIdx.x & 63) != 0) return;
+    if (threadIdx.x != 0) return;
     if (!rows::sound(beta)) r.m = r.s = NAN;
     if (r.s != r.s) r.m = NAN;
     if (lse) lse[n] = fmaf(beta, r.m, r.s);
@@ -382,7 +412,14 @@ int forward(const HeadArgs &a, char *ws, hipStream_t stream) {
     const int32_t *ids = a.logprob ? a.ids : nullptr;
     const Side w = matrix(a.weight, a.w_ld, a.v, a.h, e);
     int n_tiles = (int)tiles_of(a.v, kTile);
-    if (whole_steps(w) && whole_steps(matrix(a.hidden, a.x_ld, a.n_rows, a.h, e))) {
+    if (a.n_rows <= kThinMost) {
+        n_tiles = (int)std::min<int64_t>(kThinGroups, tiles_of(a.v, kThinRows));
+        const Side x = matrix(a.hidden, a.x_ld, a.n_rows, a.h, e);
+        const auto run = [&](auto kernel) { kernel<<<n_tiles, kThinThreads, 0, stream>>>(w, x, a.inv_temp, ids, parts, token); };
+        if (a.n_rows <= 16) run(head_parts_thin<DT, 1>);
+        else if (a.n_rows <= 32) run(head_parts_thin<DT, 2>);
+        else run(head_parts_thin<DT, 4>);
+    } else if (whole_steps(w) && whole_steps(matrix(a.hidden, a.x_ld, a.n_rows, a.h, e))) {
         for (int64_t n0 = 0; n0 < a.n_rows; n0 += kRowsPerLaunch) {
             const int64_t n = std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0);
             const Side x = matrix(static_cast<const char *>(a.hidden) + n0 * a.x_ld * e, a.x_ld, n, a.h, e);
@@ -400,7 +437,7 @@ int forward(const HeadArgs &a, char *ws, hipStream_t stream) {
         const Side x = matrix(a.hidden, a.x_ld, a.n_rows, a.h, e);
         head_parts_any<DT><<<dim3(n_tiles, (unsigned int)tiles_of(a.n_rows, Any::TN)), Any::THREADS, 0, stream>>>(w, x, a.inv_temp, ids, parts, token);
     }
-    head_join<<<(unsigned int)((a.n_rows + 3) / 4), 256, 0, stream>>>(parts, n_tiles, a.n_rows, a.v, a.inv_temp, a.ids, token, a.logprob, a.lse, a.stats);
+    head_join<<<(unsigned int)a.n_rows, 256, 0, stream>>>(parts, n_tiles, a.v, a.inv_temp, a.ids, token, a.logprob, a.lse, a.stats);
     return status();
 }
 

@@ -356,6 +356,84 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
 }
 };
 
+// ------------------------------------------------------------------------------------------------ few rows
+// Products with few rows of the second operand, bound by the reading of the first: it goes from memory to registers once, 16
+// rows to a wave, 8 loads of 16 bytes a lane ahead (4 where the columns' sums need the registers); the second operand waits in LDS (all of it, or a chunk of k at a time).
+// Any alignment, any width.
+constexpr int kThinThreads = 512, kThinRows = kThinThreads / 64 * 16;  // rows of the first operand that a workgroup takes at a time
+constexpr int kThinLds = 65536;                                      // two workgroups to a compute unit
+constexpr int kThinGroups = 512;                                     // workgroups at most: as many as run at once
+constexpr int kThinMost = 64;                                        // rows of the second operand at most
+
+// Bytes of k that fit LDS for n rows.
+__host__ __device__ inline int thin_chunk(int n, int bytes) { return min((bytes + 127) / 128 * 128, kThinLds / n / 128 * 128); }
+
+// finish(m, acc): results of rows m .. m + 3 (16-row block of the wave, a quarter of it to 16 lanes) and columns 16 j + lane % 16.
+template <int DT, int FN, typename F>
+__device__ __forceinline__ void product_thin(const Side &w, const Side &x, char *lds, F finish) {
+    constexpr int U = FN == 4 ? 4 : 8;
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, quarter = lane >> 4;
+    const int chunk = thin_chunk(x.rows, w.bytes), groups = (w.rows + kThinRows - 1) / kThinRows;
+    const char *column[FN];  // of LDS: the lane's row of the second operand
+    int turn[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int r = min(j * 16 + (lane & 15), x.rows - 1);
+        column[j] = lds + r * chunk;
+        turn[j] = (quarter ^ (r & 7)) * 16;
+    }
+    bool staged = false;
+    for (int g = (int)blockIdx.x; g < groups; g += (int)gridDim.x) {
+        const int m0 = g * kThinRows + wave * 16;
+        const char *row = w.p + (int64_t)min(m0 + (lane & 15), w.rows - 1) * w.ld + quarter * 16;
+        typename Mfma<DT>::Acc acc[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[j] = {0, 0, 0, 0};
+        for (int k0 = 0; k0 < w.bytes; k0 += chunk) {
+            const int bytes = min(chunk, w.bytes - k0), full = bytes / 64;
+            u4 a[U], b[U];
+            const auto load = [&](u4 (&f)[U], int s) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) f[u] = rows::load_global<true>(row + k0 + min(s + u, full - 1) * 64);
+            };
+            const auto multiply = [&](const u4 &f, int s) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    acc[j] = Mfma<DT>::run(f, *reinterpret_cast<const u4 *>(column[j] + (s >> 1) * 128 + (turn[j] ^ (s & 1) * 64)), acc[j]);
+            };
+            if (full > 0) load(a, 0);
+            if (!staged) {
+                __syncthreads();  // the chunk before is done with
+                const int pieces = chunk / 16;
+                for (int i = (int)threadIdx.x; i < x.rows * pieces; i += kThinThreads) {
+                    const int r = i / pieces, c = i % pieces, left = x.bytes - (k0 + c * 16);
+                    const char *q = x.p + (int64_t)r * x.ld + k0 + c * 16;
+                    const u4 v = left >= 16 ? (u4)*reinterpret_cast<const u4b *>(q) : left > 0 ? load_some(q, left) : u4{0, 0, 0, 0};
+                    *reinterpret_cast<u4 *>(lds + r * chunk + (c & ~7) * 16 + ((c ^ r) & 7) * 16) = v;
+                }
+                __syncthreads();
+                staged = chunk >= w.bytes;
+            }
+            for (int s = 0; s < full; s += 2 * U) {
+                if (s + U < full) load(b, s + U);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (s + u < full) multiply(a[u], s + u);
+                if (s + 2 * U < full) load(a, s + 2 * U);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (s + U + u < full) multiply(b[u], s + U + u);
+            }
+            if (full * 64 < bytes) {
+                const int left = bytes - full * 64 - quarter * 16;
+                const char *q = row + k0 + full * 64;
+                multiply(left >= 16 ? (u4)*reinterpret_cast<const u4b *>(q) : left > 0 ? load_some(q, left) : u4{0, 0, 0, 0}, full);
+            }
+        }
+        finish(m0 + quarter * 4, acc);
+    }
+}
+
 // The tile of workgroup `id` of mt x nt: neighbours in time on one XCD (every eighth workgroup) share rows of both operands in
 // its L2: they go through 8 tiles of the first operand by all of the second's.
 __device__ __forceinline__ void tile_of(int id, int total, int mt, int nt, int &m, int &n) {
@@ -409,6 +487,10 @@ struct Part {
 
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.0f : m; }
 
+// The factor of a sum relative to m when it becomes relative to ref, which is at least m, or 0 in the place of minus infinity
+// (a set without logits has the sum 0, which no factor may make NaN).
+__device__ __forceinline__ float factor(float m, float ref, float c) { return __builtin_amdgcn_exp2f(fminf((reference(m) - ref) * c, 0.0f)); }
+
 // The parts of the tile's columns from z(i, j, q) (minus infinity where there is no logit), left in lds[n - n0] for
 // threads below TN after the closing barrier.  scale(n): log2(e) times the row's inverse temperature.
 template <typename S, typename Z, typename C>
@@ -445,25 +527,73 @@ __device__ __forceinline__ Part column_parts(int n0, char *lds, Z z, C scale) {
 #pragma unroll
         for (int w = 0; w < S::WM; ++w) {
             const Part p = part[w * S::TN + threadIdx.x];
-            r.s += p.s * __builtin_amdgcn_exp2f((reference(p.m) - ref) * c);
+            r.s += p.s * factor(p.m, ref, c);
         }
     }
     return r;
 }
 
-// What the parts of a row give, the same in every lane of the wave that holds the row: M, ln S.
+// Adds four logits to a lane's running part.
+__device__ __forceinline__ void add_part(Part &p, const float (&z)[4], float c) {
+    const float m = fmaxf(fmaxf(p.m, fmaxf(z[0], z[1])), fmaxf(z[2], z[3])), ref = reference(m);
+    p.s *= factor(p.m, ref, c);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) p.s += __builtin_amdgcn_exp2f((z[q] - ref) * c);
+    p.m = m;
+}
+
+// The workgroup's part of column threadIdx.x (below n) from its lanes' running parts of columns 16 j + lane % 16.
+template <int FN, typename C>
+__device__ __forceinline__ Part join_lanes(const Part (&p)[FN], int n, char *lds, C scale) {
+    Part *all = reinterpret_cast<Part *>(lds);  // [wave][16 FN]
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, waves = (int)blockDim.x / 64, at = (int)threadIdx.x;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const float m = fmaxf(p[j].m, __shfl_xor(p[j].m, 16)), top = fmaxf(m, __shfl_xor(m, 32));
+        float s = p[j].s * factor(p[j].m, reference(top), scale(j * 16 + (lane & 15)));
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if (lane < 16) all[wave * 16 * FN + j * 16 + lane] = {top, s};
+    }
+    __syncthreads();
+    Part r = {-INFINITY, 0.0f};
+    if (at >= n) return r;
+    for (int w = 0; w < waves; ++w) r.m = fmaxf(r.m, all[w * 16 * FN + at].m);
+    for (int w = 0; w < waves; ++w) {
+        const Part q = all[w * 16 * FN + at];
+        r.s += q.s * factor(q.m, reference(r.m), scale(at));
+    }
+    return r;
+}
+
+// What the n parts of a row give, M and ln S, to the first of its 256 threads.
 __device__ __forceinline__ Part join_row(const Part *part, int n, float beta) {
-    const int lane = (int)threadIdx.x & 63;
+    __shared__ float tops[4];
+    __shared__ double sums[4];
+    constexpr int kHeld = 4;
+    const int t = (int)threadIdx.x, wave = t >> 6;
+    Part held[kHeld];  // read once, all at a time
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = i * 256 + t < n ? part[i * 256 + t] : Part{-INFINITY, 0.0f};
     float m = -INFINITY;
-    for (int t = lane; t < n; t += 64) m = fmaxf(m, part[t].m);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) m = fmaxf(m, held[i].m);
+    for (int i = kHeld * 256 + t; i < n; i += 256) m = fmaxf(m, part[i].m);
     m = rows::wave_max(m);
+    if ((t & 63) == 0) tops[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     const float ref = reference(m), c = beta * rows::kLog2e;
     double s = 0.0;
-    for (int t = lane; t < n; t += 64) {
-        const Part p = part[t];
-        s += (double)p.s * (double)exp2f((reference(p.m) - ref) * c);
-    }
+    const auto add = [&](const Part &p) { s += (double)p.s * (double)exp2f(fminf((reference(p.m) - ref) * c, 0.0f)); };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) add(held[i]);
+    for (int i = kHeld * 256 + t; i < n; i += 256) add(part[i]);
     s = rows::wave_sum(s);
+    if ((t & 63) == 0) sums[wave] = s;
+    __syncthreads();
+    s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     return {m, m == -INFINITY && s == 0.0 ? 0.0f : (float)log(s)};
 }
 

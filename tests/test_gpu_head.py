@@ -100,6 +100,19 @@ def test_large_and_small_values():
             check_backward(700, x, w, ids, got.stats, g, q, beta, name)
 
 
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+@pytest.mark.parametrize("n", [3, 20, 40, 100, 200])
+@pytest.mark.parametrize("v,h", [(129, 64), (257, 64), (1000, 64), (1000, 63)])
+def test_logits_all_far_from_zero(n, v, h, sign):
+    """Sets without a logit (a tile's masked end) beside sums relative to a largest logit of minus two thousand."""
+    x, w, ids, _ = uh.operands(n, v, h, "bf16")
+    x[:, 0], w[:, 0] = sign * 100.0, 20.0
+    g, _ = weights(n)
+    got = check_forward(v, x, w, ids, None, "bf16")
+    assert bool((got.stats[:, 0].abs() > 1900).all())
+    check_backward(v, x, w, ids, got.stats, g, None, None, "bf16")
+
+
 @pytest.mark.parametrize("name", ["bf16", "f16", "f32"])
 def test_rows_without_a_weight_are_not_read(name):
     n, v, h = 300, 450, 80

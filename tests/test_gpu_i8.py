@@ -139,6 +139,10 @@ def test_log_sum_exp_of_rows_of_every_kind():
     good = torch.ones(140, dtype=torch.bool)
     good[bad] = False
     assert bool(torch.isnan(got[bad]).all()) and torch.equal(got[good], want[good]) and bool(torch.isnan(out[3]).all())
+    # all logits far below zero
+    low = torch.full((300,), -5000.0, device="cuda")
+    for n in (3, 20, 40, 100, 140):
+        check_matmul(x[:n], scales(n, 3, 0.01), w, ws, low, "f32", lse=True)
     # equal logits: ln of their number
     zero = torch.zeros_like(x)
     _, got = tt.matmul_i8(zero, torch.ones(140, device="cuda"), w, ws, lse=True)
