@@ -113,6 +113,24 @@ __global__ __launch_bounds__(Any::THREADS) void head_parts_any(Side w, Side x, c
     parts_of_tile<DT, Any>(w, x, m0, n0, acc, inv_temp, ids, parts, gridDim.x, token, lds);
 }
 
+// Up to 16 rows.
+template <int DT>
+__global__ __launch_bounds__(kThinThreads, 4) void head_parts_few(Side w, Side x, const float *inv_temp, const int32_t *ids, Part *parts, float *token) {
+    __shared__ __attribute__((aligned(16))) char lds[kThinLds];
+    __shared__ float sums[8][2][256];
+    const int n = (int)threadIdx.x >> 5;
+    const float c = (n < x.rows ? rows::scale_of(inv_temp, n) : 1.0f) * rows::kLog2e;
+    const int id = ids && n < x.rows ? ids[n] : -1;
+    Part p = {-INFINITY, 0.0f};
+    product_few<DT>(w, x, lds, sums, [&](int m, int, float z) {
+        if (m >= w.rows) return;
+        if (m == id) token[n] = z;
+        add_part(p, z, c);
+    });
+    p = join_half(p, c);
+    if (((int)threadIdx.x & 31) == 0 && n < x.rows) parts[(int64_t)n * gridDim.x + blockIdx.x] = p;
+}
+
 // Few rows: every workgroup's part of them.
 template <int DT, int FN>
 __global__ __launch_bounds__(kThinThreads, 4) void head_parts_thin(Side w, Side x, const float *inv_temp, const int32_t *ids, Part *parts, float *token) {
@@ -346,7 +364,7 @@ struct Layout {
 struct ForwardLayout : Layout {
     size_t parts, token;
     ForwardLayout(int64_t n, int64_t v) {
-        parts = take((size_t)(n * tiles_of(v, Any::TM)) * sizeof(Part));
+        parts = take(most_parts(n, v) * sizeof(Part));
         token = take((size_t)n * 4);
     }
 };
@@ -413,10 +431,10 @@ int forward(const HeadArgs &a, char *ws, hipStream_t stream) {
     const Side w = matrix(a.weight, a.w_ld, a.v, a.h, e);
     int n_tiles = (int)tiles_of(a.v, kTile);
     if (a.n_rows <= kThinMost) {
-        n_tiles = (int)std::min<int64_t>(kThinGroups, tiles_of(a.v, kThinRows));
+        n_tiles = thin_groups(a.n_rows, a.v);
         const Side x = matrix(a.hidden, a.x_ld, a.n_rows, a.h, e);
         const auto run = [&](auto kernel) { kernel<<<n_tiles, kThinThreads, 0, stream>>>(w, x, a.inv_temp, ids, parts, token); };
-        if (a.n_rows <= 16) run(head_parts_thin<DT, 1>);
+        if (a.n_rows <= kFewMost) run(head_parts_few<DT>);
         else if (a.n_rows <= 32) run(head_parts_thin<DT, 2>);
         else run(head_parts_thin<DT, 4>);
     } else if (whole_steps(w) && whole_steps(matrix(a.hidden, a.x_ld, a.n_rows, a.h, e))) {

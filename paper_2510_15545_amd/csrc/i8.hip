@@ -183,6 +183,31 @@ __global__ __launch_bounds__(Any::THREADS) void product_i8_any(Side w, Side x, S
     finish_tile<DT, LSE, Any>(w, x, m0, n0, acc, scales, out, out_ld, parts, gridDim.x, lds);
 }
 
+// Up to 16 rows.
+template <int DT, bool LSE>
+__global__ __launch_bounds__(kThinThreads, 4) void product_i8_few(Side w, Side x, Scales scales, void *out, int64_t out_ld, Part *parts) {
+    __shared__ __attribute__((aligned(16))) char lds[kThinLds];
+    __shared__ float sums[8][2][256];
+    using T = typename rows::Elem<DT>::T;
+    const int column = (int)threadIdx.x >> 5;
+    const bool there = column < x.rows;
+    const float c = LSE && there ? rows::scale_of(scales.inv_temp, column) * rows::kLog2e : 0.0f, sx = there ? scales.x[column] : 0.0f;
+    T *row = static_cast<T *>(out) + column * out_ld;
+    Part p = {-INFINITY, 0.0f};
+    product_few<kI8>(w, x, lds, sums, [&](int m, int, int sum) {
+        if (!there || m >= w.rows) return;
+        float y = (float)sum * sx * scales.w[m];
+        if (scales.bias) y += scales.bias[m];
+        const uint32_t bits = rows::encode<DT>(y);
+        row[m] = (T)bits;
+        if constexpr (LSE) add_part(p, rows::decode<DT>(bits), c);  // of the results as they are written
+    });
+    if constexpr (LSE) {
+        p = join_half(p, c);
+        if (((int)threadIdx.x & 31) == 0 && there) parts[(int64_t)column * gridDim.x + blockIdx.x] = p;
+    }
+}
+
 // Few rows.
 template <int DT, bool LSE, int FN>
 __global__ __launch_bounds__(kThinThreads, 4) void product_i8_thin(Side w, Side x, Scales scales, void *out, int64_t out_ld, Part *parts) {
@@ -242,10 +267,10 @@ int multiply(const MatmulI8Args &a, Part *parts, hipStream_t stream) {
     const int64_t e = rows::element_bytes(DT);
     int n_tiles = (a.n_cols + 255) / 256;
     if (a.n_rows <= kThinMost) {
-        n_tiles = std::min(kThinGroups, (a.n_cols + kThinRows - 1) / kThinRows);
+        n_tiles = thin_groups(a.n_rows, a.n_cols);
         const Scales scales = {a.x_scale, a.w_scale, a.bias, a.inv_temp};
         const auto run = [&](auto kernel) { kernel<<<n_tiles, kThinThreads, 0, stream>>>(w, x, scales, a.out, a.out_ld, parts); };
-        if (a.n_rows <= 16) run(product_i8_thin<DT, LSE, 1>);
+        if (a.n_rows <= kFewMost) run(product_i8_few<DT, LSE>);
         else if (a.n_rows <= 32) run(product_i8_thin<DT, LSE, 2>);
         else run(product_i8_thin<DT, LSE, 4>);
     } else if (whole_steps(w) && whole_steps(x)) {
@@ -284,7 +309,7 @@ int launch_quantize_i8(const QuantizeI8Args &a, hipStream_t stream) {
 }
 
 size_t matmul_i8_workspace_bytes(int32_t n_rows, int32_t n_cols, bool lse) {
-    return lse ? round256((size_t)n_rows * ((n_cols + Any::TM - 1) / Any::TM) * sizeof(Part)) : 0;
+    return lse ? round256(most_parts(n_rows, n_cols) * sizeof(Part)) : 0;
 }
 
 int launch_matmul_i8(const MatmulI8Args &a, void *workspace, size_t workspace_bytes, hipStream_t stream) {
