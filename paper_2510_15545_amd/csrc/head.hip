@@ -117,8 +117,8 @@ __global__ __launch_bounds__(Any::THREADS) void head_parts_any(Side w, Side x, c
 template <int DT>
 __global__ __launch_bounds__(kThinThreads, 4) void head_parts_few(Side w, Side x, const float *inv_temp, const int32_t *ids, Part *parts, float *token) {
     __shared__ __attribute__((aligned(16))) char lds[kThinLds];
-    __shared__ float sums[8][2][256];
-    const int n = (int)threadIdx.x >> 5;
+    __shared__ float sums[8][256];
+    const int n = (int)threadIdx.x >> 4;
     const float c = (n < x.rows ? rows::scale_of(inv_temp, n) : 1.0f) * rows::kLog2e;
     const int id = ids && n < x.rows ? ids[n] : -1;
     Part p = {-INFINITY, 0.0f};
@@ -127,8 +127,8 @@ __global__ __launch_bounds__(kThinThreads, 4) void head_parts_few(Side w, Side x
         if (m == id) token[n] = z;
         add_part(p, z, c);
     });
-    p = join_half(p, c);
-    if (((int)threadIdx.x & 31) == 0 && n < x.rows) parts[(int64_t)n * gridDim.x + blockIdx.x] = p;
+    p = join_quarter(p, c);
+    if (((int)threadIdx.x & 15) == 0 && n < x.rows) parts[(int64_t)n * gridDim.x + blockIdx.x] = p;
 }
 
 // Few rows: every workgroup's part of them.

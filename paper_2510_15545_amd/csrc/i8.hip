@@ -187,9 +187,9 @@ __global__ __launch_bounds__(Any::THREADS) void product_i8_any(Side w, Side x, S
 template <int DT, bool LSE>
 __global__ __launch_bounds__(kThinThreads, 4) void product_i8_few(Side w, Side x, Scales scales, void *out, int64_t out_ld, Part *parts) {
     __shared__ __attribute__((aligned(16))) char lds[kThinLds];
-    __shared__ float sums[8][2][256];
+    __shared__ float sums[8][256];
     using T = typename rows::Elem<DT>::T;
-    const int column = (int)threadIdx.x >> 5;
+    const int column = (int)threadIdx.x >> 4;
     const bool there = column < x.rows;
     const float c = LSE && there ? rows::scale_of(scales.inv_temp, column) * rows::kLog2e : 0.0f, sx = there ? scales.x[column] : 0.0f;
     T *row = static_cast<T *>(out) + column * out_ld;
@@ -203,8 +203,8 @@ __global__ __launch_bounds__(kThinThreads, 4) void product_i8_few(Side w, Side x
         if constexpr (LSE) add_part(p, rows::decode<DT>(bits), c);  // of the results as they are written
     });
     if constexpr (LSE) {
-        p = join_half(p, c);
-        if (((int)threadIdx.x & 31) == 0 && there) parts[(int64_t)column * gridDim.x + blockIdx.x] = p;
+        p = join_quarter(p, c);
+        if (((int)threadIdx.x & 15) == 0 && there) parts[(int64_t)column * gridDim.x + blockIdx.x] = p;
     }
 }
 

@@ -434,15 +434,15 @@ __device__ __forceinline__ void product_thin(const Side &w, const Side &x, char 
     }
 }
 
-// Up to 16 rows of the second operand: 32 rows of the first to a workgroup, whose 8 waves lie side by side along k, 128 bytes of a
+// Up to 16 rows of the second operand: 16 rows of the first to a workgroup, whose 8 waves lie side by side along k, 128 bytes of a
 // row each, so that 1 KB of a row is read at a time (the same bytes 16 rows by 64 bytes a wave come at 5.2 TB/s, these at 5.9 to
 // 6.1, read in order at 6.8).  Loads roll: what has been multiplied makes room for the same place of the next 4 KB.  The waves'
-// sums are joined in LDS; then thread t has row t % 32 and column t / 32.
-constexpr int kFewMost = 16, kFewRows = 32, kFewBatch = 4096;
+// sums are joined in LDS; then thread t (of 256) has row t % 16 and column t / 16.
+constexpr int kFewMost = 16, kFewRows = 16, kFewBatch = 4096;
 
 // finish(m, n, y): one result.
 template <int DT, typename F>
-__device__ __forceinline__ void product_few(const Side &w, const Side &x, char *lds, float (*sums)[2][256], F finish) {
+__device__ __forceinline__ void product_few(const Side &w, const Side &x, char *lds, float (*sums)[256], F finish) {
     typedef typename Mfma<DT>::Acc Acc;
     constexpr int U = 8;
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, quarter = lane >> 4;
@@ -451,27 +451,23 @@ __device__ __forceinline__ void product_few(const Side &w, const Side &x, char *
     const int r = min(lane & 15, x.rows - 1), inside = wave * 128 + quarter * 16;  // of a KB
     const char *column = lds + r * chunk;
     const int turn = (quarter ^ (r & 7)) * 16;
-    u4 f[2][U];
-    const auto row_of = [&](int g, int i) { return w.p + (int64_t)min(g * kFewRows + i * 16 + (lane & 15), w.rows - 1) * w.ld; };
+    u4 f[U];
+    const auto row_of = [&](int g) { return w.p + (int64_t)min(g * kFewRows + (lane & 15), w.rows - 1) * w.ld; };
     const auto load = [&](const char *row, int b, int u) {
         const int at = b * kFewBatch + (u >> 1) * 1024 + (u & 1) * 64 + inside;
         if ((b + 1) * kFewBatch <= w.bytes) return (u4)rows::load_global<true>(row + at);
         const int left = w.bytes - at;
         return left >= 16 ? (u4)*reinterpret_cast<const u4b *>(row + at) : left > 0 ? load_some(row + at, left) : u4{0, 0, 0, 0};
     };
-    const auto load_batch = [&](int g, int b) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const char *row = row_of(g, i);
-#pragma unroll
-            for (int u = 0; u < U; ++u) f[i][u] = load(row, b, u);
-        }
-    };
     int g = (int)blockIdx.x;
-    if (g < groups) load_batch(g, 0);
+    if (g < groups) {
+        const char *row = row_of(g);
+#pragma unroll
+        for (int u = 0; u < U; ++u) f[u] = load(row, 0, u);
+    }
     int staged = -1;  // the chunk in LDS
     for (; g < groups; g += (int)gridDim.x) {
-        Acc acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+        Acc acc = {0, 0, 0, 0};
         for (int b = 0; b < batches; ++b) {
             const int k0 = b * kFewBatch / chunk * chunk;
             if (staged != k0) {
@@ -489,7 +485,7 @@ __device__ __forceinline__ void product_few(const Side &w, const Side &x, char *
             const bool more = b + 1 < batches;
             const int next_g = more ? g : g + (int)gridDim.x, next_b = more ? b + 1 : 0;
             const bool any = next_g < groups;
-            const char *next[2] = {row_of(min(next_g, groups - 1), 0), row_of(min(next_g, groups - 1), 1)};
+            const char *next = row_of(min(next_g, groups - 1));
             const char *at = column + (b * kFewBatch - k0) + wave * 128;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -497,34 +493,32 @@ __device__ __forceinline__ void product_few(const Side &w, const Side &x, char *
                 const int here = (u >> 1) * 1024 + (u & 1) * 64;
                 const bool inside_chunk = b * kFewBatch - k0 + wave * 128 + here < chunk;
                 const u4 y = inside_chunk ? *reinterpret_cast<const u4 *>(at + (u >> 1) * 1024 + (turn ^ (u & 1) * 64)) : u4{0, 0, 0, 0};
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    acc[i] = Mfma<DT>::run(f[i][u], y, acc[i]);
-                    if (any) f[i][u] = load(next[i], next_b, u);
-                }
+                acc = Mfma<DT>::run(f[u], y, acc);
+                if (any) f[u] = load(next, next_b, u);
             }
         }
-        // [wave][half][row][column]
+        // [wave][row][column], row r's columns turned by r
         __syncthreads();  // the sums before are read
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if constexpr (DT == kI8) sums[wave][i][(quarter * 4 + q) * 16 + (lane & 15)] = __int_as_float(acc[i][q]);
-                else sums[wave][i][(quarter * 4 + q) * 16 + (lane & 15)] = acc[i][q];
-            }
+        for (int q = 0; q < 4; ++q) {
+            const int m = quarter * 4 + q, to = m * 16 + ((lane + m) & 15);
+            if constexpr (DT == kI8) sums[wave][to] = __int_as_float(acc[q]);
+            else sums[wave][to] = acc[q];
+        }
         __syncthreads();
-        const int m = (int)threadIdx.x & 31, n = (int)threadIdx.x >> 5;
-        if constexpr (DT == kI8) {
-            int y = 0;
+        if (threadIdx.x < 256) {
+            const int m = (int)threadIdx.x & 15, n = (int)threadIdx.x >> 4, from = m * 16 + ((n + m) & 15);
+            if constexpr (DT == kI8) {
+                int y = 0;
 #pragma unroll
-            for (int v = 0; v < 8; ++v) y += __float_as_int(sums[v][m >> 4][(m & 15) * 16 + n]);
-            finish(g * kFewRows + m, n, y);
-        } else {
-            float y = 0.0f;
+                for (int v = 0; v < 8; ++v) y += __float_as_int(sums[v][from]);
+                finish(g * kFewRows + m, n, y);
+            } else {
+                float y = 0.0f;
 #pragma unroll
-            for (int v = 0; v < 8; ++v) y += sums[v][m >> 4][(m & 15) * 16 + n];
-            finish(g * kFewRows + m, n, y);
+                for (int v = 0; v < 8; ++v) y += sums[v][from];
+                finish(g * kFewRows + m, n, y);
+            }
         }
     }
 }
@@ -655,14 +649,14 @@ __device__ __forceinline__ void add_part(Part &p, float z, float c) {
     p.m = m;
 }
 
-// The part of 32 lanes that hold one column's.
-__device__ __forceinline__ Part join_half(Part p, float c) {
+// The part of 16 lanes that hold one column's.
+__device__ __forceinline__ Part join_quarter(Part p, float c) {
     float m = p.m;
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    for (int d = 1; d < 16; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
     float s = p.s * factor(p.m, reference(m), c);
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) s += __shfl_xor(s, d);
+    for (int d = 1; d < 16; d *= 2) s += __shfl_xor(s, d);
     return {m, s};
 }
 
