@@ -11,6 +11,7 @@
 // fp32, over all pieces) and the piece's rows of dW, written once.  Of these three products' operands dz, W and x each is kept
 // as it is, whichever of its indices is summed over (tiles.h).  No atomics: results do not depend on scheduling.
 #include <algorithm>
+#include <type_traits>
 
 #include "tiles.h"
 
@@ -31,8 +32,16 @@ constexpr int kRowsPerLaunch = 1 << 15;
 __host__ __device__ inline int64_t round_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
 __host__ __device__ constexpr int step_elements(int dtype) { return kStepBytes / bytes_of(dtype); }
 inline int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
-// Rows to a tile of a wide product, in units of 64.
-inline int columns_for(int64_t n, int dtype) { return n <= 128 || dtype == TT_F32 ? 2 : 4; }
+// f(FN as a constant) for the columns of the type's wide tiles: fp32 ones are bound by the matrix cores at any width, and
+// wider ones would not fit the registers.
+inline int columns_for(int64_t n, int dtype) { return dtype == TT_F32 ? 2 : tiles::columns_for(n); }
+template <int DT, typename F>
+void with_columns(int64_t n, F f) {
+    if constexpr (DT == TT_F32) f(std::integral_constant<int, 2>());
+    else if (columns_for(n, DT) == 2) f(std::integral_constant<int, 2>());
+    else if (columns_for(n, DT) == 3) f(std::integral_constant<int, 3>());
+    else f(std::integral_constant<int, 4>());
+}
 
 // A row that carries a weight, for the gradient's epilogue: p = 2^((z - m) c - l), dz = (w - g) p, and g (1 - p) + w p at
 // its token; padding rows are zeros.
@@ -72,11 +81,11 @@ __device__ __forceinline__ void parts_of_tile(const Side &w, const Side &x, int 
     if (ids)
         for_columns<S>(n0, [&](int n, int j) {
             const int at = n < n_rows ? ids[n] : -1;
-            if (at < w.rows)
+            if (__any(at >= m0 && at < m0 + S::TM && at < w.rows))
                 for_rows<S>(m0, [&](int m, int i) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        if (at == m + q) token[n] = acc[i][j][q];
+                        if (at == m + q && at < w.rows) token[n] = acc[i][j][q];
                 });
         });
     if (m0 + S::TM > w.rows)
@@ -441,14 +450,11 @@ int forward(const HeadArgs &a, char *ws, hipStream_t stream) {
         for (int64_t n0 = 0; n0 < a.n_rows; n0 += kRowsPerLaunch) {
             const int64_t n = std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0);
             const Side x = matrix(static_cast<const char *>(a.hidden) + n0 * a.x_ld * e, a.x_ld, n, a.h, e);
-            const int fn = columns_for(n, DT), nt = (int)tiles_of(n, 64 * fn);
-            const auto run = [&](auto kernel) {
-                kernel<<<(unsigned int)(n_tiles * nt), 512, 0, stream>>>(w, x, n_tiles, nt, a.inv_temp ? a.inv_temp + n0 : nullptr, ids ? ids + n0 : nullptr,
-                                                                      parts + n0 * n_tiles, token + n0);
-            };
-            if constexpr (DT == TT_F32) run(head_parts<DT, 2>);
-            else if (fn == 2) run(head_parts<DT, 2>);
-            else run(head_parts<DT, 4>);
+            with_columns<DT>(n, [&](auto fn) {
+                const int nt = (int)tiles_of(n, 64 * fn);
+                head_parts<DT, fn><<<(unsigned int)(n_tiles * nt), 512, 0, stream>>>(w, x, n_tiles, nt, a.inv_temp ? a.inv_temp + n0 : nullptr,
+                                                                                  ids ? ids + n0 : nullptr, parts + n0 * n_tiles, token + n0);
+            });
         }
     } else {
         n_tiles = (int)tiles_of(a.v, Any::TM);
@@ -501,9 +507,7 @@ int backward(const HeadGradArgs &a, char *ws, hipStream_t stream) {
                                         reinterpret_cast<Row *>(ws + lay.meta), totals);
     copy_rows(a.hidden, a.x_ld, a.n_rows, a.h, e, list, totals, ws + lay.x, lay.width, stream);
     for (int64_t v0 = 0; v0 < a.v; v0 += lay.piece) {
-        if constexpr (DT == TT_F32) backward_piece<DT, 2>(a, lay, ws, v0, copy_w, stream);
-        else if (columns_for(a.n_rows, DT) == 2) backward_piece<DT, 2>(a, lay, ws, v0, copy_w, stream);
-        else backward_piece<DT, 4>(a, lay, ws, v0, copy_w, stream);
+        with_columns<DT>(a.n_rows, [&](auto fn) { backward_piece<DT, fn>(a, lay, ws, v0, copy_w, stream); });
     }
     if (a.dhidden)
         head_place<DT><<<dim3(a.n_rows, (unsigned int)((a.h + 255) / 256)), 256, 0, stream>>>(reinterpret_cast<float *>(ws + lay.sums), lay.width,

@@ -275,7 +275,7 @@ int multiply(const MatmulI8Args &a, Part *parts, hipStream_t stream) {
         else run(product_i8_thin<DT, LSE, 4>);
     } else if (whole_steps(w) && whole_steps(x)) {
         for (int64_t n0 = 0; n0 < a.n_rows; n0 += kRowsPerLaunch) {
-            const int n = (int)std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0), fn = n <= 128 ? 2 : 4, nt = (n + 64 * fn - 1) / (64 * fn);
+            const int n = (int)std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0), fn = columns_for(n), nt = (n + 64 * fn - 1) / (64 * fn);
             const Side part = {x.p + n0 * x.ld, x.ld, n, x.bytes};
             const Scales scales = {a.x_scale + n0, a.w_scale, a.bias, a.inv_temp ? a.inv_temp + n0 : nullptr};
             const auto run = [&](auto kernel) {
@@ -283,6 +283,7 @@ int multiply(const MatmulI8Args &a, Part *parts, hipStream_t stream) {
                                                                       parts + n0 * n_tiles);
             };
             if (fn == 2) run(product_i8<DT, LSE, 2>);
+            else if (fn == 3) run(product_i8<DT, LSE, 3>);
             else run(product_i8<DT, LSE, 4>);
         }
     } else {

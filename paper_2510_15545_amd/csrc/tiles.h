@@ -269,7 +269,7 @@ template <int DT, bool AKM, bool BKM, int FN>
 struct Product {
 static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0, int n0, int step0, int steps, char *a0, char *a1, char *b0, char *b1,
                                            typename Mfma<DT>::Acc (&acc)[8][FN]) {
-    constexpr int H = FN / 2;
+    constexpr int H0 = FN / 2, H1 = FN - H0;  // of a wave's columns
     Operand<DT, AKM, 256> oa;
     Operand<DT, BKM, 64 * FN> ob;
 #pragma unroll
@@ -280,23 +280,23 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
     oa.begin(a, m0, step0);
     ob.begin(b, n0, step0);
     const int wm = oa.wave >> 2, wn = oa.wave & 3;
-    u4 fa0[4][2], fa1[4][2], fb0[H][2], fb1[H][2];
+    u4 fa0[4][2], fa1[4][2], fb0[H0][2], fb1[H1][2];
     const auto read_a = [&](u4 (&f)[4][2], const char *tile, int half) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) oa.read(f[i], tile, wm * 2 + half, i);
     };
-    const auto read_b = [&](u4 (&f)[H][2], const char *tile, int half) {
+    const auto read_b = [&](auto &f, const char *tile, int from) {
 #pragma unroll
-        for (int j = 0; j < H; ++j) ob.read(f[j], tile, wn, half * H + j);
+        for (int j = 0; j < (int)(sizeof f / sizeof f[0]); ++j) ob.read(f[j], tile, wn, from + j);
     };
-    const auto multiply = [&](const u4 (&f)[4][2], const u4 (&g)[H][2], int ah, int bh) {
+    const auto multiply = [&](const u4 (&f)[4][2], const auto &g, int ah, int from) {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < H; ++j) acc[ah * 4 + i][bh * H + j] = Mfma<DT>::run(f[i][k], g[j][k], acc[ah * 4 + i][bh * H + j]);
+                for (int j = 0; j < (int)(sizeof g / sizeof g[0]); ++j) acc[ah * 4 + i][from + j] = Mfma<DT>::run(f[i][k], g[j][k], acc[ah * 4 + i][from + j]);
         __builtin_amdgcn_s_setprio(0);
     };
     const auto wait_reads = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };
@@ -324,16 +324,16 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
         barrier();
         multiply(fa0, fb0, 0, 0);
         barrier();
-        read_b(fb1, bt, 1);
+        read_b(fb1, bt, H0);
         wait_reads();
         barrier();
-        multiply(fa0, fb1, 0, 1);
+        multiply(fa0, fb1, 0, H0);
         barrier();
         read_a(fa1, at, 1);
         wait_reads();
         wait_loads();  // the next step's
         barrier();
-        multiply(fa1, fb1, 1, 1);
+        multiply(fa1, fb1, 1, H0);
         barrier();
         if (t + 1 < steps) read_a(fa0, an, 0);
         if (t + 2 < steps) {
@@ -521,6 +521,13 @@ __device__ __forceinline__ void product_few(const Side &w, const Side &x, char *
             }
         }
     }
+}
+
+// Columns of a wide product's tiles in units of 64, for n rows of the second operand: as few tiles as 256 columns give, and no
+// wider than they need (333 rows: 2 x 192, not 2 x 256).
+inline int columns_for(int64_t n) {
+    const int64_t tiles = (n + 255) / 256, columns = ((n + tiles - 1) / tiles + 63) / 64;
+    return columns < 2 ? 2 : (int)columns;
 }
 
 // Workgroups of a product with few rows, for n rows of the second operand and m of the first: a part each of every row.
