@@ -260,16 +260,14 @@ struct Operand {
 // The tile at (m0, n0) of the product over the steps [step0, step0 + steps).  Needs 16-byte aligned rows; k contiguous: whole
 // steps of 128 bytes; 256 rows within 2^31 bytes, KM: all of the steps' lines.
 //
-// Waves 0-3 hold the upper half of the 256 rows, 4-7 the lower one; every SIMD runs one of each.  A step is four pieces of
-// 64 x 8 FN (of a wave): reads from LDS, barrier, matrix instructions, barrier.  The second half's waves are one barrier
-// behind, so that on every SIMD one wave's reads lie beside the other's matrix instructions.  Reads of a step's first rows are
-// done in the last piece of the step before, and there the loads for the step after next begin, into the memory that was
-// read last; they have a whole step's time.  LDS is read at 75% of its rate.
+// Waves 0-3 hold half of the blocks of 16 rows, 4-7 the other half; every SIMD runs one of each.  A step is two pieces of
+// 64 x 16 FN (of a wave): reads from LDS, barrier, matrix instructions, barrier.  The second half's waves are one barrier
+// behind, so that on every SIMD one wave's reads lie beside the other's matrix instructions.  The loads for the step after
+// next begin where the next step does, into the memory that was read last, and have that step's time.
 template <int DT, bool AKM, bool BKM, int FN>
 struct Product {
 static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0, int n0, int step0, int steps, char *a0, char *a1, char *b0, char *b1,
                                            typename Mfma<DT>::Acc (&acc)[8][FN]) {
-    constexpr int H0 = FN / 2, H1 = FN - H0;  // of a wave's columns
     Operand<DT, AKM, 256> oa;
     Operand<DT, BKM, 64 * FN> ob;
 #pragma unroll
@@ -280,23 +278,23 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
     oa.begin(a, m0, step0);
     ob.begin(b, n0, step0);
     const int wm = oa.wave >> 2, wn = oa.wave & 3;
-    u4 fa0[4][2], fa1[4][2], fb0[H0][2], fb1[H1][2];
-    const auto read_a = [&](u4 (&f)[4][2], const char *tile, int half) {
+    u4 fa[4][2], fb[FN][2];
+    const auto read_a = [&](const char *tile, int half) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) oa.read(f[i], tile, wm * 2 + half, i);
+        for (int i = 0; i < 4; ++i) oa.read(fa[i], tile, wm * 2 + half, i);
     };
-    const auto read_b = [&](auto &f, const char *tile, int from) {
+    const auto read_b = [&](const char *tile) {
 #pragma unroll
-        for (int j = 0; j < (int)(sizeof f / sizeof f[0]); ++j) ob.read(f[j], tile, wn, from + j);
+        for (int j = 0; j < FN; ++j) ob.read(fb[j], tile, wn, j);
     };
-    const auto multiply = [&](const u4 (&f)[4][2], const auto &g, int ah, int from) {
+    const auto multiply = [&](int half) {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < (int)(sizeof g / sizeof g[0]); ++j) acc[ah * 4 + i][from + j] = Mfma<DT>::run(f[i][k], g[j][k], acc[ah * 4 + i][from + j]);
+                for (int j = 0; j < FN; ++j) acc[half * 4 + i][j] = Mfma<DT>::run(fa[i][k], fb[j][k], acc[half * 4 + i][j]);
         __builtin_amdgcn_s_setprio(0);
     };
     const auto wait_reads = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };
@@ -308,49 +306,34 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
     };
     oa.fetch(a0, 0);
     ob.fetch(b0, 0);
-    if (steps > 1) {
-        oa.fetch(a1, 1);
-        ob.fetch(b1, 1);
-        __builtin_amdgcn_s_waitcnt(0x0f70 | (4 + FN));  // the first step's
-    } else {
-        wait_loads();
-    }
+    wait_loads();
     barrier();
-    read_a(fa0, a0, 0);
     if (wm == 1) barrier();
-    const auto step = [&](char *at, char *bt, const char *an, int t) {
-        read_b(fb0, bt, 0);
-        wait_reads();
-        barrier();
-        multiply(fa0, fb0, 0, 0);
-        barrier();
-        read_b(fb1, bt, H0);
-        wait_reads();
-        barrier();
-        multiply(fa0, fb1, 0, H0);
-        barrier();
-        read_a(fa1, at, 1);
-        wait_reads();
-        wait_loads();  // the next step's
-        barrier();
-        multiply(fa1, fb1, 1, H0);
-        barrier();
-        if (t + 1 < steps) read_a(fa0, an, 0);
-        if (t + 2 < steps) {
-            oa.fetch(at, t + 2);
-            ob.fetch(bt, t + 2);
+    const auto step = [&](const char *at, const char *bt, char *an, char *bn, int t) {
+        read_b(bt);
+        read_a(at, 0);
+        if (t + 1 < steps) {
+            oa.fetch(an, t + 1);
+            ob.fetch(bn, t + 1);
         }
         wait_reads();
         barrier();
-        multiply(fa1, fb0, 1, 0);
+        multiply(0);
+        barrier();
+        read_a(at, 1);
+        wait_reads();
+        if (wm == 1) wait_loads();
+        barrier();
+        multiply(1);
+        if (wm == 0) wait_loads();
         barrier();
     };
     int t = 0;
     for (; t + 1 < steps; t += 2) {
-        step(a0, b0, a1, t);
-        step(a1, b1, a0, t + 1);
+        step(a0, b0, a1, b1, t);
+        step(a1, b1, a0, b0, t + 1);
     }
-    if (t < steps) step(a0, b0, a1, t);
+    if (t < steps) step(a0, b0, a1, b1, t);
     if (wm == 0) barrier();
     __syncthreads();
 }
