@@ -26,7 +26,8 @@ constexpr int kAlign = 256;  // rows, tokens and pieces of the vocabulary in a w
 typedef Shape<128, 128, 2, 2> Any;  // of the products of matrices that lie in any way
 
 constexpr int64_t kSplitTiles = 256;  // workgroups that the sum over a piece's tokens is split into at most
-constexpr int64_t kPieceBytes = int64_t(160) << 20;  // what a piece of the vocabulary may take of the workspace
+constexpr int64_t kPieceBytes = int64_t(256) << 20;  // what a piece of the vocabulary may take of the workspace
+constexpr int64_t kCus = 256;
 constexpr int kRowsPerLaunch = 1 << 15;
 
 __host__ __device__ inline int64_t round_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
@@ -260,34 +261,30 @@ __global__ __launch_bounds__(512) void head_dlogits(Side w, Side x, int mt, int 
     n0 *= S::TN;
     if (n0 >= totals->rows) return;
     Product<DT, false, false, FN>::run(w, x, m0, n0, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
-    for_columns<S>(n0, [&](int n, int j) {
-        const Row r = meta[n];
-        T *row = reinterpret_cast<T *>(d) + (int64_t)n * d_ld;
-        const int id = r.id - v0;
-        const float f = r.w - r.g;
-        // the exponential's argument; at the row's token what is left of 1 beside p, not 1 - p
-        const auto exponent = [&](float z) { return fmaf(z - r.m, r.c, -r.l); };
-        if (__any(id >= m0 && id < m0 + S::TM) || m0 + S::TM > w.rows) {
-            for_rows<S>(m0, [&](int m, int i) {
-                float y[4];
+    Row r[FN];
+    for_columns<S>(n0, [&](int n, int j) { r[j] = meta[n]; });
+    bool special = m0 + S::TM > w.rows;  // the piece's end, or a row's token
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float e = exponent(acc[i][j][q]), p = __builtin_amdgcn_exp2f(e);
-                    y[q] = f * p;
-                    if (m + q == id) y[q] = r.g * -expm1f(e * (float)rows::kLn2) + r.w * p;
-                    if (m + q >= w.rows) y[q] = 0.0f;
-                }
-                store4<DT>(row, m, (int)d_ld, y);
-            });
-        } else {
-            for_rows<S>(m0, [&](int m, int i) {
-                float y[4];
+    for (int j = 0; j < FN; ++j) special |= __any(r[j].id - v0 >= m0 && r[j].id - v0 < m0 + S::TM) != 0;
+    const auto to = [&](int n) { return reinterpret_cast<T *>(d) + (int64_t)n * d_ld; };
+    const auto exponent = [&](float z, int j) { return fmaf(z - r[j].m, r[j].c, -r[j].l); };
+    if (__syncthreads_or(special)) {
+        store_tile<DT, S>(m0, (int)d_ld, n0, INT_MAX, a0, a1, [&](int, int j, int m, int i, float (&y)[4]) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) y[q] = f * __builtin_amdgcn_exp2f(exponent(acc[i][j][q]));
-                store4<DT>(row, m, (int)d_ld, y);
-            });
-        }
-    });
+            for (int q = 0; q < 4; ++q) {
+                const float e = exponent(acc[i][j][q], j), p = __builtin_amdgcn_exp2f(e);
+                y[q] = (r[j].w - r[j].g) * p;
+                if (v0 + m + q == r[j].id) y[q] = r[j].g * -expm1f(e * (float)rows::kLn2) + r[j].w * p;  // 1 - p not as a difference
+                if (m + q >= w.rows) y[q] = 0.0f;
+            }
+        }, to);
+    } else {
+        store_tile<DT, S>(m0, (int)d_ld, n0, INT_MAX, a0, a1, [&](int, int j, int, int i, float (&y)[4]) {
+            const float f = r[j].w - r[j].g;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = f * __builtin_amdgcn_exp2f(exponent(acc[i][j][q], j));
+        }, to);
+    }
 }
 
 // dx of the listed rows over one piece of the vocabulary, split into parts of its tokens, added to what the pieces before
@@ -321,15 +318,17 @@ template <int DT>
 __global__ __launch_bounds__(256) void head_place(const float *sums, int64_t ld, int64_t plane, int splits, const int32_t *place, const Totals *totals,
                                                   int h, void *dhidden, int64_t out_ld) {
     using T = typename rows::Elem<DT>::T;
-    const int n = (int)blockIdx.x, c = (int)(blockIdx.y * 256 + threadIdx.x);
+    const int n = (int)blockIdx.x, c = (int)(blockIdx.y * 256 + threadIdx.x) * 4;
     if (c >= h) return;
     const int at = place[n];
-    float y = 0.0f;
+    f4 y = {0, 0, 0, 0};
     if (at >= 0) {
-        for (int s = 0; s < splits; ++s) y += sums[s * plane + at * ld + c];
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s) y += *reinterpret_cast<const f4 *>(sums + s * plane + at * ld + c);
         y *= totals->scale;
     }
-    static_cast<T *>(dhidden)[n * out_ld + c] = (T)rows::encode<DT>(y);
+    const float z[4] = {y[0], y[1], y[2], y[3]};
+    store4<DT>(static_cast<T *>(dhidden) + n * out_ld, c, h, z);
 }
 
 // A piece's rows of dW.
@@ -346,14 +345,10 @@ __global__ __launch_bounds__(512) void head_dweight(Side x, Side d, int mt, int 
     const int steps = (totals->rows + step_elements(DT) - 1) / step_elements(DT);
     Product<DT, true, true, FN>::run(x, d, m0, n0, 0, steps, a0, a1, b0, b1, acc);
     const float scale = totals->scale;
-    for_columns<S>(n0, [&](int n, int j) {
-        if (n >= n_tokens) return;
-        T *row = static_cast<T *>(dweight) + (int64_t)n * ld;
-        for_rows<S>(m0, [&](int m, int i) {
-            const float y[4] = {acc[i][j][0] * scale, acc[i][j][1] * scale, acc[i][j][2] * scale, acc[i][j][3] * scale};
-            store4<DT>(row, m, h, y);
-        });
-    });
+    store_tile<DT, S>(m0, h, n0, n_tokens, a0, a1, [&](int, int j, int, int i, float (&y)[4]) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] = acc[i][j][q] * scale;
+    }, [&](int n) { return static_cast<T *>(dweight) + (int64_t)n * ld; });
 }
 
 __global__ __launch_bounds__(256) void head_zero(int h, int e, char *out, int64_t ld) {
@@ -388,6 +383,9 @@ struct BackwardLayout : Layout {
         width = round_to(h, step_elements(dtype));
         const int64_t row = (n_pad + width) * e;  // of dz and of the weights' copy, for a token
         piece = std::min(all, std::max<int64_t>(kAlign, kPieceBytes / row / kAlign * kAlign));
+        // pieces of one size, in whole rounds of the compute units where there are several
+        const int64_t round = std::max<int64_t>(1, kCus / row_tiles(n, dtype)) * kTile, even = round_to(tiles_of(all, tiles_of(all, piece)), kAlign);
+        if (piece < all) piece = std::min(piece, piece >= round ? std::min(round_to(even, round), piece / round * round) : even);
         splits = (int)std::min<int64_t>(std::max<int64_t>(1, kSplitTiles / (row_tiles(n, dtype) * tiles_of(width, kTile))), std::max<int64_t>(1, all / 1024));
         rows_of(n, e);
         d = take((size_t)(piece * n_pad * e));
@@ -510,7 +508,7 @@ int backward(const HeadGradArgs &a, char *ws, hipStream_t stream) {
         with_columns<DT>(a.n_rows, [&](auto fn) { backward_piece<DT, fn>(a, lay, ws, v0, copy_w, stream); });
     }
     if (a.dhidden)
-        head_place<DT><<<dim3(a.n_rows, (unsigned int)((a.h + 255) / 256)), 256, 0, stream>>>(reinterpret_cast<float *>(ws + lay.sums), lay.width,
+        head_place<DT><<<dim3(a.n_rows, (unsigned int)tiles_of(a.h, 1024)), 256, 0, stream>>>(reinterpret_cast<float *>(ws + lay.sums), lay.width,
                                                                                          lay.n_pad * lay.width, lay.splits, place, totals, a.h,
                                                                                          a.dhidden, a.dx_ld);
     return status();

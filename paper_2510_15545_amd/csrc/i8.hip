@@ -125,43 +125,30 @@ struct Scales {
     const float *x, *w, *bias, *inv_temp;
 };
 
-// A tile's results, and the parts of their rows' log-sum-exp.
-template <int DT, bool LSE, typename S>
-__device__ __forceinline__ void finish_tile(const Side &w, const Side &x, int m0, int n0, i4 (&acc)[S::FM][S::FN], const Scales &scales, void *out,
-                                            int64_t out_ld, Part *parts, int n_tiles, char *lds) {
-    using T = typename rows::Elem<DT>::T;
-    const int n_rows = x.rows;
-    float sw[S::FM][4], bias[S::FM][4];
-    for_rows<S>(m0, [&](int m, int i) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            sw[i][q] = m + q < w.rows ? scales.w[m + q] : 0.0f;
-            bias[i][q] = scales.bias && m + q < w.rows ? scales.bias[m + q] : 0.0f;
-        }
-    });
-    for_columns<S>(n0, [&](int n, int j) {
-        const float sx = n < n_rows ? scales.x[n] : 0.0f;
-        T *row = static_cast<T *>(out) + (int64_t)n * out_ld;
+// A tile's scales and biases of its rows m, for this thread's blocks.
+template <typename S>
+struct RowScales {
+    float w[S::FM][4], bias[S::FM][4];
+    __device__ __forceinline__ RowScales(const Scales &scales, int m0, int m_end) {
         for_rows<S>(m0, [&](int m, int i) {
-            float y[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                y[q] = (float)acc[i][j][q] * sx * sw[i][q];
-                if (scales.bias) y[q] += bias[i][q];
+                w[i][q] = m + q < m_end ? scales.w[m + q] : 0.0f;
+                bias[i][q] = scales.bias && m + q < m_end ? scales.bias[m + q] : 0.0f;
             }
-            if (n < n_rows) store4<DT>(row, m, w.rows, y);
-            if constexpr (LSE)  // of the results as they are written
-#pragma unroll
-                for (int q = 0; q < 4; ++q) acc[i][j][q] = __float_as_int(m + q < w.rows ? rows::decode<DT>(rows::encode<DT>(y[q])) : -INFINITY);
         });
-    });
-    if constexpr (LSE) {
-        const Part p = column_parts<S>(
-            n0, lds, [&](int i, int j, int q) { return __int_as_float(acc[i][j][q]); },
-            [&](int n) { return (n < n_rows ? rows::scale_of(scales.inv_temp, n) : 1.0f) * rows::kLog2e; });
-        const int n = n0 + (int)threadIdx.x;
-        if ((int)threadIdx.x < S::TN && n < n_rows) parts[(int64_t)n * n_tiles + m0 / S::TM] = p;
     }
+};
+
+// The parts of the rows' log-sum-exp from the results as they are written, left in acc as fp32 bits.
+template <typename S>
+__device__ __forceinline__ void leave_parts(const Side &x, int m0, int n0, const i4 (&acc)[S::FM][S::FN], const Scales &scales, Part *parts, int n_tiles, char *lds) {
+    const int n_rows = x.rows;
+    const Part p = column_parts<S>(
+        n0, lds, [&](int i, int j, int q) { return __int_as_float(acc[i][j][q]); },
+        [&](int n) { return (n < n_rows ? rows::scale_of(scales.inv_temp, n) : 1.0f) * rows::kLog2e; });
+    const int n = n0 + (int)threadIdx.x;
+    if ((int)threadIdx.x < S::TN && n < n_rows) parts[(int64_t)n * n_tiles + m0 / S::TM] = p;
 }
 
 template <int DT, bool LSE, int FN>
@@ -171,7 +158,24 @@ __global__ __launch_bounds__(512) void product_i8(Side w, Side x, int mt, int nt
     int m, n;
     tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m, n);
     Product<kI8, false, false, FN>::run(w, x, m * 256, n * 64 * FN, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
-    finish_tile<DT, LSE, Wide<FN>>(w, x, m * 256, n * 64 * FN, acc, scales, out, out_ld, parts, mt, a0);
+    typedef Wide<FN> S;
+    using T = typename rows::Elem<DT>::T;
+    const int m0 = m * S::TM, n0 = n * S::TN;
+    const RowScales<S> by_row(scales, m0, w.rows);
+    float sx[FN];
+    for_columns<S>(n0, [&](int c, int j) { sx[j] = c < x.rows ? scales.x[c] : 0.0f; });
+    store_tile<DT, S>(m0, w.rows, n0, x.rows, a0, a1, [&](int, int j, int row, int i, float (&y)[4]) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            y[q] = (float)acc[i][j][q] * sx[j] * by_row.w[i][q];
+            if (scales.bias) y[q] += by_row.bias[i][q];
+            if constexpr (LSE) acc[i][j][q] = __float_as_int(row + q < w.rows ? rows::decode<DT>(rows::encode<DT>(y[q])) : -INFINITY);
+        }
+    }, [&](int c) { return static_cast<T *>(out) + (int64_t)c * out_ld; });
+    if constexpr (LSE) {
+        __syncthreads();
+        leave_parts<S>(x, m0, n0, acc, scales, parts, mt, a0);
+    }
 }
 
 template <int DT, bool LSE>
@@ -180,7 +184,22 @@ __global__ __launch_bounds__(Any::THREADS) void product_i8_any(Side w, Side x, S
     i4 acc[Any::FM][Any::FN];
     const int m0 = (int)blockIdx.x * Any::TM, n0 = (int)blockIdx.y * Any::TN;
     product_any<kI8, Any>(w, x, m0, n0, lds, acc);
-    finish_tile<DT, LSE, Any>(w, x, m0, n0, acc, scales, out, out_ld, parts, gridDim.x, lds);
+    using T = typename rows::Elem<DT>::T;
+    const RowScales<Any> by_row(scales, m0, w.rows);
+    for_columns<Any>(n0, [&](int n, int j) {
+        const float sx = n < x.rows ? scales.x[n] : 0.0f;
+        for_rows<Any>(m0, [&](int m, int i) {
+            float y[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                y[q] = (float)acc[i][j][q] * sx * by_row.w[i][q];
+                if (scales.bias) y[q] += by_row.bias[i][q];
+                if constexpr (LSE) acc[i][j][q] = __float_as_int(m + q < w.rows ? rows::decode<DT>(rows::encode<DT>(y[q])) : -INFINITY);
+            }
+            if (n < x.rows) store4<DT>(static_cast<T *>(out) + (int64_t)n * out_ld, m, w.rows, y);
+        });
+    });
+    if constexpr (LSE) leave_parts<Any>(x, m0, n0, acc, scales, parts, gridDim.x, lds);
 }
 
 // Up to 16 rows.

@@ -176,7 +176,7 @@ __device__ __forceinline__ void load_to_lds(u4 memory, uint32_t at, uint32_t to)
 // One operand's tile of a step: ROWS rows of the result by 128 bytes of k, brought to LDS by loads that go past the
 // registers (a wave's 64 lanes fill 1 KB), from memory with k contiguous, or (KM) with the rows of the result contiguous.
 // k contiguous: rows of 128 bytes, the 16-byte pieces of row r at place piece ^ (r & 7).  KM: lines of one k; the 16
-// elements of a block at place block ^ s(k), s different for the four lines that lanes read together; the 16-bit elements are
+// elements of a block at place block ^ s(k), s different for the eight lines that 32 lanes read together; the 16-bit elements are
 // transposed by the reading (ds_read_b64_tr_b16: lane l of 16 gets element l of the four lines that their lanes' 8 bytes
 // lie in), the 32-bit ones read one by one.  All of LDS's banks are reached evenly in every case.
 template <int DT, bool KM, int ROWS>
@@ -190,7 +190,8 @@ struct Operand {
     uint32_t at[N];
     int lane, wave, lines;  // KM: lines from the first step's first to the end
 
-    static __device__ __forceinline__ int place(int k) { return (E == 2 ? k : k >> 2) & 3; }
+    static_assert(!KM || ROWS == 128 || ROWS == 256, "places of whole groups of 8 blocks");
+    static __device__ __forceinline__ int place(int k) { return E == 2 ? (k & 3) | (k >> 3 & 1) << 2 : k >> 2 & 3; }
     // r0: the tile's first row; step0: steps to leave out.  Rows past the matrix's end are those of its last row, bytes
     // past a line's end those of its end.
     __device__ __forceinline__ void begin(const Side &s, int r0, int step0) {
@@ -225,7 +226,7 @@ struct Operand {
             for (int i = 0; i < N; ++i) load_to_lds(memory, at[i], to + i * 1024);
         }
     }
-    // Both 64-byte halves of a step for the rows of block 4 i + c (c below 4: one address serves all i).
+    // Both 64-byte halves of a step for the rows of block 4 i + c (c below 4: one or two addresses serve all i).
     __device__ __forceinline__ void read(u4 (&f)[2], const char *tile, int c, int i) const {
         if constexpr (!KM) {
             const char *q = tile + c * 2048 + i * 8192 + (lane & 15) * kStepBytes;
@@ -235,7 +236,7 @@ struct Operand {
             typedef short s4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s4 *s4_ptr;
             const int k = (lane >> 4) * 8 + (lane >> 2 & 3);
-            const char *q = tile + k * LINE + (lane & 3) * 8 + (c ^ place(k)) * BLOCK + i * 4 * BLOCK;
+            const char *q = tile + k * LINE + (lane & 3) * 8 + ((i * 4 + c) ^ place(k)) * BLOCK;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4_ptr)(q + h * 32 * LINE)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4_ptr)(q + (h * 32 + 4) * LINE));
@@ -568,6 +569,48 @@ __device__ __forceinline__ void store4(typename rows::Elem<DT>::T *row, int m, i
 #pragma unroll
     for (int q = 0; q < 4; ++q)
         if (m + q < end) row[m + q] = (typename rows::Elem<DT>::T)rows::encode<DT>(y[q]);
+}
+
+// Stores a wide tile's results, values(n, j, m, i, y) giving four of a column n, to row(n): 16-bit results go through LDS, 64
+// columns at a time, so that every row gets 512 bytes at once (from the registers it would be 32 at a time); the columns' 16-byte
+// pieces at place piece ^ column there.  m_end, n_end: where the result ends.  For one after another of the columns' groups
+// each thread calls values() for its blocks.
+template <int DT, typename S, typename V, typename R>
+__device__ __forceinline__ void store_tile(int m0, int m_end, int n0, int n_end, char *a0, char *a1, V values, R row) {
+    typedef unsigned int u2 __attribute__((ext_vector_type(2)));
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int in = S::column_block(wave, j) * 16 + (lane & 15), n = n0 + in;
+        char *lds = j & 1 ? a1 : a0;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) {
+            const int at = S::row_block(wave, i) * 16 + (lane >> 4) * 4;
+            float y[4];
+            values(n, j, m0 + at, i, y);
+            if constexpr (DT == TT_F32) {
+                if (n < n_end && m0 + at < m_end) store4<DT>(row(n), m0 + at, m_end, y);
+            } else {
+                *reinterpret_cast<u2 *>(lds + (in & 63) * 512 + ((at >> 3) ^ (in & 31)) * 16 + (at & 4) * 2) = u2{rows::encode_pair<DT>(y[0], y[1]), rows::encode_pair<DT>(y[2], y[3])};
+            }
+        }
+        if constexpr (DT != TT_F32) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = k * 512 + (int)threadIdx.x, r = i >> 5, c = i & 31, m = m0 + c * 8, to = n0 + j * 64 + r;
+                const u4 v = *reinterpret_cast<const u4 *>(lds + r * 512 + (c ^ (r & 31)) * 16);
+                if (to >= n_end) continue;
+                typename rows::Elem<DT>::T *out = row(to);
+                if (m + 8 <= m_end) *reinterpret_cast<u4b *>(out + m) = v;
+                else {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (m + q < m_end) out[m + q] = (typename rows::Elem<DT>::T)(v[q >> 1] >> (q & 1) * 16);
+                }
+            }
+        }
+    }
 }
 
 // Largest value and sum of 2^((z - largest) c) of a set of logits z.  NaN passes through: the sum of a set with a NaN
