@@ -226,30 +226,25 @@ struct Operand {
             for (int i = 0; i < N; ++i) load_to_lds(memory, at[i], to + i * 1024);
         }
     }
-    // Both 64-byte halves of a step for the rows of block 4 i + c (c below 4: one or two addresses serve all i).
-    __device__ __forceinline__ void read(u4 (&f)[2], const char *tile, int c, int i) const {
+    // Half h (64 bytes of k) of a step for the rows of block 4 i + c (c below 4: one or two addresses serve all i).
+    __device__ __forceinline__ u4 read(const char *tile, int c, int i, int h) const {
         if constexpr (!KM) {
-            const char *q = tile + c * 2048 + i * 8192 + (lane & 15) * kStepBytes;
-            f[0] = *reinterpret_cast<const u4 *>(q + ((lane >> 4) ^ (lane & 7)) * 16);
-            f[1] = *reinterpret_cast<const u4 *>(q + ((4 + (lane >> 4)) ^ (lane & 7)) * 16);
+            return *reinterpret_cast<const u4 *>(tile + c * 2048 + i * 8192 + (lane & 15) * kStepBytes + ((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16);
         } else if constexpr (E == 2) {
             typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef short s8 __attribute__((ext_vector_type(8)));
             typedef __attribute__((address_space(3))) s4 *s4_ptr;
             const int k = (lane >> 4) * 8 + (lane >> 2 & 3);
-            const char *q = tile + k * LINE + (lane & 3) * 8 + ((i * 4 + c) ^ place(k)) * BLOCK;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4_ptr)(q + h * 32 * LINE)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4_ptr)(q + (h * 32 + 4) * LINE));
-                typedef short s8 __attribute__((ext_vector_type(8)));
-                f[h] = __builtin_bit_cast(u4, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-            }
+            const char *q = tile + k * LINE + (lane & 3) * 8 + ((i * 4 + c) ^ place(k)) * BLOCK + h * 32 * LINE;
+            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4_ptr)q), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4_ptr)(q + 4 * LINE));
+            return __builtin_bit_cast(u4, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             const int k = (lane >> 4) * 4;
-            const char *q = tile + k * LINE + (lane & 15) * 4 + (c ^ place(k)) * BLOCK + i * 4 * BLOCK;
+            const char *q = tile + k * LINE + (lane & 15) * 4 + (c ^ place(k)) * BLOCK + i * 4 * BLOCK + h * 16 * LINE;
+            u4 f;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) f[h][j] = *reinterpret_cast<const uint32_t *>(q + (h * 16 + j) * LINE);
+            for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const uint32_t *>(q + j * LINE);
+            return f;
         }
     }
 };
@@ -261,8 +256,8 @@ struct Operand {
 // The tile at (m0, n0) of the product over the steps [step0, step0 + steps).  Needs 16-byte aligned rows; k contiguous: whole
 // steps of 128 bytes; 256 rows within 2^31 bytes, KM: all of the steps' lines.
 //
-// Waves 0-3 hold half of the blocks of 16 rows, 4-7 the other half; every SIMD runs one of each.  A step is two pieces of
-// 64 x 16 FN (of a wave): reads from LDS, barrier, matrix instructions, barrier.  The second half's waves are one barrier
+// Waves 0-3 hold half of the blocks of 16 rows, 4-7 the other half; every SIMD runs one of each.  A step is two halves
+// of k: reads from LDS, barrier, matrix instructions, barrier.  The second half's waves are one barrier
 // behind, so that on every SIMD one wave's reads lie beside the other's matrix instructions.  The loads for the step after
 // next begin where the next step does, into the memory that was read last, and have that step's time.
 template <int DT, bool AKM, bool BKM, int FN>
@@ -279,23 +274,19 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
     oa.begin(a, m0, step0);
     ob.begin(b, n0, step0);
     const int wm = oa.wave >> 2, wn = oa.wave & 3;
-    u4 fa[4][2], fb[FN][2];
-    const auto read_a = [&](const char *tile, int half) {
+    u4 fa[8], fb[FN];
+    const auto read = [&](const char *at, const char *bt, int h) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) oa.read(fa[i], tile, wm * 2 + half, i);
-    };
-    const auto read_b = [&](const char *tile) {
+        for (int j = 0; j < FN; ++j) fb[j] = ob.read(bt, wn, j, h);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) ob.read(fb[j], tile, wn, j);
+        for (int i = 0; i < 8; ++i) fa[i] = oa.read(at, wm * 2 + (i >> 2), i & 3, h);
     };
-    const auto multiply = [&](int half) {
+    const auto multiply = [&]() {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[half * 4 + i][j] = Mfma<DT>::run(fa[i][k], fb[j][k], acc[half * 4 + i][j]);
+            for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<DT>::run(fa[i], fb[j], acc[i][j]);
         __builtin_amdgcn_s_setprio(0);
     };
     const auto wait_reads = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };
@@ -311,21 +302,20 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
     barrier();
     if (wm == 1) barrier();
     const auto step = [&](const char *at, const char *bt, char *an, char *bn, int t) {
-        read_b(bt);
-        read_a(at, 0);
+        read(at, bt, 0);
         if (t + 1 < steps) {
             oa.fetch(an, t + 1);
             ob.fetch(bn, t + 1);
         }
         wait_reads();
         barrier();
-        multiply(0);
+        multiply();
         barrier();
-        read_a(at, 1);
+        read(at, bt, 1);
         wait_reads();
         if (wm == 1) wait_loads();
         barrier();
-        multiply(1);
+        multiply();
         if (wm == 0) wait_loads();
         barrier();
     };
