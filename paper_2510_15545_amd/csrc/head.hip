@@ -11,7 +11,6 @@
 // fp32, over all pieces) and the piece's rows of dW, written once.  Of these three products' operands dz, W and x each is kept
 // as it is, whichever of its indices is summed over (tiles.h).  No atomics: results do not depend on scheduling.
 #include <algorithm>
-#include <type_traits>
 
 #include "tiles.h"
 
@@ -22,7 +21,7 @@ using namespace tiles;
 using rows::round256;
 
 constexpr int kTile = 256;   // tokens (or hidden elements) of a wide tile
-constexpr int kAlign = 256;  // rows, tokens and pieces of the vocabulary in a workspace come in multiples of this
+constexpr int kAlign = 256;  // pieces of the vocabulary come in multiples of this
 typedef Shape<128, 128, 2, 2> Any;  // of the products of matrices that lie in any way
 
 constexpr int64_t kSplitTiles = 256;  // workgroups that the sum over a piece's tokens is split into at most
@@ -33,17 +32,6 @@ constexpr int kRowsPerLaunch = 1 << 15;
 __host__ __device__ inline int64_t round_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
 __host__ __device__ constexpr int step_elements(int dtype) { return kStepBytes / bytes_of(dtype); }
 inline int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
-// f(FN as a constant) for the columns of the type's wide tiles: fp32 ones are bound by the matrix cores at any width, and
-// wider ones would not fit the registers.
-inline int columns_for(int64_t n, int dtype) { return dtype == TT_F32 ? 2 : tiles::columns_for(n); }
-template <int DT, typename F>
-void with_columns(int64_t n, F f) {
-    if constexpr (DT == TT_F32) f(std::integral_constant<int, 2>());
-    else if (columns_for(n, DT) == 2) f(std::integral_constant<int, 2>());
-    else if (columns_for(n, DT) == 3) f(std::integral_constant<int, 3>());
-    else f(std::integral_constant<int, 4>());
-}
-
 // A row that carries a weight, for the gradient's epilogue: p = 2^((z - m) c - l), dz = (w - g) p, and g (1 - p) + w p at
 // its token; padding rows are zeros.
 struct Row {
@@ -64,7 +52,7 @@ __global__ __launch_bounds__(256) void lay_out(const char *src, int64_t ld, int 
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t r = i / pieces;
     const int c = (int)(i % pieces) * 16;
-    if (r >= (totals ? round_to(count, kAlign) : n_rows)) return;
+    if (r >= (totals ? padded_rows(count) : n_rows)) return;
     u4 v = {0, 0, 0, 0};
     if (r < count && c < bytes) {
         const char *q = src + (list ? (int64_t)list[r] : r) * ld + c;
@@ -104,14 +92,15 @@ __device__ __forceinline__ void parts_of_tile(const Side &w, const Side &x, int 
     if ((int)threadIdx.x < S::TN && n < n_rows) parts[(int64_t)n * n_tiles + m0 / S::TM] = p;
 }
 
-template <int DT, int FN>
-__global__ __launch_bounds__(512) void head_parts(Side w, Side x, int mt, int nt, const float *inv_temp, const int32_t *ids, Part *parts, float *token) {
-    TT_WIDE_LDS(FN);
-    f4 acc[8][FN];
+template <int DT, typename S>
+__global__ __launch_bounds__(S::THREADS, 2) void head_parts(Side w, Side x, int mt, int nt, const float *inv_temp, const int32_t *ids, Part *parts,
+                                                            float *token) {
+    TT_TILE_LDS(S);
+    f4 acc[S::FM][S::FN];
     int m, n;
     tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m, n);
-    Product<DT, false, false, FN>::run(w, x, m * 256, n * 64 * FN, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
-    parts_of_tile<DT, Wide<FN>>(w, x, m * 256, n * 64 * FN, acc, inv_temp, ids, parts, mt, token, a0);
+    Product<DT, false, false, S>::run(w, x, m * S::TM, n * S::TN, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
+    parts_of_tile<DT, S>(w, x, m * S::TM, n * S::TN, acc, inv_temp, ids, parts, mt, token, a0);
 }
 
 template <int DT>
@@ -244,28 +233,27 @@ __global__ __launch_bounds__(1024) void head_select(int n, int v, const float *i
                        beta * g / top * store_scale, beta * w / top * store_scale, ids && g != 0.0f ? ids[i] : -1};
         }
     }
-    for (int i = before + t; i < round_to(before, kAlign); i += 1024) out[i] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, -1};
+    for (int i = before + t; i < padded_rows(before); i += 1024) out[i] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, -1};
     if (t == 0) *totals = {before, top / store_scale};
 }
 
 // dz of a piece's tokens (the first of them v0) for the listed rows, stored as [row][token].
-template <int DT, int FN>
-__global__ __launch_bounds__(512) void head_dlogits(Side w, Side x, int mt, int nt, int v0, const Row *meta, const Totals *totals, char *d, int64_t d_ld) {
-    TT_WIDE_LDS(FN);
+template <int DT, typename S>
+__global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, int mt, int nt, int v0, const Row *meta, const Totals *totals, char *d, int64_t d_ld) {
+    TT_TILE_LDS(S);
     using T = typename rows::Elem<DT>::T;
-    typedef Wide<FN> S;
-    f4 acc[8][FN];
+    f4 acc[S::FM][S::FN];
     int m0, n0;
     tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m0, n0);
     m0 *= S::TM;
     n0 *= S::TN;
     if (n0 >= totals->rows) return;
-    Product<DT, false, false, FN>::run(w, x, m0, n0, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
-    Row r[FN];
+    Product<DT, false, false, S>::run(w, x, m0, n0, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
+    Row r[S::FN];
     for_columns<S>(n0, [&](int n, int j) { r[j] = meta[n]; });
     bool special = m0 + S::TM > w.rows;  // the piece's end, or a row's token
 #pragma unroll
-    for (int j = 0; j < FN; ++j) special |= __any(r[j].id - v0 >= m0 && r[j].id - v0 < m0 + S::TM) != 0;
+    for (int j = 0; j < S::FN; ++j) special |= __any(r[j].id - v0 >= m0 && r[j].id - v0 < m0 + S::TM) != 0;
     const auto to = [&](int n) { return reinterpret_cast<T *>(d) + (int64_t)n * d_ld; };
     const auto exponent = [&](float z, int j) { return fmaf(z - r[j].m, r[j].c, -r[j].l); };
     if (__syncthreads_or(special)) {
@@ -289,12 +277,11 @@ __global__ __launch_bounds__(512) void head_dlogits(Side w, Side x, int mt, int 
 
 // dx of the listed rows over one piece of the vocabulary, split into parts of its tokens, added to what the pieces before
 // gave: sums[split][row][h] in fp32.
-template <int DT, int FN>
-__global__ __launch_bounds__(512) void head_dhidden(Side w, Side d, int mt, int nt, int split_steps, const Totals *totals, float *sums, int64_t ld,
+template <int DT, typename S>
+__global__ __launch_bounds__(S::THREADS, 2) void head_dhidden(Side w, Side d, int mt, int nt, int split_steps, const Totals *totals, float *sums, int64_t ld,
                                                     int64_t plane, int first) {
-    TT_WIDE_LDS(FN);
-    typedef Wide<FN> S;
-    f4 acc[8][FN];
+    TT_TILE_LDS(S);
+    f4 acc[S::FM][S::FN];
     const int split = (int)blockIdx.x / (mt * nt);
     int m0, n0;
     tile_of((int)blockIdx.x % (mt * nt), mt * nt, mt, nt, m0, n0);
@@ -302,7 +289,7 @@ __global__ __launch_bounds__(512) void head_dhidden(Side w, Side d, int mt, int 
     n0 *= S::TN;
     if (n0 >= totals->rows) return;
     const int steps = (w.rows + step_elements(DT) - 1) / step_elements(DT), from = split * split_steps;
-    Product<DT, true, false, FN>::run(w, d, m0, n0, from, min(split_steps, steps - from), a0, a1, b0, b1, acc);
+    Product<DT, true, false, S>::run(w, d, m0, n0, from, min(split_steps, steps - from), a0, a1, b0, b1, acc);
     for_columns<S>(n0, [&](int n, int j) {
         float *out = sums + split * plane + (int64_t)n * ld;
         for_rows<S>(m0, [&](int m, int i) {
@@ -332,18 +319,17 @@ __global__ __launch_bounds__(256) void head_place(const float *sums, int64_t ld,
 }
 
 // A piece's rows of dW.
-template <int DT, int FN>
-__global__ __launch_bounds__(512) void head_dweight(Side x, Side d, int mt, int nt, const Totals *totals, int n_tokens, int h, void *dweight, int64_t ld) {
-    TT_WIDE_LDS(FN);
+template <int DT, typename S>
+__global__ __launch_bounds__(S::THREADS, 2) void head_dweight(Side x, Side d, int mt, int nt, const Totals *totals, int n_tokens, int h, void *dweight, int64_t ld) {
+    TT_TILE_LDS(S);
     using T = typename rows::Elem<DT>::T;
-    typedef Wide<FN> S;
-    f4 acc[8][FN];
+    f4 acc[S::FM][S::FN];
     int m0, n0;
     tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m0, n0);
     m0 *= S::TM;
     n0 *= S::TN;
     const int steps = (totals->rows + step_elements(DT) - 1) / step_elements(DT);
-    Product<DT, true, true, FN>::run(x, d, m0, n0, 0, steps, a0, a1, b0, b1, acc);
+    Product<DT, true, true, S>::run(x, d, m0, n0, 0, steps, a0, a1, b0, b1, acc);
     const float scale = totals->scale;
     store_tile<DT, S>(m0, h, n0, n_tokens, a0, a1, [&](int, int j, int, int i, float (&y)[4]) {
 #pragma unroll
@@ -379,7 +365,7 @@ struct BackwardLayout : Layout {
     size_t totals, place, list, meta, x, w, d, sums;
     BackwardLayout(int64_t n, int64_t v, int64_t h, int dtype) {
         const int64_t e = rows::element_bytes(dtype), all = round_to(v, kAlign);
-        n_pad = round_to(n, kAlign);
+        n_pad = padded_rows(n);
         width = round_to(h, step_elements(dtype));
         const int64_t row = (n_pad + width) * e;  // of dz and of the weights' copy, for a token
         piece = std::min(all, std::max<int64_t>(kAlign, kPieceBytes / row / kAlign * kAlign));
@@ -396,18 +382,18 @@ struct BackwardLayout : Layout {
     static size_t most(int64_t n, int64_t v, int64_t h, int dtype) {
         BackwardLayout l;
         const int64_t e = rows::element_bytes(dtype);
-        l.n_pad = round_to(n, kAlign);
+        l.n_pad = padded_rows(n);
         l.width = round_to(h, step_elements(dtype));
         l.rows_of(n, e);
         const int64_t row = (l.n_pad + l.width) * e;
         l.take((size_t)std::min(round_to(v, kAlign) * row, std::max(kAlign * row, kPieceBytes)) + 256);
-        l.take((size_t)(std::max(kSplitTiles / tiles_of(l.width, kTile), row_tiles(n, dtype)) * kAlign * l.width * 4));
+        l.take((size_t)(std::max(kSplitTiles / tiles_of(l.width, kTile), row_tiles(n, dtype)) * 384 * l.width * 4));  // n_pad is at most 384 a tile
         return l.total;
     }
 
   private:
     BackwardLayout() {}
-    static int64_t row_tiles(int64_t n, int dtype) { return tiles_of(n, 64 * columns_for(n, dtype)); }
+    static int64_t row_tiles(int64_t n, int dtype) { return tiles_of(n, dtype == TT_F32 ? 128 : 256); }
     void rows_of(int64_t n, int64_t e) {
         totals = take(sizeof(Totals));
         place = take((size_t)n * 4);
@@ -423,7 +409,7 @@ Side matrix(const void *p, int64_t ld, int64_t n, int64_t width, int64_t e) { re
 
 void copy_rows(const void *src, int64_t ld, int64_t n_rows, int64_t width, int64_t e, const int32_t *list, const Totals *totals, char *out,
                int64_t out_width, hipStream_t stream) {
-    const int64_t pieces = (totals ? round_to(n_rows, kAlign) : n_rows) * out_width * e / 16;
+    const int64_t pieces = (totals ? padded_rows(n_rows) : n_rows) * out_width * e / 16;
     lay_out<<<(unsigned int)((pieces + 255) / 256), 256, 0, stream>>>(static_cast<const char *>(src), ld * e, (int)n_rows, (int)(width * e), list, totals,
                                                                   out, (int)(out_width * e));
 }
@@ -448,10 +434,12 @@ int forward(const HeadArgs &a, char *ws, hipStream_t stream) {
         for (int64_t n0 = 0; n0 < a.n_rows; n0 += kRowsPerLaunch) {
             const int64_t n = std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0);
             const Side x = matrix(static_cast<const char *>(a.hidden) + n0 * a.x_ld * e, a.x_ld, n, a.h, e);
-            with_columns<DT>(n, [&](auto fn) {
-                const int nt = (int)tiles_of(n, 64 * fn);
-                head_parts<DT, fn><<<(unsigned int)(n_tiles * nt), 512, 0, stream>>>(w, x, n_tiles, nt, a.inv_temp ? a.inv_temp + n0 : nullptr,
-                                                                                  ids ? ids + n0 : nullptr, parts + n0 * n_tiles, token + n0);
+            with_shape<DT, kForward>(std::min<int64_t>(kRowsPerLaunch, a.n_rows), [&](auto shape) {
+                typedef decltype(shape) S;
+                const int nt = (int)tiles_of(n, S::TN);
+                n_tiles = (int)tiles_of(a.v, S::TM);
+                head_parts<DT, S><<<(unsigned int)(n_tiles * nt), S::THREADS, 0, stream>>>(w, x, n_tiles, nt, a.inv_temp ? a.inv_temp + n0 : nullptr,
+                                                                                        ids ? ids + n0 : nullptr, parts + n0 * n_tiles, token + n0);
             });
         }
     } else {
@@ -469,7 +457,7 @@ bool copies_weight(const HeadGradArgs &a) {
     return !whole_steps(w);
 }
 
-template <int DT, int FN>
+template <int DT>
 void backward_piece(const HeadGradArgs &a, const BackwardLayout &lay, char *ws, int64_t v0, bool copy_w, hipStream_t stream) {
     const int64_t e = rows::element_bytes(DT), here = std::min<int64_t>(lay.piece, a.v - v0);
     const Totals *totals = reinterpret_cast<Totals *>(ws + lay.totals);
@@ -480,18 +468,27 @@ void backward_piece(const HeadGradArgs &a, const BackwardLayout &lay, char *ws, 
         w = matrix(ws + lay.w, lay.width, here, lay.width, e);
     }
     const Side x = matrix(ws + lay.x, lay.width, lay.n_pad, lay.width, e), d = matrix(ws + lay.d, lay.piece, lay.n_pad, lay.piece, e);
-    const int mt = (int)tiles_of(here, kTile), nt = (int)tiles_of(a.n_rows, 64 * FN), ht = (int)tiles_of(a.h, kTile);
-    head_dlogits<DT, FN><<<mt * nt, 512, 0, stream>>>(w, x, mt, nt, (int)v0, reinterpret_cast<const Row *>(ws + lay.meta), totals, ws + lay.d, lay.piece);
-    if (a.dhidden) {
-        const int steps = (int)tiles_of(here, step_elements(DT)), split = (int)tiles_of(steps, lay.splits);
-        head_dhidden<DT, FN><<<ht * nt * lay.splits, 512, 0, stream>>>(w, d, ht, nt, split, totals, reinterpret_cast<float *>(ws + lay.sums), lay.width,
-                                                                    lay.n_pad * lay.width, v0 == 0);
-    }
-    if (a.dweight) {
-        constexpr int VN = DT == TT_F32 ? 2 : 4;
-        const int vt = (int)tiles_of(here, 64 * VN);
-        head_dweight<DT, VN><<<ht * vt, 512, 0, stream>>>(x, d, ht, vt, totals, (int)here, a.h, static_cast<char *>(a.dweight) + v0 * a.dw_ld * e, a.dw_ld);
-    }
+    with_shape<DT, kGradLogits>(a.n_rows, [&](auto shape) {
+        typedef decltype(shape) S;
+        const int mt = (int)tiles_of(here, S::TM), nt = (int)tiles_of(a.n_rows, S::TN);
+        head_dlogits<DT, S><<<mt * nt, S::THREADS, 0, stream>>>(w, x, mt, nt, (int)v0, reinterpret_cast<const Row *>(ws + lay.meta), totals, ws + lay.d,
+                                                                lay.piece);
+    });
+    if (a.dhidden)
+        with_shape<DT, kGradHidden>(a.n_rows, [&](auto shape) {
+            typedef decltype(shape) S;
+            const int mt = (int)tiles_of(a.h, S::TM), nt = (int)tiles_of(a.n_rows, S::TN);
+            const int steps = (int)tiles_of(here, step_elements(DT)), split = (int)tiles_of(steps, lay.splits);
+            head_dhidden<DT, S><<<mt * nt * lay.splits, S::THREADS, 0, stream>>>(w, d, mt, nt, split, totals, reinterpret_cast<float *>(ws + lay.sums),
+                                                                              lay.width, lay.n_pad * lay.width, v0 == 0);
+        });
+    if (a.dweight)
+        with_shape<DT, kGradWeight>(a.n_rows, [&](auto shape) {
+            typedef decltype(shape) S;
+            const int mt = (int)tiles_of(a.h, S::TM), nt = (int)tiles_of(here, S::TN);
+            head_dweight<DT, S><<<mt * nt, S::THREADS, 0, stream>>>(x, d, mt, nt, totals, (int)here, a.h,
+                                                                    static_cast<char *>(a.dweight) + v0 * a.dw_ld * e, a.dw_ld);
+        });
 }
 
 template <int DT>
@@ -504,9 +501,7 @@ int backward(const HeadGradArgs &a, char *ws, hipStream_t stream) {
     head_select<<<1, 1024, 0, stream>>>(a.n_rows, a.v, a.inv_temp, a.ids, a.stats, a.grad, a.grad_lse, DT == TT_F16 ? 0x1p14f : 1.0f, place, list,
                                         reinterpret_cast<Row *>(ws + lay.meta), totals);
     copy_rows(a.hidden, a.x_ld, a.n_rows, a.h, e, list, totals, ws + lay.x, lay.width, stream);
-    for (int64_t v0 = 0; v0 < a.v; v0 += lay.piece) {
-        with_columns<DT>(a.n_rows, [&](auto fn) { backward_piece<DT, fn>(a, lay, ws, v0, copy_w, stream); });
-    }
+    for (int64_t v0 = 0; v0 < a.v; v0 += lay.piece) backward_piece<DT>(a, lay, ws, v0, copy_w, stream);
     if (a.dhidden)
         head_place<DT><<<dim3(a.n_rows, (unsigned int)tiles_of(a.h, 1024)), 256, 0, stream>>>(reinterpret_cast<float *>(ws + lay.sums), lay.width,
                                                                                          lay.n_pad * lay.width, lay.splits, place, totals, a.h,

@@ -151,18 +151,18 @@ __device__ __forceinline__ void leave_parts(const Side &x, int m0, int n0, const
     if ((int)threadIdx.x < S::TN && n < n_rows) parts[(int64_t)n * n_tiles + m0 / S::TM] = p;
 }
 
-template <int DT, bool LSE, int FN>
-__global__ __launch_bounds__(512) void product_i8(Side w, Side x, int mt, int nt, Scales scales, void *out, int64_t out_ld, Part *parts) {
-    TT_WIDE_LDS(FN);
-    i4 acc[8][FN];
-    int m, n;
-    tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m, n);
-    Product<kI8, false, false, FN>::run(w, x, m * 256, n * 64 * FN, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
-    typedef Wide<FN> S;
+template <int DT, bool LSE, typename S>
+__global__ __launch_bounds__(S::THREADS, 2) void product_i8(Side w, Side x, int mt, int nt, Scales scales, void *out, int64_t out_ld, Part *parts) {
+    TT_TILE_LDS(S);
+    i4 acc[S::FM][S::FN];
+    int m0, n0;
+    tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m0, n0);
+    m0 *= S::TM;
+    n0 *= S::TN;
+    Product<kI8, false, false, S>::run(w, x, m0, n0, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
     using T = typename rows::Elem<DT>::T;
-    const int m0 = m * S::TM, n0 = n * S::TN;
     const RowScales<S> by_row(scales, m0, w.rows);
-    float sx[FN];
+    float sx[S::FN];
     for_columns<S>(n0, [&](int c, int j) { sx[j] = c < x.rows ? scales.x[c] : 0.0f; });
     store_tile<DT, S>(m0, w.rows, n0, x.rows, a0, a1, [&](int, int j, int row, int i, float (&y)[4]) {
 #pragma unroll
@@ -294,16 +294,16 @@ int multiply(const MatmulI8Args &a, Part *parts, hipStream_t stream) {
         else run(product_i8_thin<DT, LSE, 4>);
     } else if (whole_steps(w) && whole_steps(x)) {
         for (int64_t n0 = 0; n0 < a.n_rows; n0 += kRowsPerLaunch) {
-            const int n = (int)std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0), fn = columns_for(n), nt = (n + 64 * fn - 1) / (64 * fn);
+            const int n = (int)std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0);
             const Side part = {x.p + n0 * x.ld, x.ld, n, x.bytes};
             const Scales scales = {a.x_scale + n0, a.w_scale, a.bias, a.inv_temp ? a.inv_temp + n0 : nullptr};
-            const auto run = [&](auto kernel) {
-                kernel<<<(unsigned int)(n_tiles * nt), 512, 0, stream>>>(w, part, n_tiles, nt, scales, static_cast<char *>(a.out) + n0 * a.out_ld * e, a.out_ld,
-                                                                      parts + n0 * n_tiles);
-            };
-            if (fn == 2) run(product_i8<DT, LSE, 2>);
-            else if (fn == 3) run(product_i8<DT, LSE, 3>);
-            else run(product_i8<DT, LSE, 4>);
+            with_shape<kI8, kForward>(std::min<int64_t>(kRowsPerLaunch, a.n_rows), [&](auto shape) {
+                typedef decltype(shape) S;
+                const int nt = (n + S::TN - 1) / S::TN;
+                n_tiles = (a.n_cols + S::TM - 1) / S::TM;
+                product_i8<DT, LSE, S><<<(unsigned int)(n_tiles * nt), S::THREADS, 0, stream>>>(
+                    w, part, n_tiles, nt, scales, static_cast<char *>(a.out) + n0 * a.out_ld * e, a.out_ld, parts + n0 * n_tiles);
+            });
         }
     } else {
         n_tiles = (a.n_cols + Any::TM - 1) / Any::TM;

@@ -5,6 +5,8 @@
 // block, so what goes on along a row of the result (a softmax over the vocabulary, a store) stays mostly within a lane.
 #pragma once
 
+#include <type_traits>
+
 #include "rows.h"
 
 namespace tt {
@@ -158,12 +160,28 @@ __device__ __forceinline__ void product_any(const Side &a, const Side &b, int m0
 // ------------------------------------------------------------------------------------------------ wide tiles
 typedef __attribute__((address_space(3))) void *lds_ptr;
 
-// 256 rows of the first operand by 64 FN of the second; 8 waves, each 128 x 16 FN, of every fourth block.
-template <int FN_>
+// Tiles of 64 C columns (rows of the second operand).  Wide: 256 rows of the first operand, 8 waves of 128 x 16 C, one
+// workgroup to a compute unit.  Half: 128 rows, 4 waves of 64 x 32 C, two workgroups.  A wave's blocks of 16 lie apart, in
+// groups of four: block 4 i + c of a side for a few c.
+template <int C>
 struct Wide {
-    static constexpr int TM = 256, TN = 64 * FN_, WM = 2, WN = 4, THREADS = 512, FM = 8, FN = FN_;
-    static __device__ __forceinline__ int row_block(int wave, int i) { return (i & 3) * 4 + (wave >> 2) * 2 + (i >> 2); }
-    static __device__ __forceinline__ int column_block(int wave, int j) { return j * 4 + (wave & 3); }
+    static constexpr int TM = 256, TN = 64 * C, COLUMNS = C, WAVES = 8, WM = 2, WN = 4, THREADS = 512, FM = 8, FN = C, PER_CU = 1;
+    static __device__ __forceinline__ int row_c(int wave, int i) { return (wave >> 2) * 2 + (i >> 2); }
+    static __device__ __forceinline__ int column_c(int wave, int) { return wave & 3; }
+    static constexpr __device__ int row_i(int i) { return i & 3; }
+    static constexpr __device__ int column_i(int j) { return j; }
+    static __device__ __forceinline__ int row_block(int wave, int i) { return row_i(i) * 4 + row_c(wave, i); }
+    static __device__ __forceinline__ int column_block(int wave, int j) { return column_i(j) * 4 + column_c(wave, j); }
+};
+template <int C>
+struct Half {
+    static constexpr int TM = 128, TN = 64 * C, COLUMNS = C, WAVES = 4, WM = 2, WN = 2, THREADS = 256, FM = 4, FN = 2 * C, PER_CU = 2;
+    static __device__ __forceinline__ int row_c(int wave, int i) { return (wave >> 1) * 2 + (i >> 1); }
+    static __device__ __forceinline__ int column_c(int wave, int j) { return (wave & 1) * 2 + (j & 1); }
+    static constexpr __device__ int row_i(int i) { return i & 1; }
+    static constexpr __device__ int column_i(int j) { return j >> 1; }
+    static __device__ __forceinline__ int row_block(int wave, int i) { return row_i(i) * 4 + row_c(wave, i); }
+    static __device__ __forceinline__ int column_block(int wave, int j) { return column_i(j) * 4 + column_c(wave, j); }
 };
 
 // 16 bytes a lane from the memory's start + `at`, to LDS at `to` and on, in the order of the lanes.  Written as an instruction
@@ -179,12 +197,12 @@ __device__ __forceinline__ void load_to_lds(u4 memory, uint32_t at, uint32_t to)
 // elements of a block at place block ^ s(k), s different for the eight lines that 32 lanes read together; the 16-bit elements are
 // transposed by the reading (ds_read_b64_tr_b16: lane l of 16 gets element l of the four lines that their lanes' 8 bytes
 // lie in), the 32-bit ones read one by one.  All of LDS's banks are reached evenly in every case.
-template <int DT, bool KM, int ROWS>
+template <int DT, bool KM, int ROWS, int WAVES>
 struct Operand {
     static constexpr int E = DT == TT_F32 ? 4 : 2;         // KM: bytes of an element
     static constexpr int LINE = ROWS * E, BLOCK = 16 * E;  // KM: bytes of a line and of a block in it
     static constexpr int K = kStepBytes / E;               // KM: lines of a step
-    static constexpr int N = ROWS / 64;                    // loads of a wave
+    static constexpr int N = ROWS / 8 / WAVES;             // loads of a wave
     const char *p;
     int64_t ld;
     uint32_t at[N];
@@ -249,45 +267,44 @@ struct Operand {
     }
 };
 
-// LDS of a wide product: two steps of either operand.  Arrays of their own, so that the compiler knows that what is read
+// LDS of a tile's product: two steps of either operand.  Arrays of their own, so that the compiler knows that what is read
 // of one step does not wait for the loads of the next.
-#define TT_WIDE_LDS(FN) __shared__ __attribute__((aligned(1024))) char a0[32768], a1[32768], b0[8192 * (FN)], b1[8192 * (FN)]
+#define TT_TILE_LDS(S) __shared__ __attribute__((aligned(1024))) char a0[S::TM * 128], a1[S::TM * 128], b0[S::TN * 128], b1[S::TN * 128]
 
 // The tile at (m0, n0) of the product over the steps [step0, step0 + steps).  Needs 16-byte aligned rows; k contiguous: whole
-// steps of 128 bytes; 256 rows within 2^31 bytes, KM: all of the steps' lines.
+// steps of 128 bytes.
 //
 // Waves 0-3 hold half of the blocks of 16 rows, 4-7 the other half; every SIMD runs one of each.  A step is two halves
 // of k: reads from LDS, barrier, matrix instructions, barrier.  The second half's waves are one barrier
 // behind, so that on every SIMD one wave's reads lie beside the other's matrix instructions.  The loads for the step after
 // next begin where the next step does, into the memory that was read last, and have that step's time.
-template <int DT, bool AKM, bool BKM, int FN>
+//
+// Half tiles: two workgroups to a compute unit, whose reads, matrix instructions, beginnings and ends lie beside each other as they come.
+template <int DT, bool AKM, bool BKM, typename S>
 struct Product {
 static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0, int n0, int step0, int steps, char *a0, char *a1, char *b0, char *b1,
-                                           typename Mfma<DT>::Acc (&acc)[8][FN]) {
-    Operand<DT, AKM, 256> oa;
-    Operand<DT, BKM, 64 * FN> ob;
+                                           typename Mfma<DT>::Acc (&acc)[S::FM][S::FN]) {
+    Operand<DT, AKM, S::TM, S::WAVES> oa;
+    Operand<DT, BKM, S::TN, S::WAVES> ob;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = {0, 0, 0, 0};
+        for (int j = 0; j < S::FN; ++j) acc[i][j] = {0, 0, 0, 0};
     if (steps <= 0) return;
     oa.begin(a, m0, step0);
     ob.begin(b, n0, step0);
-    const int wm = oa.wave >> 2, wn = oa.wave & 3;
-    u4 fa[8], fb[FN];
+    u4 fa[S::FM], fb[S::FN];
     const auto read = [&](const char *at, const char *bt, int h) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) fb[j] = ob.read(bt, wn, j, h);
+        for (int j = 0; j < S::FN; ++j) fb[j] = ob.read(bt, S::column_c(ob.wave, j), S::column_i(j), h);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) fa[i] = oa.read(at, wm * 2 + (i >> 2), i & 3, h);
+        for (int i = 0; i < S::FM; ++i) fa[i] = oa.read(at, S::row_c(oa.wave, i), S::row_i(i), h);
     };
     const auto multiply = [&]() {
-        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<DT>::run(fa[i], fb[j], acc[i][j]);
-        __builtin_amdgcn_s_setprio(0);
+            for (int j = 0; j < S::FN; ++j) acc[i][j] = Mfma<DT>::run(fa[i], fb[j], acc[i][j]);
     };
     const auto wait_reads = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };
     const auto wait_loads = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };
@@ -298,34 +315,61 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
     };
     oa.fetch(a0, 0);
     ob.fetch(b0, 0);
-    wait_loads();
-    barrier();
-    if (wm == 1) barrier();
-    const auto step = [&](const char *at, const char *bt, char *an, char *bn, int t) {
-        read(at, bt, 0);
-        if (t + 1 < steps) {
-            oa.fetch(an, t + 1);
-            ob.fetch(bn, t + 1);
+    if constexpr (S::WAVES == 8) {
+        const bool late = oa.wave >= 4;
+        wait_loads();
+        barrier();
+        if (late) barrier();
+        const auto step = [&](const char *at, const char *bt, char *an, char *bn, int t) {
+            read(at, bt, 0);
+            if (t + 1 < steps) {
+                oa.fetch(an, t + 1);
+                ob.fetch(bn, t + 1);
+            }
+            wait_reads();
+            barrier();
+            __builtin_amdgcn_s_setprio(1);
+            multiply();
+            __builtin_amdgcn_s_setprio(0);
+            barrier();
+            read(at, bt, 1);
+            wait_reads();
+            if (late) wait_loads();
+            barrier();
+            __builtin_amdgcn_s_setprio(1);
+            multiply();
+            __builtin_amdgcn_s_setprio(0);
+            if (!late) wait_loads();
+            barrier();
+        };
+        int t = 0;
+        for (; t + 1 < steps; t += 2) {
+            step(a0, b0, a1, b1, t);
+            step(a1, b1, a0, b0, t + 1);
         }
-        wait_reads();
-        barrier();
-        multiply();
-        barrier();
-        read(at, bt, 1);
-        wait_reads();
-        if (wm == 1) wait_loads();
-        barrier();
-        multiply();
-        if (wm == 0) wait_loads();
-        barrier();
-    };
-    int t = 0;
-    for (; t + 1 < steps; t += 2) {
-        step(a0, b0, a1, b1, t);
-        step(a1, b1, a0, b0, t + 1);
+        if (t < steps) step(a0, b0, a1, b1, t);
+        if (!late) barrier();
+    } else {
+        const auto step = [&](const char *at, const char *bt, char *an, char *bn, int t) {
+            wait_loads();
+            barrier();  // the step is there, and the memory of the one before is read
+            if (t + 1 < steps) {
+                oa.fetch(an, t + 1);
+                ob.fetch(bn, t + 1);
+            }
+            read(at, bt, 0);
+            multiply();
+            read(at, bt, 1);
+            multiply();
+            wait_reads();
+        };
+        int t = 0;
+        for (; t + 1 < steps; t += 2) {
+            step(a0, b0, a1, b1, t);
+            step(a1, b1, a0, b0, t + 1);
+        }
+        if (t < steps) step(a0, b0, a1, b1, t);
     }
-    if (t < steps) step(a0, b0, a1, b1, t);
-    if (wm == 0) barrier();
     __syncthreads();
 }
 };
@@ -497,11 +541,38 @@ __device__ __forceinline__ void product_few(const Side &w, const Side &x, char *
     }
 }
 
-// Columns of a wide product's tiles in units of 64, for n rows of the second operand: as few tiles as 256 columns give, and no
-// wider than they need (333 rows: 2 x 192, not 2 x 256).
-inline int columns_for(int64_t n) {
-    const int64_t tiles = (n + 255) / 256, columns = ((n + tiles - 1) / tiles + 63) / 64;
-    return columns < 2 ? 2 : (int)columns;
+// Rows that tiles of 64, 128, 192 or 256 columns reach where n rows are wanted.
+__host__ __device__ inline int64_t padded_rows(int64_t n) {
+    const int64_t by_256 = (n + 255) / 256 * 256, by_192 = (n + 191) / 192 * 192;
+    return by_256 > by_192 ? by_256 : by_192;
+}
+
+// f(shape) for the tiles of a product of m rows of the first operand with n of the second.
+// Few rows (up to 512): half tiles, in which more loads are on their way beside the matrix instructions.
+enum Use { kForward, kGradLogits, kGradHidden, kGradWeight };
+template <int DT, Use U, typename F>
+void with_shape(int64_t n, F f) {
+    const int64_t tiles = (n + 255) / 256;
+    const int columns = (int)(((n + tiles - 1) / tiles + 63) / 64);
+    const bool few = n <= 512;
+    if constexpr (DT == TT_F32) f(Half<2>());
+    else if constexpr (U == kGradWeight) {
+        if (few) f(Half<2>());
+        else f(Wide<4>());
+    } else if constexpr (U == kGradLogits) {
+        if (few) f(Half<2>());
+        else if (columns == 3) f(Wide<3>());
+        else f(Wide<4>());
+    } else if constexpr (U == kGradHidden) {
+        if (columns <= 2) f(Wide<2>());
+        else if (columns == 3) f(Wide<3>());
+        else f(Wide<4>());
+    } else {
+        if (n <= 128) f(Half<2>());
+        else if (few) f(Half<3>());
+        else if (columns == 3) f(Wide<3>());
+        else f(Wide<4>());
+    }
 }
 
 // Workgroups of a product with few rows, for n rows of the second operand and m of the first: a part each of every row.
@@ -561,35 +632,40 @@ __device__ __forceinline__ void store4(typename rows::Elem<DT>::T *row, int m, i
         if (m + q < end) row[m + q] = (typename rows::Elem<DT>::T)rows::encode<DT>(y[q]);
 }
 
-// Stores a wide tile's results, values(n, j, m, i, y) giving four of a column n, to row(n): 16-bit results go through LDS, 64
-// columns at a time, so that every row gets 512 bytes at once (from the registers it would be 32 at a time); the columns' 16-byte
+// Stores a tile's results, values(n, j, m, i, y) giving four of a column n, to row(n): 16-bit results go through LDS, 64
+// columns at a time, so that every row gets 512 or 256 bytes at once (from the registers it would be 32 at a time); the columns' 16-byte
 // pieces at place piece ^ column there.  m_end, n_end: where the result ends.  For one after another of the columns' groups
 // each thread calls values() for its blocks.
 template <int DT, typename S, typename V, typename R>
 __device__ __forceinline__ void store_tile(int m0, int m_end, int n0, int n_end, char *a0, char *a1, V values, R row) {
     typedef unsigned int u2 __attribute__((ext_vector_type(2)));
+    constexpr int PIECES = S::TM / 8, SAME = S::FN / S::COLUMNS;  // of a row; blocks of a wave in 64 columns
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
 #pragma unroll
-    for (int j = 0; j < S::FN; ++j) {
-        const int in = S::column_block(wave, j) * 16 + (lane & 15), n = n0 + in;
-        char *lds = j & 1 ? a1 : a0;
+    for (int g = 0; g < S::COLUMNS; ++g) {
+        char *lds = g & 1 ? a1 : a0;
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i) {
-            const int at = S::row_block(wave, i) * 16 + (lane >> 4) * 4;
-            float y[4];
-            values(n, j, m0 + at, i, y);
-            if constexpr (DT == TT_F32) {
-                if (n < n_end && m0 + at < m_end) store4<DT>(row(n), m0 + at, m_end, y);
-            } else {
-                *reinterpret_cast<u2 *>(lds + (in & 63) * 512 + ((at >> 3) ^ (in & 31)) * 16 + (at & 4) * 2) = u2{rows::encode_pair<DT>(y[0], y[1]), rows::encode_pair<DT>(y[2], y[3])};
+        for (int j = g * SAME; j < (g + 1) * SAME; ++j) {
+            const int in = S::column_block(wave, j) * 16 + (lane & 15), n = n0 + in;
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                const int at = S::row_block(wave, i) * 16 + (lane >> 4) * 4;
+                float y[4];
+                values(n, j, m0 + at, i, y);
+                if constexpr (DT == TT_F32) {
+                    if (n < n_end && m0 + at < m_end) store4<DT>(row(n), m0 + at, m_end, y);
+                } else {
+                    *reinterpret_cast<u2 *>(lds + ((in & 63) * PIECES + ((at >> 3) ^ (in & (PIECES - 1)))) * 16 + (at & 4) * 2) =
+                        u2{rows::encode_pair<DT>(y[0], y[1]), rows::encode_pair<DT>(y[2], y[3])};
+                }
             }
         }
         if constexpr (DT != TT_F32) {
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int i = k * 512 + (int)threadIdx.x, r = i >> 5, c = i & 31, m = m0 + c * 8, to = n0 + j * 64 + r;
-                const u4 v = *reinterpret_cast<const u4 *>(lds + r * 512 + (c ^ (r & 31)) * 16);
+            for (int k = 0; k < 64 * PIECES / S::THREADS; ++k) {
+                const int i = k * S::THREADS + (int)threadIdx.x, r = i / PIECES, c = i % PIECES, m = m0 + c * 8, to = n0 + g * 64 + r;
+                const u4 v = *reinterpret_cast<const u4 *>(lds + (r * PIECES + (c ^ (r & (PIECES - 1)))) * 16);
                 if (to >= n_end) continue;
                 typename rows::Elem<DT>::T *out = row(to);
                 if (m + 8 <= m_end) *reinterpret_cast<u4b *>(out + m) = v;
