@@ -99,8 +99,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_parts(Side w, Side x, int 
     f4 acc[S::FM][S::FN];
     int m, n;
     tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m, n);
-    Product<DT, false, false, S>::run(w, x, m * S::TM, n * S::TN, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
-    parts_of_tile<DT, S>(w, x, m * S::TM, n * S::TN, acc, inv_temp, ids, parts, mt, token, a0);
+    Product<DT, false, false, S>::run(w, x, m * S::TM, n * S::TN, 0, w.bytes / kStepBytes, lds, acc);
+    parts_of_tile<DT, S>(w, x, m * S::TM, n * S::TN, acc, inv_temp, ids, parts, mt, token, lds);
 }
 
 template <int DT>
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
     m0 *= S::TM;
     n0 *= S::TN;
     if (n0 >= totals->rows) return;
-    Product<DT, false, false, S>::run(w, x, m0, n0, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
+    Product<DT, false, false, S>::run(w, x, m0, n0, 0, w.bytes / kStepBytes, lds, acc);
     Row r[S::FN];
     for_columns<S>(n0, [&](int n, int j) { r[j] = meta[n]; });
     bool special = m0 + S::TM > w.rows;  // the piece's end, or a row's token
@@ -256,8 +256,16 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
     for (int j = 0; j < S::FN; ++j) special |= __any(r[j].id - v0 >= m0 && r[j].id - v0 < m0 + S::TM) != 0;
     const auto to = [&](int n) { return reinterpret_cast<T *>(d) + (int64_t)n * d_ld; };
     const auto exponent = [&](float z, int j) { return fmaf(z - r[j].m, r[j].c, -r[j].l); };
-    if (__syncthreads_or(special)) {
-        store_tile<DT, S>(m0, (int)d_ld, n0, INT_MAX, a0, a1, [&](int, int j, int m, int i, float (&y)[4]) {
+    // any of the workgroup's (by a word of the tile's memory, of which there is no more)
+    int *flag = reinterpret_cast<int *>(lds);
+    if (threadIdx.x == 0) *flag = 0;
+    __syncthreads();
+    if (special) *flag = 1;
+    __syncthreads();
+    special = *flag != 0;
+    __syncthreads();
+    if (special) {
+        store_tile<DT, S>(m0, (int)d_ld, n0, INT_MAX, lds, lds + S::TM * kStepBytes, [&](int, int j, int m, int i, float (&y)[4]) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float e = exponent(acc[i][j][q], j), p = __builtin_amdgcn_exp2f(e);
@@ -267,7 +275,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
             }
         }, to);
     } else {
-        store_tile<DT, S>(m0, (int)d_ld, n0, INT_MAX, a0, a1, [&](int, int j, int, int i, float (&y)[4]) {
+        store_tile<DT, S>(m0, (int)d_ld, n0, INT_MAX, lds, lds + S::TM * kStepBytes, [&](int, int j, int, int i, float (&y)[4]) {
             const float f = r[j].w - r[j].g;
 #pragma unroll
             for (int q = 0; q < 4; ++q) y[q] = f * __builtin_amdgcn_exp2f(exponent(acc[i][j][q], j));
@@ -289,7 +297,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dhidden(Side w, Side d, in
     n0 *= S::TN;
     if (n0 >= totals->rows) return;
     const int steps = (w.rows + step_elements(DT) - 1) / step_elements(DT), from = split * split_steps;
-    Product<DT, true, false, S>::run(w, d, m0, n0, from, min(split_steps, steps - from), a0, a1, b0, b1, acc);
+    Product<DT, true, false, S>::run(w, d, m0, n0, from, min(split_steps, steps - from), lds, acc);
     for_columns<S>(n0, [&](int n, int j) {
         float *out = sums + split * plane + (int64_t)n * ld;
         for_rows<S>(m0, [&](int m, int i) {
@@ -329,9 +337,9 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dweight(Side x, Side d, in
     m0 *= S::TM;
     n0 *= S::TN;
     const int steps = (totals->rows + step_elements(DT) - 1) / step_elements(DT);
-    Product<DT, true, true, S>::run(x, d, m0, n0, 0, steps, a0, a1, b0, b1, acc);
+    Product<DT, true, true, S>::run(x, d, m0, n0, 0, steps, lds, acc);
     const float scale = totals->scale;
-    store_tile<DT, S>(m0, h, n0, n_tokens, a0, a1, [&](int, int j, int, int i, float (&y)[4]) {
+    store_tile<DT, S>(m0, h, n0, n_tokens, lds, lds + S::TM * kStepBytes, [&](int, int j, int, int i, float (&y)[4]) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) y[q] = acc[i][j][q] * scale;
     }, [&](int n) { return static_cast<T *>(dweight) + (int64_t)n * ld; });
@@ -372,7 +380,8 @@ struct BackwardLayout : Layout {
         // pieces of one size, in whole rounds of the compute units where there are several
         const int64_t round = std::max<int64_t>(1, kCus / row_tiles(n, dtype)) * kTile, even = round_to(tiles_of(all, tiles_of(all, piece)), kAlign);
         if (piece < all) piece = std::min(piece, piece >= round ? std::min(round_to(even, round), piece / round * round) : even);
-        splits = (int)std::min<int64_t>(std::max<int64_t>(1, kSplitTiles / (row_tiles(n, dtype) * tiles_of(width, kTile))), std::max<int64_t>(1, all / 1024));
+        const int64_t tiles = row_tiles(n, dtype) * tiles_of(width, dtype == TT_F32 ? 128 : kTile);
+        splits = (int)std::min<int64_t>(std::max<int64_t>(1, kSplitTiles / tiles), std::max<int64_t>(1, all / (dtype == TT_F32 ? 512 : 1024)));
         rows_of(n, e);
         d = take((size_t)(piece * n_pad * e));
         w = take((size_t)(piece * width * e));

@@ -125,20 +125,28 @@ struct Scales {
     const float *x, *w, *bias, *inv_temp;
 };
 
-// A tile's scales and biases of its rows m, for this thread's blocks.
+// A tile's scales and biases of its rows m in LDS: [rows] of either, ones and zeros past the end.
 template <typename S>
-struct RowScales {
-    float w[S::FM][4], bias[S::FM][4];
-    __device__ __forceinline__ RowScales(const Scales &scales, int m0, int m_end) {
-        for_rows<S>(m0, [&](int m, int i) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                w[i][q] = m + q < m_end ? scales.w[m + q] : 0.0f;
-                bias[i][q] = scales.bias && m + q < m_end ? scales.bias[m + q] : 0.0f;
-            }
-        });
+__device__ __forceinline__ void stage_scales(const Scales &scales, int m0, int m_end, float *lds) {
+    for (int t = (int)threadIdx.x; t < S::TM; t += S::THREADS) {
+        const bool in = m0 + t < m_end;
+        lds[t] = in ? scales.w[m0 + t] : 1.0f;
+        lds[S::TM + t] = in && scales.bias ? scales.bias[m0 + t] : 0.0f;
     }
-};
+    __syncthreads();
+}
+
+// Four results of a column with scale sx, from the tile's row `at` on.
+template <typename S>
+__device__ __forceinline__ void scaled(const i4 &sum, float sx, const float *lds, int at, bool bias, float (&y)[4]) {
+    const f4 sw = *reinterpret_cast<const f4 *>(lds + at);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] = (float)sum[q] * sx * sw[q];
+    if (!bias) return;
+    const f4 b = *reinterpret_cast<const f4 *>(lds + S::TM + at);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] += b[q];
+}
 
 // The parts of the rows' log-sum-exp from the results as they are written, left in acc as fp32 bits.
 template <typename S>
@@ -159,22 +167,21 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_i8(Side w, Side x, int 
     tile_of((int)blockIdx.x, (int)gridDim.x, mt, nt, m0, n0);
     m0 *= S::TM;
     n0 *= S::TN;
-    Product<kI8, false, false, S>::run(w, x, m0, n0, 0, w.bytes / kStepBytes, a0, a1, b0, b1, acc);
+    Product<kI8, false, false, S>::run(w, x, m0, n0, 0, w.bytes / kStepBytes, lds, acc);
     using T = typename rows::Elem<DT>::T;
-    const RowScales<S> by_row(scales, m0, w.rows);
+    float *by_row = reinterpret_cast<float *>(lds + 2 * S::TM * kStepBytes);
+    stage_scales<S>(scales, m0, w.rows, by_row);
     float sx[S::FN];
     for_columns<S>(n0, [&](int c, int j) { sx[j] = c < x.rows ? scales.x[c] : 0.0f; });
-    store_tile<DT, S>(m0, w.rows, n0, x.rows, a0, a1, [&](int, int j, int row, int i, float (&y)[4]) {
+    store_tile<DT, S>(m0, w.rows, n0, x.rows, lds, lds + S::TM * kStepBytes, [&](int, int j, int row, int i, float (&y)[4]) {
+        scaled<S>(acc[i][j], sx[j], by_row, row - m0, scales.bias != nullptr, y);
+        if constexpr (LSE)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            y[q] = (float)acc[i][j][q] * sx[j] * by_row.w[i][q];
-            if (scales.bias) y[q] += by_row.bias[i][q];
-            if constexpr (LSE) acc[i][j][q] = __float_as_int(row + q < w.rows ? rows::decode<DT>(rows::encode<DT>(y[q])) : -INFINITY);
-        }
+            for (int q = 0; q < 4; ++q) acc[i][j][q] = __float_as_int(row + q < w.rows ? rows::decode<DT>(rows::encode<DT>(y[q])) : -INFINITY);
     }, [&](int c) { return static_cast<T *>(out) + (int64_t)c * out_ld; });
     if constexpr (LSE) {
         __syncthreads();
-        leave_parts<S>(x, m0, n0, acc, scales, parts, mt, a0);
+        leave_parts<S>(x, m0, n0, acc, scales, parts, mt, lds);
     }
 }
 
@@ -185,17 +192,16 @@ __global__ __launch_bounds__(Any::THREADS) void product_i8_any(Side w, Side x, S
     const int m0 = (int)blockIdx.x * Any::TM, n0 = (int)blockIdx.y * Any::TN;
     product_any<kI8, Any>(w, x, m0, n0, lds, acc);
     using T = typename rows::Elem<DT>::T;
-    const RowScales<Any> by_row(scales, m0, w.rows);
+    __shared__ __attribute__((aligned(16))) float by_row[2 * Any::TM];
+    stage_scales<Any>(scales, m0, w.rows, by_row);
     for_columns<Any>(n0, [&](int n, int j) {
         const float sx = n < x.rows ? scales.x[n] : 0.0f;
         for_rows<Any>(m0, [&](int m, int i) {
             float y[4];
+            scaled<Any>(acc[i][j], sx, by_row, m - m0, scales.bias != nullptr, y);
+            if constexpr (LSE)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                y[q] = (float)acc[i][j][q] * sx * by_row.w[i][q];
-                if (scales.bias) y[q] += by_row.bias[i][q];
-                if constexpr (LSE) acc[i][j][q] = __float_as_int(m + q < w.rows ? rows::decode<DT>(rows::encode<DT>(y[q])) : -INFINITY);
-            }
+                for (int q = 0; q < 4; ++q) acc[i][j][q] = __float_as_int(m + q < w.rows ? rows::decode<DT>(rows::encode<DT>(y[q])) : -INFINITY);
             if (n < x.rows) store4<DT>(static_cast<T *>(out) + (int64_t)n * out_ld, m, w.rows, y);
         });
     });

@@ -267,22 +267,22 @@ struct Operand {
     }
 };
 
-// LDS of a tile's product: two steps of either operand.  Arrays of their own, so that the compiler knows that what is read
-// of one step does not wait for the loads of the next.
-#define TT_TILE_LDS(S) __shared__ __attribute__((aligned(1024))) char a0[S::TM * 128], a1[S::TM * 128], b0[S::TN * 128], b1[S::TN * 128]
+// LDS of a tile's product: three steps of the first operand, two of the second.
+#define TT_TILE_LDS(S) __shared__ __attribute__((aligned(1024))) char lds[(3 * S::TM + 2 * S::TN) * kStepBytes]
 
 // The tile at (m0, n0) of the product over the steps [step0, step0 + steps).  Needs 16-byte aligned rows; k contiguous: whole
 // steps of 128 bytes.
 //
 // Waves 0-3 hold half of the blocks of 16 rows, 4-7 the other half; every SIMD runs one of each.  A step is two halves
 // of k: reads from LDS, barrier, matrix instructions, barrier.  The second half's waves are one barrier
-// behind, so that on every SIMD one wave's reads lie beside the other's matrix instructions.  The loads for the step after
-// next begin where the next step does, into the memory that was read last, and have that step's time.
+// behind, so that on every SIMD one wave's reads lie beside the other's matrix instructions.  The second operand (hidden states,
+// tokens: it comes from the L2) is loaded a step ahead, the first one (the weights, from HBM) two: one was too short for it
+// (8-bit 288 x 128,256 x 2,048 132 us against 127, the gradient of 391 x 50,257 x 1,024 201 against 191).
 //
 // Half tiles: two workgroups to a compute unit, whose reads, matrix instructions, beginnings and ends lie beside each other as they come.
 template <int DT, bool AKM, bool BKM, typename S>
 struct Product {
-static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0, int n0, int step0, int steps, char *a0, char *a1, char *b0, char *b1,
+static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0, int n0, int step0, int steps, char *lds,
                                            typename Mfma<DT>::Acc (&acc)[S::FM][S::FN]) {
     Operand<DT, AKM, S::TM, S::WAVES> oa;
     Operand<DT, BKM, S::TN, S::WAVES> ob;
@@ -307,25 +307,39 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
             for (int j = 0; j < S::FN; ++j) acc[i][j] = Mfma<DT>::run(fa[i], fb[j], acc[i][j]);
     };
     const auto wait_reads = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };
-    const auto wait_loads = [] { __builtin_amdgcn_s_waitcnt(0x0f70); };
+    const auto wait_loads = [](bool but_first) {  // the first operand's loads of the step after next may be on their way
+        if (but_first) __builtin_amdgcn_s_waitcnt(0x0f70 | Operand<DT, AKM, S::TM, S::WAVES>::N);
+        else __builtin_amdgcn_s_waitcnt(0x0f70);
+    };
     const auto barrier = [] {
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
     };
-    oa.fetch(a0, 0);
-    ob.fetch(b0, 0);
+    constexpr int A = S::TM * kStepBytes, B = S::TN * kStepBytes;
+    char *const bs = lds + 3 * A;
+    oa.fetch(lds, 0);
+    ob.fetch(bs, 0);
+    if (steps > 1) oa.fetch(lds + A, 1);
+    const char *at = lds, *bt = bs;
+    char *to = lds + 2 * A;  // of the step after next
+    const auto ahead = [&](int t) {
+        if (t + 1 < steps) ob.fetch(bt == bs ? bs + B : bs, t + 1);
+        if (t + 2 < steps) oa.fetch(to, t + 2);
+    };
+    const auto next = [&] {
+        to = const_cast<char *>(at);
+        at = at == lds + 2 * A ? lds : at + A;
+        bt = bt == bs ? bs + B : bs;
+    };
     if constexpr (S::WAVES == 8) {
         const bool late = oa.wave >= 4;
-        wait_loads();
+        wait_loads(steps > 1);
         barrier();
         if (late) barrier();
-        const auto step = [&](const char *at, const char *bt, char *an, char *bn, int t) {
+        for (int t = 0; t < steps; ++t) {
             read(at, bt, 0);
-            if (t + 1 < steps) {
-                oa.fetch(an, t + 1);
-                ob.fetch(bn, t + 1);
-            }
+            ahead(t);
             wait_reads();
             barrier();
             __builtin_amdgcn_s_setprio(1);
@@ -334,41 +348,28 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
             barrier();
             read(at, bt, 1);
             wait_reads();
-            if (late) wait_loads();
+            if (late) wait_loads(t + 2 < steps);
             barrier();
             __builtin_amdgcn_s_setprio(1);
             multiply();
             __builtin_amdgcn_s_setprio(0);
-            if (!late) wait_loads();
+            if (!late) wait_loads(t + 2 < steps);
             barrier();
-        };
-        int t = 0;
-        for (; t + 1 < steps; t += 2) {
-            step(a0, b0, a1, b1, t);
-            step(a1, b1, a0, b0, t + 1);
+            next();
         }
-        if (t < steps) step(a0, b0, a1, b1, t);
         if (!late) barrier();
     } else {
-        const auto step = [&](const char *at, const char *bt, char *an, char *bn, int t) {
-            wait_loads();
+        for (int t = 0; t < steps; ++t) {
+            wait_loads(t + 1 < steps);
             barrier();  // the step is there, and the memory of the one before is read
-            if (t + 1 < steps) {
-                oa.fetch(an, t + 1);
-                ob.fetch(bn, t + 1);
-            }
+            ahead(t);
             read(at, bt, 0);
             multiply();
             read(at, bt, 1);
             multiply();
             wait_reads();
-        };
-        int t = 0;
-        for (; t + 1 < steps; t += 2) {
-            step(a0, b0, a1, b1, t);
-            step(a1, b1, a0, b0, t + 1);
+            next();
         }
-        if (t < steps) step(a0, b0, a1, b1, t);
     }
     __syncthreads();
 }
@@ -547,32 +548,20 @@ __host__ __device__ inline int64_t padded_rows(int64_t n) {
     return by_256 > by_192 ? by_256 : by_192;
 }
 
-// f(shape) for the tiles of a product of m rows of the first operand with n of the second.
-// Few rows (up to 512): half tiles, in which more loads are on their way beside the matrix instructions.
+// f(shape) for the tiles of a product with n rows of the second operand.
+// As few tiles as 256 columns give, no wider than they need (333 rows: 2 x 192): every tile of columns is a reading of the
+// first operand.  Half tiles up to 128 rows, and where their smaller ones leave less undone: the gradient's logits of
+// few rows (how many carry a weight is not known here), its short sums over few rows, and fp32, which the matrix cores bound.
 enum Use { kForward, kGradLogits, kGradHidden, kGradWeight };
 template <int DT, Use U, typename F>
 void with_shape(int64_t n, F f) {
     const int64_t tiles = (n + 255) / 256;
     const int columns = (int)(((n + tiles - 1) / tiles + 63) / 64);
-    const bool few = n <= 512;
     if constexpr (DT == TT_F32) f(Half<2>());
-    else if constexpr (U == kGradWeight) {
-        if (few) f(Half<2>());
-        else f(Wide<4>());
-    } else if constexpr (U == kGradLogits) {
-        if (few) f(Half<2>());
-        else if (columns == 3) f(Wide<3>());
-        else f(Wide<4>());
-    } else if constexpr (U == kGradHidden) {
-        if (columns <= 2) f(Wide<2>());
-        else if (columns == 3) f(Wide<3>());
-        else f(Wide<4>());
-    } else {
-        if (n <= 128) f(Half<2>());
-        else if (few) f(Half<3>());
-        else if (columns == 3) f(Wide<3>());
-        else f(Wide<4>());
-    }
+    else if (n <= (U == kGradLogits || U == kGradWeight ? 512 : 128)) f(Half<2>());
+    else if constexpr (U == kGradWeight) f(Wide<4>());
+    else if (columns == 3) f(Wide<3>());
+    else f(Wide<4>());
 }
 
 // Workgroups of a product with few rows, for n rows of the second operand and m of the first: a part each of every row.
