@@ -113,7 +113,7 @@ __global__ __launch_bounds__(Any::THREADS) void head_parts_any(Side w, Side x, c
 }
 
 // Up to 16 rows.
-template <int DT>
+template <int DT, bool WHOLE>
 __global__ __launch_bounds__(kThinThreads, 4) void head_parts_few(Side w, Side x, const float *inv_temp, const int32_t *ids, Part *parts, float *token) {
     __shared__ __attribute__((aligned(16))) char lds[kThinLds];
     __shared__ float sums[8][256];
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kThinThreads, 4) void head_parts_few(Side w, Side x
     const float c = (n < x.rows ? rows::scale_of(inv_temp, n) : 1.0f) * rows::kLog2e;
     const int id = ids && n < x.rows ? ids[n] : -1;
     Part p = {-INFINITY, 0.0f};
-    product_few<DT>(w, x, lds, sums, [&](int m, int, float z) {
+    product_few<DT, WHOLE>(w, x, lds, sums, [&](int m, int, float z) {
         if (m >= w.rows) return;
         if (m == id) token[n] = z;
         add_part(p, z, c);
@@ -381,7 +381,7 @@ struct BackwardLayout : Layout {
         const int64_t round = std::max<int64_t>(1, kCus / row_tiles(n, dtype)) * kTile, even = round_to(tiles_of(all, tiles_of(all, piece)), kAlign);
         if (piece < all) piece = std::min(piece, piece >= round ? std::min(round_to(even, round), piece / round * round) : even);
         const int64_t tiles = row_tiles(n, dtype) * tiles_of(width, dtype == TT_F32 ? 128 : kTile);
-        splits = (int)std::min<int64_t>(std::max<int64_t>(1, kSplitTiles / tiles), std::max<int64_t>(1, all / (dtype == TT_F32 ? 512 : 1024)));
+        splits = (int)std::min<int64_t>(std::max<int64_t>(1, kSplitTiles / tiles), std::max<int64_t>(1, all / (dtype == TT_F32 ? 128 : 512)));  // at least 4 or 8 steps each
         rows_of(n, e);
         d = take((size_t)(piece * n_pad * e));
         w = take((size_t)(piece * width * e));
@@ -436,7 +436,8 @@ int forward(const HeadArgs &a, char *ws, hipStream_t stream) {
         n_tiles = thin_groups(a.n_rows, a.v);
         const Side x = matrix(a.hidden, a.x_ld, a.n_rows, a.h, e);
         const auto run = [&](auto kernel) { kernel<<<n_tiles, kThinThreads, 0, stream>>>(w, x, a.inv_temp, ids, parts, token); };
-        if (a.n_rows <= kFewMost) run(head_parts_few<DT>);
+        if (a.n_rows <= kFewMost && w.bytes % kFewBytes == 0) run(head_parts_few<DT, true>);
+        else if (a.n_rows <= kFewMost) run(head_parts_few<DT, false>);
         else if (a.n_rows <= 32) run(head_parts_thin<DT, 2>);
         else run(head_parts_thin<DT, 4>);
     } else if (whole_steps(w) && whole_steps(matrix(a.hidden, a.x_ld, a.n_rows, a.h, e))) {

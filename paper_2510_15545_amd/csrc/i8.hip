@@ -209,7 +209,7 @@ __global__ __launch_bounds__(Any::THREADS) void product_i8_any(Side w, Side x, S
 }
 
 // Up to 16 rows.
-template <int DT, bool LSE>
+template <int DT, bool LSE, bool WHOLE>
 __global__ __launch_bounds__(kThinThreads, 4) void product_i8_few(Side w, Side x, Scales scales, void *out, int64_t out_ld, Part *parts) {
     __shared__ __attribute__((aligned(16))) char lds[kThinLds];
     __shared__ float sums[8][256];
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(kThinThreads, 4) void product_i8_few(Side w, Side x
     const float c = LSE && there ? rows::scale_of(scales.inv_temp, column) * rows::kLog2e : 0.0f, sx = there ? scales.x[column] : 0.0f;
     T *row = static_cast<T *>(out) + column * out_ld;
     Part p = {-INFINITY, 0.0f};
-    product_few<kI8>(w, x, lds, sums, [&](int m, int, int sum) {
+    product_few<kI8, WHOLE>(w, x, lds, sums, [&](int m, int, int sum) {
         if (!there || m >= w.rows) return;
         float y = (float)sum * sx * scales.w[m];
         if (scales.bias) y += scales.bias[m];
@@ -295,7 +295,8 @@ int multiply(const MatmulI8Args &a, Part *parts, hipStream_t stream) {
         n_tiles = thin_groups(a.n_rows, a.n_cols);
         const Scales scales = {a.x_scale, a.w_scale, a.bias, a.inv_temp};
         const auto run = [&](auto kernel) { kernel<<<n_tiles, kThinThreads, 0, stream>>>(w, x, scales, a.out, a.out_ld, parts); };
-        if (a.n_rows <= kFewMost) run(product_i8_few<DT, LSE>);
+        if (a.n_rows <= kFewMost && w.bytes % kFewBytes == 0) run(product_i8_few<DT, LSE, true>);
+        else if (a.n_rows <= kFewMost) run(product_i8_few<DT, LSE, false>);
         else if (a.n_rows <= 32) run(product_i8_thin<DT, LSE, 2>);
         else run(product_i8_thin<DT, LSE, 4>);
     } else if (whole_steps(w) && whole_steps(x)) {

@@ -455,89 +455,97 @@ __device__ __forceinline__ void product_thin(const Side &w, const Side &x, char 
 
 // Up to 16 rows of the second operand: 16 rows of the first to a workgroup, whose 8 waves lie side by side along k, 128 bytes of a
 // row each, so that 1 KB of a row is read at a time (the same bytes 16 rows by 64 bytes a wave come at 5.2 TB/s, these at 5.9 to
-// 6.1, read in order at 6.8).  Loads roll: what has been multiplied makes room for the same place of the next 4 KB.  The waves'
-// sums are joined in LDS; then thread t (of 256) has row t % 16 and column t / 16.
-constexpr int kFewMost = 16, kFewRows = 16, kFewBatch = 4096;
+// 6.1, read in order at 6.8).  Loads roll through four such KBs: what has been multiplied makes room for the one four further on,
+// in this row or the next.  The waves' sums are joined in LDS; then thread t (of 256) has row t % 16 and column t / 16.
+constexpr int kFewMost = 16, kFewRows = 16, kFewBytes = 1024;
 
-// finish(m, n, y): one result.
-template <int DT, typename F>
+// finish(m, n, y): one result.  WHOLE: rows of whole KBs, loaded without a branch (past the last row the last one again).
+template <int DT, bool WHOLE, typename F>
 __device__ __forceinline__ void product_few(const Side &w, const Side &x, char *lds, float (*sums)[256], F finish) {
     typedef typename Mfma<DT>::Acc Acc;
-    constexpr int U = 8;
+    constexpr int AHEAD = 4;
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, quarter = lane >> 4;
-    const int chunk = min((w.bytes + 127) / 128 * 128, kThinLds / x.rows / kFewBatch * kFewBatch);
-    const int groups = (w.rows + kFewRows - 1) / kFewRows, batches = (w.bytes + kFewBatch - 1) / kFewBatch;
-    const int r = min(lane & 15, x.rows - 1), inside = wave * 128 + quarter * 16;  // of a KB
-    const char *column = lds + r * chunk;
+    const int chunk = min((w.bytes + 127) / 128 * 128, kThinLds / x.rows / kFewBytes * kFewBytes);
+    const int groups = (w.rows + kFewRows - 1) / kFewRows, pieces = (w.bytes + kFewBytes - 1) / kFewBytes;  // of a row
+    const int r = min(lane & 15, x.rows - 1), inside = wave * 128 + quarter * 16;                        // a piece
+    const char *column = lds + r * chunk + wave * 128;
     const int turn = (quarter ^ (r & 7)) * 16;
-    u4 f[U];
-    const auto row_of = [&](int g) { return w.p + (int64_t)min(g * kFewRows + (lane & 15), w.rows - 1) * w.ld; };
-    const auto load = [&](const char *row, int b, int u) {
-        const int at = b * kFewBatch + (u >> 1) * 1024 + (u & 1) * 64 + inside;
-        if ((b + 1) * kFewBatch <= w.bytes) return (u4)rows::load_global<true>(row + at);
-        const int left = w.bytes - at;
-        return left >= 16 ? (u4)*reinterpret_cast<const u4b *>(row + at) : left > 0 ? load_some(row + at, left) : u4{0, 0, 0, 0};
-    };
-    int g = (int)blockIdx.x;
-    if (g < groups) {
-        const char *row = row_of(g);
+    u4 f[AHEAD][2];
+    // the place that is loaded next: row group, piece
+    int load_g = (int)blockIdx.x, load_c = 0;
+    const char *load_row = w.p + (int64_t)min(load_g * kFewRows + (lane & 15), w.rows - 1) * w.ld + inside;
+    const auto load = [&](u4 (&to)[2]) {
+        const int at = load_c * kFewBytes;
+        if (WHOLE || at + kFewBytes <= w.bytes) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) f[u] = load(row, 0, u);
-    }
-    int staged = -1;  // the chunk in LDS
-    for (; g < groups; g += (int)gridDim.x) {
-        Acc acc = {0, 0, 0, 0};
-        for (int b = 0; b < batches; ++b) {
-            const int k0 = b * kFewBatch / chunk * chunk;
+            for (int h = 0; h < 2; ++h) to[h] = rows::load_global<true>(load_row + at + h * 64);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int left = w.bytes - at - inside - h * 64;
+                const char *q = load_row + at + h * 64;
+                to[h] = left >= 16 ? (u4)*reinterpret_cast<const u4b *>(q) : left > 0 ? load_some(q, left) : u4{0, 0, 0, 0};
+            }
+        }
+        if (++load_c == pieces) {
+            load_c = 0;
+            load_g += (int)gridDim.x;
+            load_row = w.p + (int64_t)min(load_g * kFewRows + (lane & 15), w.rows - 1) * w.ld + inside;
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) load(f[s]);
+    int staged = -1, c = 0;  // the chunk in LDS; the piece that is multiplied next
+    Acc acc = {0, 0, 0, 0};
+    for (int g = (int)blockIdx.x; g < groups;) {
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) {
+            if (g >= groups) break;
+            const int at = c * kFewBytes, k0 = at / chunk * chunk;
             if (staged != k0) {
                 __syncthreads();  // the chunk before is done with
-                const int pieces = chunk / 16;
-                for (int i = (int)threadIdx.x; i < x.rows * pieces; i += kThinThreads) {
-                    const int n = i / pieces, c = i % pieces, left = x.bytes - (k0 + c * 16);
-                    const char *q = x.p + (int64_t)n * x.ld + k0 + c * 16;
+                const int n_pieces = chunk / 16;
+                for (int i = (int)threadIdx.x; i < x.rows * n_pieces; i += kThinThreads) {
+                    const int n = i / n_pieces, p = i % n_pieces, left = x.bytes - (k0 + p * 16);
+                    const char *q = x.p + (int64_t)n * x.ld + k0 + p * 16;
                     const u4 v = left >= 16 ? (u4)*reinterpret_cast<const u4b *>(q) : left > 0 ? load_some(q, left) : u4{0, 0, 0, 0};
-                    *reinterpret_cast<u4 *>(lds + n * chunk + (c & ~7) * 16 + ((c ^ n) & 7) * 16) = v;
+                    *reinterpret_cast<u4 *>(lds + n * chunk + (p & ~7) * 16 + ((p ^ n) & 7) * 16) = v;
                 }
                 __syncthreads();
                 staged = k0;
             }
-            const bool more = b + 1 < batches;
-            const int next_g = more ? g : g + (int)gridDim.x, next_b = more ? b + 1 : 0;
-            const bool any = next_g < groups;
-            const char *next = row_of(min(next_g, groups - 1));
-            const char *at = column + (b * kFewBatch - k0) + wave * 128;
+            // a wave whose 128 bytes lie past the row's end has nothing to add
+            if (WHOLE || at - k0 + wave * 128 < chunk)
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                // past the row's end (the last columns of a chunk that is not whole): zeros of the first operand
-                const int here = (u >> 1) * 1024 + (u & 1) * 64;
-                const bool inside_chunk = b * kFewBatch - k0 + wave * 128 + here < chunk;
-                const u4 y = inside_chunk ? *reinterpret_cast<const u4 *>(at + (u >> 1) * 1024 + (turn ^ (u & 1) * 64)) : u4{0, 0, 0, 0};
-                acc = Mfma<DT>::run(f[u], y, acc);
-                if (any) f[u] = load(next, next_b, u);
+                for (int h = 0; h < 2; ++h) acc = Mfma<DT>::run(f[s][h], *reinterpret_cast<const u4 *>(column + (at - k0) + (turn ^ h * 64)), acc);
+            load(f[s]);
+            if (++c < pieces) continue;
+            c = 0;
+            // [wave][row][column], row r's columns turned by r
+            __syncthreads();  // the sums before are read
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int m = quarter * 4 + q, to = m * 16 + ((lane + m) & 15);
+                if constexpr (DT == kI8) sums[wave][to] = __int_as_float(acc[q]);
+                else sums[wave][to] = acc[q];
             }
-        }
-        // [wave][row][column], row r's columns turned by r
-        __syncthreads();  // the sums before are read
+            acc = {0, 0, 0, 0};
+            __syncthreads();
+            if (threadIdx.x < 256) {
+                const int m = (int)threadIdx.x & 15, n = (int)threadIdx.x >> 4, from = m * 16 + ((n + m) & 15);
+                if constexpr (DT == kI8) {
+                    int y = 0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int m = quarter * 4 + q, to = m * 16 + ((lane + m) & 15);
-            if constexpr (DT == kI8) sums[wave][to] = __int_as_float(acc[q]);
-            else sums[wave][to] = acc[q];
-        }
-        __syncthreads();
-        if (threadIdx.x < 256) {
-            const int m = (int)threadIdx.x & 15, n = (int)threadIdx.x >> 4, from = m * 16 + ((n + m) & 15);
-            if constexpr (DT == kI8) {
-                int y = 0;
+                    for (int v = 0; v < 8; ++v) y += __float_as_int(sums[v][from]);
+                    finish(g * kFewRows + m, n, y);
+                } else {
+                    float y = 0.0f;
 #pragma unroll
-                for (int v = 0; v < 8; ++v) y += __float_as_int(sums[v][from]);
-                finish(g * kFewRows + m, n, y);
-            } else {
-                float y = 0.0f;
-#pragma unroll
-                for (int v = 0; v < 8; ++v) y += sums[v][from];
-                finish(g * kFewRows + m, n, y);
+                    for (int v = 0; v < 8; ++v) y += sums[v][from];
+                    finish(g * kFewRows + m, n, y);
+                }
             }
+            g += (int)gridDim.x;
         }
     }
 }

@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 NAN = float("nan")
 SIZES = [(1, 1, 1), (1, 640, 256), (2, 2, 3), (3, 129, 65), (5, 1000, 1), (16, 513, 64), (17, 384, 72), (33, 300, 128), (64, 5000, 200),
-         (65, 1025, 192), (130, 257, 64), (257, 513, 96), (300, 131, 1031), (1, 20011, 40), (129, 128, 2048), (600, 700, 33)]
+         (9, 2100, 544), (16, 333, 1536), (12, 100, 4100), (65, 1025, 192), (400, 1500, 512), (130, 257, 64), (257, 513, 96), (300, 131, 1031), (1, 20011, 40), (129, 128, 2048), (600, 700, 33)]
 LAYOUTS = [(0, 0), (8, 0), (3, 1)]  # of rows further apart, and of the first one off its alignment
 
 
@@ -268,6 +268,24 @@ def test_one_workspace_for_batches_of_any_size():
             grads = [tt.head_logprobs_backward(v, x[:n], w, some[0], got.stats, some[2], inv_temperature=some[1], workspace=space) for space in (b, None)]
             assert all(torch.equal(s, t) for s, t in zip(*grads)), n
             assert all(bool(torch.isfinite(t.float()).all()) for t in grads[0])
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("n,v,h", [(1, 700, 64), (16, 20011, 64), (17, 3000, 128), (64, 700, 65), (65, 129, 64), (130, 1000, 64), (200, 257, 64),
+                                   (257, 600, 96), (320, 513, 64), (500, 2000, 63), (513, 700, 64), (700, 300, 256)])
+def test_nothing_behind_the_workspace_is_touched(n, v, h, name):
+    """Workspaces of exactly the bytes that the calls ask for, in memory whose rest stays as it was."""
+    x, w, ids, beta = uh.operands(n, v, h, name)
+    g, q = weights(n)
+    code = {"bf16": 0, "f32": 2}[name]
+    used = [tt._spread_bytes(f, n, v, h, code) for f in ("tt_head_logprobs_workspace_size", "tt_head_logprobs_backward_workspace_used")]
+    rooms = [torch.full((b + (1 << 20),), 93, dtype=torch.uint8, device="cuda") for b in used]
+    out = tt.head_logprobs(v, x, w, ids, inv_temperature=beta, workspace=rooms[0][:used[0]])
+    got = tt.head_logprobs_backward(v, x, w, ids, out.stats, g, grad_lse=q, inv_temperature=beta, workspace=rooms[1][:used[1]])
+    for room, b in zip(rooms, used):
+        assert bool((room[b:] == 93).all())
+    want = tt.head_logprobs_backward(v, x, w, ids, out.stats, g, grad_lse=q, inv_temperature=beta)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 @pytest.mark.parametrize("n,v,h,name", [(3, 5001, 64, "bf16"), (200, 2000, 128, "bf16"), (40, 900, 72, "f16"), (150, 700, 65, "f32")])

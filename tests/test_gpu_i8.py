@@ -94,7 +94,8 @@ def check_matmul(x, xs, w, ws, bias, name, beta=None, lse=False, **kw):
 
 
 SIZES = [(1, 1, 1), (1, 640, 256), (2, 3, 5), (3, 129, 65), (16, 513, 64), (17, 300, 130), (33, 77, 128), (64, 1025, 200), (65, 257, 1000),
-         (130, 384, 64), (257, 130, 96), (300, 500, 4096), (5, 20011, 48), (1, 5000, 4096), (129, 128, 16), (40, 33, 15)]
+         (130, 384, 64), (257, 130, 96), (300, 500, 4096), (5, 20011, 48), (1, 5000, 4096), (129, 128, 16), (40, 33, 15),
+         (12, 333, 2048), (16, 100, 5000), (7, 50, 9216), (3, 40, 70000), (520, 700, 256), (200, 1000, 384)]
 
 
 @pytest.mark.parametrize("name", ["bf16", "f16", "f32"])
@@ -176,6 +177,18 @@ def test_no_rows_and_the_callers_memory():
         got = tt.matmul_i8(x[:n], xs[:n].contiguous(), w, ws, out=mine[0], lse=mine[1], workspace=space)
         want = tt.matmul_i8(x[:n], xs[:n].contiguous(), w, ws, dtype=torch.float16, lse=True)
         assert got[0] is mine[0] and got[1] is mine[1] and all(torch.equal(a, b) for a, b in zip(got, want)), n
+
+
+@pytest.mark.parametrize("n,m,k", [(1, 700, 64), (16, 20011, 64), (17, 3000, 128), (64, 700, 65), (100, 129, 128), (200, 257, 128), (300, 600, 200),
+                                   (320, 513, 128)])
+def test_nothing_behind_the_workspace_is_touched(n, m, k):
+    x, w = ints(n, k, 1), ints(m, k, 2)
+    xs, ws = scales(n, 3, 0.05), scales(m, 4, 0.01)
+    b = tt.matmul_i8_workspace(n, m, k, lse=True).numel()
+    room = torch.full((b + (1 << 20),), 93, dtype=torch.uint8, device="cuda")
+    got = tt.matmul_i8(x, xs, w, ws, lse=True, workspace=room[:b])
+    assert bool((room[b:] == 93).all())
+    assert all(torch.equal(s, t) for s, t in zip(got, tt.matmul_i8(x, xs, w, ws, lse=True)))
 
 
 def test_on_another_stream_and_in_a_graph():
