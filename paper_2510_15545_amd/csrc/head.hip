@@ -444,7 +444,7 @@ int forward(const HeadArgs &a, char *ws, hipStream_t stream) {
         for (int64_t n0 = 0; n0 < a.n_rows; n0 += kRowsPerLaunch) {
             const int64_t n = std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0);
             const Side x = matrix(static_cast<const char *>(a.hidden) + n0 * a.x_ld * e, a.x_ld, n, a.h, e);
-            with_shape<DT, kForward>(std::min<int64_t>(kRowsPerLaunch, a.n_rows), [&](auto shape) {
+            with_shape<DT, kForward>(a.v, std::min<int64_t>(kRowsPerLaunch, a.n_rows), [&](auto shape) {
                 typedef decltype(shape) S;
                 const int nt = (int)tiles_of(n, S::TN);
                 n_tiles = (int)tiles_of(a.v, S::TM);
@@ -478,14 +478,14 @@ void backward_piece(const HeadGradArgs &a, const BackwardLayout &lay, char *ws, 
         w = matrix(ws + lay.w, lay.width, here, lay.width, e);
     }
     const Side x = matrix(ws + lay.x, lay.width, lay.n_pad, lay.width, e), d = matrix(ws + lay.d, lay.piece, lay.n_pad, lay.piece, e);
-    with_shape<DT, kGradLogits>(a.n_rows, [&](auto shape) {
+    with_shape<DT, kGradLogits>(here, a.n_rows, [&](auto shape) {
         typedef decltype(shape) S;
         const int mt = (int)tiles_of(here, S::TM), nt = (int)tiles_of(a.n_rows, S::TN);
         head_dlogits<DT, S><<<mt * nt, S::THREADS, 0, stream>>>(w, x, mt, nt, (int)v0, reinterpret_cast<const Row *>(ws + lay.meta), totals, ws + lay.d,
                                                                 lay.piece);
     });
     if (a.dhidden)
-        with_shape<DT, kGradHidden>(a.n_rows, [&](auto shape) {
+        with_shape<DT, kGradHidden>(a.h, a.n_rows, [&](auto shape) {
             typedef decltype(shape) S;
             const int mt = (int)tiles_of(a.h, S::TM), nt = (int)tiles_of(a.n_rows, S::TN);
             const int steps = (int)tiles_of(here, step_elements(DT)), split = (int)tiles_of(steps, lay.splits);
@@ -493,7 +493,7 @@ void backward_piece(const HeadGradArgs &a, const BackwardLayout &lay, char *ws, 
                                                                               lay.width, lay.n_pad * lay.width, v0 == 0);
         });
     if (a.dweight)
-        with_shape<DT, kGradWeight>(a.n_rows, [&](auto shape) {
+        with_shape<DT, kGradWeight>(a.h, a.n_rows, [&](auto shape) {
             typedef decltype(shape) S;
             const int mt = (int)tiles_of(a.h, S::TM), nt = (int)tiles_of(here, S::TN);
             head_dweight<DT, S><<<mt * nt, S::THREADS, 0, stream>>>(x, d, mt, nt, totals, (int)here, a.h,

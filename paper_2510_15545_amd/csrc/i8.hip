@@ -304,7 +304,7 @@ int multiply(const MatmulI8Args &a, Part *parts, hipStream_t stream) {
             const int n = (int)std::min<int64_t>(kRowsPerLaunch, a.n_rows - n0);
             const Side part = {x.p + n0 * x.ld, x.ld, n, x.bytes};
             const Scales scales = {a.x_scale + n0, a.w_scale, a.bias, a.inv_temp ? a.inv_temp + n0 : nullptr};
-            with_shape<kI8, kForward>(std::min<int64_t>(kRowsPerLaunch, a.n_rows), [&](auto shape) {
+            with_shape<kI8, kForward>(a.n_cols, std::min<int64_t>(kRowsPerLaunch, a.n_rows), [&](auto shape) {
                 typedef decltype(shape) S;
                 const int nt = (n + S::TN - 1) / S::TN;
                 n_tiles = (a.n_cols + S::TM - 1) / S::TM;
