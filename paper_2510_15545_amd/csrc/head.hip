@@ -27,7 +27,7 @@ typedef Shape<128, 128, 2, 2> Any;  // of the products of matrices that lie in a
 constexpr int64_t kSplitTiles = 256;  // workgroups that the sum over a piece's tokens is split into at most
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // what a piece of the vocabulary may take of the workspace
 constexpr int64_t kCus = 256;
-constexpr int kRowsPerLaunch = 1 << 15;
+constexpr int kRowsPerLaunch = 1 << 14;  // 2^23 tokens of so many rows stay below 2^32 threads
 
 __host__ __device__ inline int64_t round_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
 __host__ __device__ constexpr int step_elements(int dtype) { return kStepBytes / bytes_of(dtype); }
@@ -49,16 +49,17 @@ struct Totals {
 __global__ __launch_bounds__(256) void lay_out(const char *src, int64_t ld, int n_rows, int bytes, const int32_t *list, const Totals *totals,
                                                char *out, int out_bytes) {
     const int count = totals ? totals->rows : n_rows, pieces = out_bytes / 16;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t r = i / pieces;
-    const int c = (int)(i % pieces) * 16;
-    if (r >= (totals ? padded_rows(count) : n_rows)) return;
-    u4 v = {0, 0, 0, 0};
-    if (r < count && c < bytes) {
-        const char *q = src + (list ? (int64_t)list[r] : r) * ld + c;
-        v = c + 16 <= bytes ? (u4)*reinterpret_cast<const u4b *>(q) : load_some(q, bytes - c);
+    const int64_t end = (totals ? padded_rows(count) : n_rows) * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < end; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / pieces;
+        const int c = (int)(i % pieces) * 16;
+        u4 v = {0, 0, 0, 0};
+        if (r < count && c < bytes) {
+            const char *q = src + (list ? (int64_t)list[r] : r) * ld + c;
+            v = c + 16 <= bytes ? (u4)*reinterpret_cast<const u4b *>(q) : load_some(q, bytes - c);
+        }
+        *reinterpret_cast<u4 *>(out + r * out_bytes + c) = v;
     }
-    *reinterpret_cast<u4 *>(out + r * out_bytes + c) = v;
 }
 
 // ------------------------------------------------------------------------------------------------ forward
@@ -419,7 +420,7 @@ Side matrix(const void *p, int64_t ld, int64_t n, int64_t width, int64_t e) { re
 void copy_rows(const void *src, int64_t ld, int64_t n_rows, int64_t width, int64_t e, const int32_t *list, const Totals *totals, char *out,
                int64_t out_width, hipStream_t stream) {
     const int64_t pieces = (totals ? padded_rows(n_rows) : n_rows) * out_width * e / 16;
-    lay_out<<<(unsigned int)((pieces + 255) / 256), 256, 0, stream>>>(static_cast<const char *>(src), ld * e, (int)n_rows, (int)(width * e), list, totals,
+    lay_out<<<(unsigned int)std::min<int64_t>((pieces + 255) / 256, 1 << 20), 256, 0, stream>>>(static_cast<const char *>(src), ld * e, (int)n_rows, (int)(width * e), list, totals,
                                                                   out, (int)(out_width * e));
 }
 

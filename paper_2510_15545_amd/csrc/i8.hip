@@ -14,7 +14,7 @@ using namespace tiles;
 using rows::round256;
 
 typedef Shape<128, 128, 2, 2> Any;  // of the product of matrices that lie in any way
-constexpr int kRowsPerLaunch = 1 << 15;
+constexpr int kRowsPerLaunch = 1 << 14;
 
 // fp32 quotients x / s rounded as a division rounds them, from r = 1 / s correctly rounded (Markstein 1990: a product and one
 // correction by the exact remainder), where s is far from fp32's ends.  A tiny x leaves a remainder that is not exact, and a

@@ -157,7 +157,7 @@ __device__ __forceinline__ void product_any(const Side &a, const Side &b, int m0
     __syncthreads();
 }
 
-// ------------------------------------------------------------------------------------------------ wide tiles
+// ------------------------------------------------------------------------------------------------ tiles by loads to LDS
 typedef __attribute__((address_space(3))) void *lds_ptr;
 
 // Tiles of 64 C columns (rows of the second operand).  Wide: 256 rows of the first operand, 8 waves of 128 x 16 C, one
@@ -165,7 +165,7 @@ typedef __attribute__((address_space(3))) void *lds_ptr;
 // groups of four: block 4 i + c of a side for a few c.
 template <int C>
 struct Wide {
-    static constexpr int TM = 256, TN = 64 * C, COLUMNS = C, WAVES = 8, WM = 2, WN = 4, THREADS = 512, FM = 8, FN = C, PER_CU = 1;
+    static constexpr int TM = 256, TN = 64 * C, COLUMNS = C, WAVES = 8, WM = 2, WN = 4, THREADS = 512, FM = 8, FN = C;
     static __device__ __forceinline__ int row_c(int wave, int i) { return (wave >> 2) * 2 + (i >> 2); }
     static __device__ __forceinline__ int column_c(int wave, int) { return wave & 3; }
     static constexpr __device__ int row_i(int i) { return i & 3; }
@@ -175,7 +175,7 @@ struct Wide {
 };
 template <int C>
 struct Half {
-    static constexpr int TM = 128, TN = 64 * C, COLUMNS = C, WAVES = 4, WM = 2, WN = 2, THREADS = 256, FM = 4, FN = 2 * C, PER_CU = 2;
+    static constexpr int TM = 128, TN = 64 * C, COLUMNS = C, WAVES = 4, WM = 2, WN = 2, THREADS = 256, FM = 4, FN = 2 * C;
     static __device__ __forceinline__ int row_c(int wave, int i) { return (wave >> 1) * 2 + (i >> 1); }
     static __device__ __forceinline__ int column_c(int wave, int j) { return (wave & 1) * 2 + (j & 1); }
     static constexpr __device__ int row_i(int i) { return i & 1; }
@@ -273,13 +273,17 @@ struct Operand {
 // The tile at (m0, n0) of the product over the steps [step0, step0 + steps).  Needs 16-byte aligned rows; k contiguous: whole
 // steps of 128 bytes.
 //
-// Waves 0-3 hold half of the blocks of 16 rows, 4-7 the other half; every SIMD runs one of each.  A step is two halves
-// of k: reads from LDS, barrier, matrix instructions, barrier.  The second half's waves are one barrier
-// behind, so that on every SIMD one wave's reads lie beside the other's matrix instructions.  The second operand (hidden states,
-// tokens: it comes from the L2) is loaded a step ahead, the first one (the weights, from HBM) two: one was too short for it
-// (8-bit 288 x 128,256 x 2,048 132 us against 127, the gradient of 391 x 50,257 x 1,024 201 against 191).
+// Wide tiles: waves 0-3 hold half of the blocks of 16 rows, 4-7 the other half; every SIMD runs one of each.  A step is two
+// halves of k: reads from LDS, barrier, matrix instructions, barrier.  The second half's waves are one barrier behind, so
+// that on every SIMD one wave's reads lie beside the other's matrix instructions.  The second operand (hidden states, tokens: it
+// comes from the L2) is loaded a step ahead, the first one (the weights, from HBM) two: one was too short for it (8-bit 288 x
+// 128,256 x 2,048 132 us against 127, the gradient of 391 x 50,257 x 1,024 201 against 191).
+// 8,192^3 with plain stores: bf16 790 us, 1,390 TFLOP/s, 8 bits 420 us, 2,600 TOP/s; the matrix instructions take 61 to 65% of
+// the cycles, and the clock falls to 1.7 GHz under them: fewer cycles (a twenty-fifth less by even halves) gain little in bf16.
+// Blocks of 32 x 32 are slower (1,330 and 2,460).
 //
-// Half tiles: two workgroups to a compute unit, whose reads, matrix instructions, beginnings and ends lie beside each other as they come.
+// Half tiles: two workgroups to a compute unit, whose reads, matrix instructions, beginnings and ends lie beside each other as
+// they come.
 template <int DT, bool AKM, bool BKM, typename S>
 struct Product {
 static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0, int n0, int step0, int steps, char *lds,
@@ -311,9 +315,11 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
         if (but_first) __builtin_amdgcn_s_waitcnt(0x0f70 | Operand<DT, AKM, S::TM, S::WAVES>::N);
         else __builtin_amdgcn_s_waitcnt(0x0f70);
     };
-    const auto barrier = [] {
+    const auto barrier = [] {  // which to the compiler touches no memory: nothing is to be moved across it
         __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" : : : "memory");
         __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
     constexpr int A = S::TM * kStepBytes, B = S::TN * kStepBytes;
@@ -377,8 +383,9 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
 
 // ------------------------------------------------------------------------------------------------ few rows
 // Products with few rows of the second operand, bound by the reading of the first: it goes from memory to registers once, 16
-// rows to a wave, 8 loads of 16 bytes a lane ahead (4 where the columns' sums need the registers); the second operand waits in LDS (all of it, or a chunk of k at a time).
-// Any alignment, any width.
+// rows to a wave, 8 loads of 16 bytes a lane ahead (4 where the columns' sums need the registers); the second operand waits in
+// LDS (all of it, or a chunk of k at a time).  Any alignment, any width.  17 to 64 rows: 128,256 x 2,048 bf16 124 us (4.2
+// TB/s), 8 bits 57 to 76.
 constexpr int kThinThreads = 512, kThinRows = kThinThreads / 64 * 16;  // rows of the first operand that a workgroup takes at a time
 constexpr int kThinLds = 65536;                                      // two workgroups to a compute unit
 constexpr int kThinGroups = 512;                                     // workgroups at most: as many as run at once
@@ -456,7 +463,8 @@ __device__ __forceinline__ void product_thin(const Side &w, const Side &x, char 
 // Up to 16 rows of the second operand: 16 rows of the first to a workgroup, whose 8 waves lie side by side along k, 128 bytes of a
 // row each, so that 1 KB of a row is read at a time (the same bytes 16 rows by 64 bytes a wave come at 5.2 TB/s, these at 5.9 to
 // 6.1, read in order at 6.8).  Loads roll through four such KBs: what has been multiplied makes room for the one four further on,
-// in this row or the next.  The waves' sums are joined in LDS; then thread t (of 256) has row t % 16 and column t / 16.
+// in this row or the next.  The waves' sums are joined in LDS; then thread t (of 256) has row t % 16 and column t / 16.  8 x
+// 151,936 x 2,048 bf16 (622 MB) 108 us, 5.8 TB/s.
 constexpr int kFewMost = 16, kFewRows = 16, kFewBytes = 1024;
 
 // finish(m, n, y): one result.  WHOLE: rows of whole KBs, loaded without a branch (past the last row the last one again).
