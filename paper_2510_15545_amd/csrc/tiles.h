@@ -575,7 +575,7 @@ void with_shape(int64_t m, int64_t n, F f) {
     const int64_t tiles = (n + 255) / 256;
     const int columns = (int)(((n + tiles - 1) / tiles + 63) / 64);
     if constexpr (U != kGradWeight) {
-        if ((U != kGradHidden && (m + 127) / 128 * ((n + 127) / 128) <= 256) || (DT == TT_F32 && n <= 64)) return f(Half<1>());
+        if ((U != kGradHidden && (m + 127) / 128 * ((n + 127) / 128) <= 256) || ((DT == TT_F32 || U == kGradLogits) && n <= 64)) return f(Half<1>());
     }
     if constexpr (DT == TT_F32) f(Half<2>());
     else if (n <= (U == kGradLogits || U == kGradWeight ? 512 : 128)) f(Half<2>());

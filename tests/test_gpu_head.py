@@ -158,6 +158,23 @@ def test_row_weights_of_very_different_sizes(name):
         close(dx[i:i + 1], want, off, f"row {i}")
 
 
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("n,v,h", [(1, 640, 64), (1, 5000, 200), (3, 700, 64), (17, 300, 65), (64, 1000, 128)])
+def test_few_rows_keep_what_rounding_takes(n, v, h, name):
+    """Up to 64 rows: errors of the one rounding of the result (at most half a step of every value, and what the logits' sums are
+    off), not of the logits' gradient's as well."""
+    x, w, ids, beta = uh.operands(n, v, h, name)
+    g, _ = weights(n)
+    stats = tt.head_logprobs(v, x, w, ids, inv_temperature=beta).stats
+    got = tt.head_logprobs_backward(v, x, w, ids, stats, g, inv_temperature=beta)
+    want = uh.backward(x, w, ids, stats, g, None, beta, name)[:2]
+    for a, b in zip(got, want):
+        # errors uniform within half a step, which is at most HALF_STEP of the value: a mean square of at most HALF_STEP^2 / 3,
+        # known to 0.9 / sqrt(N) of it for N equal values, N / 3 of normal ones: the root to four of 0.45 sqrt(3 / N)
+        most = uh.HALF_STEP[name] * (3.0 ** -0.5 * (1 + 4 * 0.45 * (3 / b.numel()) ** 0.5) + 2.0 ** -5)
+        assert float((a.double() - b).norm() / b.norm()) <= most
+
+
 def test_one_gradient_alone():
     x, w, ids, beta = uh.operands(40, 300, 64, "bf16")
     g, _ = weights(40)
