@@ -636,9 +636,10 @@ int tt_head_logprobs(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, const 
  *                rounded once to nearest even; elements past h in a row are left alone.  They must meet neither the
  *                operands nor each other.
  * A row with g = w = 0, or with M minus infinity, gets zeros, adds nothing to dweight and is not read (NaN in it is harmless).
- * The logits are formed again, a piece of the vocabulary at a time; dx is rounded to the operands' type (in up to 64 rows of 16
- * bits to twice its digits) relative to the largest beta (|g| + |w|) of the rows before it is multiplied: in fp16 a row whose weight is below
- * 2^-20 of the largest loses digits.  Sums are fp32, without atomics.  With n_rows = 0 dweight is zeros.
+ * The logits are formed again, a piece of the vocabulary at a time; dx is held in the operands' type, in 16 bits with what that
+ * rounding takes off it beside it (twice the type's digits), relative to the largest beta (|g| + |w|) of the rows, before it is
+ * multiplied: in fp16 a row whose weight is below 2^-20 of the largest loses digits.  Sums are fp32, without atomics.  With n_rows = 0
+ * dweight is zeros.
  * workspace: tt_head_logprobs_backward_workspace_size bytes serve every call of up to n_rows rows, a call uses
  * ..._workspace_used bytes.  Errors and workspaces as for tt_head_logprobs, and TT_EINVAL for gradients that meet something.
  */

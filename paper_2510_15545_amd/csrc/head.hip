@@ -7,7 +7,7 @@
 // Forward: one product by tiles (tiles.h), whose epilogue leaves each tile's largest logit and sum of exponentials for
 // every row, and a second kernel that joins a row's parts.  Backward: the rows that carry a weight are gathered; then, for
 // one piece of the vocabulary after another, the product again with an epilogue that makes dz of it, rounded to the operands'
-// type (relative to the largest row weight, so that a small weight costs no digits; kRemainders), and two more products: dx += dz W (in
+// type twice, itself and what that takes off it (relative to the largest row weight; kBeside), and two more products: dx += dz W (in
 // fp32, over all pieces) and the piece's rows of dW, written once.  Of these three products' operands dz, W and x each is kept
 // as it is, whichever of its indices is summed over (tiles.h).  No atomics: results do not depend on scheduling.
 #include <algorithm>
@@ -38,11 +38,12 @@ struct Row {
     float c, m, l, g, w;
     int32_t id;
 };
-// Up to so many 16-bit rows what rounding takes off dz is kept as rows of its own, this many or half as many further on, beside
-// the same hidden states again: the roundings of few rows' largest entries do not average out, and the tiles have room.  The error
-// is then that of rounding the result (1.00 times; without it up to 1.47 at one row, 1.31 to 1.44 at 66 to 100), for 8 rows x
-// 100,000 tokens x 320 in 102 us instead of 95, for 64 x 32,000 x 1,024 in 88 instead of 76.
-constexpr int kRemainders = 64;
+// In 16 bits what rounding takes off dz is kept beside it, so that dz has twice the type's digits and the gradients' error is that
+// of rounding the result once (1.00 times; without it 1.3 to 1.5).  Up to kBeside rows as rows of their own, this many or half
+// as many further on, beside the same hidden states again: the tiles have room (8 rows x 100,000 tokens x 320: 102 us, 95 without;
+// 64 x 32,000 x 1,024: 88, 76 without).  From there on as a second matrix behind the first, and both products go through both (66 x
+// 32,000 x 1,024: 102 us, 83 without; 391 x 50,257 x 1,024 fp16: 196 to 276; 2,048 x 128,256 x 2,048: 2.90 ms to 4.67).
+constexpr int kBeside = 64;
 
 struct Totals {
     int32_t rows;  // that carry a weight
@@ -246,10 +247,11 @@ __global__ __launch_bounds__(1024) void head_select(int n, int v, const float *i
     if (t == 0) *totals = {before, top / store_scale};
 }
 
-// dz of a piece's tokens (the first of them v0) for the listed rows, stored as [row][token].
-// AGAIN: with the remainders, `again` rows further on.
-template <int DT, typename S, bool AGAIN>
-__global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, int mt, int nt, int v0, const Row *meta, const Totals *totals, int again, char *d, int64_t d_ld) {
+// dz of a piece's tokens (the first of them v0) for the listed rows, stored as [row][token] up to row n_end; in 16 bits the
+// remainders `rest` rows further on.
+template <int DT, typename S>
+__global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, int mt, int nt, int v0, const Row *meta, const Totals *totals, int rest, int n_end, char *d,
+                                                              int64_t d_ld) {
     TT_TILE_LDS(S);
     using T = typename rows::Elem<DT>::T;
     f4 acc[S::FM][S::FN];
@@ -274,21 +276,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
     __syncthreads();
     special = *flag != 0;
     __syncthreads();
-    char *second = lds + S::TM * kStepBytes;
-    const int n_end = AGAIN ? again : INT_MAX;
-    const auto store_remainders = [&](auto values) {
-        __syncthreads();
-        store_tile<DT, S>(m0, (int)d_ld, n0, again, lds, second, [&](int n, int j, int m, int i, float (&y)[4]) {
-            values(n, j, m, i, y);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float stored = rows::decode<DT>(rows::encode<DT>(y[q]));
-                y[q] = fabsf(stored) < INFINITY ? y[q] - stored : 0.0f;
-            }
-        }, [&](int n) { return to(n + again); });
+    const auto store = [&](auto values) {
+        store_tile<DT, S, DT != TT_F32>(m0, (int)d_ld, n0, n_end, lds, lds + S::TM * kStepBytes, values, to, rest * d_ld);
     };
     if (special) {
-        const auto values = [&](int, int j, int m, int i, float (&y)[4]) {
+        store([&](int, int j, int m, int i, float (&y)[4]) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float e = exponent(acc[i][j][q], j), p = __builtin_amdgcn_exp2f(e);
@@ -296,25 +288,21 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
                 if (v0 + m + q == r[j].id) y[q] = r[j].g * -expm1f(e * (float)rows::kLn2) + r[j].w * p;  // 1 - p not as a difference
                 if (m + q >= w.rows) y[q] = 0.0f;
             }
-        };
-        store_tile<DT, S>(m0, (int)d_ld, n0, n_end, lds, second, values, to);
-        if constexpr (AGAIN) store_remainders(values);
+        });
     } else {
-        const auto values = [&](int, int j, int, int i, float (&y)[4]) {
+        store([&](int, int j, int, int i, float (&y)[4]) {
             const float f = r[j].w - r[j].g;
 #pragma unroll
             for (int q = 0; q < 4; ++q) y[q] = f * __builtin_amdgcn_exp2f(exponent(acc[i][j][q], j));
-        };
-        store_tile<DT, S>(m0, (int)d_ld, n0, n_end, lds, second, values, to);
-        if constexpr (AGAIN) store_remainders(values);
+        });
     }
 }
 
 // dx of the listed rows over one piece of the vocabulary, split into parts of its tokens, added to what the pieces before
-// gave: sums[split][row][h] in fp32.
+// gave: sums[split][row][h] in fp32.  twice, rest: the remainders are a second matrix.
 template <int DT, typename S>
 __global__ __launch_bounds__(S::THREADS, 2) void head_dhidden(Side w, Side d, int mt, int nt, int split_steps, const Totals *totals, float *sums, int64_t ld,
-                                                    int64_t plane, int first) {
+                                                    int64_t plane, int first, int twice, int64_t rest) {
     TT_TILE_LDS(S);
     f4 acc[S::FM][S::FN];
     const int split = (int)blockIdx.x / (mt * nt);
@@ -324,7 +312,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dhidden(Side w, Side d, in
     n0 *= S::TN;
     if (n0 >= totals->rows) return;
     const int steps = (w.rows + step_elements(DT) - 1) / step_elements(DT), from = split * split_steps;
-    Product<DT, true, false, S>::run(w, d, m0, n0, from, min(split_steps, steps - from), lds, acc);
+    Product<DT, true, false, S>::run(w, d, m0, n0, from, min(split_steps, steps - from), lds, acc, twice, rest);
     for_columns<S>(n0, [&](int n, int j) {
         float *out = sums + split * plane + (int64_t)n * ld;
         for_rows<S>(m0, [&](int m, int i) {
@@ -359,7 +347,8 @@ __global__ __launch_bounds__(256) void head_place(const float *sums, int64_t ld,
 
 // A piece's rows of dW.
 template <int DT, typename S>
-__global__ __launch_bounds__(S::THREADS, 2) void head_dweight(Side x, Side d, int mt, int nt, const Totals *totals, int again, int n_tokens, int h, void *dweight, int64_t ld) {
+__global__ __launch_bounds__(S::THREADS, 2) void head_dweight(Side x, Side d, int mt, int nt, const Totals *totals, int again, int n_tokens, int h, void *dweight, int64_t ld,
+                                                              int twice, int64_t rest) {
     TT_TILE_LDS(S);
     using T = typename rows::Elem<DT>::T;
     f4 acc[S::FM][S::FN];
@@ -368,7 +357,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dweight(Side x, Side d, in
     m0 *= S::TM;
     n0 *= S::TN;
     const int n_rows = totals->rows == 0 ? 0 : again ? 2 * again : totals->rows, steps = (n_rows + step_elements(DT) - 1) / step_elements(DT);
-    Product<DT, true, true, S>::run(x, d, m0, n0, 0, steps, lds, acc);
+    Product<DT, true, true, S>::run(x, d, m0, n0, 0, steps, lds, acc, twice, rest);
     const float scale = totals->scale;
     store_tile<DT, S>(m0, h, n0, n_tokens, lds, lds + S::TM * kStepBytes, [&](int, int j, int, int i, float (&y)[4]) {
 #pragma unroll
@@ -399,14 +388,15 @@ struct ForwardLayout : Layout {
 };
 
 struct BackwardLayout : Layout {
-    int64_t n_pad, width, piece;  // width: elements of a hidden state in a copy
+    int64_t n_pad, d_rows, width, piece;  // d_rows: of dz with its remainders; width: elements of a hidden state in a copy
     int splits;
     size_t totals, place, list, meta, x, w, d, sums;
     BackwardLayout(int64_t n, int64_t v, int64_t h, int dtype) {
         const int64_t e = rows::element_bytes(dtype), all = round_to(v, kAlign);
         n_pad = padded_rows(n);
+        d_rows = stored_rows(n, dtype);
         width = round_to(h, step_elements(dtype));
-        const int64_t row = (n_pad + width) * e;  // of dz and of the weights' copy, for a token
+        const int64_t row = (d_rows + width) * e;  // of dz and of the weights' copy, for a token
         piece = std::min(all, std::max<int64_t>(kAlign, kPieceBytes / row / kAlign * kAlign));
         // pieces of one size, in whole rounds of the compute units where there are several
         const int64_t round = std::max<int64_t>(1, kCus / row_tiles(n, dtype)) * kTile, even = round_to(tiles_of(all, tiles_of(all, piece)), kAlign);
@@ -414,7 +404,7 @@ struct BackwardLayout : Layout {
         const int64_t tiles = row_tiles(n, dtype) * tiles_of(width, dtype == TT_F32 ? 128 : kTile);
         splits = (int)std::min<int64_t>(std::max<int64_t>(1, kSplitTiles / tiles), std::max<int64_t>(1, all / (dtype == TT_F32 ? 128 : 512)));  // at least 4 or 8 steps each
         rows_of(n, e);
-        d = take((size_t)(piece * n_pad * e));
+        d = take((size_t)(piece * d_rows * e));
         w = take((size_t)(piece * width * e));
         sums = take((size_t)(splits * n_pad * width * 4));
     }
@@ -425,7 +415,7 @@ struct BackwardLayout : Layout {
         l.n_pad = padded_rows(n);
         l.width = round_to(h, step_elements(dtype));
         l.rows_of(n, e);
-        const int64_t row = (l.n_pad + l.width) * e;
+        const int64_t row = (stored_rows(n, dtype) + l.width) * e;
         l.take((size_t)std::min(round_to(v, kAlign) * row, std::max(kAlign * row, kPieceBytes)) + 256);
         l.take((size_t)(std::max(kSplitTiles / tiles_of(l.width, kTile), row_tiles(n, dtype)) * 384 * l.width * 4));  // n_pad is at most 384 a tile
         return l.total;
@@ -433,6 +423,7 @@ struct BackwardLayout : Layout {
 
   private:
     BackwardLayout() {}
+    static int64_t stored_rows(int64_t n, int dtype) { return (dtype != TT_F32 && n > kBeside ? 2 : 1) * padded_rows(n); }
     static int64_t row_tiles(int64_t n, int dtype) { return tiles_of(n, dtype == TT_F32 ? 128 : 256); }
     void rows_of(int64_t n, int64_t e) {
         totals = take(sizeof(Totals));
@@ -498,10 +489,10 @@ bool copies_weight(const HeadGradArgs &a) {
     return !whole_steps(w);
 }
 
-// Rows that the remainders lie behind, 0 where none are kept.
+// Rows that the remainders lie behind as rows of their own, 0 where they do not.
 template <int DT>
-int remainders(const HeadGradArgs &a) {
-    return DT == TT_F32 || a.n_rows > kRemainders ? 0 : a.n_rows > kRemainders / 2 ? kRemainders : kRemainders / 2;
+int beside(const HeadGradArgs &a) {
+    return DT == TT_F32 || a.n_rows > kBeside ? 0 : a.n_rows > kBeside / 2 ? kBeside : kBeside / 2;
 }
 
 template <int DT>
@@ -514,18 +505,14 @@ void backward_piece(const HeadGradArgs &a, const BackwardLayout &lay, char *ws, 
         copy_rows(weight, a.w_ld, here, a.h, e, nullptr, nullptr, 0, ws + lay.w, lay.width, stream);
         w = matrix(ws + lay.w, lay.width, here, lay.width, e);
     }
+    const int again = beside<DT>(a), twice = lay.d_rows > lay.n_pad;
+    const int64_t rest = lay.n_pad * lay.piece * e;
     const Side x = matrix(ws + lay.x, lay.width, lay.n_pad, lay.width, e), d = matrix(ws + lay.d, lay.piece, lay.n_pad, lay.piece, e);
     with_shape<DT, kGradLogits>(here, a.n_rows, [&](auto shape) {
         typedef decltype(shape) S;
         const int mt = (int)tiles_of(here, S::TM), nt = (int)tiles_of(a.n_rows, S::TN);
-        const auto run = [&](auto kernel) {
-            kernel<<<mt * nt, S::THREADS, 0, stream>>>(w, x, mt, nt, (int)v0, reinterpret_cast<const Row *>(ws + lay.meta), totals, remainders<DT>(a),
-                                                      ws + lay.d, lay.piece);
-        };
-        if constexpr (DT != TT_F32 && S::TN == 64) {  // which up to 64 rows have
-            if (remainders<DT>(a)) return run(head_dlogits<DT, S, true>);
-        }
-        run(head_dlogits<DT, S, false>);
+        head_dlogits<DT, S><<<mt * nt, S::THREADS, 0, stream>>>(w, x, mt, nt, (int)v0, reinterpret_cast<const Row *>(ws + lay.meta), totals,
+                                                                again ? again : (int)lay.n_pad, again ? again : INT_MAX, ws + lay.d, lay.piece);
     });
     if (a.dhidden)
         with_shape<DT, kGradHidden>(a.h, a.n_rows, [&](auto shape) {
@@ -533,14 +520,14 @@ void backward_piece(const HeadGradArgs &a, const BackwardLayout &lay, char *ws, 
             const int mt = (int)tiles_of(a.h, S::TM), nt = (int)tiles_of(a.n_rows, S::TN);
             const int steps = (int)tiles_of(here, step_elements(DT)), split = (int)tiles_of(steps, lay.splits);
             head_dhidden<DT, S><<<mt * nt * lay.splits, S::THREADS, 0, stream>>>(w, d, mt, nt, split, totals, reinterpret_cast<float *>(ws + lay.sums),
-                                                                              lay.width, lay.n_pad * lay.width, v0 == 0);
+                                                                              lay.width, lay.n_pad * lay.width, v0 == 0, twice, rest);
         });
     if (a.dweight)
         with_shape<DT, kGradWeight>(a.h, a.n_rows, [&](auto shape) {
             typedef decltype(shape) S;
             const int mt = (int)tiles_of(a.h, S::TM), nt = (int)tiles_of(here, S::TN);
-            head_dweight<DT, S><<<mt * nt, S::THREADS, 0, stream>>>(x, d, mt, nt, totals, remainders<DT>(a), (int)here, a.h,
-                                                                    static_cast<char *>(a.dweight) + v0 * a.dw_ld * e, a.dw_ld);
+            head_dweight<DT, S><<<mt * nt, S::THREADS, 0, stream>>>(x, d, mt, nt, totals, again, (int)here, a.h,
+                                                                    static_cast<char *>(a.dweight) + v0 * a.dw_ld * e, a.dw_ld, twice, rest);
         });
 }
 
@@ -553,11 +540,11 @@ int backward(const HeadGradArgs &a, char *ws, hipStream_t stream) {
     int32_t *place = reinterpret_cast<int32_t *>(ws + lay.place), *list = reinterpret_cast<int32_t *>(ws + lay.list);
     head_select<<<1, 1024, 0, stream>>>(a.n_rows, a.v, a.inv_temp, a.ids, a.stats, a.grad, a.grad_lse, DT == TT_F16 ? 0x1p14f : 1.0f, place, list,
                                         reinterpret_cast<Row *>(ws + lay.meta), totals);
-    copy_rows(a.hidden, a.x_ld, a.n_rows, a.h, e, list, totals, remainders<DT>(a), ws + lay.x, lay.width, stream);
+    copy_rows(a.hidden, a.x_ld, a.n_rows, a.h, e, list, totals, beside<DT>(a), ws + lay.x, lay.width, stream);
     for (int64_t v0 = 0; v0 < a.v; v0 += lay.piece) backward_piece<DT>(a, lay, ws, v0, copy_w, stream);
     if (a.dhidden)
         head_place<DT><<<dim3(a.n_rows, (unsigned int)tiles_of(a.h, 1024)), 256, 0, stream>>>(reinterpret_cast<float *>(ws + lay.sums), lay.width,
-                                                                                         lay.n_pad * lay.width, lay.splits, place, totals, remainders<DT>(a), a.h,
+                                                                                         lay.n_pad * lay.width, lay.splits, place, totals, beside<DT>(a), a.h,
                                                                                          a.dhidden, a.dx_ld);
     return status();
 }

@@ -231,8 +231,9 @@ struct Operand {
             }
         }
     }
-    __device__ __forceinline__ void fetch(char *tile, int t) const {
-        const uint64_t from = reinterpret_cast<uint64_t>(p) + (KM ? (int64_t)t * K * ld : (int64_t)t * kStepBytes);
+    // more: bytes to a matrix of the same form.
+    __device__ __forceinline__ void fetch(char *tile, int t, int64_t more = 0) const {
+        const uint64_t from = reinterpret_cast<uint64_t>(p) + (KM ? (int64_t)t * K * ld : (int64_t)t * kStepBytes) + more;
         const u4 memory = {(uint32_t)from, (uint32_t)(from >> 32), 0xFFFFFFFFu, 0x00027000u};
         const uint32_t to = (uint32_t)reinterpret_cast<uintptr_t>((lds_ptr)tile) + wave * N * 1024;
         if (KM && (t + 1) * K > lines) {
@@ -271,7 +272,8 @@ struct Operand {
 #define TT_TILE_LDS(S) __shared__ __attribute__((aligned(1024))) char lds[(3 * S::TM + 2 * S::TN) * kStepBytes]
 
 // The tile at (m0, n0) of the product over the steps [step0, step0 + steps).  Needs 16-byte aligned rows; k contiguous: whole
-// steps of 128 bytes.
+// steps of 128 bytes.  twice = 1: the second operand is a sum of two matrices, `rest` bytes apart; each step of the first is
+// multiplied with the one's, then the other's.
 //
 // Wide tiles: waves 0-3 hold half of the blocks of 16 rows, 4-7 the other half; every SIMD runs one of each.  A step is two
 // halves of k: reads from LDS, barrier, matrix instructions, barrier.  The second half's waves are one barrier behind, so
@@ -287,7 +289,7 @@ struct Operand {
 template <int DT, bool AKM, bool BKM, typename S>
 struct Product {
 static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0, int n0, int step0, int steps, char *lds,
-                                           typename Mfma<DT>::Acc (&acc)[S::FM][S::FN]) {
+                                           typename Mfma<DT>::Acc (&acc)[S::FM][S::FN], int twice = 0, int64_t rest = 0) {
     Operand<DT, AKM, S::TM, S::WAVES> oa;
     Operand<DT, BKM, S::TN, S::WAVES> ob;
 #pragma unroll
@@ -324,14 +326,15 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
     };
     constexpr int A = S::TM * kStepBytes, B = S::TN * kStepBytes;
     char *const bs = lds + 3 * A;
+    steps <<= twice;
     oa.fetch(lds, 0);
     ob.fetch(bs, 0);
-    if (steps > 1) oa.fetch(lds + A, 1);
+    if (steps > 1) oa.fetch(lds + A, 1 >> twice);
     const char *at = lds, *bt = bs;
     char *to = lds + 2 * A;  // of the step after next
     const auto ahead = [&](int t) {
-        if (t + 1 < steps) ob.fetch(bt == bs ? bs + B : bs, t + 1);
-        if (t + 2 < steps) oa.fetch(to, t + 2);
+        if (t + 1 < steps) ob.fetch(bt == bs ? bs + B : bs, (t + 1) >> twice, (t + 1) & twice ? rest : 0);
+        if (t + 2 < steps) oa.fetch(to, (t + 2) >> twice);
     };
     const auto next = [&] {
         to = const_cast<char *>(at);
@@ -644,11 +647,14 @@ __device__ __forceinline__ void store4(typename rows::Elem<DT>::T *row, int m, i
 // Stores a tile's results, values(n, j, m, i, y) giving four of a column n, to row(n): 16-bit results go through LDS, 64
 // columns at a time, so that every row gets 512 or 256 bytes at once (from the registers it would be 32 at a time); the columns' 16-byte
 // pieces at place piece ^ column there.  m_end, n_end: where the result ends.  For one after another of the columns' groups
-// each thread calls values() for its blocks.
-template <int DT, typename S, typename V, typename R>
-__device__ __forceinline__ void store_tile(int m0, int m_end, int n0, int n_end, char *a0, char *a1, V values, R row) {
+// each thread calls values() for its blocks.  REST (16 bits): what the rounding of a result takes off it is stored `rest`
+// elements further on (0 beside an infinity); four of such LDS pieces are needed, two from a0 on and two more.
+template <int DT, typename S, bool REST = false, typename V, typename R>
+__device__ __forceinline__ void store_tile(int m0, int m_end, int n0, int n_end, char *a0, char *a1, V values, R row, int64_t rest = 0) {
     typedef unsigned int u2 __attribute__((ext_vector_type(2)));
     constexpr int PIECES = S::TM / 8, SAME = S::FN / S::COLUMNS;  // of a row; blocks of a wave in 64 columns
+    constexpr int SECOND = 2 * S::TM * kStepBytes;                // from a result's place in LDS to its rest's
+    static_assert(!REST || 2 * SECOND <= (3 * S::TM + 2 * S::TN) * kStepBytes, "four pieces in a tile's memory");
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
 #pragma unroll
     for (int g = 0; g < S::COLUMNS; ++g) {
@@ -664,19 +670,29 @@ __device__ __forceinline__ void store_tile(int m0, int m_end, int n0, int n_end,
                 if constexpr (DT == TT_F32) {
                     if (n < n_end && m0 + at < m_end) store4<DT>(row(n), m0 + at, m_end, y);
                 } else {
-                    *reinterpret_cast<u2 *>(lds + ((in & 63) * PIECES + ((at >> 3) ^ (in & (PIECES - 1)))) * 16 + (at & 4) * 2) =
-                        u2{rows::encode_pair<DT>(y[0], y[1]), rows::encode_pair<DT>(y[2], y[3])};
+                    char *to = lds + ((in & 63) * PIECES + ((at >> 3) ^ (in & (PIECES - 1)))) * 16 + (at & 4) * 2;
+                    const u2 v = {rows::encode_pair<DT>(y[0], y[1]), rows::encode_pair<DT>(y[2], y[3])};
+                    *reinterpret_cast<u2 *>(to) = v;
+                    if constexpr (REST) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const float stored = rows::decode<DT>(v[q >> 1] >> (q & 1) * 16 & 0xFFFFu);
+                            y[q] = fabsf(stored) < INFINITY ? y[q] - stored : 0.0f;
+                        }
+                        *reinterpret_cast<u2 *>(to + SECOND) = u2{rows::encode_pair<DT>(y[0], y[1]), rows::encode_pair<DT>(y[2], y[3])};
+                    }
                 }
             }
         }
         if constexpr (DT != TT_F32) {
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < 64 * PIECES / S::THREADS; ++k) {
-                const int i = k * S::THREADS + (int)threadIdx.x, r = i / PIECES, c = i % PIECES, m = m0 + c * 8, to = n0 + g * 64 + r;
-                const u4 v = *reinterpret_cast<const u4 *>(lds + (r * PIECES + (c ^ (r & (PIECES - 1)))) * 16);
+            for (int k = 0; k < (REST ? 2 : 1) * 64 * PIECES / S::THREADS; ++k) {
+                const int second = k / (64 * PIECES / S::THREADS), in = k % (64 * PIECES / S::THREADS) * S::THREADS + (int)threadIdx.x;
+                const int r = in / PIECES, c = in % PIECES, m = m0 + c * 8, to = n0 + g * 64 + r;
+                const u4 v = *reinterpret_cast<const u4 *>(lds + second * SECOND + (r * PIECES + (c ^ (r & (PIECES - 1)))) * 16);
                 if (to >= n_end) continue;
-                typename rows::Elem<DT>::T *out = row(to);
+                typename rows::Elem<DT>::T *out = row(to) + second * rest;
                 if (m + 8 <= m_end) *reinterpret_cast<u4b *>(out + m) = v;
                 else {
 #pragma unroll
