@@ -635,7 +635,8 @@ int tt_head_logprobs(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, const 
  *   dhidden, dweight      either may be NULL; n_rows and v rows of h elements of the operands' type at strides of their own,
  *                rounded once to nearest even; elements past h in a row are left alone.  They must meet neither the
  *                operands nor each other.
- * A row with g = w = 0, or with M minus infinity, gets zeros, adds nothing to dweight and is not read (NaN in it is harmless).
+ * A row with g = w = 0, or with M minus infinity, gets zeros, adds nothing to dweight and is not read (NaN in it is harmless).  A
+ * token whose logits are all minus infinity has zeros in dweight; where its weights are infinite dhidden is NaN, as 0 times them.
  * The logits are formed again, a piece of the vocabulary at a time; dx is held in the operands' type, in 16 bits with what that
  * rounding takes off it beside it (twice the type's digits), relative to the largest beta (|g| + |w|) of the rows, before it is
  * multiplied: in fp16 a row whose weight is below 2^-20 of the largest loses digits.  Sums are fp32, without atomics.  With n_rows = 0

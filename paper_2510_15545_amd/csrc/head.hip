@@ -33,7 +33,8 @@ __host__ __device__ inline int64_t round_to(int64_t x, int64_t n) { return (x + 
 __host__ __device__ constexpr int step_elements(int dtype) { return kStepBytes / bytes_of(dtype); }
 inline int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 // A row that carries a weight, for the gradient's epilogue: p = 2^((z - m) c - l), dz = (w - g) p, and g (1 - p) + w p at
-// its token; padding rows are zeros.
+// its token.  What pads the list is its first row again with g = w = 0: hidden states of zeros would make a NaN of an infinite
+// weight, and 0 times it another of dz, which reaches that token's row of dW.
 struct Row {
     float c, m, l, g, w;
     int32_t id;
@@ -52,8 +53,8 @@ struct Totals {
 
 // ------------------------------------------------------------------------------------------------ copies
 // Rows of `bytes` bytes at any address, at a stride of `ld` bytes, into rows of `out_bytes` (a multiple of 16), filled up with zeros.
-// list: the rows by their index in it, totals->rows of them, rounded up with rows of zeros (again: to that many, which are
-// written twice); or null.
+// list: the rows by their index in it, totals->rows of them, padded with the first of them (again: to that many, which are
+// written twice; zeros where there is none); or null.
 __global__ __launch_bounds__(256) void lay_out(const char *src, int64_t ld, int n_rows, int bytes, const int32_t *list, const Totals *totals,
                                                int again, char *out, int out_bytes) {
     const int count = totals ? totals->rows : n_rows, pieces = out_bytes / 16;
@@ -62,8 +63,9 @@ __global__ __launch_bounds__(256) void lay_out(const char *src, int64_t ld, int 
         const int64_t r = i / pieces;
         const int c = (int)(i % pieces) * 16;
         u4 v = {0, 0, 0, 0};
-        const int64_t from = again && r >= again ? r - again : r;
-        if (from < count && c < bytes) {
+        int64_t from = again && r >= again ? r - again : r;
+        if (from >= count) from = 0;
+        if (count > 0 && c < bytes) {
             const char *q = src + (list ? (int64_t)list[from] : from) * ld + c;
             v = c + 16 <= bytes ? (u4)*reinterpret_cast<const u4b *>(q) : load_some(q, bytes - c);
         }
@@ -243,7 +245,8 @@ __global__ __launch_bounds__(1024) void head_select(int n, int v, const float *i
                        beta * g / top * store_scale, beta * w / top * store_scale, ids && g != 0.0f ? ids[i] : -1};
         }
     }
-    for (int i = before + t; i < padded_rows(before); i += 1024) out[i] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, -1};
+    __syncthreads();  // the first row is there
+    for (int i = before + t; i < padded_rows(before); i += 1024) out[i] = {out[0].c, out[0].m, out[0].l, 0.0f, 0.0f, -1};
     if (t == 0) *totals = {before, top / store_scale};
 }
 
