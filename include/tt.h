@@ -640,7 +640,8 @@ int tt_head_logprobs(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, const 
  * The logits are formed again, a piece of the vocabulary at a time; dx is held in the operands' type, in 16 bits with what that
  * rounding takes off it beside it (twice the type's digits), relative to the largest beta (|g| + |w|) of the rows, before it is
  * multiplied: in fp16 a row whose weight is below 2^-20 of the largest loses digits.  Sums are fp32, without atomics.  With n_rows = 0
- * dweight is zeros.
+ * dweight is zeros.  lp_j carries beta times the rounding errors of the logits' sums (up to 16 rows' statistics come of sums in
+ * another order), but none is taken above 0.
  * workspace: tt_head_logprobs_backward_workspace_size bytes serve every call of up to n_rows rows, a call uses
  * ..._workspace_used bytes.  Errors and workspaces as for tt_head_logprobs, and TT_EINVAL for gradients that meet something.
  */

@@ -270,7 +270,9 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) special |= __any(r[j].id - v0 >= m0 && r[j].id - v0 < m0 + S::TM) != 0;
     const auto to = [&](int n) { return reinterpret_cast<T *>(d) + (int64_t)n * d_ld; };
-    const auto exponent = [&](float z, int j) { return fmaf(z - r[j].m, r[j].c, -r[j].l); };
+    // No probability is above 1.  Up to 16 rows' statistics come of sums in another order: the largest logit, formed again, may lie above
+    // M by a rounding, which a large inverse temperature would make an infinity.  (A minimum that is NaN beside a NaN: one instruction.)
+    const auto exponent = [&](float z, int j) { return __builtin_elementwise_minimum(fmaf(z - r[j].m, r[j].c, -r[j].l), 0.0f); };
     // any of the workgroup's (by a word of the tile's memory, of which there is no more)
     int *flag = reinterpret_cast<int *>(lds);
     if (threadIdx.x == 0) *flag = 0;
