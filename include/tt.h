@@ -657,7 +657,7 @@ int tt_head_logprobs_backward(int32_t n_rows, int32_t v, int32_t h, int32_t dtyp
  * tt_quantize_i8 -- rows of k elements (bf16, fp16 or fp32) to 8-bit integers with a scale each:
  *     scale = max |x| / 127 (fp32),  q = x / scale rounded to nearest even, in -127 .. 127.
  * A row of zeros (or with a scale that underflows) has scale 0 and q = 0; a row with a NaN or an infinity scale NaN and q = 0.
- * k <= 131,071.  One kernel on `stream`; q must not meet x.
+ * k <= 131,071.  One kernel on `stream` (for each 2^20 rows, of up to 8 KB 2^22); q must not meet x.
  */
 int tt_quantize_i8(int32_t n_rows, int32_t k, int32_t dtype, const void *x, int64_t x_ld, int8_t *q, int64_t q_ld, float *scale,
                    void *stream);

@@ -15,6 +15,7 @@ using rows::round256;
 
 typedef Shape<128, 128, 2, 2> Any;  // of the product of matrices that lie in any way
 constexpr int kRowsPerLaunch = 1 << 14;
+constexpr int64_t kGroupsPerLaunch = 1 << 20;  // of the quantisation: up to 1,024 threads each, of 2^32 that a launch can have
 
 // fp32 quotients x / s rounded as a division rounds them, from r = 1 / s correctly rounded (Markstein 1990: a product and one
 // correction by the exact remainder), where s is far from fp32's ends.  A tiny x leaves a remainder that is not exact, and a
@@ -109,8 +110,12 @@ void quantize(const QuantizeI8Args &a, hipStream_t stream) {
     constexpr int per = DT == TT_F32 ? 4 : 8;
     const int vectors = (a.k + per - 1) / per;
     const auto run = [&](auto kernel, int rows, int threads) {
-        kernel<<<(unsigned int)((a.n_rows + (int64_t)rows - 1) / rows), threads, 0, stream>>>(
-            a.n_rows, a.k, static_cast<const char *>(a.x), a.ld * rows::element_bytes(DT), a.q, a.q_ld, a.scale);
+        const int64_t ld = a.ld * rows::element_bytes(DT), most = kGroupsPerLaunch * rows;
+        for (int64_t n0 = 0; n0 < a.n_rows; n0 += most) {
+            const int n = (int)std::min<int64_t>(most, a.n_rows - n0);
+            kernel<<<(unsigned int)((n + rows - 1) / rows), threads, 0, stream>>>(n, a.k, static_cast<const char *>(a.x) + n0 * ld, ld, a.q + n0 * a.q_ld,
+                                                                                 a.q_ld, a.scale + n0);
+        }
     };
     if (vectors <= 64) run(quantize_rows<DT, 1, 1>, 4, 256);
     else if (vectors <= 128) run(quantize_rows<DT, 1, 2>, 4, 256);
