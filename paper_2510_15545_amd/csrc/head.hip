@@ -97,7 +97,7 @@ __device__ __forceinline__ void parts_of_tile(const Side &w, const Side &x, int 
                     if (m + q >= w.rows) acc[i][j][q] = -INFINITY;
             });
         });
-    const Part p = column_parts<S>(
+    const Part p = column_parts<S, true>(
         n0, lds, [&](int i, int j, int q) { return acc[i][j][q]; },
         [&](int n) { return (n < n_rows ? rows::scale_of(inv_temp, n) : 1.0f) * rows::kLog2e; });
     const int n = n0 + (int)threadIdx.x;
@@ -136,9 +136,9 @@ __global__ __launch_bounds__(kThinThreads, 4) void head_parts_few(Side w, Side x
     product_few<DT, WHOLE>(w, x, lds, sums, [&](int m, int, float z) {
         if (m >= w.rows) return;
         if (m == id) token[n] = z;
-        add_part(p, z, c);
+        add_part<true>(p, z, c);
     });
-    p = join_quarter(p, c);
+    p = join_quarter<true>(p, c);
     if (((int)threadIdx.x & 15) == 0 && n < x.rows) parts[(int64_t)n * gridDim.x + blockIdx.x] = p;
 }
 
@@ -166,10 +166,10 @@ __global__ __launch_bounds__(kThinThreads, 4) void head_parts_thin(Side w, Side 
                 z[q] = m + q < w.rows ? acc[j][q] : -INFINITY;
                 if (m + q == id[j] && m + q < w.rows) token[j * 16 + column] = acc[j][q];
             }
-            add_part(p[j], z, c[j]);
+            add_part<true>(p[j], z, c[j]);
         }
     });
-    const Part r = join_lanes<FN>(p, x.rows, lds, scale);
+    const Part r = join_lanes<FN, true>(p, x.rows, lds, scale);
     if ((int)threadIdx.x < x.rows) parts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = r;
 }
 

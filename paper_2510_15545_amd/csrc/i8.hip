@@ -157,7 +157,7 @@ __device__ __forceinline__ void scaled(const i4 &sum, float sx, const float *lds
 template <typename S>
 __device__ __forceinline__ void leave_parts(const Side &x, int m0, int n0, const i4 (&acc)[S::FM][S::FN], const Scales &scales, Part *parts, int n_tiles, char *lds) {
     const int n_rows = x.rows;
-    const Part p = column_parts<S>(
+    const Part p = column_parts<S, false>(
         n0, lds, [&](int i, int j, int q) { return __int_as_float(acc[i][j][q]); },
         [&](int n) { return (n < n_rows ? rows::scale_of(scales.inv_temp, n) : 1.0f) * rows::kLog2e; });
     const int n = n0 + (int)threadIdx.x;
@@ -230,10 +230,10 @@ __global__ __launch_bounds__(kThinThreads, 4) void product_i8_few(Side w, Side x
         if (scales.bias) y += scales.bias[m];
         const uint32_t bits = rows::encode<DT>(y);
         row[m] = (T)bits;
-        if constexpr (LSE) add_part(p, rows::decode<DT>(bits), c);  // of the results as they are written
+        if constexpr (LSE) add_part<false>(p, rows::decode<DT>(bits), c);  // of the results as they are written
     });
     if constexpr (LSE) {
-        p = join_quarter(p, c);
+        p = join_quarter<false>(p, c);
         if (((int)threadIdx.x & 15) == 0 && there) parts[(int64_t)column * gridDim.x + blockIdx.x] = p;
     }
 }
@@ -273,12 +273,12 @@ __global__ __launch_bounds__(kThinThreads, 4) void product_i8_thin(Side w, Side 
             if constexpr (LSE) {  // of the results as they are written
 #pragma unroll
                 for (int q = 0; q < 4; ++q) y[q] = m + q < w.rows ? rows::decode<DT>(rows::encode<DT>(y[q])) : -INFINITY;
-                add_part(p[j], y, c[j]);
+                add_part<false>(p[j], y, c[j]);
             }
         }
     });
     if constexpr (LSE) {
-        const Part r = join_lanes<FN>(p, x.rows, lds, scale);
+        const Part r = join_lanes<FN, false>(p, x.rows, lds, scale);
         if ((int)threadIdx.x < x.rows) parts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = r;
     }
 }

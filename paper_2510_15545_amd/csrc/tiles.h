@@ -704,8 +704,10 @@ __device__ __forceinline__ void store_tile(int m0, int m_end, int n0, int n_end,
     }
 }
 
-// Largest value and sum of 2^((z - largest) c) of a set of logits z.  NaN passes through: the sum of a set with a NaN
-// or plus infinity is NaN.
+// Largest value m of a set of logits z, and the sum s of 2^((z - m) c) over the set without one of its largest (a set without logits:
+// minus infinity and 0).  That term is 1, and what the others give beside it is all that ln (1 + s) holds where a token is almost
+// certain: in a sum with the 1 fp32 would keep steps of 2^-24 of it (1 x 640 logits, a log probability of -4e-5: 1.4e-3 off).
+// NaN passes through: s of a set with a NaN or plus infinity is NaN.
 struct Part {
     float m, s;
 };
@@ -716,9 +718,43 @@ __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.
 // (a set without logits has the sum 0, which no factor may make NaN).
 __device__ __forceinline__ float factor(float m, float ref, float c) { return __builtin_amdgcn_exp2f(fminf((reference(m) - ref) * c, 0.0f)); }
 
+constexpr float kNear = 1.03125f;  // a sum from here on leaves 2^-18 of its rest when the 1 is taken off
+
+__device__ __forceinline__ float term(float z, float ref, float c) { return __builtin_amdgcn_exp2f((z - ref) * c); }
+
+// What makes a set's s of those of its parts and logits.  FINE: the terms below 1, and how many are 1; otherwise all of them together,
+// for a log-sum-exp that is wanted beside its largest logit alone.
+template <typename F, bool FINE>
+struct Terms {
+    F s = 0, ones = 0;
+
+    __device__ __forceinline__ void logit(float z, float ref, float c) {
+        const float t = term(z, ref, c), below = FINE ? __builtin_amdgcn_fractf(t) : t;  // 1 to 0, what is below as it is, NaN as well
+        s += below;
+        if (FINE) ones += t - below;
+    }
+    // A set whose largest value may be the whole's, m.
+    __device__ __forceinline__ void part(const Part &p, float m, float c) {
+        const bool top = FINE && p.m == m && m != -INFINITY;
+        const F f = factor(p.m, reference(m), c), one = p.m == -INFINITY ? 0.0f : 1.0f;
+        s += top ? (F)p.s : (one + (F)p.s) * f;
+        if (FINE) ones += top ? 1.0f : 0.0f;
+    }
+    // f(value) for each value that lanes or waves add up.
+    template <typename A>
+    __device__ __forceinline__ void join(A f) {
+        s = f(s);
+        if (FINE) ones = f(ones);
+    }
+    __device__ __forceinline__ F rest(float m) const {
+        if (FINE) return s + (ones > 0 ? ones - 1 : (F)0);
+        return m == -INFINITY ? s : s - 1;
+    }
+};
+
 // The parts of the tile's columns from z(i, j, q) (minus infinity where there is no logit), left in lds[n - n0] for
 // threads below TN after the closing barrier.  scale(n): log2(e) times the row's inverse temperature.
-template <typename S, typename Z, typename C>
+template <typename S, bool FINE, typename Z, typename C>
 __device__ __forceinline__ Part column_parts(int n0, char *lds, Z z, C scale) {
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     const int wm = wave / S::WN;
@@ -726,7 +762,7 @@ __device__ __forceinline__ Part column_parts(int n0, char *lds, Z z, C scale) {
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
         const int at = S::column_block(wave, j) * 16 + (lane & 15);
-        float m = -INFINITY, s = 0.0f;
+        float m = -INFINITY;
 #pragma unroll
         for (int i = 0; i < S::FM; ++i)
 #pragma unroll
@@ -734,13 +770,27 @@ __device__ __forceinline__ Part column_parts(int n0, char *lds, Z z, C scale) {
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
         const float c = scale(n0 + at), ref = reference(m);
+        float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) s += __builtin_amdgcn_exp2f((z(i, j, q) - ref) * c);
+            for (int q = 0; q < 4; ++q) s += term(z(i, j, q), ref, c);
         s += __shfl_xor(s, 16);
         s += __shfl_xor(s, 32);
-        if (lane < 16) part[wm * S::TN + at] = {m, s};
+        float rest = m == -INFINITY ? s : s - 1.0f;
+        // Up to kNear the subtraction would cost digits: the terms again, without the 1 (the terms below 1 beside all of them for every
+        // set: 4,096 x 151,936 x 2,048 36 us more instead of 10 or less, 1,000 x 50,257 x 256 5.4 instead of 1.4)
+        if (FINE && __any(m != -INFINITY && s < kNear)) {
+            s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) s += __builtin_amdgcn_fractf(term(z(i, j, q), ref, c));
+            s += __shfl_xor(s, 16);
+            s += __shfl_xor(s, 32);
+            rest = m != -INFINITY && rest < kNear - 1.0f ? s : rest;  // there is but one 1 below 2
+        }
+        if (lane < 16) part[wm * S::TN + at] = {m, rest};
     }
     __syncthreads();
     Part r = {-INFINITY, 0.0f};
@@ -748,44 +798,49 @@ __device__ __forceinline__ Part column_parts(int n0, char *lds, Z z, C scale) {
         const float c = scale(n0 + (int)threadIdx.x);
 #pragma unroll
         for (int w = 0; w < S::WM; ++w) r.m = fmaxf(r.m, part[w * S::TN + threadIdx.x].m);
-        const float ref = reference(r.m);
+        Terms<float, FINE> terms;
 #pragma unroll
-        for (int w = 0; w < S::WM; ++w) {
-            const Part p = part[w * S::TN + threadIdx.x];
-            r.s += p.s * factor(p.m, ref, c);
-        }
+        for (int w = 0; w < S::WM; ++w) terms.part(part[w * S::TN + threadIdx.x], r.m, c);
+        r.s = terms.rest(r.m);
     }
     return r;
 }
 
 // Adds four logits to a lane's running part.
+template <bool FINE>
 __device__ __forceinline__ void add_part(Part &p, const float (&z)[4], float c) {
-    const float m = fmaxf(fmaxf(p.m, fmaxf(z[0], z[1])), fmaxf(z[2], z[3])), ref = reference(m);
-    p.s *= factor(p.m, ref, c);
+    const float m = fmaxf(fmaxf(p.m, fmaxf(z[0], z[1])), fmaxf(z[2], z[3]));
+    Terms<float, FINE> terms;
+    terms.part(p, m, c);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) p.s += __builtin_amdgcn_exp2f((z[q] - ref) * c);
-    p.m = m;
+    for (int q = 0; q < 4; ++q) terms.logit(z[q], reference(m), c);
+    p = {m, terms.rest(m)};
 }
 
+template <bool FINE>
 __device__ __forceinline__ void add_part(Part &p, float z, float c) {
-    const float m = fmaxf(p.m, z), ref = reference(m);
-    p.s = p.s * factor(p.m, ref, c) + __builtin_amdgcn_exp2f((z - ref) * c);
-    p.m = m;
+    const float m = fmaxf(p.m, z);
+    Terms<float, FINE> terms;
+    terms.part(p, m, c);
+    terms.logit(z, reference(m), c);
+    p = {m, terms.rest(m)};
 }
 
 // The part of 16 lanes that hold one column's.
+template <bool FINE>
 __device__ __forceinline__ Part join_quarter(Part p, float c) {
     float m = p.m;
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-    float s = p.s * factor(p.m, reference(m), c);
+    Terms<float, FINE> terms;
+    terms.part(p, m, c);
 #pragma unroll
-    for (int d = 1; d < 16; d *= 2) s += __shfl_xor(s, d);
-    return {m, s};
+    for (int d = 1; d < 16; d *= 2) terms.join([&](float x) { return x + __shfl_xor(x, d); });
+    return {m, terms.rest(m)};
 }
 
 // The workgroup's part of column threadIdx.x (below n) from its lanes' running parts of columns 16 j + lane % 16.
-template <int FN, typename C>
+template <int FN, bool FINE, typename C>
 __device__ __forceinline__ Part join_lanes(const Part (&p)[FN], int n, char *lds, C scale) {
     Part *all = reinterpret_cast<Part *>(lds);  // [wave][16 FN]
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, waves = (int)blockDim.x / 64, at = (int)threadIdx.x;
@@ -793,26 +848,26 @@ __device__ __forceinline__ Part join_lanes(const Part (&p)[FN], int n, char *lds
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const float m = fmaxf(p[j].m, __shfl_xor(p[j].m, 16)), top = fmaxf(m, __shfl_xor(m, 32));
-        float s = p[j].s * factor(p[j].m, reference(top), scale(j * 16 + (lane & 15)));
-        s += __shfl_xor(s, 16);
-        s += __shfl_xor(s, 32);
-        if (lane < 16) all[wave * 16 * FN + j * 16 + lane] = {top, s};
+        Terms<float, FINE> terms;
+        terms.part(p[j], top, scale(j * 16 + (lane & 15)));
+#pragma unroll
+        for (int d = 16; d < 64; d *= 2) terms.join([&](float x) { return x + __shfl_xor(x, d); });
+        if (lane < 16) all[wave * 16 * FN + j * 16 + lane] = {top, terms.rest(top)};
     }
     __syncthreads();
     Part r = {-INFINITY, 0.0f};
     if (at >= n) return r;
     for (int w = 0; w < waves; ++w) r.m = fmaxf(r.m, all[w * 16 * FN + at].m);
-    for (int w = 0; w < waves; ++w) {
-        const Part q = all[w * 16 * FN + at];
-        r.s += q.s * factor(q.m, reference(r.m), scale(at));
-    }
+    Terms<float, FINE> terms;
+    for (int w = 0; w < waves; ++w) terms.part(all[w * 16 * FN + at], r.m, scale(at));
+    r.s = terms.rest(r.m);
     return r;
 }
 
-// What the n parts of a row give, M and ln S, to the first of its 256 threads.
+// What the n parts of a row give, M and L = ln (1 + s), to the first of its 256 threads.
 __device__ __forceinline__ Part join_row(const Part *part, int n, float beta) {
     __shared__ float tops[4];
-    __shared__ double sums[4];
+    __shared__ double sums[4], ones[4];
     constexpr int kHeld = 4;
     const int t = (int)threadIdx.x, wave = t >> 6;
     Part held[kHeld];  // read once, all at a time
@@ -826,17 +881,20 @@ __device__ __forceinline__ Part join_row(const Part *part, int n, float beta) {
     if ((t & 63) == 0) tops[wave] = m;
     __syncthreads();
     m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const float ref = reference(m), c = beta * rows::kLog2e;
-    double s = 0.0;
-    const auto add = [&](const Part &p) { s += (double)p.s * (double)exp2f(fminf((reference(p.m) - ref) * c, 0.0f)); };
+    const float c = beta * rows::kLog2e;
+    Terms<double, true> terms;
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) add(held[i]);
-    for (int i = kHeld * 256 + t; i < n; i += 256) add(part[i]);
-    s = rows::wave_sum(s);
-    if ((t & 63) == 0) sums[wave] = s;
+    for (int i = 0; i < kHeld; ++i) terms.part(held[i], m, c);
+    for (int i = kHeld * 256 + t; i < n; i += 256) terms.part(part[i], m, c);
+    terms.join([](double x) { return rows::wave_sum(x); });
+    if ((t & 63) == 0) {
+        sums[wave] = terms.s;
+        ones[wave] = terms.ones;
+    }
     __syncthreads();
-    s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    return {m, m == -INFINITY && s == 0.0 ? 0.0f : (float)log(s)};
+    terms.s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    terms.ones = (ones[0] + ones[1]) + (ones[2] + ones[3]);
+    return {m, m == -INFINITY && terms.s == 0.0 ? 0.0f : (float)log1p(terms.rest(m))};
 }
 
 }  // namespace tiles
