@@ -250,6 +250,16 @@ __global__ __launch_bounds__(1024) void head_select(int n, int v, const float *i
     if (t == 0) *totals = {before, top / store_scale};
 }
 
+// ln p in base 2.  No probability is above 1: statistics of another product may have an M a rounding below the largest logit as it is
+// formed here, which a large inverse temperature would make an infinity.  (A minimum that is NaN beside a NaN: one instruction.)
+__device__ __forceinline__ float exponent_of(const Row &r, float z) { return __builtin_elementwise_minimum(fmaf(z - r.m, r.c, -r.l), 0.0f); }
+
+// dz of a token.
+__device__ __forceinline__ float dlogit_of(const Row &r, float z, int token) {
+    const float e = exponent_of(r, z), p = __builtin_amdgcn_exp2f(e);
+    return token == r.id ? r.g * -expm1f(e * (float)rows::kLn2) + r.w * p : (r.w - r.g) * p;  // 1 - p not as a difference
+}
+
 // dz of a piece's tokens (the first of them v0) for the listed rows, stored as [row][token] up to row n_end; in 16 bits the
 // remainders `rest` rows further on.
 template <int DT, typename S>
@@ -270,9 +280,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) special |= __any(r[j].id - v0 >= m0 && r[j].id - v0 < m0 + S::TM) != 0;
     const auto to = [&](int n) { return reinterpret_cast<T *>(d) + (int64_t)n * d_ld; };
-    // No probability is above 1.  Up to 16 rows' statistics come of sums in another order: the largest logit, formed again, may lie above
-    // M by a rounding, which a large inverse temperature would make an infinity.  (A minimum that is NaN beside a NaN: one instruction.)
-    const auto exponent = [&](float z, int j) { return __builtin_elementwise_minimum(fmaf(z - r[j].m, r[j].c, -r[j].l), 0.0f); };
+    const auto exponent = [&](float z, int j) { return exponent_of(r[j], z); };
     // any of the workgroup's (by a word of the tile's memory, of which there is no more)
     int *flag = reinterpret_cast<int *>(lds);
     if (threadIdx.x == 0) *flag = 0;
@@ -288,10 +296,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
         store([&](int, int j, int m, int i, float (&y)[4]) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float e = exponent(acc[i][j][q], j), p = __builtin_amdgcn_exp2f(e);
-                y[q] = (r[j].w - r[j].g) * p;
-                if (v0 + m + q == r[j].id) y[q] = r[j].g * -expm1f(e * (float)rows::kLn2) + r[j].w * p;  // 1 - p not as a difference
-                if (m + q >= w.rows) y[q] = 0.0f;
+                y[q] = m + q < w.rows ? dlogit_of(r[j], acc[i][j][q], v0 + m + q) : 0.0f;
             }
         });
     } else {
@@ -300,6 +305,38 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
 #pragma unroll
             for (int q = 0; q < 4; ++q) y[q] = f * __builtin_amdgcn_exp2f(exponent(acc[i][j][q], j));
         });
+    }
+}
+
+// Up to 16 rows: the logits by the same sums as head_parts_few has, so that what its statistics say of a token that is almost certain
+// holds here, too (1 - p of 1e-4 would be off by a rounding of its logit over 1e-4, a few percent).  d: `again` rows of which the
+// first x.rows are listed ones or pad the list, in 16 bits the remainders' as many; all of whole steps of tokens, zeros elsewhere.
+template <int DT, bool WHOLE>
+__global__ __launch_bounds__(kThinThreads, 4) void head_dlogits_few(Side w, Side x, int v0, const Row *meta, const Totals *totals, int again, char *d, int64_t d_ld) {
+    __shared__ __attribute__((aligned(16))) char lds[kThinLds];
+    __shared__ float sums[8][256];
+    if (totals->rows == 0) return;
+    using T = typename rows::Elem<DT>::T;
+    const int n = (int)threadIdx.x >> 4;
+    const bool there = n < x.rows;
+    const Row r = meta[there ? n : 0];
+    T *row = reinterpret_cast<T *>(d) + n * d_ld;
+    product_few<DT, WHOLE>(w, x, lds, sums, [&](int m, int, float z) {
+        if (!there || m >= w.rows) return;
+        const float y = dlogit_of(r, z, v0 + m);
+        const uint32_t bits = rows::encode<DT>(y);
+        row[m] = (T)bits;
+        if constexpr (DT != TT_F32) {
+            const float stored = rows::decode<DT>(bits);
+            row[again * d_ld + m] = (T)rows::encode<DT>(fabsf(stored) < INFINITY ? y - stored : 0.0f);
+        }
+    });
+    const int end = (int)round_to(w.rows, step_elements(DT)), id = (int)(blockIdx.x * kThinThreads + threadIdx.x), all = (int)gridDim.x * kThinThreads;
+    const int pieces = end * (int)sizeof(T) / 16, more = again - x.rows, tail = end - w.rows;
+    for (int part = 0; part < (DT == TT_F32 ? 1 : 2); ++part) {
+        T *from = reinterpret_cast<T *>(d) + part * again * d_ld;
+        for (int64_t i = id; i < (int64_t)more * pieces; i += all) reinterpret_cast<u4 *>(from + (x.rows + i / pieces) * d_ld)[i % pieces] = u4{0, 0, 0, 0};
+        for (int i = id; i < x.rows * tail; i += all) from[i / tail * d_ld + w.rows + i % tail] = 0;
     }
 }
 
@@ -506,18 +543,25 @@ void backward_piece(const HeadGradArgs &a, const BackwardLayout &lay, char *ws, 
     const Totals *totals = reinterpret_cast<Totals *>(ws + lay.totals);
     const char *weight = static_cast<const char *>(a.weight) + v0 * a.w_ld * e;
     Side w = matrix(weight, a.w_ld, here, a.h, e);
-    if (copy_w) {
+    if (copy_w && (a.dhidden || a.n_rows > kFewMost)) {
         copy_rows(weight, a.w_ld, here, a.h, e, nullptr, nullptr, 0, ws + lay.w, lay.width, stream);
         w = matrix(ws + lay.w, lay.width, here, lay.width, e);
     }
     const int again = beside<DT>(a), twice = lay.d_rows > lay.n_pad;
     const int64_t rest = lay.n_pad * lay.piece * e;
     const Side x = matrix(ws + lay.x, lay.width, lay.n_pad, lay.width, e), d = matrix(ws + lay.d, lay.piece, lay.n_pad, lay.piece, e);
-    with_shape<DT, kGradLogits>(here, a.n_rows, [&](auto shape) {
+    const Row *meta = reinterpret_cast<const Row *>(ws + lay.meta);
+    if (a.n_rows <= kFewMost) {
+        const Side weights = matrix(weight, a.w_ld, here, a.h, e), few = matrix(ws + lay.x, lay.width, a.n_rows, lay.width, e);
+        const auto run = [&](auto kernel) {
+            kernel<<<thin_groups(a.n_rows, here), kThinThreads, 0, stream>>>(weights, few, (int)v0, meta, totals, kBeside / 2, ws + lay.d, lay.piece);
+        };
+        if (weights.bytes % kFewBytes == 0) run(head_dlogits_few<DT, true>);
+        else run(head_dlogits_few<DT, false>);
+    } else with_shape<DT, kGradLogits>(here, a.n_rows, [&](auto shape) {
         typedef decltype(shape) S;
         const int mt = (int)tiles_of(here, S::TM), nt = (int)tiles_of(a.n_rows, S::TN);
-        head_dlogits<DT, S><<<mt * nt, S::THREADS, 0, stream>>>(w, x, mt, nt, (int)v0, reinterpret_cast<const Row *>(ws + lay.meta), totals,
-                                                                again ? again : (int)lay.n_pad, again ? again : INT_MAX, ws + lay.d, lay.piece);
+        head_dlogits<DT, S><<<mt * nt, S::THREADS, 0, stream>>>(w, x, mt, nt, (int)v0, meta, totals, again ? again : (int)lay.n_pad, again ? again : INT_MAX, ws + lay.d, lay.piece);
     });
     if (a.dhidden)
         with_shape<DT, kGradHidden>(a.h, a.n_rows, [&](auto shape) {

@@ -28,3 +28,48 @@ def test_probabilities_stay_below_one(n, power, name):
     some = torch.zeros(v, dtype=torch.bool, device="cuda")
     some[ids.long()] = some[top] = True
     assert not bool(dw[~some].any())
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("h", [96, 100, 512, 1000])
+@pytest.mark.parametrize("n", [1, 7, 16, 17, 33, 64, 65, 130, 300])
+def test_the_logits_formed_again_are_the_forward_pass_own(n, h, name):
+    """With the statistics of the forward pass on the same operands the largest logit is M to the last bit, however they are summed: at
+    an inverse temperature of 2^60 its p is 1 and those of the others, units below it, 0."""
+    v, beta = 700, 2.0 ** 60
+    x, w, ids, _ = uh.operands(n, v, h, name, seed=5)
+    top = (x.double() @ w.double().T).argmax(1)
+    ids = torch.where(torch.arange(n, device="cuda") % 3 == 2, ids.long(), top).int()
+    b, g = torch.full((n,), beta, device="cuda"), torch.ones(n, device="cuda")
+    stats = tt.head_logprobs(v, x, w, ids, inv_temperature=b).stats
+    assert not bool(stats[:, 1].any())
+    dx, dw = tt.head_logprobs_backward(v, x, w, ids, stats, g, inv_temperature=b)
+    want = beta * (w.double()[ids.long()] - w.double()[top])
+    # one or two entries of dz, powers of two: a sum of two and its rounding
+    assert bool(((dx.double() - want).abs() <= (2 * uh.HALF_STEP[name] + 4 * uh.U) * beta * (w.double()[ids.long()].abs() + w.double()[top].abs())).all())
+    assert not bool(dx[ids == top].any())
+
+
+@pytest.mark.parametrize("n", [1, 7, 16, 17, 64, 100])
+def test_gradients_of_tokens_that_are_almost_certain(n):
+    """1 - p from 1e-2 down: its error is that of the other tokens' exponents, as in the forward pass, not a rounding of the token's own
+    logit over 1 - p."""
+    v, h = 640, 256
+    x, w, ids, beta = uh.operands(n, v, h, "f32", seed=2, lean=0.0)
+    x = 0.5 * x + 21.0 * w[ids.long()] / (w[ids.long()] ** 2).sum(1, keepdim=True)
+    g = torch.ones(n, device="cuda")
+    got = tt.head_logprobs(v, x, w, ids, inv_temperature=beta)
+    assert float(got.logprob.min()) > -1e-2
+    dx, _ = tt.head_logprobs_backward(v, x, w, ids, got.stats, g, inv_temperature=beta)
+    z, off = uh.logits(x, w, "f32")
+    y = z * beta.double()[:, None]
+    at = ids.long()[:, None]
+    rest = torch.logsumexp(y.scatter(1, at, -float("inf")), 1) - y.gather(1, at)[:, 0]  # ln of the others' sum over the token's term
+    total = torch.log1p(rest.exp())
+    d = -torch.exp(y - y.gather(1, at) - total[:, None])
+    d.scatter_(1, at, -torch.expm1(-total)[:, None])
+    d = d * beta.double()[:, None]
+    wd = w.double()
+    # an exponent is a difference of two logits, in the statistics and here; sums of 300 and 640 terms
+    rel = 4 * beta.double()[:, None] * off[:, None] + uh.U * (300 + 640 + 100)
+    assert bool(((dx.double() - d @ wd).abs() <= rel * (d.abs() @ wd.abs())).all())
