@@ -73,3 +73,35 @@ def test_gradients_of_tokens_that_are_almost_certain(n):
     # an exponent is a difference of two logits, in the statistics and here; sums of 300 and 640 terms
     rel = 4 * beta.double()[:, None] * off[:, None] + uh.U * (300 + 640 + 100)
     assert bool(((dx.double() - d @ wd).abs() <= rel * (d.abs() @ wd.abs())).all())
+
+
+@pytest.mark.parametrize("rows", [None, "64 bits", 1, 100])
+@pytest.mark.parametrize("n", [1, 7, 16, 17, 64, 100, 300])
+def test_statistics_of_another_product(n, rows):
+    """In 64 bits and rounded, or from calls of other numbers of rows: their M is not the largest logit's sum here to the last bit.  1 - p from 1e-2 down: its error is that of the other tokens' exponents, as in the forward pass, not a rounding of the token's own
+    logit over 1 - p."""
+    v, h = 640, 256
+    x, w, ids, beta = uh.operands(n, v, h, "f32", seed=2, lean=0.0)
+    x = 0.5 * x + 21.0 * w[ids.long()] / (w[ids.long()] ** 2).sum(1, keepdim=True)
+    g = torch.ones(n, device="cuda")
+    got = tt.head_logprobs(v, x, w, ids, inv_temperature=beta)
+    assert float(got.logprob.min()) > -1e-2
+    stats = got.stats
+    if rows == "64 bits":
+        stats = uh.forward(x, w, ids, beta)[0]["stats"].float()
+    elif rows:
+        stats = torch.cat([tt.head_logprobs(v, x[i:i + rows].repeat(max(1, rows // len(x)) + 1, 1)[:rows], w).stats[:len(x[i:i + rows])] for i in range(0, n, rows)])
+        stats[:, 1] = got.stats[:, 1]  # M does not depend on the temperatures
+    dx, _ = tt.head_logprobs_backward(v, x, w, ids, stats, g, inv_temperature=beta)
+    z, off = uh.logits(x, w, "f32")
+    y = z * beta.double()[:, None]
+    at = ids.long()[:, None]
+    rest = torch.logsumexp(y.scatter(1, at, -float("inf")), 1) - y.gather(1, at)[:, 0]  # ln of the others' sum over the token's term
+    total = torch.log1p(rest.exp())
+    d = -torch.exp(y - y.gather(1, at) - total[:, None])
+    d.scatter_(1, at, -torch.expm1(-total)[:, None])
+    d = d * beta.double()[:, None]
+    wd = w.double()
+    # an exponent is a difference of two logits, in the statistics and here; sums of 300 and 640 terms
+    rel = 4 * beta.double()[:, None] * off[:, None] + uh.U * (300 + 640 + 100)
+    assert bool(((dx.double() - d @ wd).abs() <= rel * (d.abs() @ wd.abs())).all())
