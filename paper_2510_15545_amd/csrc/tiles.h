@@ -72,6 +72,11 @@ struct Shape {
     static __device__ __forceinline__ int column_block(int wave, int j) { return wave % WN * FN + j; }
 };
 
+// 16 bytes at any global address that are read once (the non-temporal hint keeps such lines from displacing others).
+__device__ __forceinline__ u4 load_once(const char *p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const __attribute__((address_space(1))) u4b *>(reinterpret_cast<uintptr_t>(p)));
+}
+
 // The first n (below 16) bytes at q, one by one; zeros behind them.
 __device__ inline u4 load_some(const char *q, int n) {
     u4 v = {0, 0, 0, 0};
@@ -423,7 +428,7 @@ __device__ __forceinline__ void product_thin(const Side &w, const Side &x, char 
             u4 a[U], b[U];
             const auto load = [&](u4 (&f)[U], int s) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) f[u] = rows::load_global<true>(row + k0 + min(s + u, full - 1) * 64);
+                for (int u = 0; u < U; ++u) f[u] = load_once(row + k0 + min(s + u, full - 1) * 64);
             };
             const auto multiply = [&](const u4 &f, int s) {
 #pragma unroll
@@ -489,7 +494,7 @@ __device__ __forceinline__ void product_few(const Side &w, const Side &x, char *
         const int at = load_c * kFewBytes;
         if (WHOLE || at + kFewBytes <= w.bytes) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) to[h] = rows::load_global<true>(load_row + at + h * 64);
+            for (int h = 0; h < 2; ++h) to[h] = load_once(load_row + at + h * 64);
         } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
