@@ -6,9 +6,9 @@
 //
 // Forward: one product by tiles (tiles.h), whose epilogue leaves each tile's largest logit and sum of exponentials for
 // every row, and a second kernel that joins a row's parts.  Backward: the rows that carry a weight are gathered; then, for
-// one piece of the vocabulary after another, the product again with an epilogue that makes dz of it, rounded to the operands'
-// type twice, itself and what that takes off it (relative to the largest row weight; kBeside), and two more products: dx += dz W (in
-// fp32, over all pieces) and the piece's rows of dW, written once.  Of these three products' operands dz, W and x each is kept
+// one piece of the vocabulary after another, the product again, by the same sums, with an epilogue that makes dz of it, rounded to
+// the operands' type twice, itself and what that takes off it (relative to the largest row weight; kBeside), and two more products:
+// dx += dz W (in fp32, over all pieces) and the piece's rows of dW, written once.  Of these three products' operands dz, W and x each is kept
 // as it is, whichever of its indices is summed over (tiles.h).  No atomics: results do not depend on scheduling.
 #include <algorithm>
 
@@ -41,9 +41,9 @@ struct Row {
 };
 // In 16 bits what rounding takes off dz is kept beside it, so that dz has twice the type's digits and the gradients' error is that
 // of rounding the result once (1.00 times; without it 1.3 to 1.5).  Up to kBeside rows as rows of their own, this many or half
-// as many further on, beside the same hidden states again: the tiles have room (8 rows x 100,000 tokens x 320: 102 us, 95 without;
-// 64 x 32,000 x 1,024: 88, 76 without).  From there on as a second matrix behind the first, and both products go through both (66 x
-// 32,000 x 1,024: 102 us, 83 without; 391 x 50,257 x 1,024 fp16: 196 to 276; 2,048 x 128,256 x 2,048: 2.90 ms to 4.67).
+// as many further on, beside the same hidden states again: the tiles have room (64 x
+// 32,000 x 1,024: 88 us, 76 without).  From there on as a second matrix behind the first, and both products go through both (66 x
+// 32,000 x 1,024: 102 us, 83 without; 391 x 50,257 x 1,024 fp16 276, 198 without; 2,048 x 128,256 x 2,048 4.6 to 4.8 ms, 2.9 without).
 constexpr int kBeside = 64;
 
 struct Totals {

@@ -27,7 +27,8 @@ __device__ __forceinline__ float quotient(float x, float s, float r) {
 
 // Rows quantised by WAVES waves each, 4 / WAVES rows to a workgroup (of 256 threads, WAVES = 16: 1,024): 16 bytes a
 // lane and load.  NV > 0: the row stays in NV registers' worth of loads; 0: it is read again.  Bound by memory: 8,192 x 4,096
-// bf16, 101 MB, 18.4 us (5.5 TB/s).
+// bf16, 101 MB, 18.3 us (5.5 TB/s), fp32, 168 MB, 28.2 (6.0); 2,048 x 16,384 bf16, 101 MB, 18.4; 512 x 131,071 bf16, read twice, 67
+// (3.0 TB/s of the 201 MB that one reading would be).
 template <int DT, int WAVES, int NV>
 __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void quantize_rows(int n_rows, int k, const char *x, int64_t ld, int8_t *q, int64_t q_ld, float *scale) {
     constexpr int E = DT == TT_F32 ? 4 : 2, PER = 16 / E, ROWS = WAVES == 16 ? 1 : 4 / WAVES, LANES = WAVES * 64;

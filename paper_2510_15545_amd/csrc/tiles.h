@@ -285,8 +285,9 @@ struct Operand {
 // that on every SIMD one wave's reads lie beside the other's matrix instructions.  The second operand (hidden states, tokens: it
 // comes from the L2) is loaded a step ahead, the first one (the weights, from HBM) two: one was too short for it (8-bit 288 x
 // 128,256 x 2,048 132 us against 127, the gradient of 391 x 50,257 x 1,024 201 against 191).
-// 8,192^3 with plain stores: bf16 790 us, 1,390 TFLOP/s, 8 bits 420 us, 2,600 TOP/s; the matrix instructions take 61 to 65% of
-// the cycles, and the clock falls to 1.7 GHz under them: fewer cycles (a twenty-fifth less by even halves) gain little in bf16.
+// 8,192^3 with plain stores: bf16 790 us, 1,390 TFLOP/s, 8 bits 420 us, 2,600 TOP/s.  The matrix instructions take 63% of the cycles
+// of 4,096 x 151,936 x 2,048 bf16, 55% of 2,304 x 151,936 x 4,096 in 8 bits, and the clock falls to 1.8 GHz under them: fewer cycles
+// (a twenty-fifth less by even halves) gain little in bf16.
 // Blocks of 32 x 32 are slower (1,330 and 2,460).
 //
 // Half tiles: two workgroups to a compute unit, whose reads, matrix instructions, beginnings and ends lie beside each other as
@@ -392,8 +393,9 @@ static __device__ __forceinline__ void run(const Side &a, const Side &b, int m0,
 // ------------------------------------------------------------------------------------------------ few rows
 // Products with few rows of the second operand, bound by the reading of the first: it goes from memory to registers once, 16
 // rows to a wave, 8 loads of 16 bytes a lane ahead (4 where the columns' sums need the registers); the second operand waits in
-// LDS (all of it, or a chunk of k at a time).  Any alignment, any width.  17 to 64 rows: 128,256 x 2,048 bf16 124 us (4.2
-// TB/s), 8 bits 57 to 76.
+// LDS (all of it, or a chunk of k at a time).  Any alignment, any width.  128,256 x 2,048 bf16, 17 / 32 / 48 / 64 rows: 130 / 122
+// / 130 / 130 us (4.0 to 4.3 TB/s), by tiles 131 / 127 / 121 / 128; 8 bits, 17 / 32 / 64: 59 / 64 / 80, by tiles 66 / 65 / 66; fp32, 64
+// x 128,256 x 1,024: 192, by tiles 156.  So tiles would gain at 48 to 64 rows and with fp32; few tokens gain here (64 x 32,000 x 512: 20, 21).
 constexpr int kThinThreads = 512, kThinRows = kThinThreads / 64 * 16;  // rows of the first operand that a workgroup takes at a time
 constexpr int kThinLds = 65536;                                      // two workgroups to a compute unit
 constexpr int kThinGroups = 512;                                     // workgroups at most: as many as run at once
@@ -472,7 +474,9 @@ __device__ __forceinline__ void product_thin(const Side &w, const Side &x, char 
 // row each, so that 1 KB of a row is read at a time (the same bytes 16 rows by 64 bytes a wave come at 5.2 TB/s, these at 5.9 to
 // 6.1, read in order at 6.8).  Loads roll through four such KBs: what has been multiplied makes room for the one four further on,
 // in this row or the next.  The waves' sums are joined in LDS; then thread t (of 256) has row t % 16 and column t / 16.  8 x
-// 151,936 x 2,048 bf16 (622 MB) 108 us, 5.8 TB/s.
+// 151,936 x 2,048 bf16 (622 MB) 108 us, 5.8 TB/s.  128,256 x 2,048, 4 / 8 / 12 / 16 rows: 98 us each, product_thin 108 to 110; fp32, 16 x
+// 1,024: 101, 117; 8 bits, 4 / 16 rows: 55 / 61, 55 / 58.  Rows that do not fit LDS as a whole are staged again for every 16 tokens: 8 x
+// 4,096 bf16 (64 KB) 182, product_thin 203, but 9 and 16 x 4,096 241 and 256, product_thin 210 and 216.
 constexpr int kFewMost = 16, kFewRows = 16, kFewBytes = 1024;
 
 // finish(m, n, y): one result.  WHOLE: rows of whole KBs, loaded without a branch (past the last row the last one again).
@@ -574,9 +578,12 @@ __host__ __device__ inline int64_t padded_rows(int64_t n) {
 
 // f(shape) for the tiles of a product of m rows of the first operand with n of the second.
 // As few tiles as 256 columns give, no wider than they need (333 rows: 2 x 192): every tile of columns is a reading of the
-// first operand.  Half tiles up to 128 rows, and where their smaller ones leave less undone: the gradient's logits of
-// few rows (how many carry a weight is not known here), its short sums over few rows, and fp32, which the matrix cores bound.
-// The smallest where even 128 x 128 would not fill the compute units (500 rows of 600 x 4,096 fp32: 152 us, not 272; bf16 34, not 84).
+// first operand.  Half tiles up to 128 rows (forward, 128,256 x 1,024 bf16: 72 rows 65 us, wide 87; 128: 66, 81; 144: wide 69, half 95;
+// 256: 79, 97), and where their smaller ones leave less undone: the gradient's logits of up to 512 rows (how many carry a weight is not
+// known here) and its short sums over them (256 x 50,257 x 1,024: 205 us, wide for both 219; 512: 329, 359; 576: wide 382, half for
+// all 412; 1,024: 650, 660), and fp32, which the matrix cores bound.  The smallest where even 128 x 128 would not fill the compute
+// units (500 rows of 600 x 4,096 fp32: 152 us, not 272; bf16 34, not 84; 300 x 8,000 x 1,024 bf16 20, not 30; 300 x 11,000 x 1,024,
+// 258 tiles, 29, which smaller ones would do in 22; 70 x 64,000: 30, smaller ones 35).
 enum Use { kForward, kGradLogits, kGradHidden, kGradWeight };
 template <int DT, Use U, typename F>
 void with_shape(int64_t m, int64_t n, F f) {
