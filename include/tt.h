@@ -642,7 +642,8 @@ int tt_head_logprobs(int32_t n_rows, int32_t v, int32_t h, int32_t dtype, const 
  * multiplied.  In fp16 it is off by up to 2^-39 of that largest weight: an entry beta g p_j below 2^-28 of it has fewer than fp16's
  * digits, below 2^-39 none.  The logits are those of tt_head_logprobs to the last bit where both calls have up to 16 rows, or
  * both more; otherwise lp_j carries beta times the roundings that they differ by, none is taken above 0, and the logit of a token id
- * within 2^-22 sqrt(h) |M| of M is taken as M.  Sums are fp32, without atomics.  With n_rows = 0 dweight is zeros.
+ * that can only be M's (L below 0.34, beta (M - x) below 0.17) is taken as M.  Sums are fp32, without atomics.  With n_rows = 0 dweight
+ * is zeros.
  * workspace: tt_head_logprobs_backward_workspace_size bytes serve every call of up to n_rows rows, a call uses
  * ..._workspace_used bytes.  Errors and workspaces as for tt_head_logprobs, and TT_EINVAL for gradients that meet something.
  */

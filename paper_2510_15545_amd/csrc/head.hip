@@ -254,25 +254,23 @@ __global__ __launch_bounds__(1024) void head_select(int n, int v, const float *i
 // formed here, which a large inverse temperature would make an infinity.  (A minimum that is NaN beside a NaN: one instruction.)
 __device__ __forceinline__ float exponent_of(const Row &r, float z) { return __builtin_elementwise_minimum(fmaf(z - r.m, r.c, -r.l), 0.0f); }
 
-// dz of a token.  At the row's own 1 - p is not a difference, and a logit within `near` of M, relative, is M: where it differs by a
-// rounding (statistics of another product, of more or fewer rows), 1 - p of a token that is almost certain would be that rounding
-// over 1 - p off.  Where M is another token's that lies so near, neither is certain, and p is off by no more than a rounding's worth.
-__device__ __forceinline__ float dlogit_of(const Row &r, float z, int token, float near) {
+// dz of a token.  At the row's own 1 - p is not a difference, and where p is above 2^-0.5 at M and the logit within 2^-0.25 of it, it
+// is M's and taken as M (a second token as near would have made the sum 1.8, and p at M 2^-0.88): where the two differ by a rounding
+// (statistics of another product, of more or fewer rows), 1 - p of a token that is almost certain would be that rounding over 1 - p off.
+__device__ __forceinline__ float dlogit_of(const Row &r, float z, int token) {
     float y = (r.w - r.g) * __builtin_amdgcn_exp2f(exponent_of(r, z));
     if (token == r.id) {
-        const float e = exponent_of(r, fabsf(z - r.m) <= near * fabsf(r.m) ? r.m : z);
+        const float e = exponent_of(r, r.l < 0.5f && fabsf(z - r.m) * r.c < 0.25f ? r.m : z);
         y = r.g * -expm1f(e * (float)rows::kLn2) + r.w * __builtin_amdgcn_exp2f(e);
     }
     return y;
 }
-// How far two sums of h products may be apart: a random walk of their roundings, four times its step.
-inline float near_of(int h) { return 4.0f * sqrtf((float)h) * 0x1p-24f; }
 
 // dz of a piece's tokens (the first of them v0) for the listed rows, stored as [row][token] up to row n_end; in 16 bits the
 // remainders `rest` rows further on.
 template <int DT, typename S>
 __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, int mt, int nt, int v0, const Row *meta, const Totals *totals, int rest, int n_end, char *d,
-                                                              int64_t d_ld, float near) {
+                                                              int64_t d_ld) {
     TT_TILE_LDS(S);
     using T = typename rows::Elem<DT>::T;
     f4 acc[S::FM][S::FN];
@@ -304,7 +302,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
         store([&](int, int j, int m, int i, float (&y)[4]) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                y[q] = m + q < w.rows ? dlogit_of(r[j], acc[i][j][q], v0 + m + q, near) : 0.0f;
+                y[q] = m + q < w.rows ? dlogit_of(r[j], acc[i][j][q], v0 + m + q) : 0.0f;
             }
         });
     } else {
@@ -320,7 +318,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void head_dlogits(Side w, Side x, in
 // holds here, too (1 - p of 1e-4 would be off by a rounding of its logit over 1e-4, a few percent).  d: `again` rows of which the
 // first x.rows are listed ones or pad the list, in 16 bits the remainders' as many; all of whole steps of tokens, zeros elsewhere.
 template <int DT, bool WHOLE>
-__global__ __launch_bounds__(kThinThreads, 4) void head_dlogits_few(Side w, Side x, int v0, const Row *meta, const Totals *totals, int again, char *d, int64_t d_ld, float near) {
+__global__ __launch_bounds__(kThinThreads, 4) void head_dlogits_few(Side w, Side x, int v0, const Row *meta, const Totals *totals, int again, char *d, int64_t d_ld) {
     __shared__ __attribute__((aligned(16))) char lds[kThinLds];
     __shared__ float sums[8][256];
     if (totals->rows == 0) return;
@@ -331,7 +329,7 @@ __global__ __launch_bounds__(kThinThreads, 4) void head_dlogits_few(Side w, Side
     T *row = reinterpret_cast<T *>(d) + n * d_ld;
     product_few<DT, WHOLE>(w, x, lds, sums, [&](int m, int, float z) {
         if (!there || m >= w.rows) return;
-        const float y = dlogit_of(r, z, v0 + m, near);
+        const float y = dlogit_of(r, z, v0 + m);
         const uint32_t bits = rows::encode<DT>(y);
         row[m] = (T)bits;
         if constexpr (DT != TT_F32) {
@@ -562,7 +560,7 @@ void backward_piece(const HeadGradArgs &a, const BackwardLayout &lay, char *ws, 
     if (a.n_rows <= kFewMost) {
         const Side weights = matrix(weight, a.w_ld, here, a.h, e), few = matrix(ws + lay.x, lay.width, a.n_rows, lay.width, e);
         const auto run = [&](auto kernel) {
-            kernel<<<thin_groups(a.n_rows, here), kThinThreads, 0, stream>>>(weights, few, (int)v0, meta, totals, kBeside / 2, ws + lay.d, lay.piece, near_of(a.h));
+            kernel<<<thin_groups(a.n_rows, here), kThinThreads, 0, stream>>>(weights, few, (int)v0, meta, totals, kBeside / 2, ws + lay.d, lay.piece);
         };
         if (weights.bytes % kFewBytes == 0) run(head_dlogits_few<DT, true>);
         else run(head_dlogits_few<DT, false>);
@@ -570,7 +568,7 @@ void backward_piece(const HeadGradArgs &a, const BackwardLayout &lay, char *ws, 
         typedef decltype(shape) S;
         const int mt = (int)tiles_of(here, S::TM), nt = (int)tiles_of(a.n_rows, S::TN);
         head_dlogits<DT, S><<<mt * nt, S::THREADS, 0, stream>>>(w, x, mt, nt, (int)v0, meta, totals, again ? again : (int)lay.n_pad, again ? again : INT_MAX,
-                                                               ws + lay.d, lay.piece, near_of(a.h));
+                                                               ws + lay.d, lay.piece);
     });
     if (a.dhidden)
         with_shape<DT, kGradHidden>(a.h, a.n_rows, [&](auto shape) {

@@ -105,3 +105,27 @@ def test_statistics_of_another_product(n, rows):
     # an exponent is a difference of two logits, in the statistics and here; sums of 300 and 640 terms
     rel = 4 * beta.double()[:, None] * off[:, None] + uh.U * (300 + 640 + 100)
     assert bool(((dx.double() - d @ wd).abs() <= rel * (d.abs() @ wd.abs())).all())
+
+
+@pytest.mark.parametrize("n", [1, 8, 20, 64, 70, 300])
+@pytest.mark.parametrize("gap,beta", [(2.0 ** -16, 1.0), (2.0 ** -16, 2.0 ** 12), (2.0 ** -16, 2.0 ** 18), (2.0 ** -16, 2.0 ** 20), (2.0 ** -19, 2.0 ** 24), (2.0 ** -4, 1.0), (0.25, 1.0)])
+@pytest.mark.parametrize("own", [0, 1])
+def test_two_tokens_side_by_side(own, gap, beta, n):
+    """The largest logit and one a gap below it, without rounding errors: each keeps its own probability, near ties and at any
+    temperature, whichever of them is the row's token."""
+    v, h, a, t = 500, 64, 130, 7
+    values = torch.full((v,), -200.0, dtype=torch.float64)
+    values[a], values[t] = 16.0, 16.0 - gap
+    w, x = torch.zeros((v, h), device="cuda"), torch.zeros((n, h), device="cuda")
+    w[:, 3], x[:, 3] = values.float().cuda(), 1.0
+    ids = torch.full((n,), (a, t)[own], dtype=torch.int32, device="cuda")
+    b, g = torch.full((n,), beta, device="cuda"), torch.ones(n, device="cuda")
+    stats = tt.head_logprobs(v, x, w, ids, inv_temperature=b).stats
+    _, dw = tt.head_logprobs_backward(v, x, w, ids, stats, g, inv_temperature=b)
+    q = torch.sigmoid(torch.tensor(-gap * beta, dtype=torch.float64))  # of the lower one, both ways as sigmoids
+    d = torch.stack((q, -q) if own == 0 else (-torch.sigmoid(torch.tensor(gap * beta, dtype=torch.float64)), torch.sigmoid(torch.tensor(gap * beta, dtype=torch.float64)))) * beta * n
+    got = dw[[a, t], 3].double().cpu()
+    # exponents of up to 46 (base 2), three roundings each, in the statistics and here; 1 - p by the difference of an exponent and L, each
+    # up to 1 where p is not small; n equal terms
+    off = uh.U * (6 * 46 * 0.7 + 64 + n)
+    assert bool(((got - d).abs() <= off * d.abs() + 2.0 ** -100 * beta).all()), (got, d)
