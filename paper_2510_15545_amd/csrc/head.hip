@@ -43,7 +43,7 @@ struct Row {
 // of rounding the result once (1.00 times; without it 1.3 to 1.5).  Up to kBeside rows as rows of their own, this many or half
 // as many further on, beside the same hidden states again: the tiles have room (64 x
 // 32,000 x 1,024: 88 us, 76 without).  From there on as a second matrix behind the first, and both products go through both (66 x
-// 32,000 x 1,024: 102 us, 83 without; 391 x 50,257 x 1,024 fp16 276, 198 without; 2,048 x 128,256 x 2,048 4.6 to 4.8 ms, 2.9 without).
+// 32,000 x 1,024: 102 us, 83 without; 391 x 50,257 x 1,024 fp16 276, 198 without; 2,048 x 128,256 x 2,048 4.55 to 4.8 ms, 2.9 without).
 constexpr int kBeside = 64;
 
 struct Totals {
